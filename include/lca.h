@@ -291,6 +291,104 @@ int lca_decode_step_update_ring(const lca_params* p, const void* q_sem, const vo
                                 int32_t* n_rep, const int32_t* n_tok, int32_t* anchor_out, void* ws,
                                 size_t ws_bytes, void* stream);
 
+/* ---- Paged 8-bit cache ----------------------------------------------------------------------
+ * The decode cache of many sequences in one pool of pages, each row element held in 8 bits (e4m3) with one
+ * fp32 scale for each (page, KV head): value = code * scale.
+ *
+ * Rows are addressed by position, so nothing moves when a group is condensed: token number n of a sequence is
+ * row n; representative j is row j, which belonged to a token condensed long before (n_rep <= n_rep * group_size).
+ * Of the row space of a sequence with n_rep representatives and n_tok tokens the rows
+ *     [0, n_rep)   and   [n_rep * group_size, n_tok)
+ * are present; lca_condense's [representatives ; tokens] order is exactly this order without the gap.  A cache that
+ * is never condensed is the case n_rep = NULL (no representatives, rows [0, n_tok)).
+ * Row x is on page block_table[b][x / page_size], at place x % page_size.  An entry outside [0, n_pages) (for
+ * instance -1) is no page: its rows take no part.  With n_rep, group_size must be a multiple of page_size, so that
+ * tokens and representatives never share a page. */
+typedef struct lca_paged8 {
+  void* pages_sem;        /* [n_pages, n_kv_heads, page_size, d_sem] e4m3 codes: latents (GQA: V) */
+  void* pages_pos;        /* [n_pages, n_kv_heads, page_size, d_pos] e4m3 codes: rope keys (GQA: K) */
+  float* scale_sem;       /* [n_pages, n_kv_heads]: scale of pages_sem (MLA: of both, the logit is one sum) */
+  float* scale_pos;       /* [n_pages, n_kv_heads]: GQA scale of pages_pos; MLA: NULL */
+  int32_t* block_table;   /* [batch, table_width] */
+  int32_t n_pages;        /* pages of the pool; n_pages * page_size < 2^31 */
+  int32_t page_size;      /* 16, 32, 64 or 128 rows */
+  int32_t table_width;    /* entries per sequence; table_width * page_size < 2^31.  Rows behind the table are absent */
+} lca_paged8;             /* a HOST structure of device pointers; pages 16-byte aligned */
+
+/* Block tables, free list and slot maps on the GPU, from the lengths of the requests.  The caller states how many
+ * representatives and tokens every sequence is to hold; the call compares that with what it holds, gives back the
+ * pages that no present row needs any more, takes pages for new rows from the free list and names the slot of every
+ * new row.  Growth, condensation (n_rep grows), rollback of rejected tokens (n_tok shrinks) and the end of a request
+ * (n_rep = n_tok = 0) are the same call.
+ *   n_rep (or NULL: 0), n_tok [batch] int32: target state.  A target must satisfy n_rep * group_size <= n_tok and
+ *       fit the table; n_rep does not shrink except to 0 together with n_tok
+ *   held_rep (NULL with n_rep), held_tok [batch] int32, in / out: what the tables cover now (0 at first)
+ *   cache->block_table in / out: entries that no present row needs become -1; only block_table, n_pages, page_size and
+ *       table_width of `cache` are used
+ *   free_pages [n_pages] int32, n_free [1] int32, in / out: stack of free pages.  Pages given back are pushed in
+ *       descending (sequence, entry) order, pages taken are popped in ascending order: taking and giving back the same
+ *       pages leaves the stack as it was
+ *   slot_map [n_rows] int32 out (NULL: not wanted): slot = page * page_size + place of every new row: of each sequence
+ *       the representatives [held_rep, n_rep), then the tokens [max(held_tok, n_rep * group_size), n_tok).
+ *       rows_per_seq = 0: packed, sequence after sequence; rows_per_seq = s > 0: sequence b starts at b * s.
+ *       Entries of no row are -1
+ *   row_offsets [batch + 1] int32 out: first new row of each sequence in the packed order (may be NULL when no packed
+ *       slot_map is wanted)
+ *   status [1] int32 out: 0; k > 0: k pages are missing; -1: a target (or the held state) is not valid; -2: slot_map
+ *       is too small.  Unless it is 0 nothing has changed, and all slots are -1
+ * Uses batch and group_size of p.  Needs no workspace. */
+int lca_page_update(const lca_params* p, const lca_paged8* cache, const int32_t* n_rep, const int32_t* n_tok,
+                    int32_t* held_rep, int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map,
+                    int32_t n_rows, int32_t rows_per_seq, int32_t* row_offsets, int32_t* status, void* stream);
+
+/* Writes rows into the paged cache.
+ *   rows_sem [n_rows, n_kv_heads, d_sem], rows_pos [n_rows, n_kv_heads, d_pos] bf16
+ *   slot_map [n_rows] int32: slot of every row; a negative one (or one behind the pool) is skipped
+ * Rows are appended: the rows of one page come together, in the order of their places, and a page is first written at
+ * place 0, which sets its scale anew (so a page needs no clearing between owners).  Two rows with the same slot, or two
+ * separate runs of rows for one page, in one call leave that page undefined.
+ * Scale of a block (page, KV head): the smallest power of two with max|x| <= 448 * scale over its finite elements (MLA:
+ * over latent and rope key together), at least 2^-100.  A later row with a larger element raises the scale; the rows
+ * the block holds already are then rounded again, which is exact except where a code falls below the normal range.
+ * Codes are rounded to nearest even; infinities become +-448 * scale, NaN stays NaN.
+ * Of `cache` the pages, scales, n_pages and page_size are used, of p variant, n_kv_heads, d_sem and d_pos. */
+int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* rows_sem, const void* rows_pos,
+                     const int32_t* slot_map, int64_t n_rows, void* stream);
+
+/* Decode attention over the paged cache (Sec. 4.3): q_len new tokens per sequence attend to the present rows.
+ *   q_sem [B, q_len, H, d_sem] (NULL for GQA), q_pos [B, q_len, H, d_pos] bf16
+ *   n_rep (or NULL), n_tok [B] int32 (device): state of each sequence, the rows of the q_len tokens included; values
+ *       outside the table are clamped to it
+ *   out [B, q_len, H, d_sem] bf16, lse_opt [B, q_len, H] fp32 or NULL
+ * The q_len tokens are the last ones of their sequence: query i sees the present rows below n_tok - q_len + 1 + i.
+ * Representatives get rep_logit_bias.  A query that sees no row (an empty sequence, fewer tokens than q_len) gives
+ * out = 0 and lse = -inf.  What absent rows and unused pages hold does not matter; a NaN in a present row reaches every
+ * query of that sequence and KV head.
+ * Products on the tensor cores with queries and softmax weights as sums of two 8-bit terms: a query element is exact to
+ * 2^-17 of the largest of its row, a weight to 2^-8 of itself or 2^-18 of the largest weight; fp32 softmax and sums,
+ * one rounding to bf16.  Results do not depend on anything but the arguments (no atomics).
+ * ws / ws_bytes: lca_paged8_workspace_bytes. */
+size_t lca_paged8_workspace_bytes(const lca_params* p, const lca_paged8* cache, int32_t q_len);
+int lca_decode_attention_paged8(const lca_params* p, const lca_paged8* cache, const void* q_sem, const void* q_pos,
+                                int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* Online update (Sec. 4.3) over the paged cache: every sequence with at least window + group_size uncondensed tokens
+ * (n_tok - n_rep * group_size) has its earliest group condensed, with the arithmetic of lca_decode_update on the values
+ * the cache stands for.  The call reads the cache and returns the representative; nothing is written to the pages:
+ * pass n_rep_new to lca_page_update (it gives back the group's pages and names the slot of the representative) and the
+ * rows to lca_paged8_write.
+ *   q_tail_sem / q_tail_pos / q_tail_batch_stride / qbar_opt: summary query, as for lca_decode_update
+ *   n_rep, n_tok [B] int32; n_rep_new [B] int32 out (another array): n_rep + 1 where a group was condensed, else n_rep
+ *   rep_sem [B, n_kv_heads, d_sem], rep_pos [B, n_kv_heads, d_pos] bf16 out: rows of sequences that are not due are
+ *       left as they are
+ *   anchor_out [B, n_kv_heads] int32: offset 0..g-1 of the anchor token, -1 where nothing was condensed
+ * A sequence whose group is not wholly on pages is left alone.  ws: LCA_WS_UPDATE. */
+int lca_decode_update_paged8(const lca_params* p, const lca_paged8* cache, const void* q_tail_sem,
+                             const void* q_tail_pos, int64_t q_tail_batch_stride, const float* qbar_opt,
+                             const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
+                             void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Value up-projection of the latent attention output (Alg. 1: v = c W^UV; Sec. 4.3: in the absorbed
  * form the attention result lives in the latent space and W^UV is applied to it once per query and
  * head):   out_v[t, h, :] = attn_latent[t, h, :] . W^UV[h]

@@ -38,6 +38,13 @@ class LcaParams(C.Structure):
                 ("rep_logit_bias", C.c_float), ("sem_reducer", C.c_int32), ("pos_reducer", C.c_int32)]
 
 
+class LcaPaged8(C.Structure):
+    """Mirror of ``lca_paged8``: device pointers of a paged 8-bit cache.  Build it with ``paged8_cache``, which also keeps
+    the tensors alive."""
+    _fields_ = [("pages_sem", C.c_void_p), ("pages_pos", C.c_void_p), ("scale_sem", C.c_void_p), ("scale_pos", C.c_void_p),
+                ("block_table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table_width", C.c_int32)]
+
+
 class LcaError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -87,6 +94,17 @@ def _load() -> C.CDLL:
     lib.lca_condense_varlen.argtypes = [P, pi32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lca_prefill_attention_varlen.restype = C.c_int
     lib.lca_prefill_attention_varlen.argtypes = [P, pi32, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    PC = C.POINTER(LcaPaged8)
+    lib.lca_page_update.restype = C.c_int
+    lib.lca_page_update.argtypes = [P, PC, vp, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, vp]
+    lib.lca_paged8_write.restype = C.c_int
+    lib.lca_paged8_write.argtypes = [P, PC, vp, vp, vp, i64, vp]
+    lib.lca_paged8_workspace_bytes.restype = sz
+    lib.lca_paged8_workspace_bytes.argtypes = [P, PC, i32]
+    lib.lca_decode_attention_paged8.restype = C.c_int
+    lib.lca_decode_attention_paged8.argtypes = [P, PC, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.lca_decode_update_paged8.restype = C.c_int
+    lib.lca_decode_update_paged8.argtypes = [P, PC, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.lca_latent_to_value.restype = C.c_int
     lib.lca_latent_to_value.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp]
     lib.lca_selftest_bounded_wait.restype = C.c_int
@@ -255,6 +273,36 @@ def lca_prefill_attention_varlen(params, seq_lens, q_sem, q_pos, kv_sem, kv_pos,
     return int(_lib.lca_prefill_attention_varlen(C.byref(params), _lens(seq_lens), _ptr(q_sem), _ptr(q_pos), _ptr(kv_sem),
                                                  _ptr(kv_pos), _ptr(cache_sem), _ptr(cache_pos), _ptr(out), _ptr(lse_opt),
                                                  _ptr(ws), wsb, _stream(stream)))
+
+
+def lca_page_update(params, cache, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, n_rows, rows_per_seq,
+                    row_offsets, status, stream=None) -> int:
+    return int(_lib.lca_page_update(C.byref(params), C.byref(cache), _ptr(n_rep), _ptr(n_tok), _ptr(held_rep), _ptr(held_tok),
+                                    _ptr(free_pages), _ptr(n_free), _ptr(slot_map), int(n_rows), int(rows_per_seq),
+                                    _ptr(row_offsets), _ptr(status), _stream(stream)))
+
+
+def lca_paged8_write(params, cache, rows_sem, rows_pos, slot_map, n_rows, stream=None) -> int:
+    return int(_lib.lca_paged8_write(C.byref(params), C.byref(cache), _ptr(rows_sem), _ptr(rows_pos), _ptr(slot_map), int(n_rows),
+                                     _stream(stream)))
+
+
+def lca_paged8_workspace_bytes(params, cache, q_len: int) -> int:
+    return int(_lib.lca_paged8_workspace_bytes(C.byref(params), C.byref(cache), int(q_len)))
+
+
+def lca_decode_attention_paged8(params, cache, q_sem, q_pos, q_len, n_rep, n_tok, out, lse_opt, ws, ws_bytes=None, stream=None) -> int:
+    wsb = _nbytes(ws) if ws_bytes is None else int(ws_bytes)
+    return int(_lib.lca_decode_attention_paged8(C.byref(params), C.byref(cache), _ptr(q_sem), _ptr(q_pos), int(q_len), _ptr(n_rep),
+                                                _ptr(n_tok), _ptr(out), _ptr(lse_opt), _ptr(ws), wsb, _stream(stream)))
+
+
+def lca_decode_update_paged8(params, cache, q_tail_sem, q_tail_pos, q_tail_batch_stride, qbar_opt, n_rep, n_tok, n_rep_new, rep_sem,
+                             rep_pos, anchor_out, ws, ws_bytes=None, stream=None) -> int:
+    wsb = _nbytes(ws) if ws_bytes is None else int(ws_bytes)
+    return int(_lib.lca_decode_update_paged8(C.byref(params), C.byref(cache), _ptr(q_tail_sem), _ptr(q_tail_pos),
+                                             int(q_tail_batch_stride), _ptr(qbar_opt), _ptr(n_rep), _ptr(n_tok), _ptr(n_rep_new),
+                                             _ptr(rep_sem), _ptr(rep_pos), _ptr(anchor_out), _ptr(ws), wsb, _stream(stream)))
 
 
 def lca_latent_to_value(attn_latent, w_uv, out_v, n_tokens, n_heads, d_latent, d_v, stream=None) -> int:
@@ -468,3 +516,83 @@ def decode_step_update_ring(params: LcaParams, q_sem, q_pos, qsum, qcount, ring_
                                      anchor, ws, stream=stream)
     _check(st, "lca_decode_step_update_ring")
     return anchor
+
+
+def paged8_cache(pages_sem, pages_pos, scale_sem, scale_pos, block_table, page_size: Optional[int] = None,
+                 n_pages: Optional[int] = None) -> LcaPaged8:
+    """Descriptor of a paged 8-bit cache over the caller's tensors (any of them may be None for calls that do not use it):
+    pages [n_pages, Hkv, page_size, d] of one byte per element (uint8 or float8_e4m3fn), scales [n_pages, Hkv] float32,
+    block_table [batch, table_width] int32."""
+    if pages_sem is not None:
+        n_pages, page_size = pages_sem.shape[0], pages_sem.shape[2]
+    for t, want in ((pages_sem, 1), (pages_pos, 1), (scale_sem, 4), (scale_pos, 4), (block_table, 4)):
+        if t is not None and t.element_size() != want:
+            raise ValueError("pages hold one byte per element, scales are float32, block tables int32")
+    c = LcaPaged8(_ptr(pages_sem), _ptr(pages_pos), _ptr(scale_sem), _ptr(scale_pos), _ptr(block_table), int(n_pages or 0),
+                  int(page_size or 0), 0 if block_table is None else block_table.shape[1])
+    c.tensors = (pages_sem, pages_pos, scale_sem, scale_pos, block_table)
+    return c
+
+
+def new_paged8_cache(params: LcaParams, n_pages: int, page_size: int, table_width: int, device) -> LcaPaged8:
+    """Allocate a pool of pages, its scales and empty block tables for params.batch sequences."""
+    Hkv = params.n_kv_heads
+    scale = torch.ones((n_pages, Hkv), dtype=torch.float32, device=device)
+    return paged8_cache(torch.zeros((n_pages, Hkv, page_size, params.d_sem), dtype=torch.uint8, device=device),
+                        torch.zeros((n_pages, Hkv, page_size, params.d_pos), dtype=torch.uint8, device=device), scale,
+                        torch.ones_like(scale) if params.variant == LCA_VARIANT_GQA else None,
+                        torch.full((params.batch, table_width), -1, dtype=torch.int32, device=device))
+
+
+def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, row_offsets,
+                status, rows_per_seq: int = 0, stream=None):
+    """Run lca_page_update in place on the tables, the free list and the held state; returns slot_map.  `status` is a device
+    tensor: read it where the caller has to know (0: done)."""
+    n_rows = 0 if slot_map is None else slot_map.numel()
+    _check(lca_page_update(params, cache, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, n_rows, rows_per_seq,
+                           row_offsets, status, stream=stream), "lca_page_update")
+    return slot_map
+
+
+def paged8_write(params: LcaParams, cache: LcaPaged8, rows_sem, rows_pos, slot_map, stream=None):
+    """Quantise rows into the pages that slot_map names (in place)."""
+    _check(lca_paged8_write(params, cache, rows_sem, rows_pos, slot_map, slot_map.numel(), stream=stream), "lca_paged8_write")
+
+
+def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) -> torch.Tensor:
+    return torch.empty(max(lca_paged8_workspace_bytes(params, cache, q_len), 16), dtype=torch.uint8, device=device)
+
+
+def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
+                            want_lse: bool = False, ws=None, stream=None):
+    """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
+    B, q_len, H = q_pos.shape[:3]
+    if out is None:
+        out = torch.empty((B, q_len, H, params.d_sem), dtype=torch.bfloat16, device=q_pos.device)
+    if lse is None and want_lse:
+        lse = torch.empty((B, q_len, H), dtype=torch.float32, device=q_pos.device)
+    if ws is None:
+        ws = workspace_paged8(params, cache, q_len, q_pos.device)
+    _check(lca_decode_attention_paged8(params, cache, q_sem, q_pos, q_len, n_rep, n_tok, out, lse, ws, stream=stream),
+           "lca_decode_attention_paged8")
+    return out, lse
+
+
+def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
+                         rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
+    """Run lca_decode_update_paged8; returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
+    dev, B, Hkv = n_tok.device, params.batch, params.n_kv_heads
+    if n_rep_new is None:
+        n_rep_new = torch.empty_like(n_rep)
+    if rep_sem is None:
+        rep_sem = torch.zeros((B, Hkv, params.d_sem), dtype=torch.bfloat16, device=dev)
+    if rep_pos is None:
+        rep_pos = torch.zeros((B, Hkv, params.d_pos), dtype=torch.bfloat16, device=dev)
+    if anchor is None:
+        anchor = torch.empty((B, Hkv), dtype=torch.int32, device=dev)
+    if ws is None:
+        ws = workspace(params, LCA_WS_UPDATE, dev)
+    n = params.n_summary_q if params.n_summary_q > 0 else params.group_size
+    _check(lca_decode_update_paged8(params, cache, q_tail_sem, q_tail_pos, n, qbar, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, anchor,
+                                    ws, stream=stream), "lca_decode_update_paged8")
+    return n_rep_new, rep_sem, rep_pos, anchor

@@ -23,6 +23,8 @@ SOURCES = {
     "attn_tc2.cu": ["--use_fast_math"],
     "attn_gqa2.cu": ["--use_fast_math"],
     "gemm_uv.cu": ["--use_fast_math"],
+    "paged8.cu": [],              # scales, codes and anchors are compared exactly
+    "attn_paged8.cu": [],         # names its approximate instructions itself
 }
 
 

@@ -1,0 +1,842 @@
+// Decode attention over the paged 8-bit cache (Sec. 4.3 over the layout of lca_paged8).
+//
+// Mathematics.  For a query row h and the present rows i of its sequence and KV head
+//     y_i = log2(e) (scale * s_k(i) * sum_c q_c k_ic + bias_i),   out = sum_i 2^y_i s_v(i) v_i / sum_i 2^y_i
+// with e4m3 codes k, v and one scale for each page and KV head.  Everything is multiplied as 8-bit numbers:
+//   * q f = q_hi + q_lo, two e4m3 terms, f the power of two that brings the row's largest element into [128, 256).
+//     Four significant bits each: exact for every element above 2^-9 of the largest, otherwise off by 2^-17 of the largest.
+//   * t_i = 2^(y_i + log2 s_v(i) - M + 8) = t_hi + t_lo, t_hi e5m2 (the wide range), t_lo e4m3: relative error 2^-8 (a bf16
+//     weight has 2^-9 at best, 2^-8 at worst), and never more than 2^-10, i.e. 2^-18 of the largest weight.  That floor
+//     would round a long flat tail all the same way, so every key adds its own offset, one of 32 spread over the last
+//     place of t_lo, before the rounding: over a tile the tail keeps its weight to 1/64 of that place.
+//   M is the running maximum of y + log2 s_v over a split; it is raised only when a weight exceeds it by 2^3.  The row
+//   sum adds the weights without s_v in fp32, unrounded.
+#include <cstring>
+
+#include "fp8_common.cuh"
+#include "lca_common.cuh"
+#include "tc_common.cuh"
+
+namespace lca {
+using namespace tc;
+
+static __device__ int g_paged8_status = 0;
+
+// --------------------------------------------------------------------------------------------------- scalar kernel
+// One warp per query row, keys one by one, fp32: the cross-check of the tensor-core kernel (lca_set_attention_impl(1)).
+struct Paged8SimtArgs {
+  const bf16* q_sem; const bf16* q_pos;
+  const uint8_t* pages_sem; const uint8_t* pages_pos; const float* scale_sem; const float* scale_pos; const int32_t* table;
+  const int32_t* n_rep; const int32_t* n_tok;
+  bf16* out; float* lse;
+  int Hq, Hkv, q_len, g, page, n_pages, width;
+  float scale, bias;
+  long long n_rows;
+};
+
+template <int D_SEM, int D_POS, bool MLA>
+__global__ void __launch_bounds__(128) attn_paged8_simt_kernel(Paged8SimtArgs a) {
+  constexpr int PS = D_SEM / 64, PP = D_POS / 64;            // element pairs per lane
+  const int lane = threadIdx.x & 31;
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= a.n_rows) return;
+  const int h = (int)(row % a.Hq), t = (int)((row / a.Hq) % a.q_len), b = (int)(row / ((long long)a.Hq * a.q_len));
+  const int hk = h / (a.Hq / a.Hkv);
+  float2 qs[PS], qp[PP], acc[PS];
+#pragma unroll
+  for (int i = 0; i < PS; ++i) {
+    acc[i] = make_float2(0.f, 0.f);
+    if (MLA) qs[i] = __bfloat1622float2(reinterpret_cast<const bf162*>(a.q_sem + (size_t)row * D_SEM)[lane + 32 * i]);
+  }
+#pragma unroll
+  for (int i = 0; i < PP; ++i) qp[i] = __bfloat1622float2(reinterpret_cast<const bf162*>(a.q_pos + (size_t)row * D_POS)[lane + 32 * i]);
+  const PagedSpan sp = paged_span(a.n_rep, a.n_tok, b, a.g, a.width * a.page);
+  const int last = sp.n_tok - a.q_len + 1 + t;               // rows below it are seen
+  float mx = -INFINITY, l = 0.f;
+  bool any = false;
+  for (int x = 0; x < last; ++x) {
+    if (x == sp.n_rep && x < sp.tok0) x = sp.tok0;
+    if (x >= last) break;
+    const int pg = a.table[(size_t)b * a.width + x / a.page];
+    if (pg < 0 || pg >= a.n_pages) continue;
+    const size_t block = (size_t)pg * a.Hkv + hk, r = block * a.page + x % a.page;
+    const float fv = fmaxf(a.scale_sem[block], exp2_int(PAGED8_MIN_EXP)), fk = MLA ? a.scale_sem[block] : a.scale_pos[block];
+    const uint16_t* vs = reinterpret_cast<const uint16_t*>(a.pages_sem + r * D_SEM);
+    const uint16_t* ks = reinterpret_cast<const uint16_t*>(a.pages_pos + r * D_POS);
+    float2 v[PS];
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+      const float4 f = e4m3x4_to_float4(vs[lane + 32 * i]);
+      v[i] = make_float2(f.x, f.y);
+      if (MLA) s += qs[i].x * f.x + qs[i].y * f.y;
+    }
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+      const float4 f = e4m3x4_to_float4(ks[lane + 32 * i]);
+      s += qp[i].x * f.x + qp[i].y * f.y;
+    }
+    s = warp_sum(s) * fk * a.scale + (x < sp.n_rep ? a.bias : 0.f);
+    any = true;
+    const float mn = fmaxf(mx, s), corr = expf(mx - mn), w = expf(s - mn);
+    l = l * corr + w;
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+      acc[i].x = acc[i].x * corr + w * (v[i].x * fv);
+      acc[i].y = acc[i].y * corr + w * (v[i].y * fv);
+    }
+    mx = mn;
+  }
+  const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < PS; ++i)
+    reinterpret_cast<bf162*>(a.out + (size_t)row * D_SEM)[lane + 32 * i] = __floats2bfloat162_rn(acc[i].x * inv, acc[i].y * inv);
+  if (a.lse && lane == 0) a.lse[row] = any ? mx + logf(l) : -INFINITY;
+}
+
+int attn_paged8_simt_launch(const Paged8Attn& q) {
+  const lca_params* p = q.p;
+  const lca_paged8* c = q.c;
+  Paged8SimtArgs a = {(const bf16*)q.q_sem, (const bf16*)q.q_pos, (const uint8_t*)c->pages_sem, (const uint8_t*)c->pages_pos, c->scale_sem,
+                      c->scale_pos, c->block_table, q.n_rep, q.n_tok, (bf16*)q.out, q.lse, p->n_q_heads, p->n_kv_heads, q.q_len,
+                      q.n_rep ? p->group_size : 1, c->page_size, c->n_pages, c->table_width, p->softmax_scale, p->rep_logit_bias,
+                      (long long)p->batch * q.q_len * p->n_q_heads};
+  const unsigned grid = (unsigned)((a.n_rows + 3) / 4);
+  if (p->variant == LCA_VARIANT_MLA) {
+    if (p->d_sem == 512) attn_paged8_simt_kernel<512, 64, true><<<grid, 128, 0, q.stream>>>(a);
+    else attn_paged8_simt_kernel<128, 64, true><<<grid, 128, 0, q.stream>>>(a);
+  } else if (p->d_sem == 128) attn_paged8_simt_kernel<128, 128, false><<<grid, 128, 0, q.stream>>>(a);
+  else attn_paged8_simt_kernel<64, 64, false><<<grid, 128, 0, q.stream>>>(a);
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+
+// ---------------------------------------------------------------------------------------------- tensor-core kernel
+// Transposed products: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T and O^T [d x NH] += V^T (T_hi + T_lo)^T, so that the key
+// tile is the 128-row operand whatever the number of heads, a row of K or V is read by the tensor core as it lies in the
+// page (K-major for S, MN-major for O: no transposition, no conversion) and a softmax thread owns one key: scale, mask and
+// bias are one value per thread.  NH (16, 32 or 64) query rows of one KV head share a tile.
+//   warps 0-3  softmax: thread = key = TMEM lane; epilogue: thread = output column d
+//   warp 4     TMA: 128-byte-wide chunks (16 KB) of the 128 rows of a tile, one request per page
+//   warp 5     MMA issue and TMEM
+// The chunks of a tile are consumed as K_0.. then V_0..; S of tile j+1 is issued before O of tile j, and the one ring of
+// slots is filled in exactly that order: K(0) K(1) V(0) K(2) V(1) ...  For MLA a latent chunk passes twice (the second
+// time out of L2): keeping it from S to O would need two whole tiles of slots.
+// Work: all tiles of all (sequence, KV head, block of NH rows) units form one line that is cut into equal ranges, one per
+// CTA; a unit that is cut leaves (O, M, l) of its pieces in the workspace, merged by paged8_combine_kernel.
+template <bool MLA_, int DS_, int DP_, int NH_>
+struct Paged8Plan {
+  static constexpr bool MLA = MLA_;
+  static constexpr int DS = DS_, DP = DP_, NH = NH_;
+  static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
+  static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 bytes wide)
+  static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
+  static constexpr int SLOT = 16384;
+  static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
+  static constexpr int P_BYTES = 128 * NH;                   // one term
+  static constexpr int TM_S = NV * NH, TM_USED = TM_S + 4 * NH;
+  static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
+  static constexpr int CTAS = (MLA && DS == 512) || TM_COLS == 512 ? 1 : 2;        // per SM
+  // floats: qs, M, d, factor, lim [NH]; wmax, lsum [4][NH].  Barriers first.
+  static constexpr int MISC_BYTES = 512 + 4 * (5 * NH + 8 * NH);
+  static constexpr int BUDGET = (CTAS == 1 ? 227 * 1024 : 113 * 1024) - 1024;      // 1 KB to align the base
+  static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / SLOT;
+  static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
+  static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
+  static constexpr int SMEM = OFF_MISC + MISC_BYTES + 1024;
+  static_assert(SLOTS >= NK + 1 && SMEM <= 227 * 1024, "ring of at least one key tile");
+};
+
+struct Paged8Params {
+  CUtensorMap sem, pos;       // [n_pages * Hkv, page, d] codes; boxes of one page x 128 (or 64) bytes
+  const bf16* q_sem; const bf16* q_pos;
+  const float* scale_k; const float* scale_v; const int32_t* table;
+  const int32_t* n_rep; const int32_t* n_tok;
+  bf16* out; float* lse;
+  float* part;                // [2 * CTAs][NH][DS] partial O, then [2 * CTAs][2][NH] M and l
+  long long* prefix;          // [B + 1] tiles before each sequence (all units), written by CTA 0
+  int B, Hq, Hkv, q_len, g, page, n_pages, width, rep, n_blk, min_tiles, grid;
+  float scale_log2, bias_log2;
+};
+
+// Tiles of 128 rows of a sequence: those with representatives, then those with tokens.
+struct TileSpan {
+  PagedSpan s;
+  int n_a, b0, n;
+  __device__ __forceinline__ int row0(int i) const { return (i < n_a ? i : b0 + (i - n_a)) * 128; }
+};
+__device__ __forceinline__ TileSpan tile_span(const Paged8Params& p, int b) {
+  TileSpan t;
+  t.s = paged_span(p.n_rep, p.n_tok, b, p.g, p.width * p.page);
+  t.n_a = (t.s.n_rep + 127) >> 7;
+  t.b0 = max(t.s.tok0 >> 7, t.n_a);
+  t.n = t.n_a + (t.s.n_tok > t.s.tok0 ? max(((t.s.n_tok + 127) >> 7) - t.b0, 0) : 0);
+  return t;
+}
+__device__ __forceinline__ int ctas_used(const Paged8Params& p, long long T) {
+  return (int)max(1ll, min((long long)p.grid, (T + p.min_tiles - 1) / p.min_tiles));
+}
+
+// The pieces of units in one CTA's range of the line.
+struct Walk {
+  int b;
+  long long off, left;        // position inside sequence b's part of the line; tiles left in this CTA's range
+  TileSpan t;
+  int hk, blk, t0, n;         // current piece: tiles [t0, t0 + n) of unit (b, hk, blk)
+  bool fresh;
+  __device__ __forceinline__ bool next(const Paged8Params& p) {
+    if (!fresh) off += n;
+    while (left > 0) {
+      if (b >= p.B) return false;
+      t = tile_span(p, b);
+      if (off < (long long)t.n * p.Hkv * p.n_blk) break;
+      off -= (long long)t.n * p.Hkv * p.n_blk;
+      ++b;
+    }
+    if (left <= 0) return false;
+    const int u = (int)(off / t.n);
+    t0 = (int)(off % t.n);
+    hk = u / p.n_blk; blk = u % p.n_blk;
+    n = (int)min((long long)(t.n - t0), left);
+    left -= n;
+    fresh = false;
+    return true;
+  }
+};
+
+__device__ __forceinline__ void umma_f8_elected(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// kind::f8f6f4, fp32 accumulator, A e4m3, B e4m3 (0) or e5m2 (1)
+__host__ __device__ constexpr uint32_t umma_idesc_f8(int M, int N, int b_format, bool a_mn_major, bool b_mn_major) {
+  return (1u << 4) | ((uint32_t)b_format << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Shared-memory descriptor for rows of `width` bytes with the swizzle of that width (16: none).  K-major: 8 rows (one
+// group) are 8 * width bytes apart.  MN-major: the same picture with the rows along K.  `lbo`: distance of the next block
+// of `width` bytes along the contiguous dimension (only used where the operand is wider than one block).
+__device__ __forceinline__ uint64_t desc_rows(uint32_t addr, int width, uint32_t lbo) {
+  const uint64_t layout = width == 128 ? 2 : width == 64 ? 4 : width == 32 ? 6 : 0;
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
+         ((uint64_t)(((uint32_t)width * 8 >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (layout << 61);
+}
+// Byte offset of 16-byte unit `u` of row `r` in such an image.
+template <int WIDTH>
+__device__ __forceinline__ uint32_t swz(int r, int u) {
+  if (WIDTH == 128) return (uint32_t)(r * 128 + ((u ^ (r & 7)) << 4));
+  if (WIDTH == 64) return (uint32_t)(r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+  if (WIDTH == 32) return (uint32_t)(r * 32 + ((u ^ ((r >> 2) & 1)) << 4));
+  return (uint32_t)(r * 16);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float warp_max_f32(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ bool softmax_any(bool v) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((uint32_t)v) : "memory");
+  return r != 0;
+}
+
+static constexpr int PAGED8_THREADS = 192;
+static constexpr float PAGED8_T_BITS = 8.f;         // the largest weight is 2^8 ...
+static constexpr float PAGED8_SLACK = 3.f;          // ... and may reach 2^11 before the maximum is raised: t_hi up to 2^11
+                                                    // leaves at most 2^8 to t_lo (e4m3 ends at 448)
+
+template <class PL>
+__global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
+  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  const uint32_t bars = base + PL::OFF_MISC;
+  auto FULL = [&](int s) { return bars + 8 * s; };
+  auto EMPTY = [&](int s) { return bars + 8 * (PL::SLOTS + s); };
+  const uint32_t SFULL = bars + 8 * (2 * PL::SLOTS), PFULL = SFULL + 16, PVDONE = SFULL + 24, QFULL = SFULL + 32;
+  unsigned char* misc = base_ptr + PL::OFF_MISC;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 256);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
+  int* s_b = reinterpret_cast<int*>(misc + 264);
+  long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
+  long long* s_warp = reinterpret_cast<long long*>(misc + 288);         // 6 warp totals
+  float* s_qs = reinterpret_cast<float*>(misc + 512);
+  float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
+  int* s_lim = reinterpret_cast<int*>(s_f + NH);
+  float* s_wmax = reinterpret_cast<float*>(s_lim + NH); float* s_lsum = s_wmax + 4 * NH;
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x;
+
+  if (tid == 0) {
+    for (int s = 0; s < PL::SLOTS; ++s) { mbar_init(FULL(s), 1); mbar_init(EMPTY(s), 1); }
+    mbar_init(SFULL, 1); mbar_init(SFULL + 8, 1); mbar_init(PFULL, 128); mbar_init(PVDONE, 1); mbar_init(QFULL, 128);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == 5) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
+  if (warp == 4 && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
+  // this CTA's range of the line: thread i sums the tiles of sequences [i q, (i + 1) q)
+  const long long upu = (long long)p.Hkv * p.n_blk;
+  long long s0 = 0;
+  {
+    const int q = (p.B + PAGED8_THREADS - 1) / PAGED8_THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
+    long long sum = 0;
+    for (int b = lo; b < hi; ++b) sum += (long long)tile_span(p, b).n * upu;
+    long long inc = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
+    if (lane == 31) s_warp[warp] = inc;
+    __syncthreads();
+    long long T = 0, before = inc - sum;
+    for (int w = 0; w < PAGED8_THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
+    const int G = ctas_used(p, T);
+    long long s1 = 0;
+    if ((int)blockIdx.x < G) { s0 = (long long)blockIdx.x * T / G; s1 = ((long long)blockIdx.x + 1) * T / G; }
+    if (blockIdx.x == 0) {                                   // for the combining kernel
+      long long at = before;
+      for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (long long)tile_span(p, b).n * upu; }
+      if (tid == 0) p.prefix[p.B] = T;
+    }
+    if (s1 > s0 && s0 >= before && s0 < before + sum) {      // exactly one thread
+      long long at = before;
+      int b = lo;
+      while (true) {
+        const long long n = (long long)tile_span(p, b).n * upu;
+        if (s0 < at + n) break;
+        at += n; ++b;
+      }
+      *s_b = b; s_off[0] = s0 - at; s_off[1] = s1 - s0;
+    }
+    if (tid == 0 && s1 <= s0) { *s_b = 0; s_off[0] = 0; s_off[1] = 0; }
+  }
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk w;
+  w.b = *s_b; w.off = s_off[0]; w.left = s_off[1]; w.fresh = true; w.n = 0;
+  auto fail = [&](int code) { atomicCAS(&g_paged8_status, 0, code); *abort_flag = 1; };
+
+  if (warp == 4) {
+    // ------------------------------------------------------------------------------------------------ producer
+    int slot = 0;
+    uint32_t phase = 0;
+    bool ok = true;
+    const int npp = 128 / p.page;
+    while (ok && w.next(p)) {
+      const PagedSpan sp = w.t.s;
+      const int32_t* table = p.table + (size_t)w.b * p.width;
+      // third coordinate of this lane's page; one past the end (filled with zeros) where no row is present
+      auto look = [&](int i) {
+        const int nowhere = p.n_pages * p.Hkv;
+        if (i >= w.n || lane >= npp) return nowhere;
+        const int x = w.t.row0(w.t0 + i) + lane * p.page;
+        if (!sp.any(x, p.page) || x / p.page >= p.width) return nowhere;
+        const int pg = table[x / p.page];
+        return pg >= 0 && pg < p.n_pages ? pg * p.Hkv + w.hk : nowhere;
+      };
+      auto load = [&](const CUtensorMap* map, int x, int width, int z) {
+        if (!ok) return;
+        if (!mbar_wait(EMPTY(slot), phase ^ 1, abort_flag)) { ok = false; }
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); return; }
+        if (lane == 0) mbar_expect_tx(FULL(slot), 128 * width);
+        __syncwarp();
+        if (lane < npp) tma_load_3d(base + slot * PL::SLOT + lane * p.page * width, map, x, 0, z, FULL(slot));
+        if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; }
+      };
+      auto load_k = [&](int z) {
+#pragma unroll
+        for (int c = 0; c < PL::KSEM; ++c) load(&p.sem, c * 128, 128, z);
+        load(&p.pos, 0, DP, z);
+      };
+      int z0 = look(0), z1 = look(1);
+      load_k(z0);
+      for (int j = 0; j < w.n && ok; ++j) {
+        const int z2 = look(j + 2);
+        if (j + 1 < w.n) load_k(z1);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) load(&p.sem, c * 128, PL::VW, z0);
+        z0 = z1; z1 = z2;
+      }
+    }
+  } else if (warp == 5) {
+    // ----------------------------------------------------------------------------------------------------- MMA
+    const uint32_t leader = elect_one();
+    constexpr uint32_t ID_S = umma_idesc_f8(128, 2 * NH, 0, false, false);
+    constexpr uint32_t ID_HI = umma_idesc_f8(128, NH, 1, true, true), ID_LO = umma_idesc_f8(128, NH, 0, true, true);
+    int slot = 0;
+    uint32_t phase = 0, g = 0, seg = 0;
+    bool ok = true;
+    auto wait_slot = [&]() {
+      ok = ok && mbar_wait(FULL(slot), phase, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok && lane == 0) fail(ERR_WAIT_KV_FULL);
+      return ok;
+    };
+    auto done_slot = [&]() {
+      umma_commit_elected(leader, EMPTY(slot));
+      if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; }
+    };
+    auto issue_s = [&](uint32_t buf) {
+      const uint32_t d = tmem + PL::TM_S + buf * 2 * NH;
+      uint32_t acc = 0;
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        if (!wait_slot()) return;
+        tc_fence_after();
+        const int width = c < PL::KSEM ? 128 : DP;
+        const uint64_t ad = desc_rows(base + slot * PL::SLOT, width, 16);
+        const uint64_t bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
+#pragma unroll
+        for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
+        done_slot();
+      }
+      umma_commit_elected(leader, SFULL + 8 * buf);
+    };
+    const uint64_t p_hi = desc_rows(base + PL::OFF_P, NH, 128), p_lo = desc_rows(base + PL::OFF_P + PL::P_BYTES, NH, 128);
+    while (ok && w.next(p)) {
+      ok = mbar_wait(QFULL, seg & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { if (lane == 0) fail(ERR_WAIT_Q); break; }
+      ++seg;
+      tc_fence_after();
+      issue_s(g & 1);
+      for (int j = 0; j < w.n && ok; ++j, ++g) {
+        if (j + 1 < w.n) issue_s((g + 1) & 1);
+        if (!ok) break;
+        ok = mbar_wait(PFULL, g & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) { if (lane == 0) fail(ERR_WAIT_P_FULL); break; }
+        tc_fence_after();
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          if (!wait_slot()) break;
+          tc_fence_after();
+          // 64-wide values: M stays 128, the second half of the operand is the unused half of the slot and the output
+          // lanes it feeds are never read
+          const uint64_t ad = desc_rows(base + slot * PL::SLOT, PL::VW, 8192);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_hi, k * 2 * NH), ID_HI, (j > 0 || k > 0) ? 1u : 0u);
+            umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_lo, k * 2 * NH), ID_LO, 1u);
+          }
+          done_slot();
+        }
+        umma_commit_elected(leader, PVDONE);
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------------------------- softmax, epilogue
+    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    const float dither = ((float)(__brev((unsigned)lane) >> 27) + 0.5f) * (1.f / 32.f) * 0.001953125f - 0.0009765625f;   // (-1/2, 1/2) of 2^-9
+    uint32_t g = 0, seg_chunks = 0;
+    bool first = true;
+    bool ok = true;
+    float l[NH];
+    // splits this unit's query rows into e4m3 terms and writes them where S reads them
+    auto load_q = [&](const Walk& u) {
+      constexpr int VS = PL::KSEM * 16, VQ = VS + DP / 8, NL = (VQ + 31) / 32;   // 8-element vectors of a row
+      const int n_rows = p.q_len * p.rep - u.blk * NH;
+      for (int r = warp; r < NH; r += 4) {
+        const int gr = u.blk * NH + r;
+        uint4 v[NL];
+        uint32_t top = 0;
+        const size_t row = ((size_t)u.b * p.q_len + gr / p.rep) * p.Hq + (size_t)u.hk * p.rep + gr % p.rep;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int c = lane + 32 * i;
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < n_rows && c < VQ)
+            v[i] = *reinterpret_cast<const uint4*>(c < VS ? p.q_sem + row * DS + 8 * c : p.q_pos + row * DP + 8 * (c - VS));
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7fffu, (x[k] >> 16) & 0x7fffu));
+        }
+        top = __reduce_max_sync(0xffffffffu, top);
+        const int e = min(max(134 - (int)(top >> 7), -119), 120);       // largest element times 2^e in [128, 256)
+        const float f = exp2_int(e);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int c = lane + 32 * i;
+          if (c >= VQ) continue;
+          const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+          uint32_t hi[2], lo[2];
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const float a0 = __uint_as_float(x[2 * k] << 16) * f, a1 = __uint_as_float(x[2 * k] & 0xffff0000u) * f;
+            const float a2 = __uint_as_float(x[2 * k + 1] << 16) * f, a3 = __uint_as_float(x[2 * k + 1] & 0xffff0000u) * f;
+            hi[k] = e4m3x4_from_float(a0, a1, a2, a3);
+            const float4 h = e4m3x4_to_float4(hi[k]);
+            lo[k] = e4m3x4_from_float(a0 - h.x, a1 - h.y, a2 - h.z, a3 - h.w);
+          }
+          const bool sem = c < VS;
+          const int chunk = sem ? c / 16 : PL::KSEM, u16 = (sem ? c % 16 : c - VS) / 2, half = c & 1;
+          unsigned char* q = base_ptr + PL::OFF_Q + chunk * 2 * NH * 128 + 8 * half;
+          const uint32_t oh = sem ? swz<128>(r, u16) : swz<DP>(r, u16), ol = sem ? swz<128>(NH + r, u16) : swz<DP>(NH + r, u16);
+          *reinterpret_cast<uint2*>(q + oh) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2*>(q + ol) = make_uint2(lo[0], lo[1]);
+        }
+        // a row with an infinity or a NaN has no finite logit; rows behind the last one never have weight
+        if (lane == 0) {
+          s_qs[r] = r < n_rows ? (top >= 0x7f80u ? __int_as_float(0x7fffffff) : exp2_int(-e)) : 0.f;
+          s_m[r] = r < n_rows ? 0.f : 3.0e38f;
+          s_lim[r] = u.t.s.n_tok - p.q_len + 1 + gr / p.rep;
+        }
+      }
+      fence_proxy_async_smem();
+      mbar_arrive(QFULL);
+      softmax_barrier();
+    };
+    bool more = w.next(p);
+    if (more) load_q(w);
+    while (more) {
+      const PagedSpan sp = w.t.s;
+      const int n_rows = min(p.q_len * p.rep - w.blk * NH, NH);
+      const int32_t* table = p.table + (size_t)w.b * p.width;
+      bool unset = tid < n_rows;                             // thread h: head h has no maximum yet
+#pragma unroll
+      for (int i = 0; i < NH; ++i) l[i] = 0.f;
+      auto page_of = [&](int j) {                            // page of this thread's key in tile j, -1: none
+        if (j >= w.n) return -1;
+        const int x = w.t.row0(w.t0 + j) + tid;
+        if (!sp.has(x)) return -1;                           // has() implies x below the table's end
+        const int pg = table[x / p.page];
+        return pg >= 0 && pg < p.n_pages ? pg : -1;
+      };
+      int pg0 = page_of(0), pg1 = page_of(1);
+      float ks = 0.f, vs = 1.f;
+      if (pg0 >= 0) { ks = p.scale_k[(size_t)pg0 * p.Hkv + w.hk]; vs = p.scale_v[(size_t)pg0 * p.Hkv + w.hk]; }
+      for (int j = 0; j < w.n; ++j, ++g) {
+        const int row0 = w.t.row0(w.t0 + j), x = row0 + tid;
+        const bool valid = pg0 >= 0;
+        // the next tile's scales and the page after that are on their way while this tile is worked on
+        float ks1 = 0.f, vs1 = 1.f;
+        if (pg1 >= 0) { ks1 = p.scale_k[(size_t)pg1 * p.Hkv + w.hk]; vs1 = p.scale_v[(size_t)pg1 * p.Hkv + w.hk]; }
+        const int pg2 = page_of(j + 2);
+        vs = fmaxf(vs, exp2_int(PAGED8_MIN_EXP));
+        // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 vs + 8): both are multiples of e = 2^(y - M + half), half way
+        // between them, so that neither is lost below 2^-126 where the scales of a sequence span more than fp32 does.
+        const float half = 0.5f * (lg2(vs) + PAGED8_T_BITS), f_t = ex2(half), f_l = ex2(PAGED8_T_BITS - half);
+        const float kf = ks * p.scale_log2, cb = half + (x < sp.n_rep ? p.bias_log2 : 0.f);
+        const bool all_valid = __all_sync(0xffffffffu, valid);
+        const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
+
+        ok = mbar_wait(SFULL + 8 * (g & 1), (g >> 1) & 1, abort_flag);
+        if (!ok) fail(ERR_WAIT_S_FULL);
+        __syncwarp();
+        tc_fence_after();
+        float z[NH];
+        float zmax = -INFINITY;
+        constexpr int CH = NH < 32 ? NH : 32;
+#pragma unroll
+        for (int h0 = 0; h0 < NH; h0 += CH) {
+          uint32_t hi[CH], lo[CH];
+          const uint32_t at = tmem + lane_base + PL::TM_S + (g & 1) * 2 * NH + h0;
+#pragma unroll
+          for (int i = 0; i < CH; i += 16) { tmem_ld16(at + i, hi + i); tmem_ld16(at + NH + i, lo + i); }
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < CH; i += 4) {
+            const float4 q4 = *reinterpret_cast<const float4*>(s_qs + h0 + i), m4 = *reinterpret_cast<const float4*>(s_m + h0 + i);
+            const float qq[4] = {q4.x, q4.y, q4.z, q4.w}, mm[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              z[h0 + i + k] = fmaf(__uint_as_float(hi[i + k]) + __uint_as_float(lo[i + k]), kf * qq[k], cb - mm[k]);
+          }
+        }
+        if (!all_valid || limited) {
+#pragma unroll
+          for (int i = 0; i < NH; ++i) z[i] = valid && (!limited || x < s_lim[i]) ? z[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < NH; i += 2) zmax = max3(zmax, z[i], z[i + 1]);
+        if (softmax_any(zmax + half > PAGED8_T_BITS + PAGED8_SLACK || unset)) {
+          // raise the maxima: per head the largest log2 t of the tile
+#pragma unroll
+          for (int i = 0; i < NH; ++i) {
+            const float m = warp_max_f32(z[i] + half);
+            if (lane == (i & 31)) s_wmax[warp * NH + i] = m;
+          }
+          softmax_barrier();
+          if (tid < NH) {
+            const float m = fmaxf(fmaxf(s_wmax[tid], s_wmax[NH + tid]), fmaxf(s_wmax[2 * NH + tid], s_wmax[3 * NH + tid]));
+            float d = 0.f, f = 1.f;
+            if (unset ? m > -INFINITY : m > PAGED8_T_BITS) {
+              d = m - PAGED8_T_BITS;
+              f = unset ? 1.f : ex2(-d);                     // nothing has been added under an unset maximum
+              s_m[tid] += d;
+              unset = false;
+            }
+            s_d[tid] = d; s_f[tid] = f;
+          }
+          if (j > 0) {
+            ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag); // O is complete up to the previous tile
+            if (!ok) fail(ERR_WAIT_O_DONE);
+            __syncwarp();
+          }
+          softmax_barrier();
+#pragma unroll
+          for (int i = 0; i < NH; ++i) { z[i] -= s_d[i]; l[i] *= s_f[i]; }
+          if (j > 0) {
+            tc_fence_after();
+#pragma unroll 1
+            for (int i = 0; i < NV * NH; i += 16) {
+              uint32_t o[16];
+              tmem_ld16(tmem + lane_base + i, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * s_f[(i + k) % NH]);
+              tmem_st16(tmem + lane_base + i, o);
+            }
+            tmem_wait_st();
+          }
+        } else if (j > 0) {
+          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);   // the weights of the previous tile have been read
+          if (!ok) fail(ERR_WAIT_O_DONE);
+          __syncwarp();
+        }
+        unsigned char* ph = base_ptr + PL::OFF_P;
+#pragma unroll
+        for (int h0 = 0; h0 < NH; h0 += 16) {
+          uint32_t wh[4], wl[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float hi[4], lo[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float e = ex2(z[h0 + 4 * i + k]), t = e * f_t;
+              l[h0 + 4 * i + k] = fmaf(e, f_l, l[h0 + 4 * i + k]);
+              hi[k] = __uint_as_float((__float_as_uint(t) + 0x00100000u) & 0xffe00000u);      // three significant bits
+              lo[k] = (t - hi[k]) + dither;
+            }
+            wh[i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
+            wl[i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
+          }
+          const uint32_t o = swz<NH>(tid, h0 / 16);
+          *reinterpret_cast<uint4*>(ph + o) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+          *reinterpret_cast<uint4*>(ph + PL::P_BYTES + o) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+        }
+        // Rows that were fetched with a page but are not present may hold anything; their weight is 0 and 0 * NaN is not.
+        const int part_r = sp.n_rep % p.page ? sp.n_rep - sp.n_rep % p.page - row0 : -1;
+        const int part_t = sp.n_tok % p.page ? sp.n_tok - sp.n_tok % p.page - row0 : -1;
+        if ((part_r >= 0 && part_r < 128) || (part_t >= 0 && part_t < 128)) {
+#pragma unroll 1
+          for (int c = 0; c < NV; ++c) {
+            const uint32_t at = seg_chunks + (uint32_t)min(j + 2, w.n) * NK + (uint32_t)j * NV + c;      // place in the order of loads
+            const int s = (int)(at % PL::SLOTS);
+            ok = mbar_wait(FULL(s), (at / PL::SLOTS) & 1, abort_flag);
+            if (!ok) fail(ERR_WAIT_KV_FULL);
+            if (!valid) {
+              uint4* row = reinterpret_cast<uint4*>(base_ptr + s * PL::SLOT + tid * PL::VW);
+#pragma unroll
+              for (int i = 0; i < PL::VW / 16; ++i) row[i] = make_uint4(0u, 0u, 0u, 0u);
+            }
+          }
+          __syncwarp();
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(PFULL);
+        pg0 = pg1; pg1 = pg2; ks = ks1; vs = vs1;
+      }
+      seg_chunks += (uint32_t)w.n * (NK + NV);
+      // ---- this piece is done: its sums, maxima and row addresses, then the next unit's queries (S of this piece is
+      // complete), then O
+      const bool whole = w.n == w.t.n;
+      const int b = w.b, hk = w.hk, blk = w.blk;
+      const size_t part = (size_t)2 * blockIdx.x + (first ? 0 : 1);
+      first = false;
+      // sums over the 128 keys: halving exchange inside the warp, then the four warps
+#pragma unroll
+      for (int i = 0; i < NH; ++i) {
+        float v = l[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == (i & 31)) s_lsum[warp * NH + i] = v;
+      }
+      softmax_barrier();
+      if (tid < NH) {
+        const float sum = (s_lsum[tid] + s_lsum[NH + tid]) + (s_lsum[2 * NH + tid] + s_lsum[3 * NH + tid]);
+        if (!whole) {
+          float* ml = p.part + (size_t)2 * p.grid * NH * DS + part * 2 * NH;
+          ml[tid] = unset ? -INFINITY : s_m[tid]; ml[NH + tid] = sum;
+        } else if (tid < n_rows) {
+          const int gr = blk * NH + tid;
+          if (p.lse) p.lse[((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep] =
+              sum == 0.f ? -INFINITY : (s_m[tid] + log2f(sum) - PAGED8_T_BITS) * 0.6931471805599453f;
+        }
+        s_f[tid] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      }
+      softmax_barrier();
+      more = w.next(p);
+      if (more) load_q(w);
+      ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
+      if (!ok) fail(ERR_WAIT_O_DONE);
+      __syncwarp();
+      tc_fence_after();
+#pragma unroll 1
+      for (int i = 0; i < NV * NH; i += 16) {
+        uint32_t o[16];
+        tmem_ld16(tmem + lane_base + i, o);
+        tmem_wait_ld();
+        const int d = (i / NH) * 128 + tid, h0 = i % NH;
+        if (DS >= 128 || tid < DS) {
+          if (whole) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) {
+              const int gr = blk * NH + h0 + k;
+              if (h0 + k < n_rows)
+                p.out[(((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep) * DS + d] =
+                    __float2bfloat16_rn(s_f[h0 + k] == 0.f ? 0.f : __uint_as_float(o[k]) * s_f[h0 + k]);   // no key: O may be 0 * NaN
+            }
+          } else {
+            float* dst = p.part + part * NH * DS + (size_t)h0 * DS + d;
+#pragma unroll
+            for (int k = 0; k < 16; ++k) dst[(size_t)k * DS] = __uint_as_float(o[k]);
+          }
+        }
+      }
+      tc_fence_before();
+      softmax_barrier();                                     // s_f is written again by the next piece
+    }
+  }
+  // ---- let straggling copies land if the CTA gave up, then free TMEM
+  if (*abort_flag && warp == 0 && lane == 0) {
+    const long long t0c = clock64();
+    while (clock64() - t0c < 2000000ll) __nanosleep(1000);
+  }
+  __syncthreads();
+  if (warp == 5) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
+}
+
+// Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
+// no tile at all.  One CTA: 1024 outputs of a unit.
+template <int DS, int NH>
+__global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
+  constexpr int SPLIT = NH * DS / 1024;
+  const long long unit = blockIdx.x / SPLIT;
+  const int x = (int)(blockIdx.x % SPLIT) * 1024 + (int)threadIdx.x * 4, h = x / DS, d = x % DS;
+  const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
+  const int gr = blk * NH + h;
+  if (gr >= p.q_len * p.rep) return;
+  const long long T = p.prefix[p.B], seq = p.prefix[b], n = (p.prefix[b + 1] - seq) / per;
+  const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float m = -INFINITY, l = 0.f;
+  if (n > 0) {
+    const int G = ctas_used(p, T);
+    const long long u0 = seq + u * n, u1 = u0 + n;
+    // CTA c owns [c T / G, (c + 1) T / G)
+    int c0 = (int)(u0 * G / T);
+    while ((long long)(c0 + 1) * T / G <= u0) ++c0;
+    if ((long long)(c0 + 1) * T / G >= u1) return;           // not cut: written by the CTA that worked on it
+    const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
+    const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
+    for (int c = c0; c < G && (long long)c * T / G < u1; ++c) m = fmaxf(m, ml[(size_t)(2 * c + (c == c0 ? first : 0)) * 2 * NH + h]);
+    for (int c = c0; c < G && (long long)c * T / G < u1; ++c) {
+      const size_t part = (size_t)(2 * c + (c == c0 ? first : 0));
+      const float lj = ml[part * 2 * NH + NH + h];
+      if (lj == 0.f) continue;                               // no key of that piece was seen
+      const float f = exp2f(0.5f * (ml[part * 2 * NH + h] - m));       // applied twice: M contains the scales, the square may be below fp32
+      const float4 v = *reinterpret_cast<const float4*>(p.part + part * NH * DS + x);
+      l = fmaf(f * lj, f, l);
+      o.x = fmaf(f * v.x, f, o.x); o.y = fmaf(f * v.y, f, o.y); o.z = fmaf(f * v.z, f, o.z); o.w = fmaf(f * v.w, f, o.w);
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint2 w;
+  w.x = pack_bf16x2(o.x * inv, o.y * inv); w.y = pack_bf16x2(o.z * inv, o.w * inv);
+  *reinterpret_cast<uint2*>(p.out + row * DS + d) = w;
+  if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d);   // attn_tc.cu
+
+static int paged8_rows_per_tile(const lca_params* p, int q_len) {
+  // The tile is padded to NH rows: the smallest that holds all rows of a KV head, so that the softmax threads (one
+  // exponential per padded row and key) do not work for nothing; 64 at most, as O takes d / 128 * NH columns of TMEM.
+  const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+}
+static int paged8_grid(const lca_params* p, int nh) {
+  const bool one = p->d_sem == 512 || (nh == 64);
+  return 148 * (one ? 1 : 2);
+}
+size_t attn_paged8_workspace_bytes(const lca_params* p, int q_len) {
+  const int nh = paged8_rows_per_tile(p, q_len), grid = paged8_grid(p, nh);
+  return (size_t)2 * grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float) + ((size_t)p->batch + 1) * sizeof(long long) + 64;
+}
+
+template <class PL>
+static int paged8_launch(Paged8Params& P, cudaStream_t stream) {
+  auto kern = attn_paged8_kernel<PL>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM) != cudaSuccess) return LCA_ERR_CUDA;
+  kern<<<P.grid, PAGED8_THREADS, PL::SMEM, stream>>>(P);
+  const long long units = (long long)P.B * P.Hkv * P.n_blk * (PL::NH * PL::DS / 1024);
+  paged8_combine_kernel<PL::DS, PL::NH><<<(unsigned)units, 256, 0, stream>>>(P);
+  note_launch(2);
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+template <bool MLA, int DS, int DP>
+static int paged8_launch_rows(Paged8Params& P, int nh, cudaStream_t stream) {
+  if (nh == 16) return paged8_launch<Paged8Plan<MLA, DS, DP, 16>>(P, stream);
+  if (nh == 32) return paged8_launch<Paged8Plan<MLA, DS, DP, 32>>(P, stream);
+  return paged8_launch<Paged8Plan<MLA, DS, DP, 64>>(P, stream);
+}
+
+int attn_paged8_launch(const Paged8Attn& a) {
+  const lca_params* p = a.p;
+  const lca_paged8* c = a.c;
+  const bool mla = p->variant == LCA_VARIANT_MLA;
+  Paged8Params P;
+  memset(&P, 0, sizeof(P));
+  const long long blocks = (long long)c->n_pages * p->n_kv_heads;
+  if (!make_tensor_map_pages(&P.sem, c->pages_sem, p->d_sem, c->page_size, blocks, p->d_sem >= 128 ? 128 : p->d_sem) ||
+      !make_tensor_map_pages(&P.pos, c->pages_pos, p->d_pos, c->page_size, blocks, p->d_pos))
+    return LCA_ERR_CUDA;
+  P.q_sem = (const bf16*)a.q_sem; P.q_pos = (const bf16*)a.q_pos;
+  P.scale_v = c->scale_sem; P.scale_k = mla ? c->scale_sem : c->scale_pos; P.table = c->block_table;
+  P.n_rep = a.n_rep; P.n_tok = a.n_tok; P.out = (bf16*)a.out; P.lse = a.lse;
+  P.B = p->batch; P.Hq = p->n_q_heads; P.Hkv = p->n_kv_heads; P.q_len = a.q_len; P.g = a.n_rep ? p->group_size : 1;
+  P.page = c->page_size; P.n_pages = c->n_pages; P.width = c->table_width; P.rep = P.Hq / P.Hkv;
+  const int nh = paged8_rows_per_tile(p, a.q_len);
+  P.n_blk = (int)(((long long)P.q_len * P.rep + nh - 1) / nh);
+  P.grid = paged8_grid(p, nh); P.min_tiles = 2;
+  P.scale_log2 = p->softmax_scale * 1.4426950408889634f; P.bias_log2 = p->rep_logit_bias * 1.4426950408889634f;
+  P.part = static_cast<float*>(a.ws);
+  const size_t part_bytes = (size_t)2 * P.grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float);
+  P.prefix = reinterpret_cast<long long*>(static_cast<char*>(a.ws) + (part_bytes + 15) / 16 * 16);
+  if ((long long)P.B * P.Hkv * P.n_blk * ((long long)nh * p->d_sem / 1024) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if (mla) return p->d_sem == 512 ? paged8_launch_rows<true, 512, 64>(P, nh, a.stream) : paged8_launch_rows<true, 128, 64>(P, nh, a.stream);
+  return p->d_sem == 128 ? paged8_launch_rows<false, 128, 128>(P, nh, a.stream) : paged8_launch_rows<false, 64, 64>(P, nh, a.stream);
+}
+
+int attn_paged8_take_status() {
+  int st = 0;
+  if (cudaMemcpyFromSymbol(&st, g_paged8_status, sizeof(int)) != cudaSuccess) return -1;
+  if (st != 0) {
+    int zero = 0;
+    cudaMemcpyToSymbol(g_paged8_status, &zero, sizeof(int));
+  }
+  return st;
+}
+
+}  // namespace lca

@@ -1214,31 +1214,41 @@ size_t update_smem_bytes(const lca_params* p) {
   return g * (size_t)(p->d_sem + p->d_pos) * sizeof(bf16) + (size_t)key_dim(p) * sizeof(double) + g * (sizeof(double) + sizeof(float));
 }
 
+int update_qbar_launch(const lca_params* p, const void* q_tail_sem, const void* q_tail_pos, int64_t q_tail_batch_stride,
+                       void* ws, cudaStream_t stream) {
+  const int dk = key_dim(p), B = p->batch, Hkv = p->n_kv_heads;
+  const int sem_in_logit = p->variant == LCA_VARIANT_MLA;
+  double* qbar = reinterpret_cast<double*>(ws);
+  double* partial = qbar + (size_t)B * Hkv * dk;
+  const int n = p->n_summary_q > 0 ? p->n_summary_q : p->group_size;
+  const int rows = n * (p->n_q_heads / Hkv);
+  const int cpc = qbar_chunks_per_cta((long long)rows * Hkv * B);
+  const int nch = (rows + QBAR_ROWS_PER_CHUNK - 1) / QBAR_ROWS_PER_CHUNK;
+  const int pieces = dk / 8;
+  const int row_lanes = qbar_row_lanes(pieces);
+  const int threads = ((pieces * row_lanes + 31) / 32) * 32;
+  qbar_partial_kernel<<<dim3((nch + cpc - 1) / cpc, Hkv, B), threads, (size_t)2 * row_lanes * dk * sizeof(double), stream>>>(
+      (const bf16*)q_tail_sem, (const bf16*)q_tail_pos, q_tail_batch_stride, n, p->n_q_heads, Hkv, p->d_sem, p->d_pos,
+      sem_in_logit, row_lanes, partial, SeqTab{}, nch, cpc);
+  qbar_final_kernel<<<dim3(Hkv, B), dk < 1024 ? ((dk + 31) / 32) * 32 : 1024, 0, stream>>>(
+      partial, nch, dk, (double)n * (double)(p->n_q_heads / Hkv), qbar, SeqTab{}, n, p->n_q_heads / Hkv);
+  note_launch(2);
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+
 int update_launch(const lca_params* p, const void* q_tail_sem, const void* q_tail_pos, int64_t q_tail_batch_stride,
                   const float* qbar_opt, void* cache_sem, void* cache_pos, int cap, int32_t* n_rep, int32_t* n_rows,
                   const int32_t* n_tok, int32_t* anchor_out, void* ws, cudaStream_t stream) {
   const int dk = key_dim(p), B = p->batch, Hkv = p->n_kv_heads;
   const int sem_in_logit = p->variant == LCA_VARIANT_MLA;
   double* qbar = reinterpret_cast<double*>(ws);
-  double* partial = qbar + (size_t)B * Hkv * dk;
   if (qbar_opt) {
     const int n = B * Hkv * dk;
     qbar_widen_kernel<<<(n + 255) / 256, 256, 0, stream>>>(qbar_opt, qbar, n);
     note_launch();
   } else {
-    const int n = p->n_summary_q > 0 ? p->n_summary_q : p->group_size;
-    const int rows = n * (p->n_q_heads / Hkv);
-    const int cpc = qbar_chunks_per_cta((long long)rows * Hkv * B);
-    const int nch = (rows + QBAR_ROWS_PER_CHUNK - 1) / QBAR_ROWS_PER_CHUNK;
-    const int pieces = dk / 8;
-    const int row_lanes = qbar_row_lanes(pieces);
-    const int threads = ((pieces * row_lanes + 31) / 32) * 32;
-    qbar_partial_kernel<<<dim3((nch + cpc - 1) / cpc, Hkv, B), threads, (size_t)2 * row_lanes * dk * sizeof(double), stream>>>(
-        (const bf16*)q_tail_sem, (const bf16*)q_tail_pos, q_tail_batch_stride, n, p->n_q_heads, Hkv, p->d_sem, p->d_pos,
-        sem_in_logit, row_lanes, partial, SeqTab{}, nch, cpc);
-    qbar_final_kernel<<<dim3(Hkv, B), dk < 1024 ? ((dk + 31) / 32) * 32 : 1024, 0, stream>>>(
-        partial, nch, dk, (double)n * (double)(p->n_q_heads / Hkv), qbar, SeqTab{}, n, p->n_q_heads / Hkv);
-    note_launch(2);
+    const int st = update_qbar_launch(p, q_tail_sem, q_tail_pos, q_tail_batch_stride, ws, stream);
+    if (st != LCA_OK) return st;
   }
   UpdateArgs a;
   a.cache_sem = (bf16*)cache_sem; a.cache_pos = (bf16*)cache_pos; a.qbar = qbar;

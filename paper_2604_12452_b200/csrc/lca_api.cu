@@ -430,6 +430,112 @@ int lca_decode_step_update_ring(const lca_params* p, const void* q_sem, const vo
                             anchor_out, ws, (cudaStream_t)stream);
 }
 
+// ---- paged 8-bit cache
+static int check_paged(const lca_paged8* c) {
+  if (!c || c->n_pages <= 0) return LCA_ERR_INVALID_ARG;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if ((int64_t)c->n_pages * c->page_size > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  return LCA_OK;
+}
+static int check_paged_table(const lca_params* p, const lca_paged8* c, bool reps) {
+  if (!c->block_table || c->table_width <= 0) return LCA_ERR_INVALID_ARG;
+  // rows are numbered with 32 bits, and a tile of 128 of them may start at the last one
+  if ((int64_t)c->table_width * c->page_size > 0x7fffff00ll) return LCA_ERR_INVALID_ARG;
+  if (reps && (p->group_size <= 0 || p->group_size % c->page_size != 0)) return LCA_ERR_INVALID_ARG;
+  return LCA_OK;
+}
+static int check_paged_pool(const lca_params* p, const lca_paged8* c) {
+  if (!c->pages_sem || !c->pages_pos || !c->scale_sem) return LCA_ERR_INVALID_ARG;
+  if ((p->variant == LCA_VARIANT_GQA) != (c->scale_pos != nullptr)) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos)) return LCA_ERR_MISALIGNED;
+  if ((int64_t)c->n_pages * p->n_kv_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (!simt_shape_ok(p)) return LCA_ERR_UNSUPPORTED_SHAPE;
+  return LCA_OK;
+}
+
+int lca_page_update(const lca_params* p, const lca_paged8* cache, const int32_t* n_rep, const int32_t* n_tok,
+                    int32_t* held_rep, int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map,
+                    int32_t n_rows, int32_t rows_per_seq, int32_t* row_offsets, int32_t* status, void* stream) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_table(p, cache, n_rep != nullptr);
+  if (st != LCA_OK) return st;
+  if (!n_tok || !held_tok || !free_pages || !n_free || !status || (n_rep != nullptr) != (held_rep != nullptr)) return LCA_ERR_INVALID_ARG;
+  if (n_rows < 0 || rows_per_seq < 0 || (n_rows > 0 && !slot_map)) return LCA_ERR_INVALID_ARG;
+  if (slot_map && rows_per_seq == 0 && !row_offsets) return LCA_ERR_INVALID_ARG;
+  if (slot_map && rows_per_seq > 0 && n_rows != (int64_t)p->batch * rows_per_seq) return LCA_ERR_INVALID_ARG;
+  return page_update_launch(p, cache, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, n_rows, rows_per_seq,
+                            row_offsets, status, (cudaStream_t)stream);
+}
+
+int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* rows_sem, const void* rows_pos,
+                     const int32_t* slot_map, int64_t n_rows, void* stream) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  if (st != LCA_OK) return st;
+  if (n_rows < 0 || n_rows > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (n_rows == 0) return LCA_OK;
+  if (!rows_sem || !rows_pos || !slot_map) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(rows_sem) || !aligned16(rows_pos)) return LCA_ERR_MISALIGNED;
+  return paged8_write_launch(p, cache, rows_sem, rows_pos, slot_map, n_rows, (cudaStream_t)stream);
+}
+
+size_t lca_paged8_workspace_bytes(const lca_params* p, const lca_paged8* cache, int32_t q_len) {
+  if (check_params(p, false) != LCA_OK || check_paged(cache) != LCA_OK || q_len <= 0 || !simt_shape_ok(p)) return 0;
+  return attn_paged8_workspace_bytes(p, q_len);
+}
+
+int lca_decode_attention_paged8(const lca_params* p, const lca_paged8* cache, const void* q_sem, const void* q_pos,
+                                int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
+                                void* ws, size_t ws_bytes, void* stream) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_table(p, cache, n_rep != nullptr);
+  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  if (st != LCA_OK) return st;
+  if (!q_pos || !n_tok || !out || q_len <= 0) return LCA_ERR_INVALID_ARG;
+  if (p->variant == LCA_VARIANT_MLA && !q_sem) return LCA_ERR_INVALID_ARG;
+  if ((int64_t)p->batch * q_len * p->n_q_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(q_pos) || !aligned16(out) || (q_sem && !aligned16(q_sem))) return LCA_ERR_MISALIGNED;
+  Paged8Attn a = {p, cache, p->variant == LCA_VARIANT_MLA ? q_sem : nullptr, q_pos, q_len, n_rep, n_tok, out, lse_opt, ws,
+                  (cudaStream_t)stream};
+  if (g_attn_impl.load() == 1) return attn_paged8_simt_launch(a);
+  if (!ws || !aligned16(ws)) return LCA_ERR_INVALID_ARG;
+  if (ws_bytes < attn_paged8_workspace_bytes(p, q_len)) return LCA_ERR_WORKSPACE_TOO_SMALL;
+  return attn_paged8_launch(a);
+}
+
+int lca_decode_update_paged8(const lca_params* p, const lca_paged8* cache, const void* q_tail_sem,
+                             const void* q_tail_pos, int64_t q_tail_batch_stride, const float* qbar_opt,
+                             const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
+                             void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_table(p, cache, true);
+  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  if (st != LCA_OK) return st;
+  if (p->window < 0 || p->n_summary_q < 0) return LCA_ERR_INVALID_ARG;
+  if (!n_rep || !n_tok || !n_rep_new || n_rep_new == n_rep || !rep_sem || !rep_pos || !anchor_out) return LCA_ERR_INVALID_ARG;
+  if (!qbar_opt) {
+    if (!q_tail_pos || (p->variant == LCA_VARIANT_MLA && !q_tail_sem)) return LCA_ERR_INVALID_ARG;
+    const int n = p->n_summary_q > 0 ? p->n_summary_q : p->group_size;
+    if (q_tail_batch_stride < n) return LCA_ERR_INVALID_ARG;
+    if (!aligned16(q_tail_pos) || (q_tail_sem && !aligned16(q_tail_sem))) return LCA_ERR_MISALIGNED;
+    if (!ws || !aligned16(ws)) return LCA_ERR_INVALID_ARG;
+    if (ws_bytes < update_workspace_bytes(p)) return LCA_ERR_WORKSPACE_TOO_SMALL;
+  }
+  if (!aligned16(rep_sem) || !aligned16(rep_pos)) return LCA_ERR_MISALIGNED;
+  if (paged8_update_smem_bytes(p) > 227u * 1024u) return LCA_ERR_UNSUPPORTED_SHAPE;
+  const double* qbar = nullptr;
+  if (!qbar_opt) {
+    st = update_qbar_launch(p, q_tail_sem, q_tail_pos, q_tail_batch_stride, ws, (cudaStream_t)stream);
+    if (st != LCA_OK) return st;
+    qbar = static_cast<const double*>(ws);
+  }
+  return paged8_update_launch(p, cache, qbar_opt, qbar, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, anchor_out, (cudaStream_t)stream);
+}
+
 int lca_latent_to_value(const void* attn_latent, const void* w_uv, void* out_v, int64_t n_tokens,
                         int32_t n_heads, int32_t d_latent, int32_t d_v, void* stream) {
   if (n_tokens < 0 || n_heads <= 0 || d_latent <= 0 || d_v <= 0) return LCA_ERR_INVALID_ARG;
@@ -446,9 +552,9 @@ int lca_selftest_bounded_wait(int64_t limit_cycles, void* stream) {
 
 int lca_last_device_status(void* stream) {
   const int st = attn_tc_device_status((cudaStream_t)stream);      // synchronises the stream
-  const int cst = condense_take_status(), ust = latent_to_value_take_status();
-  if (cst < 0 || ust < 0) return LCA_ERR_CUDA;
-  if (cst > 0 || ust > 0) return LCA_ERR_DEVICE_TIMEOUT;
+  const int cst = condense_take_status(), ust = latent_to_value_take_status(), pst = attn_paged8_take_status();
+  if (cst < 0 || ust < 0 || pst < 0) return LCA_ERR_CUDA;
+  if (cst > 0 || ust > 0 || pst > 0) return LCA_ERR_DEVICE_TIMEOUT;
   return st;
 }
 

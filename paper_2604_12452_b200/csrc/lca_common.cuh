@@ -174,4 +174,44 @@ int latent_to_value_launch(const void* latent, const void* w_uv, void* out, long
                            int d_latent, int d_v, cudaStream_t stream);
 int latent_to_value_take_status();
 
+// ---- paged 8-bit cache ----------------------------------------------------------------------
+// Which rows of a sequence's row space are present: [0, n_rep) and [tok0, n_tok), tok0 = n_rep * g, all below the
+// capacity of the table.  Counters come from the device and are clamped here.
+struct PagedSpan {
+  int n_rep, tok0, n_tok;
+  __device__ __forceinline__ bool has(int x) const { return x < n_rep || (x >= tok0 && x < n_tok); }
+  // any present row in [x, x + n)
+  __device__ __forceinline__ bool any(int x, int n) const { return x < n_rep || (x + n > tok0 && x < n_tok); }
+};
+__device__ __forceinline__ PagedSpan paged_span(const int32_t* n_rep, const int32_t* n_tok, int b, int g, int cap) {
+  PagedSpan s;
+  s.n_tok = min(max(n_tok[b], 0), cap);
+  s.n_rep = n_rep ? min(max(n_rep[b], 0), s.n_tok) : 0;
+  s.tok0 = (int)min((long long)s.n_rep * g, (long long)cap);
+  return s;
+}
+int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* n_rep, const int32_t* n_tok, int32_t* held_rep,
+                       int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map, int n_rows, int rows_per_seq,
+                       int32_t* row_offsets, int32_t* status, cudaStream_t stream);
+int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* rows_sem, const void* rows_pos,
+                        const int32_t* slot_map, long long n_rows, cudaStream_t stream);
+size_t paged8_update_smem_bytes(const lca_params* p);
+int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
+                         const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,
+                         cudaStream_t stream);
+// summary query of the last queries as fp64 at the start of `ws` (update_workspace_bytes)
+int update_qbar_launch(const lca_params* p, const void* q_tail_sem, const void* q_tail_pos, int64_t q_tail_batch_stride,
+                       void* ws, cudaStream_t stream);
+struct Paged8Attn {
+  const lca_params* p; const lca_paged8* c;
+  const void* q_sem; const void* q_pos; int q_len;
+  const int32_t* n_rep; const int32_t* n_tok;
+  void* out; float* lse;
+  void* ws; cudaStream_t stream;
+};
+size_t attn_paged8_workspace_bytes(const lca_params* p, int q_len);
+int attn_paged8_launch(const Paged8Attn& a);           // tensor-core kernel
+int attn_paged8_simt_launch(const Paged8Attn& a);      // scalar kernel
+int attn_paged8_take_status();
+
 }  // namespace lca

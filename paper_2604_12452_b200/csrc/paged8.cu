@@ -1,0 +1,499 @@
+// The paged 8-bit cache around its attention: page tables and slot maps from request lengths, the quantising write and
+// the online condensation of a group.  The row space, the pages and the scales are described in lca.h.
+#include "lca_common.cuh"
+#include "fp8_common.cuh"
+
+namespace lca {
+
+// ------------------------------------------------------------------------------------------------ page tables, slots
+// One cluster does everything, in four phases with a cluster barrier between them, so that a decode step costs one
+// launch: (1) every CTA sums pages to give back, pages to take and new rows over all sequences (a few hundred bytes to
+// a few hundred KB from L2) and decides whether the update is possible; (2) pages that no present row needs are pushed
+// on the free stack; (3) pages are popped into the tables; (4) the slot of every new row is looked up.  A sequence's
+// share of each list starts at an exclusive prefix sum, so the result does not depend on how the work is spread.
+// Bound by latency (three dependent passes over the counters), not by its few bytes.
+struct PageArgs {
+  const int32_t* n_rep; const int32_t* n_tok;
+  int32_t* held_rep; int32_t* held_tok;
+  int32_t* table; int32_t* free_pages; int32_t* n_free; int32_t* slot_map; int32_t* row_offsets; int32_t* status;
+  int B, g, page, width, n_pages, n_rows, per_seq;
+};
+
+// What one sequence gives back and takes: up to three ranges of table entries each, ascending and disjoint.
+struct PageDelta {
+  int rel_lo[3], rel_hi[3], need_lo[3], need_hi[3];
+  int r0, r1, tok_first, n_tok;     // new rows: [r0, r1) and [tok_first, n_tok)
+  bool valid;
+  __device__ __forceinline__ int n_rel() const { int s = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s += max(rel_hi[i] - rel_lo[i], 0);
+    return s; }
+  __device__ __forceinline__ int n_need() const { int s = 0;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s += max(need_hi[i] - need_lo[i], 0);
+    return s; }
+  __device__ __forceinline__ int n_rows() const { return max(r1 - r0, 0) + max(n_tok - tok_first, 0); }
+};
+
+__device__ __forceinline__ PageDelta page_delta(const PageArgs& a, int b) {
+  PageDelta d;
+  const long long r0 = a.n_rep ? a.held_rep[b] : 0, r1 = a.n_rep ? a.n_rep[b] : 0, t0 = a.held_tok[b], t1 = a.n_tok[b];
+  const long long P = a.page, cap = (long long)a.width * P, g = a.g;
+  d.valid = r0 >= 0 && r1 >= 0 && r0 * g <= t0 && r1 * g <= t1 && t0 <= cap && t1 <= cap && (r1 >= r0 || t1 == 0);
+  if (!d.valid) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) d.rel_lo[i] = d.rel_hi[i] = d.need_lo[i] = d.need_hi[i] = 0;
+    d.r0 = d.r1 = d.tok_first = d.n_tok = 0;
+    return d;
+  }
+  // pages held [0, a0) and [b0, c0), wanted [0, a1) and [b1, c1); a <= b <= c because representatives need no more pages
+  // than the tokens they stand for (page | group)
+  const int a0 = (int)((r0 + P - 1) / P), b0 = (int)(r0 * g / P), c0 = (int)((t0 + P - 1) / P);
+  const int a1 = (int)((r1 + P - 1) / P), b1 = (int)(r1 * g / P), c1 = (int)((t1 + P - 1) / P);
+  d.rel_lo[0] = a1;                          d.rel_hi[0] = a0;              // end of a request
+  d.rel_lo[1] = max(b0, a1);                 d.rel_hi[1] = min(c0, b1);     // tokens condensed meanwhile
+  d.rel_lo[2] = max(max(b0, c1), max(b1, a1)); d.rel_hi[2] = c0;            // tokens taken back
+  d.need_lo[0] = a0;                         d.need_hi[0] = min(a1, b0);    // representatives in front of the held tokens
+  d.need_lo[1] = max(a0, c0);                d.need_hi[1] = a1;             // ... and behind them
+  d.need_lo[2] = max(b1, c0);                d.need_hi[2] = c1;             // new tokens
+  d.r0 = (int)r0; d.r1 = (int)r1;
+  d.tok_first = (int)max(t0, r1 * g); d.n_tok = (int)t1;
+  return d;
+}
+
+static const int PAGE_THREADS = 512;
+
+// Exclusive prefix sums over the CTA of three counters; totals in the last three words of `sums`.
+__device__ __forceinline__ void scan3(long long (&v)[3], long long (&excl)[3], long long (&total)[3], long long (*sums)[3]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = PAGE_THREADS / 32;
+  long long inc[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    long long x = v[k];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+    inc[k] = x;
+    if (lane == 31) sums[warp][k] = x;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < 3; ++k) {
+    long long before = 0, all = 0;
+    for (int w = 0; w < nw; ++w) { const long long s = sums[w][k]; if (w < warp) before += s; all += s; }
+    excl[k] = before + inc[k] - v[k];
+    total[k] = all;
+  }
+  __syncthreads();
+}
+
+__device__ __forceinline__ void cluster_barrier() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+__global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
+  __shared__ long long sums[PAGE_THREADS / 32][3];
+  __shared__ int s_rel[PAGE_THREADS], s_need[PAGE_THREADS];
+  const int cta = blockIdx.x, n_cta = gridDim.x;            // the grid is one cluster
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = PAGE_THREADS / 32;
+  // (1) totals
+  long long tot[3] = {0, 0, 0};
+  int bad = 0;
+  {
+    long long mine[3] = {0, 0, 0};
+    for (int b = tid; b < a.B; b += PAGE_THREADS) {
+      const PageDelta d = page_delta(a, b);
+      bad |= !d.valid;
+      const int nr = d.n_rows();
+      bad |= (a.per_seq > 0 && a.slot_map && nr > a.per_seq) ? 2 : 0;
+      mine[0] += d.n_rel(); mine[1] += d.n_need(); mine[2] += nr;
+    }
+    long long ex[3];
+    scan3(mine, ex, tot, sums);
+  }
+  const int any_invalid = __syncthreads_or(bad & 1), any_long = __syncthreads_or(bad & 2);
+  const long long n_free = a.n_free[0], have = n_free + tot[0];
+  int status = 0;
+  if (any_invalid || n_free < 0 || have > a.n_pages) status = -1;
+  else if (any_long || (a.slot_map && a.per_seq == 0 && tot[2] > a.n_rows)) status = -2;
+  else if (tot[1] > have) status = (int)min(tot[1] - have, 0x7fffffffll);
+  const long long gtid = (long long)cta * PAGE_THREADS + tid, gthreads = (long long)n_cta * PAGE_THREADS;
+  if (status != 0) {                                         // nothing changes
+    for (long long i = gtid; i < a.n_rows; i += gthreads) a.slot_map[i] = -1;
+    if (a.row_offsets) for (long long i = gtid; i <= a.B; i += gthreads) a.row_offsets[i] = 0;
+    if (gtid == 0) a.status[0] = status;
+    return;                                                  // every CTA takes this branch or none
+  }
+  // (2) and (3): the sequences of a chunk share out over the warps of the cluster, 32 entries at a time
+  for (int phase = 0; phase < 2; ++phase) {
+    long long base[3] = {0, 0, 0};
+    if (phase == 0 ? tot[0] > 0 || a.row_offsets : tot[1] > 0)
+      for (int c0 = 0; c0 < a.B; c0 += PAGE_THREADS) {
+        const int b = c0 + tid;
+        long long v[3] = {0, 0, 0}, ex[3], chunk[3];
+        if (b < a.B) { const PageDelta d = page_delta(a, b); v[0] = d.n_rel(); v[1] = d.n_need(); v[2] = d.n_rows(); }
+        scan3(v, ex, chunk, sums);
+        if (phase == 0 && cta == 0 && a.row_offsets && b < a.B) {
+          if (b == 0) a.row_offsets[0] = 0;
+          a.row_offsets[b + 1] = (int32_t)min(base[2] + ex[2] + v[2], 0x7fffffffll);
+        }
+        s_rel[tid] = (int)(base[0] + ex[0]); s_need[tid] = (int)(base[1] + ex[1]);
+        __syncthreads();
+        for (int i = cta * n_warps + warp; i < PAGE_THREADS && c0 + i < a.B; i += n_cta * n_warps) {
+          const PageDelta d = page_delta(a, c0 + i);
+          int32_t* row = a.table + (size_t)(c0 + i) * a.width;
+          long long rank = phase == 0 ? s_rel[i] : s_need[i];
+#pragma unroll
+          for (int k = 0; k < 3; ++k) {
+            const int lo = phase == 0 ? d.rel_lo[k] : d.need_lo[k], hi = phase == 0 ? d.rel_hi[k] : d.need_hi[k];
+            for (int e = lo + lane; e < hi; e += 32) {
+              const long long r = rank + (e - lo);
+              if (phase == 0) { a.free_pages[have - 1 - r] = row[e]; row[e] = -1; }
+              else row[e] = a.free_pages[have - 1 - r];
+            }
+            rank += max(hi - lo, 0);
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k) base[k] += chunk[k];
+        __syncthreads();
+      }
+    cluster_barrier();
+  }
+  // (4) slots
+  if (a.slot_map)
+    for (long long i = gtid; i < a.n_rows; i += gthreads) {
+      int b = -1;
+      long long k = 0;
+      if (a.per_seq > 0) { b = (int)(i / a.per_seq); k = i % a.per_seq; }
+      else if (i < tot[2]) { b = seq_of(a.row_offsets, a.B, i); k = i - a.row_offsets[b]; }
+      int slot = -1;
+      if (b >= 0) {
+        const PageDelta d = page_delta(a, b);
+        const int reps = max(d.r1 - d.r0, 0);
+        if (k < d.n_rows()) {
+          const int x = k < reps ? d.r0 + (int)k : d.tok_first + (int)k - reps;
+          const int page = a.table[(size_t)b * a.width + x / a.page];
+          if (page >= 0 && page < a.n_pages) slot = page * a.page + x % a.page;
+        }
+      }
+      a.slot_map[i] = slot;
+    }
+  cluster_barrier();                                         // the held state is read until here
+  for (long long b = gtid; b < a.B; b += gthreads) {
+    a.held_tok[b] = a.n_tok[b];
+    if (a.n_rep) a.held_rep[b] = a.n_rep[b];
+  }
+  if (gtid == 0) { a.n_free[0] = (int32_t)(have - tot[1]); a.status[0] = 0; }
+}
+
+int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* n_rep, const int32_t* n_tok, int32_t* held_rep,
+                       int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map, int n_rows, int rows_per_seq,
+                       int32_t* row_offsets, int32_t* status, cudaStream_t stream) {
+  PageArgs a = {n_rep, n_tok, held_rep, held_tok, c->block_table, free_pages, n_free, slot_map, row_offsets, status,
+                p->batch, n_rep ? p->group_size : 1, c->page_size, c->table_width, c->n_pages, slot_map ? n_rows : 0, rows_per_seq};
+  cudaLaunchConfig_t cfg = {};
+  // one CTA for the few rows of a decode step (its barriers cost least), the largest portable cluster for prompts
+  cfg.gridDim = dim3((p->batch > 512 || a.n_rows > 4096 || n_rows == 0) ? 8 : 1);
+  cfg.blockDim = dim3(PAGE_THREADS);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = cfg.gridDim.x; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, page_update_kernel, a) != cudaSuccess) return LCA_ERR_CUDA;
+  note_launch();
+  return LCA_OK;
+}
+
+// ------------------------------------------------------------------------------------------------------------- write
+// One CTA per run of rows inside a page and per block (GQA: K or V of one KV head; MLA: latent and rope key together).
+// The rows of a run (at most a page) stay in registers between the maximum and the rounding, so the input is read once.
+// HBM-bound: 2 bytes in, 1 byte out per element.
+struct WriteArgs {
+  const bf16* rows_sem; const bf16* rows_pos; const int32_t* slots;
+  uint8_t* pages_sem; uint8_t* pages_pos; float* scale_sem; float* scale_pos;
+  long long n_rows, n_slots;
+  int Hkv, window;           // rows per CTA that may start a run
+};
+
+// log2 of the scale for a block whose largest finite |x| has these bf16 bits: smallest e with |x| <= 448 * 2^e
+__device__ __forceinline__ int scale_exponent(uint32_t bits) {
+  const int E = (int)(bits >> 7), M = (int)(bits & 0x7f);
+  const int e = E - 127 - 8 + (M > 96 ? 1 : 0);              // 448 = 1.75 * 2^8, 1.75 = 1 + 96 / 128
+  return max(E == 0 ? -1000 : e, PAGED8_MIN_EXP);
+}
+
+template <int D_SEM, int D_POS, bool MLA, int P>
+__global__ void __launch_bounds__(256) paged8_write_kernel(WriteArgs a) {
+  constexpr int NT = 256, DROW = MLA ? D_SEM + D_POS : D_SEM, V8 = DROW / 8, NV = (P * V8 + NT - 1) / NT;
+  static_assert(MLA || D_SEM == D_POS, "K and V of one width");
+  __shared__ uint32_t s_red[NT / 32];
+  __shared__ int s_head[4];                                   // bit mask of the run heads of this window (window <= 128)
+  constexpr int PARTS = MLA ? 1 : 2;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int part = (int)(blockIdx.x % PARTS);
+  const int hk = (int)((blockIdx.x / PARTS) % a.Hkv);
+  const long long i0 = (long long)(blockIdx.x / ((unsigned)PARTS * a.Hkv)) * a.window;
+  const bf16* src_sem = part == 0 ? a.rows_sem : a.rows_pos;
+  uint8_t* dst_sem = part == 0 ? a.pages_sem : a.pages_pos;
+  float* scale = part == 0 ? a.scale_sem : a.scale_pos;
+  // a row starts a run unless it follows its predecessor inside the same page
+  if (tid < 128) {
+    const long long i = i0 + tid;
+    bool head = false;
+    if (tid < a.window && i < a.n_rows) {
+      const int s = a.slots[i], prev = i > 0 ? a.slots[i - 1] : -1;
+      head = s >= 0 && s < a.n_slots && !(prev >= 0 && s == prev + 1 && s % P != 0);
+    }
+    const unsigned m = __ballot_sync(0xffffffffu, head);
+    if (lane == 0) s_head[warp] = (int)m;
+  }
+  __syncthreads();
+  for (int w = 0; w < 4; ++w)
+    for (unsigned m = (unsigned)s_head[w]; m; m &= m - 1) {
+      const long long i = i0 + 32 * w + __ffs((int)m) - 1;
+      const int slot = a.slots[i], page = slot / P, off = slot % P;
+      // length of the run: every warp finds it by itself
+      int n = 0;
+#pragma unroll
+      for (int k = 0; k < P; k += 32) {
+        const int j = k + lane;
+        const bool in = j < P - off && i + j < a.n_rows && a.slots[i + j] == slot + j;
+        const unsigned ok = __ballot_sync(0xffffffffu, in);
+        n += ok == 0xffffffffu ? 32 : __ffs((int)~ok) - 1;
+        if (ok != 0xffffffffu) break;
+      }
+      const size_t block = (size_t)page * a.Hkv + hk;
+      const float old = off > 0 ? scale[block] : 0.f;
+      uint4 v[NV];
+      uint32_t top = 0;                                       // largest |x| of a finite element, as bf16 bits
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        const int x = q * NT + tid, r = x / V8, c = x % V8;
+        v[q] = make_uint4(0u, 0u, 0u, 0u);
+        if (x < n * V8) {
+          const size_t row = (size_t)(i + r) * a.Hkv + hk;
+          const bf16* src = (!MLA || c < D_SEM / 8) ? src_sem + row * D_SEM + 8 * c : a.rows_pos + row * D_POS + 8 * (c - D_SEM / 8);
+          v[q] = __ldcs(reinterpret_cast<const uint4*>(src));
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
+          top = max(top, lo < 0x7f80u ? lo : 0u);
+          top = max(top, hi < 0x7f80u ? hi : 0u);
+        }
+      }
+      top = __reduce_max_sync(0xffffffffu, top);
+      if (lane == 0) s_red[warp] = top;
+      __syncthreads();                                        // also: every thread has read the block's old scale
+#pragma unroll
+      for (int k = 0; k < NT / 32; ++k) top = max(top, s_red[k]);
+      const float want = exp2_int(scale_exponent(top));
+      const float now = off > 0 ? fmaxf(want, old) : want;
+      if (off > 0 && now > old) {                             // the block's scale grows: its rows are rounded again
+        const float f = old / now;
+        for (int x = tid; x < off * (DROW / 16); x += NT) {
+          const int r = x / (DROW / 16), c = x % (DROW / 16);
+          uint8_t* q = (!MLA || c < D_SEM / 16) ? dst_sem + (block * P + r) * D_SEM + 16 * c
+                                                : a.pages_pos + (block * P + r) * D_POS + 16 * (c - D_SEM / 16);
+          uint4 w4 = *reinterpret_cast<const uint4*>(q);
+          w4.x = e4m3x4_scale(w4.x, f); w4.y = e4m3x4_scale(w4.y, f); w4.z = e4m3x4_scale(w4.z, f); w4.w = e4m3x4_scale(w4.w, f);
+          *reinterpret_cast<uint4*>(q) = w4;
+        }
+      }
+      const float inv = 1.f / now;                            // exact: a power of two (unless `old` came from elsewhere)
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        const int x = q * NT + tid, r = x / V8, c = x % V8;
+        if (x < n * V8) {
+          uint2 o;
+          o.x = e4m3x4_from_bf16(v[q].x, v[q].y, inv);
+          o.y = e4m3x4_from_bf16(v[q].z, v[q].w, inv);
+          uint8_t* dst = (!MLA || c < D_SEM / 8) ? dst_sem + (block * P + off + r) * D_SEM + 8 * c
+                                                 : a.pages_pos + (block * P + off + r) * D_POS + 8 * (c - D_SEM / 8);
+          *reinterpret_cast<uint2*>(dst) = o;
+        }
+      }
+      if (tid == 0) scale[block] = now;
+      __syncthreads();                                        // s_red is used again by the next run
+    }
+}
+
+template <int D_SEM, int D_POS, bool MLA>
+static int write_page_size(const WriteArgs& a, int page, unsigned grid, cudaStream_t stream) {
+  switch (page) {
+    case 16: paged8_write_kernel<D_SEM, D_POS, MLA, 16><<<grid, 256, 0, stream>>>(a); break;
+    case 32: paged8_write_kernel<D_SEM, D_POS, MLA, 32><<<grid, 256, 0, stream>>>(a); break;
+    case 64: paged8_write_kernel<D_SEM, D_POS, MLA, 64><<<grid, 256, 0, stream>>>(a); break;
+    default: paged8_write_kernel<D_SEM, D_POS, MLA, 128><<<grid, 256, 0, stream>>>(a); break;
+  }
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+
+int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* rows_sem, const void* rows_pos,
+                        const int32_t* slot_map, long long n_rows, cudaStream_t stream) {
+  const bool mla = p->variant == LCA_VARIANT_MLA;
+  const long long blocks = (long long)p->n_kv_heads * (mla ? 1 : 2);
+  WriteArgs a = {(const bf16*)rows_sem, (const bf16*)rows_pos, slot_map, (uint8_t*)c->pages_sem, (uint8_t*)c->pages_pos, c->scale_sem,
+                 c->scale_pos, n_rows, (long long)c->n_pages * c->page_size, p->n_kv_heads, 1};
+  // A decode step brings one row per page: one CTA per row, or a CTA would handle its runs one after the other.  A prompt
+  // brings whole pages: one CTA per page of rows, or most CTAs would find no run to start.
+  const long long per = n_rows * blocks / (148 * 8);
+  a.window = (int)(per < 1 ? 1 : (per > c->page_size ? c->page_size : per));
+  const long long grid = (n_rows + a.window - 1) / a.window * blocks;
+  if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if (mla) return p->d_sem == 512 ? write_page_size<512, 64, true>(a, c->page_size, (unsigned)grid, stream)
+                                  : write_page_size<128, 64, true>(a, c->page_size, (unsigned)grid, stream);
+  return p->d_sem == 128 ? write_page_size<128, 128, false>(a, c->page_size, (unsigned)grid, stream)
+                         : write_page_size<64, 64, false>(a, c->page_size, (unsigned)grid, stream);
+}
+
+// ------------------------------------------------------------------------------------------------------------ update
+// Condensation of the earliest group of every sequence that is due (Sec. 4.2 / 4.3) from the 8-bit values: fp64 scores,
+// arg-max on them (lowest index on ties), fp32 softmax and pooling, one rounding to bf16.  One CTA per (sequence, KV
+// head): the group (g rows of codes) is brought to shared memory once.  A launch of a few dozen CTAs that read 37 KB
+// each (g = 64, 576 wide): bound by latency.
+struct Update8Args {
+  const uint8_t* pages_sem; const uint8_t* pages_pos; const float* scale_sem; const float* scale_pos; const int32_t* table;
+  const float* qbar_f; const double* qbar_d;
+  const int32_t* n_rep; const int32_t* n_tok; int32_t* n_rep_new;
+  bf16* rep_sem; bf16* rep_pos; int32_t* anchor;
+  int Hkv, d_sem, d_pos, g, w, page, n_pages, width, mla;
+  double scale;
+};
+static const int UPD_THREADS = 512;
+
+__global__ void __launch_bounds__(UPD_THREADS) paged8_update_kernel(Update8Args a) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  const int hk = (int)(blockIdx.x % a.Hkv), b = (int)(blockIdx.x / a.Hkv);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = UPD_THREADS / 32;
+  const int g = a.g, dk = (a.mla ? a.d_sem : 0) + a.d_pos;
+  double* s_q = reinterpret_cast<double*>(smem_raw);
+  double* s_s = s_q + dk;
+  float* s_a = reinterpret_cast<float*>(s_s + g);
+  float* s_fs = s_a + g;                                     // scale of each row's sem / pos codes
+  float* s_fp = s_fs + g;
+  int* s_page = reinterpret_cast<int*>(s_fp + g);
+  uint8_t* t_sem = reinterpret_cast<uint8_t*>(s_page + g);   // 16-byte aligned: dk, g multiples of 8 and of 16
+  uint8_t* t_pos = t_sem + (size_t)g * a.d_sem;
+  __shared__ int s_anchor;
+  const int nr = a.n_rep[b], nt = a.n_tok[b];
+  const long long first = (long long)nr * g, cap = (long long)a.width * a.page;
+  bool due = nr >= 0 && nt >= 0 && nt <= cap && (long long)nt - first >= (long long)a.w + g;
+  int missing = 0;
+  if (due)
+    for (int i = tid; i < g; i += UPD_THREADS) {
+      const long long x = first + i;
+      const int pg = a.table[(size_t)b * a.width + x / a.page];
+      if (pg < 0 || pg >= a.n_pages) missing = 1;
+      else {
+        s_page[i] = pg;
+        s_fs[i] = a.scale_sem[(size_t)pg * a.Hkv + hk];
+        s_fp[i] = a.scale_pos ? a.scale_pos[(size_t)pg * a.Hkv + hk] : s_fs[i];
+      }
+    }
+  due = due && !__syncthreads_or(missing);
+  if (hk == 0 && tid == 0) a.n_rep_new[b] = nr + (due ? 1 : 0);
+  if (!due) {
+    if (tid == 0) a.anchor[b * a.Hkv + hk] = -1;
+    return;
+  }
+  const int x0 = (int)first;
+  const int cs = a.d_sem / 16, cp = a.d_pos / 16;
+  for (int x = tid; x < g * cs; x += UPD_THREADS) {
+    const int i = x / cs, c = x % cs;
+    reinterpret_cast<uint4*>(t_sem)[x] =
+        reinterpret_cast<const uint4*>(a.pages_sem + (((size_t)s_page[i] * a.Hkv + hk) * a.page + (x0 + i) % a.page) * a.d_sem)[c];
+  }
+  for (int x = tid; x < g * cp; x += UPD_THREADS) {
+    const int i = x / cp, c = x % cp;
+    reinterpret_cast<uint4*>(t_pos)[x] =
+        reinterpret_cast<const uint4*>(a.pages_pos + (((size_t)s_page[i] * a.Hkv + hk) * a.page + (x0 + i) % a.page) * a.d_pos)[c];
+  }
+  const size_t q0 = ((size_t)b * a.Hkv + hk) * dk;
+  for (int c = tid; c < dk; c += UPD_THREADS) s_q[c] = a.qbar_f ? (double)a.qbar_f[q0 + c] : a.qbar_d[q0 + c];
+  __syncthreads();
+  const int sem_off = a.mla ? a.d_sem : 0;
+  for (int i = warp; i < g; i += n_warps) {
+    double acc = 0.0;
+    const float fs = s_fs[i], fp = s_fp[i];
+    if (a.mla)
+      for (int c = 4 * lane; c < a.d_sem; c += 128) {
+        const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_sem + (size_t)i * a.d_sem + c));
+        acc = fma(s_q[c], (double)(f.x * fs), acc); acc = fma(s_q[c + 1], (double)(f.y * fs), acc);
+        acc = fma(s_q[c + 2], (double)(f.z * fs), acc); acc = fma(s_q[c + 3], (double)(f.w * fs), acc);
+      }
+    for (int c = 4 * lane; c < a.d_pos; c += 128) {
+      const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_pos + (size_t)i * a.d_pos + c));
+      acc = fma(s_q[sem_off + c], (double)(f.x * fp), acc); acc = fma(s_q[sem_off + c + 1], (double)(f.y * fp), acc);
+      acc = fma(s_q[sem_off + c + 2], (double)(f.z * fp), acc); acc = fma(s_q[sem_off + c + 3], (double)(f.w * fp), acc);
+    }
+    acc = warp_sum(acc);
+    if (lane == 0) s_s[i] = acc * a.scale;
+  }
+  __syncthreads();
+  if (warp == 0) {
+    double best = -INFINITY;
+    int besti = 0x7fffffff;
+    for (int i = lane; i < g; i += 32) { const double v = s_s[i]; if (v > best) { best = v; besti = i; } }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      const double ob = __shfl_xor_sync(0xffffffffu, best, o);
+      const int oi = __shfl_xor_sync(0xffffffffu, besti, o);
+      if (ob > best || (ob == best && oi < besti)) { best = ob; besti = oi; }
+    }
+    float z = 0.f;
+    for (int i = lane; i < g; i += 32) { const float e = expf((float)(s_s[i] - best)); s_a[i] = e; z += e; }
+    z = warp_sum(z);
+    const float inv = 1.f / z;
+    for (int i = lane; i < g; i += 32) s_a[i] *= inv;
+    if (lane == 0) s_anchor = min(besti, g - 1);             // no finite score at all (NaN): the last token
+  }
+  __syncthreads();
+  const size_t o = (size_t)b * a.Hkv + hk;
+  for (int c = 4 * tid; c < a.d_sem; c += 4 * UPD_THREADS) {
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = 0; i < g; ++i) {
+      const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_sem + (size_t)i * a.d_sem + c));
+      const float fs = s_fs[i], w = s_a[i];
+      acc.x = fmaf(w, f.x * fs, acc.x); acc.y = fmaf(w, f.y * fs, acc.y); acc.z = fmaf(w, f.z * fs, acc.z); acc.w = fmaf(w, f.w * fs, acc.w);
+    }
+    bf16* dst = a.rep_sem + o * a.d_sem + c;
+    dst[0] = __float2bfloat16_rn(acc.x); dst[1] = __float2bfloat16_rn(acc.y); dst[2] = __float2bfloat16_rn(acc.z); dst[3] = __float2bfloat16_rn(acc.w);
+  }
+  const int ia = s_anchor;
+  for (int c = 4 * tid; c < a.d_pos; c += 4 * UPD_THREADS) {
+    const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_pos + (size_t)ia * a.d_pos + c));
+    const float fp = s_fp[ia];
+    bf16* dst = a.rep_pos + o * a.d_pos + c;
+    dst[0] = __float2bfloat16_rn(f.x * fp); dst[1] = __float2bfloat16_rn(f.y * fp); dst[2] = __float2bfloat16_rn(f.z * fp); dst[3] = __float2bfloat16_rn(f.w * fp);
+  }
+  if (tid == 0) a.anchor[o] = ia;
+}
+
+size_t paged8_update_smem_bytes(const lca_params* p) {
+  const size_t g = (size_t)p->group_size, dk = (size_t)(p->variant == LCA_VARIANT_MLA ? p->d_sem : 0) + p->d_pos;
+  return dk * sizeof(double) + g * (sizeof(double) + 3 * sizeof(float) + sizeof(int)) + g * (size_t)(p->d_sem + p->d_pos);
+}
+
+int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
+                         const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,
+                         cudaStream_t stream) {
+  Update8Args a = {(const uint8_t*)c->pages_sem, (const uint8_t*)c->pages_pos, c->scale_sem, c->scale_pos, c->block_table, qbar_f, qbar_d,
+                   n_rep, n_tok, n_rep_new, (bf16*)rep_sem, (bf16*)rep_pos, anchor_out, p->n_kv_heads, p->d_sem, p->d_pos, p->group_size,
+                   p->window, c->page_size, c->n_pages, c->table_width, p->variant == LCA_VARIANT_MLA, (double)p->softmax_scale};
+  const long long grid = (long long)p->batch * p->n_kv_heads;
+  if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
+  const size_t smem = paged8_update_smem_bytes(p);
+  if (cudaFuncSetAttribute(paged8_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return LCA_ERR_CUDA;
+  paged8_update_kernel<<<(unsigned)grid, UPD_THREADS, smem, stream>>>(a);
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+
+}  // namespace lca
