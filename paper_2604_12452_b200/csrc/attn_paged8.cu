@@ -116,9 +116,11 @@ int attn_paged8_simt_launch(const Paged8Attn& q) {
 // tile is the 128-row operand whatever the number of heads, a row of K or V is read by the tensor core as it lies in the
 // page (K-major for S, MN-major for O: no transposition, no conversion) and a softmax thread owns one key: scale, mask and
 // bias are one value per thread.  NH (16, 32 or 64) query rows of one KV head share a tile.
-//   warps 0-3  softmax: thread = key = TMEM lane; epilogue: thread = output column d
-//   warp 4     TMA: 128-byte-wide chunks (16 KB) of the 128 rows of a tile, one request per page
-//   warp 5     MMA issue and TMEM
+//   softmax    NH / 16 groups of four warps, each for 16 of the rows: thread = key = TMEM lane; epilogue: thread = output
+//              column d.  Sixteen rows a thread keep the unrolled code within the instruction cache (one group of 64 rows spent
+//              most of its time fetching instructions: 243 us instead of 150 at 64 x 5056 rows, 128 heads).
+//   + 1 warp   TMA: 128-byte-wide chunks (16 KB) of the 128 rows of a tile, one request per page
+//   + 1 warp   MMA issue and TMEM
 // The chunks of a tile are consumed as K_0.. then V_0..; S of tile j+1 is issued before O of tile j, and the one ring of
 // slots is filled in exactly that order: K(0) K(1) V(0) K(2) V(1) ...  For MLA a latent chunk passes twice (the second
 // time out of L2): keeping it from S to O would need two whole tiles of slots.
@@ -137,8 +139,9 @@ struct Paged8Plan {
   static constexpr int TM_S = NV * NH, TM_USED = TM_S + 4 * NH;
   static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
   static constexpr int CTAS = (MLA && DS == 512) || TM_COLS == 512 ? 1 : 2;        // per SM
-  // floats: qs, M, d, factor, lim [NH]; wmax, lsum [4][NH].  Barriers first.
-  static constexpr int MISC_BYTES = 512 + 4 * (5 * NH + 8 * NH);
+  static constexpr int GROUPS = NH / 16, SOFTMAX_WARPS = 4 * GROUPS, THREADS = 32 * (SOFTMAX_WARPS + 2);
+  // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers first.
+  static constexpr int MISC_BYTES = 512 + 4 * (5 * NH + 4 * NH + 2 * NH);
   static constexpr int BUDGET = (CTAS == 1 ? 227 * 1024 : 113 * 1024) - 1024;      // 1 KB to align the base
   static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / SLOT;
   static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
@@ -155,7 +158,7 @@ struct Paged8Params {
   bf16* out; float* lse;
   float* part;                // [2 * CTAs][NH][DS] partial O, then [2 * CTAs][2][NH] M and l
   long long* prefix;          // [B + 1] tiles before each sequence (all units), written by CTA 0
-  int B, Hq, Hkv, q_len, g, page, n_pages, width, rep, n_blk, min_tiles, grid;
+  int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, min_tiles, grid;
   float scale_log2, bias_log2;
 };
 
@@ -246,22 +249,22 @@ __device__ __forceinline__ float warp_max_f32(float v) {
 }
 __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 __device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ void softmax_barrier() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
-__device__ __forceinline__ bool softmax_any(bool v) {
+// one group of softmax warps (128 threads)
+__device__ __forceinline__ void group_barrier(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); }
+__device__ __forceinline__ bool group_any(int grp, bool v) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((uint32_t)v) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((uint32_t)v), "r"(grp + 1) : "memory");
   return r != 0;
 }
 
-static constexpr int PAGED8_THREADS = 192;
 static constexpr float PAGED8_T_BITS = 8.f;         // the largest weight is 2^8 ...
 static constexpr float PAGED8_SLACK = 3.f;          // ... and may reach 2^11 before the maximum is raised: t_hi up to 2^11
                                                     // leaves at most 2^8 to t_lo (e4m3 ends at 448)
 
 template <class PL>
-__global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
-  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP;
+__global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
+  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, W_TMA = PL::SOFTMAX_WARPS, W_MMA = W_TMA + 1;
   extern __shared__ unsigned char smem_dyn[];
   const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
   unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
@@ -274,26 +277,27 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
   int* s_b = reinterpret_cast<int*>(misc + 264);
   long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
-  long long* s_warp = reinterpret_cast<long long*>(misc + 288);         // 6 warp totals
+  long long* s_warp = reinterpret_cast<long long*>(misc + 288);         // totals of up to 18 warps
   float* s_qs = reinterpret_cast<float*>(misc + 512);
   float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
   int* s_lim = reinterpret_cast<int*>(s_f + NH);
-  float* s_wmax = reinterpret_cast<float*>(s_lim + NH); float* s_lsum = s_wmax + 4 * NH;
+  float* s_wmax = reinterpret_cast<float*>(s_lim + NH);      // also the sums of the four warps of a group
+  int* s_row = reinterpret_cast<int*>(s_wmax + 4 * NH);      // output row of each query row, of this piece and of the next one
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x;
 
   if (tid == 0) {
     for (int s = 0; s < PL::SLOTS; ++s) { mbar_init(FULL(s), 1); mbar_init(EMPTY(s), 1); }
-    mbar_init(SFULL, 1); mbar_init(SFULL + 8, 1); mbar_init(PFULL, 128); mbar_init(PVDONE, 1); mbar_init(QFULL, 128);
+    mbar_init(SFULL, 1); mbar_init(SFULL + 8, 1); mbar_init(PFULL, 32 * W_TMA); mbar_init(PVDONE, 1); mbar_init(QFULL, 32 * W_TMA);
     *abort_flag = 0;
     fence_mbar_init();
   }
-  if (warp == 5) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
-  if (warp == 4 && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
+  if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
+  if (warp == W_TMA && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
   // this CTA's range of the line: thread i sums the tiles of sequences [i q, (i + 1) q)
   const long long upu = (long long)p.Hkv * p.n_blk;
   long long s0 = 0;
   {
-    const int q = (p.B + PAGED8_THREADS - 1) / PAGED8_THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
+    const int q = (p.B + PL::THREADS - 1) / PL::THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
     long long sum = 0;
     for (int b = lo; b < hi; ++b) sum += (long long)tile_span(p, b).n * upu;
     long long inc = sum;
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
     long long T = 0, before = inc - sum;
-    for (int w = 0; w < PAGED8_THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
+    for (int w = 0; w < PL::THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
     const int G = ctas_used(p, T);
     long long s1 = 0;
     if ((int)blockIdx.x < G) { s0 = (long long)blockIdx.x * T / G; s1 = ((long long)blockIdx.x + 1) * T / G; }
@@ -330,7 +334,7 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
   w.b = *s_b; w.off = s_off[0]; w.left = s_off[1]; w.fresh = true; w.n = 0;
   auto fail = [&](int code) { atomicCAS(&g_paged8_status, 0, code); *abort_flag = 1; };
 
-  if (warp == 4) {
+  if (warp == W_TMA) {
     // ------------------------------------------------------------------------------------------------ producer
     int slot = 0;
     uint32_t phase = 0;
@@ -344,8 +348,8 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
         const int nowhere = p.n_pages * p.Hkv;
         if (i >= w.n || lane >= npp) return nowhere;
         const int x = w.t.row0(w.t0 + i) + lane * p.page;
-        if (!sp.any(x, p.page) || x / p.page >= p.width) return nowhere;
-        const int pg = table[x / p.page];
+        if (!sp.any(x, p.page) || (x >> p.page_log2) >= p.width) return nowhere;
+        const int pg = table[x >> p.page_log2];
         return pg >= 0 && pg < p.n_pages ? pg * p.Hkv + w.hk : nowhere;
       };
       auto load = [&](const CUtensorMap* map, int x, int width, int z) {
@@ -373,7 +377,7 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
         z0 = z1; z1 = z2;
       }
     }
-  } else if (warp == 5) {
+  } else if (warp == W_MMA) {
     // ----------------------------------------------------------------------------------------------------- MMA
     const uint32_t leader = elect_one();
     constexpr uint32_t ID_S = umma_idesc_f8(128, 2 * NH, 0, false, false);
@@ -441,27 +445,28 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
     }
   } else {
     // ------------------------------------------------------------------------------------- softmax, epilogue
-    const uint32_t lane_base = (uint32_t)(warp * 32) << 16;
+    const int grp = warp >> 2, quad = warp & 3, t = tid & 127, hb = 16 * grp;      // this thread: key t of a tile, rows hb .. hb + 15
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const float dither = ((float)(__brev((unsigned)lane) >> 27) + 0.5f) * (1.f / 32.f) * 0.001953125f - 0.0009765625f;   // (-1/2, 1/2) of 2^-9
-    uint32_t g = 0, seg_chunks = 0;
-    bool first = true;
+    uint32_t g = 0, seg = 0, seg_chunks = 0;
     bool ok = true;
-    float l[NH];
-    // splits this unit's query rows into e4m3 terms and writes them where S reads them
-    auto load_q = [&](const Walk& u) {
+    float l[16];
+    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them
+    auto load_q = [&](const Walk& u, uint32_t which) {
       constexpr int VS = PL::KSEM * 16, VQ = VS + DP / 8, NL = (VQ + 31) / 32;   // 8-element vectors of a row
       const int n_rows = p.q_len * p.rep - u.blk * NH;
-      for (int r = warp; r < NH; r += 4) {
-        const int gr = u.blk * NH + r;
+#pragma unroll 2
+      for (int r = hb + quad; r < hb + 16; r += 4) {
+        const int gr = u.blk * NH + r, qt = gr / p.rep;
+        const int row = ((int)(u.b * p.q_len) + qt) * p.Hq + u.hk * p.rep + (gr - qt * p.rep);
         uint4 v[NL];
         uint32_t top = 0;
-        const size_t row = ((size_t)u.b * p.q_len + gr / p.rep) * p.Hq + (size_t)u.hk * p.rep + gr % p.rep;
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
           const int c = lane + 32 * i;
           v[i] = make_uint4(0u, 0u, 0u, 0u);
           if (r < n_rows && c < VQ)
-            v[i] = *reinterpret_cast<const uint4*>(c < VS ? p.q_sem + row * DS + 8 * c : p.q_pos + row * DP + 8 * (c - VS));
+            v[i] = *reinterpret_cast<const uint4*>(c < VS ? p.q_sem + (size_t)row * DS + 8 * c : p.q_pos + (size_t)row * DP + 8 * (c - VS));
         }
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
@@ -497,34 +502,39 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
         if (lane == 0) {
           s_qs[r] = r < n_rows ? (top >= 0x7f80u ? __int_as_float(0x7fffffff) : exp2_int(-e)) : 0.f;
           s_m[r] = r < n_rows ? 0.f : 3.0e38f;
-          s_lim[r] = u.t.s.n_tok - p.q_len + 1 + gr / p.rep;
+          s_lim[r] = u.t.s.n_tok - p.q_len + 1 + qt;
+          s_row[(which & 1) * NH + r] = r < n_rows ? row : -1;
         }
       }
       fence_proxy_async_smem();
       mbar_arrive(QFULL);
-      softmax_barrier();
+      group_barrier(grp);
     };
     bool more = w.next(p);
-    if (more) load_q(w);
+    if (more) load_q(w, 0);
     while (more) {
       const PagedSpan sp = w.t.s;
-      const int n_rows = min(p.q_len * p.rep - w.blk * NH, NH);
       const int32_t* table = p.table + (size_t)w.b * p.width;
-      bool unset = tid < n_rows;                             // thread h: head h has no maximum yet
+      const int* rows = s_row + (seg & 1) * NH + hb;
+      bool unset = t < 16 && rows[t & 15] >= 0;              // thread h of the group: its row has no maximum yet
 #pragma unroll
-      for (int i = 0; i < NH; ++i) l[i] = 0.f;
+      for (int i = 0; i < 16; ++i) l[i] = 0.f;
       auto page_of = [&](int j) {                            // page of this thread's key in tile j, -1: none
         if (j >= w.n) return -1;
-        const int x = w.t.row0(w.t0 + j) + tid;
+        const int x = w.t.row0(w.t0 + j) + t;
         if (!sp.has(x)) return -1;                           // has() implies x below the table's end
-        const int pg = table[x / p.page];
+        const int pg = table[x >> p.page_log2];
         return pg >= 0 && pg < p.n_pages ? pg : -1;
       };
+      // first rows of the (at most two) pages that are present in part; one past every row where there is none
+      const int none = 0x7fffffff, mask = p.page - 1;
+      const int part_r = (sp.n_rep & mask) ? sp.n_rep & ~mask : none, part_t = (sp.n_tok & mask) ? sp.n_tok & ~mask : none;
       int pg0 = page_of(0), pg1 = page_of(1);
       float ks = 0.f, vs = 1.f;
       if (pg0 >= 0) { ks = p.scale_k[(size_t)pg0 * p.Hkv + w.hk]; vs = p.scale_v[(size_t)pg0 * p.Hkv + w.hk]; }
+#pragma unroll 1
       for (int j = 0; j < w.n; ++j, ++g) {
-        const int row0 = w.t.row0(w.t0 + j), x = row0 + tid;
+        const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
         const bool valid = pg0 >= 0;
         // the next tile's scales and the page after that are on their way while this tile is worked on
         float ks1 = 0.f, vs1 = 1.f;
@@ -535,108 +545,99 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
         // between them, so that neither is lost below 2^-126 where the scales of a sequence span more than fp32 does.
         const float half = 0.5f * (lg2(vs) + PAGED8_T_BITS), f_t = ex2(half), f_l = ex2(PAGED8_T_BITS - half);
         const float kf = ks * p.scale_log2, cb = half + (x < sp.n_rep ? p.bias_log2 : 0.f);
-        const bool all_valid = __all_sync(0xffffffffu, valid);
         const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
 
         ok = mbar_wait(SFULL + 8 * (g & 1), (g >> 1) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_S_FULL);
         __syncwarp();
         tc_fence_after();
-        float z[NH];
+        float z[16];
         float zmax = -INFINITY;
-        constexpr int CH = NH < 32 ? NH : 32;
-#pragma unroll
-        for (int h0 = 0; h0 < NH; h0 += CH) {
-          uint32_t hi[CH], lo[CH];
-          const uint32_t at = tmem + lane_base + PL::TM_S + (g & 1) * 2 * NH + h0;
-#pragma unroll
-          for (int i = 0; i < CH; i += 16) { tmem_ld16(at + i, hi + i); tmem_ld16(at + NH + i, lo + i); }
+        {
+          uint32_t hi[16], lo[16];
+          const uint32_t at = tmem + lane_base + PL::TM_S + (g & 1) * 2 * NH + hb;
+          tmem_ld16(at, hi);
+          tmem_ld16(at + NH, lo);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < CH; i += 4) {
-            const float4 q4 = *reinterpret_cast<const float4*>(s_qs + h0 + i), m4 = *reinterpret_cast<const float4*>(s_m + h0 + i);
+          for (int i = 0; i < 16; i += 4) {
+            const float4 q4 = *reinterpret_cast<const float4*>(s_qs + hb + i), m4 = *reinterpret_cast<const float4*>(s_m + hb + i);
             const float qq[4] = {q4.x, q4.y, q4.z, q4.w}, mm[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
             for (int k = 0; k < 4; ++k)
-              z[h0 + i + k] = fmaf(__uint_as_float(hi[i + k]) + __uint_as_float(lo[i + k]), kf * qq[k], cb - mm[k]);
+              z[i + k] = fmaf(__uint_as_float(hi[i + k]) + __uint_as_float(lo[i + k]), kf * qq[k], cb - mm[k]);
           }
         }
-        if (!all_valid || limited) {
+        if (limited || !__all_sync(0xffffffffu, valid)) {
 #pragma unroll
-          for (int i = 0; i < NH; ++i) z[i] = valid && (!limited || x < s_lim[i]) ? z[i] : -INFINITY;
+          for (int i = 0; i < 16; ++i) z[i] = valid && (!limited || x < s_lim[hb + i]) ? z[i] : -INFINITY;
         }
 #pragma unroll
-        for (int i = 0; i < NH; i += 2) zmax = max3(zmax, z[i], z[i + 1]);
-        if (softmax_any(zmax + half > PAGED8_T_BITS + PAGED8_SLACK || unset)) {
-          // raise the maxima: per head the largest log2 t of the tile
+        for (int i = 0; i < 16; i += 2) zmax = max3(zmax, z[i], z[i + 1]);
+        const bool raise = group_any(grp, zmax + half > PAGED8_T_BITS + PAGED8_SLACK || unset);
+        if (raise) {
+          // raise the maxima: per row the largest log2 t of the tile
 #pragma unroll
-          for (int i = 0; i < NH; ++i) {
+          for (int i = 0; i < 16; ++i) {
             const float m = warp_max_f32(z[i] + half);
-            if (lane == (i & 31)) s_wmax[warp * NH + i] = m;
+            if (lane == i) s_wmax[quad * NH + hb + i] = m;
           }
-          softmax_barrier();
-          if (tid < NH) {
-            const float m = fmaxf(fmaxf(s_wmax[tid], s_wmax[NH + tid]), fmaxf(s_wmax[2 * NH + tid], s_wmax[3 * NH + tid]));
+          group_barrier(grp);
+          if (t < 16) {
+            const int h = hb + t;
+            const float m = fmaxf(fmaxf(s_wmax[h], s_wmax[NH + h]), fmaxf(s_wmax[2 * NH + h], s_wmax[3 * NH + h]));
             float d = 0.f, f = 1.f;
             if (unset ? m > -INFINITY : m > PAGED8_T_BITS) {
               d = m - PAGED8_T_BITS;
               f = unset ? 1.f : ex2(-d);                     // nothing has been added under an unset maximum
-              s_m[tid] += d;
+              s_m[h] += d;
               unset = false;
             }
-            s_d[tid] = d; s_f[tid] = f;
+            s_d[h] = d; s_f[h] = f;
           }
-          if (j > 0) {
-            ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag); // O is complete up to the previous tile
-            if (!ok) fail(ERR_WAIT_O_DONE);
-            __syncwarp();
-          }
-          softmax_barrier();
+          group_barrier(grp);
 #pragma unroll
-          for (int i = 0; i < NH; ++i) { z[i] -= s_d[i]; l[i] *= s_f[i]; }
-          if (j > 0) {
+          for (int i = 0; i < 16; ++i) { z[i] -= s_d[hb + i]; l[i] *= s_f[hb + i]; }
+        }
+        if (j > 0) {                                         // the weights of the previous tile have been read, O is complete up to it
+          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
+          if (!ok) fail(ERR_WAIT_O_DONE);
+          __syncwarp();
+          if (raise) {
             tc_fence_after();
 #pragma unroll 1
-            for (int i = 0; i < NV * NH; i += 16) {
+            for (int c = 0; c < NV; ++c) {
               uint32_t o[16];
-              tmem_ld16(tmem + lane_base + i, o);
+              tmem_ld16(tmem + lane_base + c * NH + hb, o);
               tmem_wait_ld();
 #pragma unroll
-              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * s_f[(i + k) % NH]);
-              tmem_st16(tmem + lane_base + i, o);
+              for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * s_f[hb + k]);
+              tmem_st16(tmem + lane_base + c * NH + hb, o);
             }
             tmem_wait_st();
           }
-        } else if (j > 0) {
-          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);   // the weights of the previous tile have been read
-          if (!ok) fail(ERR_WAIT_O_DONE);
-          __syncwarp();
         }
-        unsigned char* ph = base_ptr + PL::OFF_P;
-#pragma unroll
-        for (int h0 = 0; h0 < NH; h0 += 16) {
+        {
           uint32_t wh[4], wl[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float hi[4], lo[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float e = ex2(z[h0 + 4 * i + k]), t = e * f_t;
-              l[h0 + 4 * i + k] = fmaf(e, f_l, l[h0 + 4 * i + k]);
-              hi[k] = __uint_as_float((__float_as_uint(t) + 0x00100000u) & 0xffe00000u);      // three significant bits
-              lo[k] = (t - hi[k]) + dither;
+              const float e = ex2(z[4 * i + k]), tt = e * f_t;
+              l[4 * i + k] = fmaf(e, f_l, l[4 * i + k]);
+              hi[k] = __uint_as_float((__float_as_uint(tt) + 0x00100000u) & 0xffe00000u);     // three significant bits
+              lo[k] = (tt - hi[k]) + dither;
             }
             wh[i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
             wl[i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
           }
-          const uint32_t o = swz<NH>(tid, h0 / 16);
-          *reinterpret_cast<uint4*>(ph + o) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-          *reinterpret_cast<uint4*>(ph + PL::P_BYTES + o) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+          unsigned char* ph = base_ptr + PL::OFF_P + swz<NH>(t, grp);
+          *reinterpret_cast<uint4*>(ph) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+          *reinterpret_cast<uint4*>(ph + PL::P_BYTES) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
         }
         // Rows that were fetched with a page but are not present may hold anything; their weight is 0 and 0 * NaN is not.
-        const int part_r = sp.n_rep % p.page ? sp.n_rep - sp.n_rep % p.page - row0 : -1;
-        const int part_t = sp.n_tok % p.page ? sp.n_tok - sp.n_tok % p.page - row0 : -1;
-        if ((part_r >= 0 && part_r < 128) || (part_t >= 0 && part_t < 128)) {
+        if (grp == 0 && ((unsigned)(part_r - row0) < 128u || (unsigned)(part_t - row0) < 128u)) {
 #pragma unroll 1
           for (int c = 0; c < NV; ++c) {
             const uint32_t at = seg_chunks + (uint32_t)min(j + 2, w.n) * NK + (uint32_t)j * NV + c;      // place in the order of loads
@@ -644,7 +645,7 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
             ok = mbar_wait(FULL(s), (at / PL::SLOTS) & 1, abort_flag);
             if (!ok) fail(ERR_WAIT_KV_FULL);
             if (!valid) {
-              uint4* row = reinterpret_cast<uint4*>(base_ptr + s * PL::SLOT + tid * PL::VW);
+              uint4* row = reinterpret_cast<uint4*>(base_ptr + s * PL::SLOT + t * PL::VW);
 #pragma unroll
               for (int i = 0; i < PL::VW / 16; ++i) row[i] = make_uint4(0u, 0u, 0u, 0u);
             }
@@ -657,64 +658,59 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
         pg0 = pg1; pg1 = pg2; ks = ks1; vs = vs1;
       }
       seg_chunks += (uint32_t)w.n * (NK + NV);
-      // ---- this piece is done: its sums, maxima and row addresses, then the next unit's queries (S of this piece is
-      // complete), then O
+      // ---- this piece is done: its sums and maxima, then the next unit's queries (S of this piece is complete), then O
       const bool whole = w.n == w.t.n;
-      const int b = w.b, hk = w.hk, blk = w.blk;
-      const size_t part = (size_t)2 * blockIdx.x + (first ? 0 : 1);
-      first = false;
-      // sums over the 128 keys: halving exchange inside the warp, then the four warps
+      const size_t part = (size_t)2 * blockIdx.x + (seg == 0 ? 0 : 1);
 #pragma unroll
-      for (int i = 0; i < NH; ++i) {
+      for (int i = 0; i < 16; ++i) {
         float v = l[i];
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-        if (lane == (i & 31)) s_lsum[warp * NH + i] = v;
+        if (lane == i) s_wmax[quad * NH + hb + i] = v;
       }
-      softmax_barrier();
-      if (tid < NH) {
-        const float sum = (s_lsum[tid] + s_lsum[NH + tid]) + (s_lsum[2 * NH + tid] + s_lsum[3 * NH + tid]);
+      group_barrier(grp);
+      if (t < 16) {
+        const int h = hb + t;
+        const float sum = (s_wmax[h] + s_wmax[NH + h]) + (s_wmax[2 * NH + h] + s_wmax[3 * NH + h]);
         if (!whole) {
           float* ml = p.part + (size_t)2 * p.grid * NH * DS + part * 2 * NH;
-          ml[tid] = unset ? -INFINITY : s_m[tid]; ml[NH + tid] = sum;
-        } else if (tid < n_rows) {
-          const int gr = blk * NH + tid;
-          if (p.lse) p.lse[((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep] =
-              sum == 0.f ? -INFINITY : (s_m[tid] + log2f(sum) - PAGED8_T_BITS) * 0.6931471805599453f;
+          ml[h] = unset ? -INFINITY : s_m[h]; ml[NH + h] = sum;
+        } else if (p.lse && rows[t] >= 0) {
+          p.lse[rows[t]] = sum == 0.f ? -INFINITY : (s_m[h] + log2f(sum) - PAGED8_T_BITS) * 0.6931471805599453f;
         }
-        s_f[tid] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+        s_f[h] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       }
-      softmax_barrier();
+      group_barrier(grp);
       more = w.next(p);
-      if (more) load_q(w);
+      if (more) load_q(w, seg + 1);
       ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
       tc_fence_after();
 #pragma unroll 1
-      for (int i = 0; i < NV * NH; i += 16) {
+      for (int c = 0; c < NV; ++c) {
         uint32_t o[16];
-        tmem_ld16(tmem + lane_base + i, o);
+        tmem_ld16(tmem + lane_base + c * NH + hb, o);
         tmem_wait_ld();
-        const int d = (i / NH) * 128 + tid, h0 = i % NH;
-        if (DS >= 128 || tid < DS) {
+        const int d = c * 128 + t;
+        if (DS >= 128 || t < DS) {
           if (whole) {
 #pragma unroll
             for (int k = 0; k < 16; ++k) {
-              const int gr = blk * NH + h0 + k;
-              if (h0 + k < n_rows)
-                p.out[(((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep) * DS + d] =
-                    __float2bfloat16_rn(s_f[h0 + k] == 0.f ? 0.f : __uint_as_float(o[k]) * s_f[h0 + k]);   // no key: O may be 0 * NaN
+              const float f = s_f[hb + k];
+              const int row = rows[k];
+              if (row >= 0) p.out[(size_t)row * DS + d] = __float2bfloat16_rn(f == 0.f ? 0.f : __uint_as_float(o[k]) * f);   // no key: O may be 0 * NaN
             }
           } else {
-            float* dst = p.part + part * NH * DS + (size_t)h0 * DS + d;
+            float* dst = p.part + part * NH * DS + (size_t)hb * DS + d;
 #pragma unroll
             for (int k = 0; k < 16; ++k) dst[(size_t)k * DS] = __uint_as_float(o[k]);
           }
         }
       }
       tc_fence_before();
-      softmax_barrier();                                     // s_f is written again by the next piece
+      ++seg;
+      group_barrier(grp);                                    // s_f is written again by the next piece
     }
   }
   // ---- let straggling copies land if the CTA gave up, then free TMEM
@@ -723,7 +719,7 @@ __global__ void __launch_bounds__(PAGED8_THREADS, PL::CTAS) attn_paged8_kernel(c
     while (clock64() - t0c < 2000000ll) __nanosleep(1000);
   }
   __syncthreads();
-  if (warp == 5) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
+  if (warp == W_MMA) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
 }
 
 // Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
@@ -789,7 +785,7 @@ template <class PL>
 static int paged8_launch(Paged8Params& P, cudaStream_t stream) {
   auto kern = attn_paged8_kernel<PL>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM) != cudaSuccess) return LCA_ERR_CUDA;
-  kern<<<P.grid, PAGED8_THREADS, PL::SMEM, stream>>>(P);
+  kern<<<P.grid, PL::THREADS, PL::SMEM, stream>>>(P);
   const long long units = (long long)P.B * P.Hkv * P.n_blk * (PL::NH * PL::DS / 1024);
   paged8_combine_kernel<PL::DS, PL::NH><<<(unsigned)units, 256, 0, stream>>>(P);
   note_launch(2);
@@ -816,7 +812,7 @@ int attn_paged8_launch(const Paged8Attn& a) {
   P.scale_v = c->scale_sem; P.scale_k = mla ? c->scale_sem : c->scale_pos; P.table = c->block_table;
   P.n_rep = a.n_rep; P.n_tok = a.n_tok; P.out = (bf16*)a.out; P.lse = a.lse;
   P.B = p->batch; P.Hq = p->n_q_heads; P.Hkv = p->n_kv_heads; P.q_len = a.q_len; P.g = a.n_rep ? p->group_size : 1;
-  P.page = c->page_size; P.n_pages = c->n_pages; P.width = c->table_width; P.rep = P.Hq / P.Hkv;
+  P.page = c->page_size; P.page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7; P.n_pages = c->n_pages; P.width = c->table_width; P.rep = P.Hq / P.Hkv;
   const int nh = paged8_rows_per_tile(p, a.q_len);
   P.n_blk = (int)(((long long)P.q_len * P.rep + nh - 1) / nh);
   P.grid = paged8_grid(p, nh); P.min_tiles = 2;
