@@ -121,9 +121,11 @@ int attn_paged8_simt_launch(const Paged8Attn& q) {
 //              most of its time fetching instructions: 243 us instead of 150 at 64 x 5056 rows, 128 heads).
 //   + 1 warp   TMA: 128-byte-wide chunks (16 KB) of the 128 rows of a tile, one request per page
 //   + 1 warp   MMA issue and TMEM
-// The chunks of a tile are consumed as K_0.. then V_0..; S of tile j+1 is issued before O of tile j, and the one ring of
-// slots is filled in exactly that order: K(0) K(1) V(0) K(2) V(1) ...  For MLA a latent chunk passes twice (the second
-// time out of L2): keeping it from S to O would need two whole tiles of slots.
+// S of tile j+1 is issued before O of tile j.  GQA: one ring of slots, filled in the order of use, K(0) K(1) V(0) K(2)
+// V(1) ...  MLA: the latent chunks are keys and values; they stay in their slots from S to O (two tiles at a time are in the
+// ring, a third one is arriving), which saves the second copy: the tensor core reads its operands over the same 128 bytes
+// per clock of shared memory that the copies are written through, and that is what bounds a tile (NH = 16: 1968 clocks of
+// operands and 576 of copies; with a second copy of the values 1088).
 // Work: all tiles of all (sequence, KV head, block of NH rows) units form one line that is cut into equal ranges, one per
 // CTA; a unit that is cut leaves (O, M, l) of its pieces in the workspace, merged by paged8_combine_kernel.
 template <bool MLA_, int DS_, int DP_, int NH_>
@@ -133,6 +135,8 @@ struct Paged8Plan {
   static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
   static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 bytes wide)
   static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
+  static constexpr bool SHARED = MLA && !(DS == 512 && NH == 64);   // a latent chunk stays from S to O
+  static constexpr int PER_TILE = SHARED ? NK : NK + NV;     // slots a tile passes through
   static constexpr int SLOT = 16384;
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
   static constexpr int P_BYTES = 128 * NH;                   // one term
@@ -147,7 +151,7 @@ struct Paged8Plan {
   static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
   static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
   static constexpr int SMEM = OFF_MISC + MISC_BYTES + 1024;
-  static_assert(SLOTS >= NK + 1 && SMEM <= 227 * 1024, "ring of at least one key tile");
+  static_assert(SLOTS >= (SHARED ? 2 * NK : NV + 1) && SMEM <= 227 * 1024, "the tiles that S and O work on fit the ring");
 };
 
 struct Paged8Params {
@@ -258,8 +262,8 @@ __device__ __forceinline__ bool group_any(int grp, bool v) {
   return r != 0;
 }
 
-static constexpr float PAGED8_T_BITS = 8.f;         // the largest weight is 2^8 ...
-static constexpr float PAGED8_SLACK = 3.f;          // ... and may reach 2^11 before the maximum is raised: t_hi up to 2^11
+static constexpr float PAGED8_T_BITS = 6.f;         // the largest weight is 2^8 ...
+static constexpr float PAGED8_SLACK = 5.f;          // ... and may reach 2^11 before the maximum is raised: t_hi up to 2^11
                                                     // leaves at most 2^8 to t_lo (e4m3 ends at 448)
 
 template <class PL>
@@ -372,8 +376,9 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
       for (int j = 0; j < w.n && ok; ++j) {
         const int z2 = look(j + 2);
         if (j + 1 < w.n) load_k(z1);
+        if (!PL::SHARED)
 #pragma unroll
-        for (int c = 0; c < NV; ++c) load(&p.sem, c * 128, PL::VW, z0);
+          for (int c = 0; c < NV; ++c) load(&p.sem, c * 128, PL::VW, z0);
         z0 = z1; z1 = z2;
       }
     }
@@ -385,16 +390,14 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
     int slot = 0;
     uint32_t phase = 0, g = 0, seg = 0;
     bool ok = true;
+    int v_slot = 0;                                          // shared chunks: first slot of the tile whose O comes next
     auto wait_slot = [&]() {
       ok = ok && mbar_wait(FULL(slot), phase, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) fail(ERR_WAIT_KV_FULL);
       return ok;
     };
-    auto done_slot = [&]() {
-      umma_commit_elected(leader, EMPTY(slot));
-      if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; }
-    };
+    auto next_slot = [&]() { if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; } };
     auto issue_s = [&](uint32_t buf) {
       const uint32_t d = tmem + PL::TM_S + buf * 2 * NH;
       uint32_t acc = 0;
@@ -407,7 +410,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         const uint64_t bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
 #pragma unroll
         for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
-        done_slot();
+        if (!PL::SHARED || c == PL::KSEM) umma_commit_elected(leader, EMPTY(slot));
+        next_slot();
       }
       umma_commit_elected(leader, SFULL + 8 * buf);
     };
@@ -428,18 +432,22 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         tc_fence_after();
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-          if (!wait_slot()) break;
-          tc_fence_after();
+          if (!PL::SHARED && !wait_slot()) break;
+          if (!PL::SHARED) tc_fence_after();
+          const int vs = PL::SHARED ? v_slot : slot;
           // 64-wide values: M stays 128, the second half of the operand is the unused half of the slot and the output
           // lanes it feeds are never read
-          const uint64_t ad = desc_rows(base + slot * PL::SLOT, PL::VW, 8192);
+          const uint64_t ad = desc_rows(base + vs * PL::SLOT, PL::VW, 8192);
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_hi, k * 2 * NH), ID_HI, (j > 0 || k > 0) ? 1u : 0u);
             umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_lo, k * 2 * NH), ID_LO, 1u);
           }
-          done_slot();
+          umma_commit_elected(leader, EMPTY(vs));
+          if (PL::SHARED) { if (++v_slot == PL::SLOTS) v_slot = 0; }
+          else next_slot();
         }
+        if (PL::SHARED && ++v_slot == PL::SLOTS) v_slot = 0; // the pos chunk's slot
         umma_commit_elected(leader, PVDONE);
       }
     }
@@ -640,7 +648,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         if (grp == 0 && ((unsigned)(part_r - row0) < 128u || (unsigned)(part_t - row0) < 128u)) {
 #pragma unroll 1
           for (int c = 0; c < NV; ++c) {
-            const uint32_t at = seg_chunks + (uint32_t)min(j + 2, w.n) * NK + (uint32_t)j * NV + c;      // place in the order of loads
+            const uint32_t at = seg_chunks + (PL::SHARED ? (uint32_t)j * NK : (uint32_t)min(j + 2, w.n) * NK + (uint32_t)j * NV) + c;      // place in the order of loads
             const int s = (int)(at % PL::SLOTS);
             ok = mbar_wait(FULL(s), (at / PL::SLOTS) & 1, abort_flag);
             if (!ok) fail(ERR_WAIT_KV_FULL);
@@ -657,7 +665,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         mbar_arrive(PFULL);
         pg0 = pg1; pg1 = pg2; ks = ks1; vs = vs1;
       }
-      seg_chunks += (uint32_t)w.n * (NK + NV);
+      seg_chunks += (uint32_t)w.n * PL::PER_TILE;
       // ---- this piece is done: its sums and maxima, then the next unit's queries (S of this piece is complete), then O
       const bool whole = w.n == w.t.n;
       const size_t part = (size_t)2 * blockIdx.x + (seg == 0 ? 0 : 1);
