@@ -297,6 +297,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
   }
   if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
   if (warp == W_TMA && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");        // the whole grid is resident: nothing is displaced
   // this CTA's range of the line: thread i sums the tiles of sequences [i q, (i + 1) q)
   const long long upu = (long long)p.Hkv * p.n_blk;
   long long s0 = 0;
@@ -459,8 +460,19 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
     uint32_t g = 0, seg = 0, seg_chunks = 0;
     bool ok = true;
     float l[16];
-    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them
+    int pg0 = -1, pg1 = -1;                                  // page of this thread's key in the current tile and in the next one
+    float ks = 0.f, vs = 1.f;                                // scales of pg0
+    auto page_of = [&](const Walk& u, int j) {               // -1: none
+      if (j >= u.n) return -1;
+      const int x = u.t.row0(u.t0 + j) + t;
+      if (!u.t.s.has(x)) return -1;                          // has() implies x below the table's end
+      const int pg = p.table[(size_t)u.b * p.width + (x >> p.page_log2)];
+      return pg >= 0 && pg < p.n_pages ? pg : -1;
+    };
+    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them; the first lookups of the
+    // piece run underneath
     auto load_q = [&](const Walk& u, uint32_t which) {
+      pg0 = page_of(u, 0); pg1 = page_of(u, 1);
       constexpr int VS = PL::KSEM * 16, VQ = VS + DP / 8, NL = (VQ + 31) / 32;   // 8-element vectors of a row
       const int n_rows = p.q_len * p.rep - u.blk * NH;
 #pragma unroll 2
@@ -514,6 +526,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
           s_row[(which & 1) * NH + r] = r < n_rows ? row : -1;
         }
       }
+      ks = 0.f; vs = 1.f;
+      if (pg0 >= 0) { ks = p.scale_k[(size_t)pg0 * p.Hkv + u.hk]; vs = p.scale_v[(size_t)pg0 * p.Hkv + u.hk]; }
       fence_proxy_async_smem();
       mbar_arrive(QFULL);
       group_barrier(grp);
@@ -522,24 +536,13 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
     if (more) load_q(w, 0);
     while (more) {
       const PagedSpan sp = w.t.s;
-      const int32_t* table = p.table + (size_t)w.b * p.width;
       const int* rows = s_row + (seg & 1) * NH + hb;
       bool unset = t < 16 && rows[t & 15] >= 0;              // thread h of the group: its row has no maximum yet
 #pragma unroll
       for (int i = 0; i < 16; ++i) l[i] = 0.f;
-      auto page_of = [&](int j) {                            // page of this thread's key in tile j, -1: none
-        if (j >= w.n) return -1;
-        const int x = w.t.row0(w.t0 + j) + t;
-        if (!sp.has(x)) return -1;                           // has() implies x below the table's end
-        const int pg = table[x >> p.page_log2];
-        return pg >= 0 && pg < p.n_pages ? pg : -1;
-      };
       // first rows of the (at most two) pages that are present in part; one past every row where there is none
       const int none = 0x7fffffff, mask = p.page - 1;
       const int part_r = (sp.n_rep & mask) ? sp.n_rep & ~mask : none, part_t = (sp.n_tok & mask) ? sp.n_tok & ~mask : none;
-      int pg0 = page_of(0), pg1 = page_of(1);
-      float ks = 0.f, vs = 1.f;
-      if (pg0 >= 0) { ks = p.scale_k[(size_t)pg0 * p.Hkv + w.hk]; vs = p.scale_v[(size_t)pg0 * p.Hkv + w.hk]; }
 #pragma unroll 1
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
@@ -547,7 +550,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         // the next tile's scales and the page after that are on their way while this tile is worked on
         float ks1 = 0.f, vs1 = 1.f;
         if (pg1 >= 0) { ks1 = p.scale_k[(size_t)pg1 * p.Hkv + w.hk]; vs1 = p.scale_v[(size_t)pg1 * p.Hkv + w.hk]; }
-        const int pg2 = page_of(j + 2);
+        const int pg2 = page_of(w, j + 2);
         vs = fmaxf(vs, exp2_int(PAGED8_MIN_EXP));
         // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 vs + 8): both are multiples of e = 2^(y - M + half), half way
         // between them, so that neither is lost below 2^-126 where the scales of a sequence span more than fp32 does.
@@ -731,43 +734,61 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
 }
 
 // Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
-// no tile at all.  One CTA: 1024 outputs of a unit.
+// no tile at all.  One warp: 32 * VEC outputs of one row; lane i holds the maximum and the sum of piece i, so that their loads
+// and the loads of the pieces' outputs are two round trips, not one per piece (13 us instead of COMBINE_US).  Launched
+// programmatically: its CTAs are in place when the attention kernel ends.
 template <int DS, int NH>
 __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
-  constexpr int SPLIT = NH * DS / 1024;
+  constexpr int VEC = DS >= 128 ? 4 : 2, SPLIT = NH * DS / (256 * VEC);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31;
   const long long unit = blockIdx.x / SPLIT;
-  const int x = (int)(blockIdx.x % SPLIT) * 1024 + (int)threadIdx.x * 4, h = x / DS, d = x % DS;
+  const int x = ((int)(blockIdx.x % SPLIT) * 256 + (int)threadIdx.x) * VEC, h = x / DS, d = x % DS;      // h: one per warp
   const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
   const int gr = blk * NH + h;
   if (gr >= p.q_len * p.rep) return;
   const long long T = p.prefix[p.B], seq = p.prefix[b], n = (p.prefix[b + 1] - seq) / per;
   const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  float o[VEC] = {};
   float m = -INFINITY, l = 0.f;
   if (n > 0) {
     const int G = ctas_used(p, T);
     const long long u0 = seq + u * n, u1 = u0 + n;
-    // CTA c owns [c T / G, (c + 1) T / G)
-    int c0 = (int)(u0 * G / T);
-    while ((long long)(c0 + 1) * T / G <= u0) ++c0;
-    if ((long long)(c0 + 1) * T / G >= u1) return;           // not cut: written by the CTA that worked on it
+    // CTA c owns [c T / G, (c + 1) T / G): tile x is in CTA ((x + 1) G - 1) / T
+    const int c0 = (int)(((u0 + 1) * G - 1) / T), np = (int)((u1 * G - 1) / T) - c0 + 1;
+    if (np == 1) return;                                     // not cut: written by the CTA that worked on it
     const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
     const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
-    for (int c = c0; c < G && (long long)c * T / G < u1; ++c) m = fmaxf(m, ml[(size_t)(2 * c + (c == c0 ? first : 0)) * 2 * NH + h]);
-    for (int c = c0; c < G && (long long)c * T / G < u1; ++c) {
-      const size_t part = (size_t)(2 * c + (c == c0 ? first : 0));
-      const float lj = ml[part * 2 * NH + NH + h];
-      if (lj == 0.f) continue;                               // no key of that piece was seen
-      const float f = exp2f(0.5f * (ml[part * 2 * NH + h] - m));       // applied twice: M contains the scales, the square may be below fp32
-      const float4 v = *reinterpret_cast<const float4*>(p.part + part * NH * DS + x);
-      l = fmaf(f * lj, f, l);
-      o.x = fmaf(f * v.x, f, o.x); o.y = fmaf(f * v.y, f, o.y); o.z = fmaf(f * v.z, f, o.z); o.w = fmaf(f * v.w, f, o.w);
+    for (int i = lane; i < np; i += 32) m = fmaxf(m, ml[(size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h]);
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+    for (int i0 = 0; i0 < np; i0 += 32) {
+      const int i = i0 + lane;
+      float f = 0.f, lj = 0.f;
+      if (i < np) {
+        const float* q = ml + (size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h;
+        lj = q[NH];
+        // applied twice: M contains the scales, the square may be below fp32.  A piece without a seen key has no weight
+        f = lj == 0.f ? 0.f : exp2f(0.5f * (q[0] - m));
+      }
+      l += warp_sum(f * lj * f);
+      const int cnt = min(np - i0, 32);
+#pragma unroll 8
+      for (int k = 0; k < cnt; ++k) {
+        const float w = __shfl_sync(0xffffffffu, f, k);
+        const float* src = p.part + (size_t)(2 * (c0 + i0 + k) + (i0 + k == 0 ? first : 0)) * NH * DS + x;
+        float v[VEC];
+        if constexpr (VEC == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] = w == 0.f ? o[e] : fmaf(w * v[e], w, o[e]);        // without weight: may be 0 * NaN
+      }
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint2 w;
-  w.x = pack_bf16x2(o.x * inv, o.y * inv); w.y = pack_bf16x2(o.z * inv, o.w * inv);
-  *reinterpret_cast<uint2*>(p.out + row * DS + d) = w;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
+#pragma unroll
+  for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
   if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
 }
 
@@ -794,9 +815,18 @@ static int paged8_launch(Paged8Params& P, cudaStream_t stream) {
   auto kern = attn_paged8_kernel<PL>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM) != cudaSuccess) return LCA_ERR_CUDA;
   kern<<<P.grid, PL::THREADS, PL::SMEM, stream>>>(P);
-  const long long units = (long long)P.B * P.Hkv * P.n_blk * (PL::NH * PL::DS / 1024);
-  paged8_combine_kernel<PL::DS, PL::NH><<<(unsigned)units, 256, 0, stream>>>(P);
-  note_launch(2);
+  note_launch();
+  if (cudaGetLastError() != cudaSuccess) return LCA_ERR_CUDA;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((long long)P.B * P.Hkv * P.n_blk * (PL::NH * PL::DS / (PL::DS >= 128 ? 1024 : 512))));
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, paged8_combine_kernel<PL::DS, PL::NH>, P) != cudaSuccess) return LCA_ERR_CUDA;
+  note_launch();
   return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
 }
 template <bool MLA, int DS, int DP>
@@ -828,7 +858,7 @@ int attn_paged8_launch(const Paged8Attn& a) {
   P.part = static_cast<float*>(a.ws);
   const size_t part_bytes = (size_t)2 * P.grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float);
   P.prefix = reinterpret_cast<long long*>(static_cast<char*>(a.ws) + (part_bytes + 15) / 16 * 16);
-  if ((long long)P.B * P.Hkv * P.n_blk * ((long long)nh * p->d_sem / 1024) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if ((long long)P.B * P.Hkv * P.n_blk * ((long long)nh * p->d_sem / 512) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   if (mla) return p->d_sem == 512 ? paged8_launch_rows<true, 512, 64>(P, nh, a.stream) : paged8_launch_rows<true, 128, 64>(P, nh, a.stream);
   return p->d_sem == 128 ? paged8_launch_rows<false, 128, 128>(P, nh, a.stream) : paged8_launch_rows<false, 64, 64>(P, nh, a.stream);
 }
