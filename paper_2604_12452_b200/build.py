@@ -24,7 +24,8 @@ SOURCES = {
     "attn_gqa2.cu": ["--use_fast_math"],
     "gemm_uv.cu": ["--use_fast_math"],
     "paged8.cu": [],              # scales, codes and anchors are compared exactly
-    "attn_paged8.cu": [],         # names its approximate instructions itself
+    "attn_paged8.cu": [],         # these two name their approximate instructions themselves
+    "attn_paged8_pair.cu": [],
 }
 
 

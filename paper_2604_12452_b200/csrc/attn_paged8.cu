@@ -13,9 +13,7 @@
 //   sum adds the weights without s_v in fp32, unrounded.
 #include <cstring>
 
-#include "fp8_common.cuh"
-#include "lca_common.cuh"
-#include "tc_common.cuh"
+#include "attn_paged8.cuh"
 
 namespace lca {
 using namespace tc;
@@ -135,7 +133,7 @@ struct Paged8Plan {
   static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
   static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 bytes wide)
   static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
-  static constexpr bool SHARED = MLA && !(DS == 512 && NH == 64);   // a latent chunk stays from S to O
+  static constexpr bool SHARED = MLA;                        // a latent chunk stays from S to O
   static constexpr int PER_TILE = SHARED ? NK : NK + NV;     // slots a tile passes through
   static constexpr int SLOT = 16384;
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
@@ -154,105 +152,6 @@ struct Paged8Plan {
   static_assert(SLOTS >= (SHARED ? 2 * NK : NV + 1) && SMEM <= 227 * 1024, "the tiles that S and O work on fit the ring");
 };
 
-struct Paged8Params {
-  CUtensorMap sem, pos;       // [n_pages * Hkv, page, d] codes; boxes of one page x 128 (or 64) bytes
-  const bf16* q_sem; const bf16* q_pos;
-  const float* scale_k; const float* scale_v; const int32_t* table;
-  const int32_t* n_rep; const int32_t* n_tok;
-  bf16* out; float* lse;
-  float* part;                // [2 * CTAs][NH][DS] partial O, then [2 * CTAs][2][NH] M and l
-  long long* prefix;          // [B + 1] tiles before each sequence (all units), written by CTA 0
-  int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, min_tiles, grid;
-  float scale_log2, bias_log2;
-};
-
-// Tiles of 128 rows of a sequence: those with representatives, then those with tokens.
-struct TileSpan {
-  PagedSpan s;
-  int n_a, b0, n;
-  __device__ __forceinline__ int row0(int i) const { return (i < n_a ? i : b0 + (i - n_a)) * 128; }
-};
-__device__ __forceinline__ TileSpan tile_span(const Paged8Params& p, int b) {
-  TileSpan t;
-  t.s = paged_span(p.n_rep, p.n_tok, b, p.g, p.width * p.page);
-  t.n_a = (t.s.n_rep + 127) >> 7;
-  t.b0 = max(t.s.tok0 >> 7, t.n_a);
-  t.n = t.n_a + (t.s.n_tok > t.s.tok0 ? max(((t.s.n_tok + 127) >> 7) - t.b0, 0) : 0);
-  return t;
-}
-__device__ __forceinline__ int ctas_used(const Paged8Params& p, long long T) {
-  return (int)max(1ll, min((long long)p.grid, (T + p.min_tiles - 1) / p.min_tiles));
-}
-
-// The pieces of units in one CTA's range of the line.
-struct Walk {
-  int b;
-  long long off, left;        // position inside sequence b's part of the line; tiles left in this CTA's range
-  TileSpan t;
-  int hk, blk, t0, n;         // current piece: tiles [t0, t0 + n) of unit (b, hk, blk)
-  bool fresh;
-  __device__ __forceinline__ bool next(const Paged8Params& p) {
-    if (!fresh) off += n;
-    while (left > 0) {
-      if (b >= p.B) return false;
-      t = tile_span(p, b);
-      if (off < (long long)t.n * p.Hkv * p.n_blk) break;
-      off -= (long long)t.n * p.Hkv * p.n_blk;
-      ++b;
-    }
-    if (left <= 0) return false;
-    const int u = (int)(off / t.n);
-    t0 = (int)(off % t.n);
-    hk = u / p.n_blk; blk = u % p.n_blk;
-    n = (int)min((long long)(t.n - t0), left);
-    left -= n;
-    fresh = false;
-    return true;
-  }
-};
-
-__device__ __forceinline__ void umma_f8_elected(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                                uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
-// kind::f8f6f4, fp32 accumulator, A e4m3, B e4m3 (0) or e5m2 (1)
-__host__ __device__ constexpr uint32_t umma_idesc_f8(int M, int N, int b_format, bool a_mn_major, bool b_mn_major) {
-  return (1u << 4) | ((uint32_t)b_format << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
-         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
-// Shared-memory descriptor for rows of `width` bytes with the swizzle of that width (16: none).  K-major: 8 rows (one
-// group) are 8 * width bytes apart.  MN-major: the same picture with the rows along K.  `lbo`: distance of the next block
-// of `width` bytes along the contiguous dimension (only used where the operand is wider than one block).
-__device__ __forceinline__ uint64_t desc_rows(uint32_t addr, int width, uint32_t lbo) {
-  const uint64_t layout = width == 128 ? 2 : width == 64 ? 4 : width == 32 ? 6 : 0;
-  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
-         ((uint64_t)(((uint32_t)width * 8 >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (layout << 61);
-}
-// Byte offset of 16-byte unit `u` of row `r` in such an image.
-template <int WIDTH>
-__device__ __forceinline__ uint32_t swz(int r, int u) {
-  if (WIDTH == 128) return (uint32_t)(r * 128 + ((u ^ (r & 7)) << 4));
-  if (WIDTH == 64) return (uint32_t)(r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
-  if (WIDTH == 32) return (uint32_t)(r * 32 + ((u ^ ((r >> 2) & 1)) << 4));
-  return (uint32_t)(r * 16);
-}
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(taddr) : "memory");
-}
-__device__ __forceinline__ float warp_max_f32(float v) {
-  float r;
-  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-  return r;
-}
-__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
-__device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // one group of softmax warps (128 threads)
 __device__ __forceinline__ void group_barrier(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); }
 __device__ __forceinline__ bool group_any(int grp, bool v) {
@@ -261,10 +160,6 @@ __device__ __forceinline__ bool group_any(int grp, bool v) {
                : "=r"(r) : "r"((uint32_t)v), "r"(grp + 1) : "memory");
   return r != 0;
 }
-
-static constexpr float PAGED8_T_BITS = 6.f;         // the largest weight is 2^8 ...
-static constexpr float PAGED8_SLACK = 5.f;          // ... and may reach 2^11 before the maximum is raised: t_hi up to 2^11
-                                                    // leaves at most 2^8 to t_lo (e4m3 ends at 448)
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
@@ -298,40 +193,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
   if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
   if (warp == W_TMA && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");        // the whole grid is resident: nothing is displaced
-  // this CTA's range of the line: thread i sums the tiles of sequences [i q, (i + 1) q)
-  const long long upu = (long long)p.Hkv * p.n_blk;
-  long long s0 = 0;
-  {
-    const int q = (p.B + PL::THREADS - 1) / PL::THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
-    long long sum = 0;
-    for (int b = lo; b < hi; ++b) sum += (long long)tile_span(p, b).n * upu;
-    long long inc = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
-    if (lane == 31) s_warp[warp] = inc;
-    __syncthreads();
-    long long T = 0, before = inc - sum;
-    for (int w = 0; w < PL::THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
-    const int G = ctas_used(p, T);
-    long long s1 = 0;
-    if ((int)blockIdx.x < G) { s0 = (long long)blockIdx.x * T / G; s1 = ((long long)blockIdx.x + 1) * T / G; }
-    if (blockIdx.x == 0) {                                   // for the combining kernel
-      long long at = before;
-      for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (long long)tile_span(p, b).n * upu; }
-      if (tid == 0) p.prefix[p.B] = T;
-    }
-    if (s1 > s0 && s0 >= before && s0 < before + sum) {      // exactly one thread
-      long long at = before;
-      int b = lo;
-      while (true) {
-        const long long n = (long long)tile_span(p, b).n * upu;
-        if (s0 < at + n) break;
-        at += n; ++b;
-      }
-      *s_b = b; s_off[0] = s0 - at; s_off[1] = s1 - s0;
-    }
-    if (tid == 0 && s1 <= s0) { *s_b = 0; s_off[0] = 0; s_off[1] = 0; }
-  }
+  paged8_range<PL::THREADS>(p, (int)blockIdx.x, s_warp, s_b, s_off);
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
@@ -489,28 +351,16 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
             v[i] = *reinterpret_cast<const uint4*>(c < VS ? p.q_sem + (size_t)row * DS + 8 * c : p.q_pos + (size_t)row * DP + 8 * (c - VS));
         }
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-          const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7fffu, (x[k] >> 16) & 0x7fffu));
-        }
+        for (int i = 0; i < NL; ++i) top = max(top, max_abs_bf16(v[i]));
         top = __reduce_max_sync(0xffffffffu, top);
-        const int e = min(max(134 - (int)(top >> 7), -119), 120);       // largest element times 2^e in [128, 256)
+        const int e = query_exponent(top);
         const float f = exp2_int(e);
 #pragma unroll
         for (int i = 0; i < NL; ++i) {
           const int c = lane + 32 * i;
           if (c >= VQ) continue;
-          const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
           uint32_t hi[2], lo[2];
-#pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const float a0 = __uint_as_float(x[2 * k] << 16) * f, a1 = __uint_as_float(x[2 * k] & 0xffff0000u) * f;
-            const float a2 = __uint_as_float(x[2 * k + 1] << 16) * f, a3 = __uint_as_float(x[2 * k + 1] & 0xffff0000u) * f;
-            hi[k] = e4m3x4_from_float(a0, a1, a2, a3);
-            const float4 h = e4m3x4_to_float4(hi[k]);
-            lo[k] = e4m3x4_from_float(a0 - h.x, a1 - h.y, a2 - h.z, a3 - h.w);
-          }
+          split_e4m3(v[i], f, hi, lo);
           const bool sem = c < VS;
           const int chunk = sem ? c / 16 : PL::KSEM, u16 = (sem ? c % 16 : c - VS) / 2, half = c & 1;
           unsigned char* q = base_ptr + PL::OFF_Q + chunk * 2 * NH * 128 + 8 * half;
@@ -733,77 +583,20 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
   if (warp == W_MMA) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
 }
 
-// Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
-// no tile at all.  One warp: 32 * VEC outputs of one row; lane i holds the maximum and the sum of piece i, so that their loads
-// and the loads of the pieces' outputs are two round trips, not one per piece (13 us instead of COMBINE_US).  Launched
-// programmatically: its CTAs are in place when the attention kernel ends.
-template <int DS, int NH>
-__global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
-  constexpr int VEC = DS >= 128 ? 4 : 2, SPLIT = NH * DS / (256 * VEC);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
-  const int lane = threadIdx.x & 31;
-  const long long unit = blockIdx.x / SPLIT;
-  const int x = ((int)(blockIdx.x % SPLIT) * 256 + (int)threadIdx.x) * VEC, h = x / DS, d = x % DS;      // h: one per warp
-  const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
-  const int gr = blk * NH + h;
-  if (gr >= p.q_len * p.rep) return;
-  const long long T = p.prefix[p.B], seq = p.prefix[b], n = (p.prefix[b + 1] - seq) / per;
-  const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
-  float o[VEC] = {};
-  float m = -INFINITY, l = 0.f;
-  if (n > 0) {
-    const int G = ctas_used(p, T);
-    const long long u0 = seq + u * n, u1 = u0 + n;
-    // CTA c owns [c T / G, (c + 1) T / G): tile x is in CTA ((x + 1) G - 1) / T
-    const int c0 = (int)(((u0 + 1) * G - 1) / T), np = (int)((u1 * G - 1) / T) - c0 + 1;
-    if (np == 1) return;                                     // not cut: written by the CTA that worked on it
-    const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
-    const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
-    for (int i = lane; i < np; i += 32) m = fmaxf(m, ml[(size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h]);
-#pragma unroll
-    for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-    for (int i0 = 0; i0 < np; i0 += 32) {
-      const int i = i0 + lane;
-      float f = 0.f, lj = 0.f;
-      if (i < np) {
-        const float* q = ml + (size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h;
-        lj = q[NH];
-        // applied twice: M contains the scales, the square may be below fp32.  A piece without a seen key has no weight
-        f = lj == 0.f ? 0.f : exp2f(0.5f * (q[0] - m));
-      }
-      l += warp_sum(f * lj * f);
-      const int cnt = min(np - i0, 32);
-#pragma unroll 8
-      for (int k = 0; k < cnt; ++k) {
-        const float w = __shfl_sync(0xffffffffu, f, k);
-        const float* src = p.part + (size_t)(2 * (c0 + i0 + k) + (i0 + k == 0 ? first : 0)) * NH * DS + x;
-        float v[VEC];
-        if constexpr (VEC == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
-        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] = w == 0.f ? o[e] : fmaf(w * v[e], w, o[e]);        // without weight: may be 0 * NaN
-      }
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
-#pragma unroll
-  for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
-  if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
-}
-
 // ------------------------------------------------------------------------------------------------------------- host
-bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d);   // attn_tc.cu
+bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d, int box_rows);   // attn_tc.cu
 
+// Query rows that share a tile of keys.  The tile is padded to that number, so it is the smallest one that holds all rows of
+// a KV head (the softmax threads compute an exponential per padded row and key); at most 64, as O takes d / 128 * NH columns
+// of TMEM.  The MLA shape with more than 32 rows goes to CTA pairs in blocks of 128 (64 x 5056 rows, 128 heads: 128 us in
+// blocks of 64 on single CTAs, PAIR_US on pairs).
 static int paged8_rows_per_tile(const lca_params* p, int q_len) {
-  // The tile is padded to NH rows: the smallest that holds all rows of a KV head, so that the softmax threads (one
-  // exponential per padded row and key) do not work for nothing; 64 at most, as O takes d / 128 * NH columns of TMEM.
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : p->d_sem == 512 ? 128 : 64;
 }
+// CTAs (or pairs) that share the work: all that are resident at once.
 static int paged8_grid(const lca_params* p, int nh) {
-  const bool one = p->d_sem == 512 || (nh == 64);
-  return 148 * (one ? 1 : 2);
+  return nh == 128 ? 74 : (p->d_sem == 512 || nh == 64) ? 148 : 2 * 148;
 }
 size_t attn_paged8_workspace_bytes(const lca_params* p, int q_len) {
   const int nh = paged8_rows_per_tile(p, q_len), grid = paged8_grid(p, nh);
@@ -817,23 +610,14 @@ static int paged8_launch(Paged8Params& P, cudaStream_t stream) {
   kern<<<P.grid, PL::THREADS, PL::SMEM, stream>>>(P);
   note_launch();
   if (cudaGetLastError() != cudaSuccess) return LCA_ERR_CUDA;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((long long)P.B * P.Hkv * P.n_blk * (PL::NH * PL::DS / (PL::DS >= 128 ? 1024 : 512))));
-  cfg.blockDim = dim3(256);
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, paged8_combine_kernel<PL::DS, PL::NH>, P) != cudaSuccess) return LCA_ERR_CUDA;
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+  return paged8_combine_launch<PL::DS, PL::NH>(P, stream);
 }
 template <bool MLA, int DS, int DP>
 static int paged8_launch_rows(Paged8Params& P, int nh, cudaStream_t stream) {
   if (nh == 16) return paged8_launch<Paged8Plan<MLA, DS, DP, 16>>(P, stream);
   if (nh == 32) return paged8_launch<Paged8Plan<MLA, DS, DP, 32>>(P, stream);
-  return paged8_launch<Paged8Plan<MLA, DS, DP, 64>>(P, stream);
+  if constexpr (DS == 512) return attn_paged8_pair_launch(P, stream);
+  else return paged8_launch<Paged8Plan<MLA, DS, DP, 64>>(P, stream);
 }
 
 int attn_paged8_launch(const Paged8Attn& a) {
@@ -843,15 +627,17 @@ int attn_paged8_launch(const Paged8Attn& a) {
   Paged8Params P;
   memset(&P, 0, sizeof(P));
   const long long blocks = (long long)c->n_pages * p->n_kv_heads;
-  if (!make_tensor_map_pages(&P.sem, c->pages_sem, p->d_sem, c->page_size, blocks, p->d_sem >= 128 ? 128 : p->d_sem) ||
-      !make_tensor_map_pages(&P.pos, c->pages_pos, p->d_pos, c->page_size, blocks, p->d_pos))
+  const int nh = paged8_rows_per_tile(p, a.q_len);
+  // a request brings a whole page; on pairs, where a CTA takes 64 of a tile's keys, at most 64 rows
+  const int box = nh == 128 && c->page_size > 64 ? 64 : c->page_size;
+  if (!make_tensor_map_pages(&P.sem, c->pages_sem, p->d_sem, c->page_size, blocks, p->d_sem >= 128 ? 128 : p->d_sem, box) ||
+      !make_tensor_map_pages(&P.pos, c->pages_pos, p->d_pos, c->page_size, blocks, p->d_pos, box))
     return LCA_ERR_CUDA;
   P.q_sem = (const bf16*)a.q_sem; P.q_pos = (const bf16*)a.q_pos;
   P.scale_v = c->scale_sem; P.scale_k = mla ? c->scale_sem : c->scale_pos; P.table = c->block_table;
   P.n_rep = a.n_rep; P.n_tok = a.n_tok; P.out = (bf16*)a.out; P.lse = a.lse;
   P.B = p->batch; P.Hq = p->n_q_heads; P.Hkv = p->n_kv_heads; P.q_len = a.q_len; P.g = a.n_rep ? p->group_size : 1;
   P.page = c->page_size; P.page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7; P.n_pages = c->n_pages; P.width = c->table_width; P.rep = P.Hq / P.Hkv;
-  const int nh = paged8_rows_per_tile(p, a.q_len);
   P.n_blk = (int)(((long long)P.q_len * P.rep + nh - 1) / nh);
   P.grid = paged8_grid(p, nh); P.min_tiles = 2;
   P.scale_log2 = p->softmax_scale * 1.4426950408889634f; P.bias_log2 = p->rep_logit_bias * 1.4426950408889634f;
@@ -870,7 +656,8 @@ int attn_paged8_take_status() {
     int zero = 0;
     cudaMemcpyToSymbol(g_paged8_status, &zero, sizeof(int));
   }
-  return st;
+  const int pair = attn_paged8_pair_take_status();
+  return pair != 0 ? pair : st;
 }
 
 }  // namespace lca

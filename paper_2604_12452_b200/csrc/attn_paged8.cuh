@@ -1,0 +1,262 @@
+// What the two tensor-core kernels over the paged 8-bit cache share: the line of tiles and its ranges, operand splitting,
+// instruction and shared-memory descriptors, and the kernel that merges the pieces.
+#pragma once
+
+#include "fp8_common.cuh"
+#include "lca_common.cuh"
+#include "tc_common.cuh"
+
+namespace lca {
+using namespace tc;
+
+static constexpr float PAGED8_T_BITS = 6.f;         // a raised maximum puts the largest weight at 2^6 ...
+static constexpr float PAGED8_SLACK = 5.f;          // ... and it may grow to 2^11 before the maximum is raised again: t_hi up
+                                                    // to 2^11 leaves at most 2^8 to t_lo (e4m3 ends at 448)
+
+struct Paged8Params {
+  CUtensorMap sem, pos;       // [n_pages * Hkv, page, d] codes; boxes of one page x 128 (or 64) bytes
+  const bf16* q_sem; const bf16* q_pos;
+  const float* scale_k; const float* scale_v; const int32_t* table;
+  const int32_t* n_rep; const int32_t* n_tok;
+  bf16* out; float* lse;
+  float* part;                // [2 * grid][NH][DS] partial O, then [2 * grid][2][NH] M and l
+  long long* prefix;          // [B + 1] tiles before each sequence (all units), written by CTA 0
+  int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, min_tiles, grid;   // grid: CTAs (pairs of them) that share the line
+  float scale_log2, bias_log2;
+};
+
+// Tiles of 128 rows of a sequence: those with representatives, then those with tokens.
+struct TileSpan {
+  PagedSpan s;
+  int n_a, b0, n;
+  __device__ __forceinline__ int row0(int i) const { return (i < n_a ? i : b0 + (i - n_a)) * 128; }
+};
+__device__ __forceinline__ TileSpan tile_span(const Paged8Params& p, int b) {
+  TileSpan t;
+  t.s = paged_span(p.n_rep, p.n_tok, b, p.g, p.width * p.page);
+  t.n_a = (t.s.n_rep + 127) >> 7;
+  t.b0 = max(t.s.tok0 >> 7, t.n_a);
+  t.n = t.n_a + (t.s.n_tok > t.s.tok0 ? max(((t.s.n_tok + 127) >> 7) - t.b0, 0) : 0);
+  return t;
+}
+__device__ __forceinline__ int ctas_used(const Paged8Params& p, long long T) {
+  return (int)max(1ll, min((long long)p.grid, (T + p.min_tiles - 1) / p.min_tiles));
+}
+
+// The pieces of units in one CTA's range of the line.
+struct Walk {
+  int b;
+  long long off, left;        // position inside sequence b's part of the line; tiles left in this CTA's range
+  TileSpan t;
+  int hk, blk, t0, n;         // current piece: tiles [t0, t0 + n) of unit (b, hk, blk)
+  bool fresh;
+  __device__ __forceinline__ bool next(const Paged8Params& p) {
+    if (!fresh) off += n;
+    while (left > 0) {
+      if (b >= p.B) return false;
+      t = tile_span(p, b);
+      if (off < (long long)t.n * p.Hkv * p.n_blk) break;
+      off -= (long long)t.n * p.Hkv * p.n_blk;
+      ++b;
+    }
+    if (left <= 0) return false;
+    const int u = (int)(off / t.n);
+    t0 = (int)(off % t.n);
+    hk = u / p.n_blk; blk = u % p.n_blk;
+    n = (int)min((long long)(t.n - t0), left);
+    left -= n;
+    fresh = false;
+    return true;
+  }
+};
+
+// The range of CTA (or CTA pair) `id`: thread i sums the tiles of sequences [i q, (i + 1) q); every thread of the CTA calls it.
+// Leaves the first sequence in *s_b, the offset inside it and the tiles of the range in s_off[0 .. 1]; ends with a barrier
+// still to come.  CTA 0 of the grid writes the prefix sums for the merging kernel.
+template <int THREADS>
+__device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long long* s_warp, int* s_b, long long* s_off) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long upu = (long long)p.Hkv * p.n_blk;
+  const int q = (p.B + THREADS - 1) / THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
+  long long sum = 0;
+  for (int b = lo; b < hi; ++b) sum += (long long)tile_span(p, b).n * upu;
+  long long inc = sum;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
+  if (lane == 31) s_warp[warp] = inc;
+  __syncthreads();
+  long long T = 0, before = inc - sum;
+  for (int w = 0; w < THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
+  const int G = ctas_used(p, T);
+  long long s0 = 0, s1 = 0;
+  if (id < G) { s0 = (long long)id * T / G; s1 = ((long long)id + 1) * T / G; }
+  if (blockIdx.x == 0) {
+    long long at = before;
+    for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (long long)tile_span(p, b).n * upu; }
+    if (tid == 0) p.prefix[p.B] = T;
+  }
+  if (s1 > s0 && s0 >= before && s0 < before + sum) {        // exactly one thread
+    long long at = before;
+    int b = lo;
+    while (true) {
+      const long long n = (long long)tile_span(p, b).n * upu;
+      if (s0 < at + n) break;
+      at += n; ++b;
+    }
+    *s_b = b; s_off[0] = s0 - at; s_off[1] = s1 - s0;
+  }
+  if (tid == 0 && s1 <= s0) { *s_b = 0; s_off[0] = 0; s_off[1] = 0; }
+}
+
+// Splits the 8 bf16 values of `v` times f into two e4m3 terms.
+__device__ __forceinline__ void split_e4m3(const uint4& v, float f, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
+  const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const float a0 = __uint_as_float(x[2 * k] << 16) * f, a1 = __uint_as_float(x[2 * k] & 0xffff0000u) * f;
+    const float a2 = __uint_as_float(x[2 * k + 1] << 16) * f, a3 = __uint_as_float(x[2 * k + 1] & 0xffff0000u) * f;
+    hi[k] = e4m3x4_from_float(a0, a1, a2, a3);
+    const float4 h = e4m3x4_to_float4(hi[k]);
+    lo[k] = e4m3x4_from_float(a0 - h.x, a1 - h.y, a2 - h.z, a3 - h.w);
+  }
+}
+__device__ __forceinline__ uint32_t max_abs_bf16(const uint4& v) {
+  uint32_t top = 0;
+  const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) top = max(top, max(x[k] & 0x7fffu, (x[k] >> 16) & 0x7fffu));
+  return top;
+}
+// Exponent that brings a row whose largest |element| has these bf16 bits into [128, 256).
+__device__ __forceinline__ int query_exponent(uint32_t bits) { return min(max(134 - (int)(bits >> 7), -119), 120); }
+
+__device__ __forceinline__ void umma_f8_elected(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                                uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+      "@q tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+// kind::f8f6f4, fp32 accumulator, A e4m3, B e4m3 (0) or e5m2 (1)
+__host__ __device__ constexpr uint32_t umma_idesc_f8(int M, int N, int b_format, bool a_mn_major, bool b_mn_major) {
+  return (1u << 4) | ((uint32_t)b_format << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
+         ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
+}
+// Shared-memory descriptor for rows of `width` bytes with the swizzle of that width (16: none).  K-major: 8 rows (one
+// group) are 8 * width bytes apart.  MN-major: the same picture with the rows along K.  `lbo`: distance of the next block
+// of `width` bytes along the contiguous dimension (only used where the operand is wider than one block).
+__device__ __forceinline__ uint64_t desc_rows(uint32_t addr, int width, uint32_t lbo) {
+  const uint64_t layout = width == 128 ? 2 : width == 64 ? 4 : width == 32 ? 6 : 0;
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)((lbo >> 4) & 0x3FFFu) << 16) |
+         ((uint64_t)(((uint32_t)width * 8 >> 4) & 0x3FFFu) << 32) | (1ull << 46) | (layout << 61);
+}
+// Byte offset of 16-byte unit `u` of row `r` in such an image.
+template <int WIDTH>
+__device__ __forceinline__ uint32_t swz(int r, int u) {
+  if (WIDTH == 128) return (uint32_t)(r * 128 + ((u ^ (r & 7)) << 4));
+  if (WIDTH == 64) return (uint32_t)(r * 64 + ((u ^ ((r >> 1) & 3)) << 4));
+  if (WIDTH == 32) return (uint32_t)(r * 32 + ((u ^ ((r >> 2) & 1)) << 4));
+  return (uint32_t)(r * 16);
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+        "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float warp_max_f32(float v) {
+  float r;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+  return r;
+}
+__device__ __forceinline__ uint64_t mul_f32x2(uint64_t a, uint64_t b) {
+  uint64_t r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ uint64_t join(uint32_t lo, uint32_t hi) {
+  uint64_t r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+__device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
+// Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
+// no tile at all.  One warp: 32 * VEC outputs of one row; lane i holds the maximum and the sum of piece i, so that their loads
+// and the loads of the pieces' outputs are two round trips, not one per piece (13 us instead of COMBINE_US).  Launched
+// programmatically: its CTAs are in place when the attention kernel ends.
+template <int DS, int NH>
+__global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
+  constexpr int VEC = DS >= 128 ? 4 : 2, SPLIT = NH * DS / (256 * VEC);
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+  const int lane = threadIdx.x & 31;
+  const long long unit = blockIdx.x / SPLIT;
+  const int x = ((int)(blockIdx.x % SPLIT) * 256 + (int)threadIdx.x) * VEC, h = x / DS, d = x % DS;      // h: one per warp
+  const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
+  const int gr = blk * NH + h;
+  if (gr >= p.q_len * p.rep) return;
+  const long long T = p.prefix[p.B], seq = p.prefix[b], n = (p.prefix[b + 1] - seq) / per;
+  const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
+  float o[VEC] = {};
+  float m = -INFINITY, l = 0.f;
+  if (n > 0) {
+    const int G = ctas_used(p, T);
+    const long long u0 = seq + u * n, u1 = u0 + n;
+    // CTA c owns [c T / G, (c + 1) T / G): tile x is in CTA ((x + 1) G - 1) / T
+    const int c0 = (int)(((u0 + 1) * G - 1) / T), np = (int)((u1 * G - 1) / T) - c0 + 1;
+    if (np == 1) return;                                     // not cut: written by the CTA that worked on it
+    const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
+    const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
+    for (int i = lane; i < np; i += 32) m = fmaxf(m, ml[(size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h]);
+#pragma unroll
+    for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+    for (int i0 = 0; i0 < np; i0 += 32) {
+      const int i = i0 + lane;
+      float f = 0.f, lj = 0.f;
+      if (i < np) {
+        const float* q = ml + (size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h;
+        lj = q[NH];
+        // applied twice: M contains the scales, the square may be below fp32.  A piece without a seen key has no weight
+        f = lj == 0.f ? 0.f : exp2f(0.5f * (q[0] - m));
+      }
+      l += warp_sum(f * lj * f);
+      const int cnt = min(np - i0, 32);
+#pragma unroll 8
+      for (int k = 0; k < cnt; ++k) {
+        const float w = __shfl_sync(0xffffffffu, f, k);
+        const float* src = p.part + (size_t)(2 * (c0 + i0 + k) + (i0 + k == 0 ? first : 0)) * NH * DS + x;
+        float v[VEC];
+        if constexpr (VEC == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
+        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) o[e] = w == 0.f ? o[e] : fmaf(w * v[e], w, o[e]);        // without weight: may be 0 * NaN
+      }
+    }
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
+#pragma unroll
+  for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
+  if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
+}
+
+template <int DS, int NH>
+int paged8_combine_launch(const Paged8Params& P, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)((long long)P.B * P.Hkv * P.n_blk * (NH * DS / (DS >= 128 ? 1024 : 512))));
+  cfg.blockDim = dim3(256);
+  cfg.stream = stream;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = at; cfg.numAttrs = 1;
+  if (cudaLaunchKernelEx(&cfg, paged8_combine_kernel<DS, NH>, P) != cudaSuccess) return LCA_ERR_CUDA;
+  note_launch();
+  return LCA_OK;
+}
+
+int attn_paged8_pair_launch(Paged8Params& P, cudaStream_t stream);      // MLA shape, blocks of 128 rows on CTA pairs
+int attn_paged8_pair_take_status();
+
+}  // namespace lca

@@ -490,14 +490,14 @@ bool make_tensor_map_chunks(CUtensorMap* map, const void* ptr, int chunks, long 
             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// Pages of 8-bit codes, [blocks][page][d] (a block is one KV head's rows of one page): box of a whole page's rows and
-// `box_d` (64 or 128) columns, swizzled by rows of that width.  Block number `blocks` is outside: it reads as zeros.
-bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d) {
+// Pages of 8-bit codes, [blocks][page][d] (a block is one KV head's rows of one page): box of `box_rows` rows of a
+// page and `box_d` (64 or 128) columns, swizzled by rows of that width.  Block number `blocks` is outside: it reads as zeros.
+bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d, int box_rows) {
   EncodeTiledFn fn = encode_fn();
   if (!fn || !ptr) return false;
   cuuint64_t dims[3] = {(cuuint64_t)d, (cuuint64_t)page, (cuuint64_t)blocks};
   cuuint64_t strides[2] = {(cuuint64_t)d, (cuuint64_t)d * page};
-  cuuint32_t box[3] = {(cuuint32_t)box_d, (cuuint32_t)page, 1};
+  cuuint32_t box[3] = {(cuuint32_t)box_d, (cuuint32_t)box_rows, 1};
   cuuint32_t estr[3] = {1, 1, 1};
   return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
             box_d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
