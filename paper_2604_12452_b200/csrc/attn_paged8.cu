@@ -600,7 +600,7 @@ static int paged8_grid(const lca_params* p, int nh) {
 }
 size_t attn_paged8_workspace_bytes(const lca_params* p, int q_len) {
   const int nh = paged8_rows_per_tile(p, q_len), grid = paged8_grid(p, nh);
-  return (size_t)2 * grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float) + ((size_t)p->batch + 1) * sizeof(long long) + 64;
+  return (size_t)2 * grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float) + ((size_t)p->batch + 2) * sizeof(long long) + 64;
 }
 
 template <class PL>
@@ -641,9 +641,10 @@ int attn_paged8_launch(const Paged8Attn& a) {
   P.n_blk = (int)(((long long)P.q_len * P.rep + nh - 1) / nh);
   P.grid = paged8_grid(p, nh); P.min_tiles = 2;
   P.scale_log2 = p->softmax_scale * 1.4426950408889634f; P.bias_log2 = p->rep_logit_bias * 1.4426950408889634f;
-  P.part = static_cast<float*>(a.ws);
+  P.part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(a.ws) + 31) & ~(uintptr_t)31);
+  P.out_wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;
   const size_t part_bytes = (size_t)2 * P.grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float);
-  P.prefix = reinterpret_cast<long long*>(static_cast<char*>(a.ws) + (part_bytes + 15) / 16 * 16);
+  P.prefix = reinterpret_cast<long long*>(reinterpret_cast<char*>(P.part) + (part_bytes + 15) / 16 * 16);
   if ((long long)P.B * P.Hkv * P.n_blk * ((long long)nh * p->d_sem / 512) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   if (mla) return p->d_sem == 512 ? paged8_launch_rows<true, 512, 64>(P, nh, a.stream) : paged8_launch_rows<true, 128, 64>(P, nh, a.stream);
   return p->d_sem == 128 ? paged8_launch_rows<false, 128, 128>(P, nh, a.stream) : paged8_launch_rows<false, 64, 64>(P, nh, a.stream);

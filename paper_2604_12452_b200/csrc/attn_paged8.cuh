@@ -20,8 +20,9 @@ struct Paged8Params {
   const int32_t* n_rep; const int32_t* n_tok;
   bf16* out; float* lse;
   float* part;                // [2 * grid][NH][DS] partial O, then [2 * grid][2][NH] M and l
-  long long* prefix;          // [B + 1] tiles before each sequence (all units), written by CTA 0
+  long long* prefix;          // [B + 2] tiles before each sequence (all units), then 1 where every unit has a CTA; written by CTA 0
   int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, min_tiles, grid;   // grid: CTAs (pairs of them) that share the line
+  int out_wide;               // out is 32-byte aligned
   float scale_log2, bias_log2;
 };
 
@@ -73,31 +74,54 @@ struct Walk {
 // The range of CTA (or CTA pair) `id`: thread i sums the tiles of sequences [i q, (i + 1) q); every thread of the CTA calls it.
 // Leaves the first sequence in *s_b, the offset inside it and the tiles of the range in s_off[0 .. 1]; ends with a barrier
 // still to come.  CTA 0 of the grid writes the prefix sums for the merging kernel.
+// Where there are no more units than CTAs and the longest is at most WHOLE_SLACK tiles above the mean of all CTAs, every unit
+// has a CTA of its own: a cut costs a second query load, a partial result and its merging, about as much as that many tiles.
+static constexpr int WHOLE_SLACK = 8;
 template <int THREADS>
 __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long long* s_warp, int* s_b, long long* s_off) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long upu = (long long)p.Hkv * p.n_blk;
   const int q = (p.B + THREADS - 1) / THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
   long long sum = 0;
-  for (int b = lo; b < hi; ++b) sum += (long long)tile_span(p, b).n * upu;
+  int longest = 0;
+#pragma unroll 1
+  for (int b = lo; b < hi; ++b) { const int n = tile_span(p, b).n; sum += (long long)n * upu; longest = max(longest, n); }
   long long inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
-  if (lane == 31) s_warp[warp] = inc;
+  longest = __reduce_max_sync(0xffffffffu, longest);
+  if (lane == 31) s_warp[warp] = inc | (long long)longest << 40;       // fewer than 2^40 tiles
   __syncthreads();
   long long T = 0, before = inc - sum;
-  for (int w = 0; w < THREADS / 32; ++w) { if (w < warp) before += s_warp[w]; T += s_warp[w]; }
+  longest = 0;
+#pragma unroll 1
+  for (int w = 0; w < THREADS / 32; ++w) {
+    const long long v = s_warp[w], n = v & ((1ll << 40) - 1);
+    if (w < warp) before += n;
+    T += n;
+    longest = max(longest, (int)(v >> 40));
+  }
   const int G = ctas_used(p, T);
-  long long s0 = 0, s1 = 0;
-  if (id < G) { s0 = (long long)id * T / G; s1 = ((long long)id + 1) * T / G; }
+  const bool own = (long long)p.B * upu <= p.grid && longest <= T / p.grid + WHOLE_SLACK;
   if (blockIdx.x == 0) {
     long long at = before;
+#pragma unroll 1
     for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (long long)tile_span(p, b).n * upu; }
-    if (tid == 0) p.prefix[p.B] = T;
+    if (tid == 0) { p.prefix[p.B] = T; p.prefix[p.B + 1] = own; }
   }
+  if (own) {
+    if (tid == 0) {
+      const int b = min((int)(id / upu), p.B - 1), n = id < p.B * upu ? tile_span(p, b).n : 0;
+      *s_b = b; s_off[0] = (id % upu) * n; s_off[1] = n;
+    }
+    return;
+  }
+  long long s0 = 0, s1 = 0;
+  if (id < G) { s0 = (long long)id * T / G; s1 = ((long long)id + 1) * T / G; }
   if (s1 > s0 && s0 >= before && s0 < before + sum) {        // exactly one thread
     long long at = before;
     int b = lo;
+#pragma unroll 1
     while (true) {
       const long long n = (long long)tile_span(p, b).n * upu;
       if (s0 < at + n) break;
@@ -201,11 +225,12 @@ __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_consta
   float o[VEC] = {};
   float m = -INFINITY, l = 0.f;
   if (n > 0) {
+    if (p.prefix[p.B + 1]) return;                           // not cut: written by the CTA that worked on it
     const int G = ctas_used(p, T);
     const long long u0 = seq + u * n, u1 = u0 + n;
     // CTA c owns [c T / G, (c + 1) T / G): tile x is in CTA ((x + 1) G - 1) / T
     const int c0 = (int)(((u0 + 1) * G - 1) / T), np = (int)((u1 * G - 1) / T) - c0 + 1;
-    if (np == 1) return;                                     // not cut: written by the CTA that worked on it
+    if (np == 1) return;
     const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
     const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
     for (int i = lane; i < np; i += 32) m = fmaxf(m, ml[(size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h]);

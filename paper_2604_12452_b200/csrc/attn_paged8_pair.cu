@@ -276,7 +276,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
     // this warp's 16 rows of the unit's queries, as two terms, where S reads them
     auto load_q = [&](const Walk& u) {
       const int n_rows = p.q_len * p.rep - u.blk * ROWS;
-#pragma unroll 2
+#pragma unroll 4
       for (int r = quad; r < 64; r += 4) {
         const int rg = 64 * (int)rank + r, gr = u.blk * ROWS + rg, qt = gr / p.rep;
         const size_t row = ((size_t)u.b * p.q_len + qt) * p.Hq + (gr - qt * p.rep);
@@ -388,32 +388,15 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
         const float d = raise ? top - PAGED8_T_BITS : 0.f, factor = raise && !unset ? ex2(-d) : 1.f;
         m += d;
         l *= factor;
-        if (j > 0) {                                         // O is complete up to the previous tile, its weights have been read
-          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
-          if (!ok) fail(ERR_WAIT_O_DONE);
-          __syncwarp();
-          if (__any_sync(0xffffffffu, factor != 1.f)) {
-            tc_fence_after();
-#pragma unroll 1
-            for (int q = 0; q < 8; ++q) {
-              uint32_t o[32];
-              tmem_ld32(tmem + lane_base + q * 32, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
-              tmem_st32(tmem + lane_base + q * 32, o);
-            }
-            tmem_wait_st();
-          }
-        }
         unset = unset && !raise;
+        // The weights depend on S and the maximum only: they are packed while O of the previous tile is still running
+        uint32_t wh[16], wl[16];
         const uint64_t d2 = pack_f32x2(-d, -d), neg2 = pack_f32x2(-1.f, -1.f), split2 = pack_f32x2(2097153.f, 2097153.f);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float4 f = fact[q];
           const uint64_t ft2 = pack_f32x2(f.z, f.z);
           uint64_t sum2 = 0;
-          uint32_t wh[4], wl[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             float hi[4], lo[4];
@@ -434,15 +417,36 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
               unpack_f32x2(h, hi[2 * k], hi[2 * k + 1]);
               unpack_f32x2(r, lo[2 * k], lo[2 * k + 1]);
             }
-            wh[i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
-            wl[i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
+            wh[4 * q + i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
+            wl[4 * q + i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
           }
           float a, b;
           unpack_f32x2(sum2, a, b);
           l = fmaf(a + b, f.w, l);
+        }
+        if (j > 0) {                                         // O is complete up to the previous tile, its weights have been read
+          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
+          if (!ok) fail(ERR_WAIT_O_DONE);
+          __syncwarp();
+          if (__any_sync(0xffffffffu, factor != 1.f)) {
+            tc_fence_after();
+#pragma unroll 1
+            for (int q = 0; q < 8; ++q) {
+              uint32_t o[32];
+              tmem_ld32(tmem + lane_base + q * 32, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+              tmem_st32(tmem + lane_base + q * 32, o);
+            }
+            tmem_wait_st();
+          }
+        }
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
           unsigned char* dst = smem + OFF_P + swz<128>(rl, 4 * half_no + q);
-          *reinterpret_cast<uint4*>(dst) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-          *reinterpret_cast<uint4*>(dst + P_TERM) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+          *reinterpret_cast<uint4*>(dst) = make_uint4(wh[4 * q], wh[4 * q + 1], wh[4 * q + 2], wh[4 * q + 3]);
+          *reinterpret_cast<uint4*>(dst + P_TERM) = make_uint4(wl[4 * q], wl[4 * q + 1], wl[4 * q + 2], wl[4 * q + 3]);
         }
         if (partial(w, j)) {
           ok = rank == 0 ? mbar_wait(VFULL(g & 1), (g >> 1) & 1, abort_flag) : mbar_wait(VLOCAL(g & 1), (v_phase >> (g & 1)) & 1, abort_flag);
@@ -490,17 +494,19 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
         if (!whole) {
           float* dst = p.part + (part * ROWS + rg) * DS + col;
 #pragma unroll
-          for (int v = 0; v < 8; ++v)
-            reinterpret_cast<uint4*>(dst)[v] = make_uint4(o[4 * v], o[4 * v + 1], o[4 * v + 2], o[4 * v + 3]);
+          for (int v = 0; v < 4; ++v) {
+            const uint32_t x[8] = {o[8 * v], o[8 * v + 1], o[8 * v + 2], o[8 * v + 3], o[8 * v + 4], o[8 * v + 5], o[8 * v + 6], o[8 * v + 7]};
+            st_global_32B(dst + 8 * v, x, true);             // part is 32-byte aligned
+          }
         } else if (row_valid) {
           bf16* dst = p.out + row * DS + col;
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
-            uint32_t x[4];
+          for (int v = 0; v < 2; ++v) {
+            uint32_t x[8];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              x[e] = l == 0.f ? 0u : pack_bf16x2(__uint_as_float(o[8 * v + 2 * e]) * inv, __uint_as_float(o[8 * v + 2 * e + 1]) * inv);   // no key: O may be 0 * NaN
-            reinterpret_cast<uint4*>(dst)[v] = make_uint4(x[0], x[1], x[2], x[3]);
+            for (int e = 0; e < 8; ++e)                      // no key: O may be 0 * NaN
+              x[e] = l == 0.f ? 0u : pack_bf16x2(__uint_as_float(o[16 * v + 2 * e]) * inv, __uint_as_float(o[16 * v + 2 * e + 1]) * inv);
+            st_global_32B(dst + 16 * v, x, p.out_wide != 0);
           }
         }
       }
