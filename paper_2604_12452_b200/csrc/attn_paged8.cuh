@@ -132,16 +132,21 @@ __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long
   if (tid == 0 && s1 <= s0) { *s_b = 0; s_off[0] = 0; s_off[1] = 0; }
 }
 
-// Splits the 8 bf16 values of `v` times f into two e4m3 terms.
+// Splits the 8 bf16 values of `v` times f into two e4m3 terms.  By way of f16, which holds the products (below 2^8, eight
+// significant bits, nothing lost above 2^-24), the first term and what it leaves exactly.
 __device__ __forceinline__ void split_e4m3(const uint4& v, float f, uint32_t (&hi)[2], uint32_t (&lo)[2]) {
   const uint32_t x[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
-    const float a0 = __uint_as_float(x[2 * k] << 16) * f, a1 = __uint_as_float(x[2 * k] & 0xffff0000u) * f;
-    const float a2 = __uint_as_float(x[2 * k + 1] << 16) * f, a3 = __uint_as_float(x[2 * k + 1] & 0xffff0000u) * f;
-    hi[k] = e4m3x4_from_float(a0, a1, a2, a3);
-    const float4 h = e4m3x4_to_float4(hi[k]);
-    lo[k] = e4m3x4_from_float(a0 - h.x, a1 - h.y, a2 - h.z, a3 - h.w);
+    uint32_t h = 0, l = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint32_t w = x[2 * k + i];
+      const __half2 a = __floats2half2_rn(__uint_as_float(w << 16) * f, __uint_as_float(w & 0xffff0000u) * f);
+      const uint32_t hc = e4m3x2_from_half2(a), lc = e4m3x2_from_half2(__hsub2(a, half2_from_e4m3x2(hc)));
+      h |= hc << (16 * i); l |= lc << (16 * i);
+    }
+    hi[k] = h; lo[k] = l;
   }
 }
 __device__ __forceinline__ uint32_t max_abs_bf16(const uint4& v) {

@@ -49,6 +49,10 @@ __device__ __forceinline__ void umma_f8_pair_elected(uint32_t leader, uint32_t d
       "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
 }
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
 // bits [0, n) of a word of 64; n may be anything
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
@@ -67,6 +71,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
   auto GFULL = [&](uint32_t i) { return bars + 128 + 8 * i; };
   auto GEMPTY = [&](uint32_t i) { return bars + 144 + 8 * i; };
   auto VLOCAL = [&](uint32_t i) { return bars + 160 + 8 * i; };          // odd CTA, values of a tile present in part, per buffer
+  const uint32_t QRAW = bars + 176, QDONE = bars + 184;      // queries landed as bf16; ... split, the value buffers are free again
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + OFF_SCALAR);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + OFF_SCALAR + 4);
   int* s_b = reinterpret_cast<int*>(smem + OFF_SCALAR + 8);
@@ -82,7 +87,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
 
   if (threadIdx.x == 0) {
     mbar_init(QFULL, 129); mbar_init(PFULL, 129);            // 128 threads of the even CTA and the odd CTA's forwarder
-    mbar_init(PVDONE, 1); mbar_init(QLOCAL, 128); mbar_init(PLOCAL, 128);
+    mbar_init(PVDONE, 1); mbar_init(QLOCAL, 128); mbar_init(PLOCAL, 128); mbar_init(QRAW, 1); mbar_init(QDONE, 128);
     for (int i = 0; i < 2; ++i) {
       mbar_init(SFULL(i), 1); mbar_init(KFULL(i), 1); mbar_init(KEMPTY(i), 1); mbar_init(VFULL(i), 1); mbar_init(VEMPTY(i), 1); mbar_init(VLOCAL(i), 1);
     }
@@ -116,9 +121,15 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
     const bool keys = warp == 0;
     const int box = min(p.page, 64);                                                   // rows of a request
     const int n_req = (keys ? 64 : 128) / box;                                         // per chunk
-    uint32_t g = 0, bat0 = 0;
+    uint32_t g = 0, bat0 = 0, seg = 0;
     bool ok = !*abort_flag;
     while (ok && w.next(p)) {
+      if (!keys) {                                           // the queries of the piece pass through the value buffers
+        ok = mbar_wait(QDONE, seg & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) { if (lane == 0) fail(ERR_WAIT_Q); break; }
+        ++seg;
+      }
       for (int j = 0; j < w.n && ok; ++j, ++g) {
         const uint32_t bat = bat0 + (uint32_t)(j >> 2), ring = bat % BATCHES, buf = g & 1;
         if ((j & 3) == 0) ok = mbar_wait(GFULL(ring), (bat / BATCHES) & 1, abort_flag);
@@ -271,25 +282,37 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
     const int quad = warp & 3, ln = quad * 32 + lane, rl = ln & 63, half_no = ln >> 6;   // TMEM lane; row of this CTA, key half
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     const uint32_t q_bar = rank == 0 ? QFULL : QLOCAL, p_bar = rank == 0 ? PFULL : PLOCAL;
-    uint32_t g = 0, bat0 = 0, v_phase = 0;                   // v_phase: phase of VLOCAL(0), VLOCAL(1) in bits 0, 1
+    uint32_t g = 0, bat0 = 0, v_phase = 0, seg = 0;          // v_phase: phase of VLOCAL(0), VLOCAL(1) in bits 0, 1
     bool ok = true, first_piece = true;
-    // this warp's 16 rows of the unit's queries, as two terms, where S reads them
-    auto load_q = [&](const Walk& u) {
-      const int n_rows = p.q_len * p.rep - u.blk * ROWS;
-#pragma unroll 4
-      for (int r = quad; r < 64; r += 4) {
-        const int rg = 64 * (int)rank + r, gr = u.blk * ROWS + rg, qt = gr / p.rep;
+    // The queries of a piece come as bf16 rows by bulk copies into the value and weight buffers, which nothing uses between two
+    // pieces, and are split from there: the loop that splits them is then short (loaded straight into registers, several rows
+    // at a time to cover the latency, its unrolled code had to be fetched once per launch and took 14000 clocks).
+    auto start_q = [&](const Walk& u) {
+      const int valid = min(max(p.q_len * p.rep - u.blk * ROWS - 64 * (int)rank, 0), 64);      // rows of this CTA
+      if (ln == 0) mbar_expect_tx(QRAW, valid * (DS + DP) * 2);
+      if (rl < valid) {
+        const int gr = u.blk * ROWS + 64 * (int)rank + rl, qt = gr / p.rep;
         const size_t row = ((size_t)u.b * p.q_len + qt) * p.Hq + (gr - qt * p.rep);
+        if (half_no == 0) bulk_load(base + OFF_V + rl * 1024, p.q_sem + row * DS, 1024, QRAW);
+        else bulk_load(base + OFF_V + 65536 + rl * 128, p.q_pos + row * DP, 128, QRAW);
+      }
+    };
+    auto finish_q = [&](const Walk& u) {
+      const int valid = min(max(p.q_len * p.rep - u.blk * ROWS - 64 * (int)rank, 0), 64);
+      ok = mbar_wait(QRAW, seg & 1, abort_flag);
+      if (!ok) fail(ERR_WAIT_Q);
+      __syncwarp();
+#pragma unroll 1
+      for (int r = quad; r < 64; r += 4) {
         uint4 v[3];
         uint32_t top = 0;
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
           const int c = lane + 32 * i;
           v[i] = make_uint4(0u, 0u, 0u, 0u);
-          if (rg < n_rows && c < 72) v[i] = *reinterpret_cast<const uint4*>(c < 64 ? p.q_sem + row * DS + 8 * c : p.q_pos + row * DP + 8 * (c - 64));
+          if (r < valid && c < 72) v[i] = *reinterpret_cast<const uint4*>(smem + OFF_V + (c < 64 ? r * 1024 + 16 * c : 65536 + r * 128 + 16 * (c - 64)));
+          top = max(top, max_abs_bf16(v[i]));
         }
-#pragma unroll
-        for (int i = 0; i < 3; ++i) top = max(top, max_abs_bf16(v[i]));
         top = __reduce_max_sync(0xffffffffu, top);
         const int e = query_exponent(top);
 #pragma unroll
@@ -307,11 +330,14 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
       }
       fence_proxy_async_smem();
       mbar_arrive(q_bar);
+      mbar_arrive(QDONE);
       asm volatile("bar.sync 1, 128;" ::: "memory");
+      ++seg;
     };
     bool more = w.next(p);
-    if (more) load_q(w);
+    if (more) start_q(w);
     while (more) {
+      finish_q(w);
       const PagedSpan sp = w.t.s;
       const int gr = w.blk * ROWS + 64 * (int)rank + rl, qt = gr / p.rep;
       const bool row_valid = gr < p.q_len * p.rep;
@@ -466,7 +492,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
         if (lane == 0 && ((j & 3) == 3 || j + 1 == w.n)) mbar_arrive(GEMPTY(ring));
       }
       bat0 += (uint32_t)(w.n + 3) >> 2;
-      // ---- the piece is done: its sum, the next unit's queries (S of this piece is complete), then O
+      // ---- the piece is done: its sum, the next unit's queries on their way, then O
       const bool whole = w.n == w.t.n;
       const size_t part = (size_t)2 * pair_id + (first_piece ? 0 : 1);
       const size_t row = ((size_t)w.b * p.q_len + qt) * p.Hq + (gr - qt * p.rep);
@@ -477,11 +503,11 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
       asm volatile("bar.sync 1, 128;" ::: "memory");
       l += s_red[ln ^ 64];
       asm volatile("bar.sync 1, 128;" ::: "memory");
-      more = w.next(p);
-      if (more) load_q(w);
       ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
+      more = w.next(p);
+      if (more) start_q(w);
       tc_fence_after();
       const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll 1

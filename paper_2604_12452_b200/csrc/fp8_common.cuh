@@ -32,6 +32,17 @@ __device__ __forceinline__ float4 e4m3x4_to_float4(uint32_t v) {
   const float2 x = __half22float2(*reinterpret_cast<__half2*>(&lo)), y = __half22float2(*reinterpret_cast<__half2*>(&hi));
   return make_float4(x.x, x.y, y.x, y.y);
 }
+// two f16 values <-> two codes in the low half of a word
+__device__ __forceinline__ uint32_t e4m3x2_from_half2(__half2 v) {
+  unsigned short r;
+  asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(*reinterpret_cast<uint32_t*>(&v)));
+  return r;
+}
+__device__ __forceinline__ __half2 half2_from_e4m3x2(uint32_t c) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"((unsigned short)c));
+  return *reinterpret_cast<__half2*>(&r);
+}
 // codes * f, rounded again
 __device__ __forceinline__ uint32_t e4m3x4_scale(uint32_t v, float f) {
   const float4 x = e4m3x4_to_float4(v);
