@@ -223,9 +223,16 @@ __device__ __forceinline__ int scale_exponent(uint32_t bits) {
   return max(E == 0 ? -1000 : e, PAGED8_MIN_EXP);
 }
 
+// Threads of a CTA: 9 to 18 vectors of 16 bytes of a page stay in a thread's registers.
+template <int D_SEM, bool MLA, int P>
+struct WritePlan {
+  static constexpr int NT = MLA && D_SEM == 512 && P >= 64 ? 512 : 256;
+  static constexpr int NV = (P * (MLA ? D_SEM + 64 : D_SEM) / 8 + NT - 1) / NT;
+  static constexpr int CTAS = NV * NT * 16 > 80 * 1024 ? 1 : NV > 9 || NT == 512 ? 2 : 4;
+};
 template <int D_SEM, int D_POS, bool MLA, int P>
-__global__ void __launch_bounds__(256) paged8_write_kernel(WriteArgs a) {
-  constexpr int NT = 256, DROW = MLA ? D_SEM + D_POS : D_SEM, V8 = DROW / 8, NV = (P * V8 + NT - 1) / NT;
+__global__ void __launch_bounds__(WritePlan<D_SEM, MLA, P>::NT, WritePlan<D_SEM, MLA, P>::CTAS) paged8_write_kernel(WriteArgs a) {
+  constexpr int NT = WritePlan<D_SEM, MLA, P>::NT, NV = WritePlan<D_SEM, MLA, P>::NV, DROW = MLA ? D_SEM + D_POS : D_SEM, V8 = DROW / 8;
   static_assert(MLA || D_SEM == D_POS, "K and V of one width");
   __shared__ uint32_t s_red[NT / 32];
   __shared__ int s_head[4];                                   // bit mask of the run heads of this window (window <= 128)
@@ -266,7 +273,6 @@ __global__ void __launch_bounds__(256) paged8_write_kernel(WriteArgs a) {
       const size_t block = (size_t)page * a.Hkv + hk;
       const float old = off > 0 ? scale[block] : 0.f;
       uint4 v[NV];
-      uint32_t top = 0;                                       // largest |x| of a finite element, as bf16 bits
 #pragma unroll
       for (int q = 0; q < NV; ++q) {
         const int x = q * NT + tid, r = x / V8, c = x % V8;
@@ -277,14 +283,24 @@ __global__ void __launch_bounds__(256) paged8_write_kernel(WriteArgs a) {
           v[q] = __ldcs(reinterpret_cast<const uint4*>(src));
         }
       }
+      // largest |x|, as bf16 bits, two at a time; where there is an infinity or a NaN, again over the finite elements
+      uint32_t top2 = 0;
 #pragma unroll
       for (int q = 0; q < NV; ++q) {
-        const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+        top2 = __vmaxu2(top2, v[q].x & 0x7fff7fffu); top2 = __vmaxu2(top2, v[q].y & 0x7fff7fffu);
+        top2 = __vmaxu2(top2, v[q].z & 0x7fff7fffu); top2 = __vmaxu2(top2, v[q].w & 0x7fff7fffu);
+      }
+      uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+      if (top >= 0x7f80u) {
+        top = 0;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
-          top = max(top, lo < 0x7f80u ? lo : 0u);
-          top = max(top, hi < 0x7f80u ? hi : 0u);
+        for (int q = 0; q < NV; ++q) {
+          const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
+            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+          }
         }
       }
       top = __reduce_max_sync(0xffffffffu, top);
@@ -326,10 +342,10 @@ __global__ void __launch_bounds__(256) paged8_write_kernel(WriteArgs a) {
 template <int D_SEM, int D_POS, bool MLA>
 static int write_page_size(const WriteArgs& a, int page, unsigned grid, cudaStream_t stream) {
   switch (page) {
-    case 16: paged8_write_kernel<D_SEM, D_POS, MLA, 16><<<grid, 256, 0, stream>>>(a); break;
-    case 32: paged8_write_kernel<D_SEM, D_POS, MLA, 32><<<grid, 256, 0, stream>>>(a); break;
-    case 64: paged8_write_kernel<D_SEM, D_POS, MLA, 64><<<grid, 256, 0, stream>>>(a); break;
-    default: paged8_write_kernel<D_SEM, D_POS, MLA, 128><<<grid, 256, 0, stream>>>(a); break;
+    case 16: paged8_write_kernel<D_SEM, D_POS, MLA, 16><<<grid, WritePlan<D_SEM, MLA, 16>::NT, 0, stream>>>(a); break;
+    case 32: paged8_write_kernel<D_SEM, D_POS, MLA, 32><<<grid, WritePlan<D_SEM, MLA, 32>::NT, 0, stream>>>(a); break;
+    case 64: paged8_write_kernel<D_SEM, D_POS, MLA, 64><<<grid, WritePlan<D_SEM, MLA, 64>::NT, 0, stream>>>(a); break;
+    default: paged8_write_kernel<D_SEM, D_POS, MLA, 128><<<grid, WritePlan<D_SEM, MLA, 128>::NT, 0, stream>>>(a); break;
   }
   note_launch();
   return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
