@@ -312,7 +312,8 @@ typedef struct lca_paged8 {
   int32_t* block_table;   /* [batch, table_width] */
   int32_t n_pages;        /* pages of the pool; n_pages * page_size < 2^31 */
   int32_t page_size;      /* 16, 32, 64 or 128 rows */
-  int32_t table_width;    /* entries per sequence; table_width * page_size < 2^31.  Rows behind the table are absent */
+  int32_t table_width;    /* entries per sequence; table_width * page_size and batch * table_width < 2^31.
+                           * Rows behind the table are absent */
 } lca_paged8;             /* a HOST structure of device pointers; pages 16-byte aligned */
 
 /* Block tables, free list and slot maps on the GPU, from the lengths of the requests.  The caller states how many

@@ -123,22 +123,28 @@ def _ptr(x):
     if isinstance(x, torch.Tensor):
         if not x.is_contiguous():
             raise ValueError("the LCA entry points take dense row-major tensors: call .contiguous() first")
-        return C.c_void_p(x.data_ptr())
-    return C.c_void_p(int(x))
+        return x.data_ptr()
+    return int(x)
 
 
 def _nbytes(x) -> int:
     return 0 if x is None else x.numel() * x.element_size()
 
 
+_has_cuda: Optional[bool] = None
+
+
 def _stream(stream):
     if stream is None:
-        if not torch.cuda.is_available():      # host-side validation calls on a GPU-less machine
-            return C.c_void_p(0)
-        return C.c_void_p(torch.cuda.current_stream().cuda_stream)
+        global _has_cuda
+        if _has_cuda is None:                  # asked once: the answer costs more than a small call's launch
+            _has_cuda = torch.cuda.is_available()
+        if not _has_cuda:                      # host-side validation calls on a GPU-less machine
+            return 0
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
     if isinstance(stream, torch.cuda.Stream):
-        return C.c_void_p(stream.cuda_stream)
-    return C.c_void_p(int(stream))
+        return stream.cuda_stream
+    return int(stream)
 
 
 # ------------------------------------------------------------------ raw entry points (same names)

@@ -440,7 +440,7 @@ static int check_paged(const lca_paged8* c) {
 static int check_paged_table(const lca_params* p, const lca_paged8* c, bool reps) {
   if (!c->block_table || c->table_width <= 0) return LCA_ERR_INVALID_ARG;
   // rows are numbered with 32 bits, and a tile of 128 of them may start at the last one
-  if ((int64_t)c->table_width * c->page_size > 0x7fffff00ll) return LCA_ERR_INVALID_ARG;
+  if ((int64_t)c->table_width * c->page_size > 0x7fffff00ll || (int64_t)c->table_width * p->batch > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
   if (reps && (p->group_size <= 0 || p->group_size % c->page_size != 0)) return LCA_ERR_INVALID_ARG;
   return LCA_OK;
 }

@@ -6,17 +6,17 @@
 namespace lca {
 
 // ------------------------------------------------------------------------------------------------ page tables, slots
-// One cluster does everything, in four phases with a cluster barrier between them, so that a decode step costs one
-// launch: (1) every CTA sums pages to give back, pages to take and new rows over all sequences (a few hundred bytes to
-// a few hundred KB from L2) and decides whether the update is possible; (2) pages that no present row needs are pushed
-// on the free stack; (3) pages are popped into the tables; (4) the slot of every new row is looked up.  A sequence's
-// share of each list starts at an exclusive prefix sum, so the result does not depend on how the work is spread.
-// Bound by latency (three dependent passes over the counters), not by its few bytes.
+// One cluster does everything, so that a decode step costs one launch: (1) every CTA sums pages to give back, pages to take
+// and new rows over all sequences (a few hundred bytes to a few hundred KB from L2) and decides whether the update is
+// possible; (2) pages that no present row needs are pushed on the free stack; (3) pages are popped into the tables; (4) the
+// slot of every new row is looked up.  A sequence's share of each list starts at an exclusive prefix sum, so the result does
+// not depend on how the work is spread.  Bound by latency (dependent passes over the counters and cluster barriers), not by
+// its bytes: one CTA for a decode step, sixteen for prompts (64 prompts of 5000 rows).
 struct PageArgs {
   const int32_t* n_rep; const int32_t* n_tok;
   int32_t* held_rep; int32_t* held_tok;
   int32_t* table; int32_t* free_pages; int32_t* n_free; int32_t* slot_map; int32_t* row_offsets; int32_t* status;
-  int B, g, page, width, n_pages, n_rows, per_seq;
+  int B, g, page_log2, width, n_pages, n_rows, per_seq;
 };
 
 // What one sequence gives back and takes: up to three ranges of table entries each, ascending and disjoint.
@@ -38,8 +38,9 @@ struct PageDelta {
 __device__ __forceinline__ PageDelta page_delta(const PageArgs& a, int b) {
   PageDelta d;
   const long long r0 = a.n_rep ? a.held_rep[b] : 0, r1 = a.n_rep ? a.n_rep[b] : 0, t0 = a.held_tok[b], t1 = a.n_tok[b];
-  const long long P = a.page, cap = (long long)a.width * P, g = a.g;
-  d.valid = r0 >= 0 && r1 >= 0 && r0 * g <= t0 && r1 * g <= t1 && t0 <= cap && t1 <= cap && (r1 >= r0 || t1 == 0);
+  const int lg = a.page_log2, up = (1 << lg) - 1;
+  const long long cap = (long long)a.width << lg, g0 = r0 * a.g, g1 = r1 * a.g;
+  d.valid = r0 >= 0 && r1 >= 0 && g0 <= t0 && g1 <= t1 && t0 <= cap && t1 <= cap && (r1 >= r0 || t1 == 0);
   if (!d.valid) {
 #pragma unroll
     for (int i = 0; i < 3; ++i) d.rel_lo[i] = d.rel_hi[i] = d.need_lo[i] = d.need_hi[i] = 0;
@@ -47,9 +48,9 @@ __device__ __forceinline__ PageDelta page_delta(const PageArgs& a, int b) {
     return d;
   }
   // pages held [0, a0) and [b0, c0), wanted [0, a1) and [b1, c1); a <= b <= c because representatives need no more pages
-  // than the tokens they stand for (page | group)
-  const int a0 = (int)((r0 + P - 1) / P), b0 = (int)(r0 * g / P), c0 = (int)((t0 + P - 1) / P);
-  const int a1 = (int)((r1 + P - 1) / P), b1 = (int)(r1 * g / P), c1 = (int)((t1 + P - 1) / P);
+  // than the tokens they stand for (page | group).  All of them below 2^31.
+  const int a0 = (int)((r0 + up) >> lg), b0 = (int)(g0 >> lg), c0 = (int)((t0 + up) >> lg);
+  const int a1 = (int)((r1 + up) >> lg), b1 = (int)(g1 >> lg), c1 = (int)((t1 + up) >> lg);
   d.rel_lo[0] = a1;                          d.rel_hi[0] = a0;              // end of a request
   d.rel_lo[1] = max(b0, a1);                 d.rel_hi[1] = min(c0, b1);     // tokens condensed meanwhile
   d.rel_lo[2] = max(max(b0, c1), max(b1, a1)); d.rel_hi[2] = c0;            // tokens taken back
@@ -57,31 +58,35 @@ __device__ __forceinline__ PageDelta page_delta(const PageArgs& a, int b) {
   d.need_lo[1] = max(a0, c0);                d.need_hi[1] = a1;             // ... and behind them
   d.need_lo[2] = max(b1, c0);                d.need_hi[2] = c1;             // new tokens
   d.r0 = (int)r0; d.r1 = (int)r1;
-  d.tok_first = (int)max(t0, r1 * g); d.n_tok = (int)t1;
+  d.tok_first = (int)max(t0, g1); d.n_tok = (int)t1;
   return d;
 }
 
-static const int PAGE_THREADS = 512;
+static const int PAGE_THREADS = 512, PAGE_WARPS = PAGE_THREADS / 32;
 
-// Exclusive prefix sums over the CTA of three counters; totals in the last three words of `sums`.
-__device__ __forceinline__ void scan3(long long (&v)[3], long long (&excl)[3], long long (&total)[3], long long (*sums)[3]) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, nw = PAGE_THREADS / 32;
-  long long inc[3];
+// Exclusive prefix sums over the CTA of pages (given back in the low, taken in the high half: each total is below 2^31, the
+// tables have fewer entries) and of rows; totals in tot.
+__device__ __forceinline__ void scan2(const unsigned long long (&v)[2], unsigned long long (&excl)[2], unsigned long long (&tot)[2],
+                                      unsigned long long (*sums)[2]) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  unsigned long long inc[2] = {v[0], v[1]};
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    long long x = v[k];
+  for (int o = 1; o < 32; o <<= 1)
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-    inc[k] = x;
-    if (lane == 31) sums[warp][k] = x;
-  }
+    for (int k = 0; k < 2; ++k) { const unsigned long long y = __shfl_up_sync(0xffffffffu, inc[k], o); if (lane >= o) inc[k] += y; }
+  if (lane == 31) { sums[warp][0] = inc[0]; sums[warp][1] = inc[1]; }
   __syncthreads();
+  // lane w of every warp: total of warp w
+  unsigned long long s[2] = {lane < PAGE_WARPS ? sums[lane][0] : 0ull, lane < PAGE_WARPS ? sums[lane][1] : 0ull};
 #pragma unroll
-  for (int k = 0; k < 3; ++k) {
-    long long before = 0, all = 0;
-    for (int w = 0; w < nw; ++w) { const long long s = sums[w][k]; if (w < warp) before += s; all += s; }
-    excl[k] = before + inc[k] - v[k];
-    total[k] = all;
+  for (int o = 1; o < PAGE_WARPS; o <<= 1)
+#pragma unroll
+    for (int k = 0; k < 2; ++k) { const unsigned long long y = __shfl_up_sync(0xffffffffu, s[k], o); if (lane >= o) s[k] += y; }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    tot[k] = __shfl_sync(0xffffffffu, s[k], PAGE_WARPS - 1);
+    const unsigned long long before = __shfl_sync(0xffffffffu, s[k], max(warp - 1, 0));
+    excl[k] = (warp ? before : 0ull) + inc[k] - v[k];
   }
   __syncthreads();
 }
@@ -91,31 +96,34 @@ __device__ __forceinline__ void cluster_barrier() {
 }
 
 __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
-  __shared__ long long sums[PAGE_THREADS / 32][3];
-  __shared__ int s_rel[PAGE_THREADS], s_need[PAGE_THREADS];
+  __shared__ unsigned long long sums[PAGE_WARPS][2];
+  __shared__ unsigned s_rel[PAGE_THREADS];                   // first rank of each sequence of a chunk
   const int cta = blockIdx.x, n_cta = gridDim.x;            // the grid is one cluster
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = PAGE_THREADS / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const bool single = a.B <= PAGE_THREADS;                   // one sequence per thread: its delta stays in registers
+  const long long n_free = a.n_free[0];
   // (1) totals
-  long long tot[3] = {0, 0, 0};
+  unsigned long long tot[2], ex[2];
+  PageDelta mine;
   int bad = 0;
   {
-    long long mine[3] = {0, 0, 0};
+    unsigned long long v[2] = {0, 0};
+#pragma unroll 1
     for (int b = tid; b < a.B; b += PAGE_THREADS) {
-      const PageDelta d = page_delta(a, b);
-      bad |= !d.valid;
-      const int nr = d.n_rows();
-      bad |= (a.per_seq > 0 && a.slot_map && nr > a.per_seq) ? 2 : 0;
-      mine[0] += d.n_rel(); mine[1] += d.n_need(); mine[2] += nr;
+      mine = page_delta(a, b);
+      const int nr = mine.n_rows();
+      bad |= (mine.valid ? 0 : 1) | (a.per_seq > 0 && a.slot_map && nr > a.per_seq ? 2 : 0);
+      v[0] += (unsigned long long)(unsigned)mine.n_rel() | (unsigned long long)(unsigned)mine.n_need() << 32;
+      v[1] += (unsigned long long)nr;
     }
-    long long ex[3];
-    scan3(mine, ex, tot, sums);
+    scan2(v, ex, tot, sums);
   }
-  const int any_invalid = __syncthreads_or(bad & 1), any_long = __syncthreads_or(bad & 2);
-  const long long n_free = a.n_free[0], have = n_free + tot[0];
+  const int any_bad = __syncthreads_or(bad & 1) ? 1 : __syncthreads_or(bad & 2) ? 2 : 0;
+  const long long n_rel = (long long)(tot[0] & 0xffffffffull), n_need = (long long)(tot[0] >> 32), have = n_free + n_rel;
   int status = 0;
-  if (any_invalid || n_free < 0 || have > a.n_pages) status = -1;
-  else if (any_long || (a.slot_map && a.per_seq == 0 && tot[2] > a.n_rows)) status = -2;
-  else if (tot[1] > have) status = (int)min(tot[1] - have, 0x7fffffffll);
+  if (any_bad == 1 || n_free < 0 || have > a.n_pages) status = -1;
+  else if (any_bad == 2 || (a.slot_map && a.per_seq == 0 && (long long)tot[1] > a.n_rows)) status = -2;
+  else if (n_need > have) status = (int)min(n_need - have, 0x7fffffffll);
   const long long gtid = (long long)cta * PAGE_THREADS + tid, gthreads = (long long)n_cta * PAGE_THREADS;
   if (status != 0) {                                         // nothing changes
     for (long long i = gtid; i < a.n_rows; i += gthreads) a.slot_map[i] = -1;
@@ -123,83 +131,133 @@ __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
     if (gtid == 0) a.status[0] = status;
     return;                                                  // every CTA takes this branch or none
   }
-  // (2) and (3): the sequences of a chunk share out over the warps of the cluster, 32 entries at a time
+  // (2) and (3)
+#pragma unroll 1
   for (int phase = 0; phase < 2; ++phase) {
-    long long base[3] = {0, 0, 0};
-    if (phase == 0 ? tot[0] > 0 || a.row_offsets : tot[1] > 0)
+    const long long work = phase == 0 ? n_rel : n_need;
+    unsigned long long base[2] = {0, 0};
+    if (work > 0 || (phase == 0 && a.row_offsets))
+#pragma unroll 1
       for (int c0 = 0; c0 < a.B; c0 += PAGE_THREADS) {
         const int b = c0 + tid;
-        long long v[3] = {0, 0, 0}, ex[3], chunk[3];
-        if (b < a.B) { const PageDelta d = page_delta(a, b); v[0] = d.n_rel(); v[1] = d.n_need(); v[2] = d.n_rows(); }
-        scan3(v, ex, chunk, sums);
+        if (!single) {                                       // (one chunk: the sums of (1) are its prefix sums)
+          unsigned long long v[2] = {0, 0}, chunk[2];
+          if (b < a.B) {
+            mine = page_delta(a, b);
+            v[0] = (unsigned long long)(unsigned)mine.n_rel() | (unsigned long long)(unsigned)mine.n_need() << 32;
+            v[1] = (unsigned long long)mine.n_rows();
+          }
+          scan2(v, ex, chunk, sums);
+          ex[0] += base[0]; ex[1] += base[1];
+          base[0] += chunk[0]; base[1] += chunk[1];
+        }
         if (phase == 0 && cta == 0 && a.row_offsets && b < a.B) {
           if (b == 0) a.row_offsets[0] = 0;
-          a.row_offsets[b + 1] = (int32_t)min(base[2] + ex[2] + v[2], 0x7fffffffll);
+          a.row_offsets[b + 1] = (int32_t)min((long long)ex[1] + mine.n_rows(), 0x7fffffffll);
         }
-        s_rel[tid] = (int)(base[0] + ex[0]); s_need[tid] = (int)(base[1] + ex[1]);
+        if (work == 0) continue;
+        const unsigned first = phase == 0 ? (unsigned)ex[0] : (unsigned)(ex[0] >> 32);
+        if (work <= 4 * PAGE_THREADS) {                      // a few entries: every thread its own sequence's (in CTA 0)
+          if (cta == 0 && b < a.B) {
+            int32_t* row = a.table + (size_t)b * a.width;
+            long long at = have - 1 - first;
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll 1
+              for (int e = phase == 0 ? mine.rel_lo[k] : mine.need_lo[k]; e < (phase == 0 ? mine.rel_hi[k] : mine.need_hi[k]); ++e, --at) {
+                if (phase == 0) { a.free_pages[at] = row[e]; row[e] = -1; }
+                else row[e] = a.free_pages[at];
+              }
+          }
+          continue;
+        }
+        // many: a warp of the cluster for every sequence of the chunk, 32 entries at a time
+        s_rel[tid] = first;
         __syncthreads();
-        for (int i = cta * n_warps + warp; i < PAGE_THREADS && c0 + i < a.B; i += n_cta * n_warps) {
+#pragma unroll 1
+        for (int i = cta * PAGE_WARPS + warp; i < PAGE_THREADS && c0 + i < a.B; i += n_cta * PAGE_WARPS) {
           const PageDelta d = page_delta(a, c0 + i);
           int32_t* row = a.table + (size_t)(c0 + i) * a.width;
-          long long rank = phase == 0 ? s_rel[i] : s_need[i];
+          long long at = have - 1 - s_rel[i];
 #pragma unroll
           for (int k = 0; k < 3; ++k) {
             const int lo = phase == 0 ? d.rel_lo[k] : d.need_lo[k], hi = phase == 0 ? d.rel_hi[k] : d.need_hi[k];
+#pragma unroll 4
             for (int e = lo + lane; e < hi; e += 32) {
-              const long long r = rank + (e - lo);
-              if (phase == 0) { a.free_pages[have - 1 - r] = row[e]; row[e] = -1; }
-              else row[e] = a.free_pages[have - 1 - r];
+              if (phase == 0) { a.free_pages[at - (e - lo)] = row[e]; row[e] = -1; }
+              else row[e] = a.free_pages[at - (e - lo)];
             }
-            rank += max(hi - lo, 0);
+            at -= max(hi - lo, 0);
           }
         }
-#pragma unroll
-        for (int k = 0; k < 3; ++k) base[k] += chunk[k];
         __syncthreads();
       }
-    cluster_barrier();
+    if (n_cta > 1) cluster_barrier(); else __syncthreads();
   }
-  // (4) slots
-  if (a.slot_map)
-    for (long long i = gtid; i < a.n_rows; i += gthreads) {
-      int b = -1;
-      long long k = 0;
-      if (a.per_seq > 0) { b = (int)(i / a.per_seq); k = i % a.per_seq; }
-      else if (i < tot[2]) { b = seq_of(a.row_offsets, a.B, i); k = i - a.row_offsets[b]; }
-      int slot = -1;
-      if (b >= 0) {
-        const PageDelta d = page_delta(a, b);
-        const int reps = max(d.r1 - d.r0, 0);
-        if (k < d.n_rows()) {
-          const int x = k < reps ? d.r0 + (int)k : d.tok_first + (int)k - reps;
-          const int page = a.table[(size_t)b * a.width + x / a.page];
-          if (page >= 0 && page < a.n_pages) slot = page * a.page + x % a.page;
+  // (4) slots.  Packed: a warp takes 256 rows at a time, finds the sequence of the first and walks on from there.
+  if (a.slot_map) {
+    auto slot_of = [&](int b, long long k, long long rows) {
+      if (k >= rows) return -1;
+      const int r0 = a.n_rep ? a.held_rep[b] : 0, r1 = a.n_rep ? a.n_rep[b] : 0, reps = max(r1 - r0, 0);
+      const int first = (int)max((long long)a.held_tok[b], (long long)r1 * a.g);
+      const int x = k < reps ? r0 + (int)k : first + (int)(k - reps);
+      const int page = a.table[(size_t)b * a.width + (x >> a.page_log2)];
+      return page >= 0 && page < a.n_pages ? (page << a.page_log2) | (x & ((1 << a.page_log2) - 1)) : -1;
+    };
+    if (a.per_seq > 0) {
+      for (long long i = gtid; i < a.n_rows; i += gthreads) {
+        const int b = (int)i / a.per_seq;
+        const int r0 = a.n_rep ? a.held_rep[b] : 0, r1 = a.n_rep ? a.n_rep[b] : 0;
+        const long long first = max((long long)a.held_tok[b], (long long)r1 * a.g);
+        a.slot_map[i] = slot_of(b, (int)i - b * a.per_seq, max(r1 - r0, 0) + max((long long)a.n_tok[b] - first, 0ll));
+      }
+    } else {
+      const long long R = (long long)tot[1];
+#pragma unroll 1
+      for (long long i0 = ((long long)cta * PAGE_WARPS + warp) * 256; i0 < a.n_rows; i0 += (long long)n_cta * PAGE_WARPS * 256) {
+        int b = i0 < R ? seq_of(a.row_offsets, a.B, i0) : 0;
+        long long lo = i0 < R ? a.row_offsets[b] : 0, hi = i0 < R ? a.row_offsets[b + 1] : 0;
+#pragma unroll 2
+        for (int u = 0; u < 8; ++u) {
+          const long long i = i0 + 32 * u + lane;
+          if (i >= a.n_rows) break;
+          int slot = -1;
+          if (i < R) {
+            while (i >= hi) { ++b; lo = hi; hi = a.row_offsets[b + 1]; }
+            slot = slot_of(b, i - lo, hi - lo);
+          }
+          a.slot_map[i] = slot;
         }
       }
-      a.slot_map[i] = slot;
     }
-  cluster_barrier();                                         // the held state is read until here
+  }
+  if (n_cta > 1) cluster_barrier(); else __syncthreads();    // the held state is read until here
   for (long long b = gtid; b < a.B; b += gthreads) {
     a.held_tok[b] = a.n_tok[b];
     if (a.n_rep) a.held_rep[b] = a.n_rep[b];
   }
-  if (gtid == 0) { a.n_free[0] = (int32_t)(have - tot[1]); a.status[0] = 0; }
+  if (gtid == 0) { a.n_free[0] = (int32_t)(have - n_need); a.status[0] = 0; }
 }
 
 int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* n_rep, const int32_t* n_tok, int32_t* held_rep,
                        int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map, int n_rows, int rows_per_seq,
                        int32_t* row_offsets, int32_t* status, cudaStream_t stream) {
+  const int lg = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
   PageArgs a = {n_rep, n_tok, held_rep, held_tok, c->block_table, free_pages, n_free, slot_map, row_offsets, status,
-                p->batch, n_rep ? p->group_size : 1, c->page_size, c->table_width, c->n_pages, slot_map ? n_rows : 0, rows_per_seq};
+                p->batch, n_rep ? p->group_size : 1, lg, c->table_width, c->n_pages, slot_map ? n_rows : 0, rows_per_seq};
+  // The host does not know how many pages change hands.  Slots for many rows, or many tables that may be given back, want
+  // many threads; otherwise the barriers of a cluster cost more than its threads bring.
+  const long long entries = (long long)p->batch * c->table_width;
+  const bool big = p->batch > PAGE_THREADS || a.n_rows > 8192 || (!slot_map && entries > 8192);
   cudaLaunchConfig_t cfg = {};
-  // one CTA for the few rows of a decode step (its barriers cost least), the largest portable cluster for prompts
-  cfg.gridDim = dim3((p->batch > 512 || a.n_rows > 4096 || n_rows == 0) ? 8 : 1);
+  cfg.gridDim = dim3(big ? 16 : 1);
   cfg.blockDim = dim3(PAGE_THREADS);
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = cfg.gridDim.x; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = 1;
+  if (big && cudaFuncSetAttribute(page_update_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LCA_ERR_CUDA;
   if (cudaLaunchKernelEx(&cfg, page_update_kernel, a) != cudaSuccess) return LCA_ERR_CUDA;
   note_launch();
   return LCA_OK;
