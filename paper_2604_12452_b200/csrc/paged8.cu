@@ -264,14 +264,14 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
 }
 
 // ------------------------------------------------------------------------------------------------------------- write
-// One CTA per run of rows inside a page and per block (GQA: K or V of one KV head; MLA: latent and rope key together).
-// The rows of a run (at most a page) stay in registers between the maximum and the rounding, so the input is read once.
-// HBM-bound: 2 bytes in, 1 byte out per element.
+// A run (rows of one page in one call) and a block (GQA: K or V of one KV head; MLA: latent and rope key together) at a time.
+// The rows of a run stay in registers between the maximum and the rounding, so the input is read once.  HBM-bound: 2 bytes
+// in, 1 byte out per element.
 struct WriteArgs {
   const bf16* rows_sem; const bf16* rows_pos; const int32_t* slots;
   uint8_t* pages_sem; uint8_t* pages_pos; float* scale_sem; float* scale_pos;
   long long n_rows, n_slots;
-  int Hkv, window;           // rows per CTA that may start a run
+  int Hkv, window;           // rows whose runs are handled together
 };
 
 // log2 of the scale for a block whose largest finite |x| has these bf16 bits: smallest e with |x| <= 448 * 2^e
@@ -281,150 +281,215 @@ __device__ __forceinline__ int scale_exponent(uint32_t bits) {
   return max(E == 0 ? -1000 : e, PAGED8_MIN_EXP);
 }
 
-// Threads of a CTA: 9 to 18 vectors of 16 bytes of a page stay in a thread's registers.
-template <int D_SEM, bool MLA, int P>
-struct WritePlan {
-  static constexpr int NT = MLA && D_SEM == 512 && P >= 64 ? 512 : 256;
-  static constexpr int NV = (P * (MLA ? D_SEM + 64 : D_SEM) / 8 + NT - 1) / NT;
-  static constexpr int CTAS = NV * NT * 16 > 80 * 1024 ? 1 : NV > 9 || NT == 512 ? 2 : 4;
-};
-template <int D_SEM, int D_POS, bool MLA, int P>
-__global__ void __launch_bounds__(WritePlan<D_SEM, MLA, P>::NT, WritePlan<D_SEM, MLA, P>::CTAS) paged8_write_kernel(WriteArgs a) {
-  constexpr int NT = WritePlan<D_SEM, MLA, P>::NT, NV = WritePlan<D_SEM, MLA, P>::NV, DROW = MLA ? D_SEM + D_POS : D_SEM, V8 = DROW / 8;
-  static_assert(MLA || D_SEM == D_POS, "K and V of one width");
-  __shared__ uint32_t s_red[NT / 32];
-  __shared__ int s_head[4];                                   // bit mask of the run heads of this window (window <= 128)
-  constexpr int PARTS = MLA ? 1 : 2;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int part = (int)(blockIdx.x % PARTS);
-  const int hk = (int)((blockIdx.x / PARTS) % a.Hkv);
-  const long long i0 = (long long)(blockIdx.x / ((unsigned)PARTS * a.Hkv)) * a.window;
-  const bf16* src_sem = part == 0 ? a.rows_sem : a.rows_pos;
-  uint8_t* dst_sem = part == 0 ? a.pages_sem : a.pages_pos;
-  float* scale = part == 0 ? a.scale_sem : a.scale_pos;
-  // a row starts a run unless it follows its predecessor inside the same page
-  if (tid < 128) {
-    const long long i = i0 + tid;
-    bool head = false;
-    if (tid < a.window && i < a.n_rows) {
-      const int s = a.slots[i], prev = i > 0 ? a.slots[i - 1] : -1;
-      head = s >= 0 && s < a.n_slots && !(prev >= 0 && s == prev + 1 && s % P != 0);
-    }
-    const unsigned m = __ballot_sync(0xffffffffu, head);
-    if (lane == 0) s_head[warp] = (int)m;
+// The runs that start in rows [i0, i0 + window): a row starts one unless it follows its predecessor inside the same page.
+// Bit k of the result: row i0 + 32 c + k (every lane of the warp gets the word of chunk c).
+template <int P>
+__device__ __forceinline__ unsigned run_heads(const WriteArgs& a, long long i0, int c) {
+  const int k = 32 * c + (int)(threadIdx.x & 31);
+  const long long i = i0 + k;
+  bool head = false;
+  if (k < a.window && i < a.n_rows) {
+    const int s = a.slots[i], prev = i > 0 ? a.slots[i - 1] : -1;
+    head = s >= 0 && s < a.n_slots && !(prev >= 0 && s == prev + 1 && s % P != 0);
   }
-  __syncthreads();
-  for (int w = 0; w < 4; ++w)
-    for (unsigned m = (unsigned)s_head[w]; m; m &= m - 1) {
-      const long long i = i0 + 32 * w + __ffs((int)m) - 1;
-      const int slot = a.slots[i], page = slot / P, off = slot % P;
-      // length of the run: every warp finds it by itself
-      int n = 0;
+  return __ballot_sync(0xffffffffu, head);
+}
+// Rows of the run that starts at row i with this slot (every lane of the warp).
+template <int P>
+__device__ __forceinline__ int run_length(const WriteArgs& a, long long i, int slot) {
+  const int room = P - slot % P;
+  int n = 0;
+#pragma unroll 1
+  for (int k = 0; k < P; k += 32) {
+    const int j = k + (int)(threadIdx.x & 31);
+    const bool in = j < room && i + j < a.n_rows && a.slots[i + j] == slot + j;
+    const unsigned ok = __ballot_sync(0xffffffffu, in);
+    if (ok != 0xffffffffu) return n + __ffs((int)~ok) - 1;
+    n += 32;
+  }
+  return n;
+}
+// Largest finite |x| of vectors of 8 bf16 values, as bf16 bits: two at a time, and again element by element where that finds
+// an infinity or a NaN.
+template <int N>
+__device__ __forceinline__ uint32_t max_finite(const uint4 (&v)[N]) {
+  uint32_t m = 0;
 #pragma unroll
-      for (int k = 0; k < P; k += 32) {
-        const int j = k + lane;
-        const bool in = j < P - off && i + j < a.n_rows && a.slots[i + j] == slot + j;
-        const unsigned ok = __ballot_sync(0xffffffffu, in);
-        n += ok == 0xffffffffu ? 32 : __ffs((int)~ok) - 1;
-        if (ok != 0xffffffffu) break;
+  for (int q = 0; q < N; ++q) {
+    m = __vmaxu2(m, v[q].x & 0x7fff7fffu); m = __vmaxu2(m, v[q].y & 0x7fff7fffu);
+    m = __vmaxu2(m, v[q].z & 0x7fff7fffu); m = __vmaxu2(m, v[q].w & 0x7fff7fffu);
+  }
+  uint32_t top = max(m & 0xffffu, m >> 16);
+  if (top >= 0x7f80u) {
+    top = 0;
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
+        top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
       }
-      const size_t block = (size_t)page * a.Hkv + hk;
-      const float old = off > 0 ? scale[block] : 0.f;
-      uint4 v[NV];
+    }
+  }
+  return top;
+}
+__device__ __forceinline__ uint2 quantise8(const uint4& v, float inv) {
+  return make_uint2(e4m3x4_from_bf16(v.x, v.y, inv), e4m3x4_from_bf16(v.z, v.w, inv));
+}
+// Rows [0, n16) units of 16 codes, times f, rounded again: thread `t` of `nt`.
+__device__ __forceinline__ void rescale_codes(uint8_t* codes, int n16, float f, int t, int nt) {
+#pragma unroll 1
+  for (int x = t; x < n16; x += nt) {
+    uint4* q = reinterpret_cast<uint4*>(codes) + x;
+    uint4 w = *q;
+    w.x = e4m3x4_scale(w.x, f); w.y = e4m3x4_scale(w.y, f); w.z = e4m3x4_scale(w.z, f); w.w = e4m3x4_scale(w.w, f);
+    *q = w;
+  }
+}
+
+// MLA: one CTA per run; with one KV head the rows of a run are contiguous in the input and in the page.
+template <int D_SEM, int P>
+struct WriteMla {
+  static constexpr int NT = D_SEM == 512 && P >= 64 ? 512 : 256;
+  static constexpr int NS = (P * D_SEM / 8 + NT - 1) / NT, NP = (P * 8 + NT - 1) / NT;       // vectors of a thread
+  static constexpr int CTAS = NS + NP > 12 ? 1 : NT == 512 ? 2 : 4;
+};
+template <int D_SEM, int P>
+__global__ void __launch_bounds__(WriteMla<D_SEM, P>::NT, WriteMla<D_SEM, P>::CTAS) paged8_write_mla_kernel(WriteArgs a) {
+  constexpr int NT = WriteMla<D_SEM, P>::NT, NS = WriteMla<D_SEM, P>::NS, NP = WriteMla<D_SEM, P>::NP, D_POS = 64;
+  __shared__ uint32_t s_red[NT / 32];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const long long i0 = (long long)blockIdx.x * a.window;
+#pragma unroll 1
+  for (int c = 0; 32 * c < a.window; ++c)
+#pragma unroll 1
+    for (unsigned heads = run_heads<P>(a, i0, c); heads; heads &= heads - 1) {        // the same in every warp
+      const long long i = i0 + 32 * c + __ffs((int)heads) - 1;
+      const int slot = a.slots[i], page = slot / P, off = slot % P, n = run_length<P>(a, i, slot);
+      const float old = off > 0 ? a.scale_sem[page] : 0.f;
+      const uint4* src_s = reinterpret_cast<const uint4*>(a.rows_sem + (size_t)i * D_SEM);
+      const uint4* src_p = reinterpret_cast<const uint4*>(a.rows_pos + (size_t)i * D_POS);
+      uint4 vs[NS], vp[NP];
 #pragma unroll
-      for (int q = 0; q < NV; ++q) {
-        const int x = q * NT + tid, r = x / V8, c = x % V8;
-        v[q] = make_uint4(0u, 0u, 0u, 0u);
-        if (x < n * V8) {
-          const size_t row = (size_t)(i + r) * a.Hkv + hk;
-          const bf16* src = (!MLA || c < D_SEM / 8) ? src_sem + row * D_SEM + 8 * c : a.rows_pos + row * D_POS + 8 * (c - D_SEM / 8);
-          v[q] = __ldcs(reinterpret_cast<const uint4*>(src));
-        }
-      }
-      // largest |x|, as bf16 bits, two at a time; where there is an infinity or a NaN, again over the finite elements
-      uint32_t top2 = 0;
+      for (int q = 0; q < NS; ++q) vs[q] = q * NT + tid < n * (D_SEM / 8) ? __ldcs(src_s + q * NT + tid) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-      for (int q = 0; q < NV; ++q) {
-        top2 = __vmaxu2(top2, v[q].x & 0x7fff7fffu); top2 = __vmaxu2(top2, v[q].y & 0x7fff7fffu);
-        top2 = __vmaxu2(top2, v[q].z & 0x7fff7fffu); top2 = __vmaxu2(top2, v[q].w & 0x7fff7fffu);
-      }
-      uint32_t top = max(top2 & 0xffffu, top2 >> 16);
-      if (top >= 0x7f80u) {
-        top = 0;
-#pragma unroll
-        for (int q = 0; q < NV; ++q) {
-          const uint32_t u[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
-            top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-          }
-        }
-      }
-      top = __reduce_max_sync(0xffffffffu, top);
+      for (int q = 0; q < NP; ++q) vp[q] = q * NT + tid < n * (D_POS / 8) ? __ldcs(src_p + q * NT + tid) : make_uint4(0u, 0u, 0u, 0u);
+      uint32_t top = __reduce_max_sync(0xffffffffu, max(max_finite(vs), max_finite(vp)));
       if (lane == 0) s_red[warp] = top;
       __syncthreads();                                        // also: every thread has read the block's old scale
 #pragma unroll
       for (int k = 0; k < NT / 32; ++k) top = max(top, s_red[k]);
-      const float want = exp2_int(scale_exponent(top));
-      const float now = off > 0 ? fmaxf(want, old) : want;
+      const float want = exp2_int(scale_exponent(top)), now = off > 0 ? fmaxf(want, old) : want;
+      uint8_t* dst_s = a.pages_sem + (size_t)page * P * D_SEM;
+      uint8_t* dst_p = a.pages_pos + (size_t)page * P * D_POS;
       if (off > 0 && now > old) {                             // the block's scale grows: its rows are rounded again
-        const float f = old / now;
-        for (int x = tid; x < off * (DROW / 16); x += NT) {
-          const int r = x / (DROW / 16), c = x % (DROW / 16);
-          uint8_t* q = (!MLA || c < D_SEM / 16) ? dst_sem + (block * P + r) * D_SEM + 16 * c
-                                                : a.pages_pos + (block * P + r) * D_POS + 16 * (c - D_SEM / 16);
-          uint4 w4 = *reinterpret_cast<const uint4*>(q);
-          w4.x = e4m3x4_scale(w4.x, f); w4.y = e4m3x4_scale(w4.y, f); w4.z = e4m3x4_scale(w4.z, f); w4.w = e4m3x4_scale(w4.w, f);
-          *reinterpret_cast<uint4*>(q) = w4;
-        }
+        rescale_codes(dst_s, off * (D_SEM / 16), old / now, tid, NT);
+        rescale_codes(dst_p, off * (D_POS / 16), old / now, tid, NT);
       }
       const float inv = 1.f / now;                            // exact: a power of two (unless `old` came from elsewhere)
+      uint2* out_s = reinterpret_cast<uint2*>(dst_s + (size_t)off * D_SEM);
+      uint2* out_p = reinterpret_cast<uint2*>(dst_p + (size_t)off * D_POS);
 #pragma unroll
-      for (int q = 0; q < NV; ++q) {
-        const int x = q * NT + tid, r = x / V8, c = x % V8;
-        if (x < n * V8) {
-          uint2 o;
-          o.x = e4m3x4_from_bf16(v[q].x, v[q].y, inv);
-          o.y = e4m3x4_from_bf16(v[q].z, v[q].w, inv);
-          uint8_t* dst = (!MLA || c < D_SEM / 8) ? dst_sem + (block * P + off + r) * D_SEM + 8 * c
-                                                 : a.pages_pos + (block * P + off + r) * D_POS + 8 * (c - D_SEM / 8);
-          *reinterpret_cast<uint2*>(dst) = o;
-        }
-      }
-      if (tid == 0) scale[block] = now;
+      for (int q = 0; q < NS; ++q) if (q * NT + tid < n * (D_SEM / 8)) out_s[q * NT + tid] = quantise8(vs[q], inv);
+#pragma unroll
+      for (int q = 0; q < NP; ++q) if (q * NT + tid < n * (D_POS / 8)) out_p[q * NT + tid] = quantise8(vp[q], inv);
+      if (tid == 0) a.scale_sem[page] = now;
       __syncthreads();                                        // s_red is used again by the next run
     }
 }
 
-template <int D_SEM, int D_POS, bool MLA>
-static int write_page_size(const WriteArgs& a, int page, unsigned grid, cudaStream_t stream) {
-  switch (page) {
-    case 16: paged8_write_kernel<D_SEM, D_POS, MLA, 16><<<grid, WritePlan<D_SEM, MLA, 16>::NT, 0, stream>>>(a); break;
-    case 32: paged8_write_kernel<D_SEM, D_POS, MLA, 32><<<grid, WritePlan<D_SEM, MLA, 32>::NT, 0, stream>>>(a); break;
-    case 64: paged8_write_kernel<D_SEM, D_POS, MLA, 64><<<grid, WritePlan<D_SEM, MLA, 64>::NT, 0, stream>>>(a); break;
-    default: paged8_write_kernel<D_SEM, D_POS, MLA, 128><<<grid, WritePlan<D_SEM, MLA, 128>::NT, 0, stream>>>(a); break;
+// GQA: a block is one KV head's keys or values of a page, at most 16 KB of input: one warp for 32 rows of it (two or four
+// warps for larger pages), eight warps with neighbouring heads in a CTA.  No barrier but those warps' own.
+template <int D, int P>
+__global__ void __launch_bounds__(256, 2) paged8_write_gqa_kernel(WriteArgs a) {
+  constexpr int WPB = P <= 32 ? 1 : P / 32, NT = 32 * WPB, V8 = D / 8, NV = P * V8 / NT;
+  __shared__ uint32_t s_red[8];
+  const int tid = threadIdx.x, warp = tid >> 5, group = warp / WPB, t = tid % NT;
+  const long long item = (long long)blockIdx.x * (8 / WPB) + group;
+  const int hk = (int)(item % a.Hkv), part = (int)((item / a.Hkv) & 1);
+  const long long i0 = item / a.Hkv / 2 * a.window;
+  if (i0 >= a.n_rows) return;
+  const bf16* src0 = part ? a.rows_pos : a.rows_sem;
+  uint8_t* pages = part ? a.pages_pos : a.pages_sem;
+  float* scale = part ? a.scale_pos : a.scale_sem;
+  auto group_barrier = [&]() {
+    if (WPB == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(group + 1), "n"(NT) : "memory");
+  };
+#pragma unroll 1
+  for (int c = 0; 32 * c < a.window; ++c)
+#pragma unroll 1
+    for (unsigned heads = run_heads<P>(a, i0, c); heads; heads &= heads - 1) {
+      const long long i = i0 + 32 * c + __ffs((int)heads) - 1;
+      const int slot = a.slots[i], page = slot / P, off = slot % P, n = run_length<P>(a, i, slot);
+      const size_t block = (size_t)page * a.Hkv + hk;
+      const float old = off > 0 ? scale[block] : 0.f;
+      const uint4* src = reinterpret_cast<const uint4*>(src0 + ((size_t)i * a.Hkv + hk) * D);
+      uint4 v[NV];
+#pragma unroll
+      for (int q = 0; q < NV; ++q) {
+        const int x = q * NT + t, r = x / V8;
+        v[q] = r < n ? __ldcs(src + (size_t)r * a.Hkv * V8 + x % V8) : make_uint4(0u, 0u, 0u, 0u);
+      }
+      uint32_t top = __reduce_max_sync(0xffffffffu, max_finite(v));
+      if (WPB > 1) {
+        if ((tid & 31) == 0) s_red[warp] = top;
+        group_barrier();                                      // also: every thread has read the block's old scale
+#pragma unroll
+        for (int k = 0; k < WPB; ++k) top = max(top, s_red[group * WPB + k]);
+      }
+      const float want = exp2_int(scale_exponent(top)), now = off > 0 ? fmaxf(want, old) : want;
+      uint8_t* dst = pages + block * P * D;
+      if (off > 0 && now > old) rescale_codes(dst, off * (D / 16), old / now, t, NT);        // the block's scale grows
+      const float inv = 1.f / now;
+      uint2* out = reinterpret_cast<uint2*>(dst + (size_t)off * D);
+#pragma unroll
+      for (int q = 0; q < NV; ++q) if (q * NT + t < n * V8) out[q * NT + t] = quantise8(v[q], inv);
+      group_barrier();                                        // the old scale has been read, s_red is used again
+      if (t == 0) scale[block] = now;
+    }
+}
+
+template <int D_SEM, bool MLA, int P>
+static int write_launch(const WriteArgs& a, long long windows, cudaStream_t stream) {
+  long long grid;
+  if constexpr (MLA) {
+    grid = windows;
+    if (grid <= 0x7fffffffll) paged8_write_mla_kernel<D_SEM, P><<<(unsigned)grid, WriteMla<D_SEM, P>::NT, 0, stream>>>(a);
+  } else {
+    constexpr int PER = 8 / (P <= 32 ? 1 : P / 32);
+    grid = (windows * a.Hkv * 2 + PER - 1) / PER;
+    if (grid <= 0x7fffffffll) paged8_write_gqa_kernel<D_SEM, P><<<(unsigned)grid, 256, 0, stream>>>(a);
   }
+  if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   note_launch();
   return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+template <int D_SEM, bool MLA>
+static int write_page_size(const WriteArgs& a, int page, long long windows, cudaStream_t stream) {
+  switch (page) {
+    case 16: return write_launch<D_SEM, MLA, 16>(a, windows, stream);
+    case 32: return write_launch<D_SEM, MLA, 32>(a, windows, stream);
+    case 64: return write_launch<D_SEM, MLA, 64>(a, windows, stream);
+    default: return write_launch<D_SEM, MLA, 128>(a, windows, stream);
+  }
 }
 
 int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* rows_sem, const void* rows_pos,
                         const int32_t* slot_map, long long n_rows, cudaStream_t stream) {
   const bool mla = p->variant == LCA_VARIANT_MLA;
-  const long long blocks = (long long)p->n_kv_heads * (mla ? 1 : 2);
   WriteArgs a = {(const bf16*)rows_sem, (const bf16*)rows_pos, slot_map, (uint8_t*)c->pages_sem, (uint8_t*)c->pages_pos, c->scale_sem,
                  c->scale_pos, n_rows, (long long)c->n_pages * c->page_size, p->n_kv_heads, 1};
-  // A decode step brings one row per page: one CTA per row, or a CTA would handle its runs one after the other.  A prompt
-  // brings whole pages: one CTA per page of rows, or most CTAs would find no run to start.
-  const long long per = n_rows * blocks / (148 * 8);
+  // A decode step brings one row per page: a CTA (a warp) per row, or it would handle its runs one after the other.  A prompt
+  // brings whole pages: one per page of rows, or most would find no run to start.  In between: what fills the GPU twice.
+  const long long per = n_rows * (mla ? 1 : 2 * p->n_kv_heads) / (mla ? 148 * 8 : 148 * 64);
   a.window = (int)(per < 1 ? 1 : (per > c->page_size ? c->page_size : per));
-  const long long grid = (n_rows + a.window - 1) / a.window * blocks;
-  if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
-  if (mla) return p->d_sem == 512 ? write_page_size<512, 64, true>(a, c->page_size, (unsigned)grid, stream)
-                                  : write_page_size<128, 64, true>(a, c->page_size, (unsigned)grid, stream);
-  return p->d_sem == 128 ? write_page_size<128, 128, false>(a, c->page_size, (unsigned)grid, stream)
-                         : write_page_size<64, 64, false>(a, c->page_size, (unsigned)grid, stream);
+  const long long windows = (n_rows + a.window - 1) / a.window;
+  if (mla) return p->d_sem == 512 ? write_page_size<512, true>(a, c->page_size, windows, stream)
+                                  : write_page_size<128, true>(a, c->page_size, windows, stream);
+  return p->d_sem == 128 ? write_page_size<128, false>(a, c->page_size, windows, stream)
+                         : write_page_size<64, false>(a, c->page_size, windows, stream);
 }
 
 // ------------------------------------------------------------------------------------------------------------ update
