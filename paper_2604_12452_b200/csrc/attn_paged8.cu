@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
   int* s_b = reinterpret_cast<int*>(misc + 264);
   long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
-  long long* s_warp = reinterpret_cast<long long*>(misc + 288);         // totals of up to 18 warps
+  long long* s_warp = reinterpret_cast<long long*>(misc + 288);         // totals of up to 18 warps, and 18 words
   float* s_qs = reinterpret_cast<float*>(misc + 512);
   float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
   int* s_lim = reinterpret_cast<int*>(s_f + NH);

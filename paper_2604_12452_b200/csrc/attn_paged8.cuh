@@ -71,7 +71,7 @@ struct Walk {
   }
 };
 
-// The range of CTA (or CTA pair) `id`: thread i sums the tiles of sequences [i q, (i + 1) q); every thread of the CTA calls it.
+// The range of CTA (or CTA pair) `id` (s_warp: room for 12 bytes a warp): thread i sums the tiles of sequences [i q, (i + 1) q); every thread of the CTA calls it.
 // Leaves the first sequence in *s_b, the offset inside it and the tiles of the range in s_off[0 .. 1]; ends with a barrier
 // still to come.  CTA 0 of the grid writes the prefix sums for the merging kernel.
 // Where there are no more units than CTAs and the longest is at most WHOLE_SLACK tiles above the mean of all CTAs, every unit
@@ -90,16 +90,16 @@ __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
   longest = __reduce_max_sync(0xffffffffu, longest);
-  if (lane == 31) s_warp[warp] = inc | (long long)longest << 40;       // fewer than 2^40 tiles
+  int* s_longest = reinterpret_cast<int*>(s_warp + THREADS / 32);
+  if (lane == 31) { s_warp[warp] = inc; s_longest[warp] = longest; }
   __syncthreads();
   long long T = 0, before = inc - sum;
   longest = 0;
 #pragma unroll 1
   for (int w = 0; w < THREADS / 32; ++w) {
-    const long long v = s_warp[w], n = v & ((1ll << 40) - 1);
-    if (w < warp) before += n;
-    T += n;
-    longest = max(longest, (int)(v >> 40));
+    if (w < warp) before += s_warp[w];
+    T += s_warp[w];
+    longest = max(longest, s_longest[w]);
   }
   const int G = ctas_used(p, T);
   const bool own = (long long)p.B * upu <= p.grid && longest <= T / p.grid + WHOLE_SLACK;

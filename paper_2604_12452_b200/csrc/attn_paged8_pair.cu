@@ -76,7 +76,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
   volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + OFF_SCALAR + 4);
   int* s_b = reinterpret_cast<int*>(smem + OFF_SCALAR + 8);
   long long* s_off = reinterpret_cast<long long*>(smem + OFF_SCALAR + 16);
-  long long* s_warp = reinterpret_cast<long long*>(smem + OFF_SCALAR + 32);          // 8
+  long long* s_warp = reinterpret_cast<long long*>(smem + OFF_SCALAR + 32);          // 8, and 8 words
   float* s_red = reinterpret_cast<float*>(smem + OFF_RED);                             // [2][128] maxima of even / odd tiles; sums
   float4* s_fact = reinterpret_cast<float4*>(smem + OFF_FACT);                         // per 16 rows: key factor (-1: no page), half, f_t, f_l
   int* s_page = reinterpret_cast<int*>(smem + OFF_PAGE);
