@@ -5,11 +5,11 @@
 // with e4m3 codes k, v and one scale for each page and KV head.  Everything is multiplied as 8-bit numbers:
 //   * q f = q_hi + q_lo, two e4m3 terms, f the power of two that brings the row's largest element into [128, 256).
 //     Four significant bits each: exact for every element above 2^-9 of the largest, otherwise off by 2^-17 of the largest.
-//   * t_i = 2^(y_i + log2 s_v(i) - M + 8) = t_hi + t_lo, t_hi e5m2 (the wide range), t_lo e4m3: relative error 2^-8 (a bf16
-//     weight has 2^-9 at best, 2^-8 at worst), and never more than 2^-10, i.e. 2^-18 of the largest weight.  That floor
-//     would round a long flat tail all the same way, so every key adds its own offset, one of 32 spread over the last
-//     place of t_lo, before the rounding: over a tile the tail keeps its weight to 1/64 of that place.
-//   M is the running maximum of y + log2 s_v over a split; it is raised only when a weight exceeds it by 2^3.  The row
+//   * t_i = 2^(y_i + log2 s_v(i) - M + 5) = t_hi + t_lo, two e4m3 terms again: relative error 2^-9 (a bf16 weight has 2^-9), and
+//     never more than 2^-10, i.e. 2^-15 of the largest weight.  That floor would round a long flat tail all the same way, so
+//     every key adds its own offset, one of 32 spread over the last place of t_lo, before the rounding: over a tile the tail
+//     keeps its weight to 1/64 of that place.
+//   M is the running maximum of y + log2 s_v over a split; it is raised only when a weight would exceed 2^8.75.  The row
 //   sum adds the weights without s_v in fp32, unrounded.
 #include <cstring>
 
@@ -137,17 +137,17 @@ struct Paged8Plan {
   static constexpr int PER_TILE = SHARED ? NK : NK + NV;     // slots a tile passes through
   static constexpr int SLOT = 16384;
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
-  static constexpr int P_BYTES = 128 * NH;                   // one term
-  static constexpr int TM_S = NV * NH, TM_USED = TM_S + 4 * NH;
+  static constexpr int P_BYTES = 128 * 2 * NH;               // per key the first terms of all rows, then the second ones
+  static constexpr int TM_S = 2 * NV * NH, TM_USED = TM_S + 4 * NH;        // O: for each 128 columns the two terms' sums side by side
   static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
   static constexpr int CTAS = (MLA && DS == 512) || TM_COLS == 512 ? 1 : 2;        // per SM
   static constexpr int GROUPS = NH / 16, SOFTMAX_WARPS = 4 * GROUPS, THREADS = 32 * (SOFTMAX_WARPS + 2);
   // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers first.
   static constexpr int MISC_BYTES = 512 + 4 * (5 * NH + 4 * NH + 2 * NH);
   static constexpr int BUDGET = (CTAS == 1 ? 227 * 1024 : 113 * 1024) - 1024;      // 1 KB to align the base
-  static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / SLOT;
+  static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - P_BYTES - MISC_BYTES) / SLOT;
   static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
-  static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
+  static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + P_BYTES;
   static constexpr int SMEM = OFF_MISC + MISC_BYTES + 1024;
   static_assert(SLOTS >= (SHARED ? 2 * NK : NV + 1) && SMEM <= 227 * 1024, "the tiles that S and O work on fit the ring");
 };
@@ -160,6 +160,8 @@ __device__ __forceinline__ bool group_any(int grp, bool v) {
                : "=r"(r) : "r"((uint32_t)v), "r"(grp + 1) : "memory");
   return r != 0;
 }
+
+static constexpr float T_MAX = 8.75f;                        // log2 of the largest weight: e4m3 ends at 448
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
@@ -249,7 +251,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
     // ----------------------------------------------------------------------------------------------------- MMA
     const uint32_t leader = elect_one();
     constexpr uint32_t ID_S = umma_idesc_f8(128, 2 * NH, 0, false, false);
-    constexpr uint32_t ID_HI = umma_idesc_f8(128, NH, 1, true, true), ID_LO = umma_idesc_f8(128, NH, 0, true, true);
+    constexpr uint32_t ID_O = umma_idesc_f8(128, 2 * NH, 0, true, true);
     int slot = 0;
     uint32_t phase = 0, g = 0, seg = 0;
     bool ok = true;
@@ -278,7 +280,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
       }
       umma_commit_elected(leader, SFULL + 8 * buf);
     };
-    const uint64_t p_hi = desc_rows(base + PL::OFF_P, NH, 128), p_lo = desc_rows(base + PL::OFF_P + PL::P_BYTES, NH, 128);
+    const uint64_t pd = desc_rows(base + PL::OFF_P, 2 * NH, 128);
     while (ok && w.next(p)) {
       ok = mbar_wait(QFULL, seg & 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
@@ -302,10 +304,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
           // lanes it feeds are never read
           const uint64_t ad = desc_rows(base + vs * PL::SLOT, PL::VW, 8192);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_hi, k * 2 * NH), ID_HI, (j > 0 || k > 0) ? 1u : 0u);
-            umma_f8_elected(leader, tmem + c * NH, desc_add(ad, k * 2 * PL::VW), desc_add(p_lo, k * 2 * NH), ID_LO, 1u);
-          }
+          for (int k = 0; k < 4; ++k)
+            umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (j > 0 || k > 0) ? 1u : 0u);
           umma_commit_elected(leader, EMPTY(vs));
           if (PL::SHARED) { if (++v_slot == PL::SLOTS) v_slot = 0; }
           else next_slot();
@@ -435,7 +435,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         }
 #pragma unroll
         for (int i = 0; i < 16; i += 2) zmax = max3(zmax, z[i], z[i + 1]);
-        const bool raise = group_any(grp, zmax + half > PAGED8_T_BITS + PAGED8_SLACK || unset);
+        const bool raise = group_any(grp, zmax + half > T_MAX || unset);
         if (raise) {
           // raise the maxima: per row the largest log2 t of the tile
 #pragma unroll
@@ -467,7 +467,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
           if (raise) {
             tc_fence_after();
 #pragma unroll 1
-            for (int c = 0; c < NV; ++c) {
+            for (int c = 0; c < 2 * NV; ++c) {
               uint32_t o[16];
               tmem_ld16(tmem + lane_base + c * NH + hb, o);
               tmem_wait_ld();
@@ -487,15 +487,16 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
             for (int k = 0; k < 4; ++k) {
               const float e = ex2(z[4 * i + k]), tt = e * f_t;
               l[4 * i + k] = fmaf(e, f_l, l[4 * i + k]);
-              hi[k] = __uint_as_float((__float_as_uint(tt) + 0x00100000u) & 0xffe00000u);     // three significant bits
+              const float h = __uint_as_float((__float_as_uint(tt) + 0x00080000u) & 0xfff00000u);      // four significant bits
+              hi[k] = tt < 0.015625f ? 0.f : h;              // below e4m3's normal range the second term takes it all
               lo[k] = (tt - hi[k]) + dither;
             }
-            wh[i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
+            wh[i] = e4m3x4_from_float(hi[0], hi[1], hi[2], hi[3]);
             wl[i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
           }
-          unsigned char* ph = base_ptr + PL::OFF_P + swz<NH>(t, grp);
-          *reinterpret_cast<uint4*>(ph) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
-          *reinterpret_cast<uint4*>(ph + PL::P_BYTES) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
+          unsigned char* ph = base_ptr + PL::OFF_P;
+          *reinterpret_cast<uint4*>(ph + swz<2 * NH>(t, grp)) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
+          *reinterpret_cast<uint4*>(ph + swz<2 * NH>(t, PL::GROUPS + grp)) = make_uint4(wl[0], wl[1], wl[2], wl[3]);
         }
         // Rows that were fetched with a page but are not present may hold anything; their weight is 0 and 0 * NaN is not.
         if (grp == 0 && ((unsigned)(part_r - row0) < 128u || (unsigned)(part_t - row0) < 128u)) {
@@ -550,9 +551,12 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
       tc_fence_after();
 #pragma unroll 1
       for (int c = 0; c < NV; ++c) {
-        uint32_t o[16];
-        tmem_ld16(tmem + lane_base + c * NH + hb, o);
+        uint32_t o[16], o2[16];
+        tmem_ld16(tmem + lane_base + c * 2 * NH + hb, o);
+        tmem_ld16(tmem + lane_base + c * 2 * NH + NH + hb, o2);
         tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) + __uint_as_float(o2[k]));
         const int d = c * 128 + t;
         if (DS >= 128 || t < DS) {
           if (whole) {

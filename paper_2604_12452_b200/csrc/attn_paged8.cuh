@@ -9,9 +9,9 @@
 namespace lca {
 using namespace tc;
 
-static constexpr float PAGED8_T_BITS = 6.f;         // a raised maximum puts the largest weight at 2^6 ...
-static constexpr float PAGED8_SLACK = 5.f;          // ... and it may grow to 2^11 before the maximum is raised again: t_hi up
-                                                    // to 2^11 leaves at most 2^8 to t_lo (e4m3 ends at 448)
+// A raised maximum puts the largest weight at 2^5; it may grow until its leading term is as large as its format allows before
+// the maximum is raised again.  The last place of the second term is 2^-9 at least.
+static constexpr float PAGED8_T_BITS = 5.f;
 
 struct Paged8Params {
   CUtensorMap sem, pos;       // [n_pages * Hkv, page, d] codes; boxes of one page x 128 (or 64) bytes

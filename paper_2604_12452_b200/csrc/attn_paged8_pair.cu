@@ -38,6 +38,7 @@ constexpr int OFF_PAGE = OFF_FACT + BATCHES * 32 * 16, OFF_QS = OFF_PAGE + BATCH
 constexpr int SMEM_BYTES = OFF_QS + 64 * 4;
 constexpr int TM_S = 256, TM_COLS = 512;                     // O in columns 0..255, S in 256..319 and 320..383
 constexpr int THREADS = 256;
+constexpr float T_MAX = 11.f;                                // log2 of the largest weight: e5m2 leaves at most 2^8 of it to e4m3
 static_assert(SMEM_BYTES <= 232448, "shared memory of one SM");
 static_assert(OFF_QS % 16 == 0 && OFF_FACT % 16 == 0, "alignment");
 }  // namespace p8pair
@@ -410,7 +411,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
         s_red[(g & 1) * 128 + ln] = top;
         asm volatile("bar.sync 1, 128;" ::: "memory");
         top = fmaxf(top, s_red[(g & 1) * 128 + (ln ^ 64)]);
-        const bool raise = unset ? top > -INFINITY : top > PAGED8_T_BITS + PAGED8_SLACK;
+        const bool raise = unset ? top > -INFINITY : top > T_MAX;
         const float d = raise ? top - PAGED8_T_BITS : 0.f, factor = raise && !unset ? ex2(-d) : 1.f;
         m += d;
         l *= factor;

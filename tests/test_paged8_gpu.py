@@ -274,15 +274,17 @@ def compare(out, lse, want, want_lse, absv, big, n, top):
     """Logit error e: a query element is off by 2^-17 of its row's largest, so the product sum by 2^-17 max|q| sum|k| (`big`, with
     the softmax scale); fp32 sums of up to 2 * 576 products (2^-24 each, worst order) add 2^-13 of the same; exp2 / log2 and
     the scale products 2^-21 of the logits, which `big` bounds as well.  A weight is then off by the factor 2 e, its two terms
-    by 2^-8, the result by the same of sum p|v| (numerator) and of |out| (row sum, logit part only); the floor of a weight,
-    2^-18 of the largest, is dithered: at most n / 64 times that in one direction; bf16 rounds by 2^-8 |out| at most."""
+    by 2^-8, the result by the same of sum p|v| (numerator) and of |out| (row sum, logit part only); the floor of a weight, 2^-10
+    where the largest is at least 2^5, i.e. 2^-15 of it, is dithered: 1/64 of it for every key in one direction, and what the
+    offsets do not cancel within one round of 32 keys, 32 times it at most per round of different weights, i.e. the mean error
+    of independent roundings; bf16 rounds by 2^-8 |out| at most."""
     got, gl = out.double().cpu().numpy(), lse.double().cpu().numpy()
     e = big * (2.0 ** -17 + 2.0 ** -13 + 2.0 ** -20)
     empty = ~np.isfinite(want_lse)
     assert np.array_equal(np.isneginf(gl), empty) and np.all(got[empty] == 0)
     dl = np.abs(gl[~empty] - want_lse[~empty])
     assert np.all(dl <= e[~empty] + 1e-6 * np.abs(want_lse[~empty]) + 1e-6), dl.max()
-    tol = absv * (2.0 ** -8 + 4 * e[..., None]) + 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * (1 + n / 64) * absv.max(initial=0) * 4 + 1e-30
+    tol = absv * (2.0 ** -8 + 4 * e[..., None]) + 2.0 ** -8 * np.abs(want) + 2.0 ** -15 * (1 + n / 64) * absv.max(initial=0) + 1e-30
     bad = np.abs(got - want) > tol
     assert not bad.any(), (int(bad.sum()), float(np.abs(got - want).max()), np.argwhere(bad)[:4])
     if (~empty).any():
@@ -301,7 +303,7 @@ def test_attend_head_layouts(B, impl, shape, heads, kv):
 
 
 @pytest.mark.parametrize("shape,heads,kv,q_len", [("mla512", 16, 1, 2), ("mla512", 24, 1, 5), ("gqa128", 8, 2, 4), ("gqa128", 6, 2, 7), ("gqa64", 4, 2, 33),
-                                                  ("mla128", 2, 1, 16)])
+                                                  ("mla128", 2, 1, 16), ("mla512", 128, 1, 3), ("mla512", 80, 1, 1), ("mla512", 48, 1, 2)])
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 def test_attend_several_queries_and_page_sizes(B, shape, heads, kv, q_len, page):
     # short sequences leave the first queries without a row
@@ -309,7 +311,7 @@ def test_attend_several_queries_and_page_sizes(B, shape, heads, kv, q_len, page)
     check_attend(B, shape, heads, kv, page, states, 128, q_len, seed=page + q_len, bias=-0.4)
 
 
-@pytest.mark.parametrize("shape,heads,kv,rows,batch", [("mla512", 16, 1, 9000, 1), ("gqa128", 8, 2, 5003, 3), ("mla512", 64, 1, 2600, 2), ("gqa64", 3, 1, 40001, 1)])
+@pytest.mark.parametrize("shape,heads,kv,rows,batch", [("mla512", 16, 1, 9000, 1), ("mla512", 33, 1, 21000, 1), ("mla512", 128, 1, 3000, 5), ("gqa128", 8, 2, 5003, 3), ("mla512", 64, 1, 2600, 2), ("gqa64", 3, 1, 40001, 1)])
 def test_attend_long_sequences_are_cut_and_merged(B, shape, heads, kv, rows, batch):
     check_attend(B, shape, heads, kv, 64, [(0, rows - 700 * i) for i in range(batch)], 64, 1, seed=rows, reps=False)
 
@@ -332,12 +334,24 @@ def test_attend_growing_maximum(B):
     check_attend(B, "gqa128", 8, 1, 64, [(0, 64 * 30)], 64, 1, seed=9, q_gain=4.0)
     check_attend(B, "mla512", 64, 1, 64, [(0, 64 * 20 + 5)], 64, 1, seed=10, q_gain=3.0)
 
+    def rise_mla(pool_, table):
+        for e in range(table.shape[1]):
+            pool_[2][table[0, e]] = 2.0 ** (-9 + e / 3.0)                     # keys and values grow together
+    for heads in (16, 20, 72):
+        check_attend(B, "mla512", heads, 1, 64, [(0, 64 * 30)], 64, 1, seed=12, pool_edit=rise_mla, q_gain=0.05)
+
 
 def test_attend_scales_of_every_size(B):
     def edit(pool_, table):
         for e in range(table.shape[1]):
             pool_[2][table[0, e]] = [2.0 ** -100, 2.0 ** 40, 1.0, 2.0 ** -60][e % 4]
     check_attend(B, "gqa128", 8, 2, 16, [(0, 16 * 23 + 3)], 64, 1, seed=11, pool_edit=edit)
+
+    def small(pool_, table):                                                   # MLA: key and value share the scale
+        for e in range(table.shape[1]):
+            pool_[2][table[0, e]] = [2.0 ** -100, 2.0 ** -7, 2.0 ** -60][e % 3]
+    for heads in (16, 70):
+        check_attend(B, "mla512", heads, 1, 16, [(0, 16 * 23 + 3)], 64, 1, seed=11, pool_edit=small)
 
 
 def test_attend_flat_tail_behind_one_large_logit(B):
@@ -361,9 +375,10 @@ def test_attend_flat_tail_behind_one_large_logit(B):
         t = float(q[0, 0, h].double().sum())
         l = math.exp(t) + n - 1
         share = (n - 1) / l
-        # floor 2^-18 of the largest weight: the ranges of this sequence start with a maximum of their own (peak or tail), and
-        # inside the peak's range the 32 offsets leave at most 1/64 of it, 2^-24 of exp(t) per key
-        assert abs(float(out[0, 0, h, 0]) - share) <= 2.0 ** -8 * share + 2.0 ** -8 * share + 128 * 128 * 2.0 ** -24 * math.exp(t) / l
+        # floor 2^-15 of the largest weight, exp(t): the 938 tiles are cut into at least 148 ranges with a maximum of their own, so
+        # that at most 8 tiles share the peak's, and there the 32 offsets leave at most 1/64 of it for each of 1024 equal keys;
+        # elsewhere every weight is the largest (2^-9), and bf16 rounds by 2^-8
+        assert abs(float(out[0, 0, h, 0]) - share) <= 2.0 ** -7 * share + 1024 * 2.0 ** -21 * math.exp(t) / l
         assert abs(float(lse[0, 0, h]) - math.log(l)) < 1e-4
 
 
@@ -398,6 +413,23 @@ def test_attend_nan_and_infinity_stay_where_they_belong(B):
     assert torch.equal(torch.isnan(lse[:, 0]).cpu(), want.all(-1))
 
 
+@pytest.mark.parametrize("heads", [16, 96])
+def test_attend_nan_and_infinity_in_latents_and_queries(B, heads):
+    states = [(0, 50), (0, 260), (0, 140), (0, 40)]
+    pool_, table = build(B, "mla512", 1, 64, states, 64, 3)
+    pool_[0][table[1, 2], 0, 3, 7] = 0x7f                                      # one latent element: key and value
+    q = [torch.randn((4, 1, heads, d), generator=torch.Generator().manual_seed(1)).bfloat16() for d in (512, 64)]
+    q[0][3, 0, 5, 11], q[1][3, 0, heads - 1, 0] = float("inf"), float("nan")
+    p = B.make_params("mla", 4, 1, heads, 1, 512, 64, 64, 0, 0.07)
+    cache, _ = to_gpu(B, pool_, torch.from_numpy(table).to(DEV))
+    out, lse = B.decode_attention_paged8(p, cache, q[0].to(DEV), q[1].to(DEV), None, i32([s[1] for s in states]), want_lse=True)
+    want = torch.zeros((4, heads), dtype=torch.bool)
+    want[1] = True
+    want[3, 5], want[3, heads - 1] = True, True
+    assert torch.equal(torch.isnan(out[:, 0]).all(-1).cpu(), want) and torch.equal(torch.isnan(out[:, 0]).any(-1).cpu(), want)
+    assert torch.equal(torch.isnan(lse[:, 0]).cpu(), want)
+
+
 def test_attend_counters_beyond_the_table_are_clamped(B):
     pool_, table = build(B, "mla128", 1, 16, [(0, 64), (4, 64)], 16, 3)
     p = B.make_params("mla", 2, 1, 8, 1, 128, 64, 16, 0, 0.1)
@@ -426,13 +458,14 @@ def test_attend_rows_behind_the_batch_stay_as_they_are(B):
     assert torch.isfinite(out).all()
 
 
-def test_calls_are_capturable_reproducible_and_independent_of_the_stream(B):
+@pytest.mark.parametrize("heads", [32, 128])
+def test_calls_are_capturable_reproducible_and_independent_of_the_stream(B, heads):
     states = [(3, 3 * 64 + 200), (0, 700), (2, 2 * 64 + 90)]
     pool_, table = build(B, "mla512", 1, 64, states, 64, 8, hole_nan=False)
-    p = B.make_params("mla", 3, 1, 32, 1, 512, 64, 64, 0, 0.07)
+    p = B.make_params("mla", 3, 1, heads, 1, 512, 64, 64, 0, 0.07)
     cache, t = to_gpu(B, pool_, torch.from_numpy(table).to(DEV))
     g = torch.Generator().manual_seed(1)
-    q_sem, q_pos = (torch.randn((3, 1, 32, d), generator=g).bfloat16().to(DEV) for d in (512, 64))
+    q_sem, q_pos = (torch.randn((3, 1, heads, d), generator=g).bfloat16().to(DEV) for d in (512, 64))
     rows = [torch.randn((3, 1, d), generator=g).bfloat16().to(DEV) for d in (512, 64)]
     n_rep, n_tok = i32([s[0] for s in states]), i32([s[1] for s in states])
     slots = i32([int(table[b, (s[1] - 1) // 64]) * 64 + (s[1] - 1) % 64 for b, s in enumerate(states)])
@@ -442,7 +475,7 @@ def test_calls_are_capturable_reproducible_and_independent_of_the_stream(B):
         B.paged8_write(p, cache, *rows, slots, stream=stream)
         B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok, out=out, ws=ws, stream=stream)
 
-    outs = [torch.zeros((3, 1, 32, 512), dtype=torch.bfloat16, device=DEV) for _ in range(4)]
+    outs = [torch.zeros((3, 1, heads, 512), dtype=torch.bfloat16, device=DEV) for _ in range(4)]
     step(outs[0])
     side = torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
