@@ -643,7 +643,7 @@ int attn_paged8_launch(const Paged8Attn& a) {
   P.B = p->batch; P.Hq = p->n_q_heads; P.Hkv = p->n_kv_heads; P.q_len = a.q_len; P.g = a.n_rep ? p->group_size : 1;
   P.page = c->page_size; P.page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7; P.n_pages = c->n_pages; P.width = c->table_width; P.rep = P.Hq / P.Hkv;
   P.n_blk = (int)(((long long)P.q_len * P.rep + nh - 1) / nh);
-  P.grid = paged8_grid(p, nh); P.min_tiles = 2;
+  P.grid = paged8_grid(p, nh);
   P.scale_log2 = p->softmax_scale * 1.4426950408889634f; P.bias_log2 = p->rep_logit_bias * 1.4426950408889634f;
   P.part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(a.ws) + 31) & ~(uintptr_t)31);
   P.out_wide = (reinterpret_cast<uintptr_t>(a.out) & 31u) == 0;

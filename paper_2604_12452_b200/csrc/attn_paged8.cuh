@@ -21,7 +21,7 @@ struct Paged8Params {
   bf16* out; float* lse;
   float* part;                // [2 * grid][NH][DS] partial O, then [2 * grid][2][NH] M and l
   long long* prefix;          // [B + 2] tiles before each sequence (all units), then 1 where every unit has a CTA; written by CTA 0
-  int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, min_tiles, grid;   // grid: CTAs (pairs of them) that share the line
+  int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, grid;   // grid: CTAs (pairs of them) that share the line
   int out_wide;               // out is 32-byte aligned
   float scale_log2, bias_log2;
 };
@@ -40,9 +40,25 @@ __device__ __forceinline__ TileSpan tile_span(const Paged8Params& p, int b) {
   t.n = t.n_a + (t.s.n_tok > t.s.tok0 ? max(((t.s.n_tok + 127) >> 7) - t.b0, 0) : 0);
   return t;
 }
-__device__ __forceinline__ int ctas_used(const Paged8Params& p, long long T) {
-  return (int)max(1ll, min((long long)p.grid, (T + p.min_tiles - 1) / p.min_tiles));
-}
+// The line of T tiles is cut into G ranges: CTA c takes tiles [start(c), start(c + 1)), the first `rest` of them one tile more.
+// At least two tiles for a CTA that works (a range of one tile costs a partial result that another CTA has to merge).  The
+// numbers fit 32 bits except in absurd cases; a 64-bit division costs several hundred clocks of a launch's first microseconds.
+struct Cut {
+  long long per;
+  int G, rest;
+  __device__ __forceinline__ Cut(long long T, int grid) {
+    const long long half = (T + 1) >> 1;
+    G = half < grid ? max((int)half, 1) : grid;
+    if (T >> 32) { per = T / G; rest = (int)(T % G); }
+    else { per = (unsigned)T / (unsigned)G; rest = (int)((unsigned)T % (unsigned)G); }
+  }
+  __device__ __forceinline__ long long start(int c) const { return c * per + min(c, rest); }
+  __device__ __forceinline__ int owner(long long x) const {              // the CTA whose range holds tile x
+    const long long big = rest * (per + 1);
+    if (x < big) return (int)(big >> 32 ? x / (per + 1) : (unsigned)x / (unsigned)(per + 1));
+    return rest + (int)((x - big) >> 32 || per >> 32 ? (x - big) / per : (unsigned)(x - big) / (unsigned)per);
+  }
+};
 
 // The pieces of units in one CTA's range of the line.
 struct Walk {
@@ -61,9 +77,10 @@ struct Walk {
       ++b;
     }
     if (left <= 0) return false;
-    const int u = (int)(off / t.n);
-    t0 = (int)(off % t.n);
-    hk = u / p.n_blk; blk = u % p.n_blk;
+    const int u = off >> 32 ? (int)(off / t.n) : (int)((unsigned)off / (unsigned)t.n);
+    t0 = (int)(off - (long long)u * t.n);
+    if (p.n_blk == 1) { hk = u; blk = 0; }
+    else { hk = u / p.n_blk; blk = u - hk * p.n_blk; }
     n = (int)min((long long)(t.n - t0), left);
     left -= n;
     fresh = false;
@@ -83,9 +100,9 @@ __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long
   const long long upu = (long long)p.Hkv * p.n_blk;
   const int q = (p.B + THREADS - 1) / THREADS, lo = min(tid * q, p.B), hi = min(lo + q, p.B);
   long long sum = 0;
-  int longest = 0;
+  int longest = 0, n_only = 0;                               // n_only: tiles of the thread's only sequence (q = 1)
 #pragma unroll 1
-  for (int b = lo; b < hi; ++b) { const int n = tile_span(p, b).n; sum += (long long)n * upu; longest = max(longest, n); }
+  for (int b = lo; b < hi; ++b) { n_only = tile_span(p, b).n; sum += n_only * upu; longest = max(longest, n_only); }
   long long inc = sum;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
@@ -101,29 +118,28 @@ __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long
     T += s_warp[w];
     longest = max(longest, s_longest[w]);
   }
-  const int G = ctas_used(p, T);
-  const bool own = (long long)p.B * upu <= p.grid && longest <= T / p.grid + WHOLE_SLACK;
+  const bool own = p.B * upu <= p.grid && (long long)(longest - WHOLE_SLACK) * p.grid <= T;
   if (blockIdx.x == 0) {
     long long at = before;
 #pragma unroll 1
-    for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (long long)tile_span(p, b).n * upu; }
+    for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (q == 1 ? n_only : tile_span(p, b).n) * upu; }
     if (tid == 0) { p.prefix[p.B] = T; p.prefix[p.B + 1] = own; }
   }
   if (own) {
     if (tid == 0) {
-      const int b = min((int)(id / upu), p.B - 1), n = id < p.B * upu ? tile_span(p, b).n : 0;
-      *s_b = b; s_off[0] = (id % upu) * n; s_off[1] = n;
+      const int b = min(id / (int)upu, p.B - 1), n = id < p.B * upu ? tile_span(p, b).n : 0;
+      *s_b = b; s_off[0] = (long long)(id % (int)upu) * n; s_off[1] = n;
     }
     return;
   }
-  long long s0 = 0, s1 = 0;
-  if (id < G) { s0 = (long long)id * T / G; s1 = ((long long)id + 1) * T / G; }
+  const Cut cut(T, p.grid);
+  const long long s0 = id < cut.G ? cut.start(id) : 0, s1 = id < cut.G ? cut.start(id + 1) : 0;
   if (s1 > s0 && s0 >= before && s0 < before + sum) {        // exactly one thread
     long long at = before;
     int b = lo;
 #pragma unroll 1
-    while (true) {
-      const long long n = (long long)tile_span(p, b).n * upu;
+    while (q > 1) {
+      const long long n = tile_span(p, b).n * upu;
       if (s0 < at + n) break;
       at += n; ++b;
     }
@@ -225,19 +241,18 @@ __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_consta
   const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
   const int gr = blk * NH + h;
   if (gr >= p.q_len * p.rep) return;
-  const long long T = p.prefix[p.B], seq = p.prefix[b], n = (p.prefix[b + 1] - seq) / per;
+  const long long T = p.prefix[p.B], seq = p.prefix[b], n_all = p.prefix[b + 1] - seq, n = n_all >> 32 ? n_all / per : (unsigned)n_all / (unsigned)per;
   const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
   float o[VEC] = {};
   float m = -INFINITY, l = 0.f;
   if (n > 0) {
     if (p.prefix[p.B + 1]) return;                           // not cut: written by the CTA that worked on it
-    const int G = ctas_used(p, T);
+    const Cut cut(T, p.grid);
     const long long u0 = seq + u * n, u1 = u0 + n;
-    // CTA c owns [c T / G, (c + 1) T / G): tile x is in CTA ((x + 1) G - 1) / T
-    const int c0 = (int)(((u0 + 1) * G - 1) / T), np = (int)((u1 * G - 1) / T) - c0 + 1;
+    const int c0 = cut.owner(u0), np = cut.owner(u1 - 1) - c0 + 1;
     if (np == 1) return;
     const float* ml = p.part + (size_t)2 * p.grid * NH * DS;
-    const int first = (long long)c0 * T / G == u0 ? 0 : 1;   // a later piece of its CTA, or the CTA's first
+    const int first = cut.start(c0) == u0 ? 0 : 1;           // the CTA's first piece, or a later one
     for (int i = lane; i < np; i += 32) m = fmaxf(m, ml[(size_t)(2 * (c0 + i) + (i == 0 ? first : 0)) * 2 * NH + h]);
 #pragma unroll
     for (int k = 16; k > 0; k >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
