@@ -110,20 +110,20 @@ int attn_paged8_simt_launch(const Paged8Attn& q) {
 }
 
 // ---------------------------------------------------------------------------------------------- tensor-core kernel
-// Transposed products: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T and O^T [d x NH] += V^T (T_hi + T_lo)^T, so that the key
+// Transposed products: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T and O^T [d x 2 NH] += V^T [T_hi | T_lo]^T, so that the key
 // tile is the 128-row operand whatever the number of heads, a row of K or V is read by the tensor core as it lies in the
 // page (K-major for S, MN-major for O: no transposition, no conversion) and a softmax thread owns one key: scale, mask and
 // bias are one value per thread.  NH (16, 32 or 64) query rows of one KV head share a tile.
 //   softmax    NH / 16 groups of four warps, each for 16 of the rows: thread = key = TMEM lane; epilogue: thread = output
 //              column d.  Sixteen rows a thread keep the unrolled code within the instruction cache (one group of 64 rows spent
-//              most of its time fetching instructions: 243 us instead of 150 at 64 x 5056 rows, 128 heads).
+//              most of its time fetching instructions: 64 x 5056 rows of 128 heads took 243 us instead of 150).
 //   + 1 warp   TMA: 128-byte-wide chunks (16 KB) of the 128 rows of a tile, one request per page
 //   + 1 warp   MMA issue and TMEM
 // S of tile j+1 is issued before O of tile j.  GQA: one ring of slots, filled in the order of use, K(0) K(1) V(0) K(2)
 // V(1) ...  MLA: the latent chunks are keys and values; they stay in their slots from S to O (two tiles at a time are in the
 // ring, a third one is arriving), which saves the second copy: the tensor core reads its operands over the same 128 bytes
-// per clock of shared memory that the copies are written through, and that is what bounds a tile (NH = 16: 1968 clocks of
-// operands and 576 of copies; with a second copy of the values 1088).
+// per clock of shared memory that the copies are written through, and that is what bounds a tile (NH = 16: 720 clocks of
+// operands for S, 640 for O, 576 of copies; with a second copy of the values 1088).
 // Work: all tiles of all (sequence, KV head, block of NH rows) units form one line that is cut into equal ranges, one per
 // CTA; a unit that is cut leaves (O, M, l) of its pieces in the workspace, merged by paged8_combine_kernel.
 template <bool MLA_, int DS_, int DP_, int NH_>
@@ -593,7 +593,7 @@ bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, l
 // Query rows that share a tile of keys.  The tile is padded to that number, so it is the smallest one that holds all rows of
 // a KV head (the softmax threads compute an exponential per padded row and key); at most 64, as O takes d / 128 * NH columns
 // of TMEM.  The MLA shape with more than 32 rows goes to CTA pairs in blocks of 128 (64 x 5056 rows, 128 heads: 128 us in
-// blocks of 64 on single CTAs, PAIR_US on pairs).
+// blocks of 64 on single CTAs, 90 us on pairs).
 static int paged8_rows_per_tile(const lca_params* p, int q_len) {
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
   return rows <= 16 ? 16 : rows <= 32 ? 32 : p->d_sem == 512 ? 128 : 64;

@@ -3,7 +3,7 @@
 //
 // With 64 rows or more the transposed tiles of attn_paged8.cu are bound by the 128 bytes per clock of shared memory: every
 // product reads both operands from it, 2688 clocks for 64 rows x 128 keys, and the copies of the tile are written through
-// the same port (4200 clocks a tile measured).  Here two CTAs share 128 query rows (cta_group::2, M = 128): each holds 64
+// the same port (4200 clocks a tile measured; 64 x 5056 rows of 128 heads: 128 us, here 90).  Here two CTAs share 128 query rows (cta_group::2, M = 128): each holds 64
 // rows of Q and P, half of the keys for S = Q K^T (N = 128 split by keys) and half of the value columns for O += T V
 // (N = 256, twice, split by columns), so that a product reads half the bytes per SM:
 //   tensor core   S 36 x 32 + O 16 x 64 clocks = 2176 for 128 rows x 128 keys on two SMs
@@ -13,9 +13,10 @@
 //   warp 0 keys (TMA), warp 1 MMA (even CTA) / forwarding of the odd CTA's signals, warps 2-5 softmax and epilogue,
 //   warp 6 values (TMA), warp 7 page table and scales, four tiles at a time
 // Signals from the odd to the even CTA ("Q written", "P written") go through one thread that has acquired the writers'
-// arrivals and forwards a relaxed one: a release-arrival across the cluster costs its thread over a thousand clocks.  That
-// the odd SM's tensor core, started by the even CTA's later instruction, sees the writes (each followed by a proxy fence) is
-// an argument about the hardware's behaviour; the test that compares repeated runs bit for bit is its check.
+// arrivals and arrives at the even CTA's barrier with a release within its own CTA.  The data never leaves the odd SM: its
+// threads write it, each with a fence towards the async proxy before its arrival, and its own tensor core reads it once the
+// even CTA has issued the product.  A release across the cluster would order the same writes for readers on other SMs, and
+// costs its thread over a thousand clocks (119 us instead of 91).  The tests compare repeated runs bit for bit.
 #include <cstring>
 
 #include "attn_paged8.cuh"
@@ -270,11 +271,11 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
       bool ok = true;
       while (ok && w.next(p)) {
         if (!mbar_wait(QLOCAL, seg & 1, abort_flag)) { fail(ERR_WAIT_Q); break; }
-        mbar_arrive_cluster_relaxed(q_bar);
+        mbar_arrive_cluster_cta(q_bar);
         ++seg;
         for (int j = 0; j < w.n; ++j, ++g) {
           if (!mbar_wait(PLOCAL, g & 1, abort_flag)) { fail(ERR_WAIT_P_FULL); ok = false; break; }
-          mbar_arrive_cluster_relaxed(p_bar);
+          mbar_arrive_cluster_cta(p_bar);
         }
       }
     }

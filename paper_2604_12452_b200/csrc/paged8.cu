@@ -2,6 +2,7 @@
 // the online condensation of a group.  The row space, the pages and the scales are described in lca.h.
 #include "lca_common.cuh"
 #include "fp8_common.cuh"
+#include "tc_common.cuh"
 
 namespace lca {
 
@@ -11,7 +12,8 @@ namespace lca {
 // possible; (2) pages that no present row needs are pushed on the free stack; (3) pages are popped into the tables; (4) the
 // slot of every new row is looked up.  A sequence's share of each list starts at an exclusive prefix sum, so the result does
 // not depend on how the work is spread.  Bound by latency (dependent passes over the counters and cluster barriers), not by
-// its bytes: one CTA for a decode step, sixteen for prompts (64 prompts of 5000 rows).
+// its bytes: one CTA for a decode step (64 sequences: 5.7 us), sixteen for prompts (64 prompts of 5056 rows grown and given
+// back: 25 us for both calls; one CTA took 100).
 struct PageArgs {
   const int32_t* n_rep; const int32_t* n_tok;
   int32_t* held_rep; int32_t* held_tok;
@@ -266,7 +268,8 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
 // ------------------------------------------------------------------------------------------------------------- write
 // A run (rows of one page in one call) and a block (GQA: K or V of one KV head; MLA: latent and rope key together) at a time.
 // The rows of a run stay in registers between the maximum and the rounding, so the input is read once.  HBM-bound: 2 bytes
-// in, 1 byte out per element.
+// in, 1 byte out per element (323584 rows of the MLA shape: 559 MB in 96 us, 5.8 TB/s; 29000 rows of 8 KV heads: 178 MB in
+// 31 us, 5.7 TB/s).  A decode step of 64 rows is one launch's latency, 3 us.
 struct WriteArgs {
   const bf16* rows_sem; const bf16* rows_pos; const int32_t* slots;
   uint8_t* pages_sem; uint8_t* pages_pos; float* scale_sem; float* scale_pos;
@@ -495,87 +498,128 @@ int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* ro
 // ------------------------------------------------------------------------------------------------------------ update
 // Condensation of the earliest group of every sequence that is due (Sec. 4.2 / 4.3) from the 8-bit values: fp64 scores,
 // arg-max on them (lowest index on ties), fp32 softmax and pooling, one rounding to bf16.  One CTA per (sequence, KV
-// head): the group (g rows of codes) is brought to shared memory once.  A launch of a few dozen CTAs that read 37 KB
-// each (g = 64, 576 wide): bound by latency.
+// head), a launch of a few dozen CTAs that read 37 KB each (g = 64, 576 wide): bound by the latency of what depends on each
+// other, counters, table, codes.  A warp therefore takes whole rows: it looks up their pages itself, keeps its lanes' share
+// of the query in registers and multiplies the codes as they arrive; shared memory only carries them to the pooling, for
+// which the rows are split over all threads.  (With the group brought to shared memory first, the query read from there
+// and a thread per four columns in the pooling: 10.5 us instead of 8.5 for 64 sequences of the MLA shape, 8.5
+// instead of 6.2 for 48 sequences with 8 KV heads.)
 struct Update8Args {
   const uint8_t* pages_sem; const uint8_t* pages_pos; const float* scale_sem; const float* scale_pos; const int32_t* table;
   const float* qbar_f; const double* qbar_d;
   const int32_t* n_rep; const int32_t* n_tok; int32_t* n_rep_new;
   bf16* rep_sem; bf16* rep_pos; int32_t* anchor;
-  int Hkv, d_sem, d_pos, g, w, page, n_pages, width, mla;
+  int Hkv, g, w, page_log2, n_pages, width;
   double scale;
 };
-static const int UPD_THREADS = 512;
+static const int UPD_THREADS = 512, UPD_WARPS = UPD_THREADS / 32;
 
+// N consecutive codes (2, 4 or 16) as words; two codes in the low half of one
+template <int N>
+struct Codes {
+  uint32_t w[(N + 3) / 4];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    if constexpr (N == 2) w[0] = *reinterpret_cast<const uint16_t*>(p);
+    else if constexpr (N == 4) w[0] = *reinterpret_cast<const uint32_t*>(p);
+    else { const uint4 v = *reinterpret_cast<const uint4*>(p); w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w; }
+  }
+  __device__ __forceinline__ void store(uint8_t* p) const {
+    if constexpr (N == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)w[0];
+    else if constexpr (N == 4) *reinterpret_cast<uint32_t*>(p) = w[0];
+    else *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  __device__ __forceinline__ double dot(const double (&q)[N], float scale, double acc) const {
+#pragma unroll
+    for (int k = 0; k < N; k += 4) {
+      const float4 f = e4m3x4_to_float4(w[k / 4]);
+      acc = fma(q[k], (double)(f.x * scale), acc); acc = fma(q[k + 1], (double)(f.y * scale), acc);
+      if constexpr (N > 2) { acc = fma(q[k + 2], (double)(f.z * scale), acc); acc = fma(q[k + 3], (double)(f.w * scale), acc); }
+    }
+    return acc;
+  }
+};
+
+template <bool MLA, int DS, int DP>
 __global__ void __launch_bounds__(UPD_THREADS) paged8_update_kernel(Update8Args a) {
+  constexpr int NS = DS / 32, NP = DP / 32, SEM_Q = MLA ? DS : 0, DK = SEM_Q + DP;
+  constexpr int COLS = DS / 4, GROUPS = UPD_THREADS / COLS;   // pooling: threads across a row, groups of rows
+  constexpr int ROWS = 4;                                     // rows whose loads a warp has in flight
   extern __shared__ __align__(16) unsigned char smem_raw[];
-  const int hk = (int)(blockIdx.x % a.Hkv), b = (int)(blockIdx.x / a.Hkv);
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, n_warps = UPD_THREADS / 32;
-  const int g = a.g, dk = (a.mla ? a.d_sem : 0) + a.d_pos;
-  double* s_q = reinterpret_cast<double*>(smem_raw);
-  double* s_s = s_q + dk;
+  float4* s_part = reinterpret_cast<float4*>(smem_raw);       // [GROUPS][COLS]
+  const int g = a.g;                                          // a multiple of 16
+  double* s_s = reinterpret_cast<double*>(s_part + UPD_THREADS);
   float* s_a = reinterpret_cast<float*>(s_s + g);
-  float* s_fs = s_a + g;                                     // scale of each row's sem / pos codes
+  float* s_fs = s_a + g;                                      // scale of each row's sem / pos codes
   float* s_fp = s_fs + g;
-  int* s_page = reinterpret_cast<int*>(s_fp + g);
-  uint8_t* t_sem = reinterpret_cast<uint8_t*>(s_page + g);   // 16-byte aligned: dk, g multiples of 8 and of 16
-  uint8_t* t_pos = t_sem + (size_t)g * a.d_sem;
+  uint8_t* t_sem = reinterpret_cast<uint8_t*>(s_fp + g);
+  uint8_t* t_pos = t_sem + (size_t)g * DS;
   __shared__ int s_anchor;
+  const int hk = (int)(blockIdx.x % a.Hkv), b = (int)(blockIdx.x / a.Hkv);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int nr = a.n_rep[b], nt = a.n_tok[b];
-  const long long first = (long long)nr * g, cap = (long long)a.width * a.page;
-  bool due = nr >= 0 && nt >= 0 && nt <= cap && (long long)nt - first >= (long long)a.w + g;
+  const long long first = (long long)nr * g, cap = (long long)a.width << a.page_log2;
+  const bool due = nr >= 0 && nt >= 0 && nt <= cap && (long long)nt - first >= (long long)a.w + g;
   int missing = 0;
-  if (due)
-    for (int i = tid; i < g; i += UPD_THREADS) {
-      const long long x = first + i;
-      const int pg = a.table[(size_t)b * a.width + x / a.page];
-      if (pg < 0 || pg >= a.n_pages) missing = 1;
-      else {
-        s_page[i] = pg;
-        s_fs[i] = a.scale_sem[(size_t)pg * a.Hkv + hk];
-        s_fp[i] = a.scale_pos ? a.scale_pos[(size_t)pg * a.Hkv + hk] : s_fs[i];
+  if (due) {
+    const size_t q0 = ((size_t)b * a.Hkv + hk) * DK;
+    double qs[MLA ? NS : 1], qp[NP];
+    if constexpr (MLA)
+#pragma unroll
+      for (int k = 0; k < NS; ++k) qs[k] = a.qbar_f ? (double)a.qbar_f[q0 + lane * NS + k] : a.qbar_d[q0 + lane * NS + k];
+#pragma unroll
+    for (int k = 0; k < NP; ++k) qp[k] = a.qbar_f ? (double)a.qbar_f[q0 + SEM_Q + lane * NP + k] : a.qbar_d[q0 + SEM_Q + lane * NP + k];
+#pragma unroll 1
+    for (int i0 = warp; i0 < g; i0 += ROWS * UPD_WARPS) {
+      Codes<NS> cs[ROWS];
+      Codes<NP> cp[ROWS];
+      float fs[ROWS], fp[ROWS];
+      int page[ROWS];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int i = i0 + r * UPD_WARPS;
+        page[r] = i < g ? a.table[(size_t)b * a.width + ((first + i) >> a.page_log2)] : 0;
+        if (page[r] < 0 || page[r] >= a.n_pages) { missing = 1; page[r] = 0; }       // any page: nothing is made of it
+      }
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int i = i0 + r * UPD_WARPS;
+        if (i < g) {
+          const size_t block = (size_t)page[r] * a.Hkv + hk, row = (block << a.page_log2) + (size_t)((first + i) & ((1 << a.page_log2) - 1));
+          cs[r].load(a.pages_sem + row * DS + lane * NS);
+          cp[r].load(a.pages_pos + row * DP + lane * NP);
+          fs[r] = a.scale_sem[block];
+          fp[r] = a.scale_pos ? a.scale_pos[block] : fs[r];
+        }
+      }
+      double acc[ROWS];
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int i = i0 + r * UPD_WARPS;
+        acc[r] = 0.0;
+        if (i < g) {
+          cs[r].store(t_sem + (size_t)i * DS + lane * NS);
+          cp[r].store(t_pos + (size_t)i * DP + lane * NP);
+          if constexpr (MLA) acc[r] = cs[r].dot(qs, fs[r], 0.0);
+          acc[r] = cp[r].dot(qp, fp[r], acc[r]);
+        }
+      }
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1)
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+#pragma unroll
+      for (int r = 0; r < ROWS; ++r) {
+        const int i = i0 + r * UPD_WARPS;
+        if (lane == 0 && i < g) { s_s[i] = acc[r] * a.scale; s_fs[i] = fs[r]; s_fp[i] = fp[r]; }
       }
     }
-  due = due && !__syncthreads_or(missing);
-  if (hk == 0 && tid == 0) a.n_rep_new[b] = nr + (due ? 1 : 0);
-  if (!due) {
+  }
+  const bool done = !__syncthreads_or(missing) && due;
+  if (hk == 0 && tid == 0) a.n_rep_new[b] = nr + (done ? 1 : 0);
+  if (!done) {
     if (tid == 0) a.anchor[b * a.Hkv + hk] = -1;
     return;
   }
-  const int x0 = (int)first;
-  const int cs = a.d_sem / 16, cp = a.d_pos / 16;
-  for (int x = tid; x < g * cs; x += UPD_THREADS) {
-    const int i = x / cs, c = x % cs;
-    reinterpret_cast<uint4*>(t_sem)[x] =
-        reinterpret_cast<const uint4*>(a.pages_sem + (((size_t)s_page[i] * a.Hkv + hk) * a.page + (x0 + i) % a.page) * a.d_sem)[c];
-  }
-  for (int x = tid; x < g * cp; x += UPD_THREADS) {
-    const int i = x / cp, c = x % cp;
-    reinterpret_cast<uint4*>(t_pos)[x] =
-        reinterpret_cast<const uint4*>(a.pages_pos + (((size_t)s_page[i] * a.Hkv + hk) * a.page + (x0 + i) % a.page) * a.d_pos)[c];
-  }
-  const size_t q0 = ((size_t)b * a.Hkv + hk) * dk;
-  for (int c = tid; c < dk; c += UPD_THREADS) s_q[c] = a.qbar_f ? (double)a.qbar_f[q0 + c] : a.qbar_d[q0 + c];
-  __syncthreads();
-  const int sem_off = a.mla ? a.d_sem : 0;
-  for (int i = warp; i < g; i += n_warps) {
-    double acc = 0.0;
-    const float fs = s_fs[i], fp = s_fp[i];
-    if (a.mla)
-      for (int c = 4 * lane; c < a.d_sem; c += 128) {
-        const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_sem + (size_t)i * a.d_sem + c));
-        acc = fma(s_q[c], (double)(f.x * fs), acc); acc = fma(s_q[c + 1], (double)(f.y * fs), acc);
-        acc = fma(s_q[c + 2], (double)(f.z * fs), acc); acc = fma(s_q[c + 3], (double)(f.w * fs), acc);
-      }
-    for (int c = 4 * lane; c < a.d_pos; c += 128) {
-      const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_pos + (size_t)i * a.d_pos + c));
-      acc = fma(s_q[sem_off + c], (double)(f.x * fp), acc); acc = fma(s_q[sem_off + c + 1], (double)(f.y * fp), acc);
-      acc = fma(s_q[sem_off + c + 2], (double)(f.z * fp), acc); acc = fma(s_q[sem_off + c + 3], (double)(f.w * fp), acc);
-    }
-    acc = warp_sum(acc);
-    if (lane == 0) s_s[i] = acc * a.scale;
-  }
-  __syncthreads();
   if (warp == 0) {
     double best = -INFINITY;
     int besti = 0x7fffffff;
@@ -591,48 +635,66 @@ __global__ void __launch_bounds__(UPD_THREADS) paged8_update_kernel(Update8Args 
     z = warp_sum(z);
     const float inv = 1.f / z;
     for (int i = lane; i < g; i += 32) s_a[i] *= inv;
-    if (lane == 0) s_anchor = min(besti, g - 1);             // no finite score at all (NaN): the last token
+    if (lane == 0) s_anchor = min(besti, g - 1);              // no finite score at all (NaN): the last token
   }
   __syncthreads();
   const size_t o = (size_t)b * a.Hkv + hk;
-  for (int c = 4 * tid; c < a.d_sem; c += 4 * UPD_THREADS) {
+  {
+    const int c = tid % COLS, grp = tid / COLS;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int i = 0; i < g; ++i) {
-      const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_sem + (size_t)i * a.d_sem + c));
+#pragma unroll 4
+    for (int i = grp; i < g; i += GROUPS) {
+      const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_sem + (size_t)i * DS + 4 * c));
       const float fs = s_fs[i], w = s_a[i];
       acc.x = fmaf(w, f.x * fs, acc.x); acc.y = fmaf(w, f.y * fs, acc.y); acc.z = fmaf(w, f.z * fs, acc.z); acc.w = fmaf(w, f.w * fs, acc.w);
     }
-    bf16* dst = a.rep_sem + o * a.d_sem + c;
-    dst[0] = __float2bfloat16_rn(acc.x); dst[1] = __float2bfloat16_rn(acc.y); dst[2] = __float2bfloat16_rn(acc.z); dst[3] = __float2bfloat16_rn(acc.w);
+    s_part[tid] = acc;
   }
-  const int ia = s_anchor;
-  for (int c = 4 * tid; c < a.d_pos; c += 4 * UPD_THREADS) {
-    const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_pos + (size_t)ia * a.d_pos + c));
+  __syncthreads();
+  if (tid < COLS) {
+    float4 acc = s_part[tid];
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) {
+      const float4 v = s_part[k * COLS + tid];
+      acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
+    }
+    *reinterpret_cast<uint2*>(a.rep_sem + o * DS + 4 * tid) = make_uint2(tc::pack_bf16x2(acc.x, acc.y), tc::pack_bf16x2(acc.z, acc.w));
+  } else if (tid >= UPD_THREADS - DP / 4) {
+    const int ia = s_anchor, c = 4 * (tid - (UPD_THREADS - DP / 4));
+    const float4 f = e4m3x4_to_float4(*reinterpret_cast<const uint32_t*>(t_pos + (size_t)ia * DP + c));
     const float fp = s_fp[ia];
-    bf16* dst = a.rep_pos + o * a.d_pos + c;
-    dst[0] = __float2bfloat16_rn(f.x * fp); dst[1] = __float2bfloat16_rn(f.y * fp); dst[2] = __float2bfloat16_rn(f.z * fp); dst[3] = __float2bfloat16_rn(f.w * fp);
+    *reinterpret_cast<uint2*>(a.rep_pos + o * DP + c) = make_uint2(tc::pack_bf16x2(f.x * fp, f.y * fp), tc::pack_bf16x2(f.z * fp, f.w * fp));
   }
-  if (tid == 0) a.anchor[o] = ia;
+  if (tid == 0) a.anchor[o] = s_anchor;
 }
 
 size_t paged8_update_smem_bytes(const lca_params* p) {
-  const size_t g = (size_t)p->group_size, dk = (size_t)(p->variant == LCA_VARIANT_MLA ? p->d_sem : 0) + p->d_pos;
-  return dk * sizeof(double) + g * (sizeof(double) + 3 * sizeof(float) + sizeof(int)) + g * (size_t)(p->d_sem + p->d_pos);
+  const size_t g = (size_t)p->group_size;
+  return UPD_THREADS * sizeof(float4) + g * (sizeof(double) + 3 * sizeof(float)) + g * (size_t)(p->d_sem + p->d_pos);
+}
+
+template <bool MLA, int DS, int DP>
+static int update8_launch(const Update8Args& a, long long grid, size_t smem, cudaStream_t stream) {
+  auto kern = paged8_update_kernel<MLA, DS, DP>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return LCA_ERR_CUDA;
+  kern<<<(unsigned)grid, UPD_THREADS, smem, stream>>>(a);
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
 }
 
 int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
                          const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,
                          cudaStream_t stream) {
+  const int lg = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
   Update8Args a = {(const uint8_t*)c->pages_sem, (const uint8_t*)c->pages_pos, c->scale_sem, c->scale_pos, c->block_table, qbar_f, qbar_d,
-                   n_rep, n_tok, n_rep_new, (bf16*)rep_sem, (bf16*)rep_pos, anchor_out, p->n_kv_heads, p->d_sem, p->d_pos, p->group_size,
-                   p->window, c->page_size, c->n_pages, c->table_width, p->variant == LCA_VARIANT_MLA, (double)p->softmax_scale};
+                   n_rep, n_tok, n_rep_new, (bf16*)rep_sem, (bf16*)rep_pos, anchor_out, p->n_kv_heads, p->group_size,
+                   p->window, lg, c->n_pages, c->table_width, (double)p->softmax_scale};
   const long long grid = (long long)p->batch * p->n_kv_heads;
   if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   const size_t smem = paged8_update_smem_bytes(p);
-  if (cudaFuncSetAttribute(paged8_update_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return LCA_ERR_CUDA;
-  paged8_update_kernel<<<(unsigned)grid, UPD_THREADS, smem, stream>>>(a);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+  if (p->variant == LCA_VARIANT_MLA) return p->d_sem == 512 ? update8_launch<true, 512, 64>(a, grid, smem, stream)
+                                                            : update8_launch<true, 128, 64>(a, grid, smem, stream);
+  return p->d_sem == 128 ? update8_launch<false, 128, 128>(a, grid, smem, stream) : update8_launch<false, 64, 64>(a, grid, smem, stream);
 }
 
 }  // namespace lca
