@@ -43,6 +43,10 @@ class LcaPaged8(C.Structure):
     the tensors alive."""
     _fields_ = [("pages_sem", C.c_void_p), ("pages_pos", C.c_void_p), ("scale_sem", C.c_void_p), ("scale_pos", C.c_void_p),
                 ("block_table", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("table_width", C.c_int32)]
+    tensors: tuple = ()
+    device: Optional[int] = None               # CUDA device of the tensors (-1: not on one)
+    batch: Optional[int] = None                # rows of block_table
+    layout: Optional[tuple] = None             # (n_kv_heads, d_sem, d_pos) of the pages
 
 
 class LcaError(RuntimeError):
@@ -528,15 +532,29 @@ def paged8_cache(pages_sem, pages_pos, scale_sem, scale_pos, block_table, page_s
                  n_pages: Optional[int] = None) -> LcaPaged8:
     """Descriptor of a paged 8-bit cache over the caller's tensors (any of them may be None for calls that do not use it):
     pages [n_pages, Hkv, page_size, d] of one byte per element (uint8 or float8_e4m3fn), scales [n_pages, Hkv] float32,
-    block_table [batch, table_width] int32."""
+    block_table [batch, table_width] int32, all on one device.  ``page_update`` needs the table, page_size and n_pages only."""
     if pages_sem is not None:
         n_pages, page_size = pages_sem.shape[0], pages_sem.shape[2]
+    tensors = (pages_sem, pages_pos, scale_sem, scale_pos, block_table)
     for t, want in ((pages_sem, 1), (pages_pos, 1), (scale_sem, 4), (scale_pos, 4), (block_table, 4)):
-        if t is not None and t.element_size() != want:
+        if t is not None and (t.element_size() != want or (want == 4 and t.is_floating_point() == (t is block_table))):
             raise ValueError("pages hold one byte per element, scales are float32, block tables int32")
+    if len({t.device for t in tensors if t is not None}) > 1:
+        raise ValueError("the pages, scales and tables of a cache are on one device")
+    if pages_pos is not None and (pages_sem is None or pages_pos.shape[:3] != pages_sem.shape[:3]):
+        raise ValueError("both pools have the same pages: [n_pages, Hkv, page_size, d]")
+    for t in (scale_sem, scale_pos):
+        if t is not None and (pages_sem is None or t.shape != pages_sem.shape[:2]):
+            raise ValueError("a scale for each page and KV head: [n_pages, Hkv]")
+    if block_table is not None and block_table.dim() != 2:
+        raise ValueError("block_table is [batch, table_width]")
     c = LcaPaged8(_ptr(pages_sem), _ptr(pages_pos), _ptr(scale_sem), _ptr(scale_pos), _ptr(block_table), int(n_pages or 0),
                   int(page_size or 0), 0 if block_table is None else block_table.shape[1])
-    c.tensors = (pages_sem, pages_pos, scale_sem, scale_pos, block_table)
+    c.tensors = tensors
+    c.device = next((t.get_device() for t in tensors if t is not None), None)
+    c.batch = None if block_table is None else block_table.shape[0]
+    if pages_sem is not None and pages_pos is not None:
+        c.layout = (pages_sem.shape[1], pages_sem.shape[3], pages_pos.shape[3])
     return c
 
 
@@ -550,19 +568,61 @@ def new_paged8_cache(params: LcaParams, n_pages: int, page_size: int, table_widt
                         torch.full((params.batch, table_width), -1, dtype=torch.int32, device=device))
 
 
+_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+
+
+def _arg(x, dtype, n, dev):
+    """Address of a dense tensor of this type with at least n elements on device dev; None stays None."""
+    if x is None:
+        return None
+    if x.dtype is not dtype or x.get_device() != dev or x.numel() < n or not x.is_contiguous():
+        raise ValueError(f"expected a dense {dtype} tensor of at least {n} elements on cuda:{dev}, not "
+                         f"{x.dtype} {list(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _paged8_device(params: LcaParams, cache: LcaPaged8, table: bool = True) -> int:
+    """The cache's device, which has to be the current one; its tables and pages have to be those of params."""
+    dev = cache.device
+    if dev is None or dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError("the cache's tensors are not on the current CUDA device")
+    if table and (cache.batch is None or cache.batch < params.batch):
+        raise ValueError("block_table has a row for every sequence of params.batch")
+    if cache.layout is not None and cache.layout != (params.n_kv_heads, params.d_sem, params.d_pos):
+        raise ValueError(f"pages of (n_kv_heads, d_sem, d_pos) = {cache.layout} do not belong to these parameters")
+    return dev
+
+
+def _new(make, shape, dtype, device, stream):
+    """A tensor for the caller made on the stream that its call runs on: its memory, and the fill, then come before the call."""
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(stream))
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
 def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, row_offsets,
                 status, rows_per_seq: int = 0, stream=None):
     """Run lca_page_update in place on the tables, the free list and the held state; returns slot_map.  `status` is a device
     tensor: read it where the caller has to know (0: done)."""
-    n_rows = 0 if slot_map is None else slot_map.numel()
-    _check(lca_page_update(params, cache, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, n_rows, rows_per_seq,
-                           row_offsets, status, stream=stream), "lca_page_update")
+    dev, B = _paged8_device(params, cache), params.batch
+    _check(_lib.lca_page_update(C.byref(params), C.byref(cache), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev),
+                                _arg(held_rep, _I32, B, dev), _arg(held_tok, _I32, B, dev), _arg(free_pages, _I32, cache.n_pages, dev),
+                                _arg(n_free, _I32, 1, dev), _arg(slot_map, _I32, 0, dev), 0 if slot_map is None else slot_map.numel(),
+                                rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), _arg(status, _I32, 1, dev), _stream(stream)),
+           "lca_page_update")
     return slot_map
 
 
 def paged8_write(params: LcaParams, cache: LcaPaged8, rows_sem, rows_pos, slot_map, stream=None):
     """Quantise rows into the pages that slot_map names (in place)."""
-    _check(lca_paged8_write(params, cache, rows_sem, rows_pos, slot_map, slot_map.numel(), stream=stream), "lca_paged8_write")
+    dev, n = _paged8_device(params, cache, table=False), slot_map.numel()
+    rows = n * params.n_kv_heads
+    _check(_lib.lca_paged8_write(C.byref(params), C.byref(cache), _arg(rows_sem, _BF16, rows * params.d_sem, dev),
+                                 _arg(rows_pos, _BF16, rows * params.d_pos, dev), _arg(slot_map, _I32, n, dev), n, _stream(stream)),
+           "lca_paged8_write")
 
 
 def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) -> torch.Tensor:
@@ -572,33 +632,42 @@ def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) ->
 def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
                             want_lse: bool = False, ws=None, stream=None):
     """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
-    B, q_len, H = q_pos.shape[:3]
+    dev, B, q_len, H = _paged8_device(params, cache), params.batch, q_pos.shape[1], params.n_q_heads
     if out is None:
-        out = torch.empty((B, q_len, H, params.d_sem), dtype=torch.bfloat16, device=q_pos.device)
+        out = _new(torch.empty, (B, q_len, H, params.d_sem), _BF16, q_pos.device, stream)
     if lse is None and want_lse:
-        lse = torch.empty((B, q_len, H), dtype=torch.float32, device=q_pos.device)
+        lse = _new(torch.empty, (B, q_len, H), _F32, q_pos.device, stream)
     if ws is None:
-        ws = workspace_paged8(params, cache, q_len, q_pos.device)
-    _check(lca_decode_attention_paged8(params, cache, q_sem, q_pos, q_len, n_rep, n_tok, out, lse, ws, stream=stream),
-           "lca_decode_attention_paged8")
+        ws = _new(torch.empty, max(lca_paged8_workspace_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
+    rows = B * q_len * H
+    _check(_lib.lca_decode_attention_paged8(
+        C.byref(params), C.byref(cache), _arg(q_sem, _BF16, rows * params.d_sem, dev), _arg(q_pos, _BF16, rows * params.d_pos, dev), q_len,
+        _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * params.d_sem, dev), _arg(lse, _F32, rows, dev),
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), _stream(stream)), "lca_decode_attention_paged8")
     return out, lse
 
 
 def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
                          rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
-    """Run lca_decode_update_paged8; returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
-    dev, B, Hkv = n_tok.device, params.batch, params.n_kv_heads
+    """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], the n latest positions, or the ready summary query qbar
+    [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
+    dev, B, Hkv, d_sem, d_pos = _paged8_device(params, cache), params.batch, params.n_kv_heads, params.d_sem, params.d_pos
     if n_rep_new is None:
-        n_rep_new = torch.empty_like(n_rep)
+        n_rep_new = _new(torch.empty, (B,), _I32, n_tok.device, stream)
     if rep_sem is None:
-        rep_sem = torch.zeros((B, Hkv, params.d_sem), dtype=torch.bfloat16, device=dev)
+        rep_sem = _new(torch.zeros, (B, Hkv, d_sem), _BF16, n_tok.device, stream)
     if rep_pos is None:
-        rep_pos = torch.zeros((B, Hkv, params.d_pos), dtype=torch.bfloat16, device=dev)
+        rep_pos = _new(torch.zeros, (B, Hkv, d_pos), _BF16, n_tok.device, stream)
     if anchor is None:
-        anchor = torch.empty((B, Hkv), dtype=torch.int32, device=dev)
+        anchor = _new(torch.empty, (B, Hkv), _I32, n_tok.device, stream)
     if ws is None:
-        ws = workspace(params, LCA_WS_UPDATE, dev)
+        ws = _new(torch.empty, max(lca_workspace_bytes(params, LCA_WS_UPDATE), 16), torch.uint8, n_tok.device, stream)
     n = params.n_summary_q if params.n_summary_q > 0 else params.group_size
-    _check(lca_decode_update_paged8(params, cache, q_tail_sem, q_tail_pos, n, qbar, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, anchor,
-                                    ws, stream=stream), "lca_decode_update_paged8")
+    rows, blocks = B * n * params.n_q_heads, B * Hkv
+    dk = d_pos + (d_sem if params.variant == LCA_VARIANT_MLA else 0)
+    _check(_lib.lca_decode_update_paged8(
+        C.byref(params), C.byref(cache), _arg(q_tail_sem, _BF16, rows * d_sem, dev), _arg(q_tail_pos, _BF16, rows * d_pos, dev), n,
+        _arg(qbar, _F32, blocks * dk, dev), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(n_rep_new, _I32, B, dev),
+        _arg(rep_sem, _BF16, blocks * d_sem, dev), _arg(rep_pos, _BF16, blocks * d_pos, dev), _arg(anchor, _I32, blocks, dev),
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), _stream(stream)), "lca_decode_update_paged8")
     return n_rep_new, rep_sem, rep_pos, anchor

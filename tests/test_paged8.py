@@ -107,3 +107,40 @@ def test_reference_codes_are_the_format():
     # torch converts by way of float32: no difference unless a value lies within 2^-24 of a boundary
     assert np.array_equal(R.encode(x), want)
     assert R.block_scale([0.0, np.nan, np.inf]) == 2.0 ** -100 and R.block_scale([448.0]) == 1.0 and R.block_scale([449.0]) == 2.0
+
+
+def test_limits_of_tables_and_of_the_launch(B):
+    big = B.make_params("mla", 1 << 20, 1, 16, 1, 512, 64, 64, 64, 0.07)
+    before = B.lca_launch_count()
+    wide = cache(B, table_width=1 << 11)                                      # 2^20 sequences x 2^11 entries
+    assert B.lca_page_update(big, wide, 16, 16, 16, 16, 16, 16, None, 0, 0, None, 16) == -1
+    assert B.lca_decode_attention_paged8(big, wide, 16, 16, 1, 16, 16, 16, None, 16, 1 << 40) == -1
+    assert B.lca_decode_update_paged8(big, wide, None, None, 64, 16, 16, 16, 32, 16, 16, 16, 16, 1 << 40) == -1
+    heads = B.make_params("gqa", 1, 1, 1 << 16, 1 << 16, 64, 64, 64, 64, 0.07)
+    assert B.lca_paged8_write(heads, cache(B, n_pages=1 << 15, scale_pos=16), 16, 16, 16, 8) == -1       # 2^31 blocks
+    assert B.lca_launch_count() == before
+
+
+def test_helpers_refuse_tensors_that_are_not_on_the_current_device(B, p):
+    c = B.new_paged8_cache(p, 8, 16, 4, "cpu")
+    i = torch.zeros(64, dtype=torch.int32)
+    before = B.lca_launch_count()
+    with pytest.raises(ValueError):
+        B.page_update(p, c, i, i, i, i, i, i, i, i, i)
+    with pytest.raises(ValueError):
+        B.paged8_write(p, c, torch.zeros((4, 1, 512), dtype=torch.bfloat16), torch.zeros((4, 1, 64), dtype=torch.bfloat16), i[:4])
+    with pytest.raises(ValueError):
+        B.decode_attention_paged8(p, c, torch.zeros((2, 1, 16, 512)).bfloat16(), torch.zeros((2, 1, 16, 64)).bfloat16(), i, i)
+    with pytest.raises(ValueError):
+        B.decode_update_paged8(p, c, None, None, i, i, qbar=torch.zeros((2, 1, 576)))
+    assert B.lca_launch_count() == before
+
+
+def test_descriptor_refuses_pools_that_do_not_fit_together(B):
+    t, s = torch.zeros((4, 2, 16, 128), dtype=torch.uint8), torch.ones((4, 2))
+    table = torch.zeros((2, 3), dtype=torch.int32)
+    B.paged8_cache(t, t, s, s, table)
+    for bad in ((t, t[:3], s, s, table), (t, t, s[:3], s, table), (t, t, s, torch.ones((4, 1)), table), (t, t, s, s, table[0]),
+                (t, t, s.int(), s, table), (t, t, s, s, table.float()), (None, t, s, s, table)):
+        with pytest.raises(ValueError):
+            B.paged8_cache(*bad)

@@ -498,7 +498,8 @@ def test_calls_are_capturable_reproducible_and_independent_of_the_stream(B, head
 
 # ------------------------------------------------------------------------------------------------------------ update
 @pytest.mark.parametrize("shape,heads,kv,g,page,w", [("mla512", 16, 1, 64, 64, 64), ("mla512", 16, 1, 16, 16, 0), ("gqa128", 8, 2, 32, 16, 40),
-                                                     ("mla128", 4, 1, 128, 32, 7), ("gqa64", 4, 4, 64, 64, 64)])
+                                                     ("mla128", 4, 1, 128, 32, 7), ("gqa64", 4, 4, 64, 64, 64),
+                                                     ("mla512", 16, 1, 208, 16, 3), ("gqa128", 9, 3, 80, 16, 0), ("gqa64", 4, 2, 48, 16, 5)])
 def test_update_against_the_definition(B, shape, heads, kv, g, page, w):
     variant, _, d_sem, d_pos = SHAPES[shape]
     states = [(0, w + g), (0, w + g - 1), (3, 3 * g + w + g), (2, 2 * g + w + g + 5), (0, 0), (1, g), (1, g + w + g)]
@@ -544,6 +545,91 @@ def test_update_with_a_query_tail_equals_the_ready_query(B):
     assert torch.equal(a[0], b[0]) and torch.equal(a[3], b[3]) and torch.equal(a[2], b[2])
     # the fp32 summary query differs from the fp64 one by 2^-24: the weights by 2^-24 sum|q k| < 2^-17, the result by one bf16 step
     assert torch.all((a[1].float() - b[1].float()).abs() <= 2.0 ** -7 * b[1].float().abs() + 2.0 ** -15 * 30)
+
+
+# ------------------------------------------------------------------------------------------- streams, graphs, refusals
+def decode_case(B, heads, seed, variant="mla512", kv=1):
+    states = [(3, 3 * 64 + 200), (0, 700), (2, 2 * 64 + 90)]
+    pool_, table = build(B, variant, kv, 64, states, 64, seed, hole_nan=False)
+    _, _, d_sem, d_pos = SHAPES[variant]
+    p = B.make_params(SHAPES[variant][0], 3, 1, heads, kv, d_sem, d_pos, 64, 64, 0.07)
+    cache, _ = to_gpu(B, pool_, torch.from_numpy(table).to(DEV))
+    g = torch.Generator().manual_seed(seed)
+    q_sem = torch.randn((3, 1, heads, d_sem), generator=g).bfloat16().to(DEV) if variant[:3] == "mla" else None
+    q_pos = torch.randn((3, 1, heads, d_pos), generator=g).bfloat16().to(DEV)
+    qbar = torch.randn((3, kv, d_pos + (d_sem if q_sem is not None else 0)), generator=g).to(DEV)
+    return p, cache, q_sem, q_pos, i32([s[0] for s in states]), i32([s[1] for s in states]), qbar
+
+
+def test_results_made_on_another_stream(B):
+    """Outputs and workspaces that a call makes itself belong to the stream it runs on."""
+    p, cache, q_sem, q_pos, n_rep, n_tok, qbar = decode_case(B, 40, 3)
+    want = B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok, want_lse=True)
+    up = B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        for _ in range(3):
+            x = torch.full((1 << 28,), 7, dtype=torch.uint8, device=DEV)       # written, and free for reuse, on the current stream
+            x = x + 1
+            del x
+            out, lse = B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok, want_lse=True, stream=stream)
+            got = B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar, stream=stream)
+            torch.cuda.synchronize()
+            assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+            assert all(torch.equal(a, b) for a, b in zip(got, up))
+
+
+def test_two_calls_at_once(B):
+    """Two streams, each with its own cache and workspace, in flight together; then two graphs that share one workspace."""
+    cases = [decode_case(B, 128, 5), decode_case(B, 16, 6, "gqa128", 2)]
+    want = [B.decode_attention_paged8(*c[:6], want_lse=True) for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    got = [[] for _ in cases]
+    for _ in range(20):
+        for c, st, o in zip(cases, streams, got):
+            o.append(B.decode_attention_paged8(*c[:6], want_lse=True, stream=st))
+    torch.cuda.synchronize()
+    for w, o in zip(want, got):
+        assert all(torch.equal(x[0], w[0]) and torch.equal(x[1], w[1]) for x in o)
+    ws = torch.empty(max(B.lca_paged8_workspace_bytes(c[0], c[1], 1) for c in cases), dtype=torch.uint8, device=DEV)
+    outs = [torch.zeros_like(w[0]) for w in want]
+    graphs = [torch.cuda.CUDAGraph() for _ in cases]
+    for c, o, gr in zip(cases, outs, graphs):
+        with torch.cuda.graph(gr):
+            B.decode_attention_paged8(*c[:6], out=o, ws=ws)
+    ws.fill_(0xff)
+    for gr in graphs + graphs[::-1]:
+        gr.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, w[0]) for o, w in zip(outs, want))
+
+
+def test_helpers_refuse_tensors_that_do_not_fit(B):
+    p, cache, q_sem, q_pos, n_rep, n_tok, qbar = decode_case(B, 16, 4)
+    before = B.lca_launch_count()
+    more = B.make_params("mla", 4, 1, 16, 1, 512, 64, 64, 64, 0.07)             # a sequence more than the table has rows
+    other = B.make_params("gqa", 3, 1, 16, 1, 128, 128, 64, 64, 0.07)
+    calls = [lambda: B.decode_attention_paged8(p, cache, q_sem.half(), q_pos, n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, q_pos[:2], n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, q_pos.transpose(0, 2), n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok.long()),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep.cpu(), n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok, out=q_sem[:1]),
+             lambda: B.decode_attention_paged8(more, cache, q_sem, q_pos, n_rep, n_tok),
+             lambda: B.decode_attention_paged8(other, cache, None, q_pos, n_rep, n_tok),
+             lambda: B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar.double()),
+             lambda: B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar[:2]),
+             lambda: B.decode_update_paged8(p, cache, q_sem, q_pos, n_rep, n_tok),                   # one position, not group_size
+             lambda: B.paged8_write(p, cache, q_sem, q_pos, torch.zeros(100, dtype=torch.int32, device=DEV)),
+             lambda: B.paged8_write(p, cache, q_sem, q_pos, torch.zeros(3, device=DEV)),
+             lambda: B.page_update(p, cache, n_rep, n_tok, n_rep, n_tok, n_tok[:1], n_tok, None, None, n_tok)]
+    for k, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("call %d was not refused" % k)
+    assert B.lca_launch_count() == before
 
 
 # --------------------------------------------------------------------------------------------------- the run of calls
