@@ -581,16 +581,18 @@ def _arg(x, dtype, n, dev):
     return x.data_ptr()
 
 
-def _paged8_device(params: LcaParams, cache: LcaPaged8, table: bool = True) -> int:
-    """The cache's device, which has to be the current one; its tables and pages have to be those of params."""
+def _paged8_device(params: LcaParams, cache: LcaPaged8, stream, table: bool = True):
+    """The cache's device, which has to be the current one, the stream to launch on and (n_kv_heads, d_sem, d_pos); the
+    tables and pages have to be those of params."""
     dev = cache.device
     if dev is None or dev < 0 or dev != torch.cuda.current_device():
         raise ValueError("the cache's tensors are not on the current CUDA device")
     if table and (cache.batch is None or cache.batch < params.batch):
         raise ValueError("block_table has a row for every sequence of params.batch")
-    if cache.layout is not None and cache.layout != (params.n_kv_heads, params.d_sem, params.d_pos):
+    layout = (params.n_kv_heads, params.d_sem, params.d_pos)
+    if cache.layout != layout and cache.layout is not None:
         raise ValueError(f"pages of (n_kv_heads, d_sem, d_pos) = {cache.layout} do not belong to these parameters")
-    return dev
+    return dev, torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream), layout
 
 
 def _new(make, shape, dtype, device, stream):
@@ -607,22 +609,21 @@ def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, hel
                 status, rows_per_seq: int = 0, stream=None):
     """Run lca_page_update in place on the tables, the free list and the held state; returns slot_map.  `status` is a device
     tensor: read it where the caller has to know (0: done)."""
-    dev, B = _paged8_device(params, cache), params.batch
+    dev, at, _ = _paged8_device(params, cache, stream)
+    B = params.batch
     _check(_lib.lca_page_update(C.byref(params), C.byref(cache), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev),
                                 _arg(held_rep, _I32, B, dev), _arg(held_tok, _I32, B, dev), _arg(free_pages, _I32, cache.n_pages, dev),
                                 _arg(n_free, _I32, 1, dev), _arg(slot_map, _I32, 0, dev), 0 if slot_map is None else slot_map.numel(),
-                                rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), _arg(status, _I32, 1, dev), _stream(stream)),
-           "lca_page_update")
+                                rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), _arg(status, _I32, 1, dev), at), "lca_page_update")
     return slot_map
 
 
 def paged8_write(params: LcaParams, cache: LcaPaged8, rows_sem, rows_pos, slot_map, stream=None):
     """Quantise rows into the pages that slot_map names (in place)."""
-    dev, n = _paged8_device(params, cache, table=False), slot_map.numel()
-    rows = n * params.n_kv_heads
-    _check(_lib.lca_paged8_write(C.byref(params), C.byref(cache), _arg(rows_sem, _BF16, rows * params.d_sem, dev),
-                                 _arg(rows_pos, _BF16, rows * params.d_pos, dev), _arg(slot_map, _I32, n, dev), n, _stream(stream)),
-           "lca_paged8_write")
+    dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream, table=False)
+    n = slot_map.numel()
+    _check(_lib.lca_paged8_write(C.byref(params), C.byref(cache), _arg(rows_sem, _BF16, n * Hkv * d_sem, dev),
+                                 _arg(rows_pos, _BF16, n * Hkv * d_pos, dev), _arg(slot_map, _I32, n, dev), n, at), "lca_paged8_write")
 
 
 def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) -> torch.Tensor:
@@ -632,18 +633,19 @@ def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) ->
 def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
                             want_lse: bool = False, ws=None, stream=None):
     """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
-    dev, B, q_len, H = _paged8_device(params, cache), params.batch, q_pos.shape[1], params.n_q_heads
+    dev, at, (_, d_sem, d_pos) = _paged8_device(params, cache, stream)
+    B, q_len, H = params.batch, q_pos.shape[1], params.n_q_heads
     if out is None:
-        out = _new(torch.empty, (B, q_len, H, params.d_sem), _BF16, q_pos.device, stream)
+        out = _new(torch.empty, (B, q_len, H, d_sem), _BF16, q_pos.device, stream)
     if lse is None and want_lse:
         lse = _new(torch.empty, (B, q_len, H), _F32, q_pos.device, stream)
     if ws is None:
         ws = _new(torch.empty, max(lca_paged8_workspace_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
     rows = B * q_len * H
     _check(_lib.lca_decode_attention_paged8(
-        C.byref(params), C.byref(cache), _arg(q_sem, _BF16, rows * params.d_sem, dev), _arg(q_pos, _BF16, rows * params.d_pos, dev), q_len,
-        _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * params.d_sem, dev), _arg(lse, _F32, rows, dev),
-        _arg(ws, torch.uint8, 0, dev), ws.numel(), _stream(stream)), "lca_decode_attention_paged8")
+        C.byref(params), C.byref(cache), _arg(q_sem, _BF16, rows * d_sem, dev), _arg(q_pos, _BF16, rows * d_pos, dev), q_len,
+        _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * d_sem, dev), _arg(lse, _F32, rows, dev),
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_attention_paged8")
     return out, lse
 
 
@@ -651,7 +653,8 @@ def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail
                          rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
     """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], the n latest positions, or the ready summary query qbar
     [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
-    dev, B, Hkv, d_sem, d_pos = _paged8_device(params, cache), params.batch, params.n_kv_heads, params.d_sem, params.d_pos
+    dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream)
+    B = params.batch
     if n_rep_new is None:
         n_rep_new = _new(torch.empty, (B,), _I32, n_tok.device, stream)
     if rep_sem is None:
@@ -669,5 +672,5 @@ def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail
         C.byref(params), C.byref(cache), _arg(q_tail_sem, _BF16, rows * d_sem, dev), _arg(q_tail_pos, _BF16, rows * d_pos, dev), n,
         _arg(qbar, _F32, blocks * dk, dev), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(n_rep_new, _I32, B, dev),
         _arg(rep_sem, _BF16, blocks * d_sem, dev), _arg(rep_pos, _BF16, blocks * d_pos, dev), _arg(anchor, _I32, blocks, dev),
-        _arg(ws, torch.uint8, 0, dev), ws.numel(), _stream(stream)), "lca_decode_update_paged8")
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_update_paged8")
     return n_rep_new, rep_sem, rep_pos, anchor
