@@ -547,6 +547,39 @@ def test_update_with_a_query_tail_equals_the_ready_query(B):
     assert torch.all((a[1].float() - b[1].float()).abs() <= 2.0 ** -7 * b[1].float().abs() + 2.0 ** -15 * 30)
 
 
+# -------------------------------------------------------------------------------------------------------- large pools
+@pytest.mark.parametrize("shape,heads,kv,n_pages", [("mla512", 16, 1, 140000), ("mla512", 128, 1, 140000), ("gqa128", 16, 8, 70000)])
+def test_pages_behind_four_gigabytes(B, shape, heads, kv, n_pages):
+    """The last pages of a pool of 4.6 GB give what the same pages of a small pool give, bit for bit."""
+    variant, _, d_sem, d_pos = SHAPES[shape]
+    states = [(1, 64 + 200), (0, 130)]
+    pool_, table = build(B, shape, kv, 64, states, 64, 9, hole_nan=False)
+    small, t = to_gpu(B, pool_, torch.from_numpy(table).to(DEV))
+    first = n_pages - t[0].shape[0]
+    large = [None if x is None else torch.empty((n_pages,) + x.shape[1:], dtype=x.dtype, device=DEV) for x in t]
+    for x, y in zip(t, large):
+        if x is not None:
+            y[first:] = x
+    big = B.paged8_cache(*large, torch.from_numpy(np.where(table < 0, table, table + first).astype(np.int32)).to(DEV))
+    p = B.make_params(variant, 2, 1, heads, kv, d_sem, d_pos, 64, 64, 0.07)
+    g = torch.Generator().manual_seed(2)
+    q_sem = torch.randn((2, 1, heads, d_sem), generator=g).bfloat16().to(DEV) if variant == "mla" else None
+    q_pos = torch.randn((2, 1, heads, d_pos), generator=g).bfloat16().to(DEV)
+    qbar = torch.randn((2, kv, d_pos + (d_sem if variant == "mla" else 0)), generator=g).to(DEV)
+    rows = [torch.randn((70, kv, d), generator=g).bfloat16().to(DEV) for d in (d_sem, d_pos)]
+    n_rep, n_tok = i32([s[0] for s in states]), i32([s[1] for s in states])
+    slots = torch.cat([torch.arange(64, 128), torch.arange(10, 16)]).int().to(DEV)
+    got = []
+    for cache, at in ((small, 0), (big, first)):
+        out, lse = B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok, want_lse=True)
+        up = B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar)
+        B.paged8_write(p, cache, *rows, slots + 64 * at)
+        got.append([out, lse, *up])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert all(x is None or torch.equal(x, y[first:]) for x, y in zip(t, large))
+
+
 # ------------------------------------------------------------------------------------------- streams, graphs, refusals
 def decode_case(B, heads, seed, variant="mla512", kv=1):
     states = [(3, 3 * 64 + 200), (0, 700), (2, 2 * 64 + 90)]
