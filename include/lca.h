@@ -293,7 +293,7 @@ int lca_decode_step_update_ring(const lca_params* p, const void* q_sem, const vo
 
 /* ---- Paged 8-bit cache ----------------------------------------------------------------------
  * The decode cache of many sequences in one pool of pages, each row element held in 8 bits (e4m3) with one
- * fp32 scale for each (page, KV head): value = code * scale.
+ * positive fp32 scale for each (page, KV head): value = code * scale.
  *
  * Rows are addressed by position, so nothing moves when a group is condensed: token number n of a sequence is
  * row n; representative j is row j, which belonged to a token condensed long before (n_rep <= n_rep * group_size).
