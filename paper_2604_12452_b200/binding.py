@@ -568,6 +568,8 @@ def new_paged8_cache(params: LcaParams, n_pages: int, page_size: int, table_widt
                         torch.full((params.batch, table_width), -1, dtype=torch.int32, device=device))
 
 
+# The helpers below are called for every step of every layer: ctypes takes the structures as they are (the declared argument
+# types make it pass their address), which costs half of what C.byref does.
 _I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
 
 
@@ -611,7 +613,7 @@ def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, hel
     tensor: read it where the caller has to know (0: done)."""
     dev, at, _ = _paged8_device(params, cache, stream)
     B = params.batch
-    _check(_lib.lca_page_update(C.byref(params), C.byref(cache), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev),
+    _check(_lib.lca_page_update(params, cache, _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev),
                                 _arg(held_rep, _I32, B, dev), _arg(held_tok, _I32, B, dev), _arg(free_pages, _I32, cache.n_pages, dev),
                                 _arg(n_free, _I32, 1, dev), _arg(slot_map, _I32, 0, dev), 0 if slot_map is None else slot_map.numel(),
                                 rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), _arg(status, _I32, 1, dev), at), "lca_page_update")
@@ -622,7 +624,7 @@ def paged8_write(params: LcaParams, cache: LcaPaged8, rows_sem, rows_pos, slot_m
     """Quantise rows into the pages that slot_map names (in place)."""
     dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream, table=False)
     n = slot_map.numel()
-    _check(_lib.lca_paged8_write(C.byref(params), C.byref(cache), _arg(rows_sem, _BF16, n * Hkv * d_sem, dev),
+    _check(_lib.lca_paged8_write(params, cache, _arg(rows_sem, _BF16, n * Hkv * d_sem, dev),
                                  _arg(rows_pos, _BF16, n * Hkv * d_pos, dev), _arg(slot_map, _I32, n, dev), n, at), "lca_paged8_write")
 
 
@@ -643,7 +645,7 @@ def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n
         ws = _new(torch.empty, max(lca_paged8_workspace_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
     rows = B * q_len * H
     _check(_lib.lca_decode_attention_paged8(
-        C.byref(params), C.byref(cache), _arg(q_sem, _BF16, rows * d_sem, dev), _arg(q_pos, _BF16, rows * d_pos, dev), q_len,
+        params, cache, _arg(q_sem, _BF16, rows * d_sem, dev), _arg(q_pos, _BF16, rows * d_pos, dev), q_len,
         _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * d_sem, dev), _arg(lse, _F32, rows, dev),
         _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_attention_paged8")
     return out, lse
@@ -669,7 +671,7 @@ def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail
     rows, blocks = B * n * params.n_q_heads, B * Hkv
     dk = d_pos + (d_sem if params.variant == LCA_VARIANT_MLA else 0)
     _check(_lib.lca_decode_update_paged8(
-        C.byref(params), C.byref(cache), _arg(q_tail_sem, _BF16, rows * d_sem, dev), _arg(q_tail_pos, _BF16, rows * d_pos, dev), n,
+        params, cache, _arg(q_tail_sem, _BF16, rows * d_sem, dev), _arg(q_tail_pos, _BF16, rows * d_pos, dev), n,
         _arg(qbar, _F32, blocks * dk, dev), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(n_rep_new, _I32, B, dev),
         _arg(rep_sem, _BF16, blocks * d_sem, dev), _arg(rep_pos, _BF16, blocks * d_pos, dev), _arg(anchor, _I32, blocks, dev),
         _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_update_paged8")

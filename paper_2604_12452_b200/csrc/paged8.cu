@@ -251,15 +251,20 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
   // many threads; otherwise the barriers of a cluster cost more than its threads bring.
   const long long entries = (long long)p->batch * c->table_width;
   const bool big = p->batch > PAGE_THREADS || a.n_rows > 8192 || (!slot_map && entries > 8192);
+  if (!big) {
+    page_update_kernel<<<1, PAGE_THREADS, 0, stream>>>(a);
+    note_launch();
+    return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+  }
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(big ? 16 : 1);
+  cfg.gridDim = dim3(16);
   cfg.blockDim = dim3(PAGE_THREADS);
   cfg.stream = stream;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = cfg.gridDim.x; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
   cfg.attrs = at; cfg.numAttrs = 1;
-  if (big && cudaFuncSetAttribute(page_update_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LCA_ERR_CUDA;
+  if (cudaFuncSetAttribute(page_update_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LCA_ERR_CUDA;
   if (cudaLaunchKernelEx(&cfg, page_update_kernel, a) != cudaSuccess) return LCA_ERR_CUDA;
   note_launch();
   return LCA_OK;
@@ -676,7 +681,8 @@ size_t paged8_update_smem_bytes(const lca_params* p) {
 template <bool MLA, int DS, int DP>
 static int update8_launch(const Update8Args& a, long long grid, size_t smem, cudaStream_t stream) {
   auto kern = paged8_update_kernel<MLA, DS, DP>;
-  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess) return LCA_ERR_CUDA;
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+    return LCA_ERR_CUDA;
   kern<<<(unsigned)grid, UPD_THREADS, smem, stream>>>(a);
   note_launch();
   return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
