@@ -194,7 +194,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
   }
   if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
   if (warp == W_TMA && lane == 0) { prefetch_tmap(&p.sem); prefetch_tmap(&p.pos); }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");        // the whole grid is resident: nothing is displaced
+  chain_wait();
+  chain_next();                                              // the whole grid is resident: nothing is displaced
   paged8_range<PL::THREADS>(p, (int)blockIdx.x, s_warp, s_b, s_off);
   __syncthreads();
   tc_fence_after();
@@ -611,9 +612,8 @@ template <class PL>
 static int paged8_launch(Paged8Params& P, cudaStream_t stream) {
   auto kern = attn_paged8_kernel<PL>;
   if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM) != cudaSuccess) return LCA_ERR_CUDA;
-  kern<<<P.grid, PL::THREADS, PL::SMEM, stream>>>(P);
-  note_launch();
-  if (cudaGetLastError() != cudaSuccess) return LCA_ERR_CUDA;
+  const int st = launch_chained(kern, (unsigned)P.grid, PL::THREADS, PL::SMEM, stream, 1, P);
+  if (st != LCA_OK) return st;
   return paged8_combine_launch<PL::DS, PL::NH>(P, stream);
 }
 template <bool MLA, int DS, int DP>

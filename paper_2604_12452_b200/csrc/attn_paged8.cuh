@@ -20,7 +20,7 @@ struct Paged8Params {
   const int32_t* n_rep; const int32_t* n_tok;
   bf16* out; float* lse;
   float* part;                // [2 * grid][NH][DS] partial O, then [2 * grid][2][NH] M and l
-  long long* prefix;          // [B + 2] tiles before each sequence (all units), then 1 where every unit has a CTA; written by CTA 0
+  long long* prefix;          // [B + 2] tiles before each sequence (all units), then 1 where every unit has a CTA; for B > MERGE_B, written by CTA 0
   int B, Hq, Hkv, q_len, g, page, page_log2, n_pages, width, rep, n_blk, grid;   // grid: CTAs (pairs of them) that share the line
   int out_wide;               // out is 32-byte aligned
   float scale_log2, bias_log2;
@@ -90,10 +90,13 @@ struct Walk {
 
 // The range of CTA (or CTA pair) `id` (s_warp: room for 12 bytes a warp): thread i sums the tiles of sequences [i q, (i + 1) q); every thread of the CTA calls it.
 // Leaves the first sequence in *s_b, the offset inside it and the tiles of the range in s_off[0 .. 1]; ends with a barrier
-// still to come.  CTA 0 of the grid writes the prefix sums for the merging kernel.
+// still to come.  CTA 0 of the grid writes the prefix sums for the merging kernel, which finds those of few sequences itself.
 // Where there are no more units than CTAs and the longest is at most WHOLE_SLACK tiles above the mean of all CTAs, every unit
 // has a CTA of its own: a cut costs a second query load, a partial result and its merging, about as much as that many tiles.
-static constexpr int WHOLE_SLACK = 8;
+static constexpr int WHOLE_SLACK = 8, MERGE_B = 256;
+__device__ __forceinline__ bool units_whole(const Paged8Params& p, long long upu, int longest, long long T) {
+  return p.B * upu <= p.grid && (long long)(longest - WHOLE_SLACK) * p.grid <= T;
+}
 template <int THREADS>
 __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long long* s_warp, int* s_b, long long* s_off) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -118,8 +121,8 @@ __device__ __forceinline__ void paged8_range(const Paged8Params& p, int id, long
     T += s_warp[w];
     longest = max(longest, s_longest[w]);
   }
-  const bool own = p.B * upu <= p.grid && (long long)(longest - WHOLE_SLACK) * p.grid <= T;
-  if (blockIdx.x == 0) {
+  const bool own = units_whole(p, upu, longest, T);
+  if (blockIdx.x == 0 && p.B > MERGE_B) {
     long long at = before;
 #pragma unroll 1
     for (int b = lo; b < hi; ++b) { p.prefix[b] = at; at += (q == 1 ? n_only : tile_span(p, b).n) * upu; }
@@ -229,24 +232,46 @@ __device__ __forceinline__ float ex2(float x) { float r; asm("ex2.approx.ftz.f32
 __device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x)); return r; }
 // Merges the pieces of the units that were cut, in the order of their tiles, and writes the rows of sequences that have
 // no tile at all.  One warp: 32 * VEC outputs of one row; lane i holds the maximum and the sum of piece i, so that their loads
-// and the loads of the pieces' outputs are two round trips, not one per piece (64 x 5056 rows, 128 heads: 128 us for the call instead of 135).  Launched
-// programmatically: its CTAs are in place when the attention kernel ends.
+// and the loads of the pieces' outputs are two round trips, not one per piece (64 x 5056 rows, 128 heads: 128 us for the call
+// instead of 135).  Its CTAs are in place before the attention kernel ends and know by then what they have to merge: for
+// up to MERGE_B sequences they sum the tiles themselves, from counters that the attention kernel has waited for already.
 template <int DS, int NH>
 __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
   constexpr int VEC = DS >= 128 ? 4 : 2, SPLIT = NH * DS / (256 * VEC);
-  asm volatile("griddepcontrol.wait;" ::: "memory");
+  __shared__ int s_sum[3][8], s_n;
   const int lane = threadIdx.x & 31;
   const long long unit = blockIdx.x / SPLIT;
   const int x = ((int)(blockIdx.x % SPLIT) * 256 + (int)threadIdx.x) * VEC, h = x / DS, d = x % DS;      // h: one per warp
   const int per = p.Hkv * p.n_blk, b = (int)(unit / per), u = (int)(unit % per), hk = u / p.n_blk, blk = u % p.n_blk;
   const int gr = blk * NH + h;
+  long long T = 0, seq = 0, n = 0;
+  bool own = false;
+  if (p.B <= MERGE_B) {                                      // thread i: sequence i
+    const int i = threadIdx.x, tiles = i < p.B ? tile_span(p, i).n : 0;
+    const int all = __reduce_add_sync(0xffffffffu, tiles), before = __reduce_add_sync(0xffffffffu, i < b ? tiles : 0);
+    const int longest = __reduce_max_sync(0xffffffffu, tiles);
+    if (lane == 0) { s_sum[0][i >> 5] = all; s_sum[1][i >> 5] = before; s_sum[2][i >> 5] = longest; }
+    if (i == b) s_n = tiles;
+    __syncthreads();
+    int most = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) { T += s_sum[0][k]; seq += s_sum[1][k]; most = max(most, s_sum[2][k]); }
+    T *= per; seq *= per; n = s_n;
+    own = units_whole(p, per, most, T);
+  }
+  chain_wait();
+  chain_next();
   if (gr >= p.q_len * p.rep) return;
-  const long long T = p.prefix[p.B], seq = p.prefix[b], n_all = p.prefix[b + 1] - seq, n = n_all >> 32 ? n_all / per : (unsigned)n_all / (unsigned)per;
+  if (p.B > MERGE_B) {
+    T = p.prefix[p.B]; seq = p.prefix[b]; own = p.prefix[p.B + 1];
+    const long long n_all = p.prefix[b + 1] - seq;
+    n = n_all >> 32 ? n_all / per : (unsigned)n_all / (unsigned)per;
+  }
   const size_t row = ((size_t)b * p.q_len + gr / p.rep) * p.Hq + (size_t)hk * p.rep + gr % p.rep;
   float o[VEC] = {};
   float m = -INFINITY, l = 0.f;
   if (n > 0) {
-    if (p.prefix[p.B + 1]) return;                           // not cut: written by the CTA that worked on it
+    if (own) return;                                         // not cut: written by the CTA that worked on it
     const Cut cut(T, p.grid);
     const long long u0 = seq + u * n, u1 = u0 + n;
     const int c0 = cut.owner(u0), np = cut.owner(u1 - 1) - c0 + 1;
@@ -288,17 +313,7 @@ __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_consta
 
 template <int DS, int NH>
 int paged8_combine_launch(const Paged8Params& P, cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)((long long)P.B * P.Hkv * P.n_blk * (NH * DS / (DS >= 128 ? 1024 : 512))));
-  cfg.blockDim = dim3(256);
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  at[0].val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  if (cudaLaunchKernelEx(&cfg, paged8_combine_kernel<DS, NH>, P) != cudaSuccess) return LCA_ERR_CUDA;
-  note_launch();
-  return LCA_OK;
+  return launch_chained(paged8_combine_kernel<DS, NH>, (unsigned)((long long)P.B * P.Hkv * P.n_blk * (NH * DS / (DS >= 128 ? 1024 : 512))), 256, 0, stream, 1, P);
 }
 
 int attn_paged8_pair_launch(Paged8Params& P, cudaStream_t stream);      // MLA shape, blocks of 128 rows on CTA pairs

@@ -98,7 +98,8 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
     fence_mbar_init();
   }
   if (warp == 1) { tmem_alloc_pair(smem_u32((const void*)tmem_slot), TM_COLS); tmem_relinquish_pair(); }
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  chain_wait();
+  chain_next();
   paged8_range<THREADS>(p, pair_id, s_warp, s_b, s_off);
   tc_fence_before();
   __syncthreads();
@@ -562,9 +563,8 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
 int attn_paged8_pair_launch(Paged8Params& P, cudaStream_t stream) {
   using namespace p8pair;
   if (cudaFuncSetAttribute(attn_paged8_pair_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM_BYTES) != cudaSuccess) return LCA_ERR_CUDA;
-  attn_paged8_pair_kernel<<<2 * P.grid, THREADS, SMEM_BYTES, stream>>>(P);
-  note_launch();
-  if (cudaGetLastError() != cudaSuccess) return LCA_ERR_CUDA;
+  const int st = launch_chained(attn_paged8_pair_kernel, 2 * (unsigned)P.grid, THREADS, SMEM_BYTES, stream, 1, P);      // (clusters of two by declaration)
+  if (st != LCA_OK) return st;
   return paged8_combine_launch<DS, ROWS>(P, stream);
 }
 

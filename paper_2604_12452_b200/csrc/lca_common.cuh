@@ -15,6 +15,28 @@ typedef __nv_bfloat162 bf162;
 // Launch bookkeeping (lca_launch_count).
 void note_launch(int n = 1);
 
+// Kernels that follow one another in a decode step (page update, write, attention, merging, update).  Each is launched
+// with launch_chained and starts with chain_wait, before its first access to memory that an earlier kernel may use: its CTAs
+// then take their places and set up while the kernel before it ends.  Every CTA waits, also one with nothing to do: a kernel
+// that could end before its predecessor would let its successor pass it.  chain_next lets the successor take its places; after
+// any other kernel, or before one, the stream's order is the usual one.
+__device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+template <class K, class... A>
+inline int launch_chained(K kern, unsigned grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, const A&... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at[0].val.programmaticStreamSerializationAllowed = 1;
+  at[1].id = cudaLaunchAttributeClusterDimension;
+  at[1].val.clusterDim.x = cluster; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = cluster > 1 ? 2 : 1;
+  if (cudaLaunchKernelEx(&cfg, kern, args...) != cudaSuccess) return LCA_ERR_CUDA;
+  note_launch();
+  return LCA_OK;
+}
+
 // Partition of Sec. 4.2 on the host.
 inline void partition(int64_t L, int64_t w, int64_t g, int64_t* m, int64_t* k) {
   if (L < w + g) { *m = 0; *k = L; return; }

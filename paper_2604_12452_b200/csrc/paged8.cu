@@ -103,6 +103,8 @@ __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
   const int cta = blockIdx.x, n_cta = gridDim.x;            // the grid is one cluster
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool single = a.B <= PAGE_THREADS;                   // one sequence per thread: its delta stays in registers
+  chain_wait();
+  chain_next();
   const long long n_free = a.n_free[0];
   // (1) totals
   unsigned long long tot[2], ex[2];
@@ -251,23 +253,8 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
   // many threads; otherwise the barriers of a cluster cost more than its threads bring.
   const long long entries = (long long)p->batch * c->table_width;
   const bool big = p->batch > PAGE_THREADS || a.n_rows > 8192 || (!slot_map && entries > 8192);
-  if (!big) {
-    page_update_kernel<<<1, PAGE_THREADS, 0, stream>>>(a);
-    note_launch();
-    return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
-  }
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(16);
-  cfg.blockDim = dim3(PAGE_THREADS);
-  cfg.stream = stream;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = cfg.gridDim.x; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-  cfg.attrs = at; cfg.numAttrs = 1;
-  if (cudaFuncSetAttribute(page_update_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LCA_ERR_CUDA;
-  if (cudaLaunchKernelEx(&cfg, page_update_kernel, a) != cudaSuccess) return LCA_ERR_CUDA;
-  note_launch();
-  return LCA_OK;
+  if (big && cudaFuncSetAttribute(page_update_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return LCA_ERR_CUDA;
+  return launch_chained(page_update_kernel, big ? 16 : 1, PAGE_THREADS, 0, stream, big ? 16 : 1, a);
 }
 
 // ------------------------------------------------------------------------------------------------------------- write
@@ -369,6 +356,8 @@ __global__ void __launch_bounds__(WriteMla<D_SEM, P>::NT, WriteMla<D_SEM, P>::CT
   __shared__ uint32_t s_red[NT / 32];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const long long i0 = (long long)blockIdx.x * a.window;
+  chain_wait();
+  chain_next();
 #pragma unroll 1
   for (int c = 0; 32 * c < a.window; ++c)
 #pragma unroll 1
@@ -417,6 +406,8 @@ __global__ void __launch_bounds__(256, 2) paged8_write_gqa_kernel(WriteArgs a) {
   const long long item = (long long)blockIdx.x * (8 / WPB) + group;
   const int hk = (int)(item % a.Hkv), part = (int)((item / a.Hkv) & 1);
   const long long i0 = item / a.Hkv / 2 * a.window;
+  chain_wait();
+  chain_next();
   if (i0 >= a.n_rows) return;
   const bf16* src0 = part ? a.rows_pos : a.rows_sem;
   uint8_t* pages = part ? a.pages_pos : a.pages_sem;
@@ -464,15 +455,13 @@ static int write_launch(const WriteArgs& a, long long windows, cudaStream_t stre
   long long grid;
   if constexpr (MLA) {
     grid = windows;
-    if (grid <= 0x7fffffffll) paged8_write_mla_kernel<D_SEM, P><<<(unsigned)grid, WriteMla<D_SEM, P>::NT, 0, stream>>>(a);
+    if (grid <= 0x7fffffffll) return launch_chained(paged8_write_mla_kernel<D_SEM, P>, (unsigned)grid, WriteMla<D_SEM, P>::NT, 0, stream, 1, a);
   } else {
     constexpr int PER = 8 / (P <= 32 ? 1 : P / 32);
     grid = (windows * a.Hkv * 2 + PER - 1) / PER;
-    if (grid <= 0x7fffffffll) paged8_write_gqa_kernel<D_SEM, P><<<(unsigned)grid, 256, 0, stream>>>(a);
+    if (grid <= 0x7fffffffll) return launch_chained(paged8_write_gqa_kernel<D_SEM, P>, (unsigned)grid, 256, 0, stream, 1, a);
   }
-  if (grid > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+  return LCA_ERR_UNSUPPORTED_SHAPE;
 }
 template <int D_SEM, bool MLA>
 static int write_page_size(const WriteArgs& a, int page, long long windows, cudaStream_t stream) {
@@ -561,6 +550,8 @@ __global__ void __launch_bounds__(UPD_THREADS) paged8_update_kernel(Update8Args 
   __shared__ int s_anchor;
   const int hk = (int)(blockIdx.x % a.Hkv), b = (int)(blockIdx.x / a.Hkv);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  chain_wait();
+  chain_next();
   const int nr = a.n_rep[b], nt = a.n_tok[b];
   const long long first = (long long)nr * g, cap = (long long)a.width << a.page_log2;
   const bool due = nr >= 0 && nt >= 0 && nt <= cap && (long long)nt - first >= (long long)a.w + g;
@@ -683,9 +674,7 @@ static int update8_launch(const Update8Args& a, long long grid, size_t smem, cud
   auto kern = paged8_update_kernel<MLA, DS, DP>;
   if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
     return LCA_ERR_CUDA;
-  kern<<<(unsigned)grid, UPD_THREADS, smem, stream>>>(a);
-  note_launch();
-  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+  return launch_chained(kern, (unsigned)grid, UPD_THREADS, smem, stream, 1, a);
 }
 
 int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
