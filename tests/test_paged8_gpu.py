@@ -639,6 +639,64 @@ def test_two_calls_at_once(B):
     assert all(torch.equal(o, w[0]) for o, w in zip(outs, want))
 
 
+@pytest.mark.parametrize("shape,heads,kv,nb", [("mla512", 16, 1, 3), ("mla512", 128, 1, 40), ("gqa128", 8, 2, 300)])
+def test_calls_in_a_row_equal_calls_one_by_one(B, shape, heads, kv, nb):
+    """A decode loop of these calls and nothing between them, every one reading what the one before it wrote: as it comes, with
+    a synchronisation after each call, and as a replayed graph, bit for bit."""
+    variant, _, d_sem, d_pos = SHAPES[shape]
+    g, w, page, steps = 16, 16, 16, 10
+    width = 12
+    p = B.make_params(variant, nb, 1, heads, kv, d_sem, d_pos, g, w, 0.07)
+    gen = torch.Generator().manual_seed(11)
+    rnd = lambda *x: torch.randn(x, generator=gen).bfloat16().to(DEV)          # noqa: E731
+    start = torch.randint(0, 120, (nb,), generator=gen)
+    n_tok = [(start + i).int().to(DEV) for i in range(steps + 1)]
+    prompt = [rnd(int(start.sum()), kv, d) for d in (d_sem, d_pos)]
+    new_rows = [[rnd(nb, kv, d) for d in (d_sem, d_pos)] for _ in range(steps)]
+    q = [(rnd(nb, 1, heads, d_sem) if variant == "mla" else None, rnd(nb, 1, heads, d_pos)) for _ in range(steps)]
+    qbar = torch.randn((nb, kv, d_pos + (d_sem if variant == "mla" else 0)), generator=gen).to(DEV)
+
+    def state():
+        cache = B.new_paged8_cache(p, nb * width, page, width, DEV)
+        z = lambda n=nb, v=0, t=torch.int32: torch.full((n,), v, dtype=t, device=DEV)                       # noqa: E731
+        n_rep = [z() for _ in range(steps + 1)]
+        return dict(cache=cache, free=torch.arange(nb * width, dtype=torch.int32, device=DEV), n_free=z(1, nb * width), held=(z(), z()), n_rep=n_rep,
+                    slots=z(max(1, int(start.sum()))), off=z(nb + 1), one=[z() for _ in range(2 * steps)], status=[z(1, -9) for _ in range(2 * steps + 1)],
+                    out=[torch.zeros((nb, 1, heads, d_sem), dtype=torch.bfloat16, device=DEV) for _ in range(steps)],
+                    rep=[[torch.zeros((nb, kv, d), dtype=torch.bfloat16, device=DEV) for d in (d_sem, d_pos)] for _ in range(steps)],
+                    anchor=[torch.zeros((nb, kv), dtype=torch.int32, device=DEV) for _ in range(steps)],
+                    ws=B.workspace_paged8(p, cache, 1, DEV), ws2=B.workspace(p, B.LCA_WS_UPDATE, DEV))
+
+    def run(s, after):
+        c, pages = s["cache"], (*s["held"], s["free"], s["n_free"])
+        B.page_update(p, c, s["n_rep"][0], n_tok[0], *pages, s["slots"], s["off"], s["status"][-1]); after()
+        B.paged8_write(p, c, *prompt, s["slots"]); after()
+        for i in range(steps):
+            B.page_update(p, c, s["n_rep"][i], n_tok[i + 1], *pages, s["one"][2 * i], None, s["status"][2 * i], rows_per_seq=1); after()
+            B.paged8_write(p, c, *new_rows[i], s["one"][2 * i]); after()
+            B.decode_attention_paged8(p, c, *q[i], s["n_rep"][i], n_tok[i + 1], out=s["out"][i], ws=s["ws"]); after()
+            B.decode_update_paged8(p, c, None, None, s["n_rep"][i], n_tok[i + 1], s["n_rep"][i + 1], *s["rep"][i], qbar=qbar,
+                                   anchor=s["anchor"][i], ws=s["ws2"]); after()
+            B.page_update(p, c, s["n_rep"][i + 1], n_tok[i + 1], *pages, s["one"][2 * i + 1], None, s["status"][2 * i + 1], rows_per_seq=1); after()
+            B.paged8_write(p, c, *s["rep"][i], s["one"][2 * i + 1]); after()
+
+    states = [state() for _ in range(3)]
+    run(states[0], torch.cuda.synchronize)
+    run(states[1], lambda: None)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(states[2], lambda: None)
+    graph.replay()
+    torch.cuda.synchronize()
+
+    def flat(s):
+        return [*s["cache"].tensors, s["free"], s["n_free"], *s["held"], *s["n_rep"], s["slots"], *s["one"], *s["status"], *s["out"],
+                *(x for r in s["rep"] for x in r), *s["anchor"]]
+    assert all(int(x) == 0 for x in states[0]["status"]) and int((states[0]["n_rep"][-1] > 0).sum()) > 0
+    for other in states[1:]:
+        assert all(a is b or torch.equal(a, b) for a, b in zip(flat(states[0]), flat(other)))
+
+
 def test_helpers_refuse_tensors_that_do_not_fit(B):
     p, cache, q_sem, q_pos, n_rep, n_tok, qbar = decode_case(B, 16, 4)
     before = B.lca_launch_count()
