@@ -613,10 +613,13 @@ def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, hel
     tensor: read it where the caller has to know (0: done)."""
     dev, at, _ = _paged8_device(params, cache, stream)
     B = params.batch
+    done, slots = _arg(status, _I32, 1, dev), _arg(slot_map, _I32, 0, dev)
+    if slots == 0:                             # an empty tensor has no address, and no room for a row either: not "not wanted"
+        slots = done
     _check(_lib.lca_page_update(params, cache, _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev),
                                 _arg(held_rep, _I32, B, dev), _arg(held_tok, _I32, B, dev), _arg(free_pages, _I32, cache.n_pages, dev),
-                                _arg(n_free, _I32, 1, dev), _arg(slot_map, _I32, 0, dev), 0 if slot_map is None else slot_map.numel(),
-                                rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), _arg(status, _I32, 1, dev), at), "lca_page_update")
+                                _arg(n_free, _I32, 1, dev), slots, 0 if slot_map is None else slot_map.numel(),
+                                rows_per_seq, _arg(row_offsets, _I32, B + 1, dev), done, at), "lca_page_update")
     return slot_map
 
 

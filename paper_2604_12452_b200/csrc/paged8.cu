@@ -100,6 +100,9 @@ __device__ __forceinline__ void cluster_barrier() {
 __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
   __shared__ unsigned long long sums[PAGE_WARPS][2];
   __shared__ unsigned s_rel[PAGE_THREADS];                   // first rank of each sequence of a chunk
+  // up to PAGE_THREADS sequences: first packed row of each, then its new rows: first and number of representatives, first
+  // token, number in all
+  __shared__ int s_row[PAGE_THREADS + 1], s_rep0[PAGE_THREADS], s_reps[PAGE_THREADS], s_tok0[PAGE_THREADS], s_rows[PAGE_THREADS];
   const int cta = blockIdx.x, n_cta = gridDim.x;            // the grid is one cluster
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool single = a.B <= PAGE_THREADS;                   // one sequence per thread: its delta stays in registers
@@ -121,6 +124,11 @@ __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
       v[1] += (unsigned long long)nr;
     }
     scan2(v, ex, tot, sums);
+    if (single && tid < a.B) {
+      s_row[tid] = (int)min(ex[1], 0x7fffffffull);
+      s_rep0[tid] = mine.r0; s_reps[tid] = max(mine.r1 - mine.r0, 0); s_tok0[tid] = mine.tok_first; s_rows[tid] = mine.n_rows();
+      if (tid == 0) s_row[a.B] = (int)min(tot[1], 0x7fffffffull);
+    }
   }
   const int any_bad = __syncthreads_or(bad & 1) ? 1 : __syncthreads_or(bad & 2) ? 2 : 0;
   const long long n_rel = (long long)(tot[0] & 0xffffffffull), n_need = (long long)(tot[0] >> 32), have = n_free + n_rel;
@@ -198,8 +206,45 @@ __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
       }
     if (n_cta > 1) cluster_barrier(); else __syncthreads();
   }
-  // (4) slots.  Packed: a warp takes 256 rows at a time, finds the sequence of the first and walks on from there.
-  if (a.slot_map) {
+  // (4) slots.  A warp takes 256 rows at a time; packed, it finds the sequence of the first and walks on from there.
+  if (a.slot_map && single) {
+    // where row k of sequence b lies in the tables, and its place in the page
+    auto entry_of = [&](int b, int k, int& place) {
+      const int reps = s_reps[b], x = k < reps ? s_rep0[b] + k : s_tok0[b] + (k - reps);
+      place = x & ((1 << a.page_log2) - 1);
+      return a.table + (size_t)b * a.width + (x >> a.page_log2);
+    };
+    const int R = s_row[a.B];
+#pragma unroll 1
+    for (long long i0 = ((long long)cta * PAGE_WARPS + warp) * 256; i0 < a.n_rows; i0 += (long long)n_cta * PAGE_WARPS * 256) {
+      int b = 0;
+      if (a.per_seq == 0 && i0 < R) {                        // the last sequence that starts at or before row i0
+        int hi = a.B;
+        while (b + 1 < hi) { const int mid = (b + hi) >> 1; if (s_row[mid] <= i0) b = mid; else hi = mid; }
+      }
+      int page[8], place[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {                          // eight look-ups in flight
+        const long long i = i0 + 32 * u + lane;
+        page[u] = -1; place[u] = 0;
+        if (a.per_seq > 0) {
+          if (i < a.n_rows) {
+            b = (int)i / a.per_seq;
+            const int k = (int)i - b * a.per_seq;
+            if (k < s_rows[b]) page[u] = *entry_of(b, k, place[u]);
+          }
+        } else if (i < R) {
+          while (i >= s_row[b + 1]) ++b;
+          page[u] = *entry_of(b, (int)i - s_row[b], place[u]);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const long long i = i0 + 32 * u + lane;
+        if (i < a.n_rows) a.slot_map[i] = page[u] >= 0 && page[u] < a.n_pages ? (page[u] << a.page_log2) | place[u] : -1;
+      }
+    }
+  } else if (a.slot_map) {
     auto slot_of = [&](int b, long long k, long long rows) {
       if (k >= rows) return -1;
       const int r0 = a.n_rep ? a.held_rep[b] : 0, r1 = a.n_rep ? a.n_rep[b] : 0, reps = max(r1 - r0, 0);

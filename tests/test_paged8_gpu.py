@@ -120,6 +120,8 @@ def test_page_update_refuses_as_a_whole(B):
     assert T.update([(-1, 40), (0, 3), (0, 1)], 64) == -1
     assert T.update([(0, -5), (0, 3), (0, 1)], 64) == -1
     assert T.update([(0, 40), (0, 3), (0, 16)], 3) == -2                                       # 16 rows, 3 places
+    assert T.update([(0, 40), (0, 3), (0, 16)], 0) == -2                                       # an empty slot map is one
+    assert T.update([(0, 40), (0, 3), (0, 0)], 0) == 0                                         # ... and enough where there is nothing new
     assert T.update([(2, 40), (0, 3), (0, 16)], 64) == 0                                       # two pages come back, two are taken
     assert T.update([(1, 40), (0, 3), (0, 16)], 64) == -1                                      # a condensation is not undone
     T.held_tok[1] = 1 << 20                                                                    # a broken held state is refused too
