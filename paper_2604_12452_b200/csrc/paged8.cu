@@ -12,8 +12,8 @@ namespace lca {
 // possible; (2) pages that no present row needs are pushed on the free stack; (3) pages are popped into the tables; (4) the
 // slot of every new row is looked up.  A sequence's share of each list starts at an exclusive prefix sum, so the result does
 // not depend on how the work is spread.  Bound by latency (dependent passes over the counters and cluster barriers), not by
-// its bytes: one CTA for a decode step (64 sequences: 5.7 us), sixteen for prompts (64 prompts of 5056 rows grown and given
-// back: 25 us for both calls; one CTA took 100).
+// its bytes: one CTA for a decode step (64 sequences: 4 us), sixteen for prompts (64 prompts of 5056 rows grown and given
+// back: 19 us for both calls; one CTA took 100).
 struct PageArgs {
   const int32_t* n_rep; const int32_t* n_tok;
   int32_t* held_rep; int32_t* held_tok;
@@ -206,42 +206,70 @@ __global__ void __launch_bounds__(PAGE_THREADS) page_update_kernel(PageArgs a) {
       }
     if (n_cta > 1) cluster_barrier(); else __syncthreads();
   }
-  // (4) slots.  A warp takes 256 rows at a time; packed, it finds the sequence of the first and walks on from there.
+  // (4) slots.  Packed: a warp takes 256 rows at a time, finds the sequence of the first and walks on from there.
   if (a.slot_map && single) {
-    // where row k of sequence b lies in the tables, and its place in the page
-    auto entry_of = [&](int b, int k, int& place) {
-      const int reps = s_reps[b], x = k < reps ? s_rep0[b] + k : s_tok0[b] + (k - reps);
-      place = x & ((1 << a.page_log2) - 1);
-      return a.table + (size_t)b * a.width + (x >> a.page_log2);
-    };
+    const int up = (1 << a.page_log2) - 1;
+    auto slot_at = [&](int pg, int x) { return pg >= 0 && pg < a.n_pages ? (pg << a.page_log2) | (x & up) : -1; };
+    auto row_of = [&](int b, int k) { const int reps = s_reps[b]; return k < reps ? s_rep0[b] + k : s_tok0[b] + (k - reps); };
+    auto page_of = [&](int b, int x) { return a.table[(size_t)b * a.width + (x >> a.page_log2)]; };
     const int R = s_row[a.B];
+    auto seq_at = [&](long long i) {                         // packed, i < R: the last sequence that starts at or before row i
+      int lo = 0, hi = a.B;
+      while (lo + 1 < hi) { const int mid = (lo + hi) >> 1; if (s_row[mid] <= i) lo = mid; else hi = mid; }
+      return lo;
+    };
+    if (a.per_seq > 0 || a.n_rows <= gthreads) {             // a row per thread
+      for (long long i = gtid; i < a.n_rows; i += gthreads) {
+        int b = 0, k = 0x7fffffff, slot = -1;
+        if (a.per_seq > 0) { b = (int)i / a.per_seq; k = (int)i - b * a.per_seq; }
+        else if (i < R) { b = seq_at(i); k = (int)i - s_row[b]; }
+        if (k < s_rows[b]) { const int x = row_of(b, k); slot = slot_at(page_of(b, x), x); }
+        a.slot_map[i] = slot;
+      }
+    } else {
+      // Many: a warp takes 256 rows at a time, a thread twice four neighbours, which lie on two pages at most unless a sequence
+      // or its representatives end among them (a row at a time, the index arithmetic of sixteen SMs takes 10 us for 324000 rows).
+      const bool wide = (reinterpret_cast<uintptr_t>(a.slot_map) & 15u) == 0;
 #pragma unroll 1
-    for (long long i0 = ((long long)cta * PAGE_WARPS + warp) * 256; i0 < a.n_rows; i0 += (long long)n_cta * PAGE_WARPS * 256) {
-      int b = 0;
-      if (a.per_seq == 0 && i0 < R) {                        // the last sequence that starts at or before row i0
-        int hi = a.B;
-        while (b + 1 < hi) { const int mid = (b + hi) >> 1; if (s_row[mid] <= i0) b = mid; else hi = mid; }
-      }
-      int page[8], place[8];
+      for (long long i0 = ((long long)cta * PAGE_WARPS + warp) * 256; i0 < a.n_rows; i0 += (long long)n_cta * PAGE_WARPS * 256) {
+        int b = i0 < R ? seq_at(i0) : 0;
+        int x[2], p0[2], p1[2], seq[2];
+        bool plain[2];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {                          // eight look-ups in flight
-        const long long i = i0 + 32 * u + lane;
-        page[u] = -1; place[u] = 0;
-        if (a.per_seq > 0) {
-          if (i < a.n_rows) {
-            b = (int)i / a.per_seq;
-            const int k = (int)i - b * a.per_seq;
-            if (k < s_rows[b]) page[u] = *entry_of(b, k, place[u]);
+        for (int u = 0; u < 2; ++u) {
+          const long long i = i0 + 128 * u + 4 * lane;
+          plain[u] = false; x[u] = 0; p0[u] = p1[u] = -1;
+          if (i < R) {
+            while (i >= s_row[b + 1]) ++b;
+            const int k = (int)i - s_row[b], reps = s_reps[b];
+            plain[u] = k + 3 < s_rows[b] && (k >= reps || k + 3 < reps);
+            if (plain[u]) { x[u] = row_of(b, k); p0[u] = page_of(b, x[u]); p1[u] = page_of(b, x[u] + 3); }
           }
-        } else if (i < R) {
-          while (i >= s_row[b + 1]) ++b;
-          page[u] = *entry_of(b, (int)i - s_row[b], place[u]);
+          seq[u] = b;
         }
-      }
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
-        const long long i = i0 + 32 * u + lane;
-        if (i < a.n_rows) a.slot_map[i] = page[u] >= 0 && page[u] < a.n_pages ? (page[u] << a.page_log2) | place[u] : -1;
+        for (int u = 0; u < 2; ++u) {
+          const long long i = i0 + 128 * u + 4 * lane;
+          int slot[4];
+#pragma unroll
+          for (int r = 0; r < 4; ++r) slot[r] = slot_at((x[u] & up) + r <= up ? p0[u] : p1[u], x[u] + r);
+          if (!plain[u] && i < R) {
+            int c = seq[u];
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              slot[r] = -1;
+              if (i + r < R) {
+                while (i + r >= s_row[c + 1]) ++c;
+                const int y = row_of(c, (int)(i + r) - s_row[c]);
+                slot[r] = slot_at(page_of(c, y), y);
+              }
+            }
+          }
+          if (wide && i + 3 < a.n_rows) *reinterpret_cast<int4*>(a.slot_map + i) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+          else
+#pragma unroll
+            for (int r = 0; r < 4; ++r) if (i + r < a.n_rows) a.slot_map[i + r] = slot[r];
+        }
       }
     }
   } else if (a.slot_map) {
