@@ -366,8 +366,10 @@ int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* r
  * out = 0 and lse = -inf.  What absent rows and unused pages hold does not matter; a NaN in a present row reaches every
  * query of that sequence and KV head.
  * Products on the tensor cores with queries and softmax weights as sums of two 8-bit terms: a query element is exact to
- * 2^-17 of the largest of its row, a weight to 2^-8 of itself or 2^-15 of the largest weight; fp32 softmax and sums,
- * one rounding to bf16.  Results do not depend on anything but the arguments (no atomics).
+ * 2^-17 of the largest of its row, a weight to 2^-8 of itself or to a step of 2^-17 of the largest weight, whichever is more; weights
+ * near that step are rounded with offsets spread evenly over the rows, so that many of them keep their sum, whatever
+ * the period of the values, to a few dozen steps.  fp32 softmax and sums, one rounding to bf16.  Results do not depend on anything
+ * but the arguments (no atomics).
  * ws / ws_bytes: lca_paged8_workspace_bytes. */
 size_t lca_paged8_workspace_bytes(const lca_params* p, const lca_paged8* cache, int32_t q_len);
 int lca_decode_attention_paged8(const lca_params* p, const lca_paged8* cache, const void* q_sem, const void* q_pos,

@@ -5,10 +5,13 @@
 // with e4m3 codes k, v and one scale for each page and KV head.  Everything is multiplied as 8-bit numbers:
 //   * q f = q_hi + q_lo, two e4m3 terms, f the power of two that brings the row's largest element into [128, 256).
 //     Four significant bits each: exact for every element above 2^-9 of the largest, otherwise off by 2^-17 of the largest.
-//   * t_i = 2^(y_i + log2 s_v(i) - M + 5) = t_hi + t_lo, two e4m3 terms again: relative error 2^-9 (a bf16 weight has 2^-9), and
-//     never more than 2^-10, i.e. 2^-15 of the largest weight.  That floor would round a long flat tail all the same way, so
-//     every key adds its own offset, one of 32 spread over the last place of t_lo, before the rounding: over a tile the tail
-//     keeps its weight to 1/64 of that place.
+//   * t_i = 2^(y_i + log2 s_v(i) - M + 5) = t_hi + 2^-4 t_lo, two e4m3 terms again: relative error 2^-9 (a bf16 weight has 2^-8).
+//     t_hi is the nearest e4m3 value down to the format's smallest step (2^-9), so that what it leaves, times 2^4, is below e4m3's
+//     normal range wherever t is: there weights are held in steps of 2^-13, i.e. 2^-18 of the largest weight.  Such a step would round
+//     a long flat tail all the same way, so every key adds its own offset within the step before the rounding, its row times
+//     the golden ratio modulo 1: keys of every residue modulo anything small get evenly spread offsets, and a tail keeps its
+//     weight under values of whatever period, to a few dozen steps in all.  (Offsets that repeat every 32 rows hand the tail to a
+//     fixed subset of the keys: 20000 rows with +1 and -1 in turn behind one large logit, 0.38 instead of 0.)
 //   M is the running maximum of y + log2 s_v over a split; it is raised only when a weight would exceed 2^8.75.  The row
 //   sum adds the weights without s_v in fp32, unrounded.
 #include <cstring>
@@ -162,6 +165,7 @@ __device__ __forceinline__ bool group_any(int grp, bool v) {
 }
 
 static constexpr float T_MAX = 8.75f;                        // log2 of the largest weight: e4m3 ends at 448
+static constexpr float LO_GAIN = 16.f;                       // of the second term, which has columns of O of its own
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(const __grid_constant__ Paged8Params p) {
@@ -319,7 +323,6 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
     // ------------------------------------------------------------------------------------- softmax, epilogue
     const int grp = warp >> 2, quad = warp & 3, t = tid & 127, hb = 16 * grp;      // this thread: key t of a tile, rows hb .. hb + 15
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
-    const float dither = ((float)(__brev((unsigned)lane) >> 27) + 0.5f) * (1.f / 32.f) * 0.001953125f - 0.0009765625f;   // (-1/2, 1/2) of 2^-9
     uint32_t g = 0, seg = 0, seg_chunks = 0;
     bool ok = true;
     float l[16];
@@ -403,10 +406,11 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         if (pg1 >= 0) { ks1 = p.scale_k[(size_t)pg1 * p.Hkv + w.hk]; vs1 = p.scale_v[(size_t)pg1 * p.Hkv + w.hk]; }
         const int pg2 = page_of(w, j + 2);
         vs = fmaxf(vs, exp2_int(PAGED8_MIN_EXP));
-        // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 vs + 8): both are multiples of e = 2^(y - M + half), half way
+        // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 vs + 5): both are multiples of e = 2^(y - M + half), half way
         // between them, so that neither is lost below 2^-126 where the scales of a sequence span more than fp32 does.
-        const float half = 0.5f * (lg2(vs) + PAGED8_T_BITS), f_t = ex2(half), f_l = ex2(PAGED8_T_BITS - half);
+        const float half = 0.5f * (lg2(vs) + paged8_t_bits(NH)), f_t = ex2(half), f_l = ex2(paged8_t_bits(NH) - half);
         const float kf = ks * p.scale_log2, cb = half + (x < sp.n_rep ? p.bias_log2 : 0.f);
+        const float offset = weight_offset(x);
         const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
 
         ok = mbar_wait(SFULL + 8 * (g & 1), (g >> 1) & 1, abort_flag);
@@ -449,8 +453,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
             const int h = hb + t;
             const float m = fmaxf(fmaxf(s_wmax[h], s_wmax[NH + h]), fmaxf(s_wmax[2 * NH + h], s_wmax[3 * NH + h]));
             float d = 0.f, f = 1.f;
-            if (unset ? m > -INFINITY : m > PAGED8_T_BITS) {
-              d = m - PAGED8_T_BITS;
+            if (unset ? m > -INFINITY : m > paged8_t_bits(NH)) {
+              d = m - paged8_t_bits(NH);
               f = unset ? 1.f : ex2(-d);                     // nothing has been added under an unset maximum
               s_m[h] += d;
               unset = false;
@@ -483,17 +487,17 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
           uint32_t wh[4], wl[4];
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float hi[4], lo[4];
+            float tt[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-              const float e = ex2(z[4 * i + k]), tt = e * f_t;
+              const float e = ex2(z[4 * i + k]);
+              tt[k] = e * f_t;
               l[4 * i + k] = fmaf(e, f_l, l[4 * i + k]);
-              const float h = __uint_as_float((__float_as_uint(tt) + 0x00080000u) & 0xfff00000u);      // four significant bits
-              hi[k] = tt < 0.015625f ? 0.f : h;              // below e4m3's normal range the second term takes it all
-              lo[k] = (tt - hi[k]) + dither;
             }
-            wh[i] = e4m3x4_from_float(hi[0], hi[1], hi[2], hi[3]);
-            wl[i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
+            wh[i] = e4m3x4_from_float(tt[0], tt[1], tt[2], tt[3]);
+            const float4 h = e4m3x4_to_float4(wh[i]);        // what the first term leaves is exact: at most 2^4, times LO_GAIN 2^8
+            wl[i] = e4m3x4_from_float(fmaf(tt[0] - h.x, LO_GAIN, offset), fmaf(tt[1] - h.y, LO_GAIN, offset),
+                                      fmaf(tt[2] - h.z, LO_GAIN, offset), fmaf(tt[3] - h.w, LO_GAIN, offset));
           }
           unsigned char* ph = base_ptr + PL::OFF_P;
           *reinterpret_cast<uint4*>(ph + swz<2 * NH>(t, grp)) = make_uint4(wh[0], wh[1], wh[2], wh[3]);
@@ -539,7 +543,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
           float* ml = p.part + (size_t)2 * p.grid * NH * DS + part * 2 * NH;
           ml[h] = unset ? -INFINITY : s_m[h]; ml[NH + h] = sum;
         } else if (p.lse && rows[t] >= 0) {
-          p.lse[rows[t]] = sum == 0.f ? -INFINITY : (s_m[h] + log2f(sum) - PAGED8_T_BITS) * 0.6931471805599453f;
+          p.lse[rows[t]] = sum == 0.f ? -INFINITY : (s_m[h] + log2f(sum) - paged8_t_bits(NH)) * 0.6931471805599453f;
         }
         s_f[h] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
       }
@@ -557,7 +561,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
         tmem_ld16(tmem + lane_base + c * 2 * NH + NH + hb, o2);
         tmem_wait_ld();
 #pragma unroll
-        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) + __uint_as_float(o2[k]));
+        for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o2[k]), 1.f / LO_GAIN, __uint_as_float(o[k])));
         const int d = c * 128 + t;
         if (DS >= 128 || t < DS) {
           if (whole) {
@@ -594,7 +598,7 @@ bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, l
 // Query rows that share a tile of keys.  The tile is padded to that number, so it is the smallest one that holds all rows of
 // a KV head (the softmax threads compute an exponential per padded row and key); at most 64, as O takes d / 128 * NH columns
 // of TMEM.  The MLA shape with more than 32 rows goes to CTA pairs in blocks of 128 (64 x 5056 rows, 128 heads: 128 us in
-// blocks of 64 on single CTAs, 90 us on pairs).
+// blocks of 64 on single CTAs, 92 us on pairs).
 static int paged8_rows_per_tile(const lca_params* p, int q_len) {
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
   return rows <= 16 ? 16 : rows <= 32 ? 32 : p->d_sem == 512 ? 128 : 64;

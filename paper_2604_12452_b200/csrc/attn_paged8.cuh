@@ -9,9 +9,14 @@
 namespace lca {
 using namespace tc;
 
-// A raised maximum puts the largest weight at 2^5; it may grow until its leading term is as large as its format allows before
-// the maximum is raised again.  The last place of the second term is 2^-9 at least.
-static constexpr float PAGED8_T_BITS = 5.f;
+// A raised maximum puts the largest weight at 2^5 (pairs, blocks of 128 rows: 2^8); it may grow until its leading term is as large as
+// its format allows before the maximum is raised again.
+__host__ __device__ constexpr float paged8_t_bits(int rows) { return rows == 128 ? 8.f : 5.f; }
+
+// Offset of a key before the second term of its weight is rounded, in [-1/2, 1/2] of the smallest e4m3 step (2^-9): the row times the
+// golden ratio, modulo 1.  At either end a weight of 0 still rounds to 0 (a tie, to even).
+static constexpr uint32_t GOLDEN = 0x9E3779B9u;              // 2^32 / golden ratio
+__device__ __forceinline__ float weight_offset(int row) { return (float)(int)((uint32_t)row * GOLDEN) * 0x1p-41f; }
 
 struct Paged8Params {
   CUtensorMap sem, pos;       // [n_pages * Hkv, page, d] codes; boxes of one page x 128 (or 64) bytes
@@ -308,7 +313,7 @@ __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_consta
   uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
 #pragma unroll
   for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
-  if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
+  if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - paged8_t_bits(NH)) * 0.6931471805599453f;
 }
 
 template <int DS, int NH>

@@ -1,9 +1,14 @@
-// Decode attention over the paged 8-bit cache for the MLA shape and many heads, on CTA pairs.  The arithmetic is that of
+// Decode attention over the paged 8-bit cache for the MLA shape and many heads, on CTA pairs.  The mathematics is that of
 // attn_paged8.cu (two-term e4m3 queries, two-term weights, one scale per page); the layout is the other way round.
+//
+// Both terms of a weight are added up in the same columns here, O takes them all, so the second one cannot be scaled.  The first
+// term is e5m2 instead: three significant bits (relative error of a weight 2^-8), but down to 2^-16.  What it leaves has steps of 2^-9,
+// with the largest weight at 2^8 when its maximum is set (2^11 before it is raised): 2^-17 of it, with offsets spread as there.
+// (Offsets that repeat every 64 rows and a largest weight of 2^5: 20000 rows with a period of 32 behind one large logit were off by 0.057.)
 //
 // With 64 rows or more the transposed tiles of attn_paged8.cu are bound by the 128 bytes per clock of shared memory: every
 // product reads both operands from it, 2688 clocks for 64 rows x 128 keys, and the copies of the tile are written through
-// the same port (4200 clocks a tile measured; 64 x 5056 rows of 128 heads: 128 us, here 90).  Here two CTAs share 128 query rows (cta_group::2, M = 128): each holds 64
+// the same port (4200 clocks a tile measured; 64 x 5056 rows of 128 heads: 128 us, here 92).  Here two CTAs share 128 query rows (cta_group::2, M = 128): each holds 64
 // rows of Q and P, half of the keys for S = Q K^T (N = 128 split by keys) and half of the value columns for O += T V
 // (N = 256, twice, split by columns), so that a product reads half the bytes per SM:
 //   tensor core   S 36 x 32 + O 16 x 64 clocks = 2176 for 128 rows x 128 keys on two SMs
@@ -39,6 +44,7 @@ constexpr int OFF_PAGE = OFF_FACT + BATCHES * 32 * 16, OFF_QS = OFF_PAGE + BATCH
 constexpr int SMEM_BYTES = OFF_QS + 64 * 4;
 constexpr int TM_S = 256, TM_COLS = 512;                     // O in columns 0..255, S in 256..319 and 320..383
 constexpr int THREADS = 256;
+constexpr float T_BITS = paged8_t_bits(ROWS);
 constexpr float T_MAX = 11.f;                                // log2 of the largest weight: e5m2 leaves at most 2^8 of it to e4m3
 static_assert(SMEM_BYTES <= 232448, "shared memory of one SM");
 static_assert(OFF_QS % 16 == 0 && OFF_FACT % 16 == 0, "alignment");
@@ -55,6 +61,18 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
+// Offsets of the keys (weight_offset), read four at a time by whole warps.  Offsets for every row of a sequence would not fit; windows
+// of 128 of them that start anywhere are as evenly spread, so a tile takes one of 1024 windows, in an order in which any number
+// of successive ones is even as well.
+constexpr int WINDOWS = 1024, WINDOW_ORDER = 613;
+struct OffsetTable {
+  float v[4 * WINDOWS + 128];
+  constexpr OffsetTable() : v() {
+    for (int i = 0; i < 4 * WINDOWS + 128; ++i) v[i] = (float)(int32_t)((uint32_t)i * GOLDEN) * 0x1p-41f;
+  }
+};
+__constant__ const OffsetTable g_offsets{};
+
 // bits [0, n) of a word of 64; n may be anything
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
@@ -191,8 +209,8 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
             const float ks = p.scale_k[z], vs = fmaxf(ks, exp2_int(PAGED8_MIN_EXP));
             // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 vs + T): both are multiples of e = 2^(y - M + half), half
             // way between them, so that neither is lost below 2^-126 where the scales span more than fp32 does.
-            const float half = 0.5f * (lg2(vs) + PAGED8_T_BITS);
-            f = make_float4(ks * p.scale_log2, half, ex2(half), ex2(PAGED8_T_BITS - half));
+            const float half = 0.5f * (lg2(vs) + T_BITS);
+            f = make_float4(ks * p.scale_log2, half, ex2(half), ex2(T_BITS - half));
           }
         }
         ok = mbar_wait(GEMPTY(i % BATCHES), ((i / BATCHES) & 1) ^ 1, abort_flag);
@@ -414,13 +432,14 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
         asm volatile("bar.sync 1, 128;" ::: "memory");
         top = fmaxf(top, s_red[(g & 1) * 128 + (ln ^ 64)]);
         const bool raise = unset ? top > -INFINITY : top > T_MAX;
-        const float d = raise ? top - PAGED8_T_BITS : 0.f, factor = raise && !unset ? ex2(-d) : 1.f;
+        const float d = raise ? top - T_BITS : 0.f, factor = raise && !unset ? ex2(-d) : 1.f;
         m += d;
         l *= factor;
         unset = unset && !raise;
         // The weights depend on S and the maximum only: they are packed while O of the previous tile is still running
         uint32_t wh[16], wl[16];
-        const uint64_t d2 = pack_f32x2(-d, -d), neg2 = pack_f32x2(-1.f, -1.f), split2 = pack_f32x2(2097153.f, 2097153.f);
+        const uint64_t d2 = pack_f32x2(-d, -d), neg2 = pack_f32x2(-1.f, -1.f);
+        const float4* offsets = reinterpret_cast<const float4*>(g_offsets.v + 4 * ((uint32_t)(row0 >> 7) * WINDOW_ORDER % WINDOWS) + 64 * half_no);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float4 f = fact[q];
@@ -428,26 +447,26 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
           uint64_t sum2 = 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            float hi[4], lo[4];
+            uint64_t tt[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int key = 16 * q + 4 * i + 2 * k;        // of the half
               float z0, z1;
-              unpack_f32x2(add_f32x2(z[key >> 1], d2), z0, z1);
-              const uint64_t e = pack_f32x2(ex2(z0), ex2(z1)), tt = mul_f32x2(e, ft2);
+              unpack_f32x2(add_f32x2(z[8 * q + 2 * i + k], d2), z0, z1);
+              const uint64_t e = pack_f32x2(ex2(z0), ex2(z1));
+              tt[k] = mul_f32x2(e, ft2);
               sum2 = add_f32x2(sum2, e);
-              // the three leading bits (Veltkamp's splitting with 2^21 + 1), and what they leave plus the key's offset
-              const uint64_t c = mul_f32x2(tt, split2), h = fma_f32x2(fma_f32x2(tt, neg2, c), neg2, c);
-              // offsets (2 k + 1) / 64 - 1/2 of the last place of e4m3's smallest step, k running over 32 neighbouring keys
-              constexpr float step = 0.001953125f;
-              const int b0 = (key * 11) & 31, b1 = ((key + 1) * 11) & 31;
-              const uint64_t dith = pack_f32x2(((float)(2 * b0 + 1) / 64.f - 0.5f) * step, ((float)(2 * b1 + 1) / 64.f - 0.5f) * step);
-              const uint64_t r = add_f32x2(fma_f32x2(h, neg2, tt), dith);
-              unpack_f32x2(h, hi[2 * k], hi[2 * k + 1]);
-              unpack_f32x2(r, lo[2 * k], lo[2 * k + 1]);
             }
-            wh[4 * q + i] = e5m2x4_from_float(hi[0], hi[1], hi[2], hi[3]);
-            wl[4 * q + i] = e4m3x4_from_float(lo[0], lo[1], lo[2], lo[3]);
+            float t[4], h[4], r[4];
+            unpack_f32x2(tt[0], t[0], t[1]);
+            unpack_f32x2(tt[1], t[2], t[3]);
+            const uint32_t w = e5m2x4_from_float(t[0], t[1], t[2], t[3]);
+            e5m2x4_to_float(w, h);
+            const float4 off = offsets[4 * q + i];
+            // what the first term leaves (exactly) plus the key's offset
+            unpack_f32x2(add_f32x2(fma_f32x2(pack_f32x2(h[0], h[1]), neg2, tt[0]), pack_f32x2(off.x, off.y)), r[0], r[1]);
+            unpack_f32x2(add_f32x2(fma_f32x2(pack_f32x2(h[2], h[3]), neg2, tt[1]), pack_f32x2(off.z, off.w)), r[2], r[3]);
+            wh[4 * q + i] = w;
+            wl[4 * q + i] = e4m3x4_from_float(r[0], r[1], r[2], r[3]);
           }
           float a, b;
           unpack_f32x2(sum2, a, b);
@@ -544,7 +563,7 @@ attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
           float* ml = p.part + (size_t)2 * p.grid * ROWS * DS + part * 2 * ROWS;
           ml[rg] = unset ? -INFINITY : m; ml[ROWS + rg] = l;
         } else if (p.lse && row_valid) {
-          p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - PAGED8_T_BITS) * 0.6931471805599453f;
+          p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - T_BITS) * 0.6931471805599453f;
         }
       }
       tc_fence_before();

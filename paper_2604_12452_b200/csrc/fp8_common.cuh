@@ -25,6 +25,12 @@ __device__ __forceinline__ uint32_t e5m2x4_from_float(float a, float b, float c,
       "mov.b32 %0, {lo, hi};\n\t}" : "=r"(r) : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
+// e5m2 is the upper half of f16
+__device__ __forceinline__ void e5m2x4_to_float(uint32_t v, float (&f)[4]) {
+  const uint32_t lo = __byte_perm(v, 0u, 0x1404), hi = __byte_perm(v, 0u, 0x3424);
+  const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&lo)), y = __half22float2(*reinterpret_cast<const __half2*>(&hi));
+  f[0] = x.x; f[1] = x.y; f[2] = y.x; f[3] = y.y;
+}
 __device__ __forceinline__ float4 e4m3x4_to_float4(uint32_t v) {
   uint32_t lo, hi;
   asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}"
