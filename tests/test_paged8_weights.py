@@ -1,8 +1,11 @@
 """Softmax weights as sums of two 8-bit terms: what the rounding does to sums over many keys, on the CPU (no GPU needed)."""
 import numpy as np
 import pytest
+import torch
 
+from tests import paged8_reference as R
 from tests import paged8_weights as W
+from tests.paged8_errors import row_errors
 
 
 @pytest.mark.parametrize("kind", ["single", "pair"])
@@ -48,3 +51,36 @@ def test_a_flat_tail_keeps_its_weight_whatever_its_values(kind, n):
             # where a place of the second term is wider than the offsets, keys differ by that place, 2^-8 (2^-7) of a weight
             limit += W.MISS * 2.0 ** (-8 if kind == "single" else -7) * W.LARGEST[kind] * ratio
             assert abs((diff * v).sum()) <= limit, (ratio, period, (diff * v).sum(), limit)
+
+
+@pytest.mark.parametrize("kind", ["single", "pair"])
+@pytest.mark.parametrize("q_terms,w_terms", [(2, 2), (1, 2), (2, 1)])
+def test_row_errors_tell_one_term_from_two(kind, q_terms, w_terms):
+    """The bounds of tests/paged8_errors.py hold for the arithmetic as it is meant and for nothing less."""
+    r = np.random.RandomState(2)
+    heads, page, n, d_sem, d_pos = 8, 64, 1500, 512, 64
+    n_pages = -(-n // page)
+    sem, pos = (R.encode(np.clip(r.randn(n_pages, 1, page, d) * 60, -448, 448)) for d in (d_sem, d_pos))
+    scale = (2.0 ** r.randint(-7, -4, (n_pages, 1))).astype(np.float32)
+    q_sem, q_pos = (torch.from_numpy(0.4 * r.randn(1, 1, heads, d)).bfloat16().double().numpy() for d in (d_sem, d_pos))
+    table = np.arange(n_pages, dtype=np.int32)[None]
+    sm = 1.0 / np.sqrt(192.0)
+    want, want_lse, _, _ = R.attend(q_sem, q_pos, sem, pos, scale, None, table, [0], [n], page, page, sm)
+    rows = np.arange(n)
+    s = scale[rows // page, 0].astype(np.float64)
+    v, k = (R.decode(torch.from_numpy(c)).reshape(n_pages * page, -1)[:n] for c in (sem, pos))
+    q = np.concatenate([q_sem[0, 0], q_pos[0, 0]], -1)
+    f = 2.0 ** (7 - np.floor(np.log2(np.abs(q).max(-1, keepdims=True))))       # the largest element into [128, 256)
+    hi = W.e4m3(q * f)
+    q8 = (hi + (W.e4m3(q * f - hi) if q_terms == 2 else 0.0)) / f
+    y = sm * s * (q8 @ np.concatenate([v, k], -1).T)                           # [heads, n]
+    top = (y + np.log(s)).max(-1, keepdims=True)
+    t = W.rounded(kind, W.LARGEST[kind] * np.exp(y + np.log(s) - top), np.broadcast_to(rows, y.shape), w_terms)
+    total = (W.LARGEST[kind] * np.exp(y - top)).sum(-1, keepdims=True)
+    out = torch.from_numpy((t @ v) / total).bfloat16().double().numpy()[None, None]
+    lse = (np.log(total / W.LARGEST[kind]) + top)[None, None, :, 0]
+    if (q_terms, w_terms) == (2, 2):
+        row_errors(out, lse, want, want_lse)
+    else:
+        with pytest.raises(AssertionError):
+            row_errors(out, lse, want, want_lse)
