@@ -1,0 +1,90 @@
+"""Paged 8-bit cache on the GPU: the variants that only large calls take, calls from two threads, tensors of other shapes."""
+import numpy as np
+import pytest
+import torch
+
+from tests import paged8_reference as R
+from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, i32, no_timeout  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ------------------------------------------------------------------------------------------------------- page update
+@pytest.mark.parametrize("tokens", [[16 * 1000] * 3, [16 * 8] * 700, [16 * 2000 - 3], [16 * 2100], [1] * 40 + [16 * 900, 0, 16 * 1500 + 1],
+                                    [16 * 9, 16 * 8, 5], [16 * 30] * 90 + [3] * 600])
+def test_page_update_of_many_entries(B, tokens):
+    """Prompts, their condensation and their end: thousands of entries taken and given back, by few sequences and by many, one of
+    them far longer than the others; with slots (the whole cluster) and without."""
+    page = g = 16
+    nb, width = len(tokens), -(-max(tokens) // page) + 1
+    T = Tables(B, nb, width, sum(-(-t // page) for t in tokens) + nb + 5, page, g, seed=nb)
+    full = [(0, t) for t in tokens]
+    assert T.update(full, sum(tokens) + 9) == 0                                # everything taken, packed slots
+    assert T.update([(0, 0)] * nb, 0, slots=False) == 0                        # everything given back
+    assert int(T.n_free) == T.free.numel()
+    assert T.update(full, 0, slots=False) == 0                                 # taken without slots
+    half = [(t // g // 2, t) for t in tokens]
+    assert T.update(half, sum(tokens)) == 0                                    # half of it condensed: given back and taken in one call
+    assert T.update([(r, max(t - 40, r * g)) for r, t in half], 0, slots=False) == 0
+    assert T.update(half, 40 * nb, per_seq=40) == 0                            # slots in places of their own
+    assert T.update([(0, 0)] * nb, 3) == 0
+    assert int(T.n_free) == T.free.numel()
+
+
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_page_update_slot_maps_at_any_address(B, shift):
+    tokens = [3000, 0, 17, 5001, 999, 1]
+    page, width = 32, 160
+    n = sum(tokens) + 7
+    p = B.make_params("mla", len(tokens), 1, 16, 1, 512, 64, 64, 0, 1.0)
+    perm = np.random.RandomState(shift).permutation(400)
+    table = torch.full((len(tokens), width), -1, dtype=torch.int32, device=DEV)
+    cache = B.paged8_cache(None, None, None, None, table, page_size=page, n_pages=400)
+    whole = torch.full((n + 8,), -7, dtype=torch.int32, device=DEV)
+    slots, status = whole[shift:shift + n], i32([-1])
+    assert slots.data_ptr() % 16 != 0
+    B.page_update(p, cache, None, i32(tokens), None, i32([0] * len(tokens)), i32(perm), i32([400]), slots, torch.empty(len(tokens) + 1, dtype=torch.int32, device=DEV),
+                  status)
+    ref = R.Pages(np.full((len(tokens), width), -1), perm, 400, page, 64, 400)
+    want, _ = ref.update([(0, t) for t in tokens])
+    flat = [s for w in want for s in w]
+    assert int(status) == 0 and whole.cpu().tolist() == [-7] * shift + flat + [-1] * (n - len(flat)) + [-7] * (8 - shift)
+
+
+# ------------------------------------------------------------------------------------------------------------- write
+@pytest.mark.parametrize("shape,kv,page,n_rows", [("mla512", 1, 16, 20000), ("mla512", 1, 64, 80000), ("mla128", 1, 32, 40000),
+                                                  ("gqa128", 8, 16, 10000), ("gqa128", 4, 32, 9000), ("gqa64", 8, 64, 30000), ("gqa64", 2, 128, 30000)])
+def test_write_of_whole_prompts(B, shape, kv, page, n_rows):
+    """So many rows that a CTA (a warp) looks for the runs of several rows: whole pages, runs that start inside one, padding."""
+    variant, _, d_sem, d_pos = SHAPES[shape]
+    r = np.random.RandomState(page + kv)
+    slots, used = [], 0
+    pages = iter(r.permutation(2 * n_rows // page + 64))
+    while len(slots) < n_rows:
+        kind = r.randint(0, 12)
+        n, first = (page, 0) if kind < 8 else (r.randint(1, page + 1), 0) if kind < 10 else (0, 0)
+        if kind == 10:
+            first = r.randint(1, page)
+            n = r.randint(1, page - first + 1)
+        pg = int(next(pages))
+        slots += [pg * page + first + k for k in range(n)] if kind < 11 else [-1] * r.randint(1, 40)
+        used = max(used, pg + 1)
+    slots = slots[:n_rows]
+    gain = np.exp(2.0 * r.randn(n_rows, 1, 1)).astype(np.float32)
+    sem, pos = (torch.from_numpy(r.standard_normal((n_rows, kv, d)).astype(np.float32) * gain).bfloat16() for d in (d_sem, d_pos))
+    q = np.random.RandomState(3)
+    code = lambda d: q.randint(0, 127, (used, kv, page, d), dtype=np.uint8)    # noqa: E731
+    scale = lambda: (2.0 ** q.randint(-8, -4, (used, kv))).astype(np.float32)  # noqa: E731
+    check_write(B, shape, kv, page, slots, sem, pos, (code(d_sem), code(d_pos), scale(), scale() if variant == "gqa" else None), used)
+
+
+# ------------------------------------------------------------------------------------------------------------ attend
+@pytest.mark.parametrize("shape,heads,kv,nb", [("gqa64", 4, 2, 700), ("gqa128", 2, 1, 300), ("mla512", 2, 1, 600), ("mla512", 34, 1, 300), ("mla128", 20, 1, 400),
+                                               ("gqa64", 33, 1, 257)])
+def test_attend_more_sequences_than_threads(B, shape, heads, kv, nb):
+    r = np.random.RandomState(nb)
+    states = [(0, int(n)) for n in r.randint(0, 40, nb)]
+    for b in r.randint(0, nb, 12):
+        states[b] = (0, int(r.randint(200, 900)))
+    states[-1], states[0] = (2, 2 * 64 + 77), (0, 0)
+    check_attend(B, shape, heads, kv, 16, states, 64, 1, seed=nb, bias=0.3)
