@@ -11,7 +11,8 @@ pytestmark = pytest.mark.gpu
 
 # ------------------------------------------------------------------------------------------------------- page update
 @pytest.mark.parametrize("tokens", [[16 * 1000] * 3, [16 * 8] * 700, [16 * 2000 - 3], [16 * 2100], [1] * 40 + [16 * 900, 0, 16 * 1500 + 1],
-                                    [16 * 9, 16 * 8, 5], [16 * 30] * 90 + [3] * 600])
+                                    [16 * 9, 16 * 8, 5], [16 * 30] * 90 + [3] * 600,
+                                    [1] * 300 + [16 * 700] + [20] * 100, [5] * 600 + [16 * 400 - 1, 0, 16 * 300]])
 def test_page_update_of_many_entries(B, tokens):
     """Prompts, their condensation and their end: thousands of entries taken and given back, by few sequences and by many, one of
     them far longer than the others; with slots (the whole cluster) and without."""
@@ -29,6 +30,32 @@ def test_page_update_of_many_entries(B, tokens):
     assert T.update(half, 40 * nb, per_seq=40) == 0                            # slots in places of their own
     assert T.update([(0, 0)] * nb, 3) == 0
     assert int(T.n_free) == T.free.numel()
+
+
+def test_page_update_of_one_long_sequence_takes_no_longer_than_of_a_longer_one(B):
+    """What one sequence takes and gives back is shared by a warp, whatever the number of entries of the whole call."""
+    page, times = 16, []
+    for pages in (2000, 2100):
+        p = B.make_params("mla", 1, 1, 16, 1, 512, 64, page, 0, 1.0)
+        table = torch.full((1, pages), -1, dtype=torch.int32, device=DEV)
+        cache = B.paged8_cache(None, None, None, None, table, page_size=page, n_pages=pages)
+        free, n_free, held, status = torch.arange(pages, dtype=torch.int32, device=DEV), i32([pages]), i32([0]), i32([-1])
+        state = [i32([0]), i32([pages * page])]
+        ev = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+        best = 1e9
+        for _ in range(5):
+            torch.cuda.synchronize()
+            ev[0].record()
+            for _ in range(10):
+                for to in state[::-1]:
+                    B.page_update(p, cache, None, to, None, held, free, n_free, None, None, status)
+            ev[1].record()
+            torch.cuda.synchronize()
+            best = min(best, ev[0].elapsed_time(ev[1]) / 20)
+        assert int(status) == 0 and int(n_free) == pages
+        times.append(best * 1e3)
+    print("2000 pages %.1f us, 2100 pages %.1f us" % tuple(times))
+    assert times[0] <= 2 * times[1], times
 
 
 @pytest.mark.parametrize("shift", [1, 2, 3])
