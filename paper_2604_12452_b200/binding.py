@@ -583,6 +583,17 @@ def _arg(x, dtype, n, dev):
     return x.data_ptr()
 
 
+def _queries(x, B, tokens, heads, d, dev):
+    """Address of bf16 queries [B, tokens, heads, d].  More sequences may follow, but each has to have exactly these rows: the
+    library finds a sequence by them."""
+    if x is None:
+        return None
+    n = tokens * heads * d
+    if x.shape[1:] != (tokens, heads, d) if x.dim() == 4 else x.numel() != B * n:
+        raise ValueError(f"expected queries of {tokens} x {heads} x {d} for every sequence, not {list(x.shape)}")
+    return _arg(x, _BF16, B * n, dev)
+
+
 def _paged8_device(params: LcaParams, cache: LcaPaged8, stream, table: bool = True):
     """The cache's device, which has to be the current one, the stream to launch on and (n_kv_heads, d_sem, d_pos); the
     tables and pages have to be those of params."""
@@ -648,7 +659,7 @@ def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n
         ws = _new(torch.empty, max(lca_paged8_workspace_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
     rows = B * q_len * H
     _check(_lib.lca_decode_attention_paged8(
-        params, cache, _arg(q_sem, _BF16, rows * d_sem, dev), _arg(q_pos, _BF16, rows * d_pos, dev), q_len,
+        params, cache, _queries(q_sem, B, q_len, H, d_sem, dev), _queries(q_pos, B, q_len, H, d_pos, dev), q_len,
         _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * d_sem, dev), _arg(lse, _F32, rows, dev),
         _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_attention_paged8")
     return out, lse
@@ -656,8 +667,8 @@ def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n
 
 def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
                          rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
-    """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], the n latest positions, or the ready summary query qbar
-    [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
+    """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], exactly the n latest positions, n = n_summary_q or group_size, or the
+    ready summary query qbar [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
     dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream)
     B = params.batch
     if n_rep_new is None:
@@ -671,10 +682,10 @@ def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail
     if ws is None:
         ws = _new(torch.empty, max(lca_workspace_bytes(params, LCA_WS_UPDATE), 16), torch.uint8, n_tok.device, stream)
     n = params.n_summary_q if params.n_summary_q > 0 else params.group_size
-    rows, blocks = B * n * params.n_q_heads, B * Hkv
+    H, blocks = params.n_q_heads, B * Hkv
     dk = d_pos + (d_sem if params.variant == LCA_VARIANT_MLA else 0)
     _check(_lib.lca_decode_update_paged8(
-        params, cache, _arg(q_tail_sem, _BF16, rows * d_sem, dev), _arg(q_tail_pos, _BF16, rows * d_pos, dev), n,
+        params, cache, _queries(q_tail_sem, B, n, H, d_sem, dev), _queries(q_tail_pos, B, n, H, d_pos, dev), n,
         _arg(qbar, _F32, blocks * dk, dev), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(n_rep_new, _I32, B, dev),
         _arg(rep_sem, _BF16, blocks * d_sem, dev), _arg(rep_pos, _BF16, blocks * d_pos, dev), _arg(anchor, _I32, blocks, dev),
         _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_update_paged8")

@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from tests import paged8_reference as R
-from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, i32, no_timeout  # noqa: F401
+from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, decode_case, i32, no_timeout  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +115,30 @@ def test_attend_more_sequences_than_threads(B, shape, heads, kv, nb):
         states[b] = (0, int(r.randint(200, 900)))
     states[-1], states[0] = (2, 2 * 64 + 77), (0, 0)
     check_attend(B, shape, heads, kv, 16, states, 64, 1, seed=nb, bias=0.3)
+
+
+# --------------------------------------------------------------------------------------------------------- refusals
+def test_helpers_refuse_queries_of_other_strides(B):
+    """More positions than the call reads would put every sequence but the first at the wrong place."""
+    p, cache, q_sem, q_pos, n_rep, n_tok, qbar = decode_case(B, 16, 4)
+    p.n_summary_q = 10
+    tail = [torch.randn((3, 64, 16, d), device=DEV).bfloat16() for d in (512, 64)]
+    two = [torch.cat([x, x], 1) for x in (q_sem, q_pos)]
+    wide = torch.cat([q_pos, q_pos], 2)
+    before = B.lca_launch_count()
+    calls = [lambda: B.decode_update_paged8(p, cache, *tail, n_rep, n_tok),
+             lambda: B.decode_update_paged8(p, cache, tail[0][:, :10].contiguous(), tail[1], n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, two[0], q_pos, n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, wide, n_rep, n_tok),
+             lambda: B.decode_attention_paged8(p, cache, q_sem, two[1], n_rep, n_tok)]
+    for k, call in enumerate(calls):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("call %d was not refused" % k)
+    assert B.lca_launch_count() == before
+    # what fits is taken: the exact tensors, and more sequences than the call has
+    a = B.decode_update_paged8(p, cache, *[x[:, :10].contiguous() for x in tail], n_rep, n_tok)
+    b = B.decode_update_paged8(p, cache, *[torch.cat([x[:, :10], x[:1, :10]]) for x in tail], n_rep, n_tok)
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+    assert torch.equal(B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok)[0],
+                       B.decode_attention_paged8(p, cache, torch.cat([q_sem, q_sem]), torch.cat([q_pos, q_pos]), n_rep, n_tok)[0])
