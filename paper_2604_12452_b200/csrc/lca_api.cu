@@ -526,7 +526,7 @@ int lca_decode_update_paged8(const lca_params* p, const lca_paged8* cache, const
     if (ws_bytes < update_workspace_bytes(p)) return LCA_ERR_WORKSPACE_TOO_SMALL;
   }
   if (!aligned16(rep_sem) || !aligned16(rep_pos)) return LCA_ERR_MISALIGNED;
-  if (paged8_update_smem_bytes(p) > 227u * 1024u) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if (paged8_update_smem_bytes(p) > (size_t)PAGED8_UPDATE_SMEM) return LCA_ERR_UNSUPPORTED_SHAPE;
   const double* qbar = nullptr;
   if (!qbar_opt) {
     st = update_qbar_launch(p, q_tail_sem, q_tail_pos, q_tail_batch_stride, ws, (cudaStream_t)stream);

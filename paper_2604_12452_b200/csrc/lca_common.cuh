@@ -217,6 +217,7 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
                        int32_t* row_offsets, int32_t* status, cudaStream_t stream);
 int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* rows_sem, const void* rows_pos,
                         const int32_t* slot_map, long long n_rows, cudaStream_t stream);
+static constexpr int PAGED8_UPDATE_SMEM = 227 * 1024 - 128;              // most that the update kernel may ask for, beside its static part
 size_t paged8_update_smem_bytes(const lca_params* p);
 int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
                          const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,

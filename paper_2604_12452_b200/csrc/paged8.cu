@@ -765,7 +765,9 @@ size_t paged8_update_smem_bytes(const lca_params* p) {
 template <bool MLA, int DS, int DP>
 static int update8_launch(const Update8Args& a, long long grid, size_t smem, cudaStream_t stream) {
   auto kern = paged8_update_kernel<MLA, DS, DP>;
-  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != cudaSuccess)
+  // The limit belongs to the kernel, not to the call: every call sets the same one, so that another thread's call with a smaller
+  // group does not lower it before this one's launch.
+  if (smem > 48 * 1024 && cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PAGED8_UPDATE_SMEM) != cudaSuccess)
     return LCA_ERR_CUDA;
   return launch_chained(kern, (unsigned)grid, UPD_THREADS, smem, stream, 1, a);
 }

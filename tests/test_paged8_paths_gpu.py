@@ -1,10 +1,12 @@
 """Paged 8-bit cache on the GPU: the variants that only large calls take, calls from two threads, tensors of other shapes."""
+import threading
+
 import numpy as np
 import pytest
 import torch
 
 from tests import paged8_reference as R
-from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, decode_case, i32, no_timeout  # noqa: F401
+from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, decode_case, i32, no_timeout, pool, to_gpu  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -142,3 +144,58 @@ def test_helpers_refuse_queries_of_other_strides(B):
     assert all(torch.equal(x, y) for x, y in zip(a, b))
     assert torch.equal(B.decode_attention_paged8(p, cache, q_sem, q_pos, n_rep, n_tok)[0],
                        B.decode_attention_paged8(p, cache, torch.cat([q_sem, q_sem]), torch.cat([q_pos, q_pos]), n_rep, n_tok)[0])
+
+
+def test_updates_of_two_group_sizes_from_two_threads(B):
+    """The same kernel with two amounts of shared memory above 48 KB, called from two threads at once."""
+    errors = []
+
+    def worker(g):
+        try:
+            states = [(0, 2 * g)]
+            pool_ = pool("mla512", 2 * g // 16, 16, 5, 1)
+            cache, keep = to_gpu(B, pool_, torch.arange(2 * g // 16, dtype=torch.int32, device=DEV)[None].contiguous())
+            p = B.make_params("mla", 1, 1, 16, 1, 512, 64, g, 16, 0.08)
+            qbar = torch.randn((1, 1, 576), generator=torch.Generator().manual_seed(1)).to(DEV)
+            n_rep, n_tok = i32([states[0][0]]), i32([states[0][1]])
+            first = B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar)
+            outs = dict(n_rep_new=first[0].clone(), rep_sem=first[1].clone(), rep_pos=first[2].clone(), anchor=first[3].clone(),
+                        ws=B.workspace(p, B.LCA_WS_UPDATE, DEV))
+            barrier.wait()
+            for _ in range(4000):
+                B.decode_update_paged8(p, cache, None, None, n_rep, n_tok, qbar=qbar, **outs)
+        except Exception as e:                                                 # noqa: BLE001
+            errors.append((g, e))
+
+    barrier = threading.Barrier(4, timeout=60)
+    threads = [threading.Thread(target=worker, args=(g,)) for g in (96, 368, 112, 352)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    assert not errors, errors
+
+
+@pytest.mark.parametrize("shape,kv,g", [("mla512", 1, 368), ("mla128", 1, 1056), ("gqa128", 2, 800), ("gqa64", 1, 1504)])
+def test_update_of_the_largest_groups(B, shape, kv, g):
+    """The largest group that shared memory holds, and the next one, which is refused."""
+    variant, _, d_sem, d_pos = SHAPES[shape]
+    page, n_pages = 16, g // 16 + 3
+    pool_ = pool(shape, n_pages, page, 7, kv)
+    table = np.random.RandomState(g).permutation(n_pages)[None, :g // 16 + 1].astype(np.int32)
+    cache, _ = to_gpu(B, pool_, torch.from_numpy(table).to(DEV))
+    dk = d_pos + (d_sem if variant == "mla" else 0)
+    qbar = torch.randn((1, kv, dk), generator=torch.Generator().manual_seed(4)) * 0.2
+    p = B.make_params(variant, 1, 1, kv, kv, d_sem, d_pos, g, 3, 0.08)
+    new, sem, pos, anchor = B.decode_update_paged8(p, cache, None, None, i32([0]), i32([g + 3]), qbar=qbar.to(DEV))
+    _, want_sem, want_pos, want_anchor = R.update(*pool_, table, [0], [g + 3], qbar.numpy(), g, 3, page, 0.08)
+    assert new.tolist() == [1] and anchor.cpu().tolist() == want_anchor.tolist()
+    vmax = np.abs(R.decode(torch.from_numpy(pool_[0]))).max() * pool_[2].max()
+    for h in range(kv):                                                        # as in test_update_against_the_definition
+        err = np.abs(sem[0, h].double().cpu().numpy() - want_sem[0, h])
+        assert np.all(err <= 2.0 ** -8 * np.abs(want_sem[0, h]) + (g + 8) * 2.0 ** -23 * vmax)
+        assert np.array_equal(pos[0, h].double().cpu().numpy(), want_pos[0, h])
+    p.group_size = g + 16
+    with pytest.raises(B.LcaError):
+        B.decode_update_paged8(p, cache, None, None, i32([0]), i32([g + 3]), qbar=qbar.to(DEV))
