@@ -293,7 +293,8 @@ int lca_decode_step_update_ring(const lca_params* p, const void* q_sem, const vo
 
 /* ---- Paged 8-bit cache ----------------------------------------------------------------------
  * The decode cache of many sequences in one pool of pages, each row element held in 8 bits (e4m3) with one
- * positive fp32 scale for each (page, KV head): value = code * scale.
+ * fp32 scale for each (page, KV head): value = code * scale.  Scales are positive, from 2^-100 (the attention takes smaller
+ * ones of values as that) to 2^120; they need not be powers of two.
  *
  * Rows are addressed by position, so nothing moves when a group is condensed: token number n of a sequence is
  * row n; representative j is row j, which belonged to a token condensed long before (n_rep <= n_rep * group_size).
@@ -348,9 +349,12 @@ int lca_page_update(const lca_params* p, const lca_paged8* cache, const int32_t*
  * Rows are appended: the rows of one page come together, in the order of their places, and a page is first written at
  * place 0, which sets its scale anew (so a page needs no clearing between owners).  Two rows with the same slot, or two
  * separate runs of rows for one page, in one call leave that page undefined.
- * Scale of a block (page, KV head): the smallest power of two with max|x| <= 448 * scale over its finite elements (MLA:
- * over latent and rope key together), at least 2^-100.  A later row with a larger element raises the scale; the rows
- * the block holds already are then rounded again, which is exact except where a code falls below the normal range.
+ * Scale of a block (page, KV head): the smallest power of two with max|x| <= 448 * scale over the finite elements (MLA:
+ * over latent and rope key together) of every row written since place 0 of its page, at least 2^-100.  A later row with a larger
+ * element raises the scale; the rows the block holds already are then rounded again, which is exact except where a code
+ * falls below the normal range.  Rows taken back by lca_page_update count too: what a large element in a rejected token did to
+ * the scale and to the rows before it on that page is not undone, and a row appended in its place uses that scale.  Write
+ * tokens once they are accepted where that matters.
  * Codes are rounded to nearest even; infinities become +-448 * scale, NaN stays NaN.
  * Of `cache` the pages, scales, n_pages and page_size are used, of p variant, n_kv_heads, d_sem and d_pos. */
 int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* rows_sem, const void* rows_pos,

@@ -107,6 +107,34 @@ def test_write_of_whole_prompts(B, shape, kv, page, n_rows):
     check_write(B, shape, kv, page, slots, sem, pos, (code(d_sem), code(d_pos), scale(), scale() if variant == "gqa" else None), used)
 
 
+@pytest.mark.parametrize("shape,kv", [("mla512", 1), ("gqa128", 2)])
+def test_write_after_a_rollback(B, shape, kv):
+    """Draft rows, one of them large, are written, taken back, and others appended in their place: the scale covers every row
+    written since the page was opened, and the rows before the drafts stay as they were rounded with it."""
+    variant, _, d_sem, d_pos = SHAPES[shape]
+    page, g = 16, 16
+    p = B.make_params(variant, 1, 1, kv, kv, d_sem, d_pos, g, 0, 1.0)
+    cache = B.new_paged8_cache(p, 4, page, 3, DEV)
+    free, n_free, held, status = i32([2, 0, 3, 1]), i32([4]), i32([0]), i32([-1])
+    gen = torch.Generator().manual_seed(3)
+    ref, tok = [x.cpu().numpy().copy() if x is not None else None for x in cache.tensors[:4]], 0
+    for to, gain in ((7, 1.0), (12, 40.0), (7, None), (9, 0.3), (20, 5.0), (16, None), (18, 0.1)):      # the last pair: at a page's place 0
+        slots = torch.empty(max(to - tok, 1), dtype=torch.int32, device=DEV)
+        B.page_update(p, cache, None, i32([to]), None, held, free, n_free, slots, i32([0, 0]), status)
+        assert int(status) == 0
+        if gain is not None:
+            rows = [(torch.randn((to - tok, kv, d), generator=gen) * gain).bfloat16() for d in (d_sem, d_pos)]
+            B.paged8_write(p, cache, rows[0].to(DEV), rows[1].to(DEV), slots)
+            ref = list(R.write(*ref, rows[0].double().numpy(), rows[1].double().numpy(), slots.cpu().tolist(), page))
+        tok = to
+    for got, want in zip(cache.tensors[:4], ref):
+        if want is not None:
+            got = got.cpu().numpy()
+            if want.dtype == np.uint8:
+                got, want = np.where(got == 128, 0, got), np.where(want == 128, 0, want)
+            assert np.array_equal(got, want)
+
+
 # ------------------------------------------------------------------------------------------------------------ attend
 @pytest.mark.parametrize("shape,heads,kv,nb", [("gqa64", 4, 2, 700), ("gqa128", 2, 1, 300), ("mla512", 2, 1, 600), ("mla512", 34, 1, 300), ("mla128", 20, 1, 400),
                                                ("gqa64", 33, 1, 257)])
