@@ -596,12 +596,18 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged8_kernel(cons
 bool make_tensor_map_pages(CUtensorMap* map, const void* ptr, int d, int page, long long blocks, int box_d, int box_rows);   // attn_tc.cu
 
 // Query rows that share a tile of keys.  The tile is padded to that number, so it is the smallest one that holds all rows of
-// a KV head (the softmax threads compute an exponential per padded row and key); at most 64, as O takes d / 128 * NH columns
-// of TMEM.  The MLA shape with more than 32 rows goes to CTA pairs in blocks of 128 (64 x 5056 rows, 128 heads: 128 us in
-// blocks of 64 on single CTAs, 92 us on pairs).
+// a KV head (the softmax threads compute an exponential per padded row and key); at most 64.  The MLA shape has columns of TMEM for
+// 32 (O takes d / 128 * 2 NH of 512, S 4 NH): 33 to 64 rows are two such blocks, more go to CTA pairs in blocks of 128.  Single CTAs
+// against pairs, MLA 512 + 64:
+//                                     64 x 5056 rows   20 x 2500 .. 5056   1 x 2528   12 x up to 9001
+//   34 rows (two blocks)                 89 / 89 us          46 / 55        17 / 26       40 / 51
+//   64 rows (two blocks)                 92 / 92             48 / 57        17 / 26       43 / 52       (100 x 5056: 155 / 150)
+//   65 rows (three blocks)              143 / 92             56 / 57        17 / 26       47 / 52       (4 x 60000: 104 / 83)
+//   128 rows (four blocks)              187 / 95             69 / 62        18 / 27       56 / 54
 static int paged8_rows_per_tile(const lca_params* p, int q_len) {
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
-  return rows <= 16 ? 16 : rows <= 32 ? 32 : p->d_sem == 512 ? 128 : 64;
+  if (p->d_sem == 512) return rows <= 16 ? 16 : rows <= 64 ? 32 : 128;
+  return rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
 }
 // CTAs (or pairs) that share the work: all that are resident at once.
 static int paged8_grid(const lca_params* p, int nh) {

@@ -136,7 +136,7 @@ def test_write_after_a_rollback(B, shape, kv):
 
 
 # ------------------------------------------------------------------------------------------------------------ attend
-@pytest.mark.parametrize("shape,heads,kv,nb", [("gqa64", 4, 2, 700), ("gqa128", 2, 1, 300), ("mla512", 2, 1, 600), ("mla512", 34, 1, 300), ("mla128", 20, 1, 400),
+@pytest.mark.parametrize("shape,heads,kv,nb", [("gqa64", 4, 2, 700), ("gqa128", 2, 1, 300), ("mla512", 2, 1, 600), ("mla512", 34, 1, 300), ("mla512", 66, 1, 300), ("mla128", 20, 1, 400),
                                                ("gqa64", 33, 1, 257)])
 def test_attend_more_sequences_than_threads(B, shape, heads, kv, nb):
     r = np.random.RandomState(nb)

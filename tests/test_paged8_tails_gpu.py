@@ -73,6 +73,7 @@ def test_a_flat_tail_keeps_its_weight_whatever_its_values(B, shape, heads, kind,
 
 CASES = [("mla512", 16, 1, 64, [(0, 9000)], 1), ("mla512", 128, 1, 64, [(0, 3000), (0, 1700), (20, 20 * 64 + 900)], 1),
          ("mla512", 40, 1, 32, [(3, 3 * 64 + 70), (17, 17 * 64 + 333)], 2), ("mla512", 32, 1, 16, [(0, 1000), (0, 1)], 1),
+         ("mla512", 80, 1, 32, [(3, 3 * 64 + 70), (17, 17 * 64 + 333)], 1), ("mla512", 24, 1, 64, [(0, 700), (9, 9 * 64 + 64)], 3),
          ("mla128", 32, 1, 64, [(0, 777), (5, 5 * 64 + 1)], 1), ("gqa128", 32, 8, 64, [(70, 70 * 64 + 500), (0, 2000)], 1),
          ("gqa128", 8, 2, 16, [(0, 5003), (0, 130)], 4), ("gqa128", 70, 1, 64, [(0, 900)], 1), ("gqa64", 24, 2, 128, [(0, 12001), (0, 50)], 1)]
 
