@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from tests import paged8_reference as R
-from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, decode_case, i32, no_timeout, pool, to_gpu  # noqa: F401
+from tests.test_paged8_gpu import DEV, SHAPES, B, Tables, check_attend, check_write, compare, decode_case, i32, no_timeout, pool, to_gpu  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -227,3 +227,67 @@ def test_update_of_the_largest_groups(B, shape, kv, g):
     p.group_size = g + 16
     with pytest.raises(B.LcaError):
         B.decode_update_paged8(p, cache, None, None, i32([0]), i32([g + 3]), qbar=qbar.to(DEV))
+
+
+# --------------------------------------------------------------------------------------------------- the run of calls
+@pytest.mark.parametrize("variant,kv", [("mla", 1), ("gqa", 2)])
+def test_the_loop_with_the_last_queries(B, variant, kv):
+    """Prompts, then a decode loop in which the summary query is the mean of the last g queries: tables, slots, representatives,
+    anchors and attention against the 64-bit statements, the group that is condensed chosen by queries of the loop itself."""
+    g, w, page, heads, scale, lens = 16, 32, 16, 4 * kv, 0.06, [70, 33, 200]
+    d_sem, d_pos = (512, 64) if variant == "mla" else (128, 128)
+    nb, mla = len(lens), variant == "mla"
+    gen = torch.Generator().manual_seed(17)
+    rnd = lambda *s: torch.randn(s, generator=gen).bfloat16().to(DEV)          # noqa: E731
+    p = B.make_params(variant, nb, max(lens), heads, kv, d_sem, d_pos, g, w, scale)
+    T = sum(lens)
+    q_sem, q_pos = (rnd(T, heads, d_sem) if mla else None), rnd(T, heads, d_pos)
+    cond = B.condense_varlen(p, lens, q_sem, q_pos, rnd(T, kv, d_sem), rnd(T, kv, d_pos))
+    ends = np.cumsum(lens)
+    last = lambda q: torch.stack([q[e - g:e] for e in ends])                   # noqa: E731
+    tail = [last(q_sem) if mla else None, last(q_pos)]
+    m = [int(b - a) for a, b in zip(cond["group_offsets"], cond["group_offsets"][1:])]
+    n_pages, width = 48, 32
+    cache = B.new_paged8_cache(p, n_pages, page, width, DEV)
+    sem_p, pos_p, ss, sp, table = cache.tensors
+    free, n_free, held_rep, held_tok, status = i32(list(range(n_pages))), i32([n_pages]), i32([0] * nb), i32([0] * nb), i32([5])
+    n_rep, n_tok = i32(m), i32(lens)
+    slots, offsets = torch.empty(cond["cache_row_offsets"][-1], dtype=torch.int32, device=DEV), torch.empty(nb + 1, dtype=torch.int32, device=DEV)
+    slot = torch.empty(nb, dtype=torch.int32, device=DEV)
+    pages = R.Pages(table.cpu().numpy(), range(n_pages), n_pages, page, g, n_pages)
+
+    def move(out, **kw):
+        B.page_update(p, cache, n_rep, n_tok, held_rep, held_tok, free, n_free, out, offsets, status, **kw)
+        want, st = pages.update(list(zip(n_rep.tolist(), n_tok.tolist())))
+        flat = [s for x in want for s in (x + [-1] * (1 - len(x)) if kw else x)]
+        assert int(status) == st == 0 and out.tolist() == flat and table.tolist() == pages.table
+
+    move(slots)
+    B.paged8_write(p, cache, cond["cache_sem"], cond["cache_pos"], slots)
+    anchors = set()
+    for step in range(50):
+        n_tok += 1
+        move(slot, rows_per_seq=1)
+        B.paged8_write(p, cache, rnd(nb, kv, d_sem), rnd(nb, kv, d_pos), slot)
+        qs, qp = (rnd(nb, 1, heads, d_sem) if mla else None), rnd(nb, 1, heads, d_pos)
+        out, lse = B.decode_attention_paged8(p, cache, qs, qp, n_rep, n_tok, want_lse=True)
+        pools = [None if x is None else x.cpu().numpy() for x in (sem_p, pos_p, ss, sp)]
+        if step % 8 == 0:
+            want = R.attend(None if qs is None else qs.double().cpu().numpy(), qp.double().cpu().numpy(), *pools, table.cpu().numpy(),
+                            n_rep.tolist(), n_tok.tolist(), g, page, scale)
+            compare(out, lse, *want, n=260, top=1.0)
+        for t, q in zip(tail, (qs, qp)):
+            if t is not None:
+                t[:, step % g] = q[:, 0]
+        new, rsem, rpos, anchor = B.decode_update_paged8(p, cache, *tail, n_rep, n_tok)
+        mean = [t.double().view(nb, g, kv, heads // kv, -1).mean((1, 3)) for t in tail if t is not None]
+        ref = R.update(*pools, table.cpu().numpy(), n_rep.tolist(), n_tok.tolist(), torch.cat(mean, -1).cpu().numpy(), g, w, page, scale)
+        assert new.tolist() == ref[0].tolist() and anchor.tolist() == ref[3].tolist()
+        for (b, h), row in ref[1].items():                                     # g + 8 roundings of 2^-24 each way, one to bf16
+            assert np.all(np.abs(rsem[b, h].double().cpu().numpy() - row) <= 2.0 ** -8 * np.abs(row) + (g + 8) * 2.0 ** -23 * 8)
+            assert np.array_equal(rpos[b, h].double().cpu().numpy(), ref[2][b, h])
+            anchors.add(int(anchor[b, h]))
+        n_rep.copy_(new)
+        move(slot, rows_per_seq=1)
+        B.paged8_write(p, cache, rsem, rpos, slot)
+    assert len(anchors) > 3                                                    # the queries of the loop decide
