@@ -125,8 +125,12 @@ int attn_paged8_simt_launch(const Paged8Attn& q) {
 // S of tile j+1 is issued before O of tile j.  GQA: one ring of slots, filled in the order of use, K(0) K(1) V(0) K(2)
 // V(1) ...  MLA: the latent chunks are keys and values; they stay in their slots from S to O (two tiles at a time are in the
 // ring, a third one is arriving), which saves the second copy: the tensor core reads its operands over the same 128 bytes
-// per clock of shared memory that the copies are written through, and that is what bounds a tile (NH = 16: 720 clocks of
-// operands for S, 640 for O, 576 of copies; with a second copy of the values 1088).
+// per clock of shared memory that the copies are written through (NH = 16: 720 clocks of operands for S, 640 for O, 576 of
+// copies; with a second copy of the values 1088).
+// What bounds it.  GQA with one token: HBM (64 x 5056 rows, 32 heads on 8: 663 MB in 115 us, 5.8 TB/s).  MLA and several tokens: neither
+// HBM nor that port, but the chain of a tile, S, softmax, weights, O, with one group of warps and one buffer of weights for 16
+// rows; a tile's weights are stored once O of the tile before is complete.  64 x 5056 rows of 16 MLA heads, 17 tiles a CTA: 55 us, 3.1 us
+// or about 6000 clocks a tile where the port would take 1936; 32 heads 65 us; 12 sequences of up to 9001 rows and 4 tokens, GQA: 42 us.
 // Work: all tiles of all (sequence, KV head, block of NH rows) units form one line that is cut into equal ranges, one per
 // CTA; a unit that is cut leaves (O, M, l) of its pieces in the workspace, merged by paged8_combine_kernel.
 template <bool MLA_, int DS_, int DP_, int NH_>
