@@ -396,6 +396,126 @@ int lca_decode_update_paged8(const lca_params* p, const lca_paged8* cache, const
                              const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
                              void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- Paged 4-bit cache ----------------------------------------------------------------------
+ * The paged cache with each row element held in 4 bits, about half of the 8-bit cache's bytes (MLA 512 + 64: 298 a row, 8 KV heads
+ * of 128: 1072 instead of 2048).  Row space, pages, block tables and counters are those of lca_paged8, and lca_page_update manages
+ * them: pass it an lca_paged8 with the same block_table, n_pages, page_size and table_width (it uses nothing else).
+ *
+ *     value = code * 2^(exponent of its row and KV head - shift of its block of 32 columns)
+ *   code      a sign and a magnitude 0, 1/2, 1, 3/2, 2, 3, 4 or 6 (index 0..7).  Eight codes fill a little-endian 32-bit word: value
+ *             i has its magnitude's index in bits 4 i .. 4 i + 2 and its sign in bit 8 i + 7 (i < 4) or 8 (i - 4) + 3
+ *   exponent  a byte, 127 more than the exponent: 33 (-94) to 253 (126); smaller ones are taken as 33.  MLA: latent and rope key
+ *             share it, the logit is one sum
+ *   shift     four bits, 0 to 14; 15: the values of the block are NaN.  Two blocks to a byte, the first in the low half */
+typedef struct lca_paged4 {
+  void* pages_sem;        /* [n_pages, n_kv_heads, page_size, d_sem / 2] bytes: latents (GQA: V) */
+  void* pages_pos;        /* [n_pages, n_kv_heads, page_size, d_pos / 2] bytes: rope keys (GQA: K) */
+  uint8_t* shift_sem;     /* [n_pages, n_kv_heads, page_size, d_sem / 64] */
+  uint8_t* shift_pos;     /* [n_pages, n_kv_heads, page_size, d_pos / 64] */
+  uint8_t* exp_sem;       /* [n_pages, n_kv_heads, page_size] */
+  uint8_t* exp_pos;       /* [n_pages, n_kv_heads, page_size]; MLA: NULL */
+  int32_t* block_table;   /* [batch, table_width] */
+  int32_t n_pages;        /* as in lca_paged8 */
+  int32_t page_size;
+  int32_t table_width;
+} lca_paged4;             /* a HOST structure of device pointers; pages and shifts 16-byte aligned */
+
+/* Writes rows into the paged cache.  Arguments as for lca_paged8_write; but rows do not depend on one another, so they may come in
+ * any order and any number to a page, and a row is replaced by writing its slot again.  Two rows with the same slot in one call leave
+ * that row undefined.
+ * Scale of a block: the smallest power of two with max|x| <= 6 * scale over its finite elements.  The row's exponent is that of
+ * its largest block, at least -94 (MLA: over latent and rope key together), and no block is given less than 2^-14 of the row's scale.
+ * Codes are the nearest ones, ties to the even index; infinities become +-6 * scale; a NaN makes its block NaN. */
+int lca_paged4_write(const lca_params* p, const lca_paged4* cache, const void* rows_sem, const void* rows_pos,
+                     const int32_t* slot_map, int64_t n_rows, void* stream);
+
+/* The values of rows of the cache, in bf16 (exact but for values of 2^128, which a row whose largest element is above 7/8 of that may
+ * round to: infinity).
+ *   slot_map [n_rows] int32: slot of every row wanted, in any order, the same one any number of times
+ *   rows_sem [n_rows, n_kv_heads, d_sem], rows_pos [n_rows, n_kv_heads, d_pos] bf16 out: rows whose slot is negative or behind
+ *       the pool are left as they are */
+int lca_paged4_read(const lca_params* p, const lca_paged4* cache, void* rows_sem, void* rows_pos, const int32_t* slot_map,
+                    int64_t n_rows, void* stream);
+
+/* Decode attention over the paged 4-bit cache: lca_decode_attention_paged8 on the values that this cache stands for, with the same
+ * arguments and the same treatment of absent rows, of queries that see no row and of NaN.  The cached values enter the products
+ * exactly; queries and weights are sums of two 8-bit terms as there (a weight to 2^-9 of itself or to a step of 2^-18 of the largest). */
+size_t lca_paged4_workspace_bytes(const lca_params* p, const lca_paged4* cache, int32_t q_len);
+int lca_decode_attention_paged4(const lca_params* p, const lca_paged4* cache, const void* q_sem, const void* q_pos,
+                                int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
+                                void* ws, size_t ws_bytes, void* stream);
+
+/* Online update over the paged 4-bit cache: lca_decode_update_paged8 on the values that this cache stands for. */
+int lca_decode_update_paged4(const lca_params* p, const lca_paged4* cache, const void* q_tail_sem,
+                             const void* q_tail_pos, int64_t q_tail_batch_stride, const float* qbar_opt,
+                             const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
+                             void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- Rotary positions -----------------------------------------------------------------------
+ * The attention calls take queries and keys that carry their positions (q_pos, kv_pos; GQA: the whole head).  This call rotates
+ * them, from the layout that a projection leaves them in: for each token t, head and pair i of columns
+ *     (a, b) -> factor * (a cos - b sin, a sin + b cos) of the angle  positions[t] * freqs[i]
+ * Pairs are columns (2 i, 2 i + 1) where `interleaved`, else (i, i + rot_dim / 2).  Columns behind the first rot_dim are copied as they are
+ * (not multiplied by `factor`).  With `inverse` the angle is negated: that is also the gradient of the call.  Angles are exact to 64 bits,
+ * products fp32, rounded once. */
+enum { LCA_DTYPE_BF16 = 0, LCA_DTYPE_FP32 = 1 };
+typedef struct lca_rope_args {
+  int32_t dtype;              /* of q, k and the outputs */
+  int32_t interleaved;        /* 0 or 1 */
+  int32_t inverse;            /* 0 or 1 */
+  int32_t n_q_heads, n_k_heads;
+  int32_t head_dim;           /* columns of a head */
+  int32_t rot_dim;            /* even, 2 to min(head_dim, 8192): the first columns of a head */
+  float factor;
+  int64_t n_tokens;
+  const int32_t* positions;   /* [n_tokens] */
+  const double* freqs;        /* [rot_dim / 2] on the device (lca_rope_frequencies) */
+  /* Element (token, head, column) of a tensor is at token * token_stride + head * head_stride + column, in elements.  Tensors need
+   * only their element's alignment; 16-byte aligned rows and rot_dim a multiple of 16 are fast.  An output may be its input (same
+   * address and strides); otherwise they do not overlap, nor do the heads of an output.  k may be NULL, or q. */
+  const void* q; int64_t q_token_stride, q_head_stride;
+  void* q_out; int64_t q_out_token_stride, q_out_head_stride;
+  const void* k; int64_t k_token_stride, k_head_stride;
+  void* k_out; int64_t k_out_token_stride, k_out_head_stride;
+} lca_rope_args;              /* a HOST structure of device pointers */
+int lca_rope(const lca_rope_args* args, void* stream);
+
+/* Frequencies of the pairs on the HOST, f_i = base^(-2 i / rot_dim), and the factor that goes with them, for contexts `scale` times as
+ * long as `trained_len` tokens:
+ *   PLAIN   as they are, factor 1
+ *   LINEAR  f_i / scale
+ *   BASE    base * scale^(rot_dim / (rot_dim - 2)) in place of base: the fastest pair keeps its frequency, the slowest is divided by scale
+ *   RAMP    pairs that make more than `fast` turns in trained_len tokens keep f_i, those with less than `slow` take f_i / scale, between
+ *           them the share that is kept grows linearly with the turns; factor 0.1 ln(scale) + 1 where scale > 1
+ * trained_len, fast and slow are only used by RAMP (customary: fast = 32, slow = 1). */
+enum { LCA_ROPE_PLAIN = 0, LCA_ROPE_LINEAR = 1, LCA_ROPE_BASE = 2, LCA_ROPE_RAMP = 3 };
+int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scale, double trained_len, double fast,
+                         double slow, double* freqs_host, float* factor_host);
+
+/* ---- Verification of drafted tokens ----------------------------------------------------------
+ * Which of the drafted tokens of each request the target accepts, and the token that follows them, so that the outcome is distributed
+ * as the target's own samples.  With p_i the target's probabilities at draft i, q_i the drafter's and x_i the draft:
+ *   draft i is accepted while u_accept[i] * q_i(x_i) < p_i(x_i)  (the product in 64 bits, where it is exact)
+ *   the next token is drawn from max(p_i - q_i, 0) at the first rejected draft i, or from p after the last accepted one: the first
+ *       token v whose cumulative sum exceeds u_sample times the whole sum, in 64-bit sums
+ * Entries that are not positive finite numbers have no mass.  Where p_i - q_i leaves none, the token is drawn from p_i; where that has none
+ * either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
+typedef struct lca_verify_args {
+  int32_t dtype;                /* of both probabilities: LCA_DTYPE_FP32 or LCA_DTYPE_BF16 */
+  int32_t batch, n_drafts, vocab;       /* n_drafts >= 0 */
+  const void* target_probs;     /* [batch, n_drafts + 1, vocab]; they need not add up to 1 */
+  const void* draft_probs;      /* [batch, n_drafts, vocab]; NULL: the drafter is certain (q_i(x_i) = 1, 0 elsewhere) */
+  const int32_t* draft_tokens;  /* [batch, n_drafts] */
+  const int32_t* n_draft;       /* [batch]: drafts of each request, clamped to 0 .. n_drafts; NULL: n_drafts */
+  const float* u_accept;        /* [batch, n_drafts] in [0, 1) */
+  const float* u_sample;        /* [batch] in [0, 1) */
+  const int32_t* n_tok;         /* [batch], or NULL with n_tok_out: tokens in the cache, the drafts included */
+  int32_t* accepted;            /* [batch] out: number of accepted drafts */
+  int32_t* tokens_out;          /* [batch, n_drafts + 1] out: accepted drafts, the next token, then -1 */
+  int32_t* n_tok_out;           /* [batch] out, may be n_tok: n_tok less the rejected drafts, the target state for lca_page_update */
+} lca_verify_args;              /* a HOST structure of device pointers, each aligned to its element */
+int lca_verify_drafts(const lca_verify_args* args, void* stream);
+
 /* Value up-projection of the latent attention output (Alg. 1: v = c W^UV; Sec. 4.3: in the absorbed
  * form the attention result lives in the latent space and W^UV is applied to it once per query and
  * head):   out_v[t, h, :] = attn_latent[t, h, :] . W^UV[h]

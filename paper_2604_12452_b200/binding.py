@@ -26,6 +26,8 @@ LCA_STATIC_SCRATCH_BYTES = 1 << 20
 LCA_ERR_STATIC_SCRATCH_EXCEEDED = -7
 LCA_ERR_DEVICE_TIMEOUT = -6
 ATTN_AUTO, ATTN_SCALAR, ATTN_TENSOR = 0, 1, 2
+LCA_DTYPE_BF16, LCA_DTYPE_FP32 = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_RAMP = 0, 1, 2, 3
 REDUCE_DEFAULT, REDUCE_MAXPOOL, REDUCE_MEANPOOL, REDUCE_WEIGHTED, REDUCE_MAXSEL = 0, 1, 2, 3, 4
 
 
@@ -47,6 +49,38 @@ class LcaPaged8(C.Structure):
     device: Optional[int] = None               # CUDA device of the tensors (-1: not on one)
     batch: Optional[int] = None                # rows of block_table
     layout: Optional[tuple] = None             # (n_kv_heads, d_sem, d_pos) of the pages
+
+
+class LcaPaged4(C.Structure):
+    """Mirror of ``lca_paged4``: device pointers of a paged 4-bit cache.  Build it with ``paged4_cache``, which also keeps
+    the tensors alive."""
+    _fields_ = [("pages_sem", C.c_void_p), ("pages_pos", C.c_void_p), ("shift_sem", C.c_void_p), ("shift_pos", C.c_void_p),
+                ("exp_sem", C.c_void_p), ("exp_pos", C.c_void_p), ("block_table", C.c_void_p), ("n_pages", C.c_int32),
+                ("page_size", C.c_int32), ("table_width", C.c_int32)]
+    tensors: tuple = ()
+    device: Optional[int] = None
+    batch: Optional[int] = None
+    layout: Optional[tuple] = None
+    pages: Optional[LcaPaged8] = None          # the same tables for lca_page_update, which manages the pages of either cache
+
+
+class LcaRopeArgs(C.Structure):
+    """Mirror of ``lca_rope_args``."""
+    _fields_ = [("dtype", C.c_int32), ("interleaved", C.c_int32), ("inverse", C.c_int32), ("n_q_heads", C.c_int32),
+                ("n_k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("factor", C.c_float),
+                ("n_tokens", C.c_int64), ("positions", C.c_void_p), ("freqs", C.c_void_p),
+                ("q", C.c_void_p), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("q_out_token_stride", C.c_int64), ("q_out_head_stride", C.c_int64),
+                ("k", C.c_void_p), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("k_out", C.c_void_p), ("k_out_token_stride", C.c_int64), ("k_out_head_stride", C.c_int64)]
+
+
+class LcaVerifyArgs(C.Structure):
+    """Mirror of ``lca_verify_args``."""
+    _fields_ = [("dtype", C.c_int32), ("batch", C.c_int32), ("n_drafts", C.c_int32), ("vocab", C.c_int32),
+                ("target_probs", C.c_void_p), ("draft_probs", C.c_void_p), ("draft_tokens", C.c_void_p), ("n_draft", C.c_void_p),
+                ("u_accept", C.c_void_p), ("u_sample", C.c_void_p), ("n_tok", C.c_void_p), ("accepted", C.c_void_p),
+                ("tokens_out", C.c_void_p), ("n_tok_out", C.c_void_p)]
 
 
 class LcaError(RuntimeError):
@@ -109,6 +143,23 @@ def _load() -> C.CDLL:
     lib.lca_decode_attention_paged8.argtypes = [P, PC, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
     lib.lca_decode_update_paged8.restype = C.c_int
     lib.lca_decode_update_paged8.argtypes = [P, PC, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    P4 = C.POINTER(LcaPaged4)
+    lib.lca_paged4_write.restype = C.c_int
+    lib.lca_paged4_write.argtypes = [P, P4, vp, vp, vp, i64, vp]
+    lib.lca_paged4_read.restype = C.c_int
+    lib.lca_paged4_read.argtypes = [P, P4, vp, vp, vp, i64, vp]
+    lib.lca_paged4_workspace_bytes.restype = sz
+    lib.lca_paged4_workspace_bytes.argtypes = [P, P4, i32]
+    lib.lca_decode_attention_paged4.restype = C.c_int
+    lib.lca_decode_attention_paged4.argtypes = [P, P4, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+    lib.lca_decode_update_paged4.restype = C.c_int
+    lib.lca_decode_update_paged4.argtypes = [P, P4, vp, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.lca_rope.restype = C.c_int
+    lib.lca_rope.argtypes = [C.POINTER(LcaRopeArgs), vp]
+    lib.lca_rope_frequencies.restype = C.c_int
+    lib.lca_rope_frequencies.argtypes = [i32, i32] + [C.c_double] * 5 + [C.POINTER(C.c_double), C.POINTER(C.c_float)]
+    lib.lca_verify_drafts.restype = C.c_int
+    lib.lca_verify_drafts.argtypes = [C.POINTER(LcaVerifyArgs), vp]
     lib.lca_latent_to_value.restype = C.c_int
     lib.lca_latent_to_value.argtypes = [vp, vp, vp, i64, i32, i32, i32, vp]
     lib.lca_selftest_bounded_wait.restype = C.c_int
@@ -313,6 +364,48 @@ def lca_decode_update_paged8(params, cache, q_tail_sem, q_tail_pos, q_tail_batch
     return int(_lib.lca_decode_update_paged8(C.byref(params), C.byref(cache), _ptr(q_tail_sem), _ptr(q_tail_pos),
                                              int(q_tail_batch_stride), _ptr(qbar_opt), _ptr(n_rep), _ptr(n_tok), _ptr(n_rep_new),
                                              _ptr(rep_sem), _ptr(rep_pos), _ptr(anchor_out), _ptr(ws), wsb, _stream(stream)))
+
+
+def lca_paged4_write(params, cache, rows_sem, rows_pos, slot_map, n_rows, stream=None) -> int:
+    return int(_lib.lca_paged4_write(C.byref(params), C.byref(cache), _ptr(rows_sem), _ptr(rows_pos), _ptr(slot_map), int(n_rows),
+                                     _stream(stream)))
+
+
+def lca_paged4_read(params, cache, rows_sem, rows_pos, slot_map, n_rows, stream=None) -> int:
+    return int(_lib.lca_paged4_read(C.byref(params), C.byref(cache), _ptr(rows_sem), _ptr(rows_pos), _ptr(slot_map), int(n_rows),
+                                    _stream(stream)))
+
+
+def lca_paged4_workspace_bytes(params, cache, q_len: int) -> int:
+    return int(_lib.lca_paged4_workspace_bytes(C.byref(params), C.byref(cache), int(q_len)))
+
+
+def lca_decode_attention_paged4(params, cache, q_sem, q_pos, q_len, n_rep, n_tok, out, lse_opt, ws, ws_bytes=None, stream=None) -> int:
+    wsb = _nbytes(ws) if ws_bytes is None else int(ws_bytes)
+    return int(_lib.lca_decode_attention_paged4(C.byref(params), C.byref(cache), _ptr(q_sem), _ptr(q_pos), int(q_len), _ptr(n_rep),
+                                                _ptr(n_tok), _ptr(out), _ptr(lse_opt), _ptr(ws), wsb, _stream(stream)))
+
+
+def lca_decode_update_paged4(params, cache, q_tail_sem, q_tail_pos, q_tail_batch_stride, qbar_opt, n_rep, n_tok, n_rep_new, rep_sem,
+                             rep_pos, anchor_out, ws, ws_bytes=None, stream=None) -> int:
+    wsb = _nbytes(ws) if ws_bytes is None else int(ws_bytes)
+    return int(_lib.lca_decode_update_paged4(C.byref(params), C.byref(cache), _ptr(q_tail_sem), _ptr(q_tail_pos),
+                                             int(q_tail_batch_stride), _ptr(qbar_opt), _ptr(n_rep), _ptr(n_tok), _ptr(n_rep_new),
+                                             _ptr(rep_sem), _ptr(rep_pos), _ptr(anchor_out), _ptr(ws), wsb, _stream(stream)))
+
+
+def lca_rope(args: LcaRopeArgs, stream=None) -> int:
+    return int(_lib.lca_rope(C.byref(args), _stream(stream)))
+
+
+def lca_rope_frequencies(kind, rot_dim, base, scale, trained_len, fast, slow, freqs, factor) -> int:
+    """``freqs``: a ctypes array of rot_dim / 2 doubles, ``factor`` a c_float, both filled in."""
+    return int(_lib.lca_rope_frequencies(int(kind), int(rot_dim), base, scale, trained_len, fast, slow, freqs,
+                                         None if factor is None else C.byref(factor)))
+
+
+def lca_verify_drafts(args: LcaVerifyArgs, stream=None) -> int:
+    return int(_lib.lca_verify_drafts(C.byref(args), _stream(stream)))
 
 
 def lca_latent_to_value(attn_latent, w_uv, out_v, n_tokens, n_heads, d_latent, d_v, stream=None) -> int:
@@ -594,7 +687,7 @@ def _queries(x, B, tokens, heads, d, dev):
     return _arg(x, _BF16, B * n, dev)
 
 
-def _paged8_device(params: LcaParams, cache: LcaPaged8, stream, table: bool = True):
+def _paged_device(params: LcaParams, cache, stream, table: bool = True):
     """The cache's device, which has to be the current one, the stream to launch on and (n_kv_heads, d_sem, d_pos); the
     tables and pages have to be those of params."""
     dev = cache.device
@@ -618,11 +711,13 @@ def _new(make, shape, dtype, device, stream):
         return make(shape, dtype=dtype, device=device)
 
 
-def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, row_offsets,
+def page_update(params: LcaParams, cache, n_rep, n_tok, held_rep, held_tok, free_pages, n_free, slot_map, row_offsets,
                 status, rows_per_seq: int = 0, stream=None):
-    """Run lca_page_update in place on the tables, the free list and the held state; returns slot_map.  `status` is a device
-    tensor: read it where the caller has to know (0: done)."""
-    dev, at, _ = _paged8_device(params, cache, stream)
+    """Run lca_page_update in place on the tables (of an 8-bit or a 4-bit cache), the free list and the held state; returns
+    slot_map.  `status` is a device tensor: read it where the caller has to know (0: done)."""
+    dev, at, _ = _paged_device(params, cache, stream)
+    if type(cache) is LcaPaged4:
+        cache = cache.pages
     B = params.batch
     done, slots = _arg(status, _I32, 1, dev), _arg(slot_map, _I32, 0, dev)
     if slots == 0:                             # an empty tensor has no address, and no room for a row either: not "not wanted"
@@ -636,7 +731,7 @@ def page_update(params: LcaParams, cache: LcaPaged8, n_rep, n_tok, held_rep, hel
 
 def paged8_write(params: LcaParams, cache: LcaPaged8, rows_sem, rows_pos, slot_map, stream=None):
     """Quantise rows into the pages that slot_map names (in place)."""
-    dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream, table=False)
+    dev, at, (Hkv, d_sem, d_pos) = _paged_device(params, cache, stream, table=False)
     n = slot_map.numel()
     _check(_lib.lca_paged8_write(params, cache, _arg(rows_sem, _BF16, n * Hkv * d_sem, dev),
                                  _arg(rows_pos, _BF16, n * Hkv * d_pos, dev), _arg(slot_map, _I32, n, dev), n, at), "lca_paged8_write")
@@ -646,30 +741,32 @@ def workspace_paged8(params: LcaParams, cache: LcaPaged8, q_len: int, device) ->
     return torch.empty(max(lca_paged8_workspace_bytes(params, cache, q_len), 16), dtype=torch.uint8, device=device)
 
 
-def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
-                            want_lse: bool = False, ws=None, stream=None):
-    """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
-    dev, at, (_, d_sem, d_pos) = _paged8_device(params, cache, stream)
+def _decode_attention_paged(call, ws_bytes, name, params, cache, q_sem, q_pos, n_rep, n_tok, out, lse, want_lse, ws, stream):
+    dev, at, (_, d_sem, d_pos) = _paged_device(params, cache, stream)
     B, q_len, H = params.batch, q_pos.shape[1], params.n_q_heads
     if out is None:
         out = _new(torch.empty, (B, q_len, H, d_sem), _BF16, q_pos.device, stream)
     if lse is None and want_lse:
         lse = _new(torch.empty, (B, q_len, H), _F32, q_pos.device, stream)
     if ws is None:
-        ws = _new(torch.empty, max(lca_paged8_workspace_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
+        ws = _new(torch.empty, max(ws_bytes(params, cache, q_len), 16), torch.uint8, q_pos.device, stream)
     rows = B * q_len * H
-    _check(_lib.lca_decode_attention_paged8(
+    _check(call(
         params, cache, _queries(q_sem, B, q_len, H, d_sem, dev), _queries(q_pos, B, q_len, H, d_pos, dev), q_len,
         _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(out, _BF16, rows * d_sem, dev), _arg(lse, _F32, rows, dev),
-        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_attention_paged8")
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), name)
     return out, lse
 
 
-def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
-                         rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
-    """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], exactly the n latest positions, n = n_summary_q or group_size, or the
-    ready summary query qbar [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
-    dev, at, (Hkv, d_sem, d_pos) = _paged8_device(params, cache, stream)
+def decode_attention_paged8(params: LcaParams, cache: LcaPaged8, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
+                            want_lse: bool = False, ws=None, stream=None):
+    """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
+    return _decode_attention_paged(_lib.lca_decode_attention_paged8, lca_paged8_workspace_bytes, "lca_decode_attention_paged8", params, cache,
+                                   q_sem, q_pos, n_rep, n_tok, out, lse, want_lse, ws, stream)
+
+
+def _decode_update_paged(call, name, params, cache, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, qbar, anchor, ws, stream):
+    dev, at, (Hkv, d_sem, d_pos) = _paged_device(params, cache, stream)
     B = params.batch
     if n_rep_new is None:
         n_rep_new = _new(torch.empty, (B,), _I32, n_tok.device, stream)
@@ -684,9 +781,189 @@ def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail
     n = params.n_summary_q if params.n_summary_q > 0 else params.group_size
     H, blocks = params.n_q_heads, B * Hkv
     dk = d_pos + (d_sem if params.variant == LCA_VARIANT_MLA else 0)
-    _check(_lib.lca_decode_update_paged8(
+    _check(call(
         params, cache, _queries(q_tail_sem, B, n, H, d_sem, dev), _queries(q_tail_pos, B, n, H, d_pos, dev), n,
         _arg(qbar, _F32, blocks * dk, dev), _arg(n_rep, _I32, B, dev), _arg(n_tok, _I32, B, dev), _arg(n_rep_new, _I32, B, dev),
         _arg(rep_sem, _BF16, blocks * d_sem, dev), _arg(rep_pos, _BF16, blocks * d_pos, dev), _arg(anchor, _I32, blocks, dev),
-        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), "lca_decode_update_paged8")
+        _arg(ws, torch.uint8, 0, dev), ws.numel(), at), name)
     return n_rep_new, rep_sem, rep_pos, anchor
+
+
+def decode_update_paged8(params: LcaParams, cache: LcaPaged8, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
+                         rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
+    """Run lca_decode_update_paged8 (q_tail_* [B, n, H, d], exactly the n latest positions, n = n_summary_q or group_size, or the
+    ready summary query qbar [B, Hkv, dk]); returns (n_rep_new [B], rep_sem [B, Hkv, d_sem], rep_pos [B, Hkv, d_pos], anchor [B, Hkv])."""
+    return _decode_update_paged(_lib.lca_decode_update_paged8, "lca_decode_update_paged8", params, cache, q_tail_sem, q_tail_pos, n_rep, n_tok,
+                                n_rep_new, rep_sem, rep_pos, qbar, anchor, ws, stream)
+
+
+def paged4_cache(pages_sem, pages_pos, shift_sem, shift_pos, exp_sem, exp_pos, block_table) -> LcaPaged4:
+    """Descriptor of a paged 4-bit cache over the caller's tensors: pages [n_pages, Hkv, page_size, d / 2], shifts [n_pages, Hkv,
+    page_size, d / 64] and exponents [n_pages, Hkv, page_size] (exp_pos None for MLA), all of one byte per element, block_table
+    [batch, table_width] int32 (None for calls that do not use it), all on one device."""
+    if pages_sem is None or pages_pos is None or pages_sem.dim() != 4 or pages_pos.shape[:3] != pages_sem.shape[:3]:
+        raise ValueError("both pools have the same pages: [n_pages, Hkv, page_size, d / 2]")
+    tensors = (pages_sem, pages_pos, shift_sem, shift_pos, exp_sem, exp_pos, block_table)
+    n_pages, Hkv, page_size = pages_sem.shape[:3]
+    for t, pool in ((shift_sem, pages_sem), (shift_pos, pages_pos)):
+        if t is None or t.shape != pool.shape[:3] + (pool.shape[3] // 32,):
+            raise ValueError("half a byte for each 32 columns of a row: shifts [n_pages, Hkv, page_size, d / 64]")
+    if exp_sem is None or any(t is not None and t.shape != pages_sem.shape[:3] for t in (exp_sem, exp_pos)):
+        raise ValueError("an exponent for each row and KV head: [n_pages, Hkv, page_size]")
+    if any(t is not None and t.element_size() != 1 for t in tensors[:6]):
+        raise ValueError("pages, shifts and exponents hold one byte per element")
+    if block_table is not None and (block_table.dim() != 2 or block_table.dtype is not torch.int32):
+        raise ValueError("block_table is [batch, table_width] int32")
+    if len({t.device for t in tensors if t is not None}) > 1:
+        raise ValueError("the pages, scales and tables of a cache are on one device")
+    width = 0 if block_table is None else block_table.shape[1]
+    c = LcaPaged4(*(_ptr(t) for t in tensors), n_pages, page_size, width)
+    c.tensors = tensors
+    c.device = pages_sem.get_device()
+    c.batch = None if block_table is None else block_table.shape[0]
+    c.layout = (Hkv, 2 * pages_sem.shape[3], 2 * pages_pos.shape[3])
+    c.pages = LcaPaged8(None, None, None, None, _ptr(block_table), n_pages, page_size, width)
+    return c
+
+
+def new_paged4_cache(params: LcaParams, n_pages: int, page_size: int, table_width: int, device) -> LcaPaged4:
+    """Allocate a pool of pages and empty block tables for params.batch sequences."""
+    row = (n_pages, params.n_kv_heads, page_size)
+    new = lambda *d: torch.zeros(row + d, dtype=torch.uint8, device=device)  # noqa: E731
+    return paged4_cache(new(params.d_sem // 2), new(params.d_pos // 2), new(params.d_sem // 64), new(params.d_pos // 64), new(),
+                        new() if params.variant == LCA_VARIANT_GQA else None,
+                        torch.full((params.batch, table_width), -1, dtype=torch.int32, device=device))
+
+
+def paged4_write(params: LcaParams, cache: LcaPaged4, rows_sem, rows_pos, slot_map, stream=None):
+    """Quantise rows into the slots that slot_map names (in place)."""
+    dev, at, (Hkv, d_sem, d_pos) = _paged_device(params, cache, stream, table=False)
+    n = slot_map.numel()
+    _check(_lib.lca_paged4_write(params, cache, _arg(rows_sem, _BF16, n * Hkv * d_sem, dev),
+                                 _arg(rows_pos, _BF16, n * Hkv * d_pos, dev), _arg(slot_map, _I32, n, dev), n, at), "lca_paged4_write")
+
+
+def paged4_read(params: LcaParams, cache: LcaPaged4, slot_map, rows_sem=None, rows_pos=None, stream=None):
+    """The values of the rows that slot_map names: (rows_sem [n, Hkv, d_sem], rows_pos [n, Hkv, d_pos]) bf16.  Rows of a slot
+    outside the pool are left as they are, zero where this call makes the tensor."""
+    dev, at, (Hkv, d_sem, d_pos) = _paged_device(params, cache, stream, table=False)
+    n = slot_map.numel()
+    if rows_sem is None:
+        rows_sem = _new(torch.zeros, (n, Hkv, d_sem), _BF16, slot_map.device, stream)
+    if rows_pos is None:
+        rows_pos = _new(torch.zeros, (n, Hkv, d_pos), _BF16, slot_map.device, stream)
+    _check(_lib.lca_paged4_read(params, cache, _arg(rows_sem, _BF16, n * Hkv * d_sem, dev), _arg(rows_pos, _BF16, n * Hkv * d_pos, dev),
+                                _arg(slot_map, _I32, n, dev), n, at), "lca_paged4_read")
+    return rows_sem, rows_pos
+
+
+def workspace_paged4(params: LcaParams, cache: LcaPaged4, q_len: int, device) -> torch.Tensor:
+    return torch.empty(max(lca_paged4_workspace_bytes(params, cache, q_len), 16), dtype=torch.uint8, device=device)
+
+
+def decode_attention_paged4(params: LcaParams, cache: LcaPaged4, q_sem, q_pos, n_rep, n_tok, out=None, lse=None,
+                            want_lse: bool = False, ws=None, stream=None):
+    """Attention of q_pos.shape[1] new tokens per sequence (q_pos [B, q_len, H, d_pos]) over the paged cache."""
+    return _decode_attention_paged(_lib.lca_decode_attention_paged4, lca_paged4_workspace_bytes, "lca_decode_attention_paged4", params, cache,
+                                   q_sem, q_pos, n_rep, n_tok, out, lse, want_lse, ws, stream)
+
+
+def decode_update_paged4(params: LcaParams, cache: LcaPaged4, q_tail_sem, q_tail_pos, n_rep, n_tok, n_rep_new=None, rep_sem=None,
+                         rep_pos=None, qbar: Optional[torch.Tensor] = None, anchor=None, ws=None, stream=None):
+    """Run lca_decode_update_paged4; arguments and results as for decode_update_paged8."""
+    return _decode_update_paged(_lib.lca_decode_update_paged4, "lca_decode_update_paged4", params, cache, q_tail_sem, q_tail_pos, n_rep, n_tok,
+                                n_rep_new, rep_sem, rep_pos, qbar, anchor, ws, stream)
+
+
+# ------------------------------------------------------------------------------------------- around a speculative step
+def _device(device, where: str):
+    """Index of the CUDA device of a tensor, which has to be the current one."""
+    dev = device.index
+    if device.type != "cuda" or dev != torch.cuda.current_device():
+        raise ValueError(f"{where} takes tensors on the current CUDA device, not on {device}")
+    return dev
+
+
+def _raw_stream(dev, stream):
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, kind: int = ROPE_PLAIN, scale: float = 1.0, trained_len: float = 0.0,
+                     fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """(freqs [rot_dim / 2] float64 on `device`, factor): the frequencies of lca_rope_frequencies, which `rope` takes."""
+    f, factor = (C.c_double * max(int(rot_dim) // 2, 1))(), C.c_float()
+    _check(lca_rope_frequencies(kind, rot_dim, base, scale, trained_len, fast, slow, f, factor), "lca_rope_frequencies")
+    return torch.tensor(list(f), dtype=torch.float64, device=device), factor.value
+
+
+_ROPE_TYPES = {torch.bfloat16: LCA_DTYPE_BF16, torch.float32: LCA_DTYPE_FP32}
+
+
+def rope(q, k, positions, freqs, interleaved: bool = False, inverse: bool = False, factor: float = 1.0, q_out=None, k_out=None, stream=None):
+    """Rotate q [T, heads, d] and k [T, kv_heads, d] (either may be None) by the angles positions [T] int32 times freqs [rot / 2]
+    float64: columns 0 .. rot - 1 of every head, the others are copied.  The tensors may be views (slices of a projection) as long
+    as the columns of a head lie side by side; q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("rope takes queries, keys or both")
+    T, _, d = x.shape
+    dev = _device(x.device, "rope")
+    code = _ROPE_TYPES.get(x.dtype)
+    if code is None:
+        raise ValueError(f"rope takes bfloat16 or float32, not {x.dtype}")
+    rot = 2 * freqs.numel()
+    a = LcaRopeArgs(code, bool(interleaved), bool(inverse), 0, 0, d, rot, factor, T, _arg(positions, _I32, T, dev),
+                    _arg(freqs, torch.float64, 1, dev))
+    outs = []
+    for t, o in ((q, q_out), (k, k_out)):
+        if t is None:
+            outs.append(None)
+            continue
+        if o is None:
+            o = _new(torch.empty, tuple(t.shape), t.dtype, t.device, stream)
+        for v in (t, o):
+            if v.dtype is not x.dtype or v.get_device() != dev or v.dim() != 3 or v.shape[0] != T or v.shape[2] != d or (v.stride(2) != 1 and d > 1):
+                raise ValueError(f"expected [T, heads, {d}] of {x.dtype} on cuda:{dev} with neighbouring columns, T = {T}, not "
+                                 f"{v.dtype} {list(v.shape)} with strides {list(v.stride())} on {v.device}")
+        if o.shape[1] != t.shape[1] or (o.stride(0) == 0 and T > 1) or (o.stride(1) == 0 and o.shape[1] > 1):
+            raise ValueError("an output has the heads of its input, each at a place of its own")
+        outs.append(o)
+    if q is not None:
+        a.n_q_heads, a.q, a.q_token_stride, a.q_head_stride = q.shape[1], q.data_ptr(), q.stride(0), q.stride(1)
+        a.q_out, a.q_out_token_stride, a.q_out_head_stride = outs[0].data_ptr(), outs[0].stride(0), outs[0].stride(1)
+    if k is not None:
+        a.n_k_heads, a.k, a.k_token_stride, a.k_head_stride = k.shape[1], k.data_ptr(), k.stride(0), k.stride(1)
+        a.k_out, a.k_out_token_stride, a.k_out_head_stride = outs[1].data_ptr(), outs[1].stride(0), outs[1].stride(1)
+    if T > 0:
+        _check(_lib.lca_rope(a, _raw_stream(dev, stream)), "lca_rope")
+    return outs[0], outs[1]
+
+
+def verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, n_draft=None, n_tok=None, accepted=None, out=None,
+                  n_tok_out=None, stream=None):
+    """Run lca_verify_drafts on target_probs [B, n + 1, V], draft_probs [B, n, V] (None: a drafter that is certain) of float32 or
+    bfloat16, draft_tokens [B, n] int32, u_accept [B, n] and u_sample [B] float32.  Returns (accepted [B], tokens [B, n + 1],
+    n_tok_out [B] or None) int32."""
+    B, n1, V = target_probs.shape
+    n = n1 - 1
+    dev = _device(target_probs.device, "verify_drafts")
+    dt = target_probs.dtype
+    code = _ROPE_TYPES.get(dt)
+    if code is None:
+        raise ValueError(f"probabilities are float32 or bfloat16, not {dt}")
+    if draft_probs is not None and draft_probs.shape != (B, n, V):
+        raise ValueError(f"draft_probs is {[B, n, V]}, not {list(draft_probs.shape)}")
+    if accepted is None:
+        accepted = _new(torch.empty, (B,), _I32, target_probs.device, stream)
+    if out is None:
+        out = _new(torch.empty, (B, n1), _I32, target_probs.device, stream)
+    if n_tok is not None and n_tok_out is None:
+        n_tok_out = _new(torch.empty, (B,), _I32, target_probs.device, stream)
+    if n_tok is None:
+        n_tok_out = None
+    a = LcaVerifyArgs(code, B, n, V, _arg(target_probs, dt, B * n1 * V, dev), _arg(draft_probs, dt, B * n * V, dev),
+                      _arg(draft_tokens, _I32, B * n, dev), _arg(n_draft, _I32, B, dev), _arg(u_accept, _F32, B * n, dev),
+                      _arg(u_sample, _F32, B, dev), _arg(n_tok, _I32, B, dev), _arg(accepted, _I32, B, dev), _arg(out, _I32, B * n1, dev),
+                      _arg(n_tok_out, _I32, B, dev))
+    _check(_lib.lca_verify_drafts(a, _raw_stream(dev, stream)), "lca_verify_drafts")
+    return accepted, out, n_tok_out

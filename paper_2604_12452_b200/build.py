@@ -26,6 +26,10 @@ SOURCES = {
     "paged8.cu": [],              # scales, codes and anchors are compared exactly
     "attn_paged8.cu": [],         # these two name their approximate instructions themselves
     "attn_paged8_pair.cu": [],
+    "paged4.cu": [],
+    "attn_paged4.cu": [],
+    "rope.cu": [],                # angles in 64 bits, accurate sines
+    "verify.cu": [],              # 64-bit sums decide the tokens
 }
 
 

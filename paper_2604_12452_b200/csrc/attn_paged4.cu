@@ -1,0 +1,819 @@
+// Decode attention over the paged 4-bit cache (Sec. 4.3 over the layout of lca_paged4).
+//
+// Mathematics.  For a query row h and the present rows i of its sequence and KV head
+//     y_i = log2(e) (scale * f_k(i) * sum_c q_c k_ic + bias_i),   out = sum_i 2^y_i f_v(i) v_i / sum_i 2^y_i
+// where k, v are the cached rows expanded to e4m3 codes (exactly: fp4_common.cuh) and f one power of two for each row and KV head.
+// Queries and weights are sums of two e4m3 terms, as in attn_paged8.cu, which derives their errors: a query element is off by at
+// most 2^-17 of its row's largest, a weight t_i = 2^(y_i + log2 f_v(i) - M + 5) by 2^-9 of itself or by a step of 2^-18 of the largest,
+// the step rounded with an offset of the key's own.  M is the running maximum of y + log2 f_v over a split, raised when a weight
+// would exceed 2^8.75; the row sum adds the weights without f_v in fp32, unrounded.
+//
+// Transposed products, the key tile as the 128-row operand: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T, O^T [d x 2 NH] += V^T [T_hi | T_lo]^T.
+//   softmax    GROUPS groups of four warps, each for ROWS of the query rows: thread = key = TMEM lane; epilogue: thread = output column
+//   expansion  EW warps: packed rows from HBM straight to registers, DEPTH tiles ahead, to e4m3 in the operands' swizzled images
+//   + 1 warp   MMA issue and TMEM
+// The packed rows never pass through shared memory (half a byte in and out of it per value, of the 128 bytes a clock that the tensor
+// core's operands take too).  Tiles flow through the pieces of a CTA without a pause: the expansion warps run ahead of the
+// piece that the softmax warps are at.  There are two buffers of weights, so that a tile's softmax only waits for O of the tile before
+// the last one, unless it has to raise a maximum.
+// Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
+#include <cstring>
+
+#include "attn_paged8.cuh"
+#include "fp4_common.cuh"
+
+namespace lca {
+using namespace tc;
+
+static __device__ int g_paged4_status = 0;
+
+struct Paged4Params {
+  Paged8Params b;             // without the tensor maps and the scales
+  const uint8_t* sem; const uint8_t* pos;
+  const uint8_t* shift_sem; const uint8_t* shift_pos;
+  const uint8_t* exp_k; const uint8_t* exp_v;
+};
+
+// --------------------------------------------------------------------------------------------------- scalar kernel
+// One warp per query row, keys one by one, fp32: the cross-check of the tensor-core kernel (lca_set_attention_impl(1)).
+template <int D_SEM, int D_POS, bool MLA>
+__global__ void __launch_bounds__(128) attn_paged4_simt_kernel(const __grid_constant__ Paged4Params q, float scale, float bias, long long n_rows) {
+  constexpr int PS = D_SEM / 64, PP = D_POS / 64;            // element pairs per lane: 2 lane + 64 i
+  __shared__ uint2 s_table[16];
+  const Paged8Params& p = q.b;
+  const int lane = threadIdx.x & 31;
+  paged4_table_load(s_table, threadIdx.x);
+  __syncthreads();
+  const long long row = (long long)blockIdx.x * 4 + (threadIdx.x >> 5);
+  if (row >= n_rows) return;
+  const int h = (int)(row % p.Hq), t = (int)((row / p.Hq) % p.q_len), b = (int)(row / ((long long)p.Hq * p.q_len));
+  const int hk = h / p.rep;
+  float2 qs[PS], qp[PP], acc[PS];
+#pragma unroll
+  for (int i = 0; i < PS; ++i) {
+    acc[i] = make_float2(0.f, 0.f);
+    if (MLA) qs[i] = __bfloat1622float2(reinterpret_cast<const bf162*>(p.q_sem + (size_t)row * D_SEM)[lane + 32 * i]);
+  }
+#pragma unroll
+  for (int i = 0; i < PP; ++i) qp[i] = __bfloat1622float2(reinterpret_cast<const bf162*>(p.q_pos + (size_t)row * D_POS)[lane + 32 * i]);
+  // columns 2 lane, 2 lane + 1 of the 64 from 64 i on: in word 8 i + lane / 4, block 2 i + lane / 16
+  auto pair = [&](const uint8_t* codes, const uint8_t* shifts, int i) {
+    const uint32_t w = reinterpret_cast<const uint32_t*>(codes)[8 * i + (lane >> 2)];
+    const uint2 c = paged4_expand(w, s_table[(shifts[i] >> ((lane >> 4) * 4)) & 15]);
+    const float4 f = e4m3x4_to_float4(((lane & 2) ? c.y : c.x) >> ((lane & 1) * 16));
+    return make_float2(f.x, f.y);
+  };
+  const PagedSpan sp = paged_span(p.n_rep, p.n_tok, b, p.g, p.width * p.page);
+  const int last = sp.n_tok - p.q_len + 1 + t;               // rows below it are seen
+  float mx = -INFINITY, l = 0.f;
+  bool any = false;
+  for (int x = 0; x < last; ++x) {
+    if (x == sp.n_rep && x < sp.tok0) x = sp.tok0;
+    if (x >= last) break;
+    const int pg = p.table[(size_t)b * p.width + x / p.page];
+    if (pg < 0 || pg >= p.n_pages) continue;
+    const size_t r = ((size_t)pg * p.Hkv + hk) * p.page + x % p.page;
+    const float fv = paged4_factor(q.exp_v[r]), fk = paged4_factor(q.exp_k[r]);
+    float2 v[PS];
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+      v[i] = pair(q.sem + r * (D_SEM / 2), q.shift_sem + r * (D_SEM / 64), i);
+      if (MLA) s += qs[i].x * v[i].x + qs[i].y * v[i].y;
+    }
+#pragma unroll
+    for (int i = 0; i < PP; ++i) {
+      const float2 k = pair(q.pos + r * (D_POS / 2), q.shift_pos + r * (D_POS / 64), i);
+      s += qp[i].x * k.x + qp[i].y * k.y;
+    }
+    s = warp_sum(s) * fk * scale + (x < sp.n_rep ? bias : 0.f);
+    any = true;
+    const float mn = fmaxf(mx, s), corr = expf(mx - mn), w = expf(s - mn);
+    l = l * corr + w;
+#pragma unroll
+    for (int i = 0; i < PS; ++i) {
+      acc[i].x = acc[i].x * corr + w * (v[i].x * fv);
+      acc[i].y = acc[i].y * corr + w * (v[i].y * fv);
+    }
+    mx = mn;
+  }
+  const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+  for (int i = 0; i < PS; ++i)
+    reinterpret_cast<bf162*>(p.out + (size_t)row * D_SEM)[lane + 32 * i] = __floats2bfloat162_rn(acc[i].x * inv, acc[i].y * inv);
+  if (p.lse && lane == 0) p.lse[row] = any ? mx + logf(l) : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------- tensor-core kernel
+template <bool MLA_, int DS_, int DP_, int NH_, int GROUPS_, int ROWS_>
+struct Paged4Plan {
+  static constexpr bool MLA = MLA_;
+  static constexpr int DS = DS_, DP = DP_, NH = NH_, GROUPS = GROUPS_, ROWS = ROWS_;        // GROUPS * ROWS of the NH rows exist
+  static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
+  static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 columns)
+  static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
+  static constexpr int PER_TILE = MLA ? NK : NK + NV;        // slots of a tile; MLA: the latent chunks are keys and values
+  static constexpr int V0 = MLA ? 0 : NK;                    // the first of them with values
+  static constexpr int SLOT = 16384;
+  static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
+  static constexpr int P_BYTES = 128 * 2 * NH;               // per key the first terms of all rows, then the second ones
+  static constexpr int TM_S = 2 * NV * NH, TM_USED = TM_S + 4 * NH;
+  static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
+  static constexpr int CTAS = (MLA && DS == 512) || NH == 32 ? 1 : 2;        // per SM
+  static constexpr int EW = CTAS == 2 && GROUPS == 2 ? 4 : 8;                // expansion warps
+  static constexpr int SOFTMAX_WARPS = 4 * GROUPS, W_MMA = SOFTMAX_WARPS + EW, THREADS = 32 * (W_MMA + 1);
+  static constexpr int RPT = 16 / EW;                        // rows of a chunk that a thread expands, four threads a row of 128 columns
+  // 16-byte pieces of a tile that a thread expands: the latent (V) chunks row by row, then the pos chunk
+  static constexpr int UNITS_SEM = VW == 128 ? RPT : RPT / 2, UNITS_POS = DP == 128 ? RPT : RPT / 2, UNITS = NV * UNITS_SEM + UNITS_POS;
+  static constexpr int DEPTH = UNITS > 8 ? 1 : UNITS > 4 ? 1 : 2;              // tiles in registers
+  // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers first.
+  static constexpr int MISC_BYTES = 512 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH);
+  static constexpr int BUDGET = (CTAS == 1 ? 227 * 1024 : 113 * 1024) - 1024;      // 1 KB to align the base
+  static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / SLOT;
+  static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
+  static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
+  static constexpr int SMEM = OFF_MISC + MISC_BYTES + 1024;
+  static_assert(SLOTS >= 2 * PER_TILE && 8 * (2 * SLOTS + 7) <= 256 && SMEM <= 227 * 1024, "the tiles that S and O work on fit the ring");
+  static_assert(THREADS / 32 <= 26, "room for the sums of the ranges");
+};
+
+// one group of softmax warps (128 threads)
+__device__ __forceinline__ void group_sync(int grp) { asm volatile("bar.sync %0, 128;" ::"r"(grp + 1) : "memory"); }
+__device__ __forceinline__ bool group_or(int grp, bool v) {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((uint32_t)v), "r"(grp + 1) : "memory");
+  return r != 0;
+}
+// N consecutive 32-bit columns of this warp's lanes
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t at, uint32_t (&r)[N]) {
+  if constexpr (N == 4)
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+  else
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(at) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
+  if constexpr (N == 4)
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+  else
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+// 16 bytes that are read once
+__device__ __forceinline__ uint4 load_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+
+static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
+static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
+
+template <class PL>
+__global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
+  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS, W_EXP = PL::SOFTMAX_WARPS, W_MMA = PL::W_MMA;
+  const Paged8Params& p = a.b;
+  extern __shared__ unsigned char smem_dyn[];
+  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
+  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  const uint32_t bars = base + PL::OFF_MISC;
+  auto FULL = [&](int s) { return bars + 8 * s; };
+  auto EMPTY = [&](int s) { return bars + 8 * (PL::SLOTS + s); };
+  const uint32_t more_bars = bars + 8 * (2 * PL::SLOTS), QFULL = more_bars + 48;
+  auto SFULL = [&](uint32_t i) { return more_bars + 8 * i; };
+  auto PFULL = [&](uint32_t i) { return more_bars + 16 + 8 * i; };
+  auto PVDONE = [&](uint32_t i) { return more_bars + 32 + 8 * i; };
+  unsigned char* misc = base_ptr + PL::OFF_MISC;
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 256);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
+  int* s_b = reinterpret_cast<int*>(misc + 264);
+  long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
+  uint2* s_table = reinterpret_cast<uint2*>(misc + 512);
+  float* s_qs = reinterpret_cast<float*>(misc + 640);
+  float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
+  int* s_lim = reinterpret_cast<int*>(s_f + NH);
+  float* s_wmax = reinterpret_cast<float*>(s_lim + NH);      // also the sums of the four warps of a group
+  int* s_row = reinterpret_cast<int*>(s_wmax + 4 * NH);      // output row of each query row, of this piece and of the next one
+  long long* s_warp = reinterpret_cast<long long*>(base_ptr + PL::OFF_P);      // totals of the warps, and as many words; before the weights
+  const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x;
+
+  if (tid == 0) {
+    for (int s = 0; s < PL::SLOTS; ++s) { mbar_init(FULL(s), PL::EW); mbar_init(EMPTY(s), 1); }
+    for (int i = 0; i < 2; ++i) { mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); }
+    mbar_init(QFULL, 32 * PL::SOFTMAX_WARPS);
+    *abort_flag = 0;
+    fence_mbar_init();
+  }
+  if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
+  paged4_table_load(s_table, tid);
+  chain_wait();
+  chain_next();                                              // the whole grid is resident: nothing is displaced
+  paged8_range<PL::THREADS>(p, (int)blockIdx.x, s_warp, s_b, s_off);
+  __syncthreads();
+  if (PL::GROUPS * ROWS < NH) {                              // weights of rows that do not exist: 0
+    for (int i = tid; i < 2 * PL::P_BYTES / 16; i += PL::THREADS) reinterpret_cast<uint4*>(base_ptr + PL::OFF_P)[i] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
+    __syncthreads();
+  }
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  Walk w;
+  w.b = *s_b; w.off = s_off[0]; w.left = s_off[1]; w.fresh = true; w.n = 0;
+  auto fail = [&](int code) { atomicCAS(&g_paged4_status, 0, code); *abort_flag = 1; };
+
+  if (warp >= W_EXP && warp < W_MMA) {
+    // ----------------------------------------------------------------------------------------------- expansion
+    // Four threads take a row of a 128-wide chunk, rows r0 + STRIDE i; of a 64-wide one the first two take the even ones of these
+    // rows and the others the odd ones.
+    constexpr int RPT = PL::RPT, STRIDE = 128 / RPT, DEPTH = PL::DEPTH;
+    const int et = tid - 32 * W_EXP, r0 = et >> 2, u = et & 3;
+    const int mask = p.page - 1;
+    bool ok = true;
+    // the tile whose pages are looked up next
+    int j = 0;
+    bool more = w.next(p);
+    struct Tile { int page[RPT]; int hk; bool any; };        // page of each row, -1: no such row
+    auto look = [&](Tile& t) {
+      t.any = more;
+      if (!more) return;
+      t.hk = w.hk;
+      const int row0 = w.t.row0(w.t0 + j) + r0;
+#pragma unroll
+      for (int i = 0; i < RPT; ++i) {
+        const int x = row0 + STRIDE * i;
+        t.page[i] = w.t.s.has(x) ? p.table[(size_t)w.b * p.width + (x >> p.page_log2)] : -1;
+      }
+      if (++j == w.n) { j = 0; more = w.next(p); }
+    };
+    // rows of the pool, -1 where a row is absent
+    struct Rows { long long r[RPT]; bool any; };
+    auto rows_of = [&](const Tile& t, Rows& y) {
+      y.any = t.any;
+#pragma unroll
+      for (int i = 0; i < RPT; ++i)
+        y.r[i] = t.any && (unsigned)t.page[i] < (unsigned)p.n_pages
+                     ? (((long long)t.page[i] * p.Hkv + t.hk) << p.page_log2) + ((r0 + STRIDE * i) & mask) : -1;
+    };
+    struct Data { uint4 v[PL::UNITS]; uint32_t s[NV * PL::UNITS_SEM > 4 ? RPT : NV * PL::UNITS_SEM][2]; uint32_t sp[PL::UNITS_POS]; bool any; };
+    constexpr bool WIDE = DS == 512;                         // the shifts of a row are eight bytes: one load for its four chunks
+    auto load_sem = [&](const Rows& y, int c, Data& d) {
+      if constexpr (PL::VW == 128) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const bool in = y.r[i] >= 0;
+          d.v[c * RPT + i] = in ? load_stream(a.sem + (size_t)y.r[i] * (DS / 2) + c * 64 + u * 16) : make_uint4(0u, 0u, 0u, 0u);
+          if constexpr (WIDE) {
+            if (c == NV - 1) {                               // the last chunk of the tile before has been expanded
+              const uint2 s = in ? __ldg(reinterpret_cast<const uint2*>(a.shift_sem) + y.r[i]) : make_uint2(0u, 0u);
+              d.s[i][0] = s.x; d.s[i][1] = s.y;
+            }
+          } else {
+            d.s[c * RPT + i][0] = in ? (uint32_t)__ldg(a.shift_sem + (size_t)y.r[i] * (DS / 64) + c * 2 + (u >> 1)) >> (4 * (u & 1)) : 0u;
+          }
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < RPT / 2; ++i) {
+          const long long r = u < 2 ? y.r[2 * i] : y.r[2 * i + 1];
+          const bool in = r >= 0;
+          d.v[i] = in ? load_stream(a.sem + (size_t)r * 32 + (u & 1) * 16) : make_uint4(0u, 0u, 0u, 0u);
+          d.s[i][0] = in ? (uint32_t)__ldg(a.shift_sem + r) >> (4 * (u & 1)) : 0u;
+        }
+      }
+    };
+    auto load_pos = [&](const Rows& y, Data& d) {
+      constexpr int U0 = NV * PL::UNITS_SEM;
+      if constexpr (DP == 128) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const bool in = y.r[i] >= 0;
+          d.v[U0 + i] = in ? load_stream(a.pos + (size_t)y.r[i] * 64 + u * 16) : make_uint4(0u, 0u, 0u, 0u);
+          d.sp[i] = in ? (uint32_t)__ldg(a.shift_pos + (size_t)y.r[i] * 2 + (u >> 1)) >> (4 * (u & 1)) : 0u;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < RPT / 2; ++i) {
+          const long long r = u < 2 ? y.r[2 * i] : y.r[2 * i + 1];
+          const bool in = r >= 0;
+          d.v[U0 + i] = in ? load_stream(a.pos + (size_t)r * 32 + (u & 1) * 16) : make_uint4(0u, 0u, 0u, 0u);
+          d.sp[i] = in ? (uint32_t)__ldg(a.shift_pos + r) >> (4 * (u & 1)) : 0u;
+        }
+      }
+    };
+    int slot = 0;
+    uint32_t phase = 0;
+    auto begin_slot = [&]() {
+      if (ok && !mbar_wait(EMPTY(slot), phase ^ 1, abort_flag)) { fail(ERR_WAIT_KV_EMPTY); ok = false; }
+      ok = __all_sync(0xffffffffu, ok);
+    };
+    auto end_slot = [&]() {
+      fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(FULL(slot));
+      if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; }
+    };
+    auto store = [&](uint32_t off, const uint4& v, uint32_t shift) {         // 32 values of one row
+      const uint2 t = s_table[shift & 15];
+      const uint2 x0 = paged4_expand(v.x, t), x1 = paged4_expand(v.y, t), x2 = paged4_expand(v.z, t), x3 = paged4_expand(v.w, t);
+      unsigned char* q = base_ptr + slot * PL::SLOT;
+      *reinterpret_cast<uint4*>(q + off) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+      *reinterpret_cast<uint4*>(q + (off ^ 16u)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+    };
+    const uint32_t off128 = swz<128>(r0, 2 * u), off64 = swz<64>(r0 + (u < 2 ? 0 : STRIDE), 2 * (u & 1));
+    auto put_sem = [&](int c, const Data& d) {
+      if constexpr (PL::VW == 128) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+          const uint32_t s = WIDE ? (c < 2 ? d.s[i][0] : d.s[i][1]) >> (16 * (c & 1) + 4 * u) : d.s[WIDE ? 0 : c * RPT + i][0];
+          store(off128 + i * STRIDE * 128, d.v[c * RPT + i], s);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < RPT / 2; ++i) store(off64 + i * 2 * STRIDE * 64, d.v[i], d.s[i][0]);
+      }
+    };
+    auto put_pos = [&](const Data& d) {
+      constexpr int U0 = NV * PL::UNITS_SEM;
+      if constexpr (DP == 128) {
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) store(off128 + i * STRIDE * 128, d.v[U0 + i], d.sp[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < RPT / 2; ++i) store(off64 + i * 2 * STRIDE * 64, d.v[U0 + i], d.sp[i]);
+      }
+    };
+    // tiles t .. t + DEPTH - 1 in registers, pages of tile t + DEPTH on their way
+    Data d[DEPTH];
+    Tile ahead;
+    {
+      Rows y;
+#pragma unroll
+      for (int k = 0; k < DEPTH; ++k) {
+        look(ahead);
+        rows_of(ahead, y);
+        d[k].any = y.any;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) load_sem(y, c, d[k]);
+        load_pos(y, d[k]);
+      }
+    }
+    look(ahead);
+    while (ok && d[0].any) {
+#pragma unroll
+      for (int k = 0; k < DEPTH; ++k) {
+        if (!ok || !d[k].any) break;
+        Rows y;
+        rows_of(ahead, y);
+        look(ahead);
+        if constexpr (PL::MLA) {
+#pragma unroll
+          for (int c = 0; c < NV; ++c) {
+            begin_slot();
+            if (!ok) break;
+            put_sem(c, d[k]);
+            end_slot();
+            load_sem(y, c, d[k]);
+          }
+          if (!ok) break;
+          begin_slot();
+          if (!ok) break;
+          put_pos(d[k]);
+          end_slot();
+          load_pos(y, d[k]);
+        } else {
+          begin_slot();
+          if (!ok) break;
+          put_pos(d[k]);
+          end_slot();
+          load_pos(y, d[k]);
+          begin_slot();
+          if (!ok) break;
+          put_sem(0, d[k]);
+          end_slot();
+          load_sem(y, 0, d[k]);
+        }
+        d[k].any = y.any;
+      }
+    }
+  } else if (warp == W_MMA) {
+    // ----------------------------------------------------------------------------------------------------- MMA
+    const uint32_t leader = elect_one();
+    constexpr uint32_t ID_S = umma_idesc_f8(128, 2 * NH, 0, false, false);
+    constexpr uint32_t ID_O = umma_idesc_f8(128, 2 * NH, 0, true, true);
+    int s_slot = 0, v_slot = 0;                              // first slots of the tiles whose S and O come next
+    uint32_t s_phase = 0, v_phase = 0, g = 0, seg = 0;
+    bool ok = true;
+    auto wait_slot = [&](int first, uint32_t ph, int c) {    // chunk c of the tile whose slots begin at `first`
+      const int s = first + c >= PL::SLOTS ? first + c - PL::SLOTS : first + c;
+      ok = ok && mbar_wait(FULL(s), first + c >= PL::SLOTS ? ph ^ 1 : ph, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok && lane == 0) fail(ERR_WAIT_KV_FULL);
+      return s;
+    };
+    auto advance = [&](int& first, uint32_t& ph) { first += PL::PER_TILE; if (first >= PL::SLOTS) { first -= PL::SLOTS; ph ^= 1; } };
+    auto issue_s = [&](uint32_t buf) {
+      const uint32_t d = tmem + PL::TM_S + buf * 2 * NH;
+      uint32_t acc = 0;
+#pragma unroll
+      for (int c = 0; c < NK; ++c) {
+        const int s = wait_slot(s_slot, s_phase, c);
+        if (!ok) return;
+        tc_fence_after();
+        const int width = c < PL::KSEM ? 128 : DP;
+        const uint64_t ad = desc_rows(base + s * PL::SLOT, width, 16);
+        const uint64_t bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
+#pragma unroll
+        for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
+        if (!PL::MLA || c == PL::KSEM) umma_commit_elected(leader, EMPTY(s));
+      }
+      advance(s_slot, s_phase);
+      umma_commit_elected(leader, SFULL(buf));
+    };
+    while (ok && w.next(p)) {
+      ok = mbar_wait(QFULL, seg & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { if (lane == 0) fail(ERR_WAIT_Q); break; }
+      ++seg;
+      tc_fence_after();
+      issue_s(g & 1);
+      for (int j = 0; j < w.n && ok; ++j, ++g) {
+        if (j + 1 < w.n) issue_s((g + 1) & 1);
+        if (!ok) break;
+        ok = mbar_wait(PFULL(g & 1), (g >> 1) & 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) { if (lane == 0) fail(ERR_WAIT_P_FULL); break; }
+        tc_fence_after();
+        const uint64_t pd = desc_rows(base + PL::OFF_P + (g & 1) * PL::P_BYTES, 2 * NH, 128);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          const int s = wait_slot(v_slot, v_phase, PL::V0 + c);
+          if (!ok) break;
+          tc_fence_after();
+          // 64-wide values: M stays 128, the second half of the operand is the unused half of the slot and the output
+          // lanes it feeds are never read
+          const uint64_t ad = desc_rows(base + s * PL::SLOT, PL::VW, 8192);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (j > 0 || k > 0) ? 1u : 0u);
+          umma_commit_elected(leader, EMPTY(s));
+        }
+        if (!ok) break;
+        advance(v_slot, v_phase);
+        umma_commit_elected(leader, PVDONE(g & 1));
+      }
+    }
+  } else {
+    // ------------------------------------------------------------------------------------- softmax, epilogue
+    const int grp = warp >> 2, quad = warp & 3, t = tid & 127, hb = ROWS * grp;    // this thread: key t of a tile, rows hb .. hb + ROWS - 1
+    const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
+    uint32_t g = 0, seg = 0;
+    bool ok = true;
+    float l[ROWS];
+    int pg0 = -1, pg1 = -1;                                  // page of this thread's key in the current tile and in the next one
+    int ke = 0, ve = 0;                                      // exponents of pg0's row
+    auto page_of = [&](const Walk& u, int j) {               // -1: none
+      if (j >= u.n) return -1;
+      const int x = u.t.row0(u.t0 + j) + t;
+      if (!u.t.s.has(x)) return -1;                          // has() implies x below the table's end
+      const int pg = p.table[(size_t)u.b * p.width + (x >> p.page_log2)];
+      return pg >= 0 && pg < p.n_pages ? pg : -1;
+    };
+    auto exps_of = [&](int pg, int hk, int& k, int& v) {
+      k = v = 0;
+      if (pg < 0) return;
+      const size_t r = (((size_t)pg * p.Hkv + hk) << p.page_log2) + (t & (p.page - 1));
+      v = a.exp_v[r];
+      k = PL::MLA ? v : a.exp_k[r];
+    };
+    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them; the first lookups of the
+    // piece run underneath
+    auto load_q = [&](const Walk& u, uint32_t which) {
+      pg0 = page_of(u, 0); pg1 = page_of(u, 1);
+      constexpr int VS = PL::KSEM * 16, VQ = VS + DP / 8, NL = (VQ + 31) / 32;   // 8-element vectors of a row
+      const int n_rows = p.q_len * p.rep - u.blk * NH;
+#pragma unroll 2
+      for (int r = hb + quad; r < hb + ROWS; r += 4) {
+        const int gr = u.blk * NH + r, qt = gr / p.rep;
+        const int row = ((int)(u.b * p.q_len) + qt) * p.Hq + u.hk * p.rep + (gr - qt * p.rep);
+        uint4 v[NL];
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int c = lane + 32 * i;
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < n_rows && c < VQ)
+            v[i] = *reinterpret_cast<const uint4*>(c < VS ? p.q_sem + (size_t)row * DS + 8 * c : p.q_pos + (size_t)row * DP + 8 * (c - VS));
+        }
+#pragma unroll
+        for (int i = 0; i < NL; ++i) top = max(top, max_abs_bf16(v[i]));
+        top = __reduce_max_sync(0xffffffffu, top);
+        const int e = query_exponent(top);
+        const float f = exp2_int(e);
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int c = lane + 32 * i;
+          if (c >= VQ) continue;
+          uint32_t hi[2], lo[2];
+          split_e4m3(v[i], f, hi, lo);
+          const bool sem = c < VS;
+          const int chunk = sem ? c / 16 : PL::KSEM, u16 = (sem ? c % 16 : c - VS) / 2, half = c & 1;
+          unsigned char* q = base_ptr + PL::OFF_Q + chunk * 2 * NH * 128 + 8 * half;
+          const uint32_t oh = sem ? swz<128>(r, u16) : swz<DP>(r, u16), ol = sem ? swz<128>(NH + r, u16) : swz<DP>(NH + r, u16);
+          *reinterpret_cast<uint2*>(q + oh) = make_uint2(hi[0], hi[1]);
+          *reinterpret_cast<uint2*>(q + ol) = make_uint2(lo[0], lo[1]);
+        }
+        // a row with an infinity or a NaN has no finite logit; rows behind the last one never have weight
+        if (lane == 0) {
+          s_qs[r] = r < n_rows ? (top >= 0x7f80u ? __int_as_float(0x7fffffff) : exp2_int(-e)) : 0.f;
+          s_m[r] = r < n_rows ? 0.f : 3.0e38f;
+          s_lim[r] = u.t.s.n_tok - p.q_len + 1 + qt;
+          s_row[(which & 1) * NH + r] = r < n_rows ? row : -1;
+        }
+      }
+      exps_of(pg0, u.hk, ke, ve);
+      fence_proxy_async_smem();
+      mbar_arrive(QFULL);
+      group_sync(grp);
+    };
+    bool more = w.next(p);
+    if (more) load_q(w, 0);
+    while (more) {
+      const PagedSpan sp = w.t.s;
+      const int* rows = s_row + (seg & 1) * NH + hb;
+      bool unset = t < ROWS && rows[t % ROWS] >= 0;          // thread h of the group: its row has no maximum yet
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) l[i] = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < w.n; ++j, ++g) {
+        const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
+        const uint32_t buf = g & 1;
+        const bool valid = pg0 >= 0;
+        // the next tile's exponents and the page after that are on their way while this tile is worked on
+        int ke1, ve1;
+        exps_of(pg1, w.hk, ke1, ve1);
+        const int pg2 = page_of(w, j + 2);
+        // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 f_v + T): both are multiples of e = 2^(y - M + half), half way
+        // between them, so that neither is lost below 2^-126 where the factors of a sequence span more than fp32 does.
+        const float half = 0.5f * ((float)paged4_log2_factor(ve) + paged8_t_bits(NH)), f_t = ex2(half), f_l = ex2(paged8_t_bits(NH) - half);
+        const float kf = paged4_factor(ke) * p.scale_log2, cb = half + (x < sp.n_rep ? p.bias_log2 : 0.f);
+        const float offset = weight_offset(x);
+        const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
+
+        ok = mbar_wait(SFULL(buf), (g >> 1) & 1, abort_flag);
+        if (!ok) fail(ERR_WAIT_S_FULL);
+        __syncwarp();
+        tc_fence_after();
+        float z[ROWS];
+        float zmax = -INFINITY;
+        {
+          uint32_t hi[ROWS], lo[ROWS];
+          const uint32_t at = tmem + lane_base + PL::TM_S + buf * 2 * NH + hb;
+          tmem_ld<ROWS>(at, hi);
+          tmem_ld<ROWS>(at + NH, lo);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < ROWS; i += 4) {
+            const float4 q4 = *reinterpret_cast<const float4*>(s_qs + hb + i), m4 = *reinterpret_cast<const float4*>(s_m + hb + i);
+            const float qq[4] = {q4.x, q4.y, q4.z, q4.w}, mm[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+              z[i + k] = fmaf(__uint_as_float(hi[i + k]) + __uint_as_float(lo[i + k]), kf * qq[k], cb - mm[k]);
+          }
+        }
+        if (limited || !__all_sync(0xffffffffu, valid)) {
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) z[i] = valid && (!limited || x < s_lim[hb + i]) ? z[i] : -INFINITY;
+        }
+#pragma unroll
+        for (int i = 0; i < ROWS; i += 2) zmax = max3(zmax, z[i], z[i + 1]);
+        const bool raise = group_or(grp, zmax + half > T4_MAX || unset);
+        if (raise) {
+          // raise the maxima: per row the largest log2 t of the tile
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) {
+            const float m = warp_max_f32(z[i] + half);
+            if (lane == i) s_wmax[quad * NH + hb + i] = m;
+          }
+          group_sync(grp);
+          if (t < ROWS) {
+            const int h = hb + t;
+            const float m = fmaxf(fmaxf(s_wmax[h], s_wmax[NH + h]), fmaxf(s_wmax[2 * NH + h], s_wmax[3 * NH + h]));
+            float d = 0.f, f = 1.f;
+            if (unset ? m > -INFINITY : m > paged8_t_bits(NH)) {
+              d = m - paged8_t_bits(NH);
+              f = unset ? 1.f : ex2(-d);                     // nothing has been added under an unset maximum
+              s_m[h] += d;
+              unset = false;
+            }
+            s_d[h] = d; s_f[h] = f;
+          }
+          group_sync(grp);
+#pragma unroll
+          for (int i = 0; i < ROWS; ++i) { z[i] -= s_d[hb + i]; l[i] *= s_f[hb + i]; }
+        }
+        if (g > 1) {                                         // the weights of the tile before the last one have been read
+          ok = mbar_wait(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
+          if (!ok) fail(ERR_WAIT_O_DONE);
+        }
+        if (raise && j > 0) {                                // O is complete up to the last tile
+          ok = mbar_wait(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
+          if (!ok) fail(ERR_WAIT_O_DONE);
+          __syncwarp();
+          tc_fence_after();
+#pragma unroll 1
+          for (int c = 0; c < 2 * NV; ++c) {
+            uint32_t o[ROWS];
+            tmem_ld<ROWS>(tmem + lane_base + c * NH + hb, o);
+            tmem_wait_ld();
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * s_f[hb + k]);
+            tmem_st<ROWS>(tmem + lane_base + c * NH + hb, o);
+          }
+          tmem_wait_st();
+        }
+        {
+          unsigned char* ph = base_ptr + PL::OFF_P + buf * PL::P_BYTES;
+          uint32_t wh[ROWS / 4], wl[ROWS / 4];
+#pragma unroll
+          for (int i = 0; i < ROWS / 4; ++i) {
+            float tt[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              const float e = ex2(z[4 * i + k]);
+              tt[k] = e * f_t;
+              l[4 * i + k] = fmaf(e, f_l, l[4 * i + k]);
+            }
+            wh[i] = e4m3x4_from_float(tt[0], tt[1], tt[2], tt[3]);
+            const float4 h = e4m3x4_to_float4(wh[i]);        // what the first term leaves is exact: at most 2^4, times the gain 2^8
+            wl[i] = e4m3x4_from_float(fmaf(tt[0] - h.x, LO4_GAIN, offset), fmaf(tt[1] - h.y, LO4_GAIN, offset),
+                                      fmaf(tt[2] - h.z, LO4_GAIN, offset), fmaf(tt[3] - h.w, LO4_GAIN, offset));
+          }
+          const uint32_t oh = swz<2 * NH>(t, hb / 16) + hb % 16, ol = swz<2 * NH>(t, (NH + hb) / 16) + hb % 16;
+          if constexpr (ROWS == 8) {
+            *reinterpret_cast<uint2*>(ph + oh) = make_uint2(wh[0], wh[1]);
+            *reinterpret_cast<uint2*>(ph + ol) = make_uint2(wl[0], wl[1]);
+          } else {
+            *reinterpret_cast<uint32_t*>(ph + oh) = wh[0];
+            *reinterpret_cast<uint32_t*>(ph + ol) = wl[0];
+          }
+        }
+        fence_proxy_async_smem();
+        tc_fence_before();
+        mbar_arrive(PFULL(buf));
+        pg0 = pg1; pg1 = pg2; ke = ke1; ve = ve1;
+      }
+      // ---- this piece is done: its sums and maxima, then the next unit's queries (S of this piece is complete), then O
+      const bool whole = w.n == w.t.n;
+      const size_t part = (size_t)2 * blockIdx.x + (seg == 0 ? 0 : 1);
+#pragma unroll
+      for (int i = 0; i < ROWS; ++i) {
+        float v = l[i];
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+        if (lane == i) s_wmax[quad * NH + hb + i] = v;
+      }
+      group_sync(grp);
+      if (t < ROWS) {
+        const int h = hb + t;
+        const float sum = (s_wmax[h] + s_wmax[NH + h]) + (s_wmax[2 * NH + h] + s_wmax[3 * NH + h]);
+        if (!whole) {
+          float* ml = p.part + (size_t)2 * p.grid * NH * DS + part * 2 * NH;
+          ml[h] = unset ? -INFINITY : s_m[h]; ml[NH + h] = sum;
+        } else if (p.lse && rows[t] >= 0) {
+          p.lse[rows[t]] = sum == 0.f ? -INFINITY : (s_m[h] + log2f(sum) - paged8_t_bits(NH)) * 0.6931471805599453f;
+        }
+        s_f[h] = whole ? (sum == 0.f ? 0.f : 1.f / sum) : 1.f;
+      }
+      group_sync(grp);
+      more = w.next(p);
+      if (more) load_q(w, seg + 1);
+      ok = mbar_wait(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
+      if (!ok) fail(ERR_WAIT_O_DONE);
+      __syncwarp();
+      tc_fence_after();
+#pragma unroll 1
+      for (int c = 0; c < NV; ++c) {
+        uint32_t o[ROWS], o2[ROWS];
+        tmem_ld<ROWS>(tmem + lane_base + c * 2 * NH + hb, o);
+        tmem_ld<ROWS>(tmem + lane_base + c * 2 * NH + NH + hb, o2);
+        tmem_wait_ld();
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) o[k] = __float_as_uint(fmaf(__uint_as_float(o2[k]), 1.f / LO4_GAIN, __uint_as_float(o[k])));
+        const int d = c * 128 + t;
+        if (DS >= 128 || t < DS) {
+          if (whole) {
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+              const float f = s_f[hb + k];
+              const int row = rows[k];
+              if (row >= 0) p.out[(size_t)row * DS + d] = __float2bfloat16_rn(f == 0.f ? 0.f : __uint_as_float(o[k]) * f);   // no key: O may be 0 * NaN
+            }
+          } else {
+            float* dst = p.part + part * NH * DS + (size_t)hb * DS + d;
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) dst[(size_t)k * DS] = __uint_as_float(o[k]);
+          }
+        }
+      }
+      tc_fence_before();
+      ++seg;
+      group_sync(grp);                                       // s_f is written again by the next piece
+    }
+  }
+  __syncthreads();
+  if (warp == W_MMA) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
+}
+
+// ------------------------------------------------------------------------------------------------------------- host
+// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head, else blocks of 32.
+static int paged4_rows_per_tile(const lca_params* p, int q_len) {
+  return (long long)q_len * (p->n_q_heads / p->n_kv_heads) <= 16 ? 16 : 32;
+}
+// CTAs that share the work: all that are resident at once.
+static int paged4_grid(const lca_params* p, int nh) { return p->d_sem == 512 || nh == 32 ? 148 : 2 * 148; }
+size_t attn_paged4_workspace_bytes(const lca_params* p, int q_len) {
+  const int nh = paged4_rows_per_tile(p, q_len), grid = paged4_grid(p, nh);
+  return (size_t)2 * grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float) + ((size_t)p->batch + 2) * sizeof(long long) + 64;
+}
+
+template <class PL>
+static int paged4_launch(Paged4Params& P, cudaStream_t stream) {
+  auto kern = attn_paged4_kernel<PL>;
+  if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, PL::SMEM) != cudaSuccess) return LCA_ERR_CUDA;
+  const int st = launch_chained(kern, (unsigned)P.b.grid, PL::THREADS, PL::SMEM, stream, 1, P);
+  if (st != LCA_OK) return st;
+  return paged8_combine_launch<PL::DS, PL::NH>(P.b, stream);
+}
+template <bool MLA, int DS, int DP>
+static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
+  const long long rows = (long long)P.b.q_len * P.b.rep;
+  if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
+  if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
+  if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);
+  return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 2, 8>>(P, stream);
+}
+
+static void paged4_params(const Paged4Attn& q, Paged4Params& P) {
+  const lca_params* p = q.p;
+  const lca_paged4* c = q.c;
+  const bool mla = p->variant == LCA_VARIANT_MLA;
+  memset(&P, 0, sizeof(P));
+  P.sem = (const uint8_t*)c->pages_sem; P.pos = (const uint8_t*)c->pages_pos;
+  P.shift_sem = c->shift_sem; P.shift_pos = c->shift_pos;
+  P.exp_v = c->exp_sem; P.exp_k = mla ? c->exp_sem : c->exp_pos;
+  Paged8Params& b = P.b;
+  b.q_sem = (const bf16*)q.q_sem; b.q_pos = (const bf16*)q.q_pos; b.table = c->block_table;
+  b.n_rep = q.n_rep; b.n_tok = q.n_tok; b.out = (bf16*)q.out; b.lse = q.lse;
+  b.B = p->batch; b.Hq = p->n_q_heads; b.Hkv = p->n_kv_heads; b.q_len = q.q_len; b.g = q.n_rep ? p->group_size : 1;
+  b.page = c->page_size; b.page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
+  b.n_pages = c->n_pages; b.width = c->table_width; b.rep = b.Hq / b.Hkv;
+  b.scale_log2 = p->softmax_scale * 1.4426950408889634f; b.bias_log2 = p->rep_logit_bias * 1.4426950408889634f;
+}
+
+int attn_paged4_simt_launch(const Paged4Attn& q) {
+  const lca_params* p = q.p;
+  Paged4Params P;
+  paged4_params(q, P);
+  const long long n_rows = (long long)p->batch * q.q_len * p->n_q_heads;
+  const unsigned grid = (unsigned)((n_rows + 3) / 4);
+  const float scale = p->softmax_scale, bias = p->rep_logit_bias;
+  if (p->variant == LCA_VARIANT_MLA) {
+    if (p->d_sem == 512) attn_paged4_simt_kernel<512, 64, true><<<grid, 128, 0, q.stream>>>(P, scale, bias, n_rows);
+    else attn_paged4_simt_kernel<128, 64, true><<<grid, 128, 0, q.stream>>>(P, scale, bias, n_rows);
+  } else if (p->d_sem == 128) attn_paged4_simt_kernel<128, 128, false><<<grid, 128, 0, q.stream>>>(P, scale, bias, n_rows);
+  else attn_paged4_simt_kernel<64, 64, false><<<grid, 128, 0, q.stream>>>(P, scale, bias, n_rows);
+  note_launch();
+  return cudaGetLastError() == cudaSuccess ? LCA_OK : LCA_ERR_CUDA;
+}
+
+int attn_paged4_launch(const Paged4Attn& q) {
+  const lca_params* p = q.p;
+  Paged4Params P;
+  paged4_params(q, P);
+  Paged8Params& b = P.b;
+  const int nh = paged4_rows_per_tile(p, q.q_len);
+  b.n_blk = (int)(((long long)b.q_len * b.rep + nh - 1) / nh);
+  b.grid = paged4_grid(p, nh);
+  b.part = reinterpret_cast<float*>((reinterpret_cast<uintptr_t>(q.ws) + 31) & ~(uintptr_t)31);
+  const size_t part_bytes = (size_t)2 * b.grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float);
+  b.prefix = reinterpret_cast<long long*>(reinterpret_cast<char*>(b.part) + (part_bytes + 15) / 16 * 16);
+  if ((long long)b.B * b.Hkv * b.n_blk * ((long long)nh * p->d_sem / 512) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if (p->variant == LCA_VARIANT_MLA) return p->d_sem == 512 ? paged4_launch_rows<true, 512, 64>(P, nh, q.stream)
+                                                            : paged4_launch_rows<true, 128, 64>(P, nh, q.stream);
+  return p->d_sem == 128 ? paged4_launch_rows<false, 128, 128>(P, nh, q.stream) : paged4_launch_rows<false, 64, 64>(P, nh, q.stream);
+}
+
+int attn_paged4_take_status() {
+  int st = 0;
+  if (cudaMemcpyFromSymbol(&st, g_paged4_status, sizeof(int)) != cudaSuccess) return -1;
+  if (st != 0) {
+    int zero = 0;
+    cudaMemcpyToSymbol(g_paged4_status, &zero, sizeof(int));
+  }
+  return st;
+}
+
+}  // namespace lca

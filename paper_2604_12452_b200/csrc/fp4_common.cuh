@@ -1,0 +1,78 @@
+// The 4-bit format of the paged cache: value = code * 2^(exponent of its row - shift of its block of 32 columns).
+//
+// Codes have a sign and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6.  Eight fill a 32-bit word; value i has its magnitude's
+// index in bits 4 i .. 4 i + 2, so that a nibble without its top bit selects a byte of a table of eight (one byte permutation for
+// four values), and its sign in bit 8 i + 7 (i < 4) or 8 (i - 4) + 3, where the four of one permutation are the top bits of its
+// four bytes, as they stand or after one shift.  Seven instructions make eight e4m3 codes.
+//
+// A block is expanded to e4m3 relative to its row: code * 2^(6 - shift), from 2^-9 (shift 14) to 384, all of them e4m3 values.  So
+// the expansion is exact and what remains is one power of two per row, 2^(exponent - 6).
+#pragma once
+
+#include "fp8_common.cuh"
+
+namespace lca {
+
+static constexpr int PAGED4_MAX_SHIFT = 14, PAGED4_NAN_SHIFT = 15;
+static constexpr int PAGED4_MIN_EXP = PAGED8_MIN_EXP + 6;    // of a row of zeros: the factor of its expansion is then 2^PAGED8_MIN_EXP
+static constexpr int PAGED4_EXP_BIAS = 127;
+
+// log2 of the factor of an expanded row
+__host__ __device__ constexpr int paged4_log2_factor(int exp_byte) {
+  return (exp_byte > PAGED4_MIN_EXP + PAGED4_EXP_BIAS ? exp_byte : PAGED4_MIN_EXP + PAGED4_EXP_BIAS) - PAGED4_EXP_BIAS - 6;
+}
+__device__ __forceinline__ float paged4_factor(int exp_byte) { return exp2_int(paged4_log2_factor(exp_byte)); }
+
+// e4m3 code of magnitude m times 2^(6 - shift)
+constexpr uint32_t paged4_code(int m, int shift) {
+  if (shift > PAGED4_MAX_SHIFT) return 0x7f;                 // NaN
+  if (m == 0) return 0;
+  const int lead = m == 1 ? -1 : m / 2 - 1, half = m >= 2 ? m & 1 : 0;       // magnitude = 2^lead (1 + half / 2)
+  const int e = lead + 6 - shift;
+  if (e >= -6) return (uint32_t)((e + 7) << 3 | half << 2);
+  return (uint32_t)((2 + half) << (e + 9) >> 1);             // steps of 2^-9
+}
+struct Paged4Table {
+  uint2 v[16];
+  constexpr Paged4Table() : v() {
+    for (int s = 0; s < 16; ++s) {
+      v[s].x = paged4_code(0, s) | paged4_code(1, s) << 8 | paged4_code(2, s) << 16 | paged4_code(3, s) << 24;
+      v[s].y = paged4_code(4, s) | paged4_code(5, s) << 8 | paged4_code(6, s) << 16 | paged4_code(7, s) << 24;
+    }
+  }
+};
+static __constant__ const Paged4Table g_paged4_table{};
+
+// The table in shared memory (lanes read different entries); a barrier follows.
+__device__ __forceinline__ void paged4_table_load(uint2* s_table, int t) { if (t < 16) s_table[t] = g_paged4_table.v[t]; }
+
+// eight values as e4m3 codes, in order
+__device__ __forceinline__ uint2 paged4_expand(uint32_t w, const uint2& table) {
+  const uint32_t m = w & 0x77777777u;
+  return make_uint2(__byte_perm(table.x, table.y, m) | (w & 0x80808080u),
+                    __byte_perm(table.x, table.y, m >> 16) | ((w << 4) & 0x80808080u));
+}
+
+// Eight values to a word: nearest magnitude, ties to the even index; infinities become 6.
+__device__ __forceinline__ uint32_t paged4_pack(const float (&f)[8]) {
+  uint32_t w;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(w) : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
+  // nibble i: magnitude and, in its top bit, the sign of value i.  The signs go where the expansion wants them.
+  const uint32_t s = w & 0x88888888u;
+  uint32_t lo = s & 0xffffu, hi = s >> 16;
+  lo = (lo | lo << 8) & 0x00ff00ffu; lo = (lo | lo << 4) & 0x08080808u;
+  hi = (hi | hi << 8) & 0x00ff00ffu; hi = (hi | hi << 4) & 0x08080808u;
+  return (w & 0x77777777u) | lo << 4 | hi;
+}
+
+// log2 of the scale of a block whose largest finite |x| has these bf16 bits: smallest e with |x| <= 6 * 2^e; far below for 0
+__device__ __forceinline__ int paged4_block_exponent(uint32_t bits) {
+  const int E = (int)(bits >> 7), M = (int)(bits & 0x7f);
+  return E == 0 ? -1000 : E - 127 - 2 + (M > 64 ? 1 : 0);    // 6 = 1.5 * 2^2, 1.5 = 1 + 64 / 128
+}
+
+}  // namespace lca

@@ -1,5 +1,7 @@
 // C-ABI entry points of the LCA library: host-side validation and dispatch to the kernels.
+#include <algorithm>
 #include <atomic>
+#include <cmath>
 #include <vector>
 
 #include "lca_common.cuh"
@@ -75,6 +77,97 @@ static int run_attention(const AttnProblem& a) {
   }
   if (impl == 2) return LCA_ERR_UNSUPPORTED_SHAPE;
   return attn_simt_launch(a);
+}
+// Pages, tables and pools of the paged caches (lca_paged8, lca_paged4).
+template <class Cache>
+static int check_paged(const Cache* c) {
+  if (!c || c->n_pages <= 0) return LCA_ERR_INVALID_ARG;
+  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return LCA_ERR_UNSUPPORTED_SHAPE;
+  if ((int64_t)c->n_pages * c->page_size > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  return LCA_OK;
+}
+template <class Cache>
+static int check_paged_table(const lca_params* p, const Cache* c, bool reps) {
+  if (!c->block_table || c->table_width <= 0) return LCA_ERR_INVALID_ARG;
+  // rows are numbered with 32 bits, and a tile of 128 of them may start at the last one
+  if ((int64_t)c->table_width * c->page_size > 0x7fffff00ll || (int64_t)c->table_width * p->batch > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (reps && (p->group_size <= 0 || p->group_size % c->page_size != 0)) return LCA_ERR_INVALID_ARG;
+  return LCA_OK;
+}
+static int check_paged_pool(const lca_params* p, const lca_paged8* c) {
+  if (!c->pages_sem || !c->pages_pos || !c->scale_sem) return LCA_ERR_INVALID_ARG;
+  if ((p->variant == LCA_VARIANT_GQA) != (c->scale_pos != nullptr)) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos)) return LCA_ERR_MISALIGNED;
+  if ((int64_t)c->n_pages * p->n_kv_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (!simt_shape_ok(p)) return LCA_ERR_UNSUPPORTED_SHAPE;
+  return LCA_OK;
+}
+static int check_paged_pool(const lca_params* p, const lca_paged4* c) {
+  if (!c->pages_sem || !c->pages_pos || !c->shift_sem || !c->shift_pos || !c->exp_sem) return LCA_ERR_INVALID_ARG;
+  if ((p->variant == LCA_VARIANT_GQA) != (c->exp_pos != nullptr)) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos) || !aligned16(c->shift_sem) || !aligned16(c->shift_pos)) return LCA_ERR_MISALIGNED;
+  if ((int64_t)c->n_pages * p->n_kv_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (!simt_shape_ok(p)) return LCA_ERR_UNSUPPORTED_SHAPE;
+  return LCA_OK;
+}
+// Rows in or out of a paged cache.
+template <class Cache>
+static int check_paged_rows(const lca_params* p, const Cache* c, const void* rows_sem, const void* rows_pos, const int32_t* slot_map,
+                            int64_t n_rows) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(c);
+  if (st == LCA_OK) st = check_paged_pool(p, c);
+  if (st != LCA_OK) return st;
+  if (n_rows < 0 || n_rows > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (n_rows == 0) return LCA_OK;
+  if (!rows_sem || !rows_pos || !slot_map) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(rows_sem) || !aligned16(rows_pos)) return LCA_ERR_MISALIGNED;
+  return LCA_OK;
+}
+template <class Cache>
+static int check_paged_attention(const lca_params* p, const Cache* cache, const void* q_sem, const void* q_pos, int32_t q_len, bool reps,
+                                 const int32_t* n_tok, const void* out) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_table(p, cache, reps);
+  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  if (st != LCA_OK) return st;
+  if (!q_pos || !n_tok || !out || q_len <= 0) return LCA_ERR_INVALID_ARG;
+  if (p->variant == LCA_VARIANT_MLA && !q_sem) return LCA_ERR_INVALID_ARG;
+  if ((int64_t)p->batch * q_len * p->n_q_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
+  if (!aligned16(q_pos) || !aligned16(out) || (q_sem && !aligned16(q_sem))) return LCA_ERR_MISALIGNED;
+  return LCA_OK;
+}
+// Checks an online update over a paged cache; without a ready summary query computes it at the start of `ws` (*qbar).
+template <class Cache>
+static int begin_paged_update(const lca_params* p, const Cache* cache, const void* q_tail_sem, const void* q_tail_pos,
+                              int64_t q_tail_batch_stride, const float* qbar_opt, const int32_t* n_rep, const int32_t* n_tok,
+                              const int32_t* n_rep_new, const void* rep_sem, const void* rep_pos, const int32_t* anchor_out, void* ws,
+                              size_t ws_bytes, cudaStream_t stream, const double** qbar) {
+  int st = check_params(p, false);
+  if (st == LCA_OK) st = check_paged(cache);
+  if (st == LCA_OK) st = check_paged_table(p, cache, true);
+  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  if (st != LCA_OK) return st;
+  if (p->window < 0 || p->n_summary_q < 0) return LCA_ERR_INVALID_ARG;
+  if (!n_rep || !n_tok || !n_rep_new || n_rep_new == n_rep || !rep_sem || !rep_pos || !anchor_out) return LCA_ERR_INVALID_ARG;
+  if (!qbar_opt) {
+    if (!q_tail_pos || (p->variant == LCA_VARIANT_MLA && !q_tail_sem)) return LCA_ERR_INVALID_ARG;
+    const int n = p->n_summary_q > 0 ? p->n_summary_q : p->group_size;
+    if (q_tail_batch_stride < n) return LCA_ERR_INVALID_ARG;
+    if (!aligned16(q_tail_pos) || (q_tail_sem && !aligned16(q_tail_sem))) return LCA_ERR_MISALIGNED;
+    if (!ws || !aligned16(ws)) return LCA_ERR_INVALID_ARG;
+    if (ws_bytes < update_workspace_bytes(p)) return LCA_ERR_WORKSPACE_TOO_SMALL;
+  }
+  if (!aligned16(rep_sem) || !aligned16(rep_pos)) return LCA_ERR_MISALIGNED;
+  if (paged8_update_smem_bytes(p) > (size_t)PAGED8_UPDATE_SMEM) return LCA_ERR_UNSUPPORTED_SHAPE;
+  *qbar = nullptr;
+  if (!qbar_opt) {
+    st = update_qbar_launch(p, q_tail_sem, q_tail_pos, q_tail_batch_stride, ws, stream);
+    if (st != LCA_OK) return st;
+    *qbar = static_cast<const double*>(ws);
+  }
+  return LCA_OK;
 }
 }  // namespace lca
 
@@ -431,28 +524,6 @@ int lca_decode_step_update_ring(const lca_params* p, const void* q_sem, const vo
 }
 
 // ---- paged 8-bit cache
-static int check_paged(const lca_paged8* c) {
-  if (!c || c->n_pages <= 0) return LCA_ERR_INVALID_ARG;
-  if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128) return LCA_ERR_UNSUPPORTED_SHAPE;
-  if ((int64_t)c->n_pages * c->page_size > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
-  return LCA_OK;
-}
-static int check_paged_table(const lca_params* p, const lca_paged8* c, bool reps) {
-  if (!c->block_table || c->table_width <= 0) return LCA_ERR_INVALID_ARG;
-  // rows are numbered with 32 bits, and a tile of 128 of them may start at the last one
-  if ((int64_t)c->table_width * c->page_size > 0x7fffff00ll || (int64_t)c->table_width * p->batch > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
-  if (reps && (p->group_size <= 0 || p->group_size % c->page_size != 0)) return LCA_ERR_INVALID_ARG;
-  return LCA_OK;
-}
-static int check_paged_pool(const lca_params* p, const lca_paged8* c) {
-  if (!c->pages_sem || !c->pages_pos || !c->scale_sem) return LCA_ERR_INVALID_ARG;
-  if ((p->variant == LCA_VARIANT_GQA) != (c->scale_pos != nullptr)) return LCA_ERR_INVALID_ARG;
-  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos)) return LCA_ERR_MISALIGNED;
-  if ((int64_t)c->n_pages * p->n_kv_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
-  if (!simt_shape_ok(p)) return LCA_ERR_UNSUPPORTED_SHAPE;
-  return LCA_OK;
-}
-
 int lca_page_update(const lca_params* p, const lca_paged8* cache, const int32_t* n_rep, const int32_t* n_tok,
                     int32_t* held_rep, int32_t* held_tok, int32_t* free_pages, int32_t* n_free, int32_t* slot_map,
                     int32_t n_rows, int32_t rows_per_seq, int32_t* row_offsets, int32_t* status, void* stream) {
@@ -470,14 +541,8 @@ int lca_page_update(const lca_params* p, const lca_paged8* cache, const int32_t*
 
 int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* rows_sem, const void* rows_pos,
                      const int32_t* slot_map, int64_t n_rows, void* stream) {
-  int st = check_params(p, false);
-  if (st == LCA_OK) st = check_paged(cache);
-  if (st == LCA_OK) st = check_paged_pool(p, cache);
-  if (st != LCA_OK) return st;
-  if (n_rows < 0 || n_rows > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
-  if (n_rows == 0) return LCA_OK;
-  if (!rows_sem || !rows_pos || !slot_map) return LCA_ERR_INVALID_ARG;
-  if (!aligned16(rows_sem) || !aligned16(rows_pos)) return LCA_ERR_MISALIGNED;
+  const int st = check_paged_rows(p, cache, rows_sem, rows_pos, slot_map, n_rows);
+  if (st != LCA_OK || n_rows == 0) return st;
   return paged8_write_launch(p, cache, rows_sem, rows_pos, slot_map, n_rows, (cudaStream_t)stream);
 }
 
@@ -489,15 +554,8 @@ size_t lca_paged8_workspace_bytes(const lca_params* p, const lca_paged8* cache, 
 int lca_decode_attention_paged8(const lca_params* p, const lca_paged8* cache, const void* q_sem, const void* q_pos,
                                 int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
                                 void* ws, size_t ws_bytes, void* stream) {
-  int st = check_params(p, false);
-  if (st == LCA_OK) st = check_paged(cache);
-  if (st == LCA_OK) st = check_paged_table(p, cache, n_rep != nullptr);
-  if (st == LCA_OK) st = check_paged_pool(p, cache);
+  const int st = check_paged_attention(p, cache, q_sem, q_pos, q_len, n_rep != nullptr, n_tok, out);
   if (st != LCA_OK) return st;
-  if (!q_pos || !n_tok || !out || q_len <= 0) return LCA_ERR_INVALID_ARG;
-  if (p->variant == LCA_VARIANT_MLA && !q_sem) return LCA_ERR_INVALID_ARG;
-  if ((int64_t)p->batch * q_len * p->n_q_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
-  if (!aligned16(q_pos) || !aligned16(out) || (q_sem && !aligned16(q_sem))) return LCA_ERR_MISALIGNED;
   Paged8Attn a = {p, cache, p->variant == LCA_VARIANT_MLA ? q_sem : nullptr, q_pos, q_len, n_rep, n_tok, out, lse_opt, ws,
                   (cudaStream_t)stream};
   if (g_attn_impl.load() == 1) return attn_paged8_simt_launch(a);
@@ -510,30 +568,108 @@ int lca_decode_update_paged8(const lca_params* p, const lca_paged8* cache, const
                              const void* q_tail_pos, int64_t q_tail_batch_stride, const float* qbar_opt,
                              const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
                              void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream) {
-  int st = check_params(p, false);
-  if (st == LCA_OK) st = check_paged(cache);
-  if (st == LCA_OK) st = check_paged_table(p, cache, true);
-  if (st == LCA_OK) st = check_paged_pool(p, cache);
-  if (st != LCA_OK) return st;
-  if (p->window < 0 || p->n_summary_q < 0) return LCA_ERR_INVALID_ARG;
-  if (!n_rep || !n_tok || !n_rep_new || n_rep_new == n_rep || !rep_sem || !rep_pos || !anchor_out) return LCA_ERR_INVALID_ARG;
-  if (!qbar_opt) {
-    if (!q_tail_pos || (p->variant == LCA_VARIANT_MLA && !q_tail_sem)) return LCA_ERR_INVALID_ARG;
-    const int n = p->n_summary_q > 0 ? p->n_summary_q : p->group_size;
-    if (q_tail_batch_stride < n) return LCA_ERR_INVALID_ARG;
-    if (!aligned16(q_tail_pos) || (q_tail_sem && !aligned16(q_tail_sem))) return LCA_ERR_MISALIGNED;
-    if (!ws || !aligned16(ws)) return LCA_ERR_INVALID_ARG;
-    if (ws_bytes < update_workspace_bytes(p)) return LCA_ERR_WORKSPACE_TOO_SMALL;
-  }
-  if (!aligned16(rep_sem) || !aligned16(rep_pos)) return LCA_ERR_MISALIGNED;
-  if (paged8_update_smem_bytes(p) > (size_t)PAGED8_UPDATE_SMEM) return LCA_ERR_UNSUPPORTED_SHAPE;
   const double* qbar = nullptr;
-  if (!qbar_opt) {
-    st = update_qbar_launch(p, q_tail_sem, q_tail_pos, q_tail_batch_stride, ws, (cudaStream_t)stream);
-    if (st != LCA_OK) return st;
-    qbar = static_cast<const double*>(ws);
-  }
+  const int st = begin_paged_update(p, cache, q_tail_sem, q_tail_pos, q_tail_batch_stride, qbar_opt, n_rep, n_tok, n_rep_new, rep_sem, rep_pos,
+                                    anchor_out, ws, ws_bytes, (cudaStream_t)stream, &qbar);
+  if (st != LCA_OK) return st;
   return paged8_update_launch(p, cache, qbar_opt, qbar, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, anchor_out, (cudaStream_t)stream);
+}
+
+// ---- paged 4-bit cache
+int lca_paged4_write(const lca_params* p, const lca_paged4* cache, const void* rows_sem, const void* rows_pos,
+                     const int32_t* slot_map, int64_t n_rows, void* stream) {
+  const int st = check_paged_rows(p, cache, rows_sem, rows_pos, slot_map, n_rows);
+  if (st != LCA_OK || n_rows == 0) return st;
+  return paged4_rows_launch(p, cache, true, rows_sem, rows_pos, slot_map, n_rows, (cudaStream_t)stream);
+}
+
+int lca_paged4_read(const lca_params* p, const lca_paged4* cache, void* rows_sem, void* rows_pos, const int32_t* slot_map,
+                    int64_t n_rows, void* stream) {
+  const int st = check_paged_rows(p, cache, rows_sem, rows_pos, slot_map, n_rows);
+  if (st != LCA_OK || n_rows == 0) return st;
+  return paged4_rows_launch(p, cache, false, rows_sem, rows_pos, slot_map, n_rows, (cudaStream_t)stream);
+}
+
+size_t lca_paged4_workspace_bytes(const lca_params* p, const lca_paged4* cache, int32_t q_len) {
+  if (check_params(p, false) != LCA_OK || check_paged(cache) != LCA_OK || q_len <= 0 || !simt_shape_ok(p)) return 0;
+  return attn_paged4_workspace_bytes(p, q_len);
+}
+
+int lca_decode_attention_paged4(const lca_params* p, const lca_paged4* cache, const void* q_sem, const void* q_pos,
+                                int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
+                                void* ws, size_t ws_bytes, void* stream) {
+  const int st = check_paged_attention(p, cache, q_sem, q_pos, q_len, n_rep != nullptr, n_tok, out);
+  if (st != LCA_OK) return st;
+  Paged4Attn a = {p, cache, p->variant == LCA_VARIANT_MLA ? q_sem : nullptr, q_pos, q_len, n_rep, n_tok, out, lse_opt, ws,
+                  (cudaStream_t)stream};
+  if (g_attn_impl.load() == 1) return attn_paged4_simt_launch(a);
+  if (!ws || !aligned16(ws)) return LCA_ERR_INVALID_ARG;
+  if (ws_bytes < attn_paged4_workspace_bytes(p, q_len)) return LCA_ERR_WORKSPACE_TOO_SMALL;
+  return attn_paged4_launch(a);
+}
+
+int lca_decode_update_paged4(const lca_params* p, const lca_paged4* cache, const void* q_tail_sem,
+                             const void* q_tail_pos, int64_t q_tail_batch_stride, const float* qbar_opt,
+                             const int32_t* n_rep, const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem,
+                             void* rep_pos, int32_t* anchor_out, void* ws, size_t ws_bytes, void* stream) {
+  const double* qbar = nullptr;
+  const int st = begin_paged_update(p, cache, q_tail_sem, q_tail_pos, q_tail_batch_stride, qbar_opt, n_rep, n_tok, n_rep_new, rep_sem, rep_pos,
+                                    anchor_out, ws, ws_bytes, (cudaStream_t)stream, &qbar);
+  if (st != LCA_OK) return st;
+  return paged4_update_launch(p, cache, qbar_opt, qbar, n_rep, n_tok, n_rep_new, rep_sem, rep_pos, anchor_out, (cudaStream_t)stream);
+}
+
+// ---- around a speculative decode step
+int lca_rope(const lca_rope_args* a, void* stream) {
+  if (!a || (a->dtype != LCA_DTYPE_BF16 && a->dtype != LCA_DTYPE_FP32)) return LCA_ERR_INVALID_ARG;
+  if ((a->interleaved | a->inverse) & ~1) return LCA_ERR_INVALID_ARG;
+  if (!a->q && !a->k) return LCA_ERR_INVALID_ARG;
+  if ((a->q != nullptr) != (a->q_out != nullptr) || (a->k != nullptr) != (a->k_out != nullptr)) return LCA_ERR_INVALID_ARG;
+  if ((a->q && a->n_q_heads <= 0) || (a->k && a->n_k_heads <= 0)) return LCA_ERR_INVALID_ARG;
+  if (a->n_tokens < 0 || a->n_tokens > 0x7fffffffll || a->head_dim <= 0 || a->head_dim > 65536) return LCA_ERR_INVALID_ARG;
+  if ((long long)(a->q ? a->n_q_heads : 0) + (a->k ? a->n_k_heads : 0) > 1 << 20) return LCA_ERR_INVALID_ARG;
+  if (a->rot_dim < 2 || a->rot_dim % 2 != 0 || a->rot_dim > a->head_dim || a->rot_dim > 8192) return LCA_ERR_INVALID_ARG;
+  if (!(a->factor - a->factor == 0.f)) return LCA_ERR_INVALID_ARG;
+  if (a->n_tokens == 0) return LCA_OK;
+  if (!a->positions || !a->freqs) return LCA_ERR_INVALID_ARG;
+  const uintptr_t elem = a->dtype == LCA_DTYPE_BF16 ? 1 : 3;
+  for (const void* x : {a->q, (const void*)a->q_out, a->k, (const void*)a->k_out})
+    if (reinterpret_cast<uintptr_t>(x) & elem) return LCA_ERR_MISALIGNED;
+  return rope_launch(a, (cudaStream_t)stream);
+}
+
+int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scale, double trained_len, double fast,
+                         double slow, double* freqs_host, float* factor_host) {
+  if (kind < LCA_ROPE_PLAIN || kind > LCA_ROPE_RAMP || rot_dim < 2 || rot_dim % 2 != 0 || !freqs_host || !factor_host) return LCA_ERR_INVALID_ARG;
+  if (!(base > 0.0) || !std::isfinite(base)) return LCA_ERR_INVALID_ARG;
+  if (kind != LCA_ROPE_PLAIN && (!(scale > 0.0) || !std::isfinite(scale))) return LCA_ERR_INVALID_ARG;
+  if (kind == LCA_ROPE_BASE && rot_dim == 2) return LCA_ERR_INVALID_ARG;      // one pair is both the fastest and the slowest
+  if (kind == LCA_ROPE_RAMP && (!(trained_len > 0.0) || !(fast > slow) || !std::isfinite(trained_len) || !std::isfinite(fast) || !std::isfinite(slow)))
+    return LCA_ERR_INVALID_ARG;
+  if (kind == LCA_ROPE_BASE) base *= std::pow(scale, (double)rot_dim / (rot_dim - 2));
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    double f = std::pow(base, -2.0 * i / rot_dim);
+    if (kind == LCA_ROPE_LINEAR) f /= scale;
+    if (kind == LCA_ROPE_RAMP) {
+      const double turns = trained_len * f / 6.283185307179586476925;
+      const double keep = std::min(std::max((turns - slow) / (fast - slow), 0.0), 1.0);
+      f = f * keep + f / scale * (1.0 - keep);
+    }
+    freqs_host[i] = f;
+  }
+  *factor_host = kind == LCA_ROPE_RAMP && scale > 1.0 ? (float)(0.1 * std::log(scale) + 1.0) : 1.f;
+  return LCA_OK;
+}
+
+int lca_verify_drafts(const lca_verify_args* a, void* stream) {
+  if (!a || (a->dtype != LCA_DTYPE_BF16 && a->dtype != LCA_DTYPE_FP32)) return LCA_ERR_INVALID_ARG;
+  if (a->batch <= 0 || a->n_drafts < 0 || a->n_drafts >= 0x7fffffff || a->vocab <= 0) return LCA_ERR_INVALID_ARG;
+  if (!a->target_probs || !a->u_sample || !a->accepted || !a->tokens_out) return LCA_ERR_INVALID_ARG;
+  if (a->n_drafts > 0 && (!a->draft_tokens || !a->u_accept)) return LCA_ERR_INVALID_ARG;
+  if ((a->n_tok != nullptr) != (a->n_tok_out != nullptr)) return LCA_ERR_INVALID_ARG;
+  const uintptr_t elem = a->dtype == LCA_DTYPE_BF16 ? 1 : 3;
+  if ((reinterpret_cast<uintptr_t>(a->target_probs) | reinterpret_cast<uintptr_t>(a->draft_probs)) & elem) return LCA_ERR_MISALIGNED;
+  return verify_launch(a, (cudaStream_t)stream);
 }
 
 int lca_latent_to_value(const void* attn_latent, const void* w_uv, void* out_v, int64_t n_tokens,
@@ -552,9 +688,10 @@ int lca_selftest_bounded_wait(int64_t limit_cycles, void* stream) {
 
 int lca_last_device_status(void* stream) {
   const int st = attn_tc_device_status((cudaStream_t)stream);      // synchronises the stream
-  const int cst = condense_take_status(), ust = latent_to_value_take_status(), pst = attn_paged8_take_status();
-  if (cst < 0 || ust < 0 || pst < 0) return LCA_ERR_CUDA;
-  if (cst > 0 || ust > 0 || pst > 0) return LCA_ERR_DEVICE_TIMEOUT;
+  const int cst = condense_take_status(), ust = latent_to_value_take_status(), pst = attn_paged8_take_status(),
+            p4st = attn_paged4_take_status();
+  if (cst < 0 || ust < 0 || pst < 0 || p4st < 0) return LCA_ERR_CUDA;
+  if (cst > 0 || ust > 0 || pst > 0 || p4st > 0) return LCA_ERR_DEVICE_TIMEOUT;
   return st;
 }
 

@@ -23,9 +23,9 @@ void note_launch(int n = 1);
 __device__ __forceinline__ void chain_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void chain_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <class K, class... A>
-inline int launch_chained(K kern, unsigned grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, const A&... args) {
+inline int launch_chained(K kern, dim3 grid, unsigned block, size_t smem, cudaStream_t stream, unsigned cluster, const A&... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(grid); cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
+  cfg.gridDim = grid; cfg.blockDim = dim3(block); cfg.dynamicSmemBytes = smem; cfg.stream = stream;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -217,7 +217,7 @@ int page_update_launch(const lca_params* p, const lca_paged8* c, const int32_t* 
                        int32_t* row_offsets, int32_t* status, cudaStream_t stream);
 int paged8_write_launch(const lca_params* p, const lca_paged8* c, const void* rows_sem, const void* rows_pos,
                         const int32_t* slot_map, long long n_rows, cudaStream_t stream);
-static constexpr int PAGED8_UPDATE_SMEM = 227 * 1024 - 128;              // most that the update kernel may ask for, beside its static part
+static constexpr int PAGED8_UPDATE_SMEM = 227 * 1024 - 256;              // most that the update kernel may ask for, beside its static part
 size_t paged8_update_smem_bytes(const lca_params* p);
 int paged8_update_launch(const lca_params* p, const lca_paged8* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
                          const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,
@@ -236,5 +236,27 @@ size_t attn_paged8_workspace_bytes(const lca_params* p, int q_len);
 int attn_paged8_launch(const Paged8Attn& a);           // tensor-core kernel
 int attn_paged8_simt_launch(const Paged8Attn& a);      // scalar kernel
 int attn_paged8_take_status();
+
+// ---- paged 4-bit cache ----------------------------------------------------------------------
+int paged4_rows_launch(const lca_params* p, const lca_paged4* c, bool write, const void* rows_sem, const void* rows_pos,
+                       const int32_t* slot_map, long long n_rows, cudaStream_t stream);
+int paged4_update_launch(const lca_params* p, const lca_paged4* c, const float* qbar_f, const double* qbar_d, const int32_t* n_rep,
+                         const int32_t* n_tok, int32_t* n_rep_new, void* rep_sem, void* rep_pos, int32_t* anchor_out,
+                         cudaStream_t stream);
+struct Paged4Attn {
+  const lca_params* p; const lca_paged4* c;
+  const void* q_sem; const void* q_pos; int q_len;
+  const int32_t* n_rep; const int32_t* n_tok;
+  void* out; float* lse;
+  void* ws; cudaStream_t stream;
+};
+size_t attn_paged4_workspace_bytes(const lca_params* p, int q_len);
+int attn_paged4_launch(const Paged4Attn& a);           // tensor-core kernel
+int attn_paged4_simt_launch(const Paged4Attn& a);      // scalar kernel
+int attn_paged4_take_status();
+
+// ---- around a speculative decode step -------------------------------------------------------
+int rope_launch(const lca_rope_args* a, cudaStream_t stream);
+int verify_launch(const lca_verify_args* a, cudaStream_t stream);
 
 }  // namespace lca
