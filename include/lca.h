@@ -418,7 +418,7 @@ typedef struct lca_paged4 {
   int32_t n_pages;        /* as in lca_paged8 */
   int32_t page_size;
   int32_t table_width;
-} lca_paged4;             /* a HOST structure of device pointers; pages and shifts 16-byte aligned */
+} lca_paged4;             /* a HOST structure of device pointers; pages, shifts and exponents 16-byte aligned */
 
 /* Writes rows into the paged cache.  Arguments as for lca_paged8_write; but rows do not depend on one another, so they may come in
  * any order and any number to a page, and a row is replaced by writing its slot again.  Two rows with the same slot in one call leave

@@ -112,28 +112,26 @@ struct Paged4Plan {
   static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
   static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 columns)
   static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
-  static constexpr int PER_TILE = MLA ? NK : NK + NV;        // slots of a tile; MLA: the latent chunks are keys and values
-  static constexpr int V0 = MLA ? 0 : NK;                    // the first of them with values
-  static constexpr int SLOT = 16384;
+  static constexpr int K_BYTES = 128 * (KSEM * 128 + DP), V_BYTES = MLA ? 0 : 16384, TILE = K_BYTES + V_BYTES;        // expanded, two of them
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
   static constexpr int P_BYTES = 128 * 2 * NH;               // per key the first terms of all rows, then the second ones
   static constexpr int TM_S = 2 * NV * NH, TM_USED = TM_S + 4 * NH;
   static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
   static constexpr int CTAS = (MLA && DS == 512) || NH == 32 ? 1 : 2;        // per SM
-  static constexpr int EW = CTAS == 2 && GROUPS == 2 ? 4 : 8;                // expansion warps
-  static constexpr int SOFTMAX_WARPS = 4 * GROUPS, W_MMA = SOFTMAX_WARPS + EW, THREADS = 32 * (W_MMA + 1);
-  static constexpr int RPT = 16 / EW;                        // rows of a chunk that a thread expands, four threads a row of 128 columns
-  // 16-byte pieces of a tile that a thread expands: the latent (V) chunks row by row, then the pos chunk
-  static constexpr int UNITS_SEM = VW == 128 ? RPT : RPT / 2, UNITS_POS = DP == 128 ? RPT : RPT / 2, UNITS = NV * UNITS_SEM + UNITS_POS;
-  static constexpr int DEPTH = UNITS > 8 ? 1 : UNITS > 4 ? 1 : 2;              // tiles in registers
-  // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers first.
-  static constexpr int MISC_BYTES = 512 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH);
-  static constexpr int BUDGET = (CTAS == 1 ? 227 * 1024 : 113 * 1024) - 1024;      // 1 KB to align the base
-  static constexpr int SLOTS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / SLOT;
-  static constexpr int SLOTS = SLOTS_FIT > 12 ? 12 : SLOTS_FIT;
-  static constexpr int OFF_Q = SLOTS * SLOT, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
-  static constexpr int SMEM = OFF_MISC + MISC_BYTES + 1024;
-  static_assert(SLOTS >= 2 * PER_TILE && 8 * (2 * SLOTS + 7) <= 256 && SMEM <= 227 * 1024, "the tiles that S and O work on fit the ring");
+  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOAD = W_MMA + 1, THREADS = 32 * (W_LOAD + 1);
+  // packed rows as they come: a slab of codes, shifts and 32 bytes of facts
+  static constexpr int SLAB = MLA && DS == 512 ? 32 : 128, SLABS = 128 / SLAB;
+  static constexpr int ST_POS = SLAB * DS / 2, ST_SHS = ST_POS + SLAB * DP / 2, ST_SHP = ST_SHS + SLAB * DS / 64, ST_FACT = ST_SHP + SLAB * DP / 64;
+  static constexpr int STAGE = ST_FACT + 32;
+  static constexpr int FACTS = 4, FACT = 256 + 16;           // per tile: exponents of values and of keys, pages that are there
+  // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers and scalars first, then the table.
+  static constexpr int MISC_BYTES = 384 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH) + FACTS * FACT;
+  static constexpr int BUDGET = CTAS == 1 ? 227 * 1024 : 113 * 1024;
+  static constexpr int STAGES_FIT = (BUDGET - 2 * TILE - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / STAGE;
+  static constexpr int STAGES = STAGES_FIT > 4 ? 4 : STAGES_FIT;
+  static constexpr int OFF_Q = 2 * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_STAGE = OFF_P + 2 * P_BYTES, OFF_MISC = OFF_STAGE + STAGES * STAGE;
+  static constexpr int SMEM = OFF_MISC + MISC_BYTES;
+  static_assert(STAGES >= 2 && SMEM <= BUDGET && STAGE % 16 == 0 && OFF_MISC % 16 == 0, "two slabs on their way while one is expanded");
   static_assert(THREADS / 32 <= 26, "room for the sums of the ranges");
 };
 
@@ -162,11 +160,9 @@ __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-// 16 bytes that are read once
-__device__ __forceinline__ uint4 load_stream(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
+__device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
 static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
@@ -174,38 +170,49 @@ static constexpr float LO4_GAIN = 16.f;                      // of the second te
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
-  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS, W_EXP = PL::SOFTMAX_WARPS, W_MMA = PL::W_MMA;
+  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
+  constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOAD = PL::W_LOAD;
   const Paged8Params& p = a.b;
-  extern __shared__ unsigned char smem_dyn[];
-  const uint32_t base = (smem_u32(smem_dyn) + 1023u) & ~1023u;
-  unsigned char* base_ptr = smem_dyn + (base - smem_u32(smem_dyn));
+  extern __shared__ __align__(1024) unsigned char smem_p4[];
+  unsigned char* base_ptr = smem_p4;
+  const uint32_t base = smem_u32(smem_p4);
   const uint32_t bars = base + PL::OFF_MISC;
-  auto FULL = [&](int s) { return bars + 8 * s; };
-  auto EMPTY = [&](int s) { return bars + 8 * (PL::SLOTS + s); };
-  const uint32_t more_bars = bars + 8 * (2 * PL::SLOTS), QFULL = more_bars + 48;
-  auto SFULL = [&](uint32_t i) { return more_bars + 8 * i; };
-  auto PFULL = [&](uint32_t i) { return more_bars + 16 + 8 * i; };
-  auto PVDONE = [&](uint32_t i) { return more_bars + 32 + 8 * i; };
+  // two buffers of each: S complete, weights written, O complete, keys / values expanded
+  auto SFULL = [&](uint32_t i) { return bars + 8 * i; };
+  auto PFULL = [&](uint32_t i) { return bars + 16 + 8 * i; };
+  auto PVDONE = [&](uint32_t i) { return bars + 32 + 8 * i; };
+  auto KFULL = [&](uint32_t i) { return bars + 48 + 8 * i; };
+  auto VFULL = [&](uint32_t i) { return bars + 64 + 8 * i; };
+  auto GFULL = [&](uint32_t i) { return bars + 80 + 8 * i; };           // packed slab landed, read
+  auto GEMPTY = [&](uint32_t i) { return bars + 112 + 8 * i; };
+  auto FFULL = [&](uint32_t i) { return bars + 144 + 8 * i; };          // exponents of a tile landed, read
+  auto FEMPTY = [&](uint32_t i) { return bars + 176 + 8 * i; };
+  const uint32_t QFULL = bars + 208;
   unsigned char* misc = base_ptr + PL::OFF_MISC;
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 256);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
   int* s_b = reinterpret_cast<int*>(misc + 264);
   long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
-  uint2* s_table = reinterpret_cast<uint2*>(misc + 512);
-  float* s_qs = reinterpret_cast<float*>(misc + 640);
+  uint2* s_table = reinterpret_cast<uint2*>(misc + 384);
+  float* s_qs = reinterpret_cast<float*>(misc + 512);
   float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
   int* s_lim = reinterpret_cast<int*>(s_f + NH);
   float* s_wmax = reinterpret_cast<float*>(s_lim + NH);      // also the sums of the four warps of a group
   int* s_row = reinterpret_cast<int*>(s_wmax + 4 * NH);      // output row of each query row, of this piece and of the next one
+  unsigned char* s_fact = reinterpret_cast<unsigned char*>(s_row + 2 * NH);
   long long* s_warp = reinterpret_cast<long long*>(base_ptr + PL::OFF_P);      // totals of the warps, and as many words; before the weights
   const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x;
+  auto fail = [&](int code) { atomicCAS(&g_paged4_status, 0, code); *abort_flag = 1; };
 
   if (tid == 0) {
-    for (int s = 0; s < PL::SLOTS; ++s) { mbar_init(FULL(s), PL::EW); mbar_init(EMPTY(s), 1); }
-    for (int i = 0; i < 2; ++i) { mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); }
-    mbar_init(QFULL, 32 * PL::SOFTMAX_WARPS);
     *abort_flag = 0;
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); mbar_init(KFULL(i), PL::EW); mbar_init(VFULL(i), PL::EW);
+    }
+    for (int i = 0; i < 4; ++i) { mbar_init(GFULL(i), 1); mbar_init(GEMPTY(i), PL::EW); mbar_init(FFULL(i), 1); mbar_init(FEMPTY(i), PL::SOFTMAX_WARPS); }
+    mbar_init(QFULL, 32 * PL::SOFTMAX_WARPS);
     fence_mbar_init();
+    if (base & 1023u) fail(100);                             // the operands' images need it
   }
   if (warp == W_MMA) { tmem_alloc(smem_u32((const void*)tmem_slot), PL::TM_COLS); tmem_relinquish(); }
   paged4_table_load(s_table, tid);
@@ -222,180 +229,161 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
   const uint32_t tmem = *tmem_slot;
   Walk w;
   w.b = *s_b; w.off = s_off[0]; w.left = s_off[1]; w.fresh = true; w.n = 0;
-  auto fail = [&](int code) { atomicCAS(&g_paged4_status, 0, code); *abort_flag = 1; };
 
-  if (warp >= W_EXP && warp < W_MMA) {
-    // ----------------------------------------------------------------------------------------------- expansion
-    // Four threads take a row of a 128-wide chunk, rows r0 + STRIDE i; of a 64-wide one the first two take the even ones of these
-    // rows and the others the odd ones.
-    constexpr int RPT = PL::RPT, STRIDE = 128 / RPT, DEPTH = PL::DEPTH;
-    const int et = tid - 32 * W_EXP, r0 = et >> 2, u = et & 3;
-    const int mask = p.page - 1;
-    bool ok = true;
-    // the tile whose pages are looked up next
-    int j = 0;
+  if (warp == W_LOAD) {
+    // --------------------------------------------------------------------------------------------------- loads
+    // Lane i < 8 looks up the page of rows [16 i, 16 i + 16) of a tile, one tile ahead; then the lanes issue the copies: a request for
+    // each run of rows (a page, or the slab's share of it) and array.
+    bool ok = !*abort_flag;
+    int j = 0, stage = 0;
+    uint32_t phase = 0, g = 0;
     bool more = w.next(p);
-    struct Tile { int page[RPT]; int hk; bool any; };        // page of each row, -1: no such row
-    auto look = [&](Tile& t) {
-      t.any = more;
+    struct Next { long long row; int page_ok, lo, mid, hi; bool any; } nx;             // lo, mid, hi: PagedSpan from the tile's first row
+    auto look = [&]() {
+      nx.any = more;
       if (!more) return;
-      t.hk = w.hk;
-      const int row0 = w.t.row0(w.t0 + j) + r0;
-#pragma unroll
-      for (int i = 0; i < RPT; ++i) {
-        const int x = row0 + STRIDE * i;
-        t.page[i] = w.t.s.has(x) ? p.table[(size_t)w.b * p.width + (x >> p.page_log2)] : -1;
-      }
+      const PagedSpan sp = w.t.s;
+      const int row0 = w.t.row0(w.t0 + j), x = row0 + 16 * (lane & 7);
+      nx.lo = sp.n_rep - row0; nx.mid = sp.tok0 - row0; nx.hi = sp.n_tok - row0;
+      int pg = -1;
+      if (sp.any(x & ~(p.page - 1), p.page) && (x >> p.page_log2) < p.width) pg = p.table[(size_t)w.b * p.width + (x >> p.page_log2)];
+      nx.page_ok = pg >= 0 && pg < p.n_pages;
+      nx.row = nx.page_ok ? (((long long)pg * p.Hkv + w.hk) << p.page_log2) + (x & (p.page - 1)) : 0;
       if (++j == w.n) { j = 0; more = w.next(p); }
     };
-    // rows of the pool, -1 where a row is absent
-    struct Rows { long long r[RPT]; bool any; };
-    auto rows_of = [&](const Tile& t, Rows& y) {
-      y.any = t.any;
-#pragma unroll
-      for (int i = 0; i < RPT; ++i)
-        y.r[i] = t.any && (unsigned)t.page[i] < (unsigned)p.n_pages
-                     ? (((long long)t.page[i] * p.Hkv + t.hk) << p.page_log2) + ((r0 + STRIDE * i) & mask) : -1;
-    };
-    struct Data { uint4 v[PL::UNITS]; uint32_t s[NV * PL::UNITS_SEM > 4 ? RPT : NV * PL::UNITS_SEM][2]; uint32_t sp[PL::UNITS_POS]; bool any; };
-    constexpr bool WIDE = DS == 512;                         // the shifts of a row are eight bytes: one load for its four chunks
-    auto load_sem = [&](const Rows& y, int c, Data& d) {
-      if constexpr (PL::VW == 128) {
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-          const bool in = y.r[i] >= 0;
-          d.v[c * RPT + i] = in ? load_stream(a.sem + (size_t)y.r[i] * (DS / 2) + c * 64 + u * 16) : make_uint4(0u, 0u, 0u, 0u);
-          if constexpr (WIDE) {
-            if (c == NV - 1) {                               // the last chunk of the tile before has been expanded
-              const uint2 s = in ? __ldg(reinterpret_cast<const uint2*>(a.shift_sem) + y.r[i]) : make_uint2(0u, 0u);
-              d.s[i][0] = s.x; d.s[i][1] = s.y;
-            }
-          } else {
-            d.s[c * RPT + i][0] = in ? (uint32_t)__ldg(a.shift_sem + (size_t)y.r[i] * (DS / 64) + c * 2 + (u >> 1)) >> (4 * (u & 1)) : 0u;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < RPT / 2; ++i) {
-          const long long r = u < 2 ? y.r[2 * i] : y.r[2 * i + 1];
-          const bool in = r >= 0;
-          d.v[i] = in ? load_stream(a.sem + (size_t)r * 32 + (u & 1) * 16) : make_uint4(0u, 0u, 0u, 0u);
-          d.s[i][0] = in ? (uint32_t)__ldg(a.shift_sem + r) >> (4 * (u & 1)) : 0u;
-        }
-      }
-    };
-    auto load_pos = [&](const Rows& y, Data& d) {
-      constexpr int U0 = NV * PL::UNITS_SEM;
-      if constexpr (DP == 128) {
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-          const bool in = y.r[i] >= 0;
-          d.v[U0 + i] = in ? load_stream(a.pos + (size_t)y.r[i] * 64 + u * 16) : make_uint4(0u, 0u, 0u, 0u);
-          d.sp[i] = in ? (uint32_t)__ldg(a.shift_pos + (size_t)y.r[i] * 2 + (u >> 1)) >> (4 * (u & 1)) : 0u;
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < RPT / 2; ++i) {
-          const long long r = u < 2 ? y.r[2 * i] : y.r[2 * i + 1];
-          const bool in = r >= 0;
-          d.v[U0 + i] = in ? load_stream(a.pos + (size_t)r * 32 + (u & 1) * 16) : make_uint4(0u, 0u, 0u, 0u);
-          d.sp[i] = in ? (uint32_t)__ldg(a.shift_pos + r) >> (4 * (u & 1)) : 0u;
-        }
-      }
-    };
-    int slot = 0;
-    uint32_t phase = 0;
-    auto begin_slot = [&]() {
-      if (ok && !mbar_wait(EMPTY(slot), phase ^ 1, abort_flag)) { fail(ERR_WAIT_KV_EMPTY); ok = false; }
+    look();
+    while (ok && nx.any) {
+      const Next c = nx;
+      look();
+      const unsigned pages = __ballot_sync(0xffffffffu, c.page_ok) & 0xffu;
+      const bool part = !(pages == 0xffu && (c.lo >= 128 || (c.mid <= 0 && c.hi >= 128)));
+      const int f = (int)(g & 3);
+      ok = mbar_wait(FEMPTY(f), ((g >> 2) & 1) ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
-    };
-    auto end_slot = [&]() {
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(FULL(slot));
-      if (++slot == PL::SLOTS) { slot = 0; phase ^= 1; }
-    };
-    auto store = [&](uint32_t off, const uint4& v, uint32_t shift) {         // 32 values of one row
-      const uint2 t = s_table[shift & 15];
-      const uint2 x0 = paged4_expand(v.x, t), x1 = paged4_expand(v.y, t), x2 = paged4_expand(v.z, t), x3 = paged4_expand(v.w, t);
-      unsigned char* q = base_ptr + slot * PL::SLOT;
-      *reinterpret_cast<uint4*>(q + off) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-      *reinterpret_cast<uint4*>(q + (off ^ 16u)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-    };
-    const uint32_t off128 = swz<128>(r0, 2 * u), off64 = swz<64>(r0 + (u < 2 ? 0 : STRIDE), 2 * (u & 1));
-    auto put_sem = [&](int c, const Data& d) {
-      if constexpr (PL::VW == 128) {
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-          const uint32_t s = WIDE ? (c < 2 ? d.s[i][0] : d.s[i][1]) >> (16 * (c & 1) + 4 * u) : d.s[WIDE ? 0 : c * RPT + i][0];
-          store(off128 + i * STRIDE * 128, d.v[c * RPT + i], s);
+      if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
+      {
+        const uint32_t at = base + PL::OFF_MISC + (uint32_t)(s_fact - misc) + f * PL::FACT;
+        if (lane == 0) {
+          *reinterpret_cast<uint32_t*>(s_fact + f * PL::FACT + 256) = pages;
+          mbar_expect_tx(FFULL(f), __popc(pages) * 16 * (PL::MLA ? 1 : 2));
         }
-      } else {
-#pragma unroll
-        for (int i = 0; i < RPT / 2; ++i) store(off64 + i * 2 * STRIDE * 64, d.v[i], d.s[i][0]);
+        __syncwarp();
+        const int per = p.page >> 4, run = lane & 7;         // lane: run + 8 * array
+        const long long r = __shfl_sync(0xffffffffu, c.row, (run * per) & 7);
+        if (lane < (PL::MLA ? 8 : 16) && run * per < 8 && ((pages >> (run * per)) & 1u))
+          bulk_copy(at + (lane >= 8 ? 128 : 0) + run * p.page, (lane >= 8 ? a.exp_k : a.exp_v) + r, p.page, FFULL(f));
       }
-    };
-    auto put_pos = [&](const Data& d) {
-      constexpr int U0 = NV * PL::UNITS_SEM;
-      if constexpr (DP == 128) {
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) store(off128 + i * STRIDE * 128, d.v[U0 + i], d.sp[i]);
-      } else {
-#pragma unroll
-        for (int i = 0; i < RPT / 2; ++i) store(off64 + i * 2 * STRIDE * 64, d.v[U0 + i], d.sp[i]);
+#pragma unroll 1
+      for (int s = 0; s < PL::SLABS; ++s) {
+        ok = mbar_wait(GEMPTY(stage), phase ^ 1, abort_flag);
+        ok = __all_sync(0xffffffffu, ok);
+        if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
+        constexpr int GR = PL::SLAB / 16, B_SEM = DS / 2, B_POS = DP / 2, B_SHS = DS / 64, B_SHP = DP / 64;
+        const uint32_t at = base + PL::OFF_STAGE + stage * PL::STAGE;
+        const unsigned here = (pages >> (s * GR)) & ((1u << GR) - 1u);
+        if (lane == 0) {
+          int* fact = reinterpret_cast<int*>(base_ptr + PL::OFF_STAGE + stage * PL::STAGE + PL::ST_FACT);
+          fact[0] = part; fact[1] = c.lo - s * PL::SLAB; fact[2] = c.mid - s * PL::SLAB; fact[3] = c.hi - s * PL::SLAB; fact[4] = (int)here;
+          mbar_expect_tx(GFULL(stage), __popc(here) * 16 * (B_SEM + B_POS + B_SHS + B_SHP));
+        }
+        __syncwarp();
+        const int rows = min(p.page, PL::SLAB), per = rows >> 4, run = lane >> 2, arr = lane & 3;
+        const long long r = __shfl_sync(0xffffffffu, c.row, (s * GR + run * per) & 7);
+        if (run * per < GR && ((here >> (run * per)) & 1u)) {
+          const int bytes = arr == 0 ? B_SEM : arr == 1 ? B_POS : arr == 2 ? B_SHS : B_SHP;
+          const int off = arr == 0 ? 0 : arr == 1 ? PL::ST_POS : arr == 2 ? PL::ST_SHS : PL::ST_SHP;
+          const uint8_t* src = arr == 0 ? a.sem : arr == 1 ? a.pos : arr == 2 ? a.shift_sem : a.shift_pos;
+          bulk_copy(at + off + run * rows * bytes, src + r * bytes, rows * bytes, GFULL(stage));
+        }
+        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
       }
-    };
-    // tiles t .. t + DEPTH - 1 in registers, pages of tile t + DEPTH on their way
-    Data d[DEPTH];
-    Tile ahead;
-    {
-      Rows y;
-#pragma unroll
-      for (int k = 0; k < DEPTH; ++k) {
-        look(ahead);
-        rows_of(ahead, y);
-        d[k].any = y.any;
-#pragma unroll
-        for (int c = 0; c < NV; ++c) load_sem(y, c, d[k]);
-        load_pos(y, d[k]);
-      }
+      ++g;
     }
-    look(ahead);
-    while (ok && d[0].any) {
+  } else if (warp >= W_EXP && warp < W_MMA) {
+    // ----------------------------------------------------------------------------------------------- expansion
+    // A thread takes 32 values (16 bytes of codes) of a row at a time.  Eight neighbouring lanes write two rows, so that their
+    // units fall on all banks of the swizzled image.
+    const int et = tid - 32 * W_EXP, ew = warp - W_EXP;
+    const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
+    bool ok = !*abort_flag;
+    int stage = 0;
+    uint32_t phase = 0;
+    auto wait = [&](uint32_t bar, uint32_t ph, int code) {
+      if (ok && !mbar_wait(bar, ph, abort_flag)) { fail(code); ok = false; }
+      ok = __all_sync(0xffffffffu, ok);
+      return ok;
+    };
+    auto signal = [&](uint32_t bar) {
+      __syncwarp();
+      if (lane == 0) mbar_arrive(bar);
+    };
+    // units `first`, `first` + step ...: N of them; `at`: codes and shift of unit i, row in the slab and place in the tile
+    auto expand = [&](int r, const unsigned char* codes, const unsigned char* shift, int nibble, const int* fact, unsigned char* dst) {
+      const uint4 v = *reinterpret_cast<const uint4*>(codes);
+      uint32_t s = (uint32_t)*shift >> (4 * nibble) & 15u;
+      if (fact[0]) s = (r < fact[1] || (r >= fact[2] && r < fact[3])) && ((fact[4] >> (r >> 4)) & 1) ? s : 0u;      // what absent rows hold is no NaN
+      const uint2 t = s_table[s];
+      const uint2 x0 = paged4_expand(v.x, t), x1 = paged4_expand(v.y, t), x2 = paged4_expand(v.z, t), x3 = paged4_expand(v.w, t);
+      *reinterpret_cast<uint4*>(dst) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+      unsigned char* other = base_ptr + ((uint32_t)(dst - base_ptr) ^ 16u);
+      *reinterpret_cast<uint4*>(other) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+    };
+    // a 128 (64) columns wide part of 128 rows: 512 (256) units
+    auto expand_part = [&](const unsigned char* codes, const unsigned char* shifts, const int* fact, unsigned char* dst, auto width) {
+      constexpr int W = decltype(width)::value, U = W / 32;
 #pragma unroll
-      for (int k = 0; k < DEPTH; ++k) {
-        if (!ok || !d[k].any) break;
-        Rows y;
-        rows_of(ahead, y);
-        look(ahead);
-        if constexpr (PL::MLA) {
+      for (int i = 0; i < U * 128 / (32 * PL::EW); ++i) {
+        const int x = et + 32 * PL::EW * i, r = x / U, u = x % U;
+        expand(r, codes + x * 16, shifts + r * (W / 64) + (u >> 1), u & 1, fact, dst + swz<W>(r, 2 * u));
+      }
+    };
+    using W128 = std::integral_constant<int, 128>;
+    using W64 = std::integral_constant<int, 64>;
+    using WPOS = std::integral_constant<int, DP>;
+#pragma unroll 1
+    for (int t = 0; t < n_tiles; ++t) {
+      const uint32_t buf = t & 1, before = ((t >> 1) - 1) & 1;
+      unsigned char* tile = base_ptr + buf * PL::TILE;
+      if constexpr (PL::MLA && DS == 512) {
+        if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
+#pragma unroll 1
+        for (int s = 0; s < 4; ++s) {
+          if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
+          const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
+          const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
+          // a warp takes two rows at a time; its quarter q the chunk q of the first and q ^ 1 of the second
 #pragma unroll
-          for (int c = 0; c < NV; ++c) {
-            begin_slot();
-            if (!ok) break;
-            put_sem(c, d[k]);
-            end_slot();
-            load_sem(y, c, d[k]);
+          for (int i = 0; i < 2; ++i) {
+            const int r = 2 * (ew + 8 * i) + ((lane >> 2) & 1), c = (lane >> 3) ^ ((lane >> 2) & 1), u = lane & 3;
+            expand(r, st + r * 256 + c * 64 + u * 16, st + PL::ST_SHS + r * 8 + c * 2 + (u >> 1), u & 1, fact, tile + c * 16384 + swz<128>(32 * s + r, 2 * u));
           }
-          if (!ok) break;
-          begin_slot();
-          if (!ok) break;
-          put_pos(d[k]);
-          end_slot();
-          load_pos(y, d[k]);
-        } else {
-          begin_slot();
-          if (!ok) break;
-          put_pos(d[k]);
-          end_slot();
-          load_pos(y, d[k]);
-          begin_slot();
-          if (!ok) break;
-          put_sem(0, d[k]);
-          end_slot();
-          load_sem(y, 0, d[k]);
+          if ((ew >> 1) == s) {                              // the keys' 64 units: two of the warps in turn
+            const int x = (ew & 1) * 32 + lane, r = x >> 1, u = x & 1;
+            expand(r, st + PL::ST_POS + x * 16, st + PL::ST_SHP + r, u, fact, tile + 4 * 16384 + swz<64>(32 * s + r, 2 * u));
+          }
+          signal(GEMPTY(stage));
+          if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
         }
-        d[k].any = y.any;
+        if (!ok) break;
+        fence_proxy_async_smem();
+        signal(KFULL(buf));
+      } else {
+        if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
+        const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
+        const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
+        if (t > 1 && !wait(PL::MLA ? PVDONE(buf) : SFULL(buf), before, ERR_WAIT_O_DONE)) break;
+        expand_part(st + PL::ST_POS, st + PL::ST_SHP, fact, tile + PL::KSEM * 16384, WPOS());
+        if constexpr (!PL::MLA) {
+          fence_proxy_async_smem();
+          signal(KFULL(buf));
+          if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
+        }
+        if constexpr (PL::VW == 128) expand_part(st, st + PL::ST_SHS, fact, tile + (PL::MLA ? 0 : PL::K_BYTES), W128());
+        else expand_part(st, st + PL::ST_SHS, fact, tile + PL::K_BYTES, W64());
+        signal(GEMPTY(stage));
+        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
+        fence_proxy_async_smem();
+        signal(PL::MLA ? KFULL(buf) : VFULL(buf));
       }
     }
   } else if (warp == W_MMA) {
@@ -403,66 +391,50 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     const uint32_t leader = elect_one();
     constexpr uint32_t ID_S = umma_idesc_f8(128, 2 * NH, 0, false, false);
     constexpr uint32_t ID_O = umma_idesc_f8(128, 2 * NH, 0, true, true);
-    int s_slot = 0, v_slot = 0;                              // first slots of the tiles whose S and O come next
-    uint32_t s_phase = 0, v_phase = 0, g = 0, seg = 0;
-    bool ok = true;
-    auto wait_slot = [&](int first, uint32_t ph, int c) {    // chunk c of the tile whose slots begin at `first`
-      const int s = first + c >= PL::SLOTS ? first + c - PL::SLOTS : first + c;
-      ok = ok && mbar_wait(FULL(s), first + c >= PL::SLOTS ? ph ^ 1 : ph, abort_flag);
+    uint32_t g = 0, seg = 0;
+    bool ok = !*abort_flag;
+    auto wait = [&](uint32_t bar, uint32_t ph, int code) {
+      ok = ok && mbar_wait(bar, ph, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
-      if (!ok && lane == 0) fail(ERR_WAIT_KV_FULL);
-      return s;
+      if (!ok && lane == 0) fail(code);
+      return ok;
     };
-    auto advance = [&](int& first, uint32_t& ph) { first += PL::PER_TILE; if (first >= PL::SLOTS) { first -= PL::SLOTS; ph ^= 1; } };
-    auto issue_s = [&](uint32_t buf) {
-      const uint32_t d = tmem + PL::TM_S + buf * 2 * NH;
+    auto issue_s = [&](uint32_t t) {
+      const uint32_t buf = t & 1, d = tmem + PL::TM_S + buf * 2 * NH, tile = base + buf * PL::TILE;
+      if (!wait(KFULL(buf), (t >> 1) & 1, ERR_WAIT_KV_FULL)) return;
+      tc_fence_after();
       uint32_t acc = 0;
 #pragma unroll
       for (int c = 0; c < NK; ++c) {
-        const int s = wait_slot(s_slot, s_phase, c);
-        if (!ok) return;
-        tc_fence_after();
         const int width = c < PL::KSEM ? 128 : DP;
-        const uint64_t ad = desc_rows(base + s * PL::SLOT, width, 16);
-        const uint64_t bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
+        const uint64_t ad = desc_rows(tile + c * 16384, width, 16), bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
 #pragma unroll
         for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
-        if (!PL::MLA || c == PL::KSEM) umma_commit_elected(leader, EMPTY(s));
       }
-      advance(s_slot, s_phase);
       umma_commit_elected(leader, SFULL(buf));
     };
     while (ok && w.next(p)) {
-      ok = mbar_wait(QFULL, seg & 1, abort_flag);
-      ok = __all_sync(0xffffffffu, ok);
-      if (!ok) { if (lane == 0) fail(ERR_WAIT_Q); break; }
+      if (!wait(QFULL, seg & 1, ERR_WAIT_Q)) break;
       ++seg;
       tc_fence_after();
-      issue_s(g & 1);
+      issue_s(g);
       for (int j = 0; j < w.n && ok; ++j, ++g) {
-        if (j + 1 < w.n) issue_s((g + 1) & 1);
-        if (!ok) break;
-        ok = mbar_wait(PFULL(g & 1), (g >> 1) & 1, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) { if (lane == 0) fail(ERR_WAIT_P_FULL); break; }
+        if (j + 1 < w.n) issue_s(g + 1);
+        const uint32_t buf = g & 1;
+        if (!PL::MLA && !wait(VFULL(buf), (g >> 1) & 1, ERR_WAIT_KV_FULL)) break;
+        if (!wait(PFULL(buf), (g >> 1) & 1, ERR_WAIT_P_FULL)) break;
         tc_fence_after();
-        const uint64_t pd = desc_rows(base + PL::OFF_P + (g & 1) * PL::P_BYTES, 2 * NH, 128);
+        const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
 #pragma unroll
         for (int c = 0; c < NV; ++c) {
-          const int s = wait_slot(v_slot, v_phase, PL::V0 + c);
-          if (!ok) break;
-          tc_fence_after();
-          // 64-wide values: M stays 128, the second half of the operand is the unused half of the slot and the output
+          // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
           // lanes it feeds are never read
-          const uint64_t ad = desc_rows(base + s * PL::SLOT, PL::VW, 8192);
+          const uint64_t ad = desc_rows(base + buf * PL::TILE + (PL::MLA ? c * 16384 : PL::K_BYTES), PL::VW, 8192);
 #pragma unroll
           for (int k = 0; k < 4; ++k)
             umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (j > 0 || k > 0) ? 1u : 0u);
-          umma_commit_elected(leader, EMPTY(s));
         }
-        if (!ok) break;
-        advance(v_slot, v_phase);
-        umma_commit_elected(leader, PVDONE(g & 1));
+        umma_commit_elected(leader, PVDONE(buf));
       }
     }
   } else {
@@ -470,28 +442,10 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     const int grp = warp >> 2, quad = warp & 3, t = tid & 127, hb = ROWS * grp;    // this thread: key t of a tile, rows hb .. hb + ROWS - 1
     const uint32_t lane_base = (uint32_t)(quad * 32) << 16;
     uint32_t g = 0, seg = 0;
-    bool ok = true;
+    bool ok = !*abort_flag;
     float l[ROWS];
-    int pg0 = -1, pg1 = -1;                                  // page of this thread's key in the current tile and in the next one
-    int ke = 0, ve = 0;                                      // exponents of pg0's row
-    auto page_of = [&](const Walk& u, int j) {               // -1: none
-      if (j >= u.n) return -1;
-      const int x = u.t.row0(u.t0 + j) + t;
-      if (!u.t.s.has(x)) return -1;                          // has() implies x below the table's end
-      const int pg = p.table[(size_t)u.b * p.width + (x >> p.page_log2)];
-      return pg >= 0 && pg < p.n_pages ? pg : -1;
-    };
-    auto exps_of = [&](int pg, int hk, int& k, int& v) {
-      k = v = 0;
-      if (pg < 0) return;
-      const size_t r = (((size_t)pg * p.Hkv + hk) << p.page_log2) + (t & (p.page - 1));
-      v = a.exp_v[r];
-      k = PL::MLA ? v : a.exp_k[r];
-    };
-    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them; the first lookups of the
-    // piece run underneath
+    // splits this group's query rows of a unit into e4m3 terms and writes them where S reads them
     auto load_q = [&](const Walk& u, uint32_t which) {
-      pg0 = page_of(u, 0); pg1 = page_of(u, 1);
       constexpr int VS = PL::KSEM * 16, VQ = VS + DP / 8, NL = (VQ + 31) / 32;   // 8-element vectors of a row
       const int n_rows = p.q_len * p.rep - u.blk * NH;
 #pragma unroll 2
@@ -533,7 +487,6 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
           s_row[(which & 1) * NH + r] = r < n_rows ? row : -1;
         }
       }
-      exps_of(pg0, u.hk, ke, ve);
       fence_proxy_async_smem();
       mbar_arrive(QFULL);
       group_sync(grp);
@@ -550,11 +503,14 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
         const uint32_t buf = g & 1;
-        const bool valid = pg0 >= 0;
-        // the next tile's exponents and the page after that are on their way while this tile is worked on
-        int ke1, ve1;
-        exps_of(pg1, w.hk, ke1, ve1);
-        const int pg2 = page_of(w, j + 2);
+        ok = mbar_wait(FFULL(g & 3), (g >> 2) & 1, abort_flag);
+        if (!ok) fail(ERR_WAIT_KV_FULL);
+        __syncwarp();
+        const unsigned char* fact = s_fact + (g & 3) * PL::FACT;
+        const int ve = fact[t], ke = PL::MLA ? ve : fact[128 + t];
+        const bool valid = ((*reinterpret_cast<const uint32_t*>(fact + 256) >> (t >> 4)) & 1u) && sp.has(x);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(FEMPTY(g & 3));
         // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 f_v + T): both are multiples of e = 2^(y - M + half), half way
         // between them, so that neither is lost below 2^-126 where the factors of a sequence span more than fp32 does.
         const float half = 0.5f * ((float)paged4_log2_factor(ve) + paged8_t_bits(NH)), f_t = ex2(half), f_l = ex2(paged8_t_bits(NH) - half);
@@ -663,7 +619,6 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         fence_proxy_async_smem();
         tc_fence_before();
         mbar_arrive(PFULL(buf));
-        pg0 = pg1; pg1 = pg2; ke = ke1; ve = ve1;
       }
       // ---- this piece is done: its sums and maxima, then the next unit's queries (S of this piece is complete), then O
       const bool whole = w.n == w.t.n;

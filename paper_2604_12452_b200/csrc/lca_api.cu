@@ -105,7 +105,8 @@ static int check_paged_pool(const lca_params* p, const lca_paged8* c) {
 static int check_paged_pool(const lca_params* p, const lca_paged4* c) {
   if (!c->pages_sem || !c->pages_pos || !c->shift_sem || !c->shift_pos || !c->exp_sem) return LCA_ERR_INVALID_ARG;
   if ((p->variant == LCA_VARIANT_GQA) != (c->exp_pos != nullptr)) return LCA_ERR_INVALID_ARG;
-  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos) || !aligned16(c->shift_sem) || !aligned16(c->shift_pos)) return LCA_ERR_MISALIGNED;
+  if (!aligned16(c->pages_sem) || !aligned16(c->pages_pos) || !aligned16(c->shift_sem) || !aligned16(c->shift_pos) ||
+      !aligned16(c->exp_sem) || !aligned16(c->exp_pos)) return LCA_ERR_MISALIGNED;
   if ((int64_t)c->n_pages * p->n_kv_heads > 0x7fffffffll) return LCA_ERR_INVALID_ARG;
   if (!simt_shape_ok(p)) return LCA_ERR_UNSUPPORTED_SHAPE;
   return LCA_OK;

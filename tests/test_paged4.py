@@ -36,7 +36,7 @@ def test_write_and_read_refusals(B, p):
         call = lambda c=None, sem=16, pos=16, slots=16, n=8, q=None: fn(q or p, c or cache(B), sem, pos, slots, n)  # noqa: E731
         assert call(sem=None) == -1 and call(pos=None) == -1 and call(slots=None) == -1 and call(n=-1) == -1 and call(n=1 << 31) == -1
         assert call(n=0) == 0
-        assert call(sem=24) == -3 and call(pos=24) == -3 and call(c=cache(B, pages_sem=24)) == -3 and call(c=cache(B, shift_pos=20)) == -3
+        assert call(sem=24) == -3 and call(pos=24) == -3 and call(c=cache(B, pages_sem=24)) == -3 and call(c=cache(B, shift_pos=20)) == -3 and call(c=cache(B, exp_sem=24)) == -3
         for k in ("pages_sem", "pages_pos", "shift_sem", "shift_pos", "exp_sem"):
             assert call(c=cache(B, **{k: None})) == -1, k
         assert call(c=cache(B, exp_pos=16)) == -1                             # MLA: one exponent for both
