@@ -19,12 +19,20 @@
 // Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
 #include <cstring>
 
-#include "attn_paged4.cuh"
+#include "attn_paged8.cuh"
+#include "fp4_common.cuh"
 
 namespace lca {
 using namespace tc;
 
 static __device__ int g_paged4_status = 0;
+
+struct Paged4Params {
+  Paged8Params b;             // without the tensor maps and the scales
+  const uint8_t* sem; const uint8_t* pos;
+  const uint8_t* shift_sem; const uint8_t* shift_pos;
+  const uint8_t* exp_k; const uint8_t* exp_v;
+};
 
 // --------------------------------------------------------------------------------------------------- scalar kernel
 // One warp per query row, keys one by one, fp32: the cross-check of the tensor-core kernel (lca_set_attention_impl(1)).
@@ -157,22 +165,8 @@ __device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, ui
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// A bounded wait that leaves its issue slots to the others: the hardware is told to suspend the thread for up to 2 us at a time.
-// (Every warp of this kernel waits for most of a tile; polling as fast as possible took a quarter of all issue slots.)
-__device__ __forceinline__ bool wait_suspended(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  auto poll = [&]() {
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
-    return done != 0;
-  };
-  if (poll()) return true;
-  const long long t0 = clock64();
-  while (true) {
-    if (poll()) return true;
-    if (*abort_flag || clock64() - t0 > WAIT_TIMEOUT_CYCLES) return false;
-  }
-}
+static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
+static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
@@ -264,7 +258,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       const unsigned pages = __ballot_sync(0xffffffffu, c.page_ok) & 0xffu;
       const bool part = !(pages == 0xffu && (c.lo >= 128 || (c.mid <= 0 && c.hi >= 128)));
       const int f = (int)(g & 3);
-      ok = wait_suspended(FEMPTY(f), ((g >> 2) & 1) ^ 1, abort_flag);
+      ok = mbar_wait(FEMPTY(f), ((g >> 2) & 1) ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
       {
@@ -281,7 +275,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       }
 #pragma unroll 1
       for (int s = 0; s < PL::SLABS; ++s) {
-        ok = wait_suspended(GEMPTY(stage), phase ^ 1, abort_flag);
+        ok = mbar_wait(GEMPTY(stage), phase ^ 1, abort_flag);
         ok = __all_sync(0xffffffffu, ok);
         if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
         constexpr int GR = PL::SLAB / 16, B_SEM = DS / 2, B_POS = DP / 2, B_SHS = DS / 64, B_SHP = DP / 64;
@@ -307,15 +301,15 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     }
   } else if (warp >= W_EXP && warp < W_MMA) {
     // ----------------------------------------------------------------------------------------------- expansion
-    // A thread takes 32 values (16 bytes of codes) of a row at a time, a few of them from a slab: all are read, the slab is given back,
-    // then they are expanded.  Eight neighbouring lanes write two rows, so that their units fall on all banks of the swizzled image.
+    // A thread takes 32 values (16 bytes of codes) of a row at a time.  Eight neighbouring lanes write two rows, so that their
+    // units fall on all banks of the swizzled image.
     const int et = tid - 32 * W_EXP, ew = warp - W_EXP;
     const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
     bool ok = !*abort_flag;
     int stage = 0;
     uint32_t phase = 0;
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      if (ok && !wait_suspended(bar, ph, abort_flag)) { fail(code); ok = false; }
+      if (ok && !mbar_wait(bar, ph, abort_flag)) { fail(code); ok = false; }
       ok = __all_sync(0xffffffffu, ok);
       return ok;
     };
@@ -323,98 +317,71 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    struct Unit { uint4 v; uint2 t; };
-    struct Facts { bool part; int lo, mid, hi, pages; };
-    auto facts_of = [&](const unsigned char* st) {
-      const int4 f = *reinterpret_cast<const int4*>(st + PL::ST_FACT);
-      return Facts{f.x != 0, f.y, f.z, f.w, *reinterpret_cast<const int*>(st + PL::ST_FACT + 16)};
-    };
-    auto read = [&](Unit& x, int r, const unsigned char* codes, const unsigned char* shift, int nibble, const Facts& f) {
-      x.v = *reinterpret_cast<const uint4*>(codes);
+    // units `first`, `first` + step ...: N of them; `at`: codes and shift of unit i, row in the slab and place in the tile
+    auto expand = [&](int r, const unsigned char* codes, const unsigned char* shift, int nibble, const int* fact, unsigned char* dst) {
+      const uint4 v = *reinterpret_cast<const uint4*>(codes);
       uint32_t s = (uint32_t)*shift >> (4 * nibble) & 15u;
-      if (f.part) s = (r < f.lo || (r >= f.mid && r < f.hi)) && ((f.pages >> (r >> 4)) & 1) ? s : 0u;      // what absent rows hold is no NaN
-      x.t = s_table[s];
+      if (fact[0]) s = (r < fact[1] || (r >= fact[2] && r < fact[3])) && ((fact[4] >> (r >> 4)) & 1) ? s : 0u;      // what absent rows hold is no NaN
+      const uint2 t = s_table[s];
+      const uint2 x0 = paged4_expand(v.x, t), x1 = paged4_expand(v.y, t), x2 = paged4_expand(v.z, t), x3 = paged4_expand(v.w, t);
+      *reinterpret_cast<uint4*>(dst) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+      unsigned char* other = base_ptr + ((uint32_t)(dst - base_ptr) ^ 16u);
+      *reinterpret_cast<uint4*>(other) = make_uint4(x2.x, x2.y, x3.x, x3.y);
     };
-    auto put = [&](const Unit& x, uint32_t dst) {            // dst: from the start of shared memory
-      const uint2 x0 = paged4_expand(x.v.x, x.t), x1 = paged4_expand(x.v.y, x.t), x2 = paged4_expand(x.v.z, x.t), x3 = paged4_expand(x.v.w, x.t);
-      *reinterpret_cast<uint4*>(base_ptr + dst) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-      *reinterpret_cast<uint4*>(base_ptr + (dst ^ 16u)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-    };
-    if constexpr (PL::SLAB == 32) {
-      // MLA 512 + 64: a warp takes two rows of latents at a time, its quarter q the chunk q of the first and q ^ 1 of the second; the keys' 64
-      // units of slab s are those of warps 2 s and 2 s + 1.  The next slab is read before this one is expanded.
-      const int rr = 2 * ew + ((lane >> 2) & 1), c = (lane >> 3) ^ ((lane >> 2) & 1), u = lane & 3;
-      const int xp = (ew & 1) * 32 + lane;
-      const uint32_t to = c * 16384 + swz<128>(rr, 2 * u), to_pos = 4 * 16384 + swz<64>(xp >> 1, 2 * (xp & 1));
-      Unit a0, a1, ap, b0, b1, bp;
-      auto read_slab = [&](int s, Unit& x0, Unit& x1, Unit& xk) {
-        if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) return;
-        const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
-        const Facts f = facts_of(st);
-        read(x0, rr, st + rr * 256 + c * 64 + u * 16, st + PL::ST_SHS + rr * 8 + c * 2 + (u >> 1), u & 1, f);
-        read(x1, rr + 16, st + (rr + 16) * 256 + c * 64 + u * 16, st + PL::ST_SHS + (rr + 16) * 8 + c * 2 + (u >> 1), u & 1, f);
-        if ((ew >> 1) == s) read(xk, xp >> 1, st + PL::ST_POS + xp * 16, st + PL::ST_SHP + (xp >> 1), xp & 1, f);
-        signal(GEMPTY(stage));
-        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
-      };
-      auto put_slab = [&](int s, uint32_t tile, const Unit& x0, const Unit& x1, const Unit& xk) {
-        put(x0, tile + to + s * 32 * 128);
-        put(x1, tile + to + s * 32 * 128 + 16 * 128);
-        if ((ew >> 1) == s) put(xk, tile + to_pos + s * 32 * 64);
-      };
-      if (n_tiles > 0) read_slab(0, a0, a1, ap);
-#pragma unroll 1
-      for (int t = 0; t < n_tiles && ok; ++t) {
-        const uint32_t buf = t & 1, tile = buf * PL::TILE;
-        if (t > 1 && !wait(PVDONE(buf), ((t >> 1) - 1) & 1, ERR_WAIT_O_DONE)) break;
+    // a 128 (64) columns wide part of 128 rows: 512 (256) units
+    auto expand_part = [&](const unsigned char* codes, const unsigned char* shifts, const int* fact, unsigned char* dst, auto width) {
+      constexpr int W = decltype(width)::value, U = W / 32;
 #pragma unroll
-        for (int s = 0; s < 4; s += 2) {
-          read_slab(s + 1, b0, b1, bp);
-          put_slab(s, tile, a0, a1, ap);
-          if (s == 0 || t + 1 < n_tiles) read_slab((s + 2) & 3, a0, a1, ap);
-          put_slab(s + 1, tile, b0, b1, bp);
+      for (int i = 0; i < U * 128 / (32 * PL::EW); ++i) {
+        const int x = et + 32 * PL::EW * i, r = x / U, u = x % U;
+        expand(r, codes + x * 16, shifts + r * (W / 64) + (u >> 1), u & 1, fact, dst + swz<W>(r, 2 * u));
+      }
+    };
+    using W128 = std::integral_constant<int, 128>;
+    using W64 = std::integral_constant<int, 64>;
+    using WPOS = std::integral_constant<int, DP>;
+#pragma unroll 1
+    for (int t = 0; t < n_tiles; ++t) {
+      const uint32_t buf = t & 1, before = ((t >> 1) - 1) & 1;
+      unsigned char* tile = base_ptr + buf * PL::TILE;
+      if constexpr (PL::MLA && DS == 512) {
+        if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
+#pragma unroll 1
+        for (int s = 0; s < 4; ++s) {
+          if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
+          const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
+          const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
+          // a warp takes two rows at a time; its quarter q the chunk q of the first and q ^ 1 of the second
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const int r = 2 * (ew + 8 * i) + ((lane >> 2) & 1), c = (lane >> 3) ^ ((lane >> 2) & 1), u = lane & 3;
+            expand(r, st + r * 256 + c * 64 + u * 16, st + PL::ST_SHS + r * 8 + c * 2 + (u >> 1), u & 1, fact, tile + c * 16384 + swz<128>(32 * s + r, 2 * u));
+          }
+          if ((ew >> 1) == s) {                              // the keys' 64 units: two of the warps in turn
+            const int x = (ew & 1) * 32 + lane, r = x >> 1, u = x & 1;
+            expand(r, st + PL::ST_POS + x * 16, st + PL::ST_SHP + r, u, fact, tile + 4 * 16384 + swz<64>(32 * s + r, 2 * u));
+          }
+          signal(GEMPTY(stage));
+          if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
         }
+        if (!ok) break;
         fence_proxy_async_smem();
         signal(KFULL(buf));
-      }
-    } else {
-      // a chunk of 128 (64) columns has 512 (256) units of its 128 rows
-      constexpr int UP = DP / 32, NP = UP * 128 / (32 * PL::EW), US = PL::VW / 32, NS = US * 128 / (32 * PL::EW);
-#pragma unroll 1
-      for (int t = 0; t < n_tiles; ++t) {
-        const uint32_t buf = t & 1, before = ((t >> 1) - 1) & 1, tile = buf * PL::TILE;
+      } else {
         if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
         const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
-        const Facts f = facts_of(st);
-        Unit k[NP], v[NS];
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int x = et + 32 * PL::EW * i, r = x / UP, u = x % UP;
-          read(k[i], r, st + PL::ST_POS + x * 16, st + PL::ST_SHP + r * (DP / 64) + (u >> 1), u & 1, f);
-        }
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          const int x = et + 32 * PL::EW * i, r = x / US, u = x % US;
-          read(v[i], r, st + x * 16, st + PL::ST_SHS + r * (PL::VW / 64) + (u >> 1), u & 1, f);
-        }
-        signal(GEMPTY(stage));
-        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
+        const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
         if (t > 1 && !wait(PL::MLA ? PVDONE(buf) : SFULL(buf), before, ERR_WAIT_O_DONE)) break;
-#pragma unroll
-        for (int i = 0; i < NP; ++i) {
-          const int x = et + 32 * PL::EW * i;
-          put(k[i], tile + PL::KSEM * 16384 + swz<DP>(x / UP, 2 * (x % UP)));
-        }
+        expand_part(st + PL::ST_POS, st + PL::ST_SHP, fact, tile + PL::KSEM * 16384, WPOS());
         if constexpr (!PL::MLA) {
           fence_proxy_async_smem();
           signal(KFULL(buf));
           if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
         }
-#pragma unroll
-        for (int i = 0; i < NS; ++i) {
-          const int x = et + 32 * PL::EW * i;
-          put(v[i], tile + (PL::MLA ? 0 : PL::K_BYTES) + swz<PL::VW>(x / US, 2 * (x % US)));
-        }
+        if constexpr (PL::VW == 128) expand_part(st, st + PL::ST_SHS, fact, tile + (PL::MLA ? 0 : PL::K_BYTES), W128());
+        else expand_part(st, st + PL::ST_SHS, fact, tile + PL::K_BYTES, W64());
+        signal(GEMPTY(stage));
+        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
         fence_proxy_async_smem();
         signal(PL::MLA ? KFULL(buf) : VFULL(buf));
       }
@@ -427,7 +394,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     uint32_t g = 0, seg = 0;
     bool ok = !*abort_flag;
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      ok = ok && wait_suspended(bar, ph, abort_flag);
+      ok = ok && mbar_wait(bar, ph, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) fail(code);
       return ok;
@@ -446,43 +413,28 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       }
       umma_commit_elected(leader, SFULL(buf));
     };
-    auto issue_o = [&](uint32_t t, bool first) {
-      const uint32_t buf = t & 1;
-      if (!PL::MLA && !wait(VFULL(buf), (t >> 1) & 1, ERR_WAIT_KV_FULL)) return;
-      tc_fence_after();
-      const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
-#pragma unroll
-      for (int c = 0; c < NV; ++c) {
-        // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
-        // lanes it feeds are never read
-        const uint64_t ad = desc_rows(base + buf * PL::TILE + (PL::MLA ? c * 16384 : PL::K_BYTES), PL::VW, 8192);
-#pragma unroll
-        for (int k = 0; k < 4; ++k)
-          umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (!first || k > 0) ? 1u : 0u);
-      }
-      umma_commit_elected(leader, PVDONE(buf));
-    };
     while (ok && w.next(p)) {
       if (!wait(QFULL, seg & 1, ERR_WAIT_Q)) break;
       ++seg;
       tc_fence_after();
       issue_s(g);
-      // Of the next tile's S and this tile's O whichever can go first: with two expanded tiles, keys that are late must not
-      // hold up the product whose completion the expansion waits for.
-#pragma unroll 1
       for (int j = 0; j < w.n && ok; ++j, ++g) {
-        bool s_left = j + 1 < w.n, o_left = true;
-        const long long t0 = clock64();
-        while (o_left && ok) {
-          if (s_left && __all_sync(0xffffffffu, mbar_try(KFULL((g + 1) & 1), ((g + 1) >> 1) & 1))) { issue_s(g + 1); s_left = false; }
-          if (s_left ? __all_sync(0xffffffffu, mbar_try(PFULL(g & 1), (g >> 1) & 1)) : wait(PFULL(g & 1), (g >> 1) & 1, ERR_WAIT_P_FULL)) {
-            if (ok) issue_o(g, j == 0);
-            o_left = false;
-          }
-          if (o_left && (*abort_flag || clock64() - t0 > WAIT_TIMEOUT_CYCLES)) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
-          ok = __all_sync(0xffffffffu, ok);
+        if (j + 1 < w.n) issue_s(g + 1);
+        const uint32_t buf = g & 1;
+        if (!PL::MLA && !wait(VFULL(buf), (g >> 1) & 1, ERR_WAIT_KV_FULL)) break;
+        if (!wait(PFULL(buf), (g >> 1) & 1, ERR_WAIT_P_FULL)) break;
+        tc_fence_after();
+        const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+          // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
+          // lanes it feeds are never read
+          const uint64_t ad = desc_rows(base + buf * PL::TILE + (PL::MLA ? c * 16384 : PL::K_BYTES), PL::VW, 8192);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (j > 0 || k > 0) ? 1u : 0u);
         }
-        if (s_left && ok) issue_s(g + 1);
+        umma_commit_elected(leader, PVDONE(buf));
       }
     }
   } else {
@@ -551,7 +503,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
         const uint32_t buf = g & 1;
-        ok = wait_suspended(FFULL(g & 3), (g >> 2) & 1, abort_flag);
+        ok = mbar_wait(FFULL(g & 3), (g >> 2) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_KV_FULL);
         __syncwarp();
         const unsigned char* fact = s_fact + (g & 3) * PL::FACT;
@@ -566,7 +518,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         const float offset = weight_offset(x);
         const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
 
-        ok = wait_suspended(SFULL(buf), (g >> 1) & 1, abort_flag);
+        ok = mbar_wait(SFULL(buf), (g >> 1) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_S_FULL);
         __syncwarp();
         tc_fence_after();
@@ -619,11 +571,11 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
           for (int i = 0; i < ROWS; ++i) { z[i] -= s_d[hb + i]; l[i] *= s_f[hb + i]; }
         }
         if (g > 1) {                                         // the weights of the tile before the last one have been read
-          ok = wait_suspended(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
+          ok = mbar_wait(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
         }
         if (raise && j > 0) {                                // O is complete up to the last tile
-          ok = wait_suspended(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
+          ok = mbar_wait(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
           __syncwarp();
           tc_fence_after();
@@ -693,7 +645,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       group_sync(grp);
       more = w.next(p);
       if (more) load_q(w, seg + 1);
-      ok = wait_suspended(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
+      ok = mbar_wait(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
       tc_fence_after();
@@ -754,10 +706,8 @@ template <bool MLA, int DS, int DP>
 static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
   const long long rows = (long long)P.b.q_len * P.b.rep;
   if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
-  if constexpr (MLA) {
-    if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
-    if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);
-  }
+  if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
+  if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);
   return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 2, 8>>(P, stream);
 }
 
@@ -806,7 +756,6 @@ int attn_paged4_launch(const Paged4Attn& q) {
   const size_t part_bytes = (size_t)2 * b.grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float);
   b.prefix = reinterpret_cast<long long*>(reinterpret_cast<char*>(b.part) + (part_bytes + 15) / 16 * 16);
   if ((long long)b.B * b.Hkv * b.n_blk * ((long long)nh * p->d_sem / 512) > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
-  if (p->variant == LCA_VARIANT_GQA && (long long)b.q_len * b.rep <= 8) return attn_paged4_few_launch(p, P, q.stream);
   if (p->variant == LCA_VARIANT_MLA) return p->d_sem == 512 ? paged4_launch_rows<true, 512, 64>(P, nh, q.stream)
                                                             : paged4_launch_rows<true, 128, 64>(P, nh, q.stream);
   return p->d_sem == 128 ? paged4_launch_rows<false, 128, 128>(P, nh, q.stream) : paged4_launch_rows<false, 64, 64>(P, nh, q.stream);

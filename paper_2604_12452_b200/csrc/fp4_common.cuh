@@ -53,6 +53,16 @@ __device__ __forceinline__ uint2 paged4_expand(uint32_t w, const uint2& table) {
                     __byte_perm(table.x, table.y, m >> 16) | ((w << 4) & 0x80808080u));
 }
 
+// The same with the two shifts as multiplications, on the pipe that the permutations and masks leave idle; `sixteen` is 16, which the
+// compiler must not know.
+__device__ __forceinline__ uint2 paged4_expand(uint32_t w, const uint2& table, uint32_t sixteen) {
+  const uint32_t m = w & 0x77777777u;
+  uint32_t up, hi;
+  asm("mul.lo.u32 %0, %1, %2;" : "=r"(up) : "r"(w), "r"(sixteen));
+  asm("mul.hi.u32 %0, %1, %2;" : "=r"(hi) : "r"(m), "r"(sixteen << 12));
+  return make_uint2(__byte_perm(table.x, table.y, m) | (w & 0x80808080u), __byte_perm(table.x, table.y, hi) | (up & 0x80808080u));
+}
+
 // Eight values to a word: nearest magnitude, ties to the even index; infinities become 6.
 __device__ __forceinline__ uint32_t paged4_pack(const float (&f)[8]) {
   uint32_t w;
