@@ -663,7 +663,7 @@ def new_paged8_cache(params: LcaParams, n_pages: int, page_size: int, table_widt
 
 # The helpers below are called for every step of every layer: ctypes takes the structures as they are (the declared argument
 # types make it pass their address), which costs half of what C.byref does.
-_I32, _F32, _BF16 = torch.int32, torch.float32, torch.bfloat16
+_I32, _F32, _F64, _BF16 = torch.int32, torch.float32, torch.float64, torch.bfloat16
 
 
 def _arg(x, dtype, n, dev):
@@ -876,11 +876,11 @@ def decode_update_paged4(params: LcaParams, cache: LcaPaged4, q_tail_sem, q_tail
 
 
 # ------------------------------------------------------------------------------------------- around a speculative step
-def _device(device, where: str):
+def _device(x, where: str):
     """Index of the CUDA device of a tensor, which has to be the current one."""
-    dev = device.index
-    if device.type != "cuda" or dev != torch.cuda.current_device():
-        raise ValueError(f"{where} takes tensors on the current CUDA device, not on {device}")
+    dev = x.get_device()
+    if dev < 0 or dev != torch.cuda.current_device():
+        raise ValueError(f"{where} takes tensors on the current CUDA device, not on {x.device}")
     return dev
 
 
@@ -899,6 +899,15 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, kind: int = ROPE_PLAIN
 _ROPE_TYPES = {torch.bfloat16: LCA_DTYPE_BF16, torch.float32: LCA_DTYPE_FP32}
 
 
+def _heads(v, T, d, dtype, dev):
+    """(heads, address, token stride, head stride) of a tensor [T, heads, d] whose columns lie side by side."""
+    shape, strides = v.shape, v.stride()
+    if len(shape) != 3 or shape[0] != T or shape[2] != d or (strides[2] != 1 and d > 1) or v.dtype is not dtype or v.get_device() != dev:
+        raise ValueError(f"expected [T, heads, {d}] of {dtype} on cuda:{dev} with neighbouring columns, T = {T}, not "
+                         f"{v.dtype} {list(shape)} with strides {list(strides)} on {v.device}")
+    return shape[1], v.data_ptr(), strides[0], strides[1]
+
+
 def rope(q, k, positions, freqs, interleaved: bool = False, inverse: bool = False, factor: float = 1.0, q_out=None, k_out=None, stream=None):
     """Rotate q [T, heads, d] and k [T, kv_heads, d] (either may be None) by the angles positions [T] int32 times freqs [rot / 2]
     float64: columns 0 .. rot - 1 of every head, the others are copied.  The tensors may be views (slices of a projection) as long
@@ -907,35 +916,29 @@ def rope(q, k, positions, freqs, interleaved: bool = False, inverse: bool = Fals
     if x is None:
         raise ValueError("rope takes queries, keys or both")
     T, _, d = x.shape
-    dev = _device(x.device, "rope")
-    code = _ROPE_TYPES.get(x.dtype)
+    dtype, dev = x.dtype, _device(x, "rope")
+    code = _ROPE_TYPES.get(dtype)
     if code is None:
-        raise ValueError(f"rope takes bfloat16 or float32, not {x.dtype}")
-    rot = 2 * freqs.numel()
-    a = LcaRopeArgs(code, bool(interleaved), bool(inverse), 0, 0, d, rot, factor, T, _arg(positions, _I32, T, dev),
-                    _arg(freqs, torch.float64, 1, dev))
-    outs = []
+        raise ValueError(f"rope takes bfloat16 or float32, not {dtype}")
+    parts, outs = [], []
     for t, o in ((q, q_out), (k, k_out)):
         if t is None:
+            parts.append((0,) + 6 * (None,))
             outs.append(None)
             continue
         if o is None:
-            o = _new(torch.empty, tuple(t.shape), t.dtype, t.device, stream)
-        for v in (t, o):
-            if v.dtype is not x.dtype or v.get_device() != dev or v.dim() != 3 or v.shape[0] != T or v.shape[2] != d or (v.stride(2) != 1 and d > 1):
-                raise ValueError(f"expected [T, heads, {d}] of {x.dtype} on cuda:{dev} with neighbouring columns, T = {T}, not "
-                                 f"{v.dtype} {list(v.shape)} with strides {list(v.stride())} on {v.device}")
-        if o.shape[1] != t.shape[1] or (o.stride(0) == 0 and T > 1) or (o.stride(1) == 0 and o.shape[1] > 1):
+            o = _new(torch.empty, tuple(t.shape), dtype, t.device, stream)
+        n, at, st, sh = _heads(t, T, d, dtype, dev)
+        m, to, ot, oh = _heads(o, T, d, dtype, dev)
+        if m != n or (ot == 0 and T > 1) or (oh == 0 and n > 1):
             raise ValueError("an output has the heads of its input, each at a place of its own")
+        parts.append((n, at, st, sh, to, ot, oh))
         outs.append(o)
-    if q is not None:
-        a.n_q_heads, a.q, a.q_token_stride, a.q_head_stride = q.shape[1], q.data_ptr(), q.stride(0), q.stride(1)
-        a.q_out, a.q_out_token_stride, a.q_out_head_stride = outs[0].data_ptr(), outs[0].stride(0), outs[0].stride(1)
-    if k is not None:
-        a.n_k_heads, a.k, a.k_token_stride, a.k_head_stride = k.shape[1], k.data_ptr(), k.stride(0), k.stride(1)
-        a.k_out, a.k_out_token_stride, a.k_out_head_stride = outs[1].data_ptr(), outs[1].stride(0), outs[1].stride(1)
+    (nq, a, b, c, e, f, g), (nk, h, i, j, l, m, n) = parts
+    args = LcaRopeArgs(code, interleaved, inverse, nq, nk, d, 2 * freqs.numel(), factor, T, _arg(positions, _I32, T, dev), _arg(freqs, _F64, 1, dev),
+                       a, b or 0, c or 0, e, f or 0, g or 0, h, i or 0, j or 0, l, m or 0, n or 0)
     if T > 0:
-        _check(_lib.lca_rope(a, _raw_stream(dev, stream)), "lca_rope")
+        _check(_lib.lca_rope(args, _raw_stream(dev, stream)), "lca_rope")
     return outs[0], outs[1]
 
 
@@ -946,7 +949,7 @@ def verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, n
     n_tok_out [B] or None) int32."""
     B, n1, V = target_probs.shape
     n = n1 - 1
-    dev = _device(target_probs.device, "verify_drafts")
+    dev = _device(target_probs, "verify_drafts")
     dt = target_probs.dtype
     code = _ROPE_TYPES.get(dt)
     if code is None:

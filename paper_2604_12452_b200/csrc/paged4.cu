@@ -105,45 +105,54 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_write_mla_kernel(Paged4Row
   }
 }
 
-// GQA: the vectors of K or V (one for each row and KV head) lie one after the other in the input; D / 8 lanes take one.
+// GQA: a warp takes a row's keys or values, or up to 16 KV heads of them (blockIdx.y: the two parts, then groups of heads), D / 8 lanes
+// a vector and a KV head.  All its loads are under way before the first is used.
+template <int D>
+struct GqaRow {
+  static constexpr int U = D / 8, HEADS = 32 / U;            // lanes of a vector; KV heads of a step
+  static constexpr int STEPS = 16 / HEADS;
+};
 template <int D>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa_kernel(Paged4Rows a) {
-  constexpr int U = D / 8;                                   // lanes of a vector: 16 or 8
-  const long long units = a.n_rows * a.Hkv * U, threads = (long long)gridDim.x * ROW_THREADS;
-  const bool pos = blockIdx.y != 0;
+  using G = GqaRow<D>;
+  const bool pos = blockIdx.y & 1;
+  const int hk0 = (int)(blockIdx.y >> 1) * 16, lane = threadIdx.x & 31, u = lane % G::U;
   const uint4* src = reinterpret_cast<const uint4*>(pos ? a.pos : a.sem);
   uint32_t* pages = pos ? a.pages_pos : a.pages_sem;
   uint8_t* shifts = pos ? a.shift_pos : a.shift_sem;
   uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
-  const int lane = threadIdx.x & 31;
+  const long long warps = (long long)gridDim.x * ROW_WARPS;
   chain_wait();
   chain_next();
-#pragma unroll 2
-  for (long long x0 = (long long)blockIdx.x * ROW_THREADS + (threadIdx.x & ~31); x0 < units; x0 += threads) {
-    const long long x = x0 + lane;
-    const bool in = x < units;
-    const unsigned vec = in ? (unsigned)(x / U) : 0u;        // below 2^31 * Hkv: checked by the caller
-    const unsigned i = vec / (unsigned)a.Hkv, hk = vec - i * (unsigned)a.Hkv;
-    const int slot = in ? a.slots[i] : -1;
-    const bool ok = slot >= 0 && slot < a.n_slots;
-    const uint4 v = ok ? __ldcs(src + x) : make_uint4(0u, 0u, 0u, 0u);
-    bool n;
-    uint32_t top = top8(v, n);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-    const bool nan = (__ballot_sync(0xffffffffu, n) >> (lane & ~3)) & 15u;
-    uint32_t all = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
-    if (U == 16) all = max(all, __shfl_xor_sync(0xffffffffu, all, 8));
-    const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
-    const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT), s = nan ? PAGED4_NAN_SHIFT : shift;
-    const uint32_t w = pack8(v, E - shift);
-    const int next = __shfl_down_sync(0xffffffffu, s, 4);
-    if (!ok) continue;
-    const size_t row = pool_row(a, slot, (int)hk);
-    const int u = lane % U;
-    pages[row * U + u] = w;
-    if (u % 8 == 0) shifts[row * (D / 64) + u / 8] = (uint8_t)(s | next << 4);
-    if (u == 0) exps[row] = (uint8_t)(E + PAGED4_EXP_BIAS);
+  for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
+    const int slot = a.slots[i];
+    if (slot < 0 || slot >= a.n_slots) continue;
+    const uint4* row_src = src + ((size_t)i * a.Hkv + hk0) * G::U + lane;
+    uint4 v[G::STEPS];
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k)
+      if (hk0 + k * G::HEADS < a.Hkv) v[k] = hk0 + k * G::HEADS + lane / G::U < a.Hkv ? __ldcs(row_src + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      if (hk0 + k * G::HEADS >= a.Hkv) break;                // the same in every lane
+      bool n;
+      uint32_t top = top8(v[k], n);
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+      const bool nan = (__ballot_sync(0xffffffffu, n) >> (lane & ~3)) & 15u;
+      uint32_t all = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
+      if (G::U == 16) all = max(all, __shfl_xor_sync(0xffffffffu, all, 8));
+      const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
+      const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT), s = nan ? PAGED4_NAN_SHIFT : shift;
+      const uint32_t w = pack8(v[k], E - shift);
+      const int next = __shfl_down_sync(0xffffffffu, s, 4), hk = hk0 + k * G::HEADS + lane / G::U;
+      if (hk < a.Hkv) {
+        const size_t row = pool_row(a, slot, hk);
+        pages[row * G::U + u] = w;
+        if (u % 8 == 0) shifts[row * (D / 64) + u / 8] = (uint8_t)(s | next << 4);
+        if (u == 0) exps[row] = (uint8_t)(E + PAGED4_EXP_BIAS);
+      }
+    }
   }
 }
 
@@ -182,28 +191,39 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_read_mla_kernel(Paged4Rows
 
 template <int D>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa_kernel(Paged4Rows a) {
-  constexpr int U = D / 8;
+  using G = GqaRow<D>;
   __shared__ uint2 s_table[16];
-  const long long units = a.n_rows * a.Hkv * U, threads = (long long)gridDim.x * ROW_THREADS;
-  const bool pos = blockIdx.y != 0;
+  const bool pos = blockIdx.y & 1;
+  const int hk0 = (int)(blockIdx.y >> 1) * 16, lane = threadIdx.x & 31, u = lane % G::U;
   uint4* dst = reinterpret_cast<uint4*>(pos ? a.pos : a.sem);
   const uint32_t* pages = pos ? a.pages_pos : a.pages_sem;
   const uint8_t* shifts = pos ? a.shift_pos : a.shift_sem;
   const uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
+  const long long warps = (long long)gridDim.x * ROW_WARPS;
   paged4_table_load(s_table, threadIdx.x);
   __syncthreads();
   chain_wait();
   chain_next();
-#pragma unroll 4
-  for (long long x = (long long)blockIdx.x * ROW_THREADS + threadIdx.x; x < units; x += threads) {
-    const unsigned vec = (unsigned)(x / U), i = vec / (unsigned)a.Hkv, hk = vec - i * (unsigned)a.Hkv;
+  for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
     const int slot = a.slots[i];
     if (slot < 0 || slot >= a.n_slots) continue;
-    const size_t row = pool_row(a, slot, (int)hk);
-    const int u = (int)(x % U);
-    const uint32_t w = __ldcs(pages + row * U + u);
-    const int s = shifts[row * (D / 64) + u / 8] >> (u & 4) & 15;
-    __stcs(dst + x, unpack8(w, s, paged4_factor(exps[row]), s_table));
+    uint32_t w[G::STEPS];
+    int s[G::STEPS], e[G::STEPS];
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      const int hk = hk0 + k * G::HEADS + lane / G::U;
+      w[k] = 0; s[k] = 0; e[k] = 0;
+      if (hk < a.Hkv) {
+        const size_t row = pool_row(a, slot, hk);
+        w[k] = __ldcs(pages + row * G::U + u);
+        s[k] = shifts[row * (D / 64) + u / 8];
+        e[k] = exps[row];
+      }
+    }
+    uint4* row_dst = dst + ((size_t)i * a.Hkv + hk0) * G::U + lane;
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k)
+      if (hk0 + k * G::HEADS + lane / G::U < a.Hkv) __stcs(row_dst + k * 32, unpack8(w[k], s[k] >> (u & 4) & 15, paged4_factor(e[k]), s_table));
   }
 }
 
@@ -221,9 +241,9 @@ int paged4_rows_launch(const lca_params* p, const lca_paged4* c, bool write, con
                       : (p->d_sem == 512 ? paged4_read_mla_kernel<512> : paged4_read_mla_kernel<128>);
     return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a);
   }
-  if (n_rows * p->n_kv_heads > 0xffffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
-  const long long want = (n_rows * p->n_kv_heads * (p->d_sem / 8) + ROW_THREADS - 1) / ROW_THREADS;
-  const dim3 grid((unsigned)(want < most ? want : most), 2);
+  const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS, parts = 2 * ((p->n_kv_heads + 15) / 16);
+  if (parts > 65535) return LCA_ERR_UNSUPPORTED_SHAPE;
+  const dim3 grid((unsigned)(want < most ? want : most), (unsigned)parts);
   auto kern = write ? (p->d_sem == 128 ? paged4_write_gqa_kernel<128> : paged4_write_gqa_kernel<64>)
                     : (p->d_sem == 128 ? paged4_read_gqa_kernel<128> : paged4_read_gqa_kernel<64>);
   return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a);

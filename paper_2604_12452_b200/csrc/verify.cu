@@ -5,8 +5,8 @@
 // exceeds u times the whole.  Sums are 64-bit: with 32 the sum of 10^5 probabilities is off by more than many of them, and the
 // token would depend on the order.
 // Only what decides is read: two numbers for each draft, then one row of p and one of q.  A cluster takes a request, so that its CTAs
-// share the row; each sums its part warp by warp, the CTA whose part holds the crossing finds the warp and goes through that
-// warp's few hundred tokens again (from L2).  HBM-bound for many requests, else the chain of four dependent trips to memory.
+// share the row; each sums its part warp by warp; the CTA whose part holds the crossing finds the warp, spreads that warp's few
+// hundred tokens over all its warps (from L2) and goes through the last few dozen.  HBM-bound for many requests, else the chain of four dependent trips to memory.
 #include "lca_common.cuh"
 #include "tc_common.cuh"
 
@@ -44,7 +44,7 @@ __device__ __forceinline__ double mass(float p, float q) {
 
 template <class T>
 __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
-  __shared__ double s_warp[VERIFY_WARPS], s_cta[VERIFY_MOST_CTAS];
+  __shared__ double s_warp[VERIFY_WARPS], s_sub[VERIFY_WARPS], s_cta[VERIFY_MOST_CTAS];
   __shared__ int s_taken;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)tc::cluster_ctarank(), C = (int)(gridDim.x / a.B), b = (int)(blockIdx.x / C);
@@ -95,7 +95,6 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
       for (int k = 0; k < 4; ++k) if (gone == x + k) r[k] = 0.0;
     }
   };
-  int token = -1;
   // nothing is left of a rejected row only where p <= q everywhere: then p itself
 #pragma unroll 1
   for (int attempt = 0; attempt < 2; ++attempt) {
@@ -132,7 +131,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
         before += s_cta[c];
         if (s_cta[c] > 0.0 && before > want) break;
       }
-      if (rank == cta) {
+      if (rank == cta) {                                     // the same for every thread of the CTA
         int w = -1;
         before = at;
         for (int k = 0; k < VERIFY_WARPS; ++k) {
@@ -140,30 +139,44 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
           before += s_warp[k];
           if (s_warp[k] > 0.0 && before > want) break;
         }
-        if (warp == w) {
+        // that warp's part again, split over all warps: their sums, then the tokens of the one with the crossing, 32 at a time
+        const long long first = (long long)(rank * VERIFY_WARPS + w) * span;
+        const int sub = (span / VERIFY_WARPS + 31) / 32 * 32;
+        const int end = (int)min(first + span, (long long)V);
+        auto range = [&](int k, int& a0, int& a1) { a0 = (int)min(first + (long long)k * sub, (long long)end); a1 = min(a0 + sub, end); };
+        auto one = [&](int x) {
+          const float f = prob(p + x), g = residual && q ? prob(q + x) : 0.f;
+          return residual && x == gone ? 0.0 : mass(f, g);
+        };
+        int a0, a1;
+        range(warp, a0, a1);
+        double part = 0.0;
+#pragma unroll 4
+        for (int x = a0 + lane; x < a1; x += 32) part += one(x);
+        part = warp_sum(part);
+        if (lane == 0) s_sub[warp] = part;
+        __syncthreads();
+        if (warp == 0) {
+          int k0 = -1;
+          before = at;
+          for (int k = 0; k < VERIFY_WARPS; ++k) {
+            if (s_sub[k] > 0.0) { k0 = k; at = before; }
+            before += s_sub[k];
+            if (s_sub[k] > 0.0 && before > want) break;
+          }
+          range(k0, a0, a1);
           double run = at;                                   // sum of all tokens before this step's
-          int last = -1;
-          for (int x0 = lo; x0 < hi; x0 += 128) {
-            const int x = x0 + 4 * lane;
-            double r[4];
-            masses(x, residual, r);
-            const double mine = (r[0] + r[1]) + (r[2] + r[3]);
+          int token = -1;
+          for (int x0 = a0; x0 < a1; x0 += 32) {
+            const double mine = x0 + lane < a1 ? one(x0 + lane) : 0.0;
             double inc = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) { const double y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
-            double c = run + inc - mine;
-            int found = -1, seen = -1;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              c += r[k];
-              if (r[k] > 0.0) { seen = x + k; if (found < 0 && c > want) found = x + k; }
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, found >= 0), some = __ballot_sync(0xffffffffu, seen >= 0);
-            if (hit) { last = __shfl_sync(0xffffffffu, found, __ffs((int)hit) - 1); break; }
-            if (some) last = __shfl_sync(0xffffffffu, seen, 31 - __clz((int)some));
+            const unsigned some = __ballot_sync(0xffffffffu, mine > 0.0), hit = __ballot_sync(0xffffffffu, mine > 0.0 && run + inc > want);
+            if (some) token = x0 + 31 - __clz((int)some);    // the last one with mass, should rounding leave none
+            if (hit) { token = x0 + __ffs((int)hit) - 1; break; }
             run += __shfl_sync(0xffffffffu, inc, 31);
           }
-          token = last;
           if (lane == 0) a.out[(size_t)b * (K + 1) + taken] = token;
         }
       }
@@ -191,9 +204,9 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
 int verify_launch(const lca_verify_args* v, cudaStream_t stream) {
   VerifyArgs a = {v->target_probs, v->draft_probs, v->draft_tokens, v->u_accept, v->u_sample, v->n_draft, v->n_tok, v->accepted, v->tokens_out,
                   v->n_tok_out, v->batch, v->n_drafts, v->vocab};
-  // CTAs of a request: as many as give every SM work, and not so many that a warp has less than four steps of 128 tokens
+  // CTAs of a request: as many as are resident at once, and not so many that a warp has less than four steps of 128 tokens
   int c = 1;
-  while (c < VERIFY_MOST_CTAS && (long long)v->batch * c < 3 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 512) c *= 2;
+  while (c < VERIFY_MOST_CTAS && (long long)v->batch * 2 * c <= 3 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 512) c *= 2;
   if ((long long)v->batch * c > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   const bool bf = v->dtype == LCA_DTYPE_BF16;
   auto kern = bf ? verify_kernel<bf16> : verify_kernel<float>;
