@@ -498,7 +498,7 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
  *   draft i is accepted while u_accept[i] * q_i(x_i) < p_i(x_i)  (the product in 64 bits, where it is exact)
  *   the next token is drawn from max(p_i - q_i, 0) at the first rejected draft i, or from p after the last accepted one: the first
  *       token v whose cumulative sum exceeds u_sample times the whole sum, in 64-bit sums
- * Entries that are not positive finite numbers have no mass.  Where p_i - q_i leaves none, the token is drawn from p_i; where that has none
+ * Entries (and differences) that are not positive finite fp32 numbers have no mass.  Where p_i - q_i leaves none, the token is drawn from p_i; where that has none
  * either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
 typedef struct lca_verify_args {
   int32_t dtype;                /* of both probabilities: LCA_DTYPE_FP32 or LCA_DTYPE_BF16 */

@@ -9,6 +9,8 @@
 // the expansion is exact and what remains is one power of two per row, 2^(exponent - 6).
 #pragma once
 
+#include <cuda_bf16.h>
+
 #include "fp8_common.cuh"
 
 namespace lca {
@@ -63,26 +65,46 @@ __device__ __forceinline__ uint2 paged4_expand(uint32_t w, const uint2& table, u
   return make_uint2(__byte_perm(table.x, table.y, m) | (w & 0x80808080u), __byte_perm(table.x, table.y, hi) | (up & 0x80808080u));
 }
 
-// Eight values to a word: nearest magnitude, ties to the even index; infinities become 6.
-__device__ __forceinline__ uint32_t paged4_pack(const float (&f)[8]) {
+// Eight bf16 values (two a word) times f to a word of codes: nearest magnitude, ties to the even index; infinities become 6.
+__device__ __forceinline__ uint32_t paged4_pack(const uint4& v, float f) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+  float x[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) { x[2 * k] = __uint_as_float(u[k] << 16) * f; x[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u) * f; }
   uint32_t w;
   asm("{\n\t.reg .b8 a, b, c, d;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
       "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
       "mov.b32 %0, {a, b, c, d};\n\t}"
-      : "=r"(w) : "f"(f[0]), "f"(f[1]), "f"(f[2]), "f"(f[3]), "f"(f[4]), "f"(f[5]), "f"(f[6]), "f"(f[7]));
-  // nibble i: magnitude and, in its top bit, the sign of value i.  The signs go where the expansion wants them.
-  const uint32_t s = w & 0x88888888u;
-  uint32_t lo = s & 0xffffu, hi = s >> 16;
-  lo = (lo | lo << 8) & 0x00ff00ffu; lo = (lo | lo << 4) & 0x08080808u;
-  hi = (hi | hi << 8) & 0x00ff00ffu; hi = (hi | hi << 4) & 0x08080808u;
-  return (w & 0x77777777u) | lo << 4 | hi;
+      : "=r"(w) : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  // nibble i: magnitude and sign of value i.  The signs go where the expansion wants them; they are the top bits of the values' halves
+  const uint32_t lo = __byte_perm(v.x, v.y, 0x7531), hi = __byte_perm(v.z, v.w, 0x7531);
+  return (w & 0x77777777u) | (lo & 0x80808080u) | ((hi >> 4) & 0x08080808u);
+}
+// Eight codes to bf16 values, two a word, times a power of two (or NaN): exact.  Both bytes of a magnitude come from a table.
+__device__ __forceinline__ uint4 paged4_unpack(uint32_t w, __nv_bfloat162 scale) {
+  const uint32_t m = w & 0x77777777u, n = m >> 16, up = w << 4;
+  // 0, 0.5, 1, 1.5 / 2, 3, 4, 6 are 0000 3f00 3f80 3fc0 / 4000 4040 4080 40c0
+  const uint32_t l0 = __byte_perm(0xc0800000u, 0xc0804000u, m), h0 = __byte_perm(0x3f3f3f00u, 0x40404040u, m) | (w & 0x80808080u);
+  const uint32_t l1 = __byte_perm(0xc0800000u, 0xc0804000u, n), h1 = __byte_perm(0x3f3f3f00u, 0x40404040u, n) | (up & 0x80808080u);
+  uint4 r = make_uint4(__byte_perm(l0, h0, 0x5140), __byte_perm(l0, h0, 0x7362), __byte_perm(l1, h1, 0x5140), __byte_perm(l1, h1, 0x7362));
+  uint32_t* q = &r.x;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const __nv_bfloat162 x = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(q + k), scale);
+    q[k] = *reinterpret_cast<const uint32_t*>(&x);
+  }
+  return r;
+}
+// the power of two of a block, NaN for a NaN block
+__device__ __forceinline__ __nv_bfloat162 paged4_scale(int exp_byte, int shift) {
+  const int e = (exp_byte > PAGED4_MIN_EXP + PAGED4_EXP_BIAS ? exp_byte : PAGED4_MIN_EXP + PAGED4_EXP_BIAS) - shift;       // 19 .. 255, biased
+  const uint32_t bits = shift == PAGED4_NAN_SHIFT ? 0x7fffu : (uint32_t)e << 7, two = bits | bits << 16;
+  return *reinterpret_cast<const __nv_bfloat162*>(&two);
 }
 
-// log2 of the scale of a block whose largest finite |x| has these bf16 bits: smallest e with |x| <= 6 * 2^e; far below for 0
-__device__ __forceinline__ int paged4_block_exponent(uint32_t bits) {
-  const int E = (int)(bits >> 7), M = (int)(bits & 0x7f);
-  return E == 0 ? -1000 : E - 127 - 2 + (M > 64 ? 1 : 0);    // 6 = 1.5 * 2^2, 1.5 = 1 + 64 / 128
-}
+// log2 of the scale of a block whose largest finite |x| has these bf16 bits: smallest e with |x| <= 6 * 2^e.  6 = 1.5 * 2^2, and a
+// significand above 1.5 = 1 + 64 / 128 carries into the exponent.  (Zero and subnormal numbers: far below PAGED4_MIN_EXP.)
+__device__ __forceinline__ int paged4_block_exponent(uint32_t bits) { return (int)((bits + 63u) >> 7) - 129; }
 
 }  // namespace lca

@@ -19,12 +19,12 @@ struct Paged4Rows {
 __device__ __forceinline__ size_t pool_row(const Paged4Rows& a, int s, int hk) {
   return (((size_t)(s >> a.page_log2) * a.Hkv + hk) << a.page_log2) + (size_t)(s & ((1 << a.page_log2) - 1));
 }
-// Largest finite |x| of eight bf16 values as bf16 bits; nan: whether one of them is NaN.
+// Largest finite |x| of eight bf16 values as bf16 bits; nan: whether one of them is NaN.  Every lane of the warp calls it.
 __device__ __forceinline__ uint32_t top8(const uint4& v, bool& nan) {
-  uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
+  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
   uint32_t top = max(m & 0xffffu, m >> 16);
   nan = top > 0x7f80u;
-  if (top >= 0x7f80u) {
+  if (__any_sync(0xffffffffu, top >= 0x7f80u)) {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};
     top = 0;
 #pragma unroll
@@ -34,23 +34,6 @@ __device__ __forceinline__ uint32_t top8(const uint4& v, bool& nan) {
     }
   }
   return top;
-}
-__device__ __forceinline__ uint32_t pack8(const uint4& v, int e) {
-  const float f = exp2_int(-e);                              // -108 <= e <= 126; the products are exact
-  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-  float x[8];
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    x[2 * k] = __uint_as_float(u[k] << 16) * f;
-    x[2 * k + 1] = __uint_as_float(u[k] & 0xffff0000u) * f;
-  }
-  return paged4_pack(x);
-}
-__device__ __forceinline__ uint4 unpack8(uint32_t w, int shift, float f, const uint2* s_table) {
-  const uint2 c = paged4_expand(w, s_table[shift]);
-  const float4 a = e4m3x4_to_float4(c.x), b = e4m3x4_to_float4(c.y);
-  return make_uint4(tc::pack_bf16x2(a.x * f, a.y * f), tc::pack_bf16x2(a.z * f, a.w * f),
-                    tc::pack_bf16x2(b.x * f, b.y * f), tc::pack_bf16x2(b.z * f, b.w * f));
 }
 
 static const int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
@@ -90,7 +73,7 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_write_mla_kernel(Paged4Row
 #pragma unroll
     for (int q = 0; q <= NS; ++q) {
       const int shift = min(E - paged4_block_exponent(top[q]), PAGED4_MAX_SHIFT), s = (nan >> q) & 1u ? PAGED4_NAN_SHIFT : shift;
-      const uint32_t w = pack8(v[q], E - shift);
+      const uint32_t w = paged4_pack(v[q], exp2_int(shift - E));
       const int next = __shfl_down_sync(0xffffffffu, s, 4);
       if (q < NS && lane + 32 * q < US) {
         a.pages_sem[row * (D_SEM / 8) + lane + 32 * q] = w;
@@ -105,53 +88,55 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_write_mla_kernel(Paged4Row
   }
 }
 
-// GQA: a warp takes a row's keys or values, or up to 16 KV heads of them (blockIdx.y: the two parts, then groups of heads), D / 8 lanes
-// a vector and a KV head.  All its loads are under way before the first is used.
+// GQA: a warp takes a row's keys or values, up to eight KV heads of them (blockIdx.y: the two parts, then groups of heads), D / 8 lanes
+// a vector and a KV head.  All its loads are under way before the first is used; heads lie a page's rows apart in the pool.
 template <int D>
 struct GqaRow {
-  static constexpr int U = D / 8, HEADS = 32 / U;            // lanes of a vector; KV heads of a step
-  static constexpr int STEPS = 16 / HEADS;
+  static constexpr int U = D / 8, HEADS = 32 / U, STEPS = 8 / HEADS;         // lanes of a vector; KV heads of a step; steps
 };
 template <int D>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa_kernel(Paged4Rows a) {
   using G = GqaRow<D>;
   const bool pos = blockIdx.y & 1;
-  const int hk0 = (int)(blockIdx.y >> 1) * 16, lane = threadIdx.x & 31, u = lane % G::U;
-  const uint4* src = reinterpret_cast<const uint4*>(pos ? a.pos : a.sem);
-  uint32_t* pages = pos ? a.pages_pos : a.pages_sem;
-  uint8_t* shifts = pos ? a.shift_pos : a.shift_sem;
+  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U, left = a.Hkv - hk;
+  const uint4* src = reinterpret_cast<const uint4*>(pos ? a.pos : a.sem) + (size_t)(hk - lane / G::U) * G::U + lane;
+  uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
+  uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
   uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
   const long long warps = (long long)gridDim.x * ROW_WARPS;
+  const int apart = G::HEADS << a.page_log2;                 // rows of the pool from one step's head to the next one's
   chain_wait();
   chain_next();
   for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
     const int slot = a.slots[i];
     if (slot < 0 || slot >= a.n_slots) continue;
-    const uint4* row_src = src + ((size_t)i * a.Hkv + hk0) * G::U + lane;
+    const uint4* row_src = src + (size_t)i * a.Hkv * G::U;
     uint4 v[G::STEPS];
 #pragma unroll
-    for (int k = 0; k < G::STEPS; ++k)
-      if (hk0 + k * G::HEADS < a.Hkv) v[k] = hk0 + k * G::HEADS + lane / G::U < a.Hkv ? __ldcs(row_src + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+    for (int k = 0; k < G::STEPS; ++k) v[k] = k * G::HEADS < left ? __ldcs(row_src + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+    const size_t row0 = pool_row(a, slot, hk);
+    uint32_t* to = pages + row0 * G::U;
+    uint8_t* to_shift = shifts + row0 * (D / 64);
+    uint8_t* to_exp = exps + row0;
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k) {
-      if (hk0 + k * G::HEADS >= a.Hkv) break;                // the same in every lane
       bool n;
       uint32_t top = top8(v[k], n);
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const bool nan = (__ballot_sync(0xffffffffu, n) >> (lane & ~3)) & 15u;
       uint32_t all = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
       if (G::U == 16) all = max(all, __shfl_xor_sync(0xffffffffu, all, 8));
       const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
-      const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT), s = nan ? PAGED4_NAN_SHIFT : shift;
-      const uint32_t w = pack8(v[k], E - shift);
-      const int next = __shfl_down_sync(0xffffffffu, s, 4), hk = hk0 + k * G::HEADS + lane / G::U;
-      if (hk < a.Hkv) {
-        const size_t row = pool_row(a, slot, hk);
-        pages[row * G::U + u] = w;
-        if (u % 8 == 0) shifts[row * (D / 64) + u / 8] = (uint8_t)(s | next << 4);
-        if (u == 0) exps[row] = (uint8_t)(E + PAGED4_EXP_BIAS);
+      const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT);
+      const int s = (__ballot_sync(0xffffffffu, n) >> (lane & ~3)) & 15u ? PAGED4_NAN_SHIFT : shift;
+      const uint32_t w = paged4_pack(v[k], exp2_int(shift - E));
+      const int next = __shfl_down_sync(0xffffffffu, s, 4);
+      if (k * G::HEADS < left) {
+        *to = w;
+        if (u % 8 == 0) *to_shift = (uint8_t)(s | next << 4);
+        if (u == 0) *to_exp = (uint8_t)(E + PAGED4_EXP_BIAS);
       }
+      to += (size_t)apart * G::U; to_shift += (size_t)apart * (D / 64); to_exp += apart;
     }
   }
 }
@@ -159,11 +144,8 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa_kernel(Paged4Row
 template <int D_SEM>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_read_mla_kernel(Paged4Rows a) {
   constexpr int D_POS = 64, NS = D_SEM / 256 > 0 ? D_SEM / 256 : 1, US = D_SEM / 8;
-  __shared__ uint2 s_table[16];
   const int lane = threadIdx.x & 31;
   const long long warps = (long long)gridDim.x * ROW_WARPS;
-  paged4_table_load(s_table, threadIdx.x);
-  __syncthreads();
   chain_wait();
   chain_next();
 #pragma unroll 2
@@ -181,49 +163,48 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_read_mla_kernel(Paged4Rows
     }
     w[NS] = lane < D_POS / 8 ? __ldcs(a.pages_pos + row * (D_POS / 8) + lane) : 0u;
     s[NS] = lane < D_POS / 8 ? a.shift_pos[row] >> (lane & 4) & 15 : 0;
-    const float f = paged4_factor(a.exp_sem[row]);
+    const int e = a.exp_sem[row];
 #pragma unroll
     for (int q = 0; q < NS; ++q)
-      if (lane + 32 * q < US) __stcs(reinterpret_cast<uint4*>(a.sem + (size_t)i * D_SEM) + lane + 32 * q, unpack8(w[q], s[q], f, s_table));
-    if (lane < D_POS / 8) __stcs(reinterpret_cast<uint4*>(a.pos + (size_t)i * D_POS) + lane, unpack8(w[NS], s[NS], f, s_table));
+      if (lane + 32 * q < US) __stcs(reinterpret_cast<uint4*>(a.sem + (size_t)i * D_SEM) + lane + 32 * q, paged4_unpack(w[q], paged4_scale(e, s[q])));
+    if (lane < D_POS / 8) __stcs(reinterpret_cast<uint4*>(a.pos + (size_t)i * D_POS) + lane, paged4_unpack(w[NS], paged4_scale(e, s[NS])));
   }
 }
 
 template <int D>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa_kernel(Paged4Rows a) {
   using G = GqaRow<D>;
-  __shared__ uint2 s_table[16];
   const bool pos = blockIdx.y & 1;
-  const int hk0 = (int)(blockIdx.y >> 1) * 16, lane = threadIdx.x & 31, u = lane % G::U;
-  uint4* dst = reinterpret_cast<uint4*>(pos ? a.pos : a.sem);
-  const uint32_t* pages = pos ? a.pages_pos : a.pages_sem;
-  const uint8_t* shifts = pos ? a.shift_pos : a.shift_sem;
+  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U, left = a.Hkv - hk;
+  uint4* dst = reinterpret_cast<uint4*>(pos ? a.pos : a.sem) + (size_t)(hk - lane / G::U) * G::U + lane;
+  const uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
+  const uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
   const uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
   const long long warps = (long long)gridDim.x * ROW_WARPS;
-  paged4_table_load(s_table, threadIdx.x);
-  __syncthreads();
+  const int apart = G::HEADS << a.page_log2;
   chain_wait();
   chain_next();
   for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
     const int slot = a.slots[i];
     if (slot < 0 || slot >= a.n_slots) continue;
+    const size_t row0 = pool_row(a, slot, hk);
+    const uint32_t* from = pages + row0 * G::U;
+    const uint8_t* from_shift = shifts + row0 * (D / 64);
+    const uint8_t* from_exp = exps + row0;
     uint32_t w[G::STEPS];
     int s[G::STEPS], e[G::STEPS];
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k) {
-      const int hk = hk0 + k * G::HEADS + lane / G::U;
-      w[k] = 0; s[k] = 0; e[k] = 0;
-      if (hk < a.Hkv) {
-        const size_t row = pool_row(a, slot, hk);
-        w[k] = __ldcs(pages + row * G::U + u);
-        s[k] = shifts[row * (D / 64) + u / 8];
-        e[k] = exps[row];
-      }
+      const bool in = k * G::HEADS < left;
+      w[k] = in ? __ldcs(from) : 0u;
+      s[k] = in ? *from_shift : 0;
+      e[k] = in ? *from_exp : 0;
+      from += (size_t)apart * G::U; from_shift += (size_t)apart * (D / 64); from_exp += apart;
     }
-    uint4* row_dst = dst + ((size_t)i * a.Hkv + hk0) * G::U + lane;
+    uint4* row_dst = dst + (size_t)i * a.Hkv * G::U;
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k)
-      if (hk0 + k * G::HEADS + lane / G::U < a.Hkv) __stcs(row_dst + k * 32, unpack8(w[k], s[k] >> (u & 4) & 15, paged4_factor(e[k]), s_table));
+      if (k * G::HEADS < left) __stcs(row_dst + k * 32, paged4_unpack(w[k], paged4_scale(e[k], s[k] >> (u & 4) & 15)));
   }
 }
 
@@ -233,7 +214,7 @@ int paged4_rows_launch(const lca_params* p, const lca_paged4* c, bool write, con
   Paged4Rows a = {(bf16*)rows_sem, (bf16*)rows_pos, slot_map, (uint32_t*)c->pages_sem, (uint32_t*)c->pages_pos, c->shift_sem, c->shift_pos,
                   c->exp_sem, c->exp_pos, n_rows, (long long)c->n_pages * c->page_size, p->n_kv_heads,
                   c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7};
-  const long long most = 148 * 8 * 8;                        // eight waves of all CTAs that are resident
+  const long long most = 148 * 8 * 8;                        // a few waves of all CTAs that are resident
   if (mla) {
     const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS;
     const dim3 grid((unsigned)(want < most ? want : most), 1);
@@ -241,7 +222,7 @@ int paged4_rows_launch(const lca_params* p, const lca_paged4* c, bool write, con
                       : (p->d_sem == 512 ? paged4_read_mla_kernel<512> : paged4_read_mla_kernel<128>);
     return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a);
   }
-  const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS, parts = 2 * ((p->n_kv_heads + 15) / 16);
+  const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS, parts = 2 * ((p->n_kv_heads + 7) / 8);
   if (parts > 65535) return LCA_ERR_UNSUPPORTED_SHAPE;
   const dim3 grid((unsigned)(want < most ? want : most), (unsigned)parts);
   auto kern = write ? (p->d_sem == 128 ? paged4_write_gqa_kernel<128> : paged4_write_gqa_kernel<64>)

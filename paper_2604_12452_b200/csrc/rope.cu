@@ -91,7 +91,7 @@ __global__ void __launch_bounds__(ROPE_THREADS) rope_kernel(const __grid_constan
   const int units = rot_units + (VEC ? (a.d - a.rot) / 8 : a.d - a.rot);
   const int h0 = (int)blockIdx.y * a.heads, n_heads = min(a.heads, a.part[0].heads + a.part[1].heads - h0);
   const unsigned total = (unsigned)n_tok * n_heads * units;
-#pragma unroll 2
+#pragma unroll 4
   for (unsigned x = threadIdx.x; x < total; x += ROPE_THREADS) {
     const unsigned th = x / (unsigned)units, t = th / (unsigned)n_heads;
     const int u = (int)(x - th * units);

@@ -12,7 +12,7 @@
 
 namespace lca {
 
-static const int VERIFY_THREADS = 512, VERIFY_WARPS = VERIFY_THREADS / 32, VERIFY_MOST_CTAS = 16;
+static const int VERIFY_THREADS = 256, VERIFY_WARPS = VERIFY_THREADS / 32, VERIFY_MOST_CTAS = 16;
 
 struct VerifyArgs {
   const void* target; const void* draft; const int32_t* tokens; const float* u_accept; const float* u_sample;
@@ -24,22 +24,26 @@ struct VerifyArgs {
 template <class T> __device__ __forceinline__ float prob(const T* p) {
   if constexpr (sizeof(T) == 2) return __bfloat162float(*p); else return *p;
 }
+template <class T>
+__device__ __forceinline__ float4 vec4(const T* p) {
+  if constexpr (sizeof(T) == 2) {
+    const uint2 v = *reinterpret_cast<const uint2*>(p);
+    return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
+  } else return *reinterpret_cast<const float4*>(p);
+}
 // Values [x, x + 4) of a row (zero behind V), one vector where the row allows it.
 template <class T>
 __device__ __forceinline__ float4 four(const T* row, int x, int V, bool wide) {
-  if (wide && x + 4 <= V) {
-    if constexpr (sizeof(T) == 2) {
-      const uint2 v = *reinterpret_cast<const uint2*>(row + x);
-      return make_float4(__uint_as_float(v.x << 16), __uint_as_float(v.x & 0xffff0000u), __uint_as_float(v.y << 16), __uint_as_float(v.y & 0xffff0000u));
-    } else return *reinterpret_cast<const float4*>(row + x);
-  }
+  if (wide && x + 4 <= V) return vec4(row + x);
   return make_float4(x < V ? prob(row + x) : 0.f, x + 1 < V ? prob(row + x + 1) : 0.f, x + 2 < V ? prob(row + x + 2) : 0.f,
                      x + 3 < V ? prob(row + x + 3) : 0.f);
 }
-// Mass of a token; what is not a positive finite number has none.
+// Mass of a token, max(p - q, 0).  Its sign does not need 64 bits (a difference of two fp32 numbers is not rounded to 0), and what is no
+// positive finite number has none; compared in 64 bits, the comparisons were half of the kernel's instructions.
 __device__ __forceinline__ double mass(float p, float q) {
-  const double r = (double)p - (double)q;
-  return r > 0.0 && r < INFINITY ? r : 0.0;
+  const float r = p - q;
+  const bool some = r > 0.f && r < INFINITY;
+  return (double)(some ? p : 0.f) - (double)(some ? q : 0.f);
 }
 
 template <class T>
@@ -85,26 +89,30 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
   const int span = (int)(((long long)V + C * VERIFY_WARPS * 128 - 1) / (C * VERIFY_WARPS * 128)) * 128;
   const long long begin = (long long)(rank * VERIFY_WARPS + warp) * span;
   const int lo = (int)min(begin, (long long)V), hi = (int)min(begin + span, (long long)V);
-  auto masses = [&](int x, bool residual, double (&r)[4]) {
-    const float4 f = four(p, x, V, p_wide);
-    float4 g = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (residual && q) g = four(q, x, V, q_wide);
-    r[0] = mass(f.x, g.x); r[1] = mass(f.y, g.y); r[2] = mass(f.z, g.z); r[3] = mass(f.w, g.w);
-    if (residual && (unsigned)(gone - x) < 4u) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k) if (gone == x + k) r[k] = 0.0;
-    }
-  };
   // nothing is left of a rejected row only where p <= q everywhere: then p itself
 #pragma unroll 1
   for (int attempt = 0; attempt < 2; ++attempt) {
     const bool residual = attempt == 0;
     double sum = 0.0;
-#pragma unroll 4
-    for (int x = lo + 4 * lane; x < hi; x += 128) {
-      double r[4];
-      masses(x, residual, r);
-      sum += (r[0] + r[1]) + (r[2] + r[3]);
+    const bool with_q = residual && q;
+    const float4 zero = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto mass4 = [&](const float4& f, const float4& g) { return (mass(f.x, g.x) + mass(f.y, g.y)) + (mass(f.z, g.z) + mass(f.w, g.w)); };
+    int x = lo + 4 * lane;
+    const bool skip = residual && gone >= lo && gone < hi;   // the one token that a certain drafter proposed and the target rejected
+    if (p_wide && (!with_q || q_wide) && !skip) {
+      const int stop = min(hi, V & ~3);                      // eight whole vectors on their way
+      for (; x + 7 * 128 < stop; x += 8 * 128) {
+        float4 f[8], g[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { f[k] = vec4(p + x + 128 * k); g[k] = with_q ? vec4(q + x + 128 * k) : zero; }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += mass4(f[k], g[k]);
+      }
+    }
+    for (; x < hi; x += 128) {
+      float4 f = four(p, x, V, p_wide);
+      if (skip && (unsigned)(gone - x) < 4u) { if (gone == x) f.x = 0.f; else if (gone == x + 1) f.y = 0.f; else if (gone == x + 2) f.z = 0.f; else f.w = 0.f; }
+      sum += mass4(f, with_q ? four(q, x, V, q_wide) : zero);
     }
     sum = warp_sum(sum);
     if (lane == 0) s_warp[warp] = sum;
@@ -206,7 +214,7 @@ int verify_launch(const lca_verify_args* v, cudaStream_t stream) {
                   v->n_tok_out, v->batch, v->n_drafts, v->vocab};
   // CTAs of a request: as many as are resident at once, and not so many that a warp has less than four steps of 128 tokens
   int c = 1;
-  while (c < VERIFY_MOST_CTAS && (long long)v->batch * 2 * c <= 3 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 512) c *= 2;
+  while (c < VERIFY_MOST_CTAS && (long long)v->batch * 2 * c <= 4 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 512) c *= 2;
   if ((long long)v->batch * c > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   const bool bf = v->dtype == LCA_DTYPE_BF16;
   auto kern = bf ? verify_kernel<bf16> : verify_kernel<float>;
