@@ -34,6 +34,12 @@ struct Paged4Params {
   const uint8_t* exp_k; const uint8_t* exp_v;
 };
 
+
+static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
+static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
+
+
+
 // --------------------------------------------------------------------------------------------------- scalar kernel
 // One warp per query row, keys one by one, fp32: the cross-check of the tensor-core kernel (lca_set_attention_impl(1)).
 template <int D_SEM, int D_POS, bool MLA>
@@ -112,26 +118,24 @@ struct Paged4Plan {
   static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
   static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 columns)
   static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
-  static constexpr int K_BYTES = 128 * (KSEM * 128 + DP), V_BYTES = MLA ? 0 : 16384, TILE = K_BYTES + V_BYTES;        // expanded, two of them
+  static constexpr int K_BYTES = 128 * (KSEM * 128 + DP), V_BYTES = MLA ? 0 : 16384, TILE = K_BYTES + V_BYTES;        // expanded
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
   static constexpr int P_BYTES = 128 * 2 * NH;               // per key the first terms of all rows, then the second ones
   static constexpr int TM_S = 2 * NV * NH, TM_USED = TM_S + 4 * NH;
   static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
   static constexpr int CTAS = (MLA && DS == 512) || NH == 32 ? 1 : 2;        // per SM
-  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOAD = W_MMA + 1, THREADS = 32 * (W_LOAD + 1);
-  // packed rows as they come: a slab of codes, shifts and 32 bytes of facts
-  static constexpr int SLAB = MLA && DS == 512 ? 32 : 128, SLABS = 128 / SLAB;
-  static constexpr int ST_POS = SLAB * DS / 2, ST_SHS = ST_POS + SLAB * DP / 2, ST_SHP = ST_SHS + SLAB * DS / 64, ST_FACT = ST_SHP + SLAB * DP / 64;
-  static constexpr int STAGE = ST_FACT + 32;
-  static constexpr int FACTS = 4, FACT = 256 + 16;           // per tile: exponents of values and of keys, pages that are there
+  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, THREADS = 32 * (W_LOOK + 1);
+  // 32 values at a time: a thread's share of a tile, latents (V) and keys; tiles of them that are on their way to its registers
+  static constexpr int U_SEM = DS * 128 / 32 / (32 * EW), U_POS = DP * 128 / 32 / (32 * EW), UNITS = U_SEM + U_POS, DEPTH = UNITS > 4 ? 1 : 2;
+  static constexpr int FACTS = 8, FACT = 256 + 48;           // per tile: exponents of values and of keys, where its rows are
   // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers and scalars first, then the table.
-  static constexpr int MISC_BYTES = 384 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH) + FACTS * FACT;
+  static constexpr int MISC_BYTES = 512 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH) + FACTS * FACT;
   static constexpr int BUDGET = CTAS == 1 ? 227 * 1024 : 113 * 1024;
-  static constexpr int STAGES_FIT = (BUDGET - 2 * TILE - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / STAGE;
-  static constexpr int STAGES = STAGES_FIT > 4 ? 4 : STAGES_FIT;
-  static constexpr int OFF_Q = 2 * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_STAGE = OFF_P + 2 * P_BYTES, OFF_MISC = OFF_STAGE + STAGES * STAGE;
+  static constexpr int BUFS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / TILE;
+  static constexpr int BUFS = BUFS_FIT > 4 ? 4 : BUFS_FIT;   // expanded tiles
+  static constexpr int OFF_Q = BUFS * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
   static constexpr int SMEM = OFF_MISC + MISC_BYTES;
-  static_assert(STAGES >= 2 && SMEM <= BUDGET && STAGE % 16 == 0 && OFF_MISC % 16 == 0, "two slabs on their way while one is expanded");
+  static_assert(BUFS >= 2 && SMEM <= BUDGET && OFF_MISC % 16 == 0 && OFF_Q % 1024 == 0, "one tile is expanded while another is used");
   static_assert(THREADS / 32 <= 26, "room for the sums of the ranges");
 };
 
@@ -160,41 +164,58 @@ __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
 }
-__device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
-  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-               ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+// 16 bytes that are read once
+__device__ __forceinline__ uint4 load_stream(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
 }
 
-static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
-static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
+// A bounded wait that leaves its issue slots to the others: the hardware is told to suspend the thread for up to 2 us at a time.
+// (Every warp of this kernel waits for most of a tile; polling as fast as possible took a quarter of all issue slots.)
+__device__ __forceinline__ bool wait_suspended(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  auto poll = [&]() {
+    uint32_t done;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
+    return done != 0;
+  };
+  if (poll()) return true;
+  const long long t0 = clock64();
+  while (true) {
+    if (poll()) return true;
+    if (*abort_flag || clock64() - t0 > WAIT_TIMEOUT_CYCLES) return false;
+  }
+}
 
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
   constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
-  constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOAD = PL::W_LOAD;
+  constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOOK = PL::W_LOOK;
   const Paged8Params& p = a.b;
   extern __shared__ __align__(1024) unsigned char smem_p4[];
   unsigned char* base_ptr = smem_p4;
   const uint32_t base = smem_u32(smem_p4);
   const uint32_t bars = base + PL::OFF_MISC;
-  // two buffers of each: S complete, weights written, O complete, keys / values expanded
+  // two buffers of each: S complete, weights written, O complete
   auto SFULL = [&](uint32_t i) { return bars + 8 * i; };
   auto PFULL = [&](uint32_t i) { return bars + 16 + 8 * i; };
   auto PVDONE = [&](uint32_t i) { return bars + 32 + 8 * i; };
+  // BUFS of each: keys / values expanded, read by the products (MLA: the keys' barriers are not used for the latter)
   auto KFULL = [&](uint32_t i) { return bars + 48 + 8 * i; };
-  auto VFULL = [&](uint32_t i) { return bars + 64 + 8 * i; };
-  auto GFULL = [&](uint32_t i) { return bars + 80 + 8 * i; };           // packed slab landed, read
-  auto GEMPTY = [&](uint32_t i) { return bars + 112 + 8 * i; };
-  auto FFULL = [&](uint32_t i) { return bars + 144 + 8 * i; };          // exponents of a tile landed, read
-  auto FEMPTY = [&](uint32_t i) { return bars + 176 + 8 * i; };
-  const uint32_t QFULL = bars + 208;
+  auto VFULL = [&](uint32_t i) { return bars + 80 + 8 * i; };
+  auto KEMPTY = [&](uint32_t i) { return bars + 112 + 8 * i; };
+  auto VEMPTY = [&](uint32_t i) { return bars + 144 + 8 * i; };
+  auto FFULL = [&](uint32_t i) { return bars + 176 + 8 * i; };          // facts of a tile written, read
+  auto FEMPTY = [&](uint32_t i) { return bars + 240 + 8 * i; };
+  const uint32_t QFULL = bars + 304;
   unsigned char* misc = base_ptr + PL::OFF_MISC;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 256);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 260);
-  int* s_b = reinterpret_cast<int*>(misc + 264);
-  long long* s_off = reinterpret_cast<long long*>(misc + 272);          // offset inside sequence s_b, tiles of this CTA
-  uint2* s_table = reinterpret_cast<uint2*>(misc + 384);
-  float* s_qs = reinterpret_cast<float*>(misc + 512);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 320);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 324);
+  int* s_b = reinterpret_cast<int*>(misc + 328);
+  long long* s_off = reinterpret_cast<long long*>(misc + 336);          // offset inside sequence s_b, tiles of this CTA
+  uint2* s_table = reinterpret_cast<uint2*>(misc + 512);
+  float* s_qs = reinterpret_cast<float*>(misc + 640);
   float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
   int* s_lim = reinterpret_cast<int*>(s_f + NH);
   float* s_wmax = reinterpret_cast<float*>(s_lim + NH);      // also the sums of the four warps of a group
@@ -206,10 +227,10 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 
   if (tid == 0) {
     *abort_flag = 0;
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); mbar_init(KFULL(i), PL::EW); mbar_init(VFULL(i), PL::EW);
-    }
-    for (int i = 0; i < 4; ++i) { mbar_init(GFULL(i), 1); mbar_init(GEMPTY(i), PL::EW); mbar_init(FFULL(i), 1); mbar_init(FEMPTY(i), PL::SOFTMAX_WARPS); }
+    *reinterpret_cast<uint32_t*>(misc + 352) = 16u;
+    for (int i = 0; i < 2; ++i) { mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); }
+    for (int i = 0; i < 4; ++i) { mbar_init(KFULL(i), PL::EW); mbar_init(VFULL(i), PL::EW); mbar_init(KEMPTY(i), 1); mbar_init(VEMPTY(i), 1); }
+    for (int i = 0; i < PL::FACTS; ++i) { mbar_init(FFULL(i), 1); mbar_init(FEMPTY(i), PL::SOFTMAX_WARPS + PL::EW); }
     mbar_init(QFULL, 32 * PL::SOFTMAX_WARPS);
     fence_mbar_init();
     if (base & 1023u) fail(100);                             // the operands' images need it
@@ -230,86 +251,73 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
   Walk w;
   w.b = *s_b; w.off = s_off[0]; w.left = s_off[1]; w.fresh = true; w.n = 0;
 
-  if (warp == W_LOAD) {
-    // --------------------------------------------------------------------------------------------------- loads
-    // Lane i < 8 looks up the page of rows [16 i, 16 i + 16) of a tile, one tile ahead; then the lanes issue the copies: a request for
-    // each run of rows (a page, or the slab's share of it) and array.
+  if (warp == W_LOOK) {
+    // ------------------------------------------------------------------------------------------------- look-ups
+    // Where the rows of a tile are and what their exponents are, for all other warps: lane i < 8 the page of rows [16 i, 16 i + 16),
+    // every lane the exponents of four rows.  Three tiles are under way, one step each: page, exponents, written.
     bool ok = !*abort_flag;
-    int j = 0, stage = 0;
-    uint32_t phase = 0, g = 0;
+    int j = 0;
     bool more = w.next(p);
-    struct Next { long long row; int page_ok, lo, mid, hi; bool any; } nx;             // lo, mid, hi: PagedSpan from the tile's first row
-    auto look = [&]() {
-      nx.any = more;
+    struct Tile { int page, hk, lo, mid, hi; bool any; };    // page: of this lane's rows; lo, mid, hi: PagedSpan from the tile's first row
+    auto look = [&](Tile& y) {
+      y.any = more;
       if (!more) return;
       const PagedSpan sp = w.t.s;
       const int row0 = w.t.row0(w.t0 + j), x = row0 + 16 * (lane & 7);
-      nx.lo = sp.n_rep - row0; nx.mid = sp.tok0 - row0; nx.hi = sp.n_tok - row0;
-      int pg = -1;
-      if (sp.any(x & ~(p.page - 1), p.page) && (x >> p.page_log2) < p.width) pg = p.table[(size_t)w.b * p.width + (x >> p.page_log2)];
-      nx.page_ok = pg >= 0 && pg < p.n_pages;
-      nx.row = nx.page_ok ? (((long long)pg * p.Hkv + w.hk) << p.page_log2) + (x & (p.page - 1)) : 0;
+      y.lo = sp.n_rep - row0; y.mid = sp.tok0 - row0; y.hi = sp.n_tok - row0; y.hk = w.hk;
+      y.page = -1;
+      if (sp.any(x, 16) && (x >> p.page_log2) < p.width) y.page = p.table[(size_t)w.b * p.width + (x >> p.page_log2)];
       if (++j == w.n) { j = 0; more = w.next(p); }
     };
-    look();
-    while (ok && nx.any) {
-      const Next c = nx;
-      look();
-      const unsigned pages = __ballot_sync(0xffffffffu, c.page_ok) & 0xffu;
-      const bool part = !(pages == 0xffu && (c.lo >= 128 || (c.mid <= 0 && c.hi >= 128)));
-      const int f = (int)(g & 3);
-      ok = mbar_wait(FEMPTY(f), ((g >> 2) & 1) ^ 1, abort_flag);
+    // The pool's group of 16 rows, ~0: none.  (A group takes 512 bytes at least: 32 bits count those of more memory than there is.)
+    auto group_of = [&](const Tile& y) {
+      return y.any && (unsigned)y.page < (unsigned)p.n_pages
+                 ? (((uint32_t)y.page * (uint32_t)p.Hkv + (uint32_t)y.hk) << (p.page_log2 - 4)) + (uint32_t)(lane & ((p.page >> 4) - 1)) : ~0u;
+    };
+    auto exponents = [&](uint32_t group, uint32_t& v, uint32_t& k) {
+      const uint32_t gr = __shfl_sync(0xffffffffu, group, lane >> 2);
+      v = k = 0;
+      if (gr == ~0u) return;
+      v = __ldg(reinterpret_cast<const uint32_t*>(a.exp_v) + (size_t)gr * 4 + (lane & 3));
+      if (!PL::MLA) k = __ldg(reinterpret_cast<const uint32_t*>(a.exp_k) + (size_t)gr * 4 + (lane & 3));
+    };
+    Tile t0, t1;
+    uint32_t g0, v0, k0;
+    look(t0);
+    look(t1);
+    g0 = group_of(t0);
+    exponents(g0, v0, k0);
+    uint32_t f = 0, phase = 0;
+    while (ok && t0.any) {
+      const uint32_t g1 = group_of(t1);
+      uint32_t v1, k1;
+      exponents(g1, v1, k1);
+      Tile t2;
+      look(t2);
+      ok = wait_suspended(FEMPTY(f), phase ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
-      {
-        const uint32_t at = base + PL::OFF_MISC + (uint32_t)(s_fact - misc) + f * PL::FACT;
-        if (lane == 0) {
-          *reinterpret_cast<uint32_t*>(s_fact + f * PL::FACT + 256) = pages;
-          mbar_expect_tx(FFULL(f), __popc(pages) * 16 * (PL::MLA ? 1 : 2));
-        }
-        __syncwarp();
-        const int per = p.page >> 4, run = lane & 7;         // lane: run + 8 * array
-        const long long r = __shfl_sync(0xffffffffu, c.row, (run * per) & 7);
-        if (lane < (PL::MLA ? 8 : 16) && run * per < 8 && ((pages >> (run * per)) & 1u))
-          bulk_copy(at + (lane >= 8 ? 128 : 0) + run * p.page, (lane >= 8 ? a.exp_k : a.exp_v) + r, p.page, FFULL(f));
-      }
-#pragma unroll 1
-      for (int s = 0; s < PL::SLABS; ++s) {
-        ok = mbar_wait(GEMPTY(stage), phase ^ 1, abort_flag);
-        ok = __all_sync(0xffffffffu, ok);
-        if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
-        constexpr int GR = PL::SLAB / 16, B_SEM = DS / 2, B_POS = DP / 2, B_SHS = DS / 64, B_SHP = DP / 64;
-        const uint32_t at = base + PL::OFF_STAGE + stage * PL::STAGE;
-        const unsigned here = (pages >> (s * GR)) & ((1u << GR) - 1u);
-        if (lane == 0) {
-          int* fact = reinterpret_cast<int*>(base_ptr + PL::OFF_STAGE + stage * PL::STAGE + PL::ST_FACT);
-          fact[0] = part; fact[1] = c.lo - s * PL::SLAB; fact[2] = c.mid - s * PL::SLAB; fact[3] = c.hi - s * PL::SLAB; fact[4] = (int)here;
-          mbar_expect_tx(GFULL(stage), __popc(here) * 16 * (B_SEM + B_POS + B_SHS + B_SHP));
-        }
-        __syncwarp();
-        const int rows = min(p.page, PL::SLAB), per = rows >> 4, run = lane >> 2, arr = lane & 3;
-        const long long r = __shfl_sync(0xffffffffu, c.row, (s * GR + run * per) & 7);
-        if (run * per < GR && ((here >> (run * per)) & 1u)) {
-          const int bytes = arr == 0 ? B_SEM : arr == 1 ? B_POS : arr == 2 ? B_SHS : B_SHP;
-          const int off = arr == 0 ? 0 : arr == 1 ? PL::ST_POS : arr == 2 ? PL::ST_SHS : PL::ST_SHP;
-          const uint8_t* src = arr == 0 ? a.sem : arr == 1 ? a.pos : arr == 2 ? a.shift_sem : a.shift_pos;
-          bulk_copy(at + off + run * rows * bytes, src + r * bytes, rows * bytes, GFULL(stage));
-        }
-        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
-      }
-      ++g;
+      unsigned char* fact = s_fact + f * PL::FACT;
+      const bool all = (__ballot_sync(0xffffffffu, g0 != ~0u) & 0xffu) == 0xffu && (t0.lo >= 128 || (t0.mid <= 0 && t0.hi >= 128));
+      reinterpret_cast<uint32_t*>(fact)[lane] = v0;
+      if (!PL::MLA) reinterpret_cast<uint32_t*>(fact + 128)[lane] = k0;
+      if (lane < 8) reinterpret_cast<uint32_t*>(fact + 256)[lane] = g0;
+      if (lane == 8) *reinterpret_cast<int4*>(fact + 288) = make_int4(all, t0.lo, t0.mid, t0.hi);
+      __syncwarp();
+      if (lane == 0) mbar_arrive(FFULL(f));
+      if (++f == PL::FACTS) { f = 0; phase ^= 1; }
+      t0 = t1; t1 = t2; g0 = g1; v0 = v1; k0 = k1;
     }
   } else if (warp >= W_EXP && warp < W_MMA) {
     // ----------------------------------------------------------------------------------------------- expansion
-    // A thread takes 32 values (16 bytes of codes) of a row at a time.  Eight neighbouring lanes write two rows, so that their
-    // units fall on all banks of the swizzled image.
+    // A thread takes 32 values (16 bytes of codes) of a row at a time, from HBM to registers while it expands those of the tile
+    // before.  Eight neighbouring lanes write two rows, so that their units fall on all banks of the swizzled image.
     const int et = tid - 32 * W_EXP, ew = warp - W_EXP;
     const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
     bool ok = !*abort_flag;
-    int stage = 0;
-    uint32_t phase = 0;
+    const uint32_t sixteen = *reinterpret_cast<const volatile uint32_t*>(misc + 352);
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      if (ok && !mbar_wait(bar, ph, abort_flag)) { fail(code); ok = false; }
+      if (ok && !wait_suspended(bar, ph, abort_flag)) { fail(code); ok = false; }
       ok = __all_sync(0xffffffffu, ok);
       return ok;
     };
@@ -317,73 +325,122 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
     };
-    // units `first`, `first` + step ...: N of them; `at`: codes and shift of unit i, row in the slab and place in the tile
-    auto expand = [&](int r, const unsigned char* codes, const unsigned char* shift, int nibble, const int* fact, unsigned char* dst) {
-      const uint4 v = *reinterpret_cast<const uint4*>(codes);
-      uint32_t s = (uint32_t)*shift >> (4 * nibble) & 15u;
-      if (fact[0]) s = (r < fact[1] || (r >= fact[2] && r < fact[3])) && ((fact[4] >> (r >> 4)) & 1) ? s : 0u;      // what absent rows hold is no NaN
-      const uint2 t = s_table[s];
-      const uint2 x0 = paged4_expand(v.x, t), x1 = paged4_expand(v.y, t), x2 = paged4_expand(v.z, t), x3 = paged4_expand(v.w, t);
-      *reinterpret_cast<uint4*>(dst) = make_uint4(x0.x, x0.y, x1.x, x1.y);
-      unsigned char* other = base_ptr + ((uint32_t)(dst - base_ptr) ^ 16u);
-      *reinterpret_cast<uint4*>(other) = make_uint4(x2.x, x2.y, x3.x, x3.y);
-    };
-    // a 128 (64) columns wide part of 128 rows: 512 (256) units
-    auto expand_part = [&](const unsigned char* codes, const unsigned char* shifts, const int* fact, unsigned char* dst, auto width) {
-      constexpr int W = decltype(width)::value, U = W / 32;
+    constexpr bool LATENT = PL::MLA && DS == 512;
+    constexpr int US = PL::VW / 32, UP = DP / 32, STEP = 32 * PL::EW;
+    // unit i of this thread: row and unit in the row, place in the expanded tile
+    //   512 latents: a warp takes two rows at a time, its quarter q the chunk q of the first and q ^ 1 of the second
+    //   otherwise: neighbouring threads neighbouring units
+    const int c = LATENT ? (lane >> 3) ^ ((lane >> 2) & 1) : 0;
+    auto sem_row = [&](int i) { return LATENT ? 16 * i + 2 * ew + ((lane >> 2) & 1) : (et + STEP * i) / US; };
+    const int sem_u = LATENT ? 4 * c + (lane & 3) : et % US, pos_u = et % UP;
+    auto pos_row = [&](int i) { return (et + STEP * i) / UP; };
+    const uint32_t sem_to = (PL::MLA ? c * 16384 : PL::K_BYTES) + swz<PL::VW>(sem_row(0), 2 * (lane & (US - 1)));
+    const uint32_t pos_to = PL::KSEM * 16384 + swz<DP>(pos_row(0), 2 * pos_u);
+    struct Facts { bool all; int lo, mid, hi; const uint32_t* group; };
+    auto has = [&](const Facts& f, int r) { return f.all || r < f.lo || (r >= f.mid && r < f.hi); };
+    struct Unit { uint4 v; uint32_t s; };
+    // N units of the next tile on their way (a tile without absent rows takes the short path)
+    auto load = [&](auto count, Unit* x, int i0, const Facts& f, auto row_of, const uint8_t* codes, const uint8_t* shifts, int d, int u) {
+      constexpr int N = decltype(count)::value;
+      uint32_t gr[N];
 #pragma unroll
-      for (int i = 0; i < U * 128 / (32 * PL::EW); ++i) {
-        const int x = et + 32 * PL::EW * i, r = x / U, u = x % U;
-        expand(r, codes + x * 16, shifts + r * (W / 64) + (u >> 1), u & 1, fact, dst + swz<W>(r, 2 * u));
+      for (int i = 0; i < N; ++i) gr[i] = f.group[row_of(i0 + i) >> 4];
+      codes += u * 16; shifts += u >> 1;
+      if (f.all) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const size_t row = (size_t)gr[i] * 16 + (row_of(i0 + i) & 15);
+          x[i].v = load_stream(codes + row * (d / 2));
+          x[i].s = (uint32_t)__ldg(shifts + row * (d / 64));
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int r = row_of(i0 + i);
+          x[i].v = make_uint4(0u, 0u, 0u, 0u);
+          x[i].s = 0;
+          if (gr[i] != ~0u && has(f, r)) {                   // what absent rows hold is left alone
+            const size_t row = (size_t)gr[i] * 16 + (r & 15);
+            x[i].v = load_stream(codes + row * (d / 2));
+            x[i].s = (uint32_t)__ldg(shifts + row * (d / 64));
+          }
+        }
       }
     };
-    using W128 = std::integral_constant<int, 128>;
-    using W64 = std::integral_constant<int, 64>;
-    using WPOS = std::integral_constant<int, DP>;
-#pragma unroll 1
-    for (int t = 0; t < n_tiles; ++t) {
-      const uint32_t buf = t & 1, before = ((t >> 1) - 1) & 1;
-      unsigned char* tile = base_ptr + buf * PL::TILE;
-      if constexpr (PL::MLA && DS == 512) {
-        if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
-#pragma unroll 1
-        for (int s = 0; s < 4; ++s) {
-          if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
-          const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
-          const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
-          // a warp takes two rows at a time; its quarter q the chunk q of the first and q ^ 1 of the second
+    // N units expanded; dst: from the start of shared memory, `step` from one to the next
+    auto put = [&](auto count, const Unit* x, int u, uint32_t dst, uint32_t step) {
+      constexpr int N = decltype(count)::value;
+      uint2 t[N];
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const int r = 2 * (ew + 8 * i) + ((lane >> 2) & 1), c = (lane >> 3) ^ ((lane >> 2) & 1), u = lane & 3;
-            expand(r, st + r * 256 + c * 64 + u * 16, st + PL::ST_SHS + r * 8 + c * 2 + (u >> 1), u & 1, fact, tile + c * 16384 + swz<128>(32 * s + r, 2 * u));
-          }
-          if ((ew >> 1) == s) {                              // the keys' 64 units: two of the warps in turn
-            const int x = (ew & 1) * 32 + lane, r = x >> 1, u = x & 1;
-            expand(r, st + PL::ST_POS + x * 16, st + PL::ST_SHP + r, u, fact, tile + 4 * 16384 + swz<64>(32 * s + r, 2 * u));
-          }
-          signal(GEMPTY(stage));
-          if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
-        }
-        if (!ok) break;
-        fence_proxy_async_smem();
-        signal(KFULL(buf));
-      } else {
-        if (!wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
-        const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
-        const int* fact = reinterpret_cast<const int*>(st + PL::ST_FACT);
-        if (t > 1 && !wait(PL::MLA ? PVDONE(buf) : SFULL(buf), before, ERR_WAIT_O_DONE)) break;
-        expand_part(st + PL::ST_POS, st + PL::ST_SHP, fact, tile + PL::KSEM * 16384, WPOS());
+      for (int i = 0; i < N; ++i) t[i] = s_table[(x[i].s >> (4 * (u & 1))) & 15];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const uint2 x0 = paged4_expand(x[i].v.x, t[i], sixteen), x1 = paged4_expand(x[i].v.y, t[i], sixteen), x2 = paged4_expand(x[i].v.z, t[i], sixteen),
+                    x3 = paged4_expand(x[i].v.w, t[i], sixteen);
+        *reinterpret_cast<uint4*>(base_ptr + dst + i * step) = make_uint4(x0.x, x0.y, x1.x, x1.y);
+        *reinterpret_cast<uint4*>(base_ptr + (dst ^ 16u) + i * step) = make_uint4(x2.x, x2.y, x3.x, x3.y);
+      }
+    };
+    constexpr int BATCH = PL::U_SEM > 4 ? 4 : PL::U_SEM;
+    using CP = std::integral_constant<int, PL::U_POS>;
+    using CS = std::integral_constant<int, BATCH>;
+    auto load_sem = [&](Unit* x, const Facts& f, int i0) { load(CS(), x, i0, f, sem_row, a.sem, a.shift_sem, DS, sem_u); };
+    auto load_pos = [&](Unit* x, const Facts& f) { load(CP(), x, 0, f, pos_row, a.pos, a.shift_pos, DP, pos_u); };
+    uint32_t ff = 0, fphase = 0;
+    auto facts = [&](Facts& f, bool any) {                   // of the next tile; its groups are read until `signal`
+      if (!any) return;
+      if (!wait(FFULL(ff), fphase, ERR_WAIT_KV_FULL)) return;
+      const unsigned char* fact = s_fact + ff * PL::FACT;
+      const int4 y = *reinterpret_cast<const int4*>(fact + 288);
+      f = Facts{y.x != 0, y.y, y.z, y.w, reinterpret_cast<const uint32_t*>(fact + 256)};
+    };
+    auto facts_done = [&](bool any) {
+      if (!any) return;
+      signal(FEMPTY(ff));
+      if (++ff == PL::FACTS) { ff = 0; fphase ^= 1; }
+    };
+    constexpr int DEPTH = PL::DEPTH;
+    Unit sem[DEPTH][PL::U_SEM], pos[DEPTH][PL::U_POS];
+    Facts fx = {};
+#pragma unroll
+    for (int k = 0; k < DEPTH; ++k) {
+      const bool any = k < n_tiles;
+      facts(fx, any);
+      if (any && ok) {
+        load_pos(pos[k], fx);
+#pragma unroll
+        for (int i = 0; i < PL::U_SEM; i += BATCH) load_sem(sem[k] + i, fx, i);
+        facts_done(any);
+      }
+    }
+    uint32_t buf = 0, use = 0;                               // use: how often the buffer has been filled before
+#pragma unroll 1
+    for (int t1 = 0; t1 < n_tiles && ok; t1 += DEPTH) {
+#pragma unroll
+      for (int k = 0; k < DEPTH; ++k) {
+        const int t = t1 + k;
+        if (t >= n_tiles || !ok) break;
+        const bool any = t + DEPTH < n_tiles;
+        const uint32_t tile = buf * PL::TILE;
+        facts(fx, any);
+        if (use > 0 && !wait(PL::MLA ? VEMPTY(buf) : KEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
+        put(CP(), pos[k], pos_u, tile + pos_to, (STEP / UP) * DP);
+        if (any) load_pos(pos[k], fx);
         if constexpr (!PL::MLA) {
           fence_proxy_async_smem();
           signal(KFULL(buf));
-          if (t > 1 && !wait(PVDONE(buf), before, ERR_WAIT_O_DONE)) break;
+          if (use > 0 && !wait(VEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
         }
-        if constexpr (PL::VW == 128) expand_part(st, st + PL::ST_SHS, fact, tile + (PL::MLA ? 0 : PL::K_BYTES), W128());
-        else expand_part(st, st + PL::ST_SHS, fact, tile + PL::K_BYTES, W64());
-        signal(GEMPTY(stage));
-        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
+#pragma unroll
+        for (int i = 0; i < PL::U_SEM; i += BATCH) {
+          constexpr int APART = (LATENT ? 16 : STEP / US) * PL::VW;
+          put(CS(), sem[k] + i, sem_u, tile + sem_to + i * APART, APART);
+          if (any) load_sem(sem[k] + i, fx, i);
+        }
+        facts_done(any);
         fence_proxy_async_smem();
         signal(PL::MLA ? KFULL(buf) : VFULL(buf));
+        if (++buf == PL::BUFS) { buf = 0; ++use; }
       }
     }
   } else if (warp == W_MMA) {
@@ -393,15 +450,17 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     constexpr uint32_t ID_O = umma_idesc_f8(128, 2 * NH, 0, true, true);
     uint32_t g = 0, seg = 0;
     bool ok = !*abort_flag;
+    struct Ring { uint32_t buf, phase; __device__ __forceinline__ void next() { if (++buf == PL::BUFS) { buf = 0; phase ^= 1; } } };
+    Ring sb = {0, 0}, ob = {0, 0};                           // expanded tiles whose S and O come next
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      ok = ok && mbar_wait(bar, ph, abort_flag);
+      ok = ok && wait_suspended(bar, ph, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) fail(code);
       return ok;
     };
     auto issue_s = [&](uint32_t t) {
-      const uint32_t buf = t & 1, d = tmem + PL::TM_S + buf * 2 * NH, tile = base + buf * PL::TILE;
-      if (!wait(KFULL(buf), (t >> 1) & 1, ERR_WAIT_KV_FULL)) return;
+      const uint32_t buf = t & 1, d = tmem + PL::TM_S + buf * 2 * NH, tile = base + sb.buf * PL::TILE;
+      if (!wait(KFULL(sb.buf), sb.phase, ERR_WAIT_KV_FULL)) return;
       tc_fence_after();
       uint32_t acc = 0;
 #pragma unroll
@@ -412,30 +471,46 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
       }
       umma_commit_elected(leader, SFULL(buf));
+      if (!PL::MLA) umma_commit_elected(leader, KEMPTY(sb.buf));
+      sb.next();
+    };
+    auto issue_o = [&](uint32_t t, bool first) {
+      const uint32_t buf = t & 1;
+      if (!PL::MLA && !wait(VFULL(ob.buf), ob.phase, ERR_WAIT_KV_FULL)) return;
+      tc_fence_after();
+      const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
+#pragma unroll
+      for (int c = 0; c < NV; ++c) {
+        // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
+        // lanes it feeds are never read
+        const uint64_t ad = desc_rows(base + ob.buf * PL::TILE + (PL::MLA ? c * 16384 : PL::K_BYTES), PL::VW, 8192);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (!first || k > 0) ? 1u : 0u);
+      }
+      umma_commit_elected(leader, PVDONE(buf));
+      umma_commit_elected(leader, VEMPTY(ob.buf));
+      ob.next();
     };
     while (ok && w.next(p)) {
       if (!wait(QFULL, seg & 1, ERR_WAIT_Q)) break;
       ++seg;
       tc_fence_after();
-      issue_s(g);
-      for (int j = 0; j < w.n && ok; ++j, ++g) {
-        if (j + 1 < w.n) issue_s(g + 1);
-        const uint32_t buf = g & 1;
-        if (!PL::MLA && !wait(VFULL(buf), (g >> 1) & 1, ERR_WAIT_KV_FULL)) break;
-        if (!wait(PFULL(buf), (g >> 1) & 1, ERR_WAIT_P_FULL)) break;
-        tc_fence_after();
-        const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
-#pragma unroll
-        for (int c = 0; c < NV; ++c) {
-          // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
-          // lanes it feeds are never read
-          const uint64_t ad = desc_rows(base + buf * PL::TILE + (PL::MLA ? c * 16384 : PL::K_BYTES), PL::VW, 8192);
-#pragma unroll
-          for (int k = 0; k < 4; ++k)
-            umma_f8_elected(leader, tmem + c * 2 * NH, desc_add(ad, k * 2 * PL::VW), desc_add(pd, k * 4 * NH), ID_O, (j > 0 || k > 0) ? 1u : 0u);
-        }
-        umma_commit_elected(leader, PVDONE(buf));
+      // Each kind in order; of the next S and the next O whichever can go first.  S of a tile takes the columns of the last but one,
+      // whose weights have been written (and S read) before its O is issued.
+      uint32_t js = 0, jo = 0;
+      const uint32_t n = (uint32_t)w.n;
+      long long since = clock64();
+#pragma unroll 1
+      while (jo < n && ok) {
+        bool idle = true;
+        if (js < n && js < jo + 2 && __all_sync(0xffffffffu, mbar_try(KFULL(sb.buf), sb.phase))) { issue_s(g + js); ++js; idle = false; }
+        if (jo < js && ok && __all_sync(0xffffffffu, mbar_try(PFULL((g + jo) & 1), ((g + jo) >> 1) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
+        if (!idle) since = clock64();
+        else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
+        ok = __all_sync(0xffffffffu, ok);
       }
+      g += n;
     }
   } else {
     // ------------------------------------------------------------------------------------- softmax, epilogue
@@ -503,14 +578,14 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
         const uint32_t buf = g & 1;
-        ok = mbar_wait(FFULL(g & 3), (g >> 2) & 1, abort_flag);
+        ok = wait_suspended(FFULL(g % PL::FACTS), (g / PL::FACTS) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_KV_FULL);
         __syncwarp();
-        const unsigned char* fact = s_fact + (g & 3) * PL::FACT;
+        const unsigned char* fact = s_fact + (g % PL::FACTS) * PL::FACT;
         const int ve = fact[t], ke = PL::MLA ? ve : fact[128 + t];
-        const bool valid = ((*reinterpret_cast<const uint32_t*>(fact + 256) >> (t >> 4)) & 1u) && sp.has(x);
+        const bool valid = reinterpret_cast<const uint32_t*>(fact + 256)[t >> 4] != ~0u && sp.has(x);
         __syncwarp();
-        if (lane == 0) mbar_arrive(FEMPTY(g & 3));
+        if (lane == 0) mbar_arrive(FEMPTY(g % PL::FACTS));
         // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 f_v + T): both are multiples of e = 2^(y - M + half), half way
         // between them, so that neither is lost below 2^-126 where the factors of a sequence span more than fp32 does.
         const float half = 0.5f * ((float)paged4_log2_factor(ve) + paged8_t_bits(NH)), f_t = ex2(half), f_l = ex2(paged8_t_bits(NH) - half);
@@ -518,7 +593,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         const float offset = weight_offset(x);
         const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
 
-        ok = mbar_wait(SFULL(buf), (g >> 1) & 1, abort_flag);
+        ok = wait_suspended(SFULL(buf), (g >> 1) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_S_FULL);
         __syncwarp();
         tc_fence_after();
@@ -571,11 +646,11 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
           for (int i = 0; i < ROWS; ++i) { z[i] -= s_d[hb + i]; l[i] *= s_f[hb + i]; }
         }
         if (g > 1) {                                         // the weights of the tile before the last one have been read
-          ok = mbar_wait(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
+          ok = wait_suspended(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
         }
         if (raise && j > 0) {                                // O is complete up to the last tile
-          ok = mbar_wait(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
+          ok = wait_suspended(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
           __syncwarp();
           tc_fence_after();
@@ -645,7 +720,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       group_sync(grp);
       more = w.next(p);
       if (more) load_q(w, seg + 1);
-      ok = mbar_wait(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
+      ok = wait_suspended(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
       tc_fence_after();
