@@ -124,19 +124,26 @@ struct Paged4Plan {
   static constexpr int TM_S = 2 * NV * NH, TM_USED = TM_S + 4 * NH;
   static constexpr int TM_COLS = TM_USED <= 64 ? 64 : TM_USED <= 128 ? 128 : TM_USED <= 256 ? 256 : 512;
   static constexpr int CTAS = (MLA && DS == 512) || NH == 32 ? 1 : 2;        // per SM
-  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, THREADS = 32 * (W_LOOK + 1);
+  // Packed rows come by bulk copies into shared memory where there is room for it, else straight to the registers of the threads that
+  // expand them.
+  static constexpr bool STAGED = !(MLA && DS == 512);
+  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_LOAD = W_LOOK + (STAGED ? 1 : 0);
+  static constexpr int THREADS = 32 * (W_LOAD + 1);
+  static constexpr int STAGE = STAGED ? 128 * (DS + DP) / 2 : 0, ST_POS = 128 * DS / 2;      // codes of a tile: latents or V, keys
   // 32 values at a time: a thread's share of a tile, latents (V) and keys; tiles of them that are on their way to its registers
-  static constexpr int U_SEM = DS * 128 / 32 / (32 * EW), U_POS = DP * 128 / 32 / (32 * EW), UNITS = U_SEM + U_POS, DEPTH = UNITS > 4 ? 1 : 2;
-  static constexpr int FACTS = 8, FACT = 256 + 48;           // per tile: exponents of values and of keys, where its rows are
+  static constexpr int U_SEM = DS * 128 / 32 / (32 * EW), U_POS = DP * 128 / 32 / (32 * EW), UNITS = U_SEM + U_POS;
+  // per tile: exponents of values and of keys, where its rows are, STAGED: shifts
+  static constexpr int FACTS = 4, F_GROUP = 256, F_SPAN = 288, F_SHS = 304, F_SHP = F_SHS + (STAGED ? 2 * DS : 0), FACT = F_SHP + (STAGED ? 2 * DP : 0);
   // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers and scalars first, then the table.
   static constexpr int MISC_BYTES = 512 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH) + FACTS * FACT;
   static constexpr int BUDGET = CTAS == 1 ? 227 * 1024 : 113 * 1024;
-  static constexpr int BUFS_FIT = (BUDGET - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / TILE;
-  static constexpr int BUFS = BUFS_FIT > 4 ? 4 : BUFS_FIT;   // expanded tiles
-  static constexpr int OFF_Q = BUFS * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_MISC = OFF_P + 2 * P_BYTES;
+  static constexpr int BUFS = CTAS == 1 && STAGED ? 3 : 2;   // expanded tiles
+  static constexpr int STAGES_FIT = STAGED ? (BUDGET - BUFS * TILE - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / (STAGED ? STAGE : 1) : 0;
+  static constexpr int STAGES = STAGES_FIT > 4 ? 4 : STAGES_FIT;
+  static constexpr int OFF_Q = BUFS * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_STAGE = OFF_P + 2 * P_BYTES, OFF_MISC = OFF_STAGE + STAGES * STAGE;
   static constexpr int SMEM = OFF_MISC + MISC_BYTES;
-  static_assert(BUFS >= 2 && SMEM <= BUDGET && OFF_MISC % 16 == 0 && OFF_Q % 1024 == 0, "one tile is expanded while another is used");
-  static_assert(THREADS / 32 <= 26, "room for the sums of the ranges");
+  static_assert((!STAGED || STAGES >= 2) && SMEM <= BUDGET && OFF_MISC % 16 == 0 && OFF_Q % 1024 == 0 && FACT % 16 == 0, "one tile is expanded while another is used");
+  static_assert(THREADS <= 32 * 28, "72 registers a thread");
 };
 
 // one group of softmax warps (128 threads)
@@ -163,6 +170,10 @@ __device__ __forceinline__ void tmem_st(uint32_t at, const uint32_t (&r)[N]) {
   else
     asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"r"(at), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 // 16 bytes that are read once
 __device__ __forceinline__ uint4 load_stream(const void* p) {
@@ -191,7 +202,7 @@ __device__ __forceinline__ bool wait_suspended(uint32_t bar, uint32_t parity, vo
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
   constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
-  constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOOK = PL::W_LOOK;
+  constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOOK = PL::W_LOOK, W_LOAD = PL::W_LOAD;
   const Paged8Params& p = a.b;
   extern __shared__ __align__(1024) unsigned char smem_p4[];
   unsigned char* base_ptr = smem_p4;
@@ -201,19 +212,21 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
   auto SFULL = [&](uint32_t i) { return bars + 8 * i; };
   auto PFULL = [&](uint32_t i) { return bars + 16 + 8 * i; };
   auto PVDONE = [&](uint32_t i) { return bars + 32 + 8 * i; };
-  // BUFS of each: keys / values expanded, read by the products (MLA: the keys' barriers are not used for the latter)
+  // BUFS of each: keys / values expanded, read by the products (MLA: latents are both, KFULL and VEMPTY)
   auto KFULL = [&](uint32_t i) { return bars + 48 + 8 * i; };
-  auto VFULL = [&](uint32_t i) { return bars + 80 + 8 * i; };
-  auto KEMPTY = [&](uint32_t i) { return bars + 112 + 8 * i; };
-  auto VEMPTY = [&](uint32_t i) { return bars + 144 + 8 * i; };
-  auto FFULL = [&](uint32_t i) { return bars + 176 + 8 * i; };          // facts of a tile written, read
-  auto FEMPTY = [&](uint32_t i) { return bars + 240 + 8 * i; };
-  const uint32_t QFULL = bars + 304;
+  auto VFULL = [&](uint32_t i) { return bars + 128 + 8 * i; };
+  auto KEMPTY = [&](uint32_t i) { return bars + 152 + 8 * i; };
+  auto VEMPTY = [&](uint32_t i) { return bars + 176 + 8 * i; };
+  auto FFULL = [&](uint32_t i) { return bars + 240 + 8 * i; };          // facts of a tile written, read
+  auto FEMPTY = [&](uint32_t i) { return bars + 272 + 8 * i; };
+  auto GFULL = [&](uint32_t i) { return bars + 304 + 8 * i; };          // packed tile landed, read
+  auto GEMPTY = [&](uint32_t i) { return bars + 336 + 8 * i; };
+  const uint32_t QFULL = bars + 368;
   unsigned char* misc = base_ptr + PL::OFF_MISC;
-  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 320);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 324);
-  int* s_b = reinterpret_cast<int*>(misc + 328);
-  long long* s_off = reinterpret_cast<long long*>(misc + 336);          // offset inside sequence s_b, tiles of this CTA
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(misc + 384);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(misc + 388);
+  int* s_b = reinterpret_cast<int*>(misc + 392);
+  long long* s_off = reinterpret_cast<long long*>(misc + 400);          // offset inside sequence s_b, tiles of this CTA
   uint2* s_table = reinterpret_cast<uint2*>(misc + 512);
   float* s_qs = reinterpret_cast<float*>(misc + 640);
   float* s_m = s_qs + NH; float* s_d = s_m + NH; float* s_f = s_d + NH;
@@ -227,10 +240,13 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 
   if (tid == 0) {
     *abort_flag = 0;
-    *reinterpret_cast<uint32_t*>(misc + 352) = 16u;
+    *reinterpret_cast<uint32_t*>(misc + 416) = 16u;
     for (int i = 0; i < 2; ++i) { mbar_init(SFULL(i), 1); mbar_init(PFULL(i), 32 * PL::SOFTMAX_WARPS); mbar_init(PVDONE(i), 1); }
-    for (int i = 0; i < 4; ++i) { mbar_init(KFULL(i), PL::EW); mbar_init(VFULL(i), PL::EW); mbar_init(KEMPTY(i), 1); mbar_init(VEMPTY(i), 1); }
-    for (int i = 0; i < PL::FACTS; ++i) { mbar_init(FFULL(i), 1); mbar_init(FEMPTY(i), PL::SOFTMAX_WARPS + PL::EW); }
+    for (int i = 0; i < PL::BUFS; ++i) {
+      mbar_init(KFULL(i), PL::EW); mbar_init(VFULL(i), PL::EW); mbar_init(KEMPTY(i), 1); mbar_init(VEMPTY(i), 1);
+    }
+    for (int i = 0; i < 4; ++i) { mbar_init(GFULL(i), 1); mbar_init(GEMPTY(i), PL::EW); }
+    for (int i = 0; i < PL::FACTS; ++i) { mbar_init(FFULL(i), 1); mbar_init(FEMPTY(i), PL::SOFTMAX_WARPS + PL::EW + (PL::STAGED ? 1 : 0)); }
     mbar_init(QFULL, 32 * PL::SOFTMAX_WARPS);
     fence_mbar_init();
     if (base & 1023u) fail(100);                             // the operands' images need it
@@ -274,24 +290,38 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       return y.any && (unsigned)y.page < (unsigned)p.n_pages
                  ? (((uint32_t)y.page * (uint32_t)p.Hkv + (uint32_t)y.hk) << (p.page_log2 - 4)) + (uint32_t)(lane & ((p.page >> 4) - 1)) : ~0u;
     };
-    auto exponents = [&](uint32_t group, uint32_t& v, uint32_t& k) {
+    // exponents of this lane's four rows, and their shifts: DS / 64 (DP / 64) bytes a row
+    constexpr int WS = PL::STAGED ? DS / 64 : 1, WP = PL::STAGED ? DP / 64 : 1;
+    struct Scales { uint32_t v, k, ss[WS], sp[WP]; };
+    auto scales_of = [&](uint32_t group, Scales& y) {
       const uint32_t gr = __shfl_sync(0xffffffffu, group, lane >> 2);
-      v = k = 0;
+      y.v = y.k = 0;
+#pragma unroll
+      for (int i = 0; i < WS; ++i) y.ss[i] = 0;
+#pragma unroll
+      for (int i = 0; i < WP; ++i) y.sp[i] = 0;
       if (gr == ~0u) return;
-      v = __ldg(reinterpret_cast<const uint32_t*>(a.exp_v) + (size_t)gr * 4 + (lane & 3));
-      if (!PL::MLA) k = __ldg(reinterpret_cast<const uint32_t*>(a.exp_k) + (size_t)gr * 4 + (lane & 3));
+      const size_t at = (size_t)gr * 4 + (lane & 3);
+      y.v = __ldg(reinterpret_cast<const uint32_t*>(a.exp_v) + at);
+      if (!PL::MLA) y.k = __ldg(reinterpret_cast<const uint32_t*>(a.exp_k) + at);
+      if (PL::STAGED) {
+#pragma unroll
+        for (int i = 0; i < WS; ++i) y.ss[i] = __ldg(reinterpret_cast<const uint32_t*>(a.shift_sem) + at * WS + i);
+#pragma unroll
+        for (int i = 0; i < WP; ++i) y.sp[i] = __ldg(reinterpret_cast<const uint32_t*>(a.shift_pos) + at * WP + i);
+      }
     };
     Tile t0, t1;
-    uint32_t g0, v0, k0;
+    uint32_t g0;
+    Scales s0, s1;
     look(t0);
     look(t1);
     g0 = group_of(t0);
-    exponents(g0, v0, k0);
+    scales_of(g0, s0);
     uint32_t f = 0, phase = 0;
     while (ok && t0.any) {
       const uint32_t g1 = group_of(t1);
-      uint32_t v1, k1;
-      exponents(g1, v1, k1);
+      scales_of(g1, s1);
       Tile t2;
       look(t2);
       ok = wait_suspended(FEMPTY(f), phase ^ 1, abort_flag);
@@ -299,23 +329,67 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
       unsigned char* fact = s_fact + f * PL::FACT;
       const bool all = (__ballot_sync(0xffffffffu, g0 != ~0u) & 0xffu) == 0xffu && (t0.lo >= 128 || (t0.mid <= 0 && t0.hi >= 128));
-      reinterpret_cast<uint32_t*>(fact)[lane] = v0;
-      if (!PL::MLA) reinterpret_cast<uint32_t*>(fact + 128)[lane] = k0;
-      if (lane < 8) reinterpret_cast<uint32_t*>(fact + 256)[lane] = g0;
-      if (lane == 8) *reinterpret_cast<int4*>(fact + 288) = make_int4(all, t0.lo, t0.mid, t0.hi);
+      reinterpret_cast<uint32_t*>(fact)[lane] = s0.v;
+      if (!PL::MLA) reinterpret_cast<uint32_t*>(fact + 128)[lane] = s0.k;
+      if (lane < 8) reinterpret_cast<uint32_t*>(fact + PL::F_GROUP)[lane] = g0;
+      if (lane == 8) *reinterpret_cast<int4*>(fact + PL::F_SPAN) = make_int4(all, t0.lo, t0.mid, t0.hi);
+      if (PL::STAGED) {                                      // of absent rows: whatever they hold must be no NaN
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const int r = 4 * lane + i; m |= all || r < t0.lo || (r >= t0.mid && r < t0.hi) ? 0xffu << (8 * i) : 0u; }
+        // a row's bytes: one (WS = 1), or two, which lie in one half of a word
+#pragma unroll
+        for (int i = 0; i < WS; ++i) reinterpret_cast<uint32_t*>(fact + PL::F_SHS)[lane * WS + i] = s0.ss[i] & (WS == 1 ? m : __byte_perm(m, 0u, i ? 0x3322 : 0x1100));
+#pragma unroll
+        for (int i = 0; i < WP; ++i) reinterpret_cast<uint32_t*>(fact + PL::F_SHP)[lane * WP + i] = s0.sp[i] & (WP == 1 ? m : __byte_perm(m, 0u, i ? 0x3322 : 0x1100));
+      }
       __syncwarp();
       if (lane == 0) mbar_arrive(FFULL(f));
       if (++f == PL::FACTS) { f = 0; phase ^= 1; }
-      t0 = t1; t1 = t2; g0 = g1; v0 = v1; k0 = k1;
+      t0 = t1; t1 = t2; g0 = g1; s0 = s1;
+    }
+  } else if (PL::STAGED && warp == W_LOAD) {
+    // --------------------------------------------------------------------------------------------- loads
+    // A request for each page (or the 128 rows of it that belong to the tile) and part; a lane's requests are issued one after the other,
+    // 200 clocks each, so the small arrays come another way (with the look-ups).
+    const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
+    bool ok = !*abort_flag;
+    uint32_t f = 0, fphase = 0, stage = 0, phase = 0;
+    const int per = p.page >> 4;                             // groups of 16 rows to a request
+#pragma unroll 1
+    for (int t = 0; t < n_tiles && ok; ++t) {
+      ok = wait_suspended(FFULL(f), fphase, abort_flag);
+      if (ok) ok = wait_suspended(GEMPTY(stage), phase ^ 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);
+      if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
+      // lane: request + 8 * part
+      const uint32_t* groups = reinterpret_cast<const uint32_t*>(s_fact + f * PL::FACT + PL::F_GROUP);
+      const int first = (lane & 7) * per;
+      uint32_t gr = ~0u;
+      // a page that is present in part: groups without a present row are not looked up, the page starts at its first one that is
+      if (first < 8)
+        for (int i = 0; i < per; ++i) { const uint32_t y = groups[first + i]; if (gr == ~0u && y != ~0u) gr = y - i; }
+      const unsigned there = __popc(__ballot_sync(0xffffffffu, gr != ~0u) & 0xffu);
+      if (lane == 0) mbar_expect_tx(GFULL(stage), there * p.page * ((DS + DP) / 2));
+      __syncwarp();
+      if (lane == 0) mbar_arrive(FEMPTY(f));
+      const uint32_t at = base + PL::OFF_STAGE + stage * PL::STAGE;
+      if (gr != ~0u && lane < 16) {
+        if (lane < 8) bulk_copy(at + first * 16 * (DS / 2), a.sem + (size_t)gr * (16 * (DS / 2)), p.page * (DS / 2), GFULL(stage));
+        else bulk_copy(at + PL::ST_POS + first * 16 * (DP / 2), a.pos + (size_t)gr * (16 * (DP / 2)), p.page * (DP / 2), GFULL(stage));
+      }
+      __syncwarp();
+      if (++f == PL::FACTS) { f = 0; fphase ^= 1; }
+      if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
     }
   } else if (warp >= W_EXP && warp < W_MMA) {
     // ----------------------------------------------------------------------------------------------- expansion
     // A thread takes 32 values (16 bytes of codes) of a row at a time, from HBM to registers while it expands those of the tile
     // before.  Eight neighbouring lanes write two rows, so that their units fall on all banks of the swizzled image.
-    const int et = tid - 32 * W_EXP, ew = warp - W_EXP;
+    const int et = tid - 32 * W_EXP;
     const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
     bool ok = !*abort_flag;
-    const uint32_t sixteen = *reinterpret_cast<const volatile uint32_t*>(misc + 352);
+    const uint32_t sixteen = *reinterpret_cast<const volatile uint32_t*>(misc + 416);
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
       if (ok && !wait_suspended(bar, ph, abort_flag)) { fail(code); ok = false; }
       ok = __all_sync(0xffffffffu, ok);
@@ -328,13 +402,11 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     constexpr bool LATENT = PL::MLA && DS == 512;
     constexpr int US = PL::VW / 32, UP = DP / 32, STEP = 32 * PL::EW;
     // unit i of this thread: row and unit in the row, place in the expanded tile
-    //   512 latents: a warp takes two rows at a time, its quarter q the chunk q of the first and q ^ 1 of the second
-    //   otherwise: neighbouring threads neighbouring units
-    const int c = LATENT ? (lane >> 3) ^ ((lane >> 2) & 1) : 0;
-    auto sem_row = [&](int i) { return LATENT ? 16 * i + 2 * ew + ((lane >> 2) & 1) : (et + STEP * i) / US; };
-    const int sem_u = LATENT ? 4 * c + (lane & 3) : et % US, pos_u = et % UP;
+    // (512 latents: units 2 c and 2 c + 1 of chunk c), neighbouring threads neighbouring units
+    auto sem_row = [&](int i) { return (et + STEP * (LATENT ? i & 1 : i)) / US; };
+    const int sem_u = et % US, pos_u = et % UP;
     auto pos_row = [&](int i) { return (et + STEP * i) / UP; };
-    const uint32_t sem_to = (PL::MLA ? c * 16384 : PL::K_BYTES) + swz<PL::VW>(sem_row(0), 2 * (lane & (US - 1)));
+    const uint32_t sem_to = (PL::MLA ? 0 : PL::K_BYTES) + swz<PL::VW>(sem_row(0), 2 * sem_u);
     const uint32_t pos_to = PL::KSEM * 16384 + swz<DP>(pos_row(0), 2 * pos_u);
     struct Facts { bool all; int lo, mid, hi; const uint32_t* group; };
     auto has = [&](const Facts& f, int r) { return f.all || r < f.lo || (r >= f.mid && r < f.hi); };
@@ -381,63 +453,86 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         *reinterpret_cast<uint4*>(base_ptr + (dst ^ 16u) + i * step) = make_uint4(x2.x, x2.y, x3.x, x3.y);
       }
     };
-    constexpr int BATCH = PL::U_SEM > 4 ? 4 : PL::U_SEM;
+    constexpr int BATCH = LATENT ? 2 : PL::U_SEM;
     using CP = std::integral_constant<int, PL::U_POS>;
     using CS = std::integral_constant<int, BATCH>;
-    auto load_sem = [&](Unit* x, const Facts& f, int i0) { load(CS(), x, i0, f, sem_row, a.sem, a.shift_sem, DS, sem_u); };
+    auto load_sem = [&](Unit* x, const Facts& f, int i0) { load(CS(), x, i0, f, sem_row, a.sem, a.shift_sem, DS, sem_u + (LATENT ? 2 * i0 : 0)); };
     auto load_pos = [&](Unit* x, const Facts& f) { load(CP(), x, 0, f, pos_row, a.pos, a.shift_pos, DP, pos_u); };
     uint32_t ff = 0, fphase = 0;
     auto facts = [&](Facts& f, bool any) {                   // of the next tile; its groups are read until `signal`
       if (!any) return;
       if (!wait(FFULL(ff), fphase, ERR_WAIT_KV_FULL)) return;
       const unsigned char* fact = s_fact + ff * PL::FACT;
-      const int4 y = *reinterpret_cast<const int4*>(fact + 288);
-      f = Facts{y.x != 0, y.y, y.z, y.w, reinterpret_cast<const uint32_t*>(fact + 256)};
+      const int4 y = *reinterpret_cast<const int4*>(fact + PL::F_SPAN);
+      f = Facts{y.x != 0, y.y, y.z, y.w, reinterpret_cast<const uint32_t*>(fact + PL::F_GROUP)};
     };
     auto facts_done = [&](bool any) {
       if (!any) return;
       signal(FEMPTY(ff));
       if (++ff == PL::FACTS) { ff = 0; fphase ^= 1; }
     };
-    constexpr int DEPTH = PL::DEPTH;
-    Unit sem[DEPTH][PL::U_SEM], pos[DEPTH][PL::U_POS];
-    Facts fx = {};
-#pragma unroll
-    for (int k = 0; k < DEPTH; ++k) {
-      const bool any = k < n_tiles;
-      facts(fx, any);
-      if (any && ok) {
-        load_pos(pos[k], fx);
-#pragma unroll
-        for (int i = 0; i < PL::U_SEM; i += BATCH) load_sem(sem[k] + i, fx, i);
-        facts_done(any);
-      }
-    }
     uint32_t buf = 0, use = 0;                               // use: how often the buffer has been filled before
-#pragma unroll 1
-    for (int t1 = 0; t1 < n_tiles && ok; t1 += DEPTH) {
+    Unit sem[PL::U_SEM], pos[PL::U_POS];
+    Facts fx = {};
+    constexpr uint32_t SEM_APART = STEP / US * PL::VW, POS_APART = (STEP / UP) * DP;
+    if constexpr (!PL::STAGED) {
+      facts(fx, n_tiles > 0);
+      if (n_tiles > 0 && ok) {
+        load_pos(pos, fx);
 #pragma unroll
-      for (int k = 0; k < DEPTH; ++k) {
-        const int t = t1 + k;
-        if (t >= n_tiles || !ok) break;
-        const bool any = t + DEPTH < n_tiles;
+        for (int i = 0; i < PL::U_SEM; i += BATCH) load_sem(sem + i, fx, i);
+        facts_done(true);
+      }
+#pragma unroll 1
+      for (int t = 0; t < n_tiles && ok; ++t) {
+        const bool any = t + 1 < n_tiles;
         const uint32_t tile = buf * PL::TILE;
+        if (use > 0 && !wait(VEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
+        put(CP(), pos, pos_u, tile + pos_to, POS_APART);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) put(CS(), sem + BATCH * c, sem_u, tile + sem_to + c * 16384, SEM_APART);
+        // the fence waits for loads under way too: those of the next tile come behind it
+        fence_proxy_async_smem();
+        signal(KFULL(buf));
         facts(fx, any);
+        if (any) {
+          load_pos(pos, fx);
+#pragma unroll
+          for (int c = 0; c < NV; ++c) load_sem(sem + BATCH * c, fx, BATCH * c);
+        }
+        facts_done(any);
+        if (++buf == PL::BUFS) { buf = 0; ++use; }
+      }
+    } else {
+      uint32_t stage = 0, phase = 0;
+#pragma unroll 1
+      for (int t = 0; t < n_tiles; ++t) {
+        const uint32_t tile = buf * PL::TILE;
+        if (!wait(FFULL(ff), fphase, ERR_WAIT_KV_FULL) || !wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
+        const unsigned char* fact = s_fact + ff * PL::FACT;
+        const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
+#pragma unroll
+        for (int i = 0; i < PL::U_POS; ++i) {
+          pos[i].v = *reinterpret_cast<const uint4*>(st + PL::ST_POS + (et + STEP * i) * 16);
+          pos[i].s = fact[PL::F_SHP + pos_row(i) * (DP / 64) + (pos_u >> 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < PL::U_SEM; ++i) {
+          sem[i].v = *reinterpret_cast<const uint4*>(st + (et + STEP * i) * 16);
+          sem[i].s = fact[PL::F_SHS + sem_row(i) * (DS / 64) + (sem_u >> 1)];
+        }
+        __syncwarp();
+        if (lane == 0) { mbar_arrive(GEMPTY(stage)); mbar_arrive(FEMPTY(ff)); }
+        if (++ff == PL::FACTS) { ff = 0; fphase ^= 1; }
+        if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
         if (use > 0 && !wait(PL::MLA ? VEMPTY(buf) : KEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
-        put(CP(), pos[k], pos_u, tile + pos_to, (STEP / UP) * DP);
-        if (any) load_pos(pos[k], fx);
+        put(CP(), pos, pos_u, tile + pos_to, POS_APART);
         if constexpr (!PL::MLA) {
           fence_proxy_async_smem();
           signal(KFULL(buf));
           if (use > 0 && !wait(VEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
         }
-#pragma unroll
-        for (int i = 0; i < PL::U_SEM; i += BATCH) {
-          constexpr int APART = (LATENT ? 16 : STEP / US) * PL::VW;
-          put(CS(), sem[k] + i, sem_u, tile + sem_to + i * APART, APART);
-          if (any) load_sem(sem[k] + i, fx, i);
-        }
-        facts_done(any);
+        put(CS(), sem, sem_u, tile + sem_to, SEM_APART);
         fence_proxy_async_smem();
         signal(PL::MLA ? KFULL(buf) : VFULL(buf));
         if (++buf == PL::BUFS) { buf = 0; ++use; }
@@ -460,7 +555,6 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     };
     auto issue_s = [&](uint32_t t) {
       const uint32_t buf = t & 1, d = tmem + PL::TM_S + buf * 2 * NH, tile = base + sb.buf * PL::TILE;
-      if (!wait(KFULL(sb.buf), sb.phase, ERR_WAIT_KV_FULL)) return;
       tc_fence_after();
       uint32_t acc = 0;
 #pragma unroll
@@ -583,7 +677,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         __syncwarp();
         const unsigned char* fact = s_fact + (g % PL::FACTS) * PL::FACT;
         const int ve = fact[t], ke = PL::MLA ? ve : fact[128 + t];
-        const bool valid = reinterpret_cast<const uint32_t*>(fact + 256)[t >> 4] != ~0u && sp.has(x);
+        const bool valid = reinterpret_cast<const uint32_t*>(fact + PL::F_GROUP)[t >> 4] != ~0u && sp.has(x);
         __syncwarp();
         if (lane == 0) mbar_arrive(FEMPTY(g % PL::FACTS));
         // The row sum needs 2^(y - M), the weight t = 2^(y - M + log2 f_v + T): both are multiples of e = 2^(y - M + half), half way
