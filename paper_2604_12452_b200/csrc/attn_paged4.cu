@@ -35,6 +35,14 @@ struct Paged4Params {
 };
 
 
+// whether the phase is complete, at once (try_wait may suspend the thread while the other barrier that it looks at completes)
+__device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+
 static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
 static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
 
@@ -598,8 +606,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 #pragma unroll 1
       while (jo < n && ok) {
         bool idle = true;
-        if (js < n && js < jo + 2 && __all_sync(0xffffffffu, mbar_try(KFULL(sb.buf), sb.phase))) { issue_s(g + js); ++js; idle = false; }
-        if (jo < js && ok && __all_sync(0xffffffffu, mbar_try(PFULL((g + jo) & 1), ((g + jo) >> 1) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
+        if (js < n && js < jo + 2 && __all_sync(0xffffffffu, phase_done(KFULL(sb.buf), sb.phase))) { issue_s(g + js); ++js; idle = false; }
+        if (jo < js && ok && __all_sync(0xffffffffu, phase_done(PFULL((g + jo) & 1), ((g + jo) >> 1) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
         if (!idle) since = clock64();
         else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
         ok = __all_sync(0xffffffffu, ok);
