@@ -28,6 +28,7 @@ SOURCES = {
     "attn_paged8_pair.cu": [],
     "paged4.cu": [],
     "attn_paged4.cu": [],
+    "attn_paged4_pair.cu": [],
     "rope.cu": [],                # angles in 64 bits, accurate sines
     "verify.cu": [],              # 64-bit sums decide the tokens
 }

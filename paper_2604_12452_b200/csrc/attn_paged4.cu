@@ -19,29 +19,12 @@
 // Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
 #include <cstring>
 
-#include "attn_paged8.cuh"
-#include "fp4_common.cuh"
+#include "attn_paged4.cuh"
 
 namespace lca {
 using namespace tc;
 
 static __device__ int g_paged4_status = 0;
-
-struct Paged4Params {
-  Paged8Params b;             // without the tensor maps and the scales
-  const uint8_t* sem; const uint8_t* pos;
-  const uint8_t* shift_sem; const uint8_t* shift_pos;
-  const uint8_t* exp_k; const uint8_t* exp_v;
-};
-
-
-// whether the phase is complete, at once (try_wait may suspend the thread while the other barrier that it looks at completes)
-__device__ __forceinline__ bool phase_done(uint32_t bar, uint32_t parity) {
-  uint32_t done;
-  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-               : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-  return done != 0;
-}
 
 static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
 static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
@@ -183,30 +166,6 @@ __device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, ui
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// 16 bytes that are read once
-__device__ __forceinline__ uint4 load_stream(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-
-// A bounded wait that leaves its issue slots to the others: the hardware is told to suspend the thread for up to 2 us at a time.
-// (Every warp of this kernel waits for most of a tile; polling as fast as possible took a quarter of all issue slots.)
-__device__ __forceinline__ bool wait_suspended(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  auto poll = [&]() {
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
-    return done != 0;
-  };
-  if (poll()) return true;
-  const long long t0 = clock64();
-  while (true) {
-    if (poll()) return true;
-    if (*abort_flag || clock64() - t0 > WAIT_TIMEOUT_CYCLES) return false;
-  }
-}
-
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
   constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
@@ -860,12 +819,16 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head, else blocks of 32.
+// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head, else blocks of 32.  MLA 512 + 64
+// with more than 64 rows: blocks of 128 on CTA pairs
+// (64 x 5056 rows: 128 query rows 128 us, in blocks of 32 on single CTAs 232; 64 query rows 126 and 123).
 static int paged4_rows_per_tile(const lca_params* p, int q_len) {
-  return (long long)q_len * (p->n_q_heads / p->n_kv_heads) <= 16 ? 16 : 32;
+  const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
+  if (p->d_sem == 512 && rows > 64) return 128;
+  return rows <= 16 ? 16 : 32;
 }
-// CTAs that share the work: all that are resident at once.
-static int paged4_grid(const lca_params* p, int nh) { return p->d_sem == 512 || nh == 32 ? 148 : 2 * 148; }
+// CTAs (or pairs) that share the work: all that are resident at once.
+static int paged4_grid(const lca_params* p, int nh) { return nh == 128 ? 74 : p->d_sem == 512 || nh == 32 ? 148 : 2 * 148; }
 size_t attn_paged4_workspace_bytes(const lca_params* p, int q_len) {
   const int nh = paged4_rows_per_tile(p, q_len), grid = paged4_grid(p, nh);
   return (size_t)2 * grid * (nh * (size_t)p->d_sem + 2 * nh) * sizeof(float) + ((size_t)p->batch + 2) * sizeof(long long) + 64;
@@ -882,6 +845,7 @@ static int paged4_launch(Paged4Params& P, cudaStream_t stream) {
 template <bool MLA, int DS, int DP>
 static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
   const long long rows = (long long)P.b.q_len * P.b.rep;
+  if constexpr (DS == 512) if (nh == 128) return attn_paged4_pair_launch(P, stream);
   if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
   if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
   if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);
@@ -899,6 +863,7 @@ static void paged4_params(const Paged4Attn& q, Paged4Params& P) {
   Paged8Params& b = P.b;
   b.q_sem = (const bf16*)q.q_sem; b.q_pos = (const bf16*)q.q_pos; b.table = c->block_table;
   b.n_rep = q.n_rep; b.n_tok = q.n_tok; b.out = (bf16*)q.out; b.lse = q.lse;
+  b.out_wide = (reinterpret_cast<uintptr_t>(q.out) & 31u) == 0;
   b.B = p->batch; b.Hq = p->n_q_heads; b.Hkv = p->n_kv_heads; b.q_len = q.q_len; b.g = q.n_rep ? p->group_size : 1;
   b.page = c->page_size; b.page_log2 = c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7;
   b.n_pages = c->n_pages; b.width = c->table_width; b.rep = b.Hq / b.Hkv;
@@ -945,7 +910,8 @@ int attn_paged4_take_status() {
     int zero = 0;
     cudaMemcpyToSymbol(g_paged4_status, &zero, sizeof(int));
   }
-  return st;
+  const int pair = attn_paged4_pair_take_status();
+  return pair != 0 ? pair : st;
 }
 
 }  // namespace lca

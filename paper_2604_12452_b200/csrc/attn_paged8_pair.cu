@@ -24,7 +24,7 @@
 // costs its thread over a thousand clocks (119 us instead of 91).  The tests compare repeated runs bit for bit.
 #include <cstring>
 
-#include "attn_paged8.cuh"
+#include "attn_paged_pair.cuh"
 
 namespace lca {
 using namespace tc;
@@ -50,31 +50,10 @@ static_assert(SMEM_BYTES <= 232448, "shared memory of one SM");
 static_assert(OFF_QS % 16 == 0 && OFF_FACT % 16 == 0, "alignment");
 }  // namespace p8pair
 
-__device__ __forceinline__ void umma_f8_pair_elected(uint32_t leader, uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
-                                                     uint32_t accumulate) {
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t"
-      "@q tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
-}
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint32_t bar) {
   asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
-// Offsets of the keys (weight_offset), read four at a time by whole warps.  Offsets for every row of a sequence would not fit; windows
-// of 128 of them that start anywhere are as evenly spread, so a tile takes one of 1024 windows, in an order in which any number
-// of successive ones is even as well.
-constexpr int WINDOWS = 1024, WINDOW_ORDER = 613;
-struct OffsetTable {
-  float v[4 * WINDOWS + 128];
-  constexpr OffsetTable() : v() {
-    for (int i = 0; i < 4 * WINDOWS + 128; ++i) v[i] = (float)(int32_t)((uint32_t)i * GOLDEN) * 0x1p-41f;
-  }
-};
-__constant__ const OffsetTable g_offsets{};
-
-// bits [0, n) of a word of 64; n may be anything
-__device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1ull; }
 
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(p8pair::THREADS, 1)
 attn_paged8_pair_kernel(const __grid_constant__ Paged8Params p) {
