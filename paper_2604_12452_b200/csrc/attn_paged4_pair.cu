@@ -24,7 +24,7 @@ static __device__ int g_paged4_pair_status = 0;
 
 namespace p4pair {
 constexpr int ROWS = 128, DS = 512, DP = 64;
-constexpr int SW = 8, EW = 8, W_EXP = SW, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_COPY = W_LOOK + 1, W_DONE = W_COPY + 1, THREADS = 32 * (W_DONE + 1);
+constexpr int SW = 8, EW = 8, W_EXP = SW, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_COPY = W_LOOK + 1, W_FWD = W_COPY + 1, THREADS = 32 * (W_FWD + 1);
 constexpr int Q_TERM = 4 * 64 * 128 + 64 * 64;               // 36 KB: four latent chunks and the rope chunk of 64 rows
 constexpr int K_CHUNK = 64 * 128, K_BUF = 4 * K_CHUNK + 64 * 64;      // the same of 64 keys
 constexpr int V_CHUNK = 128 * 128, V_BUF = 2 * V_CHUNK;      // 128 keys x 128 columns, twice
@@ -37,7 +37,7 @@ constexpr int OFF_BAR = OFF_MISC, OFF_SCALAR = OFF_BAR + 224, OFF_TABLE = OFF_SC
 constexpr int OFF_FACT = OFF_RED + 256 * 4, SMEM_BYTES = OFF_FACT + FACTS * FACT;
 constexpr int TM_S = 256, TM_COLS = 512;                     // O in columns 0..255, S in 256..319 and 320..383
 constexpr float T_BITS = paged8_t_bits(ROWS);
-constexpr float T_MAX = 11.f;                                // log2 of the largest weight: e5m2 leaves at most 2^8 of it to e4m3
+constexpr float T_MAX = 12.f;                                // log2 of the largest weight: e5m2 has steps of 2^9 below, and leaves at most 2^8 of it to e4m3
 static_assert(SMEM_BYTES <= 232448, "shared memory of one SM");
 static_assert(OFF_FACT % 16 == 0 && FACT % 16 == 0 && OFF_TABLE % 16 == 0, "alignment");
 }  // namespace p4pair
@@ -47,12 +47,13 @@ __device__ __forceinline__ void smem_copy(uint32_t dst_cluster, uint32_t src, ui
   asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                ::"r"(dst_cluster), "r"(src), "r"(bytes), "r"(bar_cluster) : "memory");
 }
-// all softmax warps
+// all softmax warps; the four of them that share 32 rows
 __device__ __forceinline__ void softmax_sync() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
-__device__ __forceinline__ bool softmax_or(bool v) {
+__device__ __forceinline__ void rows_sync(int half) { asm volatile("bar.sync %0, 128;" ::"r"(half + 2) : "memory"); }
+__device__ __forceinline__ bool rows_or(int half, bool v) {
   uint32_t r;
-  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 1, 256, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
-               : "=r"(r) : "r"((uint32_t)v) : "memory");
+  asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, %2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+               : "=r"(r) : "r"((uint32_t)v), "r"(half + 2) : "memory");
   return r != 0;
 }
 
@@ -229,17 +230,19 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     for (uint32_t t = 0; t < n_tiles && ok; ++t) {
       const uint32_t buf = t & 1, to = buf * K_BUF;
       if (t > 1 && !wait(KEMPTY(buf), ((t >> 1) - 1) & 1, ERR_WAIT_KV_EMPTY)) break;
+      uint2 tab[5];                                          // block 4 c + u of the row, two shifts a byte
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {                          // block 4 c + u of the row, two shifts a byte
-        const uint2 tab = s_table[((c < 2 ? shift.x : shift.y) >> (16 * (c & 1) + 4 * u)) & 15];
-        const uint2 x0 = paged4_expand(sem[c].x, tab, sixteen), x1 = paged4_expand(sem[c].y, tab, sixteen),
-                    x2 = paged4_expand(sem[c].z, tab, sixteen), x3 = paged4_expand(sem[c].w, tab, sixteen);
+      for (int c = 0; c < 4; ++c) tab[c] = s_table[((c < 2 ? shift.x : shift.y) >> (16 * (c & 1) + 4 * u)) & 15];
+      tab[4] = s_table[(shift_pos >> (4 * (u >> 1))) & 15];
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint2 x0 = paged4_expand(sem[c].x, tab[c], sixteen), x1 = paged4_expand(sem[c].y, tab[c], sixteen),
+                    x2 = paged4_expand(sem[c].z, tab[c], sixteen), x3 = paged4_expand(sem[c].w, tab[c], sixteen);
         *reinterpret_cast<uint4*>(smem + to + c * K_CHUNK + sem_to) = make_uint4(x0.x, x0.y, x1.x, x1.y);
         *reinterpret_cast<uint4*>(smem + to + c * K_CHUNK + (sem_to ^ 16u)) = make_uint4(x2.x, x2.y, x3.x, x3.y);
       }
       {
-        const uint2 tab = s_table[(shift_pos >> (4 * (u >> 1))) & 15];
-        const uint2 x0 = paged4_expand(pos.x, tab, sixteen), x1 = paged4_expand(pos.y, tab, sixteen);
+        const uint2 x0 = paged4_expand(pos.x, tab[4], sixteen), x1 = paged4_expand(pos.y, tab[4], sixteen);
         *reinterpret_cast<uint4*>(smem + to + pos_to) = make_uint4(x0.x, x0.y, x1.x, x1.y);
       }
       // the fence waits for loads under way too: those of the next tile come behind it
@@ -255,7 +258,6 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       for (uint32_t t = 0; t < n_tiles; ++t) {
         const uint32_t buf = t & 1;
         if (!wait_suspended(KLOCAL(buf), (t >> 1) & 1, abort_flag)) { fail(ERR_WAIT_KV_FULL); break; }
-        mbar_arrive_cluster_cta(mapa_u32(KFULL(buf), 0));
         // (both CTAs' values of the tile before the last one have been read: one signal to both)
         if (t > 1 && !wait_suspended(VEMPTY(buf), ((t >> 1) - 1) & 1, abort_flag)) { fail(ERR_WAIT_O_DONE); break; }
         mbar_expect_tx(VFULL(buf), V_BUF);                   // two copies of this CTA and two of the other one
@@ -267,16 +269,24 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
         }
       }
     }
-  } else if (warp == W_DONE) {
-    // ------------------------------------------------------------------------------------------ values are there
+  } else if (warp == W_FWD) {
+    // ------------------------------------------- keys are there: the product may start; values are there: so it may, and a keys' buffer is free
     if (lane == 0 && !*abort_flag) {
+      uint32_t k = 0, v = 0;
+      long long since = clock64();
 #pragma unroll 1
-      for (uint32_t t = 0; t < n_tiles; ++t) {
-        const uint32_t buf = t & 1;
-        if (!wait_suspended(VFULL(buf), (t >> 1) & 1, abort_flag)) { fail(ERR_WAIT_KV_FULL); break; }
-        mbar_arrive_cluster_cta(mapa_u32(KEMPTY(buf), 0));
-        mbar_arrive_cluster_cta(mapa_u32(KEMPTY(buf), 1));
-        if (rank == 1) mbar_arrive_cluster_cta(mapa_u32(VPEER(buf), 0));
+      while (v < n_tiles) {
+        bool idle = true;
+        if (k < n_tiles && phase_done(KLOCAL(k & 1), (k >> 1) & 1)) { mbar_arrive_cluster_cta(mapa_u32(KFULL(k & 1), 0)); ++k; idle = false; }
+        if (phase_done(VFULL(v & 1), (v >> 1) & 1)) {
+          mbar_arrive_cluster_cta(mapa_u32(KEMPTY(v & 1), 0));
+          mbar_arrive_cluster_cta(mapa_u32(KEMPTY(v & 1), 1));
+          if (rank == 1) mbar_arrive_cluster_cta(mapa_u32(VPEER(v & 1), 0));
+          ++v;
+          idle = false;
+        }
+        if (!idle) since = clock64();
+        else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { fail(ERR_WAIT_KV_FULL); break; }
       }
     }
   } else if (warp == W_MMA && rank == 0) {
@@ -298,9 +308,10 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     auto issue_s = [&](uint32_t t) {
       const uint32_t buf = t & 1, d = tmem + TM_S + 64 * buf, off = buf * (K_BUF / 16);
       tc_fence_after();
-#pragma unroll
+      // (rolled up, for the instructions of all these roles to be near: fetching them bound the kernel)
+#pragma unroll 1
       for (int c = 0; c < 4; ++c)
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < 4; ++k)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -315,11 +326,10 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     };
     auto issue_o = [&](uint32_t t, bool first) {
       const uint32_t buf = t & 1, off = buf * (V_BUF / 16);
-      if (!wait(VFULL(buf), (t >> 1) & 1, ERR_WAIT_KV_FULL) || !wait(VPEER(buf), (t >> 1) & 1, ERR_WAIT_PEER)) return;
       tc_fence_after();
-#pragma unroll
+#pragma unroll 1
       for (int n2 = 0; n2 < 2; ++n2)
-#pragma unroll
+#pragma unroll 1
         for (int k = 0; k < 4; ++k)
 #pragma unroll
           for (int h = 0; h < 2; ++h)
@@ -334,14 +344,18 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       tc_fence_after();
       // of the next S and the next O whichever can go first; S of a tile takes the columns of the last but one, whose S was
       // read before its weights were written and its O issued
-      uint32_t js = 0, jo = 0;
+      uint32_t js = 0, jo = 0, jv = 0;                       // jv: values that are there
       const uint32_t n = (uint32_t)w.n;
       long long since = clock64();
 #pragma unroll 1
       while (jo < n && ok) {
         bool idle = true;
         if (js < n && js < jo + 2 && __all_sync(0xffffffffu, phase_done(KFULL((g + js) & 1), ((g + js) >> 1) & 1))) { issue_s(g + js); ++js; idle = false; }
-        if (jo < js && ok && __all_sync(0xffffffffu, phase_done(PFULL, (g + jo) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
+        if (jv == jo) {
+          const uint32_t t = g + jv;
+          if (__all_sync(0xffffffffu, phase_done(VFULL(t & 1), (t >> 1) & 1) && phase_done(VPEER(t & 1), (t >> 1) & 1))) ++jv;
+        }
+        if (jo < js && jo < jv && __all_sync(0xffffffffu, phase_done(PFULL, (g + jo) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
         if (!idle) since = clock64();
         else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
         ok = __all_sync(0xffffffffu, ok);
@@ -481,22 +495,23 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
           top = fmaxf(top, most + __uint_as_float((q ? hw.y : hw.x) & 0xffff0000u));
         }
         float factor = 1.f;
-        if (softmax_or(unset || top > T_MAX)) {
+        if (rows_or(quad & 1, unset || top > T_MAX)) {
           top = -INFINITY;                                   // largest log2 t of this row's keys
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const uint4 kf = factors(i);
             const uint32_t f[4] = {kf.x, kf.y, kf.z, kf.w};
-            const float c = T_BITS - 127.f - h[i >> 1];
+            const float c = T_BITS - 127.f - h[i >> 1];      // (an exponent's bits below those of 2^23 are that many more: exact)
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float z0, z1;
               unpack_f32x2(z[4 * i + k], z0, z1);
-              top = max3(top, z0 + ((float)(f[k] >> 7 & 255u) + c), z1 + ((float)(f[k] >> 23) + c));
+              const float e0 = __uint_as_float(0x4b000000u | (f[k] >> 7 & 255u)) - 0x1p23f, e1 = __uint_as_float(0x4b000000u | f[k] >> 23) - 0x1p23f;
+              top = max3(top, z0 + (e0 + c), z1 + (e1 + c));
             }
           }
           s_red[cg * 128 + ln] = top;
-          softmax_sync();
+          rows_sync(quad & 1);
           top = fmaxf(fmaxf(s_red[rl], s_red[64 + rl]), fmaxf(s_red[128 + rl], s_red[192 + rl]));
           const bool raise = unset ? top > -INFINITY : top > T_MAX;
           const float d = raise ? top - T_BITS : 0.f;
