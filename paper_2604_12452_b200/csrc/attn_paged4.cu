@@ -524,13 +524,15 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       const uint32_t buf = t & 1, d = tmem + PL::TM_S + buf * 2 * NH, tile = base + sb.buf * PL::TILE;
       tc_fence_after();
       uint32_t acc = 0;
+#pragma unroll 1
+      for (int c = 0; c < PL::KSEM; ++c) {
+        const uint64_t ad = desc_rows(tile + c * 16384, 128, 16), bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, 128, 16);
 #pragma unroll
-      for (int c = 0; c < NK; ++c) {
-        const int width = c < PL::KSEM ? 128 : DP;
-        const uint64_t ad = desc_rows(tile + c * 16384, width, 16), bd = desc_rows(base + PL::OFF_Q + c * 2 * NH * 128, width, 16);
-#pragma unroll
-        for (int k = 0; k < width / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
+        for (int k = 0; k < 4; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
       }
+      const uint64_t ad = desc_rows(tile + PL::KSEM * 16384, DP, 16), bd = desc_rows(base + PL::OFF_Q + PL::KSEM * 2 * NH * 128, DP, 16);
+#pragma unroll
+      for (int k = 0; k < DP / 32; ++k) { umma_f8_elected(leader, d, desc_add(ad, 2 * k), desc_add(bd, 2 * k), ID_S, acc); acc = 1; }
       umma_commit_elected(leader, SFULL(buf));
       if (!PL::MLA) umma_commit_elected(leader, KEMPTY(sb.buf));
       sb.next();
@@ -540,7 +542,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       if (!PL::MLA && !wait(VFULL(ob.buf), ob.phase, ERR_WAIT_KV_FULL)) return;
       tc_fence_after();
       const uint64_t pd = desc_rows(base + PL::OFF_P + buf * PL::P_BYTES, 2 * NH, 128);
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < NV; ++c) {
         // 64-wide values: M stays 128, the second half of the operand is the unused half of their 16 KB and the output
         // lanes it feeds are never read
