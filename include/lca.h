@@ -439,7 +439,8 @@ int lca_paged4_read(const lca_params* p, const lca_paged4* cache, void* rows_sem
 
 /* Decode attention over the paged 4-bit cache: lca_decode_attention_paged8 on the values that this cache stands for, with the same
  * arguments and the same treatment of absent rows, of queries that see no row and of NaN.  The cached values enter the products
- * exactly; queries and weights are sums of two 8-bit terms as there (a weight to 2^-9 of itself or to a step of 2^-18 of the largest). */
+ * exactly; queries and weights are sums of two 8-bit terms as there: a weight to 2^-9 of itself or to a step of 2^-18 of the largest; MLA
+ * 512 + 64 with more than 64 rows (q_len * n_q_heads): 2^-8 and 2^-17. */
 size_t lca_paged4_workspace_bytes(const lca_params* p, const lca_paged4* cache, int32_t q_len);
 int lca_decode_attention_paged4(const lca_params* p, const lca_paged4* cache, const void* q_sem, const void* q_pos,
                                 int32_t q_len, const int32_t* n_rep, const int32_t* n_tok, void* out, float* lse_opt,
@@ -502,7 +503,7 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
  * either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
 typedef struct lca_verify_args {
   int32_t dtype;                /* of both probabilities: LCA_DTYPE_FP32 or LCA_DTYPE_BF16 */
-  int32_t batch, n_drafts, vocab;       /* n_drafts >= 0 */
+  int32_t batch, n_drafts, vocab;       /* n_drafts >= 0, vocab below 2^31 - 4096 */
   const void* target_probs;     /* [batch, n_drafts + 1, vocab]; they need not add up to 1 */
   const void* draft_probs;      /* [batch, n_drafts, vocab]; NULL: the drafter is certain (q_i(x_i) = 1, 0 elsewhere) */
   const int32_t* draft_tokens;  /* [batch, n_drafts] */

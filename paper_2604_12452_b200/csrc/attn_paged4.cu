@@ -10,13 +10,19 @@
 //
 // Transposed products, the key tile as the 128-row operand: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T, O^T [d x 2 NH] += V^T [T_hi | T_lo]^T.
 //   softmax    GROUPS groups of four warps, each for ROWS of the query rows: thread = key = TMEM lane; epilogue: thread = output column
-//   expansion  EW warps: packed rows from HBM straight to registers, DEPTH tiles ahead, to e4m3 in the operands' swizzled images
-//   + 1 warp   MMA issue and TMEM
-// The packed rows never pass through shared memory (half a byte in and out of it per value, of the 128 bytes a clock that the tensor
-// core's operands take too).  Tiles flow through the pieces of a CTA without a pause: the expansion warps run ahead of the
-// piece that the softmax warps are at.  There are two buffers of weights, so that a tile's softmax only waits for O of the tile before
-// the last one, unless it has to raise a maximum.
+//   expansion  8 warps: 32 values (16 bytes of codes) at a time to e4m3, into the operands' swizzled images
+//   + a warp each for page look-ups and exponents, for bulk copies of codes (STAGED), for the products and TMEM
+// Tiles flow through the pieces of a CTA without a pause: look-ups, copies and expansion run ahead of the piece that the softmax
+// warps are at.  There are two buffers of S and of weights; of the next S and the next O the product warp issues whichever can go first, so
+// that a tile's softmax only waits for O of the tile before the last one, unless it has to raise a maximum.
+// Codes: where two tiles of them fit into shared memory beside the expanded tiles (all shapes but MLA 512 + 64) they come by bulk copies, one for
+// each page and part; else the expansion warps load them to registers a tile ahead, behind the fence that ends a tile (in front of it the
+// fence waits for them).  GQA, 64 x 5056 rows of 8 KV heads: 131 us by copies, 145 by registers.
 // Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
+// What bounds it: not HBM (64 x 5056 rows, GQA 32 heads on 8: 348 MB in 125 us, 2.8 TB/s; MLA 16 heads: 97 MB in 56 us) but the chain of a tile -
+// expansion (seven instructions at half rate for eight values, 2000 warp instructions a tile for MLA 512 + 64, and 72 KB written through the port of
+// shared memory that feeds the products), S, softmax, weights, O, each handed on at 300 to 400 clocks - about 3000 clocks a tile and CTA for
+// GQA (two CTAs an SM), 3800 for MLA with 16 rows, 4800 with 32, and 22 us of launch, ranges, queries and merging.
 #include <cstring>
 
 #include "attn_paged4.cuh"
@@ -106,8 +112,7 @@ template <bool MLA_, int DS_, int DP_, int NH_, int GROUPS_, int ROWS_>
 struct Paged4Plan {
   static constexpr bool MLA = MLA_;
   static constexpr int DS = DS_, DP = DP_, NH = NH_, GROUPS = GROUPS_, ROWS = ROWS_;        // GROUPS * ROWS of the NH rows exist
-  static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product
-  static constexpr int NK = KSEM + 1;                        // + the pos chunk (64 or 128 columns)
+  static constexpr int KSEM = MLA ? DS / 128 : 0;            // latent chunks of the key product; then the pos chunk (64 or 128 columns)
   static constexpr int NV = DS >= 128 ? DS / 128 : 1, VW = DS >= 128 ? 128 : DS;
   static constexpr int K_BYTES = 128 * (KSEM * 128 + DP), V_BYTES = MLA ? 0 : 16384, TILE = K_BYTES + V_BYTES;        // expanded
   static constexpr int Q_BYTES = 2 * NH * (KSEM * 128 + DP);
@@ -121,8 +126,8 @@ struct Paged4Plan {
   static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_LOAD = W_LOOK + (STAGED ? 1 : 0);
   static constexpr int THREADS = 32 * (W_LOAD + 1);
   static constexpr int STAGE = STAGED ? 128 * (DS + DP) / 2 : 0, ST_POS = 128 * DS / 2;      // codes of a tile: latents or V, keys
-  // 32 values at a time: a thread's share of a tile, latents (V) and keys; tiles of them that are on their way to its registers
-  static constexpr int U_SEM = DS * 128 / 32 / (32 * EW), U_POS = DP * 128 / 32 / (32 * EW), UNITS = U_SEM + U_POS;
+  // 32 values at a time: a thread's share of a tile, latents (V) and keys
+  static constexpr int U_SEM = DS * 128 / 32 / (32 * EW), U_POS = DP * 128 / 32 / (32 * EW);
   // per tile: exponents of values and of keys, where its rows are, STAGED: shifts
   static constexpr int FACTS = 4, F_GROUP = 256, F_SPAN = 288, F_SHS = 304, F_SHP = F_SHS + (STAGED ? 2 * DS : 0), FACT = F_SHP + (STAGED ? 2 * DP : 0);
   // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers and scalars first, then the table.
@@ -168,7 +173,7 @@ __device__ __forceinline__ void bulk_copy(uint32_t smem_dst, const void* src, ui
 }
 template <class PL>
 __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(const __grid_constant__ Paged4Params a) {
-  constexpr int NH = PL::NH, NK = PL::NK, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
+  constexpr int NH = PL::NH, NV = PL::NV, DS = PL::DS, DP = PL::DP, ROWS = PL::ROWS;
   constexpr int W_EXP = PL::W_EXP, W_MMA = PL::W_MMA, W_LOOK = PL::W_LOOK, W_LOAD = PL::W_LOAD;
   const Paged8Params& p = a.b;
   extern __shared__ __align__(1024) unsigned char smem_p4[];
@@ -821,9 +826,14 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head, else blocks of 32.  MLA 512 + 64
-// with more than 64 rows: blocks of 128 on CTA pairs
-// (64 x 5056 rows: 128 query rows 128 us, in blocks of 32 on single CTAs 232; 64 query rows 126 and 123).
+// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head (16 rows of GQA, 64 x 5056: 188 us, with
+// room for 32: 213; MLA 512 + 64: 55 / 70), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
+// single CTAs against pairs:
+//                 64 x 5056 rows   20 x up to 5056   1 x 2528   12 x up to 9001   100 x 5056   4 x 60000
+//   40 rows           122 / 121 us      42 / 55        22 / 27       45 / 57       182 / 191     96 / 105
+//   64 rows           123 / 124         43 / 56        22 / 27       45 / 57       188 / 203     96 / 106
+//   66 rows           176 / 124         54 / 56        22 / 27       56 / 57       256 / 202    127 / 106
+//   128 rows          233 / 127         66 / 60        23 / 27       67 / 58       355 / 217    161 / 106
 static int paged4_rows_per_tile(const lca_params* p, int q_len) {
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
   if (p->d_sem == 512 && rows > 64) return 128;
@@ -848,6 +858,8 @@ template <bool MLA, int DS, int DP>
 static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
   const long long rows = (long long)P.b.q_len * P.b.rep;
   if constexpr (DS == 512) if (nh == 128) return attn_paged4_pair_launch(P, stream);
+  // Groups of softmax warps and rows a thread: what exists is computed, no more (GQA 128, 64 x 5056 rows: 4 rows 125 us, as 8 rows 142, as 16
+  // 181; 8 rows 144, as 16 184; GQA 64, 4 rows: 99, 116, 148).
   if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
   if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
   if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);

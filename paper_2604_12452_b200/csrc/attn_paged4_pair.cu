@@ -9,9 +9,16 @@
 // has those columns.  So they go there as they are by bulk copies of 8 KB from shared memory to shared memory, two within the CTA and two
 // to the other one, on the reader's barrier.
 //   softmax    8 warps: thread = row and a quarter of the keys (TMEM lane = row and half of them)
-//   expansion  8 warps: packed rows from HBM to registers one tile ahead, to e4m3 in the operand's image; then signals on
-//   warp 16 products (even CTA) / forwarding of the odd CTA's signals, warp 17 page table and exponents, warp 18 copies, warp 19 their end
-// An expanded tile's buffer is free once its product and the copies from it, at both ends, are done.
+//   expansion  8 warps: packed rows from HBM to registers one tile ahead, to e4m3 in the operand's image
+//   a warp each for products (even CTA; odd CTA: forwarding of its weights and queries), page table and exponents, copies, forwarding of
+//   expanded keys and copied values
+// An expanded tile's buffer is free once its product and the copies from it, at both ends, are done.  Signals from one CTA to the
+// other go through one thread, as in attn_paged8_pair.cu.
+// 64 x 5056 rows, 128 heads: 126 us (blocks of 32 rows on single CTAs: 232; the 8-bit cache, which expands nothing: 92).  A tile takes 5700
+// clocks: S 2000 and O 1100 (36 x 32 + 16 x 64 if nothing else used the port of shared memory), between them the softmax's
+// chain of 4400, which waits for neither.  Its instructions once did not fit the instruction cache (39 % of the stalls, products issued by
+// unrolled code, keys and values expanded by warps of their own).  Values expanded a second time in place of the copies: 154 us;
+// sixteen softmax warps with half the keys each: 131; maxima raised by a bound of 2^11 in place of 2^12, by all warps: 128.
 #include <cstring>
 
 #include "attn_paged4.cuh"

@@ -636,6 +636,7 @@ int lca_rope(const lca_rope_args* a, void* stream) {
   const uintptr_t elem = a->dtype == LCA_DTYPE_BF16 ? 1 : 3;
   for (const void* x : {a->q, (const void*)a->q_out, a->k, (const void*)a->k_out})
     if (reinterpret_cast<uintptr_t>(x) & elem) return LCA_ERR_MISALIGNED;
+  if ((reinterpret_cast<uintptr_t>(a->positions) & 3u) || (reinterpret_cast<uintptr_t>(a->freqs) & 7u)) return LCA_ERR_MISALIGNED;
   return rope_launch(a, (cudaStream_t)stream);
 }
 
@@ -665,11 +666,15 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
 int lca_verify_drafts(const lca_verify_args* a, void* stream) {
   if (!a || (a->dtype != LCA_DTYPE_BF16 && a->dtype != LCA_DTYPE_FP32)) return LCA_ERR_INVALID_ARG;
   if (a->batch <= 0 || a->n_drafts < 0 || a->n_drafts >= 0x7fffffff || a->vocab <= 0) return LCA_ERR_INVALID_ARG;
+  if (a->vocab > 0x7fffffff - 4096) return LCA_ERR_UNSUPPORTED_SHAPE;      // a token behind the row is still an int
   if (!a->target_probs || !a->u_sample || !a->accepted || !a->tokens_out) return LCA_ERR_INVALID_ARG;
   if (a->n_drafts > 0 && (!a->draft_tokens || !a->u_accept)) return LCA_ERR_INVALID_ARG;
   if ((a->n_tok != nullptr) != (a->n_tok_out != nullptr)) return LCA_ERR_INVALID_ARG;
   const uintptr_t elem = a->dtype == LCA_DTYPE_BF16 ? 1 : 3;
   if ((reinterpret_cast<uintptr_t>(a->target_probs) | reinterpret_cast<uintptr_t>(a->draft_probs)) & elem) return LCA_ERR_MISALIGNED;
+  for (const void* x : {(const void*)a->draft_tokens, (const void*)a->n_draft, (const void*)a->u_accept, (const void*)a->u_sample, (const void*)a->n_tok,
+                        (const void*)a->accepted, (const void*)a->tokens_out, (const void*)a->n_tok_out})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return LCA_ERR_MISALIGNED;
   return verify_launch(a, (cudaStream_t)stream);
 }
 

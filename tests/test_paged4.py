@@ -88,6 +88,7 @@ def test_rope_refusals(B):
                dict(head_dim=16384, rot_dim=16384)):
         assert call(**kw) == -1, kw
     assert call(q=17) == -3 and call(k_out=17) == -3 and call(dtype=1, q_out=18) == -3
+    assert call(positions=18) == -3 and call(freqs=20) == -3
     assert call(n_tokens=0, positions=None) == 0
     assert B.lca_launch_count() == before
     x = torch.zeros((3, 2, 64), dtype=torch.bfloat16)
@@ -133,6 +134,9 @@ def test_verify_refusals(B):
                dict(u_sample=None), dict(accepted=None), dict(tokens_out=None), dict(n_tok=None), dict(n_tok_out=None)):
         assert call(**kw) == -1, kw
     assert call(target_probs=18) == -3 and call(draft_probs=18) == -3 and call(dtype=0, draft_probs=17) == -3
+    for name in ("draft_tokens", "n_draft", "u_accept", "u_sample", "n_tok", "accepted", "tokens_out", "n_tok_out"):
+        assert call(**{name: 18}) == -3, name
+    assert call(vocab=0x7fffffff) == -2 and call(vocab=0x7fffffff - 4095) == -2
     assert B.lca_launch_count() == before
     with pytest.raises(ValueError):
         B.verify_drafts(torch.zeros((2, 4, 100)), None, torch.zeros((2, 3), dtype=torch.int32), torch.zeros((2, 3)), torch.zeros(2))

@@ -178,7 +178,8 @@ def build(shape, kv, page, states, g, seed, spare=3):
     return pool, table
 
 
-def check_attend(B, shape, heads, kv, page, states, g, q_len, seed=0, bias=0.0, reps=True, impl=0, edit=None, q_gain=1.0, softmax_scale=None):
+def check_attend(B, shape, heads, kv, page, states, g, q_len, seed=0, bias=0.0, reps=True, impl=0, edit=None, q_gain=1.0, softmax_scale=None,
+                 weight=2.0 ** -9, floor=2.0 ** -18):
     variant, d_sem, d_pos = SHAPES[shape]
     pool, table = build(shape, kv, page, states, g, seed)
     if edit:
@@ -200,11 +201,11 @@ def check_attend(B, shape, heads, kv, page, states, g, q_len, seed=0, bias=0.0, 
         B.lca_set_attention_impl(old)
     want, want_lse, absv, big = R.attend(None if q_sem is None else q_sem.double().numpy(), q_pos.double().numpy(), pool, table,
                                          [s[0] for s in states] if reps else [0] * nb, [s[1] for s in states], g, scale, bias)
-    compare(out, lse, want, want_lse, absv, big, n=max(t for _, t in states))
+    compare(out, lse, want, want_lse, absv, big, n=max(t for _, t in states), weight=weight, floor=floor)
     return out, lse, want
 
 
-def compare(out, lse, want, want_lse, absv, big, n):
+def compare(out, lse, want, want_lse, absv, big, n, weight=2.0 ** -9, floor=2.0 ** -18):
     """Logit error e: a query element is off by 2^-17 of its row's largest, so the product sum by 2^-17 max|q| sum|k| (`big`, with
     the softmax scale); fp32 sums of up to 2 * 576 products (2^-24 each, worst order) add 2^-13 of the same; exp2 / log2 and
     the scale products 2^-20 of the logits, which `big` bounds as well.  The cached values enter exactly.  A weight is then off
@@ -217,7 +218,7 @@ def compare(out, lse, want, want_lse, absv, big, n):
     assert np.array_equal(np.isneginf(gl), empty) and np.all(got[empty] == 0)
     dl = np.abs(gl[~empty] - want_lse[~empty])
     assert np.all(dl <= e[~empty] + 1e-6 * np.abs(want_lse[~empty]) + 1e-6), dl.max()
-    tol = absv * (2.0 ** -9 + 4 * e[..., None]) + 2.0 ** -8 * np.abs(want) + 2.0 ** -18 * (1 + n / 64) * absv.max(initial=0) + 1e-30
+    tol = absv * (weight + 4 * e[..., None]) + 2.0 ** -8 * np.abs(want) + floor * (1 + n / 64) * absv.max(initial=0) + 1e-30
     bad = np.abs(got - want) > tol
     assert not bad.any(), (int(bad.sum()), float(np.abs(got - want).max()), np.argwhere(bad)[:4])
 
