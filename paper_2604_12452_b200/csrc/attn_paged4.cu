@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       scales_of(g1, s1);
       Tile t2;
       look(t2);
-      ok = wait_suspended(FEMPTY(f), phase ^ 1, abort_flag);
+      ok = mbar_wait(FEMPTY(f), phase ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
       unsigned char* fact = s_fact + f * PL::FACT;
@@ -330,8 +330,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     const int per = p.page >> 4;                             // groups of 16 rows to a request
 #pragma unroll 1
     for (int t = 0; t < n_tiles && ok; ++t) {
-      ok = wait_suspended(FFULL(f), fphase, abort_flag);
-      if (ok) ok = wait_suspended(GEMPTY(stage), phase ^ 1, abort_flag);
+      ok = mbar_wait(FFULL(f), fphase, abort_flag);
+      if (ok) ok = mbar_wait(GEMPTY(stage), phase ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
       // lane: request + 8 * part
@@ -363,10 +363,12 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     bool ok = !*abort_flag;
     const uint32_t sixteen = *reinterpret_cast<const volatile uint32_t*>(misc + 416);
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      if (ok && !wait_suspended(bar, ph, abort_flag)) { fail(code); ok = false; }
+      if (ok && !mbar_wait(bar, ph, abort_flag)) { fail(code); ok = false; }
       ok = __all_sync(0xffffffffu, ok);
       return ok;
     };
+    // STAGED: goes on after a failure too (nothing that it would read from then on is an address)
+    auto hold = [&](uint32_t bar, uint32_t ph, int code) { if (!mbar_wait(bar, ph, abort_flag)) fail(code); };
     auto signal = [&](uint32_t bar) {
       __syncwarp();
       if (lane == 0) mbar_arrive(bar);
@@ -459,7 +461,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       for (int t = 0; t < n_tiles && ok; ++t) {
         const bool any = t + 1 < n_tiles;
         const uint32_t tile = buf * PL::TILE;
-        if (use > 0 && !wait(VEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
+        if (!wait(VEMPTY(buf), (use & 1) ^ 1, ERR_WAIT_O_DONE)) break;
         put(CP(), pos, pos_u, tile + pos_to, POS_APART);
 #pragma unroll
         for (int c = 0; c < NV; ++c) put(CS(), sem + BATCH * c, sem_u, tile + sem_to + c * 16384, SEM_APART);
@@ -480,7 +482,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 #pragma unroll 1
       for (int t = 0; t < n_tiles; ++t) {
         const uint32_t tile = buf * PL::TILE;
-        if (!wait(FFULL(ff), fphase, ERR_WAIT_KV_FULL) || !wait(GFULL(stage), phase, ERR_WAIT_KV_FULL)) break;
+        hold(GFULL(stage), phase, ERR_WAIT_KV_FULL);         // (and so the facts are there: the loading warp has waited for them)
         const unsigned char* fact = s_fact + ff * PL::FACT;
         const unsigned char* st = base_ptr + PL::OFF_STAGE + stage * PL::STAGE;
 #pragma unroll
@@ -497,12 +499,12 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         if (lane == 0) { mbar_arrive(GEMPTY(stage)); mbar_arrive(FEMPTY(ff)); }
         if (++ff == PL::FACTS) { ff = 0; fphase ^= 1; }
         if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
-        if (use > 0 && !wait(PL::MLA ? VEMPTY(buf) : KEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
+        hold(PL::MLA ? VEMPTY(buf) : KEMPTY(buf), (use & 1) ^ 1, ERR_WAIT_O_DONE);
         put(CP(), pos, pos_u, tile + pos_to, POS_APART);
         if constexpr (!PL::MLA) {
           fence_proxy_async_smem();
           signal(KFULL(buf));
-          if (use > 0 && !wait(VEMPTY(buf), (use - 1) & 1, ERR_WAIT_O_DONE)) break;
+          hold(VEMPTY(buf), (use & 1) ^ 1, ERR_WAIT_O_DONE);
         }
         put(CS(), sem, sem_u, tile + sem_to, SEM_APART);
         fence_proxy_async_smem();
@@ -520,7 +522,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     struct Ring { uint32_t buf, phase; __device__ __forceinline__ void next() { if (++buf == PL::BUFS) { buf = 0; phase ^= 1; } } };
     Ring sb = {0, 0}, ob = {0, 0};                           // expanded tiles whose S and O come next
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      ok = ok && wait_suspended(bar, ph, abort_flag);
+      ok = ok && mbar_wait(bar, ph, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) fail(code);
       return ok;
@@ -569,13 +571,14 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       uint32_t js = 0, jo = 0;
       const uint32_t n = (uint32_t)w.n;
       long long since = clock64();
+      uint32_t tries = 0;
 #pragma unroll 1
       while (jo < n && ok) {
         bool idle = true;
         if (js < n && js < jo + 2 && __all_sync(0xffffffffu, phase_done(KFULL(sb.buf), sb.phase))) { issue_s(g + js); ++js; idle = false; }
         if (jo < js && ok && __all_sync(0xffffffffu, phase_done(PFULL((g + jo) & 1), ((g + jo) >> 1) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
-        if (!idle) since = clock64();
-        else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
+        if (!idle) { since = clock64(); tries = 0; }
+        else if ((++tries & 63u) == 0 && (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES)) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
         ok = __all_sync(0xffffffffu, ok);
       }
       g += n;
@@ -646,7 +649,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x = row0 + t;
         const uint32_t buf = g & 1;
-        ok = wait_suspended(FFULL(g % PL::FACTS), (g / PL::FACTS) & 1, abort_flag);
+        ok = mbar_wait(FFULL(g % PL::FACTS), (g / PL::FACTS) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_KV_FULL);
         __syncwarp();
         const unsigned char* fact = s_fact + (g % PL::FACTS) * PL::FACT;
@@ -661,7 +664,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         const float offset = weight_offset(x);
         const bool limited = row0 + 127 >= sp.n_tok - p.q_len + 1;      // some query may not see some row of this tile
 
-        ok = wait_suspended(SFULL(buf), (g >> 1) & 1, abort_flag);
+        ok = mbar_wait(SFULL(buf), (g >> 1) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_S_FULL);
         __syncwarp();
         tc_fence_after();
@@ -714,11 +717,11 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
           for (int i = 0; i < ROWS; ++i) { z[i] -= s_d[hb + i]; l[i] *= s_f[hb + i]; }
         }
         if (g > 1) {                                         // the weights of the tile before the last one have been read
-          ok = wait_suspended(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
+          ok = mbar_wait(PVDONE(buf), ((g >> 1) - 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
         }
         if (raise && j > 0) {                                // O is complete up to the last tile
-          ok = wait_suspended(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
+          ok = mbar_wait(PVDONE(buf ^ 1), ((g - 1) >> 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
           __syncwarp();
           tc_fence_after();
@@ -788,7 +791,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       group_sync(grp);
       more = w.next(p);
       if (more) load_q(w, seg + 1);
-      ok = wait_suspended(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
+      ok = mbar_wait(PVDONE((g - 1) & 1), ((g - 1) >> 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
       tc_fence_after();

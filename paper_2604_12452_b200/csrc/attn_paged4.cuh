@@ -28,23 +28,6 @@ __device__ __forceinline__ uint4 load_stream(const void* p) {
   return v;
 }
 
-// A bounded wait that leaves its issue slots to the others: the hardware is told to suspend the thread for up to 2 us at a time.
-// (Every warp of this kernel waits for most of a tile; polling as fast as possible took a quarter of all issue slots.)
-__device__ __forceinline__ bool wait_suspended(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  auto poll = [&]() {
-    uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                 : "=r"(done) : "r"(bar), "r"(parity), "r"(2000u) : "memory");
-    return done != 0;
-  };
-  if (poll()) return true;
-  const long long t0 = clock64();
-  while (true) {
-    if (poll()) return true;
-    if (*abort_flag || clock64() - t0 > WAIT_TIMEOUT_CYCLES) return false;
-  }
-}
-
 int attn_paged4_pair_launch(Paged4Params& P, cudaStream_t stream);      // MLA shape, blocks of 128 rows on CTA pairs
 int attn_paged4_pair_take_status();
 

@@ -176,7 +176,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
         least = min(least, __shfl_xor_sync(0xffffffffu, least, o));
       }
       const bool all = (__ballot_sync(0xffffffffu, g0 != ~0u) & 0xffu) == 0xffu && (t0.lo >= 128 || (t0.mid <= 0 && t0.hi >= 128));
-      ok = wait_suspended(FEMPTY(f), phase ^ 1, abort_flag);
+      ok = mbar_wait(FEMPTY(f), phase ^ 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok) { if (lane == 0) fail(ERR_WAIT_KV_EMPTY); break; }
       unsigned char* fact = s_fact + f * FACT;
@@ -200,7 +200,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     const uint32_t sixteen = *s_sixteen;
     bool ok = !*abort_flag;
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      if (ok && !wait_suspended(bar, ph, abort_flag)) { fail(code); ok = false; }
+      if (ok && !mbar_wait(bar, ph, abort_flag)) { fail(code); ok = false; }
       ok = __all_sync(0xffffffffu, ok);
       return ok;
     };
@@ -264,9 +264,9 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
 #pragma unroll 1
       for (uint32_t t = 0; t < n_tiles; ++t) {
         const uint32_t buf = t & 1;
-        if (!wait_suspended(KLOCAL(buf), (t >> 1) & 1, abort_flag)) { fail(ERR_WAIT_KV_FULL); break; }
+        if (!mbar_wait(KLOCAL(buf), (t >> 1) & 1, abort_flag)) { fail(ERR_WAIT_KV_FULL); break; }
         // (both CTAs' values of the tile before the last one have been read: one signal to both)
-        if (t > 1 && !wait_suspended(VEMPTY(buf), ((t >> 1) - 1) & 1, abort_flag)) { fail(ERR_WAIT_O_DONE); break; }
+        if (t > 1 && !mbar_wait(VEMPTY(buf), ((t >> 1) - 1) & 1, abort_flag)) { fail(ERR_WAIT_O_DONE); break; }
         mbar_expect_tx(VFULL(buf), V_BUF);                   // two copies of this CTA and two of the other one
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i) {                   // the other CTA's columns first
@@ -281,6 +281,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     if (lane == 0 && !*abort_flag) {
       uint32_t k = 0, v = 0;
       long long since = clock64();
+      uint32_t tries = 0;
 #pragma unroll 1
       while (v < n_tiles) {
         bool idle = true;
@@ -292,8 +293,8 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
           ++v;
           idle = false;
         }
-        if (!idle) since = clock64();
-        else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { fail(ERR_WAIT_KV_FULL); break; }
+        if (!idle) { since = clock64(); tries = 0; }
+        else if ((++tries & 63u) == 0 && (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES)) { fail(ERR_WAIT_KV_FULL); break; }
       }
     }
   } else if (warp == W_MMA && rank == 0) {
@@ -307,7 +308,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
     uint32_t g = 0, seg = 0;
     bool ok = !*abort_flag;
     auto wait = [&](uint32_t bar, uint32_t ph, int code) {
-      ok = ok && wait_suspended(bar, ph, abort_flag);
+      ok = ok && mbar_wait(bar, ph, abort_flag);
       ok = __all_sync(0xffffffffu, ok);
       if (!ok && lane == 0) fail(code);
       return ok;
@@ -354,6 +355,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       uint32_t js = 0, jo = 0, jv = 0;                       // jv: values that are there
       const uint32_t n = (uint32_t)w.n;
       long long since = clock64();
+      uint32_t tries = 0;
 #pragma unroll 1
       while (jo < n && ok) {
         bool idle = true;
@@ -363,8 +365,8 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
           if (__all_sync(0xffffffffu, phase_done(VFULL(t & 1), (t >> 1) & 1) && phase_done(VPEER(t & 1), (t >> 1) & 1))) ++jv;
         }
         if (jo < js && jo < jv && __all_sync(0xffffffffu, phase_done(PFULL, (g + jo) & 1))) { issue_o(g + jo, jo == 0); ++jo; idle = false; }
-        if (!idle) since = clock64();
-        else if (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
+        if (!idle) { since = clock64(); tries = 0; }
+        else if ((++tries & 63u) == 0 && (*abort_flag || clock64() - since > WAIT_TIMEOUT_CYCLES)) { if (lane == 0) fail(ERR_WAIT_P_FULL); ok = false; }
         ok = __all_sync(0xffffffffu, ok);
       }
       g += n;
@@ -376,11 +378,11 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       uint32_t g = 0, seg = 0;
       bool ok = true;
       while (ok && w.next(p)) {
-        if (!wait_suspended(QLOCAL, seg & 1, abort_flag)) { fail(ERR_WAIT_Q); break; }
+        if (!mbar_wait(QLOCAL, seg & 1, abort_flag)) { fail(ERR_WAIT_Q); break; }
         mbar_arrive_cluster_cta(q_bar);
         ++seg;
         for (int j = 0; j < w.n; ++j, ++g) {
-          if (!wait_suspended(PLOCAL, g & 1, abort_flag)) { fail(ERR_WAIT_P_FULL); ok = false; break; }
+          if (!mbar_wait(PLOCAL, g & 1, abort_flag)) { fail(ERR_WAIT_P_FULL); ok = false; break; }
           mbar_arrive_cluster_cta(p_bar);
         }
       }
@@ -442,7 +444,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       for (int j = 0; j < w.n; ++j, ++g) {
         const int row0 = w.t.row0(w.t0 + j), x0 = row0 + key0;
         const uint32_t fr = g % FACTS;
-        ok = wait_suspended(FFULL(fr), (g / FACTS) & 1, abort_flag);
+        ok = mbar_wait(FFULL(fr), (g / FACTS) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_KV_FULL);
         __syncwarp();
         const unsigned char* fact = s_fact + fr * FACT;
@@ -454,7 +456,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
         const bool tile_reps = row0 < sp.n_rep && p.bias_log2 != 0.f;
         const bool whole_tile = row0 + 128 <= min(sp.n_tok, lim_all) && (row0 >= sp.tok0 || row0 + 128 <= sp.n_rep);
         const bool special = !whole_tile || tile_reps || groups.x == ~0u || groups.y == ~0u;
-        ok = wait_suspended(SFULL(g & 1), (g >> 1) & 1, abort_flag);
+        ok = mbar_wait(SFULL(g & 1), (g >> 1) & 1, abort_flag);
         if (!ok) fail(ERR_WAIT_S_FULL);
         __syncwarp();
         tc_fence_after();
@@ -571,7 +573,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
         __syncwarp();
         if (lane == 0) mbar_arrive(FEMPTY(fr));
         if (j > 0) {                                         // O is complete up to the previous tile, its weights have been read
-          ok = wait_suspended(PVDONE, (g - 1) & 1, abort_flag);
+          ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
           if (!ok) fail(ERR_WAIT_O_DONE);
           __syncwarp();
           if (__any_sync(0xffffffffu, factor != 1.f)) {
@@ -610,7 +612,7 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       l = (s_red[rl] + s_red[64 + rl]) + (s_red[128 + rl] + s_red[192 + rl]);
       more = w.next(p);
       if (more) load_q(w);
-      ok = wait_suspended(PVDONE, (g - 1) & 1, abort_flag);
+      ok = mbar_wait(PVDONE, (g - 1) & 1, abort_flag);
       if (!ok) fail(ERR_WAIT_O_DONE);
       __syncwarp();
       tc_fence_after();
