@@ -240,9 +240,9 @@ __device__ __forceinline__ float lg2(float x) { float r; asm("lg2.approx.f32 %0,
 // and the loads of the pieces' outputs are two round trips, not one per piece (64 x 5056 rows, 128 heads: 128 us for the call
 // instead of 135).  Its CTAs are in place before the attention kernel ends and know by then what they have to merge: for
 // up to MERGE_B sequences they sum the tiles themselves, from counters that the attention kernel has waited for already.
-template <int DS, int NH>
+template <int DS, int NH, int VEC>
 __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_constant__ Paged8Params p) {
-  constexpr int VEC = DS >= 128 ? 4 : 2, SPLIT = NH * DS / (256 * VEC);
+  constexpr int SPLIT = NH * DS / (256 * VEC);
   __shared__ int s_sum[3][8], s_n;
   const int lane = threadIdx.x & 31;
   const long long unit = blockIdx.x / SPLIT;
@@ -303,22 +303,32 @@ __global__ void __launch_bounds__(256) paged8_combine_kernel(const __grid_consta
         const float* src = p.part + (size_t)(2 * (c0 + i0 + k) + (i0 + k == 0 ? first : 0)) * NH * DS + x;
         float v[VEC];
         if constexpr (VEC == 4) *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(src);
-        else *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
+        else if constexpr (VEC == 2) *reinterpret_cast<float2*>(v) = *reinterpret_cast<const float2*>(src);
+        else v[0] = *src;
 #pragma unroll
         for (int e = 0; e < VEC; ++e) o[e] = w == 0.f ? o[e] : fmaf(w * v[e], w, o[e]);        // without weight: may be 0 * NaN
       }
     }
   }
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
+  if constexpr (VEC == 1) p.out[row * DS + d] = __float2bfloat16_rn(o[0] * inv);
+  else {
+    uint32_t* dst = reinterpret_cast<uint32_t*>(p.out + row * DS + d);
 #pragma unroll
-  for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
+    for (int k = 0; k < VEC / 2; ++k) dst[k] = pack_bf16x2(o[2 * k] * inv, o[2 * k + 1] * inv);
+  }
   if (p.lse && d == 0) p.lse[row] = l == 0.f ? -INFINITY : (m + log2f(l) - paged8_t_bits(NH)) * 0.6931471805599453f;
 }
 
+// Where VEC outputs a thread would fill less than one CTA an SM, a thread takes one: more warps have their pieces' loads under way, and the
+// sums are the same.  The whole call over the 4-bit cache, 1 x 9000 / 1 x 30000 rows: MLA 128 heads 37 / 58 us with 4, 31 / 43 with 1;
+// 16 heads and 4 tokens 34 / 54 and 29 / 39; 64 x 5056 rows (many CTAs): 126 with 4, 136 with 2.
 template <int DS, int NH>
 int paged8_combine_launch(const Paged8Params& P, cudaStream_t stream) {
-  return launch_chained(paged8_combine_kernel<DS, NH>, (unsigned)((long long)P.B * P.Hkv * P.n_blk * (NH * DS / (DS >= 128 ? 1024 : 512))), 256, 0, stream, 1, P);
+  constexpr int VEC = DS >= 128 ? 4 : 2, FEW = 1;
+  const long long units = (long long)P.B * P.Hkv * P.n_blk, ctas = units * (NH * DS / (256 * VEC));
+  if (ctas <= 148) return launch_chained(paged8_combine_kernel<DS, NH, FEW>, (unsigned)(units * (NH * DS / (256 * FEW))), 256, 0, stream, 1, P);
+  return launch_chained(paged8_combine_kernel<DS, NH, VEC>, (unsigned)ctas, 256, 0, stream, 1, P);
 }
 
 int attn_paged8_pair_launch(Paged8Params& P, cudaStream_t stream);      // MLA shape, blocks of 128 rows on CTA pairs
