@@ -7,98 +7,286 @@ namespace lca {
 
 // ------------------------------------------------------------------------------------------------- write, read back
 // Rows do not depend on one another (the exponent is the row's own), so there are no runs and no order to keep: a lane takes eight
-// values (16 bytes in, 4 out), four lanes a block.  HBM-bound.
+// values (16 bytes in, 4 out), four lanes a block.  Before HBM the integer instructions bound a write (74 % of their peak with a
+// row at a time and idle lanes), so that a warp takes vectors as they lie in the input, whatever rows they belong to, and no lane is idle: MLA four rows
+// at a time, their rope keys in one step of 32 lanes; GQA eight vectors of one KV head each.
 struct Paged4Rows {
   bf16* sem; bf16* pos;                                      // [n_rows, Hkv, d]: in (write), out (read)
   const int32_t* slots;
   uint32_t* pages_sem; uint32_t* pages_pos; uint8_t* shift_sem; uint8_t* shift_pos; uint8_t* exp_sem; uint8_t* exp_pos;
   long long n_rows, n_slots;
   int Hkv, page_log2;
+  uint32_t by_Hkv;                                           // 2^32 / Hkv, rounded up: quotients of numbers below 2^16
 };
 // Row of the pool for slot s and KV head hk.
 __device__ __forceinline__ size_t pool_row(const Paged4Rows& a, int s, int hk) {
   return (((size_t)(s >> a.page_log2) * a.Hkv + hk) << a.page_log2) + (size_t)(s & ((1 << a.page_log2) - 1));
 }
-// Largest finite |x| of eight bf16 values as bf16 bits; nan: whether one of them is NaN.  Every lane of the warp calls it.
-__device__ __forceinline__ uint32_t top8(const uint4& v, bool& nan) {
-  const uint32_t m = __vmaxu2(__vmaxu2(v.x & 0x7fff7fffu, v.y & 0x7fff7fffu), __vmaxu2(v.z & 0x7fff7fffu, v.w & 0x7fff7fffu));
-  uint32_t top = max(m & 0xffffu, m >> 16);
-  nan = top > 0x7f80u;
-  if (__any_sync(0xffffffffu, top >= 0x7f80u)) {
-    const uint32_t u[4] = {v.x, v.y, v.z, v.w};
-    top = 0;
+// Largest |x| of eight bf16 values as bf16 bits: above 0x7f80 with a NaN among them.
+__device__ __forceinline__ uint32_t top8(const uint4& v) {
+  uint32_t m, n;
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(m) : "r"(v.x), "r"(v.y));
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %1, %2;" : "=r"(n) : "r"(v.z), "r"(v.w));
+  asm("max.NaN.xorsign.abs.bf16x2 %0, %0, %1;" : "+r"(m) : "r"(n));
+  return max(m & 0x7fffu, (m >> 16) & 0x7fffu);
+}
+// The same of the finite ones among them.
+__device__ __noinline__ uint32_t finite_top8(uint4 v) {
+  const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+  uint32_t top = 0;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
-      top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
-    }
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t lo = u[k] & 0x7fffu, hi = (u[k] >> 16) & 0x7fffu;
+    top = max(top, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
   }
   return top;
 }
+// Tops of N vectors a lane, over each block's four lanes; nan: bit q where a block of vector q has one.
+template <int N>
+__device__ __forceinline__ uint32_t block_tops(const uint4 (&v)[N], uint32_t (&top)[N]) {
+  uint32_t all = 0, nan = 0;
+#pragma unroll
+  for (int q = 0; q < N; ++q) { top[q] = top8(v[q]); all = max(all, top[q]); }
+  if (__any_sync(0xffffffffu, all >= 0x7f80u)) {             // infinities and NaN do not count
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      const unsigned b = __ballot_sync(0xffffffffu, top[q] > 0x7f80u);
+      nan |= (b >> (threadIdx.x & 28)) & 15u ? 1u << q : 0u;
+      if (top[q] >= 0x7f80u) top[q] = finite_top8(v[q]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < N; ++q) {
+    top[q] = max(top[q], __shfl_xor_sync(0xffffffffu, top[q], 1));
+    top[q] = max(top[q], __shfl_xor_sync(0xffffffffu, top[q], 2));
+  }
+  return nan;
+}
+// One vector of a row with exponent E: its codes, and the shift of its block with that of the next block above it.
+__device__ __forceinline__ uint32_t encode8(const uint4& v, uint32_t top, bool nan, int E, uint32_t& shifts) {
+  const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT);
+  const uint32_t s = nan ? (uint32_t)PAGED4_NAN_SHIFT : (uint32_t)shift;
+  shifts = s | __shfl_down_sync(0xffffffffu, s, 4) << 4;
+  return paged4_pack(v, exp2_int(shift - E));
+}
 
 static const int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
+// Up to here a warp takes one MLA row (128 + 64: two), for its fewer instructions; beyond, four, for their smaller number in all.  Written with one
+// row a warp and with four: 64 rows 1.8 / 2.6 us, 4800 rows 3.3 / 3.7, 9600 rows 5.1 / 4.7, 20000 rows 8.7 / 7.1; 323584 rows 132 / 83.
+static const long long FEW_ROWS = 4096;
 
-// MLA: a warp per row.  Units of eight values: lane and lane + 32 of the latent (512 wide; 128 wide: lanes 0..15), lanes 0..7 the key.
-template <int D_SEM>
+// MLA, ROWS rows: step q < S takes units 32 q + lane of their latents (US of a row), step S units lane % 8 of their keys.
+template <int D_SEM, int ROWS>
+struct MlaRows {
+  static constexpr int US = D_SEM / 8, S = ROWS * US / 32;
+  static __device__ __forceinline__ int row(int q, int lane) { return q == S ? lane >> 3 : US == 64 ? q / 2 : 2 * q + (lane >> 4); }
+  static __device__ __forceinline__ int unit(int q, int lane) { return q == S ? lane & 7 : US == 64 ? (q & 1) * 32 + lane : lane & 15; }
+};
+template <int D_SEM, int ROWS>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_write_mla_kernel(Paged4Rows a) {
-  constexpr int D_POS = 64, NS = D_SEM / 256 > 0 ? D_SEM / 256 : 1, US = D_SEM / 8;
+  using M = MlaRows<D_SEM, ROWS>;
+  constexpr int S = M::S;
   const int lane = threadIdx.x & 31;
-  const long long warps = (long long)gridDim.x * ROW_WARPS;
+  const long long warps = (long long)gridDim.x * ROW_WARPS, groups = (a.n_rows + ROWS - 1) / ROWS;
   chain_wait();
   chain_next();
-#pragma unroll 2
-  for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
-    const int slot = a.slots[i];
-    if (slot < 0 || slot >= a.n_slots) continue;
-    uint4 v[NS + 1];
+  for (long long g = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); g < groups; g += warps) {
+    const int left = (int)min(a.n_rows - ROWS * g, (long long)ROWS);
+    int slot = lane < left ? a.slots[ROWS * g + lane] : -1;  // lane r < ROWS: of row r
+    if (slot >= a.n_slots) slot = -1;
+    uint4 v[S + 1];
 #pragma unroll
-    for (int q = 0; q < NS; ++q)
-      v[q] = lane + 32 * q < US ? __ldcs(reinterpret_cast<const uint4*>(a.sem + (size_t)i * D_SEM) + lane + 32 * q) : make_uint4(0u, 0u, 0u, 0u);
-    v[NS] = lane < D_POS / 8 ? __ldcs(reinterpret_cast<const uint4*>(a.pos + (size_t)i * D_POS) + lane) : make_uint4(0u, 0u, 0u, 0u);
-    uint32_t top[NS + 1], all = 0;
-    unsigned nan = 0;
-#pragma unroll
-    for (int q = 0; q <= NS; ++q) {
-      bool n;
-      uint32_t t = top8(v[q], n);
-      t = max(t, __shfl_xor_sync(0xffffffffu, t, 1));
-      t = max(t, __shfl_xor_sync(0xffffffffu, t, 2));
-      const unsigned b = __ballot_sync(0xffffffffu, n);
-      nan |= ((b >> (lane & ~3)) & 15u) ? 1u << q : 0u;
-      top[q] = t; all = max(all, t);
+    for (int q = 0; q <= S; ++q) {
+      const uint4* src = q == S ? reinterpret_cast<const uint4*>(a.pos) + g * (8 * ROWS) + lane : reinterpret_cast<const uint4*>(a.sem) + g * (ROWS * M::US) + 32 * q + lane;
+      v[q] = M::row(q, lane) < left ? __ldcs(src) : make_uint4(0u, 0u, 0u, 0u);
     }
-    all = __reduce_max_sync(0xffffffffu, all);
-    const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
-    const size_t row = pool_row(a, slot, 0);
+    uint32_t top[S + 1];
+    const uint32_t nan = block_tops(v, top);
+    // exponents of the rows: E[r], and of the key's row in this lane
+    const uint32_t key = max(top[S], __shfl_xor_sync(0xffffffffu, top[S], 4));
+    int E[S], Ek;
+    if constexpr (M::US == 64) {
+      int e[ROWS];
 #pragma unroll
-    for (int q = 0; q <= NS; ++q) {
-      const int shift = min(E - paged4_block_exponent(top[q]), PAGED4_MAX_SHIFT), s = (nan >> q) & 1u ? PAGED4_NAN_SHIFT : shift;
-      const uint32_t w = paged4_pack(v[q], exp2_int(shift - E));
-      const int next = __shfl_down_sync(0xffffffffu, s, 4);
-      if (q < NS && lane + 32 * q < US) {
-        a.pages_sem[row * (D_SEM / 8) + lane + 32 * q] = w;
-        if ((lane & 7) == 0) a.shift_sem[row * (D_SEM / 64) + (lane + 32 * q) / 8] = (uint8_t)(s | next << 4);
+      for (int r = 0; r < ROWS; ++r) {
+        const uint32_t t = __reduce_max_sync(0xffffffffu, max(max(top[2 * r], top[2 * r + 1]), (lane >> 3) == r ? key : 0u));
+        e[r] = max(paged4_block_exponent(t), PAGED4_MIN_EXP);
+        E[2 * r] = E[2 * r + 1] = e[r];
       }
-      if (q == NS && lane < D_POS / 8) {
-        a.pages_pos[row * (D_POS / 8) + lane] = w;
-        if (lane == 0) a.shift_pos[row] = (uint8_t)(s | next << 4);
+      Ek = e[0];
+#pragma unroll
+      for (int r = 1; r < ROWS; ++r) Ek = (lane >> 3) == r ? e[r] : Ek;
+    } else {
+      uint32_t t[S];
+#pragma unroll
+      for (int q = 0; q < S; ++q) {
+        t[q] = max(top[q], __shfl_xor_sync(0xffffffffu, top[q], 4));
+        t[q] = max(t[q], __shfl_xor_sync(0xffffffffu, t[q], 8));
+        t[q] = max(t[q], __shfl_sync(0xffffffffu, key, 8 * M::row(q, lane)));
+        E[q] = max(paged4_block_exponent(t[q]), PAGED4_MIN_EXP);
+      }
+#pragma unroll
+      for (int q = 0; q < S; ++q) { const int e = __shfl_sync(0xffffffffu, E[q], (lane & 8) * 2); Ek = (lane >> 4) == q || q == 0 ? e : Ek; }
+    }
+#pragma unroll
+    for (int q = 0; q <= S; ++q) {
+      uint32_t shifts;
+      const int Eq = q < S ? E[q < S ? q : 0] : Ek, u = M::unit(q, lane);
+      const uint32_t w = encode8(v[q], top[q], (nan >> q) & 1u, Eq, shifts);
+      const int to = __shfl_sync(0xffffffffu, slot, M::row(q, lane));      // (-1 behind the last row)
+      if (to < 0) continue;                                  // (a slot is its row in the pool: there is one KV head)
+      if (q < S) {
+        a.pages_sem[(size_t)to * M::US + u] = w;
+        if ((lane & 7) == 0) a.shift_sem[(size_t)to * (D_SEM / 64) + u / 8] = (uint8_t)shifts;
+      } else {
+        a.pages_pos[(size_t)to * 8 + u] = w;
+        if ((lane & 7) == 0) { a.shift_pos[to] = (uint8_t)shifts; a.exp_sem[to] = (uint8_t)(Eq + PAGED4_EXP_BIAS); }
       }
     }
-    if (lane == 0) a.exp_sem[row] = (uint8_t)(E + PAGED4_EXP_BIAS);
   }
 }
 
-// GQA: a warp takes a row's keys or values, up to eight KV heads of them (blockIdx.y: the two parts, then groups of heads), D / 8 lanes
-// a vector and a KV head.  All its loads are under way before the first is used; heads lie a page's rows apart in the pool.
+// GQA: eight vectors of one row and KV head each, in the order of the input (blockIdx.y: keys or values), D / 8 lanes a vector.
 template <int D>
-struct GqaRow {
-  static constexpr int U = D / 8, HEADS = 32 / U, STEPS = 8 / HEADS;         // lanes of a vector; KV heads of a step; steps
+struct GqaRows {
+  static constexpr int U = D / 8, HEADS = 32 / U, STEPS = 8 / HEADS;         // lanes of a vector; vectors of a step; steps
+};
+// Where a warp stands in the input: KV head `rem` of row `row`.
+struct GqaWalk {
+  long long row, rows_on;
+  int rem, rem_on;
+  __device__ __forceinline__ GqaWalk(const Paged4Rows& a) {
+    const long long first = 8 * ((long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5)), on = 8ll * gridDim.x * ROW_WARPS;
+    row = first / a.Hkv; rem = (int)(first - row * a.Hkv);
+    rows_on = on / a.Hkv; rem_on = (int)(on - rows_on * a.Hkv);
+  }
+  __device__ __forceinline__ void next(int Hkv) {
+    row += rows_on; rem += rem_on;
+    if (rem >= Hkv) { rem -= Hkv; ++row; }
+  }
+  // row and head `ahead` vectors on
+  __device__ __forceinline__ long long at(const Paged4Rows& a, int ahead, int& hk) const {
+    const uint32_t j = (uint32_t)(rem + ahead), d = a.Hkv == 1 ? j : __umulhi(j, a.by_Hkv);
+    hk = (int)(j - d * (uint32_t)a.Hkv);
+    return row + d;
+  }
 };
 template <int D>
 __global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa_kernel(Paged4Rows a) {
-  using G = GqaRow<D>;
+  using G = GqaRows<D>;
   const bool pos = blockIdx.y & 1;
-  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U, left = a.Hkv - hk;
+  const int lane = threadIdx.x & 31, u = lane % G::U;
+  const uint4* src = reinterpret_cast<const uint4*>(pos ? a.pos : a.sem) + lane;
+  uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
+  uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
+  uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
+  chain_wait();
+  chain_next();
+  for (GqaWalk at(a); at.row < a.n_rows; at.next(a.Hkv)) {
+    const uint4* here = src + ((size_t)at.row * a.Hkv + at.rem) * G::U;
+    uint4 v[G::STEPS];
+    long long to[G::STEPS];                                  // row of the pool, or none
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      int hk;
+      const long long i = at.at(a, k * G::HEADS + lane / G::U, hk);
+      const bool in = i < a.n_rows;
+      v[k] = in ? __ldcs(here + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+      const int slot = in ? a.slots[i] : -1;
+      to[k] = slot >= 0 && slot < a.n_slots ? (long long)pool_row(a, slot, hk) : -1ll;
+    }
+    uint32_t top[G::STEPS];
+    const uint32_t nan = block_tops(v, top);
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      uint32_t all = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], 4)), s;
+      if (G::U == 16) all = max(all, __shfl_xor_sync(0xffffffffu, all, 8));
+      const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
+      const uint32_t w = encode8(v[k], top[k], (nan >> k) & 1u, E, s);
+      if (to[k] < 0) continue;
+      pages[to[k] * G::U] = w;
+      if (u % 8 == 0) shifts[to[k] * (D / 64)] = (uint8_t)s;
+      if (u == 0) exps[to[k]] = (uint8_t)(E + PAGED4_EXP_BIAS);
+    }
+  }
+}
+
+template <int D_SEM, int ROWS>
+__global__ void __launch_bounds__(ROW_THREADS) paged4_read_mla_kernel(Paged4Rows a) {
+  using M = MlaRows<D_SEM, ROWS>;
+  constexpr int S = M::S;
+  const int lane = threadIdx.x & 31;
+  const long long warps = (long long)gridDim.x * ROW_WARPS, groups = (a.n_rows + ROWS - 1) / ROWS;
+  chain_wait();
+  chain_next();
+  for (long long g = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); g < groups; g += warps) {
+    const int left = (int)min(a.n_rows - ROWS * g, (long long)ROWS);
+    int slot = lane < left ? a.slots[ROWS * g + lane] : -1;
+    if (slot >= a.n_slots) slot = -1;
+    uint32_t w[S + 1];
+    int s[S + 1], e[S + 1], from[S + 1];
+#pragma unroll
+    for (int q = 0; q <= S; ++q) {
+      const int u = M::unit(q, lane);
+      from[q] = __shfl_sync(0xffffffffu, slot, M::row(q, lane));
+      const size_t row = (size_t)max(from[q], 0);            // (of slot 0 where there is none: not written)
+      w[q] = __ldcs(q < S ? a.pages_sem + row * M::US + u : a.pages_pos + row * 8 + u);
+      s[q] = q < S ? a.shift_sem[row * (D_SEM / 64) + u / 8] : a.shift_pos[row];
+      e[q] = a.exp_sem[row];
+    }
+#pragma unroll
+    for (int q = 0; q <= S; ++q) {
+      if (from[q] < 0) continue;
+      uint4* dst = q == S ? reinterpret_cast<uint4*>(a.pos) + g * (8 * ROWS) + lane : reinterpret_cast<uint4*>(a.sem) + g * (ROWS * M::US) + 32 * q + lane;
+      __stcs(dst, paged4_unpack(w[q], paged4_scale(e[q], s[q] >> (M::unit(q, lane) & 4) & 15)));
+    }
+  }
+}
+
+template <int D>
+__global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa_kernel(Paged4Rows a) {
+  using G = GqaRows<D>;
+  const bool pos = blockIdx.y & 1;
+  const int lane = threadIdx.x & 31, u = lane % G::U;
+  uint4* dst = reinterpret_cast<uint4*>(pos ? a.pos : a.sem) + lane;
+  const uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
+  const uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
+  const uint8_t* exps = pos ? a.exp_pos : a.exp_sem;
+  chain_wait();
+  chain_next();
+  for (GqaWalk at(a); at.row < a.n_rows; at.next(a.Hkv)) {
+    uint4* here = dst + ((size_t)at.row * a.Hkv + at.rem) * G::U;
+    long long from[G::STEPS];
+    uint32_t w[G::STEPS];
+    int s[G::STEPS], e[G::STEPS];
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      int hk;
+      const long long i = at.at(a, k * G::HEADS + lane / G::U, hk);
+      const int slot = i < a.n_rows ? a.slots[i] : -1;
+      from[k] = slot >= 0 && slot < a.n_slots ? (long long)pool_row(a, slot, hk) : -1ll;
+    }
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k) {
+      const bool in = from[k] >= 0;
+      w[k] = in ? __ldcs(pages + from[k] * G::U) : 0u;
+      s[k] = in ? shifts[from[k] * (D / 64)] : 0;
+      e[k] = in ? exps[from[k]] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < G::STEPS; ++k)
+      if (from[k] >= 0) __stcs(here + k * 32, paged4_unpack(w[k], paged4_scale(e[k], s[k] >> (u & 4) & 15)));
+  }
+}
+
+// The same where Hkv is a multiple of eight: a warp takes eight KV heads of a row (blockIdx.y: the two parts, then groups of heads), one look-up
+// and one step through the pool for all (29000 rows of 8 KV heads of 128: written 34 us, one by one 41; read 26 and 30.  2 KV heads,
+// 100000 rows, a warp a row: 99 and 40; one by one 35 and 27).
+template <int D>
+__global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa8_kernel(Paged4Rows a) {
+  using G = GqaRows<D>;
+  const bool pos = blockIdx.y & 1;
+  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U;
   const uint4* src = reinterpret_cast<const uint4*>(pos ? a.pos : a.sem) + (size_t)(hk - lane / G::U) * G::U + lane;
   uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
   uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
@@ -113,69 +301,31 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_write_gqa_kernel(Paged4Row
     const uint4* row_src = src + (size_t)i * a.Hkv * G::U;
     uint4 v[G::STEPS];
 #pragma unroll
-    for (int k = 0; k < G::STEPS; ++k) v[k] = k * G::HEADS < left ? __ldcs(row_src + k * 32) : make_uint4(0u, 0u, 0u, 0u);
+    for (int k = 0; k < G::STEPS; ++k) v[k] = __ldcs(row_src + k * 32);
     const size_t row0 = pool_row(a, slot, hk);
     uint32_t* to = pages + row0 * G::U;
     uint8_t* to_shift = shifts + row0 * (D / 64);
     uint8_t* to_exp = exps + row0;
+    uint32_t top[G::STEPS];
+    const uint32_t nan = block_tops(v, top);
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k) {
-      bool n;
-      uint32_t top = top8(v[k], n);
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      uint32_t all = max(top, __shfl_xor_sync(0xffffffffu, top, 4));
+      uint32_t all = max(top[k], __shfl_xor_sync(0xffffffffu, top[k], 4)), s;
       if (G::U == 16) all = max(all, __shfl_xor_sync(0xffffffffu, all, 8));
       const int E = max(paged4_block_exponent(all), PAGED4_MIN_EXP);
-      const int shift = min(E - paged4_block_exponent(top), PAGED4_MAX_SHIFT);
-      const int s = (__ballot_sync(0xffffffffu, n) >> (lane & ~3)) & 15u ? PAGED4_NAN_SHIFT : shift;
-      const uint32_t w = paged4_pack(v[k], exp2_int(shift - E));
-      const int next = __shfl_down_sync(0xffffffffu, s, 4);
-      if (k * G::HEADS < left) {
-        *to = w;
-        if (u % 8 == 0) *to_shift = (uint8_t)(s | next << 4);
-        if (u == 0) *to_exp = (uint8_t)(E + PAGED4_EXP_BIAS);
-      }
+      *to = encode8(v[k], top[k], (nan >> k) & 1u, E, s);
+      if (u % 8 == 0) *to_shift = (uint8_t)s;
+      if (u == 0) *to_exp = (uint8_t)(E + PAGED4_EXP_BIAS);
       to += (size_t)apart * G::U; to_shift += (size_t)apart * (D / 64); to_exp += apart;
     }
   }
 }
 
-template <int D_SEM>
-__global__ void __launch_bounds__(ROW_THREADS) paged4_read_mla_kernel(Paged4Rows a) {
-  constexpr int D_POS = 64, NS = D_SEM / 256 > 0 ? D_SEM / 256 : 1, US = D_SEM / 8;
-  const int lane = threadIdx.x & 31;
-  const long long warps = (long long)gridDim.x * ROW_WARPS;
-  chain_wait();
-  chain_next();
-#pragma unroll 2
-  for (long long i = (long long)blockIdx.x * ROW_WARPS + (threadIdx.x >> 5); i < a.n_rows; i += warps) {
-    const int slot = a.slots[i];
-    if (slot < 0 || slot >= a.n_slots) continue;
-    const size_t row = pool_row(a, slot, 0);
-    uint32_t w[NS + 1];
-    int s[NS + 1];
-#pragma unroll
-    for (int q = 0; q < NS; ++q) {
-      const int u = lane + 32 * q;
-      w[q] = u < US ? __ldcs(a.pages_sem + row * US + u) : 0u;
-      s[q] = u < US ? a.shift_sem[row * (D_SEM / 64) + u / 8] >> (u & 4) & 15 : 0;
-    }
-    w[NS] = lane < D_POS / 8 ? __ldcs(a.pages_pos + row * (D_POS / 8) + lane) : 0u;
-    s[NS] = lane < D_POS / 8 ? a.shift_pos[row] >> (lane & 4) & 15 : 0;
-    const int e = a.exp_sem[row];
-#pragma unroll
-    for (int q = 0; q < NS; ++q)
-      if (lane + 32 * q < US) __stcs(reinterpret_cast<uint4*>(a.sem + (size_t)i * D_SEM) + lane + 32 * q, paged4_unpack(w[q], paged4_scale(e, s[q])));
-    if (lane < D_POS / 8) __stcs(reinterpret_cast<uint4*>(a.pos + (size_t)i * D_POS) + lane, paged4_unpack(w[NS], paged4_scale(e, s[NS])));
-  }
-}
-
 template <int D>
-__global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa_kernel(Paged4Rows a) {
-  using G = GqaRow<D>;
+__global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa8_kernel(Paged4Rows a) {
+  using G = GqaRows<D>;
   const bool pos = blockIdx.y & 1;
-  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U, left = a.Hkv - hk;
+  const int lane = threadIdx.x & 31, u = lane % G::U, hk = (int)(blockIdx.y >> 1) * 8 + lane / G::U;
   uint4* dst = reinterpret_cast<uint4*>(pos ? a.pos : a.sem) + (size_t)(hk - lane / G::U) * G::U + lane;
   const uint32_t* pages = (pos ? a.pages_pos : a.pages_sem) + u;
   const uint8_t* shifts = (pos ? a.shift_pos : a.shift_sem) + u / 8;
@@ -195,16 +345,15 @@ __global__ void __launch_bounds__(ROW_THREADS) paged4_read_gqa_kernel(Paged4Rows
     int s[G::STEPS], e[G::STEPS];
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k) {
-      const bool in = k * G::HEADS < left;
-      w[k] = in ? __ldcs(from) : 0u;
-      s[k] = in ? *from_shift : 0;
-      e[k] = in ? *from_exp : 0;
+      w[k] = __ldcs(from);
+      s[k] = *from_shift;
+      e[k] = *from_exp;
       from += (size_t)apart * G::U; from_shift += (size_t)apart * (D / 64); from_exp += apart;
     }
     uint4* row_dst = dst + (size_t)i * a.Hkv * G::U;
 #pragma unroll
     for (int k = 0; k < G::STEPS; ++k)
-      if (k * G::HEADS < left) __stcs(row_dst + k * 32, paged4_unpack(w[k], paged4_scale(e[k], s[k] >> (u & 4) & 15)));
+      __stcs(row_dst + k * 32, paged4_unpack(w[k], paged4_scale(e[k], s[k] >> (u & 4) & 15)));
   }
 }
 
@@ -213,21 +362,31 @@ int paged4_rows_launch(const lca_params* p, const lca_paged4* c, bool write, con
   const bool mla = p->variant == LCA_VARIANT_MLA;
   Paged4Rows a = {(bf16*)rows_sem, (bf16*)rows_pos, slot_map, (uint32_t*)c->pages_sem, (uint32_t*)c->pages_pos, c->shift_sem, c->shift_pos,
                   c->exp_sem, c->exp_pos, n_rows, (long long)c->n_pages * c->page_size, p->n_kv_heads,
-                  c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7};
-  const long long most = 148 * 8 * 8;                        // a few waves of all CTAs that are resident
+                  c->page_size == 16 ? 4 : c->page_size == 32 ? 5 : c->page_size == 64 ? 6 : 7,
+                  (uint32_t)(((1ull << 32) + p->n_kv_heads - 1) / p->n_kv_heads)};
+  if (p->n_kv_heads >= 1 << 15) return LCA_ERR_UNSUPPORTED_SHAPE;      // by_Hkv
+  // A few waves of all CTAs that are resident, a warp the least that it can take ...
+  const bool eight = p->n_kv_heads % 8 == 0, few = n_rows <= FEW_ROWS;
+  const long long most = 148 * 8 * 8;
+  const int mla_rows = few ? (p->d_sem == 512 ? 1 : 2) : 4;
+  const long long items = mla ? (n_rows + mla_rows - 1) / mla_rows : eight ? n_rows : (n_rows * p->n_kv_heads + 7) / 8;
+  const long long want = (items + ROW_WARPS - 1) / ROW_WARPS;
+  const dim3 grid((unsigned)(want < most ? want : most), mla ? 1 : eight ? (unsigned)(p->n_kv_heads / 4) : 2);
+  auto go = [&](auto kern) { return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a); };
   if (mla) {
-    const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS;
-    const dim3 grid((unsigned)(want < most ? want : most), 1);
-    auto kern = write ? (p->d_sem == 512 ? paged4_write_mla_kernel<512> : paged4_write_mla_kernel<128>)
-                      : (p->d_sem == 512 ? paged4_read_mla_kernel<512> : paged4_read_mla_kernel<128>);
-    return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a);
+    if (p->d_sem == 512) {
+      if (few) return write ? go(paged4_write_mla_kernel<512, 1>) : go(paged4_read_mla_kernel<512, 1>);
+      return write ? go(paged4_write_mla_kernel<512, 4>) : go(paged4_read_mla_kernel<512, 4>);
+    }
+    if (few) return write ? go(paged4_write_mla_kernel<128, 2>) : go(paged4_read_mla_kernel<128, 2>);
+    return write ? go(paged4_write_mla_kernel<128, 4>) : go(paged4_read_mla_kernel<128, 4>);
   }
-  const long long want = (n_rows + ROW_WARPS - 1) / ROW_WARPS, parts = 2 * ((p->n_kv_heads + 7) / 8);
-  if (parts > 65535) return LCA_ERR_UNSUPPORTED_SHAPE;
-  const dim3 grid((unsigned)(want < most ? want : most), (unsigned)parts);
-  auto kern = write ? (p->d_sem == 128 ? paged4_write_gqa_kernel<128> : paged4_write_gqa_kernel<64>)
-                    : (p->d_sem == 128 ? paged4_read_gqa_kernel<128> : paged4_read_gqa_kernel<64>);
-  return launch_chained(kern, grid, ROW_THREADS, 0, stream, 1, a);
+  if (eight) {
+    if (p->d_sem == 128) return write ? go(paged4_write_gqa8_kernel<128>) : go(paged4_read_gqa8_kernel<128>);
+    return write ? go(paged4_write_gqa8_kernel<64>) : go(paged4_read_gqa8_kernel<64>);
+  }
+  if (p->d_sem == 128) return write ? go(paged4_write_gqa_kernel<128>) : go(paged4_read_gqa_kernel<128>);
+  return write ? go(paged4_write_gqa_kernel<64>) : go(paged4_read_gqa_kernel<64>);
 }
 
 // ------------------------------------------------------------------------------------------------------------ update

@@ -66,12 +66,14 @@ def check_write(B, shape, kv, page, slots, rows_sem, rows_pos, pool):
     B.paged4_read(p, cache, i32(ask), sem, pos)
     for x, w in ((sem, want["sem"]), (pos, want["pos"])):
         x = x.double().cpu().numpy()
+        w = torch.from_numpy(w).float().bfloat16().double().numpy()            # 2^128: infinity
         for i, s in enumerate(ask):
             ref = w[s // page, :, s % page] if 0 <= s < w.shape[0] * page else np.full(x[i].shape, 7.0)
             assert np.array_equal(x[i], ref, equal_nan=True), (i, s)
 
 
-@pytest.mark.parametrize("shape,kv", [("mla512", 1), ("mla128", 1), ("gqa128", 3), ("gqa64", 2), ("gqa64", 1)])
+@pytest.mark.parametrize("shape,kv", [("mla512", 1), ("mla128", 1), ("gqa128", 3), ("gqa64", 2), ("gqa64", 1), ("gqa128", 8), ("gqa128", 16), ("gqa64", 8),
+                                      ("gqa64", 9), ("gqa128", 5)])
 @pytest.mark.parametrize("page", [16, 32, 64, 128])
 def test_write_and_read_rows_in_any_order(B, shape, kv, page):
     variant, d_sem, d_pos = SHAPES[shape]
@@ -85,7 +87,7 @@ def test_write_and_read_rows_in_any_order(B, shape, kv, page):
     check_write(B, shape, kv, page, slots, sem, pos, new_pool(shape, n_pages, page, 3, kv))
 
 
-@pytest.mark.parametrize("shape,kv", [("mla512", 1), ("gqa128", 2), ("gqa64", 1)])
+@pytest.mark.parametrize("shape,kv", [("mla512", 1), ("gqa128", 2), ("gqa64", 1), ("mla128", 1), ("gqa128", 8), ("gqa64", 8), ("gqa128", 3)])
 def test_write_extreme_values(B, shape, kv):
     variant, d_sem, d_pos = SHAPES[shape]
     r = np.random.RandomState(5)
@@ -110,6 +112,24 @@ def test_write_extreme_values(B, shape, kv):
     sem[33], pos[33] = float("inf"), float("nan")
     sem[34], pos[34, :, :32] = float("nan"), float("-inf")
     check_write(B, shape, kv, page, list(range(2, 2 + T)), sem.bfloat16(), pos.bfloat16(), new_pool(shape, 4, page, 4, kv))
+
+
+@pytest.mark.parametrize("shape,n", [("mla512", 4097), ("mla512", 4106), ("mla128", 4099), ("mla128", 5000)])
+def test_write_and_read_more_rows_than_a_warp_has_for_itself(B, shape, n):
+    # several rows to a warp: neighbours of every kind side by side, rows without a slot among them, a last warp that is not full
+    _, d_sem, d_pos = SHAPES[shape]
+    r = np.random.RandomState(n)
+    page, n_pages = 64, n // 64 + 3
+    slots = r.permutation(n_pages * page)[:n]
+    slots[r.permutation(n)[:n // 9]] = -1
+    slots[[1, 6, n - 2]] = [n_pages * page, 2 ** 31 - 1, -(2 ** 31)]
+    sem, pos = (torch.from_numpy(r.randn(n, 1, d) * np.exp(3 * r.randn(n, 1, 1)) * np.exp(r.randn(d // 32).repeat(32) * 2)).bfloat16() for d in (d_sem, d_pos))
+    for x in (sem, pos):
+        for value in (float("inf"), float("-inf"), float("nan"), 0.0, 1e-40, 3e38):
+            x[torch.from_numpy(r.permutation(n)[:n // 20]), 0, r.randint(x.shape[-1])] = value
+        x[torch.from_numpy(r.permutation(n)[:n // 20])] = 0.0
+        x[torch.from_numpy(r.permutation(n)[:n // 50])] = float("nan")
+    check_write(B, shape, 1, page, [int(s) for s in slots], sem, pos, new_pool(shape, n_pages, page, 3, 1))
 
 
 def test_read_gives_what_the_bytes_say_for_every_byte(B):
