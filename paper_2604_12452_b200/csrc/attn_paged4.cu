@@ -132,13 +132,13 @@ struct Paged4Plan {
   static constexpr int FACTS = 4, F_GROUP = 256, F_SPAN = 288, F_SHS = 304, F_SHP = F_SHS + (STAGED ? 2 * DS : 0), FACT = F_SHP + (STAGED ? 2 * DP : 0);
   // words: qs, M, d, factor, lim [NH]; wmax / sums [4][NH]; output rows [2][NH].  Barriers and scalars first, then the table.
   static constexpr int MISC_BYTES = 512 + 128 + 4 * (5 * NH + 4 * NH + 2 * NH) + FACTS * FACT;
-  static constexpr int BUDGET = CTAS == 1 ? 227 * 1024 : 113 * 1024;
+  static constexpr int ROOM = CTAS == 1 ? 227 * 1024 : 113 * 1024;
   static constexpr int BUFS = CTAS == 1 && STAGED ? 3 : 2;   // expanded tiles
-  static constexpr int STAGES_FIT = STAGED ? (BUDGET - BUFS * TILE - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / (STAGED ? STAGE : 1) : 0;
+  static constexpr int STAGES_FIT = STAGED ? (ROOM - BUFS * TILE - Q_BYTES - 2 * P_BYTES - MISC_BYTES) / (STAGED ? STAGE : 1) : 0;
   static constexpr int STAGES = STAGES_FIT > 4 ? 4 : STAGES_FIT;
   static constexpr int OFF_Q = BUFS * TILE, OFF_P = OFF_Q + Q_BYTES, OFF_STAGE = OFF_P + 2 * P_BYTES, OFF_MISC = OFF_STAGE + STAGES * STAGE;
   static constexpr int SMEM = OFF_MISC + MISC_BYTES;
-  static_assert((!STAGED || STAGES >= 2) && SMEM <= BUDGET && OFF_MISC % 16 == 0 && OFF_Q % 1024 == 0 && FACT % 16 == 0, "one tile is expanded while another is used");
+  static_assert((!STAGED || STAGES >= 2) && SMEM <= ROOM && OFF_MISC % 16 == 0 && OFF_Q % 1024 == 0 && FACT % 16 == 0, "one tile is expanded while another is used");
   static_assert(THREADS <= 32 * 28, "72 registers a thread");
 };
 

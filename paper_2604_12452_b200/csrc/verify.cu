@@ -6,7 +6,8 @@
 // token would depend on the order.
 // Only what decides is read: two numbers for each draft, then one row of p and one of q.  A cluster takes a request, so that its CTAs
 // share the row; each sums its part warp by warp; the CTA whose part holds the crossing finds the warp, spreads that warp's few
-// hundred tokens over all its warps (from L2) and goes through the last few dozen.  HBM-bound for many requests, else the chain of four dependent trips to memory.
+// hundred tokens over all its warps (from L2) and goes through the last few dozen.  Bound by the chain of
+// four dependent trips to memory, for many requests by HBM and by conversions to 64 bits too (64 x 128000 fp32 tokens: 21 us, 3.1 TB/s).
 #include "lca_common.cuh"
 #include "tc_common.cuh"
 
@@ -212,9 +213,11 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
 int verify_launch(const lca_verify_args* v, cudaStream_t stream) {
   VerifyArgs a = {v->target_probs, v->draft_probs, v->draft_tokens, v->u_accept, v->u_sample, v->n_draft, v->n_tok, v->accepted, v->tokens_out,
                   v->n_tok_out, v->batch, v->n_drafts, v->vocab};
-  // CTAs of a request: as many as are resident at once, and not so many that a warp has less than four steps of 128 tokens
+  // CTAs of a request: as many as are resident at once, and not so many that a warp has nothing to read.  With 1 / 4 / 8 / 16: 1 request,
+  // 32001 tokens bf16 34 / 12 / 7.7 / 5.9 us; 8000 tokens 7.6 / 5.1 / 4.6 / 4.9; 64 requests, 128000 tokens 83 / 23 / 21 / 21; 256 requests,
+  // 32000 tokens 26 / 20 / 28 / 42.
   int c = 1;
-  while (c < VERIFY_MOST_CTAS && (long long)v->batch * 2 * c <= 4 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 512) c *= 2;
+  while (c < VERIFY_MOST_CTAS && (long long)v->batch * 2 * c <= 5 * 148 && (long long)v->vocab > (long long)c * VERIFY_WARPS * 128) c *= 2;
   if ((long long)v->batch * c > 0x7fffffffll) return LCA_ERR_UNSUPPORTED_SHAPE;
   const bool bf = v->dtype == LCA_DTYPE_BF16;
   auto kern = bf ? verify_kernel<bf16> : verify_kernel<float>;
