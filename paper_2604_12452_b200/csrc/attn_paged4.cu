@@ -10,7 +10,7 @@
 //
 // Transposed products, the key tile as the 128-row operand: S^T [128 keys x 2 NH] = K [Q_hi | Q_lo]^T, O^T [d x 2 NH] += V^T [T_hi | T_lo]^T.
 //   softmax    GROUPS groups of four warps, each for ROWS of the query rows: thread = key = TMEM lane; epilogue: thread = output column
-//   expansion  8 warps: 32 values (16 bytes of codes) at a time to e4m3, into the operands' swizzled images
+//   expansion  4 warps, or 8: 32 values (16 bytes of codes) at a time to e4m3, into the operands' swizzled images
 //   + a warp each for page look-ups and exponents, for bulk copies of codes (STAGED), for the products and TMEM
 // Tiles flow through the pieces of a CTA without a pause: look-ups, copies and expansion run ahead of the piece that the softmax
 // warps are at.  There are two buffers of S and of weights; of the next S and the next O the product warp issues whichever can go first, so
@@ -19,7 +19,7 @@
 // each page and part; else the expansion warps load them to registers a tile ahead, behind the fence that ends a tile (in front of it the
 // fence waits for them).  GQA, 64 x 5056 rows of 8 KV heads: 131 us by copies, 145 by registers.
 // Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
-// What bounds it: not HBM (64 x 5056 rows, GQA 32 heads on 8: 348 MB in 125 us, 2.8 TB/s; MLA 16 heads: 97 MB in 56 us) but the chain of a tile -
+// What bounds it: not HBM (64 x 5056 rows, GQA 32 heads on 8: 348 MB in 121 us, 2.9 TB/s; MLA 16 heads: 97 MB in 55 us) but the chain of a tile -
 // expansion (seven instructions at half rate for eight values, 2000 warp instructions a tile for MLA 512 + 64, and 72 KB written through the port of
 // shared memory that feeds the products), S, softmax, weights, O, each handed on at 300 to 400 clocks - about 3000 clocks a tile and CTA for
 // GQA (two CTAs an SM), 3800 for MLA with 16 rows, 4800 with 32, and 22 us of launch, ranges, queries and merging.
@@ -123,7 +123,9 @@ struct Paged4Plan {
   // Packed rows come by bulk copies into shared memory where there is room for it, else straight to the registers of the threads that
   // expand them.
   static constexpr bool STAGED = !(MLA && DS == 512);
-  static constexpr int EW = 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_LOAD = W_LOOK + (STAGED ? 1 : 0);
+  // Expansion warps.  More of them hide more latency, fewer leave more registers and issue slots to the others: with 4 and 8, 64 x 5056 rows,
+  // GQA 128 with 4 / 16 / 32 rows a KV head 121 / 157 / 206 and 121 / 174 / 208 us, GQA 64 90 and 101; MLA 512 + 64 with 16 rows 60 and 55.
+  static constexpr int EW = STAGED ? 4 : 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_LOAD = W_LOOK + (STAGED ? 1 : 0);
   static constexpr int THREADS = 32 * (W_LOAD + 1);
   static constexpr int STAGE = STAGED ? 128 * (DS + DP) / 2 : 0, ST_POS = 128 * DS / 2;      // codes of a tile: latents or V, keys
   // 32 values at a time: a thread's share of a tile, latents (V) and keys
@@ -374,10 +376,10 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       if (lane == 0) mbar_arrive(bar);
     };
     constexpr bool LATENT = PL::MLA && DS == 512;
-    constexpr int US = PL::VW / 32, UP = DP / 32, STEP = 32 * PL::EW;
+    constexpr int US = PL::VW / 32, UP = DP / 32, STEP = 32 * PL::EW, PER_CHUNK = US * 128 / STEP;
     // unit i of this thread: row and unit in the row, place in the expanded tile
-    // (512 latents: units 2 c and 2 c + 1 of chunk c), neighbouring threads neighbouring units
-    auto sem_row = [&](int i) { return (et + STEP * (LATENT ? i & 1 : i)) / US; };
+    // (512 latents: PER_CHUNK of each chunk), neighbouring threads neighbouring units
+    auto sem_row = [&](int i) { return (et + STEP * (LATENT ? i % PER_CHUNK : i)) / US; };
     const int sem_u = et % US, pos_u = et % UP;
     auto pos_row = [&](int i) { return (et + STEP * i) / UP; };
     const uint32_t sem_to = (PL::MLA ? 0 : PL::K_BYTES) + swz<PL::VW>(sem_row(0), 2 * sem_u);
@@ -427,10 +429,10 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         *reinterpret_cast<uint4*>(base_ptr + (dst ^ 16u) + i * step) = make_uint4(x2.x, x2.y, x3.x, x3.y);
       }
     };
-    constexpr int BATCH = LATENT ? 2 : PL::U_SEM;
+    constexpr int BATCH = LATENT ? PER_CHUNK : PL::U_SEM;
     using CP = std::integral_constant<int, PL::U_POS>;
     using CS = std::integral_constant<int, BATCH>;
-    auto load_sem = [&](Unit* x, const Facts& f, int i0) { load(CS(), x, i0, f, sem_row, a.sem, a.shift_sem, DS, sem_u + (LATENT ? 2 * i0 : 0)); };
+    auto load_sem = [&](Unit* x, const Facts& f, int i0) { load(CS(), x, i0, f, sem_row, a.sem, a.shift_sem, DS, sem_u + (LATENT ? US * (i0 / PER_CHUNK) : 0)); };
     auto load_pos = [&](Unit* x, const Facts& f) { load(CP(), x, 0, f, pos_row, a.pos, a.shift_pos, DP, pos_u); };
     uint32_t ff = 0, fphase = 0;
     auto facts = [&](Facts& f, bool any) {                   // of the next tile; its groups are read until `signal`
@@ -829,8 +831,8 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
-// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head (16 rows of GQA, 64 x 5056: 188 us, with
-// room for 32: 213; MLA 512 + 64: 55 / 70), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
+// Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head (16 rows of GQA, 64 x 5056: 157 us, with
+// room for 32: 206; MLA 512 + 64: 55 / 70), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
 // single CTAs against pairs:
 //                 64 x 5056 rows   20 x up to 5056   1 x 2528   12 x up to 9001   100 x 5056   4 x 60000
 //   40 rows           122 / 121 us      42 / 55        22 / 27       45 / 57       182 / 191     96 / 105
@@ -861,8 +863,8 @@ template <bool MLA, int DS, int DP>
 static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
   const long long rows = (long long)P.b.q_len * P.b.rep;
   if constexpr (DS == 512) if (nh == 128) return attn_paged4_pair_launch(P, stream);
-  // Groups of softmax warps and rows a thread: what exists is computed, no more (GQA 128, 64 x 5056 rows: 4 rows 125 us, as 8 rows 142, as 16
-  // 181; 8 rows 144, as 16 184; GQA 64, 4 rows: 99, 116, 148).
+  // Groups of softmax warps and rows a thread: what exists is computed, no more (GQA 128, 64 x 5056 rows: with 8 expansion warps 4 rows 125 us, as 8 rows 142,
+  // as 16 181; 8 rows 144, as 16 184; GQA 64, 4 rows: 99, 116, 148).
   if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
   if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
   if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);
