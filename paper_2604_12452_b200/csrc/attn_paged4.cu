@@ -832,13 +832,13 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 
 // ------------------------------------------------------------------------------------------------------------- host
 // Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head (16 rows of GQA, 64 x 5056: 157 us, with
-// room for 32: 206; MLA 512 + 64: 55 / 70), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
+// room for 32: 202; MLA 512 + 64: 55 / 69), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
 // single CTAs against pairs:
 //                 64 x 5056 rows   20 x up to 5056   1 x 2528   12 x up to 9001   100 x 5056   4 x 60000
-//   40 rows           122 / 121 us      42 / 55        22 / 27       45 / 57       182 / 191     96 / 105
-//   64 rows           123 / 124         43 / 56        22 / 27       45 / 57       188 / 203     96 / 106
-//   66 rows           176 / 124         54 / 56        22 / 27       56 / 57       256 / 202    127 / 106
-//   128 rows          233 / 127         66 / 60        23 / 27       67 / 58       355 / 217    161 / 106
+//   40 rows           119 / 120 us      42 / 54        21 / 25       44 / 57       178 / 188     91 / 104
+//   64 rows           120 / 123         43 / 56        21 / 26       44 / 57       184 / 198     90 / 103
+//   66 rows           173 / 123         53 / 56        21 / 26       55 / 57       251 / 198    124 / 104
+//   128 rows          228 / 125         66 / 59        21 / 26       66 / 58       347 / 213    158 / 104
 static int paged4_rows_per_tile(const lca_params* p, int q_len) {
   const long long rows = (long long)q_len * (p->n_q_heads / p->n_kv_heads);
   if (p->d_sem == 512 && rows > 64) return 128;

@@ -14,7 +14,7 @@
 //   expanded keys and copied values
 // An expanded tile's buffer is free once its product and the copies from it, at both ends, are done.  Signals from one CTA to the
 // other go through one thread, as in attn_paged8_pair.cu.
-// 64 x 5056 rows, 128 heads: 126 us (blocks of 32 rows on single CTAs: 232; the 8-bit cache, which expands nothing: 92).  A tile takes 5700
+// 64 x 5056 rows, 128 heads: 125 us (blocks of 32 rows on single CTAs: 228; the 8-bit cache, which expands nothing: 92).  A tile takes 5700
 // clocks: S 2000 and O 1100 (36 x 32 + 16 x 64 if nothing else used the port of shared memory), between them the softmax's
 // chain of 4400, which waits for neither.  Its instructions once did not fit the instruction cache (39 % of the stalls, products issued by
 // unrolled code, keys and values expanded by warps of their own).  Values expanded a second time in place of the copies: 154 us;
