@@ -53,6 +53,9 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
   __shared__ int s_taken;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int rank = (int)tc::cluster_ctarank(), C = (int)(gridDim.x / a.B), b = (int)(blockIdx.x / C);
+  // The CTAs write to one another's shared memory, which each may do once all have started: the other half of this barrier stands before
+  // the first of those writes, so that the wait lies behind the reads up to there.
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
   chain_wait();
   chain_next();
   const int K = a.K, V = a.V;
@@ -118,6 +121,7 @@ __global__ void __launch_bounds__(VERIFY_THREADS) verify_kernel(VerifyArgs a) {
     sum = warp_sum(sum);
     if (lane == 0) s_warp[warp] = sum;
     __syncthreads();
+    if (attempt == 0) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // all CTAs have started
     if (warp == 0) {                                         // the CTA's sum to every CTA of the cluster
       double s = lane < VERIFY_WARPS ? s_warp[lane] : 0.0;
       s = warp_sum(s);
