@@ -826,8 +826,17 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
       group_sync(grp);                                       // s_f is written again by the next piece
     }
   }
+  // ---- free TMEM.  Behind the barrier no warp gives up any more; if one did, this one keeps the CTA's memory until straggling copies have landed
   __syncthreads();
-  if (warp == W_MMA) { tc_fence_after(); tmem_dealloc(tmem, PL::TM_COLS); }
+  if (warp == W_MMA) {
+    if (*abort_flag) {
+      const long long t0c = clock64();
+      while (clock64() - t0c < 2000000ll) __nanosleep(1000);
+      __syncwarp();
+    }
+    tc_fence_after();
+    tmem_dealloc(tmem, PL::TM_COLS);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------- host

@@ -654,12 +654,14 @@ attn_paged4_pair_kernel(const __grid_constant__ Paged4Params a) {
       tc_fence_before();                                     // O is overwritten once all threads have signalled the next piece's first weights
     }
   }
-  // ---- let straggling copies land if the CTA gave up; the peer is done with this CTA's memory; free TMEM
-  if (*abort_flag && warp == W_COPY && lane == 0) {
+  // ---- free TMEM, once the peer is done with this CTA's memory.  Behind the first barrier no warp gives up any more; if one did, straggling
+  // copies land before the second one
+  __syncthreads();
+  if (*abort_flag && warp == W_MMA) {
     const long long t0c = clock64();
     while (clock64() - t0c < 2000000ll) __nanosleep(1000);
+    __syncwarp();
   }
-  __syncthreads();
   cluster_sync_all();
   if (warp == W_MMA) { tc_fence_after(); tmem_dealloc_pair(tmem, TM_COLS); }
 }
