@@ -503,7 +503,7 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
  * either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
 typedef struct lca_verify_args {
   int32_t dtype;                /* of both probabilities: LCA_DTYPE_FP32 or LCA_DTYPE_BF16 */
-  int32_t batch, n_drafts, vocab;       /* n_drafts >= 0, vocab below 2^31 - 4096 */
+  int32_t batch, n_drafts, vocab;       /* n_drafts >= 0; n_drafts and vocab below 2^31 - 4096 */
   const void* target_probs;     /* [batch, n_drafts + 1, vocab]; they need not add up to 1 */
   const void* draft_probs;      /* [batch, n_drafts, vocab]; NULL: the drafter is certain (q_i(x_i) = 1, 0 elsewhere) */
   const int32_t* draft_tokens;  /* [batch, n_drafts] */

@@ -665,8 +665,8 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
 
 int lca_verify_drafts(const lca_verify_args* a, void* stream) {
   if (!a || (a->dtype != LCA_DTYPE_BF16 && a->dtype != LCA_DTYPE_FP32)) return LCA_ERR_INVALID_ARG;
-  if (a->batch <= 0 || a->n_drafts < 0 || a->n_drafts >= 0x7fffffff || a->vocab <= 0) return LCA_ERR_INVALID_ARG;
-  if (a->vocab > 0x7fffffff - 4096) return LCA_ERR_UNSUPPORTED_SHAPE;      // a token behind the row is still an int
+  if (a->batch <= 0 || a->n_drafts < 0 || a->vocab <= 0) return LCA_ERR_INVALID_ARG;
+  if (a->vocab > 0x7fffffff - 4096 || a->n_drafts > 0x7fffffff - 4096) return LCA_ERR_UNSUPPORTED_SHAPE;      // what is counted on behind the last one is still an int
   if (!a->target_probs || !a->u_sample || !a->accepted || !a->tokens_out) return LCA_ERR_INVALID_ARG;
   if (a->n_drafts > 0 && (!a->draft_tokens || !a->u_accept)) return LCA_ERR_INVALID_ARG;
   if ((a->n_tok != nullptr) != (a->n_tok_out != nullptr)) return LCA_ERR_INVALID_ARG;
