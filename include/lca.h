@@ -473,7 +473,8 @@ typedef struct lca_rope_args {
   const double* freqs;        /* [rot_dim / 2] on the device (lca_rope_frequencies) */
   /* Element (token, head, column) of a tensor is at token * token_stride + head * head_stride + column, in elements.  Tensors need
    * only their element's alignment; 16-byte aligned rows and rot_dim a multiple of 16 are fast.  An output may be its input (same
-   * address and strides); otherwise they do not overlap, nor do the heads of an output.  k may be NULL, or q. */
+   * address and strides); otherwise no output overlaps an input, its own or the other one, or the other output, nor do the heads of
+   * an output overlap.  Either of q and k may be NULL (its output too). */
   const void* q; int64_t q_token_stride, q_head_stride;
   void* q_out; int64_t q_out_token_stride, q_out_head_stride;
   const void* k; int64_t k_token_stride, k_head_stride;

@@ -911,7 +911,7 @@ def _heads(v, T, d, dtype, dev):
 def rope(q, k, positions, freqs, interleaved: bool = False, inverse: bool = False, factor: float = 1.0, q_out=None, k_out=None, stream=None):
     """Rotate q [T, heads, d] and k [T, kv_heads, d] (either may be None) by the angles positions [T] int32 times freqs [rot / 2]
     float64: columns 0 .. rot - 1 of every head, the others are copied.  The tensors may be views (slices of a projection) as long
-    as the columns of a head lie side by side; q_out / k_out may be q / k themselves.  Returns (q_out, k_out)."""
+    as the columns of a head lie side by side; q_out may be q and k_out may be k, otherwise outputs overlap nothing.  Returns (q_out, k_out)."""
     x = q if q is not None else k
     if x is None:
         raise ValueError("rope takes queries, keys or both")

@@ -637,6 +637,13 @@ int lca_rope(const lca_rope_args* a, void* stream) {
   for (const void* x : {a->q, (const void*)a->q_out, a->k, (const void*)a->k_out})
     if (reinterpret_cast<uintptr_t>(x) & elem) return LCA_ERR_MISALIGNED;
   if ((reinterpret_cast<uintptr_t>(a->positions) & 3u) || (reinterpret_cast<uintptr_t>(a->freqs) & 7u)) return LCA_ERR_MISALIGNED;
+  // The threads of a call run in any order: what one writes, no other may read or write.
+  if (a->q && a->k && (a->q_out == a->k || a->k_out == a->q || a->q_out == a->k_out)) return LCA_ERR_INVALID_ARG;
+  auto moved = [&](const void* x, const void* y, int heads, int64_t xt, int64_t yt, int64_t xh, int64_t yh) {      // an output on its input with other strides
+    return x && x == y && ((a->n_tokens > 1 && xt != yt) || (heads > 1 && xh != yh));
+  };
+  if (moved(a->q, a->q_out, a->n_q_heads, a->q_token_stride, a->q_out_token_stride, a->q_head_stride, a->q_out_head_stride) ||
+      moved(a->k, a->k_out, a->n_k_heads, a->k_token_stride, a->k_out_token_stride, a->k_head_stride, a->k_out_head_stride)) return LCA_ERR_INVALID_ARG;
   return rope_launch(a, (cudaStream_t)stream);
 }
 

@@ -17,3 +17,22 @@ def test_more_drafts_than_a_step_of_a_block_can_be_added_to(B, n_drafts):
     before = B.lca_launch_count()
     assert verify(B, n_drafts=n_drafts, vocab=1) == -2
     assert B.lca_launch_count() == before
+
+
+def rope(B, **kw):
+    a = B.LcaRopeArgs(0, 0, 0, 4, 2, 64, 64, 1.0, 8, 16, 16, 1 << 20, 256, 64, 2 << 20, 256, 64, 3 << 20, 128, 64, 4 << 20, 128, 64)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return B.lca_rope(a)
+
+
+def test_outputs_on_what_others_read_or_write(B):
+    before = B.lca_launch_count()
+    q, q_out, k, k_out = (i << 20 for i in (1, 2, 3, 4))
+    for kw in (dict(q_out=k), dict(k_out=q), dict(k_out=q_out), dict(k=q, q_out=q), dict(k=q, k_out=q), dict(k=q, q_out=q, k_out=q)):
+        assert rope(B, **kw) == -1, kw
+    # in place, but element for element
+    for kw in (dict(q_out=q, q_out_token_stride=512), dict(q_out=q, q_head_stride=192), dict(k_out=k, k_token_stride=576), dict(k_out=k, k_out_head_stride=80),
+               dict(k=None, k_out=None, q_out=q, q_token_stride=768)):
+        assert rope(B, **kw) == -1, kw
+    assert B.lca_launch_count() == before
