@@ -956,6 +956,9 @@ def verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, n
         raise ValueError(f"probabilities are float32 or bfloat16, not {dt}")
     if draft_probs is not None and draft_probs.shape != (B, n, V):
         raise ValueError(f"draft_probs is {[B, n, V]}, not {list(draft_probs.shape)}")
+    for x, m in ((draft_tokens, n), (u_accept, n), (out, n1)):                 # the library finds a request by the length of these rows
+        if x is not None and m > 0 and (x.shape[1] != m if x.dim() == 2 else x.numel() != B * m):
+            raise ValueError(f"expected {m} elements for each of {B} requests, not {list(x.shape)}")
     if accepted is None:
         accepted = _new(torch.empty, (B,), _I32, target_probs.device, stream)
     if out is None:

@@ -1,5 +1,6 @@
 """Rotary positions and draft verification, host side: calls whose sizes or addresses no kernel may be given (no GPU needed)."""
 import pytest
+import torch
 
 from tests.test_paged4 import B  # noqa: F401
 
@@ -36,3 +37,25 @@ def test_outputs_on_what_others_read_or_write(B):
                dict(k=None, k_out=None, q_out=q, q_token_stride=768)):
         assert rope(B, **kw) == -1, kw
     assert B.lca_launch_count() == before
+
+
+@pytest.fixture()
+def on_host(B, monkeypatch):
+    """The verify helper with its checks alone: tensors of the host stand for the device's, and the library is not called."""
+    monkeypatch.setattr(B, "_device", lambda x, where: x.get_device())
+    monkeypatch.setattr(B, "_raw_stream", lambda dev, stream: 0)
+    monkeypatch.setattr(B._lib, "lca_verify_drafts", lambda *a: 0)
+    i32, f32 = dict(dtype=torch.int32), dict(dtype=torch.float32)
+    good = dict(target_probs=torch.zeros((2, 4, 9), **f32), draft_probs=torch.zeros((2, 3, 9), **f32), draft_tokens=torch.zeros((2, 3), **i32),
+                u_accept=torch.zeros((2, 3), **f32), u_sample=torch.zeros(2, **f32))
+    return lambda **kw: B.verify_drafts(**{**good, **kw})
+
+
+def test_rows_of_another_length_are_not_taken_for_a_request_s(on_host):
+    i32, f32 = dict(dtype=torch.int32), dict(dtype=torch.float32)
+    on_host()
+    on_host(draft_tokens=torch.zeros((5, 3), **i32), u_accept=torch.zeros((2 * 3,), **f32), out=torch.zeros((3, 4), **i32))      # more requests, no rows at all
+    for bad in (dict(draft_tokens=torch.zeros((2, 4), **i32)), dict(u_accept=torch.zeros((2, 5), **f32)), dict(out=torch.zeros((2, 5), **i32)),
+                dict(u_accept=torch.zeros((3, 2), **f32)), dict(draft_tokens=torch.zeros((7,), **i32)), dict(out=torch.zeros((4, 4, 1), **i32))):
+        with pytest.raises(ValueError):
+            on_host(**bad)
