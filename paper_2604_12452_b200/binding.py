@@ -959,14 +959,14 @@ def verify_drafts(target_probs, draft_probs, draft_tokens, u_accept, u_sample, n
     for x, m in ((draft_tokens, n), (u_accept, n), (out, n1)):                 # the library finds a request by the length of these rows
         if x is not None and m > 0 and (x.shape[1] != m if x.dim() == 2 else x.numel() != B * m):
             raise ValueError(f"expected {m} elements for each of {B} requests, not {list(x.shape)}")
+    if n_tok is None and n_tok_out is not None:
+        raise ValueError("n_tok_out is n_tok less the rejected drafts: n_tok is missing")
     if accepted is None:
         accepted = _new(torch.empty, (B,), _I32, target_probs.device, stream)
     if out is None:
         out = _new(torch.empty, (B, n1), _I32, target_probs.device, stream)
     if n_tok is not None and n_tok_out is None:
         n_tok_out = _new(torch.empty, (B,), _I32, target_probs.device, stream)
-    if n_tok is None:
-        n_tok_out = None
     a = LcaVerifyArgs(code, B, n, V, _arg(target_probs, dt, B * n1 * V, dev), _arg(draft_probs, dt, B * n * V, dev),
                       _arg(draft_tokens, _I32, B * n, dev), _arg(n_draft, _I32, B, dev), _arg(u_accept, _F32, B * n, dev),
                       _arg(u_sample, _F32, B, dev), _arg(n_tok, _I32, B, dev), _arg(accepted, _I32, B, dev), _arg(out, _I32, B * n1, dev),

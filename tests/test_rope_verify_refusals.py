@@ -59,3 +59,10 @@ def test_rows_of_another_length_are_not_taken_for_a_request_s(on_host):
                 dict(u_accept=torch.zeros((3, 2), **f32)), dict(draft_tokens=torch.zeros((7,), **i32)), dict(out=torch.zeros((4, 4, 1), **i32))):
         with pytest.raises(ValueError):
             on_host(**bad)
+
+
+def test_counters_out_without_counters_in(on_host):
+    n = torch.full((2,), 7, dtype=torch.int32)
+    assert on_host()[2] is None and on_host(n_tok=n, n_tok_out=n)[2] is n
+    with pytest.raises(ValueError):                                            # not left as it was, with no word
+        on_host(n_tok_out=n)
