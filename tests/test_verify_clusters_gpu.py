@@ -22,3 +22,12 @@ def test_the_shortest_way_to_the_exchange(B, ctas, V):
         B.verify_drafts(target, None, tokens, ua, us, accepted=accepted[i], out=out[i])
     torch.cuda.synchronize()
     assert torch.equal(accepted, first[0].expand_as(accepted)) and torch.equal(out, first[1].expand_as(out))
+
+
+@pytest.mark.parametrize("nb,n,V", [(100, 3, 2049), (185, 1, 4000), (93, 2, 30011), (64, 4, 128000), (5, 3, 3001), (370, 1, 2600), (371, 1, 2600)])
+def test_requests_for_every_number_of_ctas(B, nb, n, V):
+    # four CTAs for up to 185 requests, two for up to 370, then one
+    for dtype in (torch.float32, torch.bfloat16):
+        target, q, tokens, ua, us = make(nb, n, V, nb + V, dtype)
+        check_verify(B, target, q, tokens, ua, us, n_tok=torch.arange(50, 50 + nb, dtype=torch.int32, device=DEV))
+        check_verify(B, target, None, tokens, ua, us)
