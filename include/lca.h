@@ -368,7 +368,7 @@ int lca_paged8_write(const lca_params* p, const lca_paged8* cache, const void* r
  * The q_len tokens are the last ones of their sequence: query i sees the present rows below n_tok - q_len + 1 + i.
  * Representatives get rep_logit_bias.  A query that sees no row (an empty sequence, fewer tokens than q_len) gives
  * out = 0 and lse = -inf.  What absent rows and unused pages hold does not matter; a NaN in a present row reaches every
- * query of that sequence and KV head.
+ * query of that sequence and KV head that sees the row, and through its value those of the q_len that do not see it may become NaN too.
  * Products on the tensor cores with queries and softmax weights as sums of two 8-bit terms: a query element is exact to
  * 2^-17 of the largest of its row, a weight to 2^-8 of itself or to a step of 2^-17 of the largest weight, whichever is more; weights
  * near that step are rounded with offsets spread evenly over the rows, so that many of them keep their sum, whatever
@@ -457,8 +457,8 @@ int lca_decode_update_paged4(const lca_params* p, const lca_paged4* cache, const
  * them, from the layout that a projection leaves them in: for each token t, head and pair i of columns
  *     (a, b) -> factor * (a cos - b sin, a sin + b cos) of the angle  positions[t] * freqs[i]
  * Pairs are columns (2 i, 2 i + 1) where `interleaved`, else (i, i + rot_dim / 2).  Columns behind the first rot_dim are copied as they are
- * (not multiplied by `factor`).  With `inverse` the angle is negated: that is also the gradient of the call.  Angles are exact to 64 bits,
- * products fp32, rounded once. */
+ * (not multiplied by `factor`).  With `inverse` the angle is negated: that is also the gradient of the call.  Angles and their whole
+ * turns are taken in 64 bits, what is left of half a turn, its cosine and sine (to 2^-22) and the products in fp32; rounded once. */
 enum { LCA_DTYPE_BF16 = 0, LCA_DTYPE_FP32 = 1 };
 typedef struct lca_rope_args {
   int32_t dtype;              /* of q, k and the outputs */
@@ -489,6 +489,8 @@ int lca_rope(const lca_rope_args* args, void* stream);
  *   BASE    base * scale^(rot_dim / (rot_dim - 2)) in place of base: the fastest pair keeps its frequency, the slowest is divided by scale
  *   RAMP    pairs that make more than `fast` turns in trained_len tokens keep f_i, those with less than `slow` take f_i / scale, between
  *           them the share that is kept grows linearly with the turns; factor 0.1 ln(scale) + 1 where scale > 1
+ *           (one of two customs: others let the share grow with the pair's index between two bounds, and put part of the factor into the
+ *           softmax scale.  A model trained that way needs its own frequencies; lca_rope takes any)
  * trained_len, fast and slow are only used by RAMP (customary: fast = 32, slow = 1). */
 enum { LCA_ROPE_PLAIN = 0, LCA_ROPE_LINEAR = 1, LCA_ROPE_BASE = 2, LCA_ROPE_RAMP = 3 };
 int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scale, double trained_len, double fast,
@@ -500,8 +502,8 @@ int lca_rope_frequencies(int32_t kind, int32_t rot_dim, double base, double scal
  *   draft i is accepted while u_accept[i] * q_i(x_i) < p_i(x_i)  (the product in 64 bits, where it is exact)
  *   the next token is drawn from max(p_i - q_i, 0) at the first rejected draft i, or from p after the last accepted one: the first
  *       token v whose cumulative sum exceeds u_sample times the whole sum, in 64-bit sums
- * Entries (and differences) that are not positive finite fp32 numbers have no mass.  Where p_i - q_i leaves none, the token is drawn from p_i; where that has none
- * either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
+ * A token has mass where the difference (where it is drawn from p: the entry) is a positive finite fp32 number.  Where p_i - q_i leaves none, the token
+ * is drawn from p_i; where that has none either it is -1.  A draft outside the vocabulary is rejected (and with it all behind it). */
 typedef struct lca_verify_args {
   int32_t dtype;                /* of both probabilities: LCA_DTYPE_FP32 or LCA_DTYPE_BF16 */
   int32_t batch, n_drafts, vocab;       /* n_drafts >= 0; n_drafts and vocab below 2^31 - 4096 */
