@@ -17,7 +17,8 @@
 // that a tile's softmax only waits for O of the tile before the last one, unless it has to raise a maximum.
 // Codes: where two tiles of them fit into shared memory beside the expanded tiles (all shapes but MLA 512 + 64) they come by bulk copies, one for
 // each page and part; else the expansion warps load them to registers a tile ahead, behind the fence that ends a tile (in front of it the
-// fence waits for them).  GQA, 64 x 5056 rows of 8 KV heads: 131 us by copies, 145 by registers.
+// fence waits for them).  GQA, 64 x 5056 rows of 8 KV heads, when either was built for it, before the steps to today's 121 us: 131 us by copies, 145
+// by registers.
 // Work: as in attn_paged8.cu, one line of tiles cut into equal ranges, pieces merged by paged8_combine_kernel.
 // What bounds it: not HBM (64 x 5056 rows, GQA 32 heads on 8: 348 MB in 121 us, 2.9 TB/s; MLA 16 heads: 97 MB in 55 us) but the chain of a tile -
 // expansion (seven instructions at half rate for eight values, 2000 warp instructions a tile for MLA 512 + 64, and 72 KB written through the port of
@@ -34,8 +35,6 @@ static __device__ int g_paged4_status = 0;
 
 static constexpr float T4_MAX = 8.75f;                       // log2 of the largest weight: e4m3 ends at 448
 static constexpr float LO4_GAIN = 16.f;                      // of the second term, which has columns of O of its own
-
-
 
 // --------------------------------------------------------------------------------------------------- scalar kernel
 // One warp per query row, keys one by one, fp32: the cross-check of the tensor-core kernel (lca_set_attention_impl(1)).
@@ -124,7 +123,8 @@ struct Paged4Plan {
   // expand them.
   static constexpr bool STAGED = !(MLA && DS == 512);
   // Expansion warps.  More of them hide more latency, fewer leave more registers and issue slots to the others: with 4 and 8, 64 x 5056 rows,
-  // GQA 128 with 4 / 16 / 32 rows a KV head 121 / 157 / 206 and 121 / 174 / 208 us, GQA 64 90 and 101; MLA 512 + 64 with 16 rows 60 and 55.
+  // GQA 128 with 4 / 16 / 32 rows a KV head 121 / 157 / 206 and 121 / 173 / 208 us, GQA 64 90 and 101, MLA 128 + 64 with 4 / 16 / 32 rows 25 / 33 / 38 and 26 / 38 / 39;
+  // MLA 512 + 64 with 16 rows 60 and 55.
   static constexpr int EW = STAGED ? 4 : 8, SOFTMAX_WARPS = 4 * GROUPS, W_EXP = SOFTMAX_WARPS, W_MMA = W_EXP + EW, W_LOOK = W_MMA + 1, W_LOAD = W_LOOK + (STAGED ? 1 : 0);
   static constexpr int THREADS = 32 * (W_LOAD + 1);
   static constexpr int STAGE = STAGED ? 128 * (DS + DP) / 2 : 0, ST_POS = 128 * DS / 2;      // codes of a tile: latents or V, keys
@@ -358,8 +358,9 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
     }
   } else if (warp >= W_EXP && warp < W_MMA) {
     // ----------------------------------------------------------------------------------------------- expansion
-    // A thread takes 32 values (16 bytes of codes) of a row at a time, from HBM to registers while it expands those of the tile
-    // before.  Eight neighbouring lanes write two rows, so that their units fall on all banks of the swizzled image.
+    // A thread takes 32 values (16 bytes of codes) of a row at a time, STAGED: from the copies in shared memory, else from HBM to registers
+    // while it expands those of the tile before.  Eight neighbouring lanes write two rows, so that their units fall on all banks of the
+    // swizzled image.
     const int et = tid - 32 * W_EXP;
     const int n_tiles = (int)min(s_off[1], 0x7fffffffll);
     bool ok = !*abort_flag;
@@ -499,7 +500,7 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
         }
         __syncwarp();
         if (lane == 0) { mbar_arrive(GEMPTY(stage)); mbar_arrive(FEMPTY(ff)); }
-        if (++ff == PL::FACTS) { ff = 0; fphase ^= 1; }
+        if (++ff == PL::FACTS) ff = 0;
         if (++stage == PL::STAGES) { stage = 0; phase ^= 1; }
         hold(PL::MLA ? VEMPTY(buf) : KEMPTY(buf), (use & 1) ^ 1, ERR_WAIT_O_DONE);
         put(CP(), pos, pos_u, tile + pos_to, POS_APART);
@@ -841,8 +842,10 @@ __global__ void __launch_bounds__(PL::THREADS, PL::CTAS) attn_paged4_kernel(cons
 
 // ------------------------------------------------------------------------------------------------------------- host
 // Query rows that share a tile of keys: 16 or 32, the smaller one that holds all rows of a KV head (16 rows of GQA, 64 x 5056: 157 us, with
-// room for 32: 202; MLA 512 + 64: 55 / 69), else blocks of 32.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs.  Blocks of 32 on
-// single CTAs against pairs:
+// room for 32: 202; MLA 512 + 64: 55 / 69), else blocks of 32.  Every block expands all tiles again: 64 x 5056 rows, GQA 128 on 8 KV heads with
+// 32 / 33 / 64 / 112 / 128 rows a KV head 206 / 384 / 396 / 775 / 780 us, GQA 64 with 32 / 64 / 128 184 / 351 / 687, MLA 128 + 64 with 32 / 64 / 128 / 512
+// 38 / 56 / 100 / 362.  MLA 512 + 64 with more than 64 rows: blocks of 128 on CTA pairs, whatever the lengths (which the host does not know),
+// although single CTAs are faster where the tiles are few (66 rows: columns two and three, level in the fourth; 128 rows: the third).  Blocks of 32 on single CTAs against pairs:
 //                 64 x 5056 rows   20 x up to 5056   1 x 2528   12 x up to 9001   100 x 5056   4 x 60000
 //   40 rows           119 / 120 us      42 / 54        21 / 25       44 / 57       178 / 188     91 / 104
 //   64 rows           120 / 123         43 / 56        21 / 26       44 / 57       184 / 198     90 / 103
@@ -872,8 +875,8 @@ template <bool MLA, int DS, int DP>
 static int paged4_launch_rows(Paged4Params& P, int nh, cudaStream_t stream) {
   const long long rows = (long long)P.b.q_len * P.b.rep;
   if constexpr (DS == 512) if (nh == 128) return attn_paged4_pair_launch(P, stream);
-  // Groups of softmax warps and rows a thread: what exists is computed, no more (GQA 128, 64 x 5056 rows: with 8 expansion warps 4 rows 125 us, as 8 rows 142,
-  // as 16 181; 8 rows 144, as 16 184; GQA 64, 4 rows: 99, 116, 148).
+  // Groups of softmax warps and rows a thread: what exists is computed, no more (GQA 128, 64 x 5056 rows: 4 rows 121 us, as 8 rows 134, as 16 152; 8 rows 135,
+  // as 16 155; GQA 64, 4 rows: 90, 98, 123).
   if (nh == 32) return paged4_launch<Paged4Plan<MLA, DS, DP, 32, 4, 8>>(P, stream);
   if (rows <= 4) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 4>>(P, stream);
   if (rows <= 8) return paged4_launch<Paged4Plan<MLA, DS, DP, 16, 1, 8>>(P, stream);

@@ -71,8 +71,11 @@ __device__ __forceinline__ uint32_t encode8(const uint4& v, uint32_t top, bool n
 }
 
 static const int ROW_THREADS = 256, ROW_WARPS = ROW_THREADS / 32;
-// Up to here a warp takes one MLA row (128 + 64: two), for its fewer instructions; beyond, four, for their smaller number in all.  Written with one
-// row a warp and with four: 64 rows 1.8 / 2.6 us, 4800 rows 3.3 / 3.7, 9600 rows 5.1 / 4.7, 20000 rows 8.7 / 7.1; 323584 rows 132 / 83.
+// Up to here a warp takes one MLA row (128 + 64: two), for its fewer instructions; beyond, four, for their smaller number in all.  One row a warp
+// and four, us: 512 + 64 written, 256 rows 1.7 / 2.4, 2048 rows 2.1 / 2.7, 4096 rows 3.2 / 2.9, 4800 rows 3.1 / 3.4, 8192 rows 4.1 / 4.5, 9600 rows 4.8 / 4.6,
+// 20000 rows 8.2 / 6.8, 323584 rows 132 / 83; read back 1.7 / 2.1, 2.0 / 2.3, 2.7 / 2.3, 2.8 / 3.0, 3.6 / 3.8, 3.9 / 3.9, 6.5 / 5.6.  Two rows and four, 128 + 64
+// written, 256 rows 1.5 / 1.7, 4096 rows 2.4 / 2.2, 8192 rows 2.9 / 2.4, 20000 rows 4.3 / 3.9; read back 1.5 / 1.5, 2.0 / 1.8, 2.7 / 2.0, 3.6 / 3.2.  Between
+// 3000 and 9600 rows neither is ahead by more than 0.5 us, and which one is changes with the waves that the rows make.
 static const long long FEW_ROWS = 4096;
 
 // MLA, ROWS rows: step q < S takes units 32 q + lane of their latents (US of a row), step S units lane % 8 of their keys.
