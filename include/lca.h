@@ -429,8 +429,8 @@ typedef struct lca_paged4 {
 int lca_paged4_write(const lca_params* p, const lca_paged4* cache, const void* rows_sem, const void* rows_pos,
                      const int32_t* slot_map, int64_t n_rows, void* stream);
 
-/* The values of rows of the cache, in bf16 (exact but for values of 2^128, which a row whose largest element is above 7/8 of that may
- * round to: infinity).
+/* The values of rows of the cache, in bf16, exact but for those of 2^128 and more, which are infinity: codes that elements from 7/8 of 2^128 on, or
+ * infinities beside elements above 3/4 of it, were rounded to.
  *   slot_map [n_rows] int32: slot of every row wanted, in any order, the same one any number of times
  *   rows_sem [n_rows, n_kv_heads, d_sem], rows_pos [n_rows, n_kv_heads, d_pos] bf16 out: rows whose slot is negative or behind
  *       the pool are left as they are */
